@@ -194,7 +194,7 @@ def prepare(case, seed):
             st["q"] = (2 * normal(n, H, HEAD_DIM)).to(dt)
             kc, ks = _packed(*_four_bits(key_like(n_pages, page, KH, HEAD_DIM).transpose(1, 2).double()))
             vc, vs = _packed(*_four_bits(normal(n_pages, KH, page, HEAD_DIM).double()))
-            st["cache"] = (kc, vc, ks, vs)
+            st["cache"] = tuple(t.contiguous() for t in (kc, vc, ks, vs))
     else:
         m = sum(keys)
         st["kv_start"] = _starts(keys, dev)
