@@ -63,15 +63,19 @@ typedef enum { S3R_F32 = 0, S3R_BF16 = 1 } s3r_dtype;
 
 /* Bits of the device status word (s3r_params.status). */
 enum { S3R_DIAG_FORCED_RANGE = 1, S3R_DIAG_FORCED_ORDER = 2 };
+/* Bits of the status word of the cache and cross attention calls: a page number outside [0, n_pages); a list of row
+ * starts that is out of range or not ascending; a length outside the page table (for append and read also one below the
+ * sequence's rows); a position outside the tables. */
+enum { S3R_DIAG_PAGE = 4, S3R_DIAG_SPANS = 8, S3R_DIAG_LENGTH = 16, S3R_DIAG_POSITION = 32 };
 
 /* Stages of the path, for speed3r_get_stage_ms(). */
 enum {
-    S3R_STAGE_POOL = 0,     /* block pooling (+ K/V tile re-layout for the MFMA path) */
+    S3R_STAGE_POOL = 0,     /* block pooling (+ K/V tile re-layout for the MFMA path); cache rows in and out */
     S3R_STAGE_SPLIT = 1,    /* pooled fp32 -> operand tiles (+ their per-head statistics) */
     S3R_STAGE_COMPRESS = 2, /* S_guide + compressed attention (short sequences: + TopK) */
     S3R_STAGE_TOPK = 3,     /* per-query-block TopK (incl. its filter sweep)          */
     S3R_STAGE_SELECT = 4,   /* block-sparse attention + merge                         */
-    S3R_STAGE_DENSE = 5,    /* dense attention                                        */
+    S3R_STAGE_DENSE = 5,    /* dense, cross and cache attention, and the gradient of cross attention */
     S3R_N_STAGES = 6
 };
 
@@ -240,6 +244,105 @@ s3r_status speed3r_select_attn(const void *q, const void *k, const void *v, cons
                                const float *o_comp, const void *gate_logits, void *out, void *o_sel,
                                float *lse, int64_t n_tok, int heads, int head_dim, int block, int kk,
                                s3r_dtype dtype, float softmax_scale, void *stream);
+
+/* ---- cross attention and its gradient --------------------------------------------------------- */
+
+/* out[i,h] = softmax_j(scale q[i,h] . k[j,h']) v[j,h'] with keys of another length than the queries: a decoder's rows over the
+ * states of a scene (dense attention, eq. 2 form, is the case q, k, v of one length).  heads is a multiple of kv_heads; query head h
+ * reads head h' = h / (heads / kv_heads) of k and v.
+ *   Batches: sequences lie one behind the other; sequence b has query rows q_start[b] .. q_start[b+1] - 1 and keys kv_start[b] ..
+ *   kv_start[b+1] - 1 (both may be none).  The starts are in DEVICE memory, ascending, within [0, n_q] and [0, n_kv].  A list that breaks
+ *   this is reported through `status`; the call then runs on entries held into range (memory-safe).  Rows outside all sequences are
+ *   left as they were, in outputs and gradients alike.
+ *   Mask: keys with key_mask 0 take no part, whatever their k and v hold (padding, invalid patches); their gradients are 0.
+ *   A query row without any key gets out = 0, lse = -inf and gradient 0.
+ *   Sums, maxima and log-sums are fp32.  bf16 data: probabilities (and dS, in the gradient) enter the second product rounded to
+ *   bf16.  fp32 data: products in bf16 parts, to fp32 precision (an infinity in v or
+ *   d_out may come out as NaN).
+ *   The gradient takes out and lse as the forward call left them; the gradients of shared heads are summed.  Its results do not
+ *   depend on the order in which workgroups run. */
+typedef struct s3r_cross_params {
+    const void *q;           /* in  [n_q][heads][64] (or q_stride_*)                                    */
+    const void *k, *v;       /* in  [n_kv][kv_heads][64] (or kv_stride_*)                               */
+    void *out;               /* out [n_q][heads][64]; the gradient reads it                              */
+    float *lse;              /* out, optional [heads][n_q], natural log; the gradient reads it (required) */
+    const void *d_out;       /* gradient: in [n_q][heads][64]                                            */
+    void *dq, *dk, *dv;      /* gradient: out [n_q][heads][64], [n_kv][kv_heads][64] twice               */
+    const int32_t *q_start, *kv_start; /* in, optional [batch + 1] (both NULL: one sequence of all rows) */
+    const uint8_t *key_mask; /* in, optional [n_kv]                                                      */
+    int32_t *status;         /* out, optional: one device word, 0 or S3R_DIAG_SPANS                      */
+    int64_t n_q, n_kv;       /* rows of the tensors; 0 is allowed (their pointers are then not read)     */
+    int64_t q_stride_tok, q_stride_head;   /* elements between rows and heads of q (0: packed), multiples of 8 */
+    int64_t kv_stride_tok, kv_stride_head; /* of k and of v                                               */
+    int batch;               /* sequences; 1 (or 0) without starts                                       */
+    int heads, kv_heads, head_dim;
+    s3r_dtype dtype;
+    float softmax_scale;     /* <= 0: 1/sqrt(head_dim)                                                   */
+    void *workspace;         /* caller-owned device scratch, 256-byte aligned                            */
+    size_t workspace_bytes;  /* >= speed3r_cross_workspace_bytes(...)                                    */
+    void *stream;
+} s3r_cross_params;
+
+/* Bytes of device scratch that the forward call (backward 0) or the gradient (1) needs; only the shape fields are read.  May be 0;
+ * SIZE_MAX on invalid arguments. */
+size_t speed3r_cross_workspace_bytes(const s3r_cross_params *p, int backward);
+s3r_status speed3r_cross_attn(const s3r_cross_params *p);
+s3r_status speed3r_cross_attn_backward(const s3r_cross_params *p);
+
+/* ---- a cache of keys and values in 4 bits ------------------------------------------------------ */
+
+/* Views (or tokens) that arrive one after another: keys and values of earlier rows are kept in pages, 34 bytes for the 64 channels of a
+ * head.  The form is that of the microscaling formats (MXFP4): 32 channels share a power of two 2^e, the smallest in [-100, 125] with
+ * max |x| < 7 * 2^e, and each is the nearest of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} * 2^e, ties to the even code.  Magnitudes from
+ * 6 * 2^125 on are held as 6 * 2^125, those below 2^-102 as 0; a block of 32 with a NaN or an infinity reads as NaN.
+ *   Pages: `page` tokens each (16, 32, 64 or 128).  Token t of sequence b is token t % page of page page_table[b][t / page].
+ *   A sequence has kv_len[b] tokens.  page_table and kv_len are in DEVICE memory, so that a captured graph may be replayed with other contents;
+ *   a broken entry is reported through `status`, and memory-safe: lengths are held into the table, and tokens on a page outside
+ *   [0, n_pages) are not written, read as 0 and are not attended.
+ *   Rows: those of sequence b are row_start[b] .. row_start[b+1] - 1 (as in s3r_cross_params) and are its LAST tokens: of n rows,
+ *   row i is token kv_len[b] - n + i.  kv_len counts the rows of the call.  Rows outside all sequences are left as they were.  */
+typedef struct s3r_cache_params {
+    uint8_t *k_codes, *v_codes;   /* [n_pages][kv_heads][page][32], channels 2 i (low half) and 2 i + 1 in byte i; 16-byte aligned */
+    uint8_t *k_scales, *v_scales; /* [n_pages][kv_heads][page][2], e + 127 of channels 0..31 and 32..63; 255: NaN                   */
+    const int32_t *page_table;    /* [batch][max_pages]                                                  */
+    const int32_t *kv_len;        /* [batch]                                                             */
+    const int32_t *row_start;     /* [batch + 1], NULL: one sequence of all n_rows rows                  */
+    int64_t n_pages, n_rows;      /* n_rows may be 0                                                     */
+    int page, max_pages, batch;
+    int heads, kv_heads, head_dim;
+    s3r_dtype dtype;              /* of q, k, v and out                                                  */
+    const void *q;                /* append: in, optional, rotated into out; attention: in [n_rows][heads][64] */
+    void *out;                    /* [n_rows][heads][64]: q rotated; attention                           */
+    void *k, *v;                  /* append: in; read: out [n_rows][kv_heads][64] (or kv_stride_*)       */
+    int64_t q_stride_tok, q_stride_head, kv_stride_tok, kv_stride_head; /* 0: packed; multiples of 8 elements */
+    /* append: rotation of k and q, or NULL: none.  The 64 channels of a head are rot_axes (1 or 2) groups, each with a position of
+     * its own (2: row and column of a patch); a group's channels are turned in pairs, i and i + half a group (rot_neighbours 0) or 2 i and
+     * 2 i + 1 (1), by the angle with cosine cos[position][i].  Computed in 64 bits and rounded once. */
+    const float *cos, *sin;       /* [n_positions][32 / rot_axes], 16-byte aligned                       */
+    const int32_t *positions;     /* [n_rows][rot_axes]; NULL (rot_axes 1): the row's token number.  Held into [0, n_positions) */
+    int64_t n_positions;
+    int rot_axes, rot_neighbours;
+    /* attention */
+    int causal;                   /* 1: row i of n sees tokens 0 .. kv_len - n + i; 0: all kv_len        */
+    float softmax_scale;          /* <= 0: 1/sqrt(head_dim)                                              */
+    float *lse;                   /* out, optional [heads][n_rows], natural log                          */
+    int32_t *status;              /* out, optional: one device word, 0 or S3R_DIAG_* bits                */
+    void *workspace;              /* attention: caller-owned device scratch, 256-byte aligned            */
+    size_t workspace_bytes;       /* >= speed3r_cache_workspace_bytes(...)                               */
+    void *stream;
+} s3r_cache_params;
+
+/* Keys and values of the rows go to the cache, k rotated; q rotated goes to out.  One launch.  Two rows of a call must not be the
+ * same token of the same page (which of them is kept is not specified). */
+s3r_status speed3r_cache_append(const s3r_cache_params *p);
+/* The rows' tokens as values: what the cache holds for them, exactly (to k and v). */
+s3r_status speed3r_cache_read(const s3r_cache_params *p);
+/* out = softmax(scale q . k) v over the cached tokens that a row sees; a row that sees none gets out = 0, lse = -inf.  q is taken as it is
+ * (rotated by append).  NaNs in the cache reach only the rows that see them.  Sums, maxima and log-sums are fp32; cached values enter
+ * exactly; bf16 rows: probabilities enter the second product rounded to bf16. */
+s3r_status speed3r_cache_attn(const s3r_cache_params *p);
+/* Bytes of device scratch of speed3r_cache_attn; only the shape fields are read.  May be 0; SIZE_MAX on invalid arguments. */
+size_t speed3r_cache_workspace_bytes(const s3r_cache_params *p);
 
 /* ---- utilities ------------------------------------------------------------------------------ */
 

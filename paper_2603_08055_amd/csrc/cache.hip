@@ -1,0 +1,371 @@
+// A cache of keys and values in 4 bits: appending to its pages with the position rotation on the way, reading rows back, and
+// attention over it.
+//
+// The form is that of the OCP microscaling formats, which gfx950 converts in hardware: 32 channels share a power of two 2^e and
+// are e2m1 numbers (+-0, 0.5, 1, 1.5, 2, 3, 4, 6) in its units.  e is the smallest with max |x| < 7 * 2^e, so that the largest
+// channel, too, is off by half a step at most (where e is cut to the largest exponent below max |x|, up to a quarter of it is lost).
+// A block with a NaN or an infinity gets the exponent byte 255 and reads as NaN.
+#include "s3r_unit_device.h"
+
+namespace s3r {
+
+namespace {
+
+// x with its last bit set if it is not y exactly (round to odd): rounding it once more to fewer bits, or comparing it with a number of
+// fewer bits, gives what y itself would.
+__device__ __forceinline__ float round_to_odd(double y)
+{
+    const float x = static_cast<float>(y);
+    const double off = y - static_cast<double>(x);
+    unsigned bits = __float_as_uint(x);
+    if (off != 0.0 && (bits & 1) == 0 && __builtin_isfinite(y)) bits += (off > 0.0) == (y > 0.0) ? 1 : -1;
+    return __uint_as_float(bits);
+}
+
+template <typename T> __device__ __forceinline__ float rounded(double y)  // for storing as T
+{
+    if constexpr (sizeof(T) == 4) return static_cast<float>(y);
+    return round_to_odd(y);
+}
+
+// ---- append and read ----------------------------------------------------------------------------------
+// Eight lanes for a row of a head, eight channels each: 16 bytes of bf16 in, 4 bytes of codes out per lane.  Both are
+// bound by HBM; the products of the rotation are exact in 64 bits and their sum is rounded once, so that the codes are those of the exact
+// values (64-bit FMAs run at half the rate of 32-bit ones here and stay under the loads).
+
+// Channels 8 c .. 8 c + 7 of a row, turned by the angles of its positions; lane bits 0 .. 2 are c.
+__device__ __forceinline__ void rotate(const Rotation &rot, int64_t row, int token, int c, const float (&x)[8], double (&y)[8])
+{
+    const int pairs = 32 / rot.axes, axis = rot.axes == 2 ? c >> 2 : 0;
+    int64_t at = rot.positions != nullptr ? rot.positions[row * rot.axes + axis] : token;
+    at = at < 0 ? 0 : (at >= rot.places ? rot.places - 1 : at);
+    const int index = rot.neighbours ? (4 * c) % pairs : (8 * c) % pairs;
+    const float *cs = rot.cos + at * pairs + index, *sn = rot.sin + at * pairs + index;
+    if (rot.neighbours) {
+        const floatx4 co = *reinterpret_cast<const floatx4 *>(cs), si = *reinterpret_cast<const floatx4 *>(sn);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const double a = x[2 * j], b = x[2 * j + 1], co_j = co[j], si_j = si[j];
+            y[2 * j] = fma(a, co_j, -(b * si_j));
+            y[2 * j + 1] = fma(b, co_j, a * si_j);
+        }
+        return;
+    }
+    float co[8], si[8];
+    load8(cs, co);
+    load8(sn, si);
+    const int away = rot.axes == 2 ? 2 : 4;
+    const bool second = (c & away) != 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const double other = __shfl_xor(x[j], away, 64), turned = other * static_cast<double>(si[j]);
+        y[j] = fma(static_cast<double>(x[j]), static_cast<double>(co[j]), second ? turned : -turned);
+    }
+}
+
+template <typename T> __global__ __launch_bounds__(256) void cache_append_kernel(CacheArgs a)
+{
+    const unsigned id = blockIdx.x * 256u + threadIdx.x, item = id >> 3;
+    const int c = id & 7, kv_heads = a.cache.kv_heads;
+    const unsigned items = 2 * kv_heads + (a.q != nullptr ? a.heads : 0);
+    const unsigned row = item / items;
+    if (row >= a.n_rows || !a.spans.covers(row)) return;
+    int which = static_cast<int>(item - row * items);
+    const int b = a.spans.find(row);
+    int first, len;
+    a.spans.of(b, first, len);
+    const int n = a.cache.length(b), token = n - len + static_cast<int>(row) - first;
+    float x[8];
+    if (which >= 2 * kv_heads) {  // a head of q
+        const int h = which - 2 * kv_heads;
+        load8(static_cast<const T *>(a.q) + row * a.q_row + h * a.q_head + 8 * c, x);
+        double y[8];
+        rotate(a.rot, row, token, c, x, y);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = rounded<T>(y[j]);
+        Io8<T>::store(static_cast<T *>(a.to.out) + (static_cast<int64_t>(row) * a.heads + h) * 64 + 8 * c, x);
+        return;
+    }
+    const bool is_v = which >= kv_heads;
+    if (is_v) which -= kv_heads;
+    load8(static_cast<const T *>(is_v ? a.v : a.k) + row * a.kv_row + which * a.kv_head + 8 * c, x);
+    if (!is_v && a.rot.cos != nullptr) {
+        double y[8];
+        rotate(a.rot, row, token, c, x, y);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = round_to_odd(y[j]);
+    }
+    unsigned most = 0;  // magnitudes compare as integers; infinities and NaNs are the largest
+#pragma unroll
+    for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);
+    most = max(most, static_cast<unsigned>(__shfl_xor(static_cast<int>(most), 1, 64)));
+    most = max(most, static_cast<unsigned>(__shfl_xor(static_cast<int>(most), 2, 64)));
+    int e = static_cast<int>(most >> 23) - 129 + ((most & 0x7fffffu) >= 0x600000u ? 1 : 0);
+    e = e < -100 ? -100 : (e > 125 ? 125 : e);
+    const bool none = most >= 0x7f800000u;
+    const unsigned scale = none ? 255u : static_cast<unsigned>(e + 127);
+    const float unit = __uint_as_float(static_cast<unsigned>(e + 127) << 23);
+    unsigned codes = 0;
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0], x[1], unit, 0);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2], x[3], unit, 1);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4], x[5], unit, 2);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6], x[7], unit, 3);
+    const unsigned second = static_cast<unsigned>(__shfl_xor(static_cast<int>(scale), 4, 64));
+    if (token < 0 || token >= n) return;
+    int64_t slot = a.cache.slot(b, token);
+    if (slot < 0) return;
+    slot += static_cast<int64_t>(which) << a.cache.page_shift;
+    uint8_t *to = is_v ? a.cache.v_codes : a.cache.k_codes, *scales = is_v ? a.cache.v_scales : a.cache.k_scales;
+    *reinterpret_cast<unsigned *>(to + slot * 32 + 4 * c) = none ? 0u : codes;
+    if (c == 0) *reinterpret_cast<unsigned short *>(scales + slot * 2) = static_cast<unsigned short>(scale | second << 8);
+}
+
+// Two codes at a time -> bf16, exactly; `scale`: the exponent byte.
+__device__ __forceinline__ bf16x8 values8(unsigned codes, unsigned scale)
+{
+    const float unit = __uint_as_float(scale << 23);
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 1);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 3);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+template <typename T> __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs a)
+{
+    const unsigned id = blockIdx.x * 256u + threadIdx.x, item = id >> 3;
+    const int c = id & 7, kv_heads = a.cache.kv_heads;
+    const unsigned row = item / (2 * kv_heads);
+    if (row >= a.n_rows || !a.spans.covers(row)) return;
+    int which = static_cast<int>(item - row * (2 * kv_heads));
+    const int b = a.spans.find(row);
+    int first, len;
+    a.spans.of(b, first, len);
+    const int n = a.cache.length(b), token = n - len + static_cast<int>(row) - first;
+    const bool is_v = which >= kv_heads;
+    if (is_v) which -= kv_heads;
+    int64_t slot = token < 0 || token >= n ? -1 : a.cache.slot(b, token);
+    bf16x8 x = {};
+    if (slot >= 0) {
+        slot += static_cast<int64_t>(which) << a.cache.page_shift;
+        const uint8_t *codes = is_v ? a.cache.v_codes : a.cache.k_codes, *scales = is_v ? a.cache.v_scales : a.cache.k_scales;
+        x = values8(*reinterpret_cast<const unsigned *>(codes + slot * 32 + 4 * c), scales[slot * 2 + (c >> 2)]);
+    }
+    T *to = static_cast<T *>(is_v ? a.v : a.k) + row * a.kv_row + which * a.kv_head + 8 * c;
+    if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<bf16x8 *>(to) = x;
+    } else {
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = static_cast<float>(x[j]);
+        Io8<T>::store(to, f);
+    }
+}
+
+// ---- attention -------------------------------------------------------------------------------------------
+
+// Units of 64 cached tokens: a lane has one token; of the four pieces of a unit (keys, values; 32 channels each) a thread brings one
+// (256 threads) or all (64).  In LDS they are bf16, which holds the values exactly.  Blocks of values that read as NaN are put as zeros and
+// told apart by a word per 32 channels, because only rows that see their token may become NaN.
+constexpr int kCacheStage = 2 * kPlane + 32;  // bf16 elements: keys, values, two 64-bit words and room to stay aligned
+
+template <int THREADS> struct PageUnits {
+    static constexpr int kPieces = 256 / THREADS;
+    Cache cache;
+    int seq, kv_head, len;
+    int64_t next;  // slot of the lane's token of the unit to be fetched next
+    uint4 codes[kPieces];
+    unsigned scale[kPieces];
+    bool there;
+
+    __device__ __forceinline__ void find(int unit, int lane)
+    {
+        const int t = unit * kUnitRows + lane;
+        next = t < len ? cache.slot(seq, t) : -1;
+    }
+    __device__ __forceinline__ void fetch(int t, int lane)
+    {
+        there = next >= 0;
+        if (!there) return;
+        const int64_t slot = next + (static_cast<int64_t>(kv_head) << cache.page_shift);
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+            const int id = THREADS == 256 ? t >> 6 : p, half = id & 1;
+            codes[p] = *reinterpret_cast<const uint4 *>((id >= 2 ? cache.v_codes : cache.k_codes) + slot * 32 + 16 * half);
+            scale[p] = ((id >= 2 ? cache.v_scales : cache.k_scales) + slot * 2)[half];
+        }
+    }
+    __device__ __forceinline__ unsigned long long put(bf16_t *lds, int t, int lane)
+    {
+        unsigned long long *words = reinterpret_cast<unsigned long long *>(lds + 2 * kPlane);
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+            const int id = THREADS == 256 ? t >> 6 : p, half = id & 1;
+            uint4 x = codes[p];
+            unsigned s = scale[p];
+            const bool none = id >= 2 && there && s == 255u;
+            if (id >= 2) {
+                const unsigned long long w = __ballot(none);
+                if (lane == 0) words[half] = w;
+            }
+            if (!there || none) { x = uint4{0, 0, 0, 0}; s = 127; }
+            bf16_t *to = lds + (id >= 2 ? kPlane : 0);
+            *reinterpret_cast<bf16x8 *>(to + unit_chunk(lane, 4 * half + 0)) = values8(x.x, s);
+            *reinterpret_cast<bf16x8 *>(to + unit_chunk(lane, 4 * half + 1)) = values8(x.y, s);
+            *reinterpret_cast<bf16x8 *>(to + unit_chunk(lane, 4 * half + 2)) = values8(x.z, s);
+            *reinterpret_cast<bf16x8 *>(to + unit_chunk(lane, 4 * half + 3)) = values8(x.w, s);
+        }
+        return __ballot(there);
+    }
+};
+
+template <int PQ>
+__device__ __forceinline__ void cache_unit(SoftRow<PQ> &soft, const bf16_t *lds, unsigned long long seen, float factor, int lane)
+{
+    soft.template unit<1>(lds, lds + kPlane, seen, factor, lane);
+    const unsigned long long *words = reinterpret_cast<const unsigned long long *>(lds + 2 * kPlane);
+#pragma unroll
+    for (int dt = 0; dt < 2; ++dt) {
+        const unsigned long long none = words[dt];
+        if (none != 0 && (none & seen) != 0)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) soft.o[dt][r] = NAN;
+    }
+}
+
+template <typename T, bool WIDE> __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a)
+{
+    constexpr int P = sizeof(T) == 4 ? 3 : 1, kRows = WIDE ? 32 : 128;
+    extern __shared__ __align__(16) unsigned char smem[];
+    bf16_t *lds = reinterpret_cast<bf16_t *>(smem);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Share sh;
+    if (!find_share(a.spans, a.per_row, kRows, a.tiles, a.n_split, a.cache.kv_heads, sh)) return;
+    int first, rows;
+    a.spans.of(sh.seq, first, rows);
+    const int len = a.cache.length(sh.seq);
+    const int64_t items = static_cast<int64_t>(rows) * a.per_row, item0 = static_cast<int64_t>(sh.tile) * kRows;
+    const int64_t item = item0 + (WIDE ? 0 : 32 * wave) + (lane & 31);
+    const bool ok = item < items;
+    const int in_seq = static_cast<int>(item / a.per_row);
+    const int64_t row = first + in_seq;
+    const int head = sh.kv_head * a.per_row + static_cast<int>(item - static_cast<int64_t>(in_seq) * a.per_row);
+    SoftRow<P> soft;
+    soft.clear();
+    soft.load(static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head, ok, lane);
+
+    // tokens that the lane's row sees, and the last row of the tile
+    int sees = len, most = len;
+    if (a.causal) {
+        sees = min(len, len - rows + in_seq + 1);
+        const int64_t last = (item0 + kRows < items ? item0 + kRows : items) - 1;
+        most = max(0, min(len, len - rows + static_cast<int>(last / a.per_row) + 1));
+        if (!ok) sees = most;
+    }
+    int u0, u1;
+    piece((most + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
+    if constexpr (WIDE) {
+        PageUnits<64> units;
+        units.cache = a.cache; units.seq = sh.seq; units.kv_head = sh.kv_head; units.len = len;
+        bf16_t *mine = lds + wave * kCacheStage;
+        int u = u0 + wave;
+        if (u < u1) { units.find(u, lane); units.fetch(lane, lane); units.find(u + 4, lane); }
+        for (; u < u1; u += 4) {
+            const unsigned long long seen = units.put(mine, lane, lane) & low_bits(sees - u * kUnitRows);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (u + 4 < u1) { units.fetch(lane, lane); units.find(u + 8, lane); }
+            cache_unit(soft, mine, seen, a.factor, lane);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+        __syncthreads();
+        join_waves<4>(soft, a.factor, reinterpret_cast<float *>(smem), wave, lane);
+        if (wave == 0) store_soft<T>(soft, a.factor, a.to, sh.split, row, head, ok, lane);
+    } else {
+        PageUnits<256> units;
+        units.cache = a.cache; units.seq = sh.seq; units.kv_head = sh.kv_head; units.len = len;
+        if (u0 < u1) { units.find(u0, lane); units.fetch(threadIdx.x, lane); units.find(u0 + 1, lane); }
+        for (int u = u0; u < u1; ++u) {
+            bf16_t *stage = lds + ((u - u0) & 1) * kCacheStage;
+            const unsigned long long seen = units.put(stage, threadIdx.x, lane) & low_bits(sees - u * kUnitRows);
+            __syncthreads();
+            if (u + 1 < u1) { units.fetch(threadIdx.x, lane); units.find(u + 2, lane); }
+            cache_unit(soft, stage, seen, a.factor, lane);
+        }
+        store_soft<T>(soft, a.factor, a.to, sh.split, row, head, ok, lane);
+    }
+}
+
+// ---- faults of what a call was given ---------------------------------------------------------------------
+__global__ __launch_bounds__(1024) void cache_status_kernel(CacheArgs a, bool appends, int *status)
+{
+    int bad = spans_bad(a.spans) ? kDiagSpans : 0;
+    for (int b = 0; b < a.spans.batch; ++b) {
+        const int n = a.cache.length(b);
+        int first, len;
+        a.spans.of(b, first, len);
+        if (a.cache.kv_len[b] != n || (appends && len > n)) bad |= kDiagLength;
+        const int pages = (n + (1 << a.cache.page_shift) - 1) >> a.cache.page_shift;
+        for (int p = threadIdx.x; p < pages; p += 1024)
+            if (a.cache.slot(b, p << a.cache.page_shift) < 0) bad |= kDiagPage;
+        if (appends && a.rot.cos != nullptr && a.rot.positions == nullptr && len > 0 && n > a.rot.places) bad |= kDiagPosition;
+    }
+    if (appends && a.rot.cos != nullptr && a.rot.positions != nullptr)
+        for (int64_t i = threadIdx.x; i < a.n_rows * a.rot.axes; i += 1024)
+            if (a.spans.covers(i / a.rot.axes) && (a.rot.positions[i] < 0 || a.rot.positions[i] >= a.rot.places)) bad |= kDiagPosition;
+    __shared__ int all;
+    if (threadIdx.x == 0) all = 0;
+    __syncthreads();
+    if (bad != 0) atomicOr(&all, bad);
+    __syncthreads();
+    if (threadIdx.x == 0) *status = all;
+}
+
+template <typename T> hipError_t launch_cache_attn_t(const CacheArgs &a, bool few_rows, hipStream_t stream)
+{
+    const int64_t n = xcd_padded(a.tiles * a.n_split * a.cache.kv_heads);
+    if (!grid_ok(n)) return hipErrorInvalidValue;
+    constexpr size_t kStage = kCacheStage * sizeof(bf16_t);
+    if (few_rows) {
+        const hipError_t e = allow_lds(&cache_attn_kernel<T, true>, 4 * kStage);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((cache_attn_kernel<T, true>), dim3(static_cast<unsigned>(n)), dim3(256), 4 * kStage, stream, a);
+    } else {
+        hipLaunchKernelGGL((cache_attn_kernel<T, false>), dim3(static_cast<unsigned>(n)), dim3(256), 2 * kStage, stream, a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_cache_append(const CacheArgs &a, bool is_bf16, hipStream_t stream)
+{
+    const int64_t items = a.n_rows * (2 * a.cache.kv_heads + (a.q != nullptr ? a.heads : 0)), blocks = (items * 8 + 255) / 256;
+    if (!grid_ok(blocks)) return hipErrorInvalidValue;
+    if (is_bf16)
+        hipLaunchKernelGGL(cache_append_kernel<bf16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
+    else
+        hipLaunchKernelGGL(cache_append_kernel<float>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_read(const CacheArgs &a, bool is_bf16, hipStream_t stream)
+{
+    const int64_t blocks = (a.n_rows * 2 * a.cache.kv_heads * 8 + 255) / 256;
+    if (!grid_ok(blocks)) return hipErrorInvalidValue;
+    if (is_bf16)
+        hipLaunchKernelGGL(cache_read_kernel<bf16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
+    else
+        hipLaunchKernelGGL(cache_read_kernel<float>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_attn(const CacheArgs &a, bool few_rows, bool is_bf16, hipStream_t stream)
+{
+    return is_bf16 ? launch_cache_attn_t<bf16_t>(a, few_rows, stream) : launch_cache_attn_t<float>(a, few_rows, stream);
+}
+
+hipError_t launch_cache_status(const CacheArgs &a, bool appends, int *status, hipStream_t stream)
+{
+    hipLaunchKernelGGL(cache_status_kernel, dim3(1), dim3(1024), 0, stream, a, appends, status);
+    return hipGetLastError();
+}
+
+}  // namespace s3r

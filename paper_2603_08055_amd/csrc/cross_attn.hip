@@ -1,0 +1,496 @@
+// Cross attention, out[i] = sum_j softmax_j(scale q_i . k_j) v_j, with keys of another length than the queries, and its gradient
+//   P = exp(scale q k^T - lse),  D_i = out_i . d_out_i,  dS = scale P (d_out v^T - D),
+//   dq = dS k,  dk = dS^T q,  dv = P^T d_out.
+// Batches of ragged sequences lie one behind the other; several query heads may share a head of keys: their rows are then
+// items of one tile, and the gradient of the shared head is one sum over all of them.  No atomics: a sum that is split over workgroups
+// goes through partial results in the workspace, which another launch adds up in a fixed order.
+#include "s3r_unit_device.h"
+
+namespace s3r {
+
+namespace {
+
+constexpr int kTile = 128;  // held rows of a workgroup: 32 for each of four waves
+
+// LDS of a kernel that streams two tensors of `parts` planes: two stages where the operands are bf16 (32 KiB; one barrier per unit), one where
+// they are in three parts (48 KiB).
+template <typename T> struct Stages {
+    static constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
+    static constexpr int kCount = kParts == 1 ? 2 : 1;
+    static constexpr int kElems = 2 * kParts * kPlane;
+    static constexpr int kWideWaves = kParts == 1 ? 4 : 2;  // waves with an LDS stage each: 64 or 96 KiB
+};
+
+template <typename T, int THREADS>
+__device__ __forceinline__ RowUnits<T, THREADS> key_units(const CrossArgs &a, int kv_head, int first, int len)
+{
+    RowUnits<T, THREADS> u;
+    u.a = static_cast<const T *>(a.k) + first * a.kv_row + kv_head * a.kv_head;
+    u.b = static_cast<const T *>(a.v) + first * a.kv_row + kv_head * a.kv_head;
+    u.a_row = u.b_row = a.kv_row;
+    u.a_head = u.b_head = 0;
+    u.mask = a.key_mask != nullptr ? a.key_mask + first : nullptr;
+    u.items = len;
+    u.per_row = 1;
+    return u;
+}
+
+// Many rows: four waves hold 32 rows each and share every unit.
+// Few rows (WIDE): the waves hold the same 32 rows and take the units in turn, each through an LDS stage of its own.
+template <typename T, bool WIDE> __global__ __launch_bounds__(256, WIDE && sizeof(T) == 4 ? 1 : 2) void cross_kernel(CrossArgs a)
+{
+    constexpr int P = Stages<T>::kParts;
+    constexpr int kStage = Stages<T>::kElems, kStages = Stages<T>::kCount, kWaves = Stages<T>::kWideWaves;
+    extern __shared__ __align__(16) unsigned char smem[];
+    bf16_t *lds = reinterpret_cast<bf16_t *>(smem);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Share sh;
+    if (!find_share(a.q_spans, a.per_row, WIDE ? 32 : kTile, a.tiles, a.n_split, a.kv_heads, sh)) return;
+    int q0, q_len, k0, k_len;
+    a.q_spans.of(sh.seq, q0, q_len);
+    a.kv_spans.of(sh.seq, k0, k_len);
+
+    const int64_t item = static_cast<int64_t>(sh.tile) * (WIDE ? 32 : kTile) + (WIDE ? 0 : 32 * wave) + (lane & 31);
+    const bool ok = item < static_cast<int64_t>(q_len) * a.per_row;
+    const int64_t row = q0 + item / a.per_row;
+    const int head = sh.kv_head * a.per_row + static_cast<int>(item % a.per_row);
+    SoftRow<P> soft;
+    soft.clear();
+    soft.load(static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head, ok, lane);
+
+    int u0, u1;
+    piece((k_len + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
+    if constexpr (WIDE) {
+        auto units = key_units<T, 64>(a, sh.kv_head, k0, k_len);
+        bf16_t *mine = lds + wave * kStage;
+        int u = u0 + wave;
+        if (u < u1) units.fetch(u, lane);
+        for (; u < u1; u += kWaves) {
+            const unsigned long long seen = units.put(mine, lane);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (u + kWaves < u1) units.fetch(u + kWaves, lane);
+            soft.template unit<P>(mine, mine + P * kPlane, seen, a.factor, lane);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+        __syncthreads();
+        join_waves<kWaves>(soft, a.factor, reinterpret_cast<float *>(smem), wave, lane);
+        if (wave == 0) store_soft<T>(soft, a.factor, a.to, sh.split, row, head, ok, lane);
+    } else {
+        auto units = key_units<T, 256>(a, sh.kv_head, k0, k_len);
+        if (u0 < u1) units.fetch(u0, threadIdx.x);
+        for (int u = u0; u < u1; ++u) {
+            bf16_t *stage = lds + ((u - u0) % kStages) * kStage;
+            if (kStages == 1 && u > u0) __syncthreads();
+            const unsigned long long seen = units.put(stage, threadIdx.x);
+            __syncthreads();
+            if (u + 1 < u1) units.fetch(u + 1, threadIdx.x);
+            soft.template unit<P>(stage, stage + P * kPlane, seen, a.factor, lane);
+        }
+        store_soft<T>(soft, a.factor, a.to, sh.split, row, head, ok, lane);
+    }
+}
+
+// One result from the splits' normalised ones: weights 2^(lse_j - lse).  16 threads for a row of a head.
+template <typename T> __global__ __launch_bounds__(256) void soft_combine_kernel(SoftOut to, Spans spans, int n_split)
+{
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, at = i >> 4, share = to.rows * to.heads;
+    if (at >= share) return;
+    const int64_t row = at / to.heads;
+    if (!spans.covers(row)) return;
+    const int c = static_cast<int>(i & 15) * 4;
+    float top = -INFINITY, total = 0.f;
+    for (int j = 0; j < n_split; ++j) top = fmaxf(top, to.part_lse[j * share + at]);
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < n_split; ++j) {
+        const float l = to.part_lse[j * share + at];
+        if (l == -INFINITY) continue;  // no keys in this piece
+        const float w = l == top ? 1.f : exp2f(l - top);
+        const floatx4 o = *reinterpret_cast<const floatx4 *>(to.part_o + (j * share + at) * 64 + c);
+        total += w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += w * o[e];
+    }
+    const float w = total == 0.f ? 0.f : 1.f / total;
+    T *dst = static_cast<T *>(to.out) + at * 64 + c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dst[e] = from_float<T>(acc[e] * w);
+    if (c == 0 && to.lse != nullptr)
+        to.lse[(at - row * to.heads) * to.rows + row] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
+}
+
+// ---- gradient --------------------------------------------------------------------------------------------
+
+// D from the stored out: in bf16 it is off by the rounding of out, the same amount for all keys of a row, and
+// that would be most of the error of dq and dk (three times all other roundings together at 2748 rows over 10992 keys).  The sum of
+// a row's P (dP - D) over all keys, in fp32, is what D lacks: the query gradient adds it up and leaves D whole for the gradient of keys.
+// Its own result it mends by the sum of the dS as they entered the product, which should be 0: dS k - sum(dS) * P k.  That takes out
+// the lack of D and of the rounding of dS what all keys of the row have in common.  One product more of eight.
+template <typename T> constexpr bool kMendD = sizeof(T) == 2;
+
+// What the gradient needs of every row of a head: its log-sum (in log2; +inf where it saw no keys, so that every probability is 0) and
+// D = out . d_out.  16 threads for a row of a head.
+template <typename T>
+__global__ __launch_bounds__(256) void row_stats_kernel(const T *__restrict__ out, const T *__restrict__ d_out,
+                                                        const float *__restrict__ lse, float *__restrict__ stats, int64_t rows, int heads)
+{
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, at = i >> 4;
+    if (at >= rows * heads) return;
+    const int c = static_cast<int>(i & 15) * 4;
+    float d = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) d += to_float(out[at * 64 + c + e]) * to_float(d_out[at * 64 + c + e]);
+#pragma unroll
+    for (int m = 1; m < 16; m <<= 1) d += __shfl_xor(d, m, 64);
+    if (c != 0) return;
+    const int64_t row = at / heads, to = (at - row * heads) * rows + row;
+    const float l = lse[to];
+    stats[2 * to] = l == -INFINITY ? INFINITY : l * kLog2e;
+    stats[2 * to + 1] = d;
+}
+
+__device__ __forceinline__ float sum8(const bf16x8 &x)
+{
+    const bf16x2 one = {static_cast<bf16_t>(1.f), static_cast<bf16_t>(1.f)};
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) s = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{x[i], x[i + 1]}, one, s, false);
+    return s;
+}
+
+template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void grad_q_kernel(CrossArgs a)
+{
+    constexpr int P = Stages<T>::kParts, kStage = Stages<T>::kElems, kStages = Stages<T>::kCount;
+    extern __shared__ __align__(16) unsigned char smem[];
+    bf16_t *lds = reinterpret_cast<bf16_t *>(smem);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Share sh;
+    if (!find_share(a.q_spans, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, sh)) return;
+    int q0, q_len, k0, k_len;
+    a.q_spans.of(sh.seq, q0, q_len);
+    a.kv_spans.of(sh.seq, k0, k_len);
+    const int64_t item = static_cast<int64_t>(sh.tile) * kTile + 32 * wave + (lane & 31);
+    const bool ok = item < static_cast<int64_t>(q_len) * a.per_row;
+    const int64_t row = q0 + item / a.per_row;
+    const int head = sh.kv_head * a.per_row + static_cast<int>(item % a.per_row);
+    SoftRow<P> held, grad;  // q, and d_out; held.o: P k, grad.o: the gradient
+    held.clear();
+    held.load(static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head, ok, lane);
+    grad.clear();
+    grad.load(static_cast<const T *>(a.d_out) + (row * a.heads + head) * 64, ok, lane);
+    float l2 = INFINITY, d = 0.f, defect = 0.f, entered = 0.f;
+    float *stats = a.stats + 2 * (head * a.n_q + row);
+    if (ok) { l2 = stats[0]; d = stats[1]; }
+    int u0, u1;
+    piece((k_len + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
+    auto units = key_units<T, 256>(a, sh.kv_head, k0, k_len);
+    if (u0 < u1) units.fetch(u0, threadIdx.x);
+    for (int u = u0; u < u1; ++u) {
+        bf16_t *k = lds + ((u - u0) % kStages) * kStage, *v = k + P * kPlane;
+        if (kStages == 1 && u > u0) __syncthreads();
+        const unsigned long long seen = units.put(k, threadIdx.x);
+        __syncthreads();
+        if (u + 1 < u1) units.fetch(u + 1, threadIdx.x);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            floatx16 s = {}, dp = {};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                multiply<P>(s, held.q[i], [&](int part) { return unit_rows(k + part * kPlane, half, i, lane); });
+                multiply<P>(dp, grad.q[i], [&](int part) { return unit_rows(v + part * kPlane, half, i, lane); });
+            }
+            const uint32_t bits = lane_bits(seen, half, lane);
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                float x[8], y[8], sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int r = 8 * w + j;
+                    const bool counts = lane_bit(bits, r);
+                    y[j] = counts ? fast_exp2(fmaf(s[r], a.factor, -l2)) : 0.f;
+                    x[j] = counts ? y[j] * (dp[r] - d) : 0.f;
+                    sum += x[j];
+                }
+                defect += sum;
+                bf16x8 ds[P], p[P];
+                split_parts<P>(x, ds);
+                if constexpr (kMendD<T>) {
+                    split_parts<P>(y, p);
+                    entered += sum8(ds[0]);
+                }
+#pragma unroll
+                for (int dt = 0; dt < 2; ++dt) {
+                    multiply<P>(grad.o[dt], ds, [&](int part) { return unit_channels(k + part * kPlane, half, w, dt, lane); });
+                    if constexpr (kMendD<T>)
+                        multiply<P>(held.o[dt], p, [&](int part) { return unit_channels(k + part * kPlane, half, w, dt, lane); });
+                }
+            }
+        }
+    }
+    const int64_t at = row * a.heads + head, part = sh.split * a.n_q * a.heads + at;
+    if constexpr (kMendD<T>) {
+        defect = sum_with_other_half(defect);
+        entered = sum_with_other_half(entered);
+        if (a.part_q == nullptr) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                grad.o[0][r] -= entered * held.o[0][r];
+                grad.o[1][r] -= entered * held.o[1][r];
+            }
+            if (ok && lane < 32) stats[1] = d + defect;
+        } else {
+            store_row(held.o, 1.f, a.part_pk + part * 64, ok, lane);
+            if (ok && lane < 32) { a.part_defect[2 * part] = defect; a.part_defect[2 * part + 1] = entered; }
+        }
+    }
+    if (a.part_q != nullptr)
+        store_row(grad.o, 1.f, a.part_q + part * 64, ok, lane);
+    else
+        store_row(grad.o, a.scale, static_cast<T *>(a.dq) + at * 64, ok, lane);
+}
+
+// The query gradient from its pieces over keys.  16 threads for a row of a head.
+template <typename T> __global__ __launch_bounds__(256) void grad_q_combine_kernel(CrossArgs a)
+{
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, at = i >> 4, share = a.n_q * a.heads;
+    if (at >= share) return;
+    const int64_t row = at / a.heads;
+    if (!a.q_spans.covers(row)) return;
+    const int c = static_cast<int>(i & 15) * 4;
+    floatx4 g = {0.f, 0.f, 0.f, 0.f}, pk = {0.f, 0.f, 0.f, 0.f};
+    float defect = 0.f, entered = 0.f;
+    for (int j = 0; j < a.n_split; ++j) {
+        g += *reinterpret_cast<const floatx4 *>(a.part_q + (j * share + at) * 64 + c);
+        if constexpr (kMendD<T>) {
+            pk += *reinterpret_cast<const floatx4 *>(a.part_pk + (j * share + at) * 64 + c);
+            defect += a.part_defect[2 * (j * share + at)];
+            entered += a.part_defect[2 * (j * share + at) + 1];
+        }
+    }
+    T *dst = static_cast<T *>(a.dq) + at * 64 + c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dst[e] = from_float<T>(a.scale * (g[e] - entered * pk[e]));
+    if (kMendD<T> && c == 0) a.stats[2 * ((at - row * a.heads) * a.n_q + row) + 1] += defect;
+}
+
+template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void grad_kv_kernel(CrossArgs a)
+{
+    constexpr int P = Stages<T>::kParts, kStage = Stages<T>::kElems, kStages = Stages<T>::kCount;
+    extern __shared__ __align__(16) unsigned char smem[];
+    bf16_t *lds = reinterpret_cast<bf16_t *>(smem);
+    float *row_stats = reinterpret_cast<float *>(smem + sizeof(bf16_t) * kStages * kStage);  // [stages][2][64]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Share sh;
+    if (!find_share(a.kv_spans, 1, kTile, a.tiles, a.n_split, a.kv_heads, sh)) return;
+    int q0, q_len, k0, k_len;
+    a.q_spans.of(sh.seq, q0, q_len);
+    a.kv_spans.of(sh.seq, k0, k_len);
+    const int key = sh.tile * kTile + 32 * wave + (lane & 31);
+    const bool ok = key < k_len, seen = ok && (a.key_mask == nullptr || a.key_mask[k0 + key] != 0);
+    const int64_t row = k0 + key;
+    SoftRow<P> kk, vv;  // k and v; .o: their gradients
+    kk.clear();
+    vv.clear();
+    kk.load(static_cast<const T *>(a.k) + row * a.kv_row + sh.kv_head * a.kv_head, seen, lane);
+    vv.load(static_cast<const T *>(a.v) + row * a.kv_row + sh.kv_head * a.kv_head, seen, lane);
+
+    const int items = q_len * a.per_row, head0 = sh.kv_head * a.per_row;
+    RowUnits<T, 256> units;
+    units.a = static_cast<const T *>(a.q) + q0 * a.q_row + head0 * a.q_head;
+    units.a_row = a.q_row;
+    units.a_head = a.q_head;
+    units.b = static_cast<const T *>(a.d_out) + (static_cast<int64_t>(q0) * a.heads + head0) * 64;
+    units.b_row = static_cast<int64_t>(a.heads) * 64;
+    units.b_head = 64;
+    units.mask = nullptr;
+    units.items = items;
+    units.per_row = a.per_row;
+    float st = 0.f;
+    const int which = threadIdx.x >> 6;  // threads 0 .. 63 bring the rows' log-sums, 64 .. 127 their D
+    auto fetch_stats = [&](int u) {
+        const int r = u * kUnitRows + lane;
+        st = which == 0 ? INFINITY : 0.f;
+        if (which < 2 && r < items) {
+            const int i = r / a.per_row;
+            st = a.stats[2 * ((head0 + r - i * a.per_row) * a.n_q + q0 + i) + which];
+        }
+    };
+    int u0, u1;
+    piece((items + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
+    if (u0 < u1) { units.fetch(u0, threadIdx.x); fetch_stats(u0); }
+    for (int u = u0; u < u1; ++u) {
+        const int n = (u - u0) % kStages;
+        bf16_t *q = lds + n * kStage, *g = q + P * kPlane;
+        float *stats = row_stats + n * 128;
+        if (kStages == 1 && u > u0) __syncthreads();
+        units.put(q, threadIdx.x);
+        if (which < 2) stats[which * 64 + lane] = st;
+        __syncthreads();
+        if (u + 1 < u1) { units.fetch(u + 1, threadIdx.x); fetch_stats(u + 1); }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            floatx16 s = {}, dp = {};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                multiply<P>(s, kk.q[i], [&](int part) { return unit_rows(q + part * kPlane, half, i, lane); });
+                multiply<P>(dp, vv.q[i], [&](int part) { return unit_rows(g + part * kPlane, half, i, lane); });
+            }
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                float x[8], y[8];
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const int r0 = 32 * half + 16 * w + 8 * b + 4 * (lane >> 5);
+                    const floatx4 l2 = *reinterpret_cast<const floatx4 *>(stats + r0), d = *reinterpret_cast<const floatx4 *>(stats + 64 + r0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int r = 8 * w + 4 * b + e;
+                        x[4 * b + e] = fast_exp2(fmaf(s[r], a.factor, -l2[e]));
+                        y[4 * b + e] = x[4 * b + e] * (dp[r] - d[e]);
+                    }
+                }
+                bf16x8 p[P], ds[P];
+                split_parts<P>(x, p);
+                split_parts<P>(y, ds);
+#pragma unroll
+                for (int dt = 0; dt < 2; ++dt) {
+                    multiply<P>(vv.o[dt], p, [&](int part) { return unit_channels(g + part * kPlane, half, w, dt, lane); });
+                    multiply<P>(kk.o[dt], ds, [&](int part) { return unit_channels(q + part * kPlane, half, w, dt, lane); });
+                }
+            }
+        }
+    }
+    if (!seen)  // a masked key gets no gradient, whatever its lanes added up
+#pragma unroll
+        for (int r = 0; r < 16; ++r) kk.o[0][r] = kk.o[1][r] = vv.o[0][r] = vv.o[1][r] = 0.f;
+    const int64_t at = (row * a.kv_heads + sh.kv_head) * 64, share = a.n_kv * a.kv_heads * 64;
+    if (a.part_k != nullptr) {
+        store_row(kk.o, a.scale, a.part_k + sh.split * share + at, ok, lane);
+        store_row(vv.o, 1.f, a.part_v + sh.split * share + at, ok, lane);
+    } else {
+        store_row(kk.o, a.scale, static_cast<T *>(a.dk) + at, ok, lane);
+        store_row(vv.o, 1.f, static_cast<T *>(a.dv) + at, ok, lane);
+    }
+}
+
+// out = the sum of n_split partial results, for the rows of the sequences.  16 threads for a row of a head.
+template <typename T>
+__global__ __launch_bounds__(256) void add_parts_kernel(const float *__restrict__ part, T *__restrict__ out, Spans spans, int64_t rows,
+                                                        int heads, int n_split)
+{
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, n = rows * heads * 16;
+    if (i >= n || !spans.covers(i / (heads * 16))) return;
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < n_split; ++j) acc += *reinterpret_cast<const floatx4 *>(part + (j * n + i) * 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[i * 4 + e] = from_float<T>(acc[e]);
+}
+
+// Faults of the lists a call was given, as bits of *status.  One workgroup.
+__global__ __launch_bounds__(1024) void span_status_kernel(Spans q, Spans kv, int *status)
+{
+    const int bad = __syncthreads_or(spans_bad(q) || spans_bad(kv));
+    if (threadIdx.x == 0) *status = bad ? kDiagSpans : 0;
+}
+
+template <typename T> hipError_t launch_cross_t(const CrossArgs &a, bool few_rows, hipStream_t stream)
+{
+    const int64_t n = xcd_padded(a.tiles * a.n_split * a.kv_heads);
+    if (!grid_ok(n)) return hipErrorInvalidValue;
+    constexpr size_t kStage = Stages<T>::kElems * sizeof(bf16_t);
+    if (few_rows) {
+        const hipError_t e = allow_lds(&cross_kernel<T, true>, Stages<T>::kWideWaves * kStage);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((cross_kernel<T, true>), dim3(static_cast<unsigned>(n)), dim3(64 * Stages<T>::kWideWaves),
+                           Stages<T>::kWideWaves * kStage, stream, a);
+    } else {
+        hipLaunchKernelGGL((cross_kernel<T, false>), dim3(static_cast<unsigned>(n)), dim3(256), Stages<T>::kCount * kStage, stream, a);
+    }
+    return hipGetLastError();
+}
+
+template <typename T> hipError_t launch_grad_t(const CrossArgs &a, bool of_keys, hipStream_t stream)
+{
+    const int64_t n = xcd_padded(a.tiles * a.n_split * a.kv_heads);
+    if (!grid_ok(n)) return hipErrorInvalidValue;
+    const size_t lds = Stages<T>::kCount * (Stages<T>::kElems * sizeof(bf16_t) + (of_keys ? 128 * sizeof(float) : 0));
+    if (of_keys)
+        hipLaunchKernelGGL(grad_kv_kernel<T>, dim3(static_cast<unsigned>(n)), dim3(256), lds, stream, a);
+    else
+        hipLaunchKernelGGL(grad_q_kernel<T>, dim3(static_cast<unsigned>(n)), dim3(256), lds, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_cross(const CrossArgs &a, bool few_rows, bool is_bf16, hipStream_t stream)
+{
+    return is_bf16 ? launch_cross_t<bf16_t>(a, few_rows, stream) : launch_cross_t<float>(a, few_rows, stream);
+}
+
+hipError_t launch_grad_q(const CrossArgs &a, bool is_bf16, hipStream_t stream)
+{
+    return is_bf16 ? launch_grad_t<bf16_t>(a, false, stream) : launch_grad_t<float>(a, false, stream);
+}
+
+hipError_t launch_grad_q_combine(const CrossArgs &a, bool is_bf16, hipStream_t stream)
+{
+    const int64_t blocks = (a.n_q * a.heads * 16 + 255) / 256;
+    if (!grid_ok(blocks)) return hipErrorInvalidValue;
+    if (is_bf16)
+        hipLaunchKernelGGL(grad_q_combine_kernel<bf16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
+    else
+        hipLaunchKernelGGL(grad_q_combine_kernel<float>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_grad_kv(const CrossArgs &a, bool is_bf16, hipStream_t stream)
+{
+    return is_bf16 ? launch_grad_t<bf16_t>(a, true, stream) : launch_grad_t<float>(a, true, stream);
+}
+
+hipError_t launch_soft_combine(const SoftOut &to, const Spans &spans, int n_split, bool is_bf16, hipStream_t stream)
+{
+    const int64_t blocks = (to.rows * to.heads * 16 + 255) / 256;
+    if (!grid_ok(blocks)) return hipErrorInvalidValue;
+    if (is_bf16)
+        hipLaunchKernelGGL(soft_combine_kernel<bf16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, to, spans, n_split);
+    else
+        hipLaunchKernelGGL(soft_combine_kernel<float>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, to, spans, n_split);
+    return hipGetLastError();
+}
+
+hipError_t launch_row_stats(const void *out, const void *d_out, const float *lse, float *stats, int64_t rows, int heads, bool is_bf16,
+                            hipStream_t stream)
+{
+    const int64_t blocks = (rows * heads * 16 + 255) / 256;
+    if (!grid_ok(blocks)) return hipErrorInvalidValue;
+    if (is_bf16)
+        hipLaunchKernelGGL(row_stats_kernel<bf16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
+                           static_cast<const bf16_t *>(out), static_cast<const bf16_t *>(d_out), lse, stats, rows, heads);
+    else
+        hipLaunchKernelGGL(row_stats_kernel<float>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
+                           static_cast<const float *>(out), static_cast<const float *>(d_out), lse, stats, rows, heads);
+    return hipGetLastError();
+}
+
+hipError_t launch_add_parts(const float *part, void *out, const Spans &spans, int64_t rows, int heads, int n_split, bool is_bf16,
+                            hipStream_t stream)
+{
+    const int64_t blocks = (rows * heads * 16 + 255) / 256;
+    if (!grid_ok(blocks)) return hipErrorInvalidValue;
+    if (is_bf16)
+        hipLaunchKernelGGL(add_parts_kernel<bf16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, part,
+                           static_cast<bf16_t *>(out), spans, rows, heads, n_split);
+    else
+        hipLaunchKernelGGL(add_parts_kernel<float>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, part,
+                           static_cast<float *>(out), spans, rows, heads, n_split);
+    return hipGetLastError();
+}
+
+hipError_t launch_span_status(const Spans &q, const Spans &kv, int *status, hipStream_t stream)
+{
+    hipLaunchKernelGGL(span_status_kernel, dim3(1), dim3(1024), 0, stream, q, kv, status);
+    return hipGetLastError();
+}
+
+}  // namespace s3r

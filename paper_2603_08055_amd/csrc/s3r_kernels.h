@@ -233,4 +233,133 @@ hipError_t launch_select_pipe(const SelectArgs &a, hipStream_t stream);
 // registers (launch_select_mfma routes here).
 hipError_t launch_select_direct(const SelectArgs &a, hipStream_t stream);
 
+// ---- cross attention and attention over a 4-bit cache ----------------------------------------------
+
+// Rows of sequence b: start [batch + 1] in device memory, or null for one sequence of all n rows.  Entries are held into [0, n] and
+// made ascending, so that a broken list stays memory-safe.
+struct Spans {
+    const int32_t *start;
+    int batch;
+    int64_t n;
+    __device__ __forceinline__ void of(int b, int &first, int &len) const
+    {
+        if (start == nullptr) { first = 0; len = static_cast<int>(n); return; }
+        const int64_t s0 = start[b], s1 = start[b + 1];
+        const int64_t a = s0 < 0 ? 0 : (s0 > n ? n : s0), e = s1 < a ? a : (s1 > n ? n : s1);
+        first = static_cast<int>(a);
+        len = static_cast<int>(e - a);
+    }
+    // Whether some sequence of a valid list has this row.
+    __device__ __forceinline__ bool covers(int64_t row) const { return start == nullptr || (row >= start[0] && row < start[batch]); }
+    // The sequence that has this row (the last that starts at or before it).
+    __device__ __forceinline__ int find(int64_t row) const
+    {
+        if (start == nullptr) return 0;
+        int lo = 0, hi = batch - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (start[mid] <= row) lo = mid; else hi = mid - 1;
+        }
+        return lo;
+    }
+};
+
+// Where attention results go: the caller's tensors, or one split's part of the workspace.
+struct SoftOut {
+    void *out;        // [rows][heads][64]
+    float *lse;       // [heads][rows], natural logarithm, or null
+    float *part_o;    // [splits][rows][heads][64], or null: no splits
+    float *part_lse;  // [splits][rows][heads], log2
+    int64_t rows;
+    int heads;
+};
+
+// Faults that a call reports in its status word (S3R_DIAG_* of the public header).
+constexpr int kDiagPage = 4, kDiagSpans = 8, kDiagLength = 16, kDiagPosition = 32;
+
+// q and d_out rows, k and v rows: element strides between rows and between heads.  per_row = heads / kv_heads.  factor = scale * log2(e).
+// tiles: most tiles of the held rows (most_tiles); n_split: pieces of the streamed rows.  stats: see launch_row_stats.  part_*: partial
+// sums [n_split][rows][heads][64] where n_split > 1, else null (part_defect: [n_split][rows][heads][2]; it and part_pk for bf16 alone).
+struct CrossArgs {
+    const void *q, *k, *v, *d_out;
+    int64_t q_row, q_head, kv_row, kv_head;
+    const uint8_t *key_mask;
+    Spans q_spans, kv_spans;
+    int64_t n_q, n_kv, tiles;
+    int heads, kv_heads, per_row, n_split;
+    float scale, factor;
+    SoftOut to;
+    float *stats;
+    void *dq, *dk, *dv;
+    float *part_q, *part_pk, *part_defect, *part_k, *part_v;
+};
+
+// few_rows: a workgroup's waves divide the keys of 32 rows, and not 128 rows, among them.
+hipError_t launch_cross(const CrossArgs &a, bool few_rows, bool is_bf16, hipStream_t stream);
+hipError_t launch_soft_combine(const SoftOut &to, const Spans &spans, int n_split, bool is_bf16, hipStream_t stream);
+// stats [heads][rows][2]: log-sum in log2 (+inf for a row without keys) and out . d_out
+hipError_t launch_row_stats(const void *out, const void *d_out, const float *lse, float *stats, int64_t rows, int heads, bool is_bf16,
+                            hipStream_t stream);
+// bf16: D in stats is made whole, for launch_grad_kv, which comes after (n_split > 1: by the combine launch).
+hipError_t launch_grad_q(const CrossArgs &a, bool is_bf16, hipStream_t stream);
+hipError_t launch_grad_q_combine(const CrossArgs &a, bool is_bf16, hipStream_t stream);
+hipError_t launch_grad_kv(const CrossArgs &a, bool is_bf16, hipStream_t stream);
+hipError_t launch_add_parts(const float *part, void *out, const Spans &spans, int64_t rows, int heads, int n_split, bool is_bf16,
+                            hipStream_t stream);
+hipError_t launch_span_status(const Spans &q, const Spans &kv, int *status, hipStream_t stream);
+
+// A cache of keys and values in 4 bits: pages of `page` = 2^page_shift tokens; of every token and head 32 bytes of codes (64 channels of
+// e2m1, the even one in the low half of a byte) and two exponents with a bias of 127, one for 32 channels (255: they read as NaN).
+struct Cache {
+    uint8_t *k_codes, *v_codes, *k_scales, *v_scales;  // [n_pages][kv_heads][page][32 or 2]
+    const int32_t *page_table;                         // [batch][max_pages]
+    const int32_t *kv_len;                             // [batch]
+    int64_t n_pages;
+    int max_pages, page_shift, kv_heads;
+    __device__ __forceinline__ int length(int b) const
+    {
+        const int n = kv_len[b];
+        const int64_t most = static_cast<int64_t>(max_pages) << page_shift;
+        return n < 0 ? 0 : (n > most ? static_cast<int>(most) : n);
+    }
+    // Where token t of sequence b is in head 0's arrays, in tokens; -1: its page is none.
+    __device__ __forceinline__ int64_t slot(int b, int t) const
+    {
+        const int64_t p = page_table[static_cast<int64_t>(b) * max_pages + (t >> page_shift)];
+        return p < 0 || p >= n_pages ? -1 : ((p * kv_heads) << page_shift) + (t & ((1 << page_shift) - 1));
+    }
+};
+
+// Rotation of q and k: cos, sin [places][32 / axes]; positions [rows][axes], or null: the token's number.
+struct Rotation {
+    const float *cos, *sin;  // null: none
+    const int32_t *positions;
+    int64_t places;
+    int axes;
+    bool neighbours;
+};
+
+struct CacheArgs {
+    Cache cache;
+    Spans spans;      // of the rows
+    Rotation rot;
+    const void *q;
+    void *k, *v;      // rows to append, or room for rows read
+    int64_t q_row, q_head, kv_row, kv_head, n_rows;
+    int heads, per_row, n_split;
+    int64_t tiles;
+    bool causal;
+    float factor;
+    SoftOut to;       // to.out: attention, or q rotated
+};
+
+hipError_t launch_cache_append(const CacheArgs &a, bool is_bf16, hipStream_t stream);
+hipError_t launch_cache_read(const CacheArgs &a, bool is_bf16, hipStream_t stream);
+hipError_t launch_cache_attn(const CacheArgs &a, bool few_rows, bool is_bf16, hipStream_t stream);
+// appends: the rows' tokens have to be in the sequences, and positions in the table.
+hipError_t launch_cache_status(const CacheArgs &a, bool appends, int *status, hipStream_t stream);
+
+// Most tiles that `batch` sequences of n rows together can have.
+inline int64_t most_tiles(int64_t n, int per_row, int tile, int batch) { return n * per_row / tile + batch; }
+
 }  // namespace s3r

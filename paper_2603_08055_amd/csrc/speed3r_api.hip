@@ -964,4 +964,371 @@ s3r_status speed3r_dense_attn(const void *q, const void *k, const void *v, void 
     return S3R_OK;
 }
 
+// ---- cross attention ---------------------------------------------------------------------------------
+namespace {
+
+constexpr int64_t kMaxRowHeads = int64_t(1) << 28;  // rows * heads: 16 threads each stay below the 2^32 of a launch
+
+bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+s3r_status check_heads(int heads, int kv_heads, int head_dim, int dtype)
+{
+    if (heads <= 0 || kv_heads <= 0 || heads % kv_heads != 0)
+        return fail(S3R_ERR_INVALID_ARG, "heads (%d) must be a positive multiple of kv_heads (%d)", heads, kv_heads);
+    if (heads > 65535) return fail(S3R_ERR_UNSUPPORTED, "heads %d unsupported (max 65535)", heads);
+    if (head_dim != 64) return fail(S3R_ERR_UNSUPPORTED, "head_dim %d unsupported (must be 64)", head_dim);
+    if (dtype != S3R_F32 && dtype != S3R_BF16) return fail(S3R_ERR_UNSUPPORTED, "unknown dtype %d", dtype);
+    return S3R_OK;
+}
+
+s3r_status check_strides(const char *what, int64_t tok, int64_t head)
+{
+    if (tok < 0 || head < 0 || tok % 8 != 0 || head % 8 != 0)
+        return fail(S3R_ERR_INVALID_ARG, "the strides of %s (%lld, %lld) must be non-negative multiples of 8 elements", what,
+                    static_cast<long long>(tok), static_cast<long long>(head));
+    return S3R_OK;
+}
+
+// Pieces of the streamed units, where the tiles alone would not fill 256 CUs twice: at least `least` units each.
+int pieces(int64_t workgroups, int64_t units, int64_t least)
+{
+    int64_t s = (512 + workgroups - 1) / workgroups, most = units / least;
+    if (most > 64) most = 64;
+    if (s > most) s = most;
+    return s < 1 ? 1 : static_cast<int>(s);
+}
+
+struct CrossPlan {
+    bool few_rows;
+    int batch, per_row, split, split_q, split_kv;
+    int64_t tiles, q_tiles, kv_tiles;
+    size_t part_o, part_lse, forward;                   // workspace of the forward call
+    size_t stats, part_q, part_pk, part_defect, part_k, part_v, backward;     // of the gradient
+};
+
+s3r_status plan_cross(const s3r_cross_params *p, CrossPlan *out)
+{
+    if (!p) return fail(S3R_ERR_INVALID_ARG, "params is null");
+    s3r_status st = check_heads(p->heads, p->kv_heads, p->head_dim, p->dtype);
+    if (st != S3R_OK) return st;
+    if (p->n_q < 0 || p->n_kv < 0) return fail(S3R_ERR_INVALID_ARG, "n_q and n_kv must not be negative");
+    if (p->batch < 0 || (p->batch > 1 && !p->q_start))
+        return fail(S3R_ERR_INVALID_ARG, "batch (%d) must be 1 without q_start and kv_start, and never negative", p->batch);
+    if ((p->q_start != nullptr) != (p->kv_start != nullptr)) return fail(S3R_ERR_INVALID_ARG, "q_start and kv_start must be given together");
+    if (p->q_start && p->batch == 0) return fail(S3R_ERR_INVALID_ARG, "batch must be positive with q_start and kv_start");
+    CrossPlan c{};
+    c.batch = p->batch == 0 ? 1 : p->batch;
+    c.per_row = p->heads / p->kv_heads;
+    if (p->n_q > kMaxRowHeads / p->heads || p->n_kv > kMaxRowHeads / p->kv_heads || c.batch > (1 << 22) / p->kv_heads)
+        return fail(S3R_ERR_UNSUPPORTED, "rows * heads exceeds 2^28, or batch * kv_heads 2^22");
+    const int64_t items = p->n_q * c.per_row, units = (p->n_kv / c.batch + 63) / 64;
+    c.few_rows = items <= int64_t(32) * c.batch;
+    c.tiles = s3r::most_tiles(p->n_q, c.per_row, c.few_rows ? 32 : 128, c.batch);
+    c.split = pieces(c.tiles * p->kv_heads, units, c.few_rows ? 8 : 4);
+    c.q_tiles = s3r::most_tiles(p->n_q, c.per_row, 128, c.batch);
+    c.split_q = pieces(c.q_tiles * p->kv_heads, units, 4);
+    c.kv_tiles = s3r::most_tiles(p->n_kv, 1, 128, c.batch);
+    c.split_kv = pieces(c.kv_tiles * p->kv_heads, (items / c.batch + 63) / 64, 4);
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
+    const size_t rows = static_cast<size_t>(p->n_q) * p->heads, keys = static_cast<size_t>(p->n_kv) * p->kv_heads;
+    c.part_o = take(c.split > 1 ? c.split * rows * 64 * sizeof(float) : 0);
+    c.part_lse = take(c.split > 1 ? c.split * rows * sizeof(float) : 0);
+    c.forward = off;
+    off = 0;
+    c.stats = take(rows * 2 * sizeof(float));
+    c.part_q = take(c.split_q > 1 ? c.split_q * rows * 64 * sizeof(float) : 0);
+    const bool mend = c.split_q > 1 && p->dtype == S3R_BF16;
+    c.part_pk = take(mend ? c.split_q * rows * 64 * sizeof(float) : 0);
+    c.part_defect = take(mend ? c.split_q * rows * 2 * sizeof(float) : 0);
+    c.part_k = take(c.split_kv > 1 ? c.split_kv * keys * 64 * sizeof(float) : 0);
+    c.part_v = take(c.split_kv > 1 ? c.split_kv * keys * 64 * sizeof(float) : 0);
+    c.backward = off;
+    *out = c;
+    return S3R_OK;
+}
+
+s3r_status check_workspace(const void *ws, size_t have, size_t need)
+{
+    if (need == 0) return S3R_OK;
+    if (!ws || have < need) return fail(S3R_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", ws ? have : size_t(0), need);
+    if (!aligned(ws, kAlign)) return fail(S3R_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    return S3R_OK;
+}
+
+// Checks and arguments that the forward call and the gradient have in common.
+s3r_status cross_args(const s3r_cross_params *p, const CrossPlan &c, s3r::CrossArgs *out)
+{
+    if (p->n_q > 0 && (!p->q || !p->out)) return fail(S3R_ERR_INVALID_ARG, "q and out must be non-null");
+    if (p->n_kv > 0 && (!p->k || !p->v)) return fail(S3R_ERR_INVALID_ARG, "k and v must be non-null");
+    if (!aligned16(p->q) || !aligned16(p->k) || !aligned16(p->v) || !aligned16(p->out) || !aligned(p->lse, 4) ||
+        !aligned(p->q_start, 4) || !aligned(p->kv_start, 4) || !aligned(p->status, 4))
+        return fail(S3R_ERR_INVALID_ARG, "device pointers must be 16-byte aligned (lse, starts and status: 4)");
+    if (p->n_q > 0 && (p->out == p->q || p->out == p->k || p->out == p->v)) return fail(S3R_ERR_INVALID_ARG, "out must not alias an input");
+    s3r_status st = check_strides("q", p->q_stride_tok, p->q_stride_head);
+    if (st != S3R_OK) return st;
+    st = check_strides("k and v", p->kv_stride_tok, p->kv_stride_head);
+    if (st != S3R_OK) return st;
+    s3r::CrossArgs a{};
+    a.q = p->q; a.k = p->k; a.v = p->v;
+    a.q_row = p->q_stride_tok ? p->q_stride_tok : int64_t(p->heads) * 64;
+    a.q_head = p->q_stride_head ? p->q_stride_head : 64;
+    a.kv_row = p->kv_stride_tok ? p->kv_stride_tok : int64_t(p->kv_heads) * 64;
+    a.kv_head = p->kv_stride_head ? p->kv_stride_head : 64;
+    a.key_mask = p->key_mask;
+    a.q_spans = s3r::Spans{p->q_start, c.batch, p->n_q};
+    a.kv_spans = s3r::Spans{p->kv_start, c.batch, p->n_kv};
+    a.n_q = p->n_q; a.n_kv = p->n_kv;
+    a.heads = p->heads; a.kv_heads = p->kv_heads; a.per_row = c.per_row;
+    a.scale = resolve_scale(p->softmax_scale, 64);
+    a.factor = a.scale * 1.4426950408889634f;
+    a.to.out = p->out; a.to.lse = p->lse; a.to.rows = p->n_q; a.to.heads = p->heads;
+    *out = a;
+    return S3R_OK;
+}
+
+float *floats_at(void *base, size_t off) { return reinterpret_cast<float *>(at(base, off)); }
+
+}  // namespace
+
+size_t speed3r_cross_workspace_bytes(const s3r_cross_params *p, int backward)
+{
+    CrossPlan c;
+    if (plan_cross(p, &c) != S3R_OK) return SIZE_MAX;
+    return backward ? c.backward : c.forward;
+}
+
+s3r_status speed3r_cross_attn(const s3r_cross_params *p)
+{
+    CrossPlan c;
+    s3r_status st = plan_cross(p, &c);
+    if (st != S3R_OK) return st;
+    s3r::CrossArgs a;
+    st = cross_args(p, c, &a);
+    if (st != S3R_OK) return st;
+    st = check_workspace(p->workspace, p->workspace_bytes, c.forward);
+    if (st != S3R_OK) return st;
+    hipStream_t s = static_cast<hipStream_t>(p->stream);
+    const bool bf16 = p->dtype == S3R_BF16;
+    if (p->status) S3R_HIP(s3r::launch_span_status(a.q_spans, a.kv_spans, p->status, s), "status kernel launch");
+    if (p->n_q == 0) return S3R_OK;
+    a.tiles = c.tiles;
+    a.n_split = c.split;
+    if (c.split > 1) {
+        a.to.part_o = floats_at(p->workspace, c.part_o);
+        a.to.part_lse = floats_at(p->workspace, c.part_lse);
+    }
+    StageTimer tm(S3R_STAGE_DENSE, s);
+    S3R_HIP(s3r::launch_cross(a, c.few_rows, bf16, s), "cross attention kernel launch");
+    if (c.split > 1) S3R_HIP(s3r::launch_soft_combine(a.to, a.q_spans, c.split, bf16, s), "cross attention combine kernel launch");
+    return S3R_OK;
+}
+
+s3r_status speed3r_cross_attn_backward(const s3r_cross_params *p)
+{
+    CrossPlan c;
+    s3r_status st = plan_cross(p, &c);
+    if (st != S3R_OK) return st;
+    s3r::CrossArgs a;
+    st = cross_args(p, c, &a);
+    if (st != S3R_OK) return st;
+    if (p->n_q > 0 && (!p->lse || !p->d_out || !p->dq)) return fail(S3R_ERR_INVALID_ARG, "lse, d_out and dq must be non-null");
+    if (p->n_kv > 0 && (!p->dk || !p->dv)) return fail(S3R_ERR_INVALID_ARG, "dk and dv must be non-null");
+    if (!aligned16(p->d_out) || !aligned16(p->dq) || !aligned16(p->dk) || !aligned16(p->dv))
+        return fail(S3R_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+    for (const void *g : {p->dq, p->dk, p->dv})
+        if (g && (g == p->q || g == p->k || g == p->v || g == p->out || g == p->d_out))
+            return fail(S3R_ERR_INVALID_ARG, "gradients must not alias inputs");
+    if ((p->dk && (p->dk == p->dv || p->dk == p->dq)) || (p->dq && p->dq == p->dv))
+        return fail(S3R_ERR_INVALID_ARG, "gradients must not alias each other");
+    st = check_workspace(p->workspace, p->workspace_bytes, c.backward);
+    if (st != S3R_OK) return st;
+    hipStream_t s = static_cast<hipStream_t>(p->stream);
+    const bool bf16 = p->dtype == S3R_BF16;
+    if (p->status) S3R_HIP(s3r::launch_span_status(a.q_spans, a.kv_spans, p->status, s), "status kernel launch");
+    float *stats = p->n_q > 0 ? floats_at(p->workspace, c.stats) : nullptr;
+    a.d_out = p->d_out; a.stats = stats;
+    a.dq = p->dq; a.dk = p->dk; a.dv = p->dv;
+    StageTimer tm(S3R_STAGE_DENSE, s);
+    if (p->n_q > 0) {
+        S3R_HIP(s3r::launch_row_stats(p->out, p->d_out, p->lse, stats, p->n_q, p->heads, bf16, s), "row statistics kernel launch");
+        a.tiles = c.q_tiles;
+        a.n_split = c.split_q;
+        if (c.split_q > 1) {
+            a.part_q = floats_at(p->workspace, c.part_q);
+            a.part_pk = floats_at(p->workspace, c.part_pk);
+            a.part_defect = floats_at(p->workspace, c.part_defect);
+        }
+        S3R_HIP(s3r::launch_grad_q(a, bf16, s), "query gradient kernel launch");
+        if (c.split_q > 1) S3R_HIP(s3r::launch_grad_q_combine(a, bf16, s), "query gradient combine kernel launch");
+    }
+    if (p->n_kv > 0) {
+        a.tiles = c.kv_tiles;
+        a.n_split = c.split_kv;
+        if (c.split_kv > 1) {
+            a.part_k = floats_at(p->workspace, c.part_k);
+            a.part_v = floats_at(p->workspace, c.part_v);
+        }
+        S3R_HIP(s3r::launch_grad_kv(a, bf16, s), "key gradient kernel launch");
+        if (c.split_kv > 1) {
+            S3R_HIP(s3r::launch_add_parts(a.part_k, p->dk, a.kv_spans, p->n_kv, p->kv_heads, c.split_kv, bf16, s), "key gradient sum launch");
+            S3R_HIP(s3r::launch_add_parts(a.part_v, p->dv, a.kv_spans, p->n_kv, p->kv_heads, c.split_kv, bf16, s), "value gradient sum launch");
+        }
+    }
+    return S3R_OK;
+}
+
+// ---- a cache in 4 bits ---------------------------------------------------------------------------------
+namespace {
+
+struct CachePlan {
+    bool few_rows;
+    int split;
+    int64_t tiles;
+    size_t part_o, part_lse, total;
+};
+
+s3r_status plan_cache(const s3r_cache_params *p, CachePlan *out)
+{
+    if (!p) return fail(S3R_ERR_INVALID_ARG, "params is null");
+    s3r_status st = check_heads(p->heads, p->kv_heads, p->head_dim, p->dtype);
+    if (st != S3R_OK) return st;
+    if (p->page != 16 && p->page != 32 && p->page != 64 && p->page != 128)
+        return fail(S3R_ERR_UNSUPPORTED, "page %d unsupported (must be 16, 32, 64 or 128)", p->page);
+    if (p->n_pages <= 0 || p->max_pages <= 0 || p->batch <= 0 || p->n_rows < 0)
+        return fail(S3R_ERR_INVALID_ARG, "n_pages (%lld), max_pages (%d) and batch (%d) must be positive, n_rows (%lld) not negative",
+                    static_cast<long long>(p->n_pages), p->max_pages, p->batch, static_cast<long long>(p->n_rows));
+    if (p->batch > 1 && !p->row_start) return fail(S3R_ERR_INVALID_ARG, "batch (%d) must be 1 without row_start", p->batch);
+    if (int64_t(p->max_pages) * p->page > 0x7fffffffLL - 4096 || p->n_pages > 0x7fffffffLL)
+        return fail(S3R_ERR_UNSUPPORTED, "max_pages * page exceeds 2^31 - 4097 tokens, or n_pages 2^31 - 1");
+    if (p->n_rows > kMaxRowHeads / (p->heads + 2 * p->kv_heads) || p->batch > (1 << 22) / p->kv_heads)
+        return fail(S3R_ERR_UNSUPPORTED, "rows * (heads + 2 kv_heads) exceeds 2^28, or batch * kv_heads 2^22");
+    CachePlan c{};
+    const int per_row = p->heads / p->kv_heads;
+    const int64_t units = (int64_t(p->max_pages) * p->page + 63) / 64;
+    c.few_rows = p->n_rows * per_row <= int64_t(32) * p->batch;
+    c.tiles = s3r::most_tiles(p->n_rows, per_row, c.few_rows ? 32 : 128, p->batch);
+    c.split = pieces(c.tiles * p->kv_heads, units, c.few_rows ? 8 : 4);
+    const size_t rows = static_cast<size_t>(p->n_rows) * p->heads;
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
+    c.part_o = take(c.split > 1 ? c.split * rows * 64 * sizeof(float) : 0);
+    c.part_lse = take(c.split > 1 ? c.split * rows * sizeof(float) : 0);
+    c.total = off;
+    *out = c;
+    return S3R_OK;
+}
+
+s3r_status cache_args(const s3r_cache_params *p, s3r::CacheArgs *out)
+{
+    if (!p->k_codes || !p->v_codes || !p->k_scales || !p->v_scales || !p->page_table || !p->kv_len)
+        return fail(S3R_ERR_INVALID_ARG, "the cache's four arrays, page_table and kv_len must be non-null");
+    if (!aligned16(p->k_codes) || !aligned16(p->v_codes) || !aligned(p->k_scales, 4) || !aligned(p->v_scales, 4) || !aligned(p->page_table, 4) ||
+        !aligned(p->kv_len, 4) || !aligned(p->row_start, 4) || !aligned(p->status, 4) || !aligned(p->lse, 4) || !aligned(p->positions, 4) ||
+        !aligned16(p->q) || !aligned16(p->k) || !aligned16(p->v) || !aligned16(p->out) || !aligned16(p->cos) || !aligned16(p->sin))
+        return fail(S3R_ERR_INVALID_ARG, "device pointers must be 16-byte aligned (scales, lists, lse and status: 4)");
+    s3r_status st = check_strides("q", p->q_stride_tok, p->q_stride_head);
+    if (st != S3R_OK) return st;
+    st = check_strides("k and v", p->kv_stride_tok, p->kv_stride_head);
+    if (st != S3R_OK) return st;
+    s3r::CacheArgs a{};
+    int shift = 4;
+    while ((1 << shift) < p->page) ++shift;
+    a.cache = s3r::Cache{p->k_codes, p->v_codes, p->k_scales, p->v_scales, p->page_table, p->kv_len, p->n_pages, p->max_pages, shift, p->kv_heads};
+    a.spans = s3r::Spans{p->row_start, p->batch, p->n_rows};
+    a.q = p->q; a.k = p->k; a.v = p->v;
+    a.q_row = p->q_stride_tok ? p->q_stride_tok : int64_t(p->heads) * 64;
+    a.q_head = p->q_stride_head ? p->q_stride_head : 64;
+    a.kv_row = p->kv_stride_tok ? p->kv_stride_tok : int64_t(p->kv_heads) * 64;
+    a.kv_head = p->kv_stride_head ? p->kv_stride_head : 64;
+    a.n_rows = p->n_rows; a.heads = p->heads; a.per_row = p->heads / p->kv_heads;
+    a.causal = p->causal != 0;
+    a.factor = resolve_scale(p->softmax_scale, 64) * 1.4426950408889634f;
+    a.to.out = p->out; a.to.lse = p->lse; a.to.rows = p->n_rows; a.to.heads = p->heads;
+    *out = a;
+    return S3R_OK;
+}
+
+}  // namespace
+
+size_t speed3r_cache_workspace_bytes(const s3r_cache_params *p)
+{
+    CachePlan c;
+    return plan_cache(p, &c) == S3R_OK ? c.total : SIZE_MAX;
+}
+
+s3r_status speed3r_cache_append(const s3r_cache_params *p)
+{
+    CachePlan c;
+    s3r_status st = plan_cache(p, &c);
+    if (st != S3R_OK) return st;
+    s3r::CacheArgs a;
+    st = cache_args(p, &a);
+    if (st != S3R_OK) return st;
+    if (p->n_rows > 0 && (!p->k || !p->v)) return fail(S3R_ERR_INVALID_ARG, "k and v must be non-null");
+    if ((p->cos != nullptr) != (p->sin != nullptr)) return fail(S3R_ERR_INVALID_ARG, "cos and sin must be given together");
+    if (p->n_rows > 0 && (p->q != nullptr) != (p->out != nullptr)) return fail(S3R_ERR_INVALID_ARG, "q and out must be given together");
+    if (p->q && !p->cos) return fail(S3R_ERR_INVALID_ARG, "q is given to be rotated: cos and sin are needed");
+    if (p->q && p->q == p->out) return fail(S3R_ERR_INVALID_ARG, "out must not alias an input");
+    if (p->cos) {
+        if (p->rot_axes != 1 && p->rot_axes != 2) return fail(S3R_ERR_INVALID_ARG, "rot_axes (%d) must be 1 or 2", p->rot_axes);
+        if (p->rot_axes == 2 && !p->positions) return fail(S3R_ERR_INVALID_ARG, "two axes need positions");
+        if (p->rot_neighbours != 0 && p->rot_neighbours != 1) return fail(S3R_ERR_INVALID_ARG, "rot_neighbours (%d) must be 0 or 1", p->rot_neighbours);
+        if (p->n_positions <= 0) return fail(S3R_ERR_INVALID_ARG, "n_positions must be positive");
+        a.rot = s3r::Rotation{p->cos, p->sin, p->positions, p->n_positions, p->rot_axes, p->rot_neighbours != 0};
+    }
+    hipStream_t s = static_cast<hipStream_t>(p->stream);
+    if (p->status) S3R_HIP(s3r::launch_cache_status(a, true, p->status, s), "status kernel launch");
+    if (p->n_rows == 0) return S3R_OK;
+    StageTimer tm(S3R_STAGE_POOL, s);
+    S3R_HIP(s3r::launch_cache_append(a, p->dtype == S3R_BF16, s), "cache append kernel launch");
+    return S3R_OK;
+}
+
+s3r_status speed3r_cache_read(const s3r_cache_params *p)
+{
+    CachePlan c;
+    s3r_status st = plan_cache(p, &c);
+    if (st != S3R_OK) return st;
+    s3r::CacheArgs a;
+    st = cache_args(p, &a);
+    if (st != S3R_OK) return st;
+    if (p->n_rows > 0 && (!p->k || !p->v || p->k == p->v)) return fail(S3R_ERR_INVALID_ARG, "k and v must be non-null and apart");
+    hipStream_t s = static_cast<hipStream_t>(p->stream);
+    if (p->status) S3R_HIP(s3r::launch_cache_status(a, true, p->status, s), "status kernel launch");
+    if (p->n_rows == 0) return S3R_OK;
+    StageTimer tm(S3R_STAGE_POOL, s);
+    S3R_HIP(s3r::launch_cache_read(a, p->dtype == S3R_BF16, s), "cache read kernel launch");
+    return S3R_OK;
+}
+
+s3r_status speed3r_cache_attn(const s3r_cache_params *p)
+{
+    CachePlan c;
+    s3r_status st = plan_cache(p, &c);
+    if (st != S3R_OK) return st;
+    s3r::CacheArgs a;
+    st = cache_args(p, &a);
+    if (st != S3R_OK) return st;
+    if (p->n_rows > 0 && (!p->q || !p->out)) return fail(S3R_ERR_INVALID_ARG, "q and out must be non-null");
+    if (p->n_rows > 0 && p->q == p->out) return fail(S3R_ERR_INVALID_ARG, "out must not alias an input");
+    if (p->causal != 0 && p->causal != 1) return fail(S3R_ERR_INVALID_ARG, "causal (%d) must be 0 or 1", p->causal);
+    st = check_workspace(p->workspace, p->workspace_bytes, c.total);
+    if (st != S3R_OK) return st;
+    hipStream_t s = static_cast<hipStream_t>(p->stream);
+    const bool bf16 = p->dtype == S3R_BF16;
+    if (p->status) S3R_HIP(s3r::launch_cache_status(a, false, p->status, s), "status kernel launch");
+    if (p->n_rows == 0) return S3R_OK;
+    a.tiles = c.tiles;
+    a.n_split = c.split;
+    if (c.split > 1) {
+        a.to.part_o = floats_at(p->workspace, c.part_o);
+        a.to.part_lse = floats_at(p->workspace, c.part_lse);
+    }
+    StageTimer tm(S3R_STAGE_DENSE, s);
+    S3R_HIP(s3r::launch_cache_attn(a, c.few_rows, bf16, s), "cache attention kernel launch");
+    if (c.split > 1) S3R_HIP(s3r::launch_soft_combine(a.to, a.spans, c.split, bf16, s), "cache attention combine kernel launch");
+    return S3R_OK;
+}
+
 }  // extern "C"

@@ -4,8 +4,10 @@ streams, nothing else); every step of the path runs in the library's HIP kernels
 fallback: if the library is missing or a call fails, an exception is raised."""
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -15,6 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libspeed3r.so")
 S3R_OK, S3R_ERR_INVALID_ARG, S3R_ERR_UNSUPPORTED, S3R_ERR_WORKSPACE, S3R_ERR_HIP = range(5)
 S3R_F32, S3R_BF16 = 0, 1
 S3R_DIAG_FORCED_RANGE, S3R_DIAG_FORCED_ORDER = 1, 2
+S3R_DIAG_PAGE, S3R_DIAG_SPANS, S3R_DIAG_LENGTH, S3R_DIAG_POSITION = 4, 8, 16, 32
 STAGES = ("pool", "split", "compress", "topk", "select", "dense")
 HEAD_DIM = 64
 
@@ -35,6 +38,26 @@ class s3r_params(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_size_t), ("stream", _vp)]
 
 
+class s3r_cross_params(ctypes.Structure):
+    _fields_ = [("q", _vp), ("k", _vp), ("v", _vp), ("out", _vp), ("lse", _vp), ("d_out", _vp),
+                ("dq", _vp), ("dk", _vp), ("dv", _vp), ("q_start", _vp), ("kv_start", _vp), ("key_mask", _vp),
+                ("status", _vp), ("n_q", _i64), ("n_kv", _i64), ("q_stride_tok", _i64), ("q_stride_head", _i64),
+                ("kv_stride_tok", _i64), ("kv_stride_head", _i64), ("batch", _int), ("heads", _int),
+                ("kv_heads", _int), ("head_dim", _int), ("dtype", _int), ("softmax_scale", _flt),
+                ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t), ("stream", _vp)]
+
+
+class s3r_cache_params(ctypes.Structure):
+    _fields_ = [("k_codes", _vp), ("v_codes", _vp), ("k_scales", _vp), ("v_scales", _vp), ("page_table", _vp),
+                ("kv_len", _vp), ("row_start", _vp), ("n_pages", _i64), ("n_rows", _i64), ("page", _int),
+                ("max_pages", _int), ("batch", _int), ("heads", _int), ("kv_heads", _int), ("head_dim", _int),
+                ("dtype", _int), ("q", _vp), ("out", _vp), ("k", _vp), ("v", _vp), ("q_stride_tok", _i64),
+                ("q_stride_head", _i64), ("kv_stride_tok", _i64), ("kv_stride_head", _i64), ("cos", _vp), ("sin", _vp),
+                ("positions", _vp), ("n_positions", _i64), ("rot_axes", _int), ("rot_neighbours", _int),
+                ("causal", _int), ("softmax_scale", _flt), ("lse", _vp), ("status", _vp), ("workspace", _vp),
+                ("workspace_bytes", ctypes.c_size_t), ("stream", _vp)]
+
+
 EXPORTS = {
     "speed3r_workspace_bytes": (ctypes.c_size_t, [_i64, _int, _int, _int, _int, _int, _int]),
     "speed3r_workspace_bytes_ex": (ctypes.c_size_t, [ctypes.POINTER(s3r_params)]),
@@ -51,6 +74,13 @@ EXPORTS = {
     "speed3r_topk_blocks": (_int, [_vp, _i64, _vp, _i64, _int, _int, _vp]),
     "speed3r_select_attn": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _int, _int,
                                    _int, _int, _int, _flt, _vp]),
+    "speed3r_cross_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(s3r_cross_params), _int]),
+    "speed3r_cross_attn": (_int, [ctypes.POINTER(s3r_cross_params)]),
+    "speed3r_cross_attn_backward": (_int, [ctypes.POINTER(s3r_cross_params)]),
+    "speed3r_cache_append": (_int, [ctypes.POINTER(s3r_cache_params)]),
+    "speed3r_cache_read": (_int, [ctypes.POINTER(s3r_cache_params)]),
+    "speed3r_cache_attn": (_int, [ctypes.POINTER(s3r_cache_params)]),
+    "speed3r_cache_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(s3r_cache_params)]),
     "speed3r_probe_select_loads": (_int, [_vp, _vp, _vp, _vp, _vp, _i64, _int, _int, _int, _int, _int, _int, _vp]),
     "speed3r_set_profiling": (_int, [_int]),
     "speed3r_get_stage_ms": (_int, [ctypes.POINTER(_flt), ctypes.POINTER(_int)]),
@@ -301,6 +331,247 @@ def speed3r_select_attn(q, k, v, idx, out, block, *, o_comp=None, gate_logits=No
                                       _dev(out, "out", q.dtype), _dev(o_sel, "o_sel", q.dtype),
                                       _dev(lse, "lse", torch.float32), n_tok, heads, head_dim, block,
                                       idx.shape[2], dt, float(softmax_scale), _stream(stream)))
+
+
+# ---- cross attention and a cache in 4 bits: tensors may be on any GPU, all of a call on one ------------------
+
+def _on(device):
+    """The context in which a call's launches go to `device`."""
+    if device.type != "cuda":
+        raise TypeError(f"tensors must be on the GPU, not on {device}")
+    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _arg(t, name, device, dtype, shape):
+    """data_ptr of a contiguous tensor of that shape on the call's GPU (None -> NULL)."""
+    if t is None:
+        return None
+    if not (isinstance(t, torch.Tensor) and t.device == device and t.is_contiguous()):
+        raise TypeError(f"{name} must be a contiguous tensor on {device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
+    return t.data_ptr()
+
+
+def _rows_arg(tensors, names, device, dtype, shape):
+    """data_ptrs and common (row, head) strides of tensors [rows, heads, head_dim] with contiguous channels; strides
+    of 0 mean packed.  A stride along an axis of one entry is not used and may be anything."""
+    strides = []
+    for t, name in zip(tensors, names):
+        if not (isinstance(t, torch.Tensor) and t.device == device):
+            raise TypeError(f"{name} must be a tensor on {device}")
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
+        if t.is_contiguous():
+            strides.append((t.shape[1] * t.shape[2], t.shape[2]))
+            continue
+        if t.stride(2) != 1:
+            raise TypeError(f"the channels of {name} must be contiguous")
+        if (t.stride(0) == 0 and t.shape[0] > 1) or (t.stride(1) == 0 and t.shape[1] > 1):
+            raise TypeError(f"{name} must not be broadcast along its rows or heads")
+        strides.append((t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2],
+                        t.stride(1) if t.shape[1] > 1 else t.shape[2]))
+    if any(s != strides[0] for s in strides):
+        raise TypeError(f"{' and '.join(names)} must share their row and head strides")
+    return [t.data_ptr() for t in tensors], strides[0]
+
+
+def _workspace(workspace, need, device):
+    """A uint8 tensor of `need` bytes, the caller's where there is one (2^64 - 1: the call itself says why)."""
+    if workspace is not None:
+        if not (isinstance(workspace, torch.Tensor) and workspace.device == device and workspace.is_contiguous()
+                and workspace.dtype == torch.uint8):
+            raise TypeError(f"workspace must be a contiguous uint8 tensor on {device}")
+        return workspace
+    return torch.empty(need, dtype=torch.uint8, device=device) if 0 < need < 1 << 62 else None
+
+
+def _cross_params(q, k, v, q_start, kv_start, key_mask, softmax_scale, status, stream):
+    if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or k.shape[2] != q.shape[2]:
+        raise ValueError("q must be [n_q, heads, head_dim], k and v [n_kv, kv_heads, head_dim]")
+    if not q.is_cuda:
+        raise TypeError("q must be a tensor on the GPU")
+    p, dev = s3r_cross_params(), q.device
+    p.n_q, p.heads, p.head_dim = q.shape
+    p.n_kv, p.kv_heads = k.shape[0], k.shape[1]
+    p.dtype = _dtype_code(q)
+    (p.q,), (p.q_stride_tok, p.q_stride_head) = _rows_arg((q,), ("q",), dev, q.dtype, q.shape)
+    (p.k, p.v), (p.kv_stride_tok, p.kv_stride_head) = _rows_arg((k, v), ("k", "v"), dev, q.dtype, k.shape)
+    p.batch = 1 if q_start is None else q_start.numel() - 1
+    starts = (p.batch + 1,)
+    p.q_start = _arg(q_start, "q_start", dev, torch.int32, starts)
+    p.kv_start = _arg(kv_start, "kv_start", dev, torch.int32, starts)
+    if key_mask is not None and key_mask.dtype == torch.bool:
+        key_mask = key_mask.view(torch.uint8)
+    p.key_mask = _arg(key_mask, "key_mask", dev, torch.uint8, (p.n_kv,))
+    p.softmax_scale = float(softmax_scale)
+    p.status = _arg(status, "status", dev, torch.int32, (1,))
+    p.stream = _stream(stream)
+    return p
+
+
+def speed3r_cross_workspace_bytes(q, k, *, q_start=None, backward=False) -> int:
+    """Bytes of workspace that speed3r_cross_attn, or its gradient, needs for these shapes (tensors, or anything
+    with their `shape` and `dtype`)."""
+    p = s3r_cross_params()
+    p.n_q, p.heads, p.head_dim = q.shape
+    p.n_kv, p.kv_heads = k.shape[0], k.shape[1]
+    p.dtype = _dtype_code(q)
+    p.batch = 1 if q_start is None else q_start.numel() - 1
+    p.q_start = p.kv_start = None if q_start is None else 4          # only whether they are given counts here
+    need = int(load().speed3r_cross_workspace_bytes(ctypes.byref(p), int(bool(backward))))
+    if need >= 1 << 62:
+        raise Speed3rError(S3R_ERR_INVALID_ARG, speed3r_last_error())
+    return need
+
+
+def _run_cross(fn, p, backward, workspace, device):
+    workspace = _workspace(workspace, int(load().speed3r_cross_workspace_bytes(ctypes.byref(p), backward)), device)
+    if workspace is not None:
+        p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    _check(fn(ctypes.byref(p)))
+    return workspace
+
+
+def speed3r_cross_attn(q, k, v, out, *, lse=None, q_start=None, kv_start=None, key_mask=None, softmax_scale=0.0,
+                       workspace=None, status=None, stream=None):
+    """Attention of q [n_q, heads, 64] over k, v [n_kv, kv_heads, 64] into out (contiguous, like q); lse: fp32 [heads, n_q].
+    q_start, kv_start: int32 [batch + 1], the sequences of a ragged batch; key_mask: bool or uint8 [n_kv], 0 leaves a key
+    out; status: int32 [1], receives 0 or S3R_DIAG_SPANS.  k and v (and q) may be strided views.  Returns the workspace
+    used (None: none was needed)."""
+    with _on(q.device):
+        p = _cross_params(q, k, v, q_start, kv_start, key_mask, softmax_scale, status, stream)
+        p.out = _arg(out, "out", q.device, q.dtype, q.shape)
+        p.lse = _arg(lse, "lse", q.device, torch.float32, (q.shape[1], q.shape[0]))
+        return _run_cross(load().speed3r_cross_attn, p, 0, workspace, q.device)
+
+
+def speed3r_cross_attn_backward(q, k, v, out, lse, d_out, dq, dk, dv, *, q_start=None, kv_start=None, key_mask=None,
+                                softmax_scale=0.0, workspace=None, status=None, stream=None):
+    """Gradients of speed3r_cross_attn into dq, dk, dv (contiguous, like q, k, v), from its out and lse and the gradient
+    d_out of out.  The other arguments are those of the forward call.  Returns the workspace used."""
+    with _on(q.device):
+        p = _cross_params(q, k, v, q_start, kv_start, key_mask, softmax_scale, status, stream)
+        for name, t, shape in (("out", out, q.shape), ("d_out", d_out, q.shape), ("dq", dq, q.shape), ("dk", dk, k.shape),
+                               ("dv", dv, k.shape)):
+            setattr(p, name, _arg(t, name, q.device, q.dtype, shape))
+        p.lse = _arg(lse, "lse", q.device, torch.float32, (q.shape[1], q.shape[0]))
+        return _run_cross(load().speed3r_cross_attn_backward, p, 1, workspace, q.device)
+
+
+class PagedCache(NamedTuple):
+    """The four uint8 tensors of a cache in 4 bits: codes [n_pages, kv_heads, page, 32], scales [n_pages, kv_heads, page, 2]."""
+    k_codes: torch.Tensor
+    v_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_scales: torch.Tensor
+
+    @classmethod
+    def empty(cls, n_pages, kv_heads, page, device="cuda"):
+        return cls(*(torch.zeros((n_pages, kv_heads, page, w), dtype=torch.uint8, device=device) for w in (32, 32, 2, 2)))
+
+
+def _cache_params(cache, n_rows, heads, head_dim, dtype, page_table, kv_len, row_start, status, stream):
+    p, dev = s3r_cache_params(), cache.k_codes.device
+    if not cache.k_codes.is_cuda:
+        raise TypeError("the cache must be on the GPU")
+    if cache.k_codes.dim() != 4 or cache.k_codes.shape[3] != 32:
+        raise ValueError("codes must be [n_pages, kv_heads, page, 32]")
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [batch, max_pages]")
+    p.n_pages, p.kv_heads, p.page, _ = shape = tuple(cache.k_codes.shape)
+    for name, t, width in zip(cache._fields, cache, (32, 32, 2, 2)):
+        setattr(p, name, _arg(t, name, dev, torch.uint8, shape[:3] + (width,)))
+    p.batch, p.max_pages = page_table.shape
+    p.page_table = _arg(page_table, "page_table", dev, torch.int32, page_table.shape)
+    p.kv_len = _arg(kv_len, "kv_len", dev, torch.int32, (p.batch,))
+    p.row_start = _arg(row_start, "row_start", dev, torch.int32, (p.batch + 1,))
+    p.n_rows, p.heads, p.head_dim, p.dtype = n_rows, heads, head_dim, dtype
+    p.status = _arg(status, "status", dev, torch.int32, (1,))
+    p.stream = _stream(stream)
+    return p
+
+
+def speed3r_cache_append(cache, k, v, page_table, kv_len, row_start=None, *, q=None, q_out=None, cos=None, sin=None,
+                         positions=None, pairs="halves", status=None, stream=None):
+    """k, v [n_rows, kv_heads, 64] become the last tokens of their sequences in the cache (a PagedCache); kv_len int32 [batch]
+    counts them.  page_table: int32 [batch, max_pages]; row_start: int32 [batch + 1] (None: one sequence).
+    cos, sin: fp32 [n_positions, 32] rotate k by positions int32 [n_rows] (None: token numbers); of width 16 they rotate by
+    two positions, int32 [n_rows, 2].  pairs: "halves" or "neighbours".  q [n_rows, heads, 64] is rotated into q_out."""
+    with _on(cache.k_codes.device):
+        dev, like = cache.k_codes.device, k if q is None else q
+        if pairs not in ("halves", "neighbours"):
+            raise ValueError('pairs must be "halves" or "neighbours"')
+        if k.dim() != 3 or like.dim() != 3:
+            raise ValueError("k, v must be [n_rows, kv_heads, head_dim], q [n_rows, heads, head_dim]")
+        p = _cache_params(cache, k.shape[0], like.shape[1], k.shape[2], _dtype_code(k), page_table, kv_len, row_start, status, stream)
+        (p.k, p.v), (p.kv_stride_tok, p.kv_stride_head) = _rows_arg((k, v), ("k", "v"), dev, k.dtype, (k.shape[0], p.kv_heads, k.shape[2]))
+        if q is not None:
+            shape = (k.shape[0], q.shape[1], k.shape[2])
+            (p.q,), (p.q_stride_tok, p.q_stride_head) = _rows_arg((q,), ("q",), dev, k.dtype, shape)
+            p.out = _arg(q_out, "q_out", dev, k.dtype, shape)
+        elif q_out is not None:
+            raise ValueError("q_out is given without q")
+        if cos is not None:
+            if cos.dim() != 2 or cos.shape[1] not in (16, 32):
+                raise ValueError("cos and sin must be [n_positions, 32], or [n_positions, 16] for two axes")
+            p.rot_axes, p.n_positions, p.rot_neighbours = 32 // cos.shape[1], cos.shape[0], int(pairs == "neighbours")
+            if positions is not None:
+                shape = (k.shape[0],) if p.rot_axes == 1 and positions.dim() == 1 else (k.shape[0], p.rot_axes)
+                p.positions = _arg(positions, "positions", dev, torch.int32, shape)
+            p.cos = _arg(cos, "cos", dev, torch.float32, cos.shape)
+            p.sin = _arg(sin, "sin", dev, torch.float32, cos.shape)
+        elif sin is not None or positions is not None:
+            raise ValueError("sin and positions need cos")
+        _check(load().speed3r_cache_append(ctypes.byref(p)))
+
+
+def speed3r_cache_read(cache, k, v, page_table, kv_len, row_start=None, *, status=None, stream=None):
+    """The last tokens of the sequences, as many as k, v [n_rows, kv_heads, 64] have rows for them, as values into k and v."""
+    with _on(cache.k_codes.device):
+        if k.dim() != 3:
+            raise ValueError("k, v must be [n_rows, kv_heads, head_dim]")
+        p = _cache_params(cache, k.shape[0], k.shape[1], k.shape[2], _dtype_code(k), page_table, kv_len, row_start, status, stream)
+        (p.k, p.v), (p.kv_stride_tok, p.kv_stride_head) = _rows_arg((k, v), ("k", "v"), cache.k_codes.device, k.dtype,
+                                                                    (k.shape[0], p.kv_heads, k.shape[2]))
+        _check(load().speed3r_cache_read(ctypes.byref(p)))
+
+
+def speed3r_cache_workspace_bytes(cache, n_rows, heads, dtype, batch, max_pages) -> int:
+    """Bytes of workspace of speed3r_cache_attn; dtype: S3R_BF16 or S3R_F32."""
+    p = s3r_cache_params()
+    p.n_pages, p.kv_heads, p.page, _ = cache.k_codes.shape
+    p.n_rows, p.heads, p.head_dim, p.dtype, p.batch, p.max_pages = n_rows, heads, HEAD_DIM, dtype, batch, max_pages
+    p.row_start = 4                                                  # only whether it is given counts here
+    need = int(load().speed3r_cache_workspace_bytes(ctypes.byref(p)))
+    if need >= 1 << 62:
+        raise Speed3rError(S3R_ERR_INVALID_ARG, speed3r_last_error())
+    return need
+
+
+def speed3r_cache_attn(cache, q, out, page_table, kv_len, row_start=None, *, causal=True, lse=None, softmax_scale=0.0,
+                       workspace=None, status=None, stream=None):
+    """Attention of q [n_rows, heads, 64] (rotated already) over the cached tokens of their sequences into out.  The rows of a
+    sequence are its last tokens; causal: each sees the tokens up to its own, otherwise all.  Returns the workspace used
+    (None: none was needed)."""
+    with _on(cache.k_codes.device):
+        dev = cache.k_codes.device
+        if q.dim() != 3:
+            raise ValueError("q must be [n_rows, heads, head_dim]")
+        p = _cache_params(cache, q.shape[0], q.shape[1], q.shape[2], _dtype_code(q), page_table, kv_len, row_start, status, stream)
+        (p.q,), (p.q_stride_tok, p.q_stride_head) = _rows_arg((q,), ("q",), dev, q.dtype, q.shape)
+        p.out = _arg(out, "out", dev, q.dtype, q.shape)
+        p.lse = _arg(lse, "lse", dev, torch.float32, (q.shape[1], q.shape[0]))
+        p.causal, p.softmax_scale = int(bool(causal)), float(softmax_scale)
+        workspace = _workspace(workspace, int(load().speed3r_cache_workspace_bytes(ctypes.byref(p))), dev)
+        if workspace is not None:
+            p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel()
+        _check(load().speed3r_cache_attn(ctypes.byref(p)))
+        return workspace
 
 
 def speed3r_probe_select_loads(q, k, v, idx, out, block, ring_stages=0, wg_per_cu=0, stream=None):
