@@ -4,7 +4,6 @@ streams, nothing else); every step of the path runs in the library's HIP kernels
 fallback: if the library is missing or a call fails, an exception is raised."""
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from typing import NamedTuple
@@ -333,85 +332,107 @@ def speed3r_select_attn(q, k, v, idx, out, block, *, o_comp=None, gate_logits=No
                                       idx.shape[2], dt, float(softmax_scale), _stream(stream)))
 
 
-# ---- cross attention and a cache in 4 bits: tensors may be on any GPU, all of a call on one ------------------
+# ---- cross attention and a cache in 4 bits ------------------------------------------------------------------
+# Tensors may be on any GPU, all of a call on one; the launches go to that GPU's current stream.  A decoding step makes these
+# calls for every layer and token: the checks are written to cost 3 to 4 us of a call's 8 (the launch itself takes 3.5).
 
-def _on(device):
-    """The context in which a call's launches go to `device`."""
-    if device.type != "cuda":
-        raise TypeError(f"tensors must be on the GPU, not on {device}")
-    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+def _gpu(t, name):
+    """Index of the tensor's GPU."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise TypeError(f"{name} must be a tensor on the GPU")
+    return t.get_device()
 
 
-def _arg(t, name, device, dtype, shape):
-    """data_ptr of a contiguous tensor of that shape on the call's GPU (None -> NULL)."""
+def _arg(t, name, index, dtype, shape):
+    """data_ptr of a contiguous tensor of that type and shape on GPU `index` (None -> NULL)."""
     if t is None:
         return None
-    if not (isinstance(t, torch.Tensor) and t.device == device and t.is_contiguous()):
-        raise TypeError(f"{name} must be a contiguous tensor on {device}")
-    if t.dtype != dtype:
+    if not isinstance(t, torch.Tensor) or t.get_device() != index:
+        raise TypeError(f"{name} must be a tensor on GPU {index}")
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
+    if not t.is_contiguous():
+        raise TypeError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
-def _rows_arg(tensors, names, device, dtype, shape):
-    """data_ptrs and common (row, head) strides of tensors [rows, heads, head_dim] with contiguous channels; strides
-    of 0 mean packed.  A stride along an axis of one entry is not used and may be anything."""
-    strides = []
-    for t, name in zip(tensors, names):
-        if not (isinstance(t, torch.Tensor) and t.device == device):
-            raise TypeError(f"{name} must be a tensor on {device}")
-        if t.dtype != dtype:
-            raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
-        if tuple(t.shape) != tuple(shape):
-            raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
-        if t.is_contiguous():
-            strides.append((t.shape[1] * t.shape[2], t.shape[2]))
-            continue
+def _rows_arg(t, name, index, dtype, shape):
+    """data_ptr and (row, head) strides of a tensor [rows, heads, head_dim] with contiguous channels.  A stride along an
+    axis of one entry is not used and may be anything."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != index:
+        raise TypeError(f"{name} must be a tensor on GPU {index}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
+    row, head = shape[1] * shape[2], shape[2]
+    if not t.is_contiguous():
         if t.stride(2) != 1:
             raise TypeError(f"the channels of {name} must be contiguous")
-        if (t.stride(0) == 0 and t.shape[0] > 1) or (t.stride(1) == 0 and t.shape[1] > 1):
+        if shape[0] > 1:
+            row = t.stride(0)
+        if shape[1] > 1:
+            head = t.stride(1)
+        if row == 0 or head == 0:
             raise TypeError(f"{name} must not be broadcast along its rows or heads")
-        strides.append((t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2],
-                        t.stride(1) if t.shape[1] > 1 else t.shape[2]))
-    if any(s != strides[0] for s in strides):
-        raise TypeError(f"{' and '.join(names)} must share their row and head strides")
-    return [t.data_ptr() for t in tensors], strides[0]
+    return t.data_ptr(), row, head
 
 
-def _workspace(workspace, need, device):
-    """A uint8 tensor of `need` bytes, the caller's where there is one (2^64 - 1: the call itself says why)."""
+def _kv_arg(k, v, index, dtype, shape):
+    """data_ptrs of k and v and their common strides."""
+    pk, row, head = _rows_arg(k, "k", index, dtype, shape)
+    pv, v_row, v_head = _rows_arg(v, "v", index, dtype, shape)
+    if (row, head) != (v_row, v_head):
+        raise TypeError("k and v must share their row and head strides")
+    return pk, pv, row, head
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+def _stream_of(stream, index):
+    return _raw_stream(index) if stream is None else _stream(stream)
+
+
+def _call(fn, p, need, workspace, index):
+    """The call with a workspace of `need` bytes (2^64 - 1: its arguments are wrong and the call says why), the caller's where there
+    is one.  Returns the workspace."""
     if workspace is not None:
-        if not (isinstance(workspace, torch.Tensor) and workspace.device == device and workspace.is_contiguous()
-                and workspace.dtype == torch.uint8):
-            raise TypeError(f"workspace must be a contiguous uint8 tensor on {device}")
-        return workspace
-    return torch.empty(need, dtype=torch.uint8, device=device) if 0 < need < 1 << 62 else None
+        if not isinstance(workspace, torch.Tensor) or workspace.get_device() != index or workspace.dtype is not torch.uint8 \
+                or not workspace.is_contiguous():
+            raise TypeError(f"workspace must be a contiguous uint8 tensor on GPU {index}")
+    elif 0 < need < 1 << 62:
+        workspace = torch.empty(need, dtype=torch.uint8, device=f"cuda:{index}")
+    if workspace is not None:
+        p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    if index == torch.cuda.current_device():
+        status = fn(ctypes.byref(p))
+    else:
+        with torch.cuda.device(index):
+            status = fn(ctypes.byref(p))
+    if status != S3R_OK:
+        raise Speed3rError(status, speed3r_last_error())
+    return workspace
 
 
-def _cross_params(q, k, v, q_start, kv_start, key_mask, softmax_scale, status, stream):
-    if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or k.shape[2] != q.shape[2]:
+def _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, status, stream, index):
+    if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q must be [n_q, heads, head_dim], k and v [n_kv, kv_heads, head_dim]")
-    if not q.is_cuda:
-        raise TypeError("q must be a tensor on the GPU")
-    p, dev = s3r_cross_params(), q.device
-    p.n_q, p.heads, p.head_dim = q.shape
-    p.n_kv, p.kv_heads = k.shape[0], k.shape[1]
-    p.dtype = _dtype_code(q)
-    (p.q,), (p.q_stride_tok, p.q_stride_head) = _rows_arg((q,), ("q",), dev, q.dtype, q.shape)
-    (p.k, p.v), (p.kv_stride_tok, p.kv_stride_head) = _rows_arg((k, v), ("k", "v"), dev, q.dtype, k.shape)
-    p.batch = 1 if q_start is None else q_start.numel() - 1
-    starts = (p.batch + 1,)
-    p.q_start = _arg(q_start, "q_start", dev, torch.int32, starts)
-    p.kv_start = _arg(kv_start, "kv_start", dev, torch.int32, starts)
-    if key_mask is not None and key_mask.dtype == torch.bool:
+    n_q, heads, head_dim = shape = q.shape
+    n_kv, kv_heads, _ = kv_shape = (k.shape[0], k.shape[1], head_dim)
+    dtype = q.dtype
+    pq, q_row, q_head = _rows_arg(q, "q", index, dtype, shape)
+    pk, pv, kv_row, kv_head = _kv_arg(k, v, index, dtype, kv_shape)
+    batch = 1 if q_start is None else q_start.numel() - 1
+    if key_mask is not None and key_mask.dtype is torch.bool:
         key_mask = key_mask.view(torch.uint8)
-    p.key_mask = _arg(key_mask, "key_mask", dev, torch.uint8, (p.n_kv,))
-    p.softmax_scale = float(softmax_scale)
-    p.status = _arg(status, "status", dev, torch.int32, (1,))
-    p.stream = _stream(stream)
-    return p
+    return s3r_cross_params(
+        pq, pk, pv, _arg(out, "out", index, dtype, shape), _arg(lse, "lse", index, torch.float32, (heads, n_q)), None, None, None, None,
+        _arg(q_start, "q_start", index, torch.int32, (batch + 1,)), _arg(kv_start, "kv_start", index, torch.int32, (batch + 1,)),
+        _arg(key_mask, "key_mask", index, torch.uint8, (n_kv,)), _arg(status, "status", index, torch.int32, (1,)), n_q, n_kv,
+        q_row, q_head, kv_row, kv_head, batch, heads, kv_heads, head_dim, _dtype_code(q), softmax_scale, None, 0, _stream_of(stream, index))
 
 
 def speed3r_cross_workspace_bytes(q, k, *, q_start=None, backward=False) -> int:
@@ -423,44 +444,32 @@ def speed3r_cross_workspace_bytes(q, k, *, q_start=None, backward=False) -> int:
     p.dtype = _dtype_code(q)
     p.batch = 1 if q_start is None else q_start.numel() - 1
     p.q_start = p.kv_start = None if q_start is None else 4          # only whether they are given counts here
-    need = int(load().speed3r_cross_workspace_bytes(ctypes.byref(p), int(bool(backward))))
+    need = load().speed3r_cross_workspace_bytes(ctypes.byref(p), int(bool(backward)))
     if need >= 1 << 62:
         raise Speed3rError(S3R_ERR_INVALID_ARG, speed3r_last_error())
     return need
-
-
-def _run_cross(fn, p, backward, workspace, device):
-    workspace = _workspace(workspace, int(load().speed3r_cross_workspace_bytes(ctypes.byref(p), backward)), device)
-    if workspace is not None:
-        p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    _check(fn(ctypes.byref(p)))
-    return workspace
 
 
 def speed3r_cross_attn(q, k, v, out, *, lse=None, q_start=None, kv_start=None, key_mask=None, softmax_scale=0.0,
                        workspace=None, status=None, stream=None):
     """Attention of q [n_q, heads, 64] over k, v [n_kv, kv_heads, 64] into out (contiguous, like q); lse: fp32 [heads, n_q].
     q_start, kv_start: int32 [batch + 1], the sequences of a ragged batch; key_mask: bool or uint8 [n_kv], 0 leaves a key
-    out; status: int32 [1], receives 0 or S3R_DIAG_SPANS.  k and v (and q) may be strided views.  Returns the workspace
+    out; status: int32 [1], receives 0 or S3R_DIAG_SPANS.  q, and k and v alike, may be strided views.  Returns the workspace
     used (None: none was needed)."""
-    with _on(q.device):
-        p = _cross_params(q, k, v, q_start, kv_start, key_mask, softmax_scale, status, stream)
-        p.out = _arg(out, "out", q.device, q.dtype, q.shape)
-        p.lse = _arg(lse, "lse", q.device, torch.float32, (q.shape[1], q.shape[0]))
-        return _run_cross(load().speed3r_cross_attn, p, 0, workspace, q.device)
+    index, lib = _gpu(q, "q"), load()
+    p = _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, status, stream, index)
+    return _call(lib.speed3r_cross_attn, p, lib.speed3r_cross_workspace_bytes(ctypes.byref(p), 0), workspace, index)
 
 
 def speed3r_cross_attn_backward(q, k, v, out, lse, d_out, dq, dk, dv, *, q_start=None, kv_start=None, key_mask=None,
                                 softmax_scale=0.0, workspace=None, status=None, stream=None):
     """Gradients of speed3r_cross_attn into dq, dk, dv (contiguous, like q, k, v), from its out and lse and the gradient
     d_out of out.  The other arguments are those of the forward call.  Returns the workspace used."""
-    with _on(q.device):
-        p = _cross_params(q, k, v, q_start, kv_start, key_mask, softmax_scale, status, stream)
-        for name, t, shape in (("out", out, q.shape), ("d_out", d_out, q.shape), ("dq", dq, q.shape), ("dk", dk, k.shape),
-                               ("dv", dv, k.shape)):
-            setattr(p, name, _arg(t, name, q.device, q.dtype, shape))
-        p.lse = _arg(lse, "lse", q.device, torch.float32, (q.shape[1], q.shape[0]))
-        return _run_cross(load().speed3r_cross_attn_backward, p, 1, workspace, q.device)
+    index, lib = _gpu(q, "q"), load()
+    p = _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, status, stream, index)
+    p.d_out, p.dq = _arg(d_out, "d_out", index, q.dtype, q.shape), _arg(dq, "dq", index, q.dtype, q.shape)
+    p.dk, p.dv = _arg(dk, "dk", index, q.dtype, k.shape), _arg(dv, "dv", index, q.dtype, k.shape)
+    return _call(lib.speed3r_cross_attn_backward, p, lib.speed3r_cross_workspace_bytes(ctypes.byref(p), 1), workspace, index)
 
 
 class PagedCache(NamedTuple):
@@ -475,25 +484,45 @@ class PagedCache(NamedTuple):
         return cls(*(torch.zeros((n_pages, kv_heads, page, w), dtype=torch.uint8, device=device) for w in (32, 32, 2, 2)))
 
 
-def _cache_params(cache, n_rows, heads, head_dim, dtype, page_table, kv_len, row_start, status, stream):
-    p, dev = s3r_cache_params(), cache.k_codes.device
-    if not cache.k_codes.is_cuda:
-        raise TypeError("the cache must be on the GPU")
-    if cache.k_codes.dim() != 4 or cache.k_codes.shape[3] != 32:
+def _cache_params(cache, rows, page_table, kv_len, row_start, status, stream, index, *, q=None, out=None, k=None, v=None,
+                  cos=None, sin=None, positions=None, pairs="halves", causal=0, softmax_scale=0.0, lse=None):
+    """rows: the tensor [n_rows, heads, head_dim] whose heads count as the queries' and whose type as the rows'."""
+    k_codes, v_codes, k_scales, v_scales = cache
+    if k_codes.dim() != 4 or k_codes.shape[3] != 32:
         raise ValueError("codes must be [n_pages, kv_heads, page, 32]")
-    if page_table.dim() != 2:
-        raise ValueError("page_table must be [batch, max_pages]")
-    p.n_pages, p.kv_heads, p.page, _ = shape = tuple(cache.k_codes.shape)
-    for name, t, width in zip(cache._fields, cache, (32, 32, 2, 2)):
-        setattr(p, name, _arg(t, name, dev, torch.uint8, shape[:3] + (width,)))
-    p.batch, p.max_pages = page_table.shape
-    p.page_table = _arg(page_table, "page_table", dev, torch.int32, page_table.shape)
-    p.kv_len = _arg(kv_len, "kv_len", dev, torch.int32, (p.batch,))
-    p.row_start = _arg(row_start, "row_start", dev, torch.int32, (p.batch + 1,))
-    p.n_rows, p.heads, p.head_dim, p.dtype = n_rows, heads, head_dim, dtype
-    p.status = _arg(status, "status", dev, torch.int32, (1,))
-    p.stream = _stream(stream)
-    return p
+    if rows.dim() != 3:
+        raise ValueError("rows must be [n_rows, heads, head_dim]")
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        raise ValueError("page_table must be an int32 tensor [batch, max_pages]")
+    u8, i32, dtype = torch.uint8, torch.int32, rows.dtype
+    n_pages, kv_heads, page, _ = codes = k_codes.shape
+    scales = (n_pages, kv_heads, page, 2)
+    batch, max_pages = page_table.shape
+    n_rows, heads, head_dim = rows.shape
+    pq = pk = pv = None
+    q_row = q_head = kv_row = kv_head = axes = places = 0
+    if q is not None:
+        pq, q_row, q_head = _rows_arg(q, "q", index, dtype, (n_rows, heads, head_dim))
+    if k is not None:
+        pk, pv, kv_row, kv_head = _kv_arg(k, v, index, dtype, (n_rows, kv_heads, head_dim))
+    if cos is not None:
+        if cos.dim() != 2 or cos.shape[1] not in (16, 32):
+            raise ValueError("cos and sin must be [n_positions, 32], or [n_positions, 16] for two axes")
+        axes, places = 32 // cos.shape[1], cos.shape[0]
+        if positions is not None and axes == 1 and positions.dim() == 1:
+            positions = positions[:, None]
+    elif sin is not None or positions is not None:
+        raise ValueError("sin and positions need cos")
+    f32 = torch.float32
+    return s3r_cache_params(
+        _arg(k_codes, "k_codes", index, u8, codes), _arg(v_codes, "v_codes", index, u8, codes),
+        _arg(k_scales, "k_scales", index, u8, scales), _arg(v_scales, "v_scales", index, u8, scales),
+        _arg(page_table, "page_table", index, i32, page_table.shape), _arg(kv_len, "kv_len", index, i32, (batch,)),
+        _arg(row_start, "row_start", index, i32, (batch + 1,)), n_pages, n_rows, page, max_pages, batch, heads, kv_heads, head_dim,
+        _dtype_code(rows), pq, _arg(out, "out", index, dtype, (n_rows, heads, head_dim)), pk, pv, q_row, q_head, kv_row, kv_head,
+        _arg(cos, "cos", index, f32, (places, 32 // max(axes, 1))), _arg(sin, "sin", index, f32, (places, 32 // max(axes, 1))),
+        _arg(positions, "positions", index, i32, (n_rows, axes)), places, axes, int(pairs == "neighbours"), causal, softmax_scale,
+        _arg(lse, "lse", index, f32, (heads, n_rows)), _arg(status, "status", index, i32, (1,)), None, 0, _stream_of(stream, index))
 
 
 def speed3r_cache_append(cache, k, v, page_table, kv_len, row_start=None, *, q=None, q_out=None, cos=None, sin=None,
@@ -502,43 +531,19 @@ def speed3r_cache_append(cache, k, v, page_table, kv_len, row_start=None, *, q=N
     counts them.  page_table: int32 [batch, max_pages]; row_start: int32 [batch + 1] (None: one sequence).
     cos, sin: fp32 [n_positions, 32] rotate k by positions int32 [n_rows] (None: token numbers); of width 16 they rotate by
     two positions, int32 [n_rows, 2].  pairs: "halves" or "neighbours".  q [n_rows, heads, 64] is rotated into q_out."""
-    with _on(cache.k_codes.device):
-        dev, like = cache.k_codes.device, k if q is None else q
-        if pairs not in ("halves", "neighbours"):
-            raise ValueError('pairs must be "halves" or "neighbours"')
-        if k.dim() != 3 or like.dim() != 3:
-            raise ValueError("k, v must be [n_rows, kv_heads, head_dim], q [n_rows, heads, head_dim]")
-        p = _cache_params(cache, k.shape[0], like.shape[1], k.shape[2], _dtype_code(k), page_table, kv_len, row_start, status, stream)
-        (p.k, p.v), (p.kv_stride_tok, p.kv_stride_head) = _rows_arg((k, v), ("k", "v"), dev, k.dtype, (k.shape[0], p.kv_heads, k.shape[2]))
-        if q is not None:
-            shape = (k.shape[0], q.shape[1], k.shape[2])
-            (p.q,), (p.q_stride_tok, p.q_stride_head) = _rows_arg((q,), ("q",), dev, k.dtype, shape)
-            p.out = _arg(q_out, "q_out", dev, k.dtype, shape)
-        elif q_out is not None:
-            raise ValueError("q_out is given without q")
-        if cos is not None:
-            if cos.dim() != 2 or cos.shape[1] not in (16, 32):
-                raise ValueError("cos and sin must be [n_positions, 32], or [n_positions, 16] for two axes")
-            p.rot_axes, p.n_positions, p.rot_neighbours = 32 // cos.shape[1], cos.shape[0], int(pairs == "neighbours")
-            if positions is not None:
-                shape = (k.shape[0],) if p.rot_axes == 1 and positions.dim() == 1 else (k.shape[0], p.rot_axes)
-                p.positions = _arg(positions, "positions", dev, torch.int32, shape)
-            p.cos = _arg(cos, "cos", dev, torch.float32, cos.shape)
-            p.sin = _arg(sin, "sin", dev, torch.float32, cos.shape)
-        elif sin is not None or positions is not None:
-            raise ValueError("sin and positions need cos")
-        _check(load().speed3r_cache_append(ctypes.byref(p)))
+    index, lib = _gpu(cache[0], "the cache"), load()
+    if pairs != "halves" and pairs != "neighbours":
+        raise ValueError('pairs must be "halves" or "neighbours"')
+    p = _cache_params(cache, k if q is None else q, page_table, kv_len, row_start, status, stream, index, q=q, out=q_out, k=k, v=v,
+                      cos=cos, sin=sin, positions=positions, pairs=pairs)
+    _call(lib.speed3r_cache_append, p, 0, None, index)
 
 
 def speed3r_cache_read(cache, k, v, page_table, kv_len, row_start=None, *, status=None, stream=None):
     """The last tokens of the sequences, as many as k, v [n_rows, kv_heads, 64] have rows for them, as values into k and v."""
-    with _on(cache.k_codes.device):
-        if k.dim() != 3:
-            raise ValueError("k, v must be [n_rows, kv_heads, head_dim]")
-        p = _cache_params(cache, k.shape[0], k.shape[1], k.shape[2], _dtype_code(k), page_table, kv_len, row_start, status, stream)
-        (p.k, p.v), (p.kv_stride_tok, p.kv_stride_head) = _rows_arg((k, v), ("k", "v"), cache.k_codes.device, k.dtype,
-                                                                    (k.shape[0], p.kv_heads, k.shape[2]))
-        _check(load().speed3r_cache_read(ctypes.byref(p)))
+    index, lib = _gpu(cache[0], "the cache"), load()
+    p = _cache_params(cache, k, page_table, kv_len, row_start, status, stream, index, k=k, v=v)
+    _call(lib.speed3r_cache_read, p, 0, None, index)
 
 
 def speed3r_cache_workspace_bytes(cache, n_rows, heads, dtype, batch, max_pages) -> int:
@@ -547,7 +552,7 @@ def speed3r_cache_workspace_bytes(cache, n_rows, heads, dtype, batch, max_pages)
     p.n_pages, p.kv_heads, p.page, _ = cache.k_codes.shape
     p.n_rows, p.heads, p.head_dim, p.dtype, p.batch, p.max_pages = n_rows, heads, HEAD_DIM, dtype, batch, max_pages
     p.row_start = 4                                                  # only whether it is given counts here
-    need = int(load().speed3r_cache_workspace_bytes(ctypes.byref(p)))
+    need = load().speed3r_cache_workspace_bytes(ctypes.byref(p))
     if need >= 1 << 62:
         raise Speed3rError(S3R_ERR_INVALID_ARG, speed3r_last_error())
     return need
@@ -558,20 +563,10 @@ def speed3r_cache_attn(cache, q, out, page_table, kv_len, row_start=None, *, cau
     """Attention of q [n_rows, heads, 64] (rotated already) over the cached tokens of their sequences into out.  The rows of a
     sequence are its last tokens; causal: each sees the tokens up to its own, otherwise all.  Returns the workspace used
     (None: none was needed)."""
-    with _on(cache.k_codes.device):
-        dev = cache.k_codes.device
-        if q.dim() != 3:
-            raise ValueError("q must be [n_rows, heads, head_dim]")
-        p = _cache_params(cache, q.shape[0], q.shape[1], q.shape[2], _dtype_code(q), page_table, kv_len, row_start, status, stream)
-        (p.q,), (p.q_stride_tok, p.q_stride_head) = _rows_arg((q,), ("q",), dev, q.dtype, q.shape)
-        p.out = _arg(out, "out", dev, q.dtype, q.shape)
-        p.lse = _arg(lse, "lse", dev, torch.float32, (q.shape[1], q.shape[0]))
-        p.causal, p.softmax_scale = int(bool(causal)), float(softmax_scale)
-        workspace = _workspace(workspace, int(load().speed3r_cache_workspace_bytes(ctypes.byref(p))), dev)
-        if workspace is not None:
-            p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel()
-        _check(load().speed3r_cache_attn(ctypes.byref(p)))
-        return workspace
+    index, lib = _gpu(cache[0], "the cache"), load()
+    p = _cache_params(cache, q, page_table, kv_len, row_start, status, stream, index, q=q, out=out, causal=int(bool(causal)),
+                      softmax_scale=softmax_scale, lse=lse)
+    return _call(lib.speed3r_cache_attn, p, lib.speed3r_cache_workspace_bytes(ctypes.byref(p)), workspace, index)
 
 
 def speed3r_probe_select_loads(q, k, v, idx, out, block, ring_stages=0, wg_per_cu=0, stream=None):

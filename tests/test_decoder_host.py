@@ -155,19 +155,24 @@ def test_binding_refuses_what_it_can_see(s3r):
     c, lists = s3r.PagedCache.empty(4, 2, 16, device="cpu"), torch.zeros((1, 4), dtype=torch.int32)
     with pytest.raises(TypeError, match="GPU"):
         s3r.speed3r_cache_attn(c, q, q.clone(), lists, lists[0, :1], stream=0)
-    m = torch.empty((4, 2, 64), dtype=torch.bfloat16, device="meta")
-    dev = m.device
+    m = torch.zeros((4, 2, 64), dtype=torch.bfloat16)                  # on the CPU: index -1, for the checks that need no GPU
     with pytest.raises(TypeError, match="contiguous"):
-        s3r._rows_arg((m.transpose(1, 2),), ("q",), dev, m.dtype, (4, 64, 2))
+        s3r._rows_arg(m.transpose(1, 2), "q", -1, m.dtype, (4, 64, 2))
     with pytest.raises(TypeError, match="broadcast"):
-        s3r._rows_arg((m[:1].expand(4, 2, 64),), ("q",), dev, m.dtype, (4, 2, 64))
+        s3r._rows_arg(m[:1].expand(4, 2, 64), "q", -1, m.dtype, (4, 2, 64))
     with pytest.raises(TypeError, match="share"):
-        s3r._rows_arg((m, torch.empty((4, 4, 64), dtype=m.dtype, device="meta")[:, ::2]), ("k", "v"), dev, m.dtype, (4, 2, 64))
+        s3r._kv_arg(m, torch.zeros((4, 4, 64), dtype=m.dtype)[:, ::2], -1, m.dtype, (4, 2, 64))
+    with pytest.raises(TypeError, match="GPU 0"):
+        s3r._rows_arg(m, "q", 0, m.dtype, (4, 2, 64))
     with pytest.raises(ValueError, match="shape"):
-        s3r._arg(m, "out", dev, m.dtype, (4, 3, 64))
+        s3r._arg(m, "out", -1, m.dtype, (4, 3, 64))
     with pytest.raises(TypeError, match="dtype"):
-        s3r._arg(m, "out", dev, torch.float32, (4, 2, 64))
-    assert s3r._rows_arg((m,), ("q",), dev, m.dtype, (4, 2, 64))[1] == (128, 64)
+        s3r._arg(m, "out", -1, torch.float32, (4, 2, 64))
+    with pytest.raises(TypeError, match="contiguous"):
+        s3r._arg(m[:, :1], "out", -1, m.dtype, (4, 1, 64))
+    assert s3r._rows_arg(m, "q", -1, m.dtype, (4, 2, 64))[1:] == (128, 64)
+    assert s3r._rows_arg(m[:, 1:], "q", -1, m.dtype, (4, 1, 64))[1:] == (128, 64)
+    assert s3r._arg(None, "lse", -1, torch.float32, (1,)) is None
 
 
 # ---- the 64-bit forms themselves ------------------------------------------------------------------------
