@@ -22,102 +22,152 @@ __device__ __forceinline__ float round_to_odd(double y)
     return __uint_as_float(bits);
 }
 
-template <typename T> __device__ __forceinline__ float rounded(double y)  // for storing as T
-{
-    if constexpr (sizeof(T) == 4) return static_cast<float>(y);
-    return round_to_odd(y);
-}
-
 // ---- append and read ----------------------------------------------------------------------------------
-// Eight lanes for a row of a head, eight channels each: 16 bytes of bf16 in, 4 bytes of codes out per lane.  Both are
-// bound by HBM; the products of the rotation are exact in 64 bits and their sum is rounded once, so that the codes are those of the exact
-// values (64-bit FMAs run at half the rate of 32-bit ones here and stay under the loads).
+// Bound by HBM: 256 bytes of bf16 for 68 in the cache, of every token and head.  A wave takes eight rows, eight lanes each with eight
+// channels, and a run of heads: what a row needs (its sequence, its place, the angles) is found once for them, and the 32 bytes of
+// codes of neighbouring tokens, which lie side by side in a page, are written together.  The products of the rotation are exact in 64
+// bits and their sum is rounded once, so that the codes are those of the exact values.
 
-// Channels 8 c .. 8 c + 7 of a row, turned by the angles of its positions; lane bits 0 .. 2 are c.
-__device__ __forceinline__ void rotate(const Rotation &rot, int64_t row, int token, int c, const float (&x)[8], double (&y)[8])
+// The rows of a wave and its heads: `octets` of rows, and for each heads h0 .. h1 - 1 of `heads`, `run` at a time.
+struct HeadRun { int64_t row; int h0, h1; };
+__device__ __forceinline__ bool head_run(int64_t rows, int heads, int run, HeadRun &r)
 {
-    const int pairs = 32 / rot.axes, axis = rot.axes == 2 ? c >> 2 : 0;
-    int64_t at = rot.positions != nullptr ? rot.positions[row * rot.axes + axis] : token;
-    at = at < 0 ? 0 : (at >= rot.places ? rot.places - 1 : at);
-    const int index = rot.neighbours ? (4 * c) % pairs : (8 * c) % pairs;
-    const float *cs = rot.cos + at * pairs + index, *sn = rot.sin + at * pairs + index;
-    if (rot.neighbours) {
-        const floatx4 co = *reinterpret_cast<const floatx4 *>(cs), si = *reinterpret_cast<const floatx4 *>(sn);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const double a = x[2 * j], b = x[2 * j + 1], co_j = co[j], si_j = si[j];
-            y[2 * j] = fma(a, co_j, -(b * si_j));
-            y[2 * j + 1] = fma(b, co_j, a * si_j);
-        }
-        return;
-    }
-    float co[8], si[8];
-    load8(cs, co);
-    load8(sn, si);
-    const int away = rot.axes == 2 ? 2 : 4;
-    const bool second = (c & away) != 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const double other = __shfl_xor(x[j], away, 64), turned = other * static_cast<double>(si[j]);
-        y[j] = fma(static_cast<double>(x[j]), static_cast<double>(co[j]), second ? turned : -turned);
-    }
+    const unsigned wave = blockIdx.x * 4u + (threadIdx.x >> 6), runs = (heads + run - 1) / run, octet = wave / runs;
+    r.row = static_cast<int64_t>(octet) * 8 + ((threadIdx.x & 63) >> 3);
+    r.h0 = static_cast<int>(wave - octet * runs) * run;
+    r.h1 = min(r.h0 + run, heads);
+    return static_cast<int64_t>(octet) * 8 < rows;
 }
 
-template <typename T> __global__ __launch_bounds__(256) void cache_append_kernel(CacheArgs a)
+// A row's token in its sequence and the place of head 0's 64 channels in the cache, in tokens; -1: none.
+__device__ __forceinline__ int64_t place(const CacheArgs &a, int64_t row, bool covered, int &token)
 {
-    const unsigned id = blockIdx.x * 256u + threadIdx.x, item = id >> 3;
-    const int c = id & 7, kv_heads = a.cache.kv_heads;
-    const unsigned items = 2 * kv_heads + (a.q != nullptr ? a.heads : 0);
-    const unsigned row = item / items;
-    if (row >= a.n_rows || !a.spans.covers(row)) return;
-    int which = static_cast<int>(item - row * items);
+    token = 0;
+    if (!covered) return -1;
     const int b = a.spans.find(row);
     int first, len;
     a.spans.of(b, first, len);
-    const int n = a.cache.length(b), token = n - len + static_cast<int>(row) - first;
-    float x[8];
-    if (which >= 2 * kv_heads) {  // a head of q
-        const int h = which - 2 * kv_heads;
-        load8(static_cast<const T *>(a.q) + row * a.q_row + h * a.q_head + 8 * c, x);
-        double y[8];
-        rotate(a.rot, row, token, c, x, y);
+    const int n = a.cache.length(b);
+    token = n - len + static_cast<int>(row) - first;
+    return token < 0 || token >= n ? -1 : a.cache.slot(b, token);
+}
+
+// Cosines and sines for channels 8 c .. 8 c + 7 of a row (halves: of the eight pairs they belong to; neighbours: of four), the sines with
+// the sign that the channel's own half takes.
+struct Angles {
+    float co[8], si[8];
+    __device__ __forceinline__ void load(const Rotation &rot, int64_t row, int token, int c)
+    {
+        const int pairs = 32 / rot.axes, axis = rot.axes == 2 ? c >> 2 : 0;
+        int64_t at = rot.positions != nullptr ? rot.positions[row * rot.axes + axis] : token;
+        at = at < 0 ? 0 : (at >= rot.places ? rot.places - 1 : at);
+        const int index = rot.neighbours ? (4 * c) % pairs : (8 * c) % pairs;
+        const float *cs = rot.cos + at * pairs + index, *sn = rot.sin + at * pairs + index;
+        if (rot.neighbours) {
+            const floatx4 x = *reinterpret_cast<const floatx4 *>(cs), y = *reinterpret_cast<const floatx4 *>(sn);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = rounded<T>(y[j]);
-        Io8<T>::store(static_cast<T *>(a.to.out) + (static_cast<int64_t>(row) * a.heads + h) * 64 + 8 * c, x);
-        return;
+            for (int j = 0; j < 8; ++j) { co[j] = x[j >> 1]; si[j] = (j & 1) != 0 ? y[j >> 1] : -y[j >> 1]; }
+        } else {
+            load8(cs, co);
+            load8(sn, si);
+            const bool second = (c & (rot.axes == 2 ? 2 : 4)) != 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) si[j] = second ? si[j] : -si[j];
+        }
     }
-    const bool is_v = which >= kv_heads;
-    if (is_v) which -= kv_heads;
-    load8(static_cast<const T *>(is_v ? a.v : a.k) + row * a.kv_row + which * a.kv_head + 8 * c, x);
-    if (!is_v && a.rot.cos != nullptr) {
-        double y[8];
-        rotate(a.rot, row, token, c, x, y);
+    // A channel a of a pair becomes a cos - b sin, its partner b cos + a sin: rounded to odd (the last bit is set where the value is not
+    // exact), so that rounding to fewer bits, or comparing with numbers of fewer bits, gives what the exact value would.  Only values whose
+    // lower bits are all the same as those of such a number can tell the difference: 15 zero bits, or 20 for the codes.
+    // odd = false: rounded to fp32, to be kept as that.
+    __device__ __forceinline__ void turn(const Rotation &rot, const float (&x)[8], float (&y)[8], bool odd) const
+    {
+        float other[8];
+        if (rot.neighbours) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = round_to_odd(y[j]);
+            for (int j = 0; j < 8; ++j) other[j] = x[j ^ 1];
+        } else {
+            const int away = rot.axes == 2 ? 2 : 4;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) other[j] = __shfl_xor(x[j], away, 64);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const double exact = fma(static_cast<double>(x[j]), static_cast<double>(co[j]), static_cast<double>(other[j]) * static_cast<double>(si[j]));
+            y[j] = static_cast<float>(exact);
+            if (odd && (__float_as_uint(y[j]) & 0x7fffu) == 0) y[j] = round_to_odd(exact);
+        }
     }
-    unsigned most = 0;  // magnitudes compare as integers; infinities and NaNs are the largest
+};
+
+// Heads whose rows are requested at once: 64 bytes of a lane.
+template <typename T> constexpr int kAhead = sizeof(T) == 4 ? 2 : 4;
+
+template <typename T> __global__ __launch_bounds__(256) void cache_append_kernel(CacheArgs a, int run)
+{
+    const int kv_heads = a.cache.kv_heads, turned = a.q != nullptr ? a.heads : 0;  // the heads in turn: q, k, v
+    HeadRun r;
+    if (!head_run(a.n_rows, turned + 2 * kv_heads, run, r)) return;
+    const int c = threadIdx.x & 7;
+    const bool covered = r.row < a.n_rows && a.spans.covers(r.row);
+    int token;
+    const int64_t slot = place(a, r.row, covered, token);
+    Angles angles;
+    const bool turns = a.rot.cos != nullptr;
+    if (turns && r.h0 < turned + kv_heads && covered) angles.load(a.rot, r.row, token, c);
+    for (int h0 = r.h0; h0 < r.h1; h0 += kAhead<T>) {
+        Io8<T> in[kAhead<T>];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);
-    most = max(most, static_cast<unsigned>(__shfl_xor(static_cast<int>(most), 1, 64)));
-    most = max(most, static_cast<unsigned>(__shfl_xor(static_cast<int>(most), 2, 64)));
-    int e = static_cast<int>(most >> 23) - 129 + ((most & 0x7fffffu) >= 0x600000u ? 1 : 0);
-    e = e < -100 ? -100 : (e > 125 ? 125 : e);
-    const bool none = most >= 0x7f800000u;
-    const unsigned scale = none ? 255u : static_cast<unsigned>(e + 127);
-    const float unit = __uint_as_float(static_cast<unsigned>(e + 127) << 23);
-    unsigned codes = 0;
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0], x[1], unit, 0);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2], x[3], unit, 1);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4], x[5], unit, 2);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6], x[7], unit, 3);
-    const unsigned second = static_cast<unsigned>(__shfl_xor(static_cast<int>(scale), 4, 64));
-    if (token < 0 || token >= n) return;
-    int64_t slot = a.cache.slot(b, token);
-    if (slot < 0) return;
-    slot += static_cast<int64_t>(which) << a.cache.page_shift;
-    uint8_t *to = is_v ? a.cache.v_codes : a.cache.k_codes, *scales = is_v ? a.cache.v_scales : a.cache.k_scales;
-    *reinterpret_cast<unsigned *>(to + slot * 32 + 4 * c) = none ? 0u : codes;
-    if (c == 0) *reinterpret_cast<unsigned short *>(scales + slot * 2) = static_cast<unsigned short>(scale | second << 8);
+        for (int i = 0; i < kAhead<T>; ++i) {
+            const int h = h0 + i;
+            if (h >= r.h1 || !covered) continue;
+            if (h < turned)
+                in[i].load(static_cast<const T *>(a.q) + r.row * a.q_row + h * a.q_head + 8 * c);
+            else if (h < turned + kv_heads)
+                in[i].load(static_cast<const T *>(a.k) + r.row * a.kv_row + (h - turned) * a.kv_head + 8 * c);
+            else
+                in[i].load(static_cast<const T *>(a.v) + r.row * a.kv_row + (h - turned - kv_heads) * a.kv_head + 8 * c);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead<T>; ++i) {
+            const int h = h0 + i;
+            if (h >= r.h1) continue;
+            float x[8], y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = in[i].get(j);
+            if (turns && h < turned + kv_heads) {
+                angles.turn(a.rot, x, y, sizeof(T) == 2 || h >= turned);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = x[j];
+            }
+            if (h < turned) {
+                if (covered) Io8<T>::store(static_cast<T *>(a.to.out) + (r.row * a.heads + h) * 64 + 8 * c, y);
+                continue;
+            }
+            const bool is_v = h >= turned + kv_heads;
+            unsigned most = 0;  // magnitudes compare as integers; infinities and NaNs are the largest
+#pragma unroll
+            for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(y[j]) & 0x7fffffffu);
+            most = max(most, static_cast<unsigned>(__shfl_xor(static_cast<int>(most), 1, 64)));
+            most = max(most, static_cast<unsigned>(__shfl_xor(static_cast<int>(most), 2, 64)));
+            int e = static_cast<int>(most >> 23) - 129 + ((most & 0x7fffffu) >= 0x600000u ? 1 : 0);
+            e = e < -100 ? -100 : (e > 125 ? 125 : e);
+            const bool none = most >= 0x7f800000u;
+            const unsigned scale = none ? 255u : static_cast<unsigned>(e + 127);
+            const float unit = __uint_as_float(static_cast<unsigned>(e + 127) << 23);
+            unsigned codes = 0;
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[0], y[1], unit, 0);
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[2], y[3], unit, 1);
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[4], y[5], unit, 2);
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[6], y[7], unit, 3);
+            const unsigned second = static_cast<unsigned>(__shfl_xor(static_cast<int>(scale), 4, 64));
+            if (slot < 0) continue;
+            const int64_t at = slot + (static_cast<int64_t>(h - turned - (is_v ? kv_heads : 0)) << a.cache.page_shift);
+            *reinterpret_cast<unsigned *>((is_v ? a.cache.v_codes : a.cache.k_codes) + at * 32 + 4 * c) = none ? 0u : codes;
+            if (c == 0)
+                *reinterpret_cast<unsigned short *>((is_v ? a.cache.v_scales : a.cache.k_scales) + at * 2) = static_cast<unsigned short>(scale | second << 8);
+        }
+    }
 }
 
 // Two codes at a time -> bf16, exactly; `scale`: the exponent byte.
@@ -129,34 +179,42 @@ __device__ __forceinline__ bf16x8 values8(unsigned codes, unsigned scale)
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-template <typename T> __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs a)
+template <typename T> __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs a, int run)
 {
-    const unsigned id = blockIdx.x * 256u + threadIdx.x, item = id >> 3;
-    const int c = id & 7, kv_heads = a.cache.kv_heads;
-    const unsigned row = item / (2 * kv_heads);
-    if (row >= a.n_rows || !a.spans.covers(row)) return;
-    int which = static_cast<int>(item - row * (2 * kv_heads));
-    const int b = a.spans.find(row);
-    int first, len;
-    a.spans.of(b, first, len);
-    const int n = a.cache.length(b), token = n - len + static_cast<int>(row) - first;
-    const bool is_v = which >= kv_heads;
-    if (is_v) which -= kv_heads;
-    int64_t slot = token < 0 || token >= n ? -1 : a.cache.slot(b, token);
-    bf16x8 x = {};
-    if (slot >= 0) {
-        slot += static_cast<int64_t>(which) << a.cache.page_shift;
-        const uint8_t *codes = is_v ? a.cache.v_codes : a.cache.k_codes, *scales = is_v ? a.cache.v_scales : a.cache.k_scales;
-        x = values8(*reinterpret_cast<const unsigned *>(codes + slot * 32 + 4 * c), scales[slot * 2 + (c >> 2)]);
-    }
-    T *to = static_cast<T *>(is_v ? a.v : a.k) + row * a.kv_row + which * a.kv_head + 8 * c;
-    if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<bf16x8 *>(to) = x;
-    } else {
-        float f[8];
+    const int kv_heads = a.cache.kv_heads;  // the heads in turn: k, v
+    HeadRun r;
+    if (!head_run(a.n_rows, 2 * kv_heads, run, r)) return;
+    if (r.row >= a.n_rows || !a.spans.covers(r.row)) return;
+    const int c = threadIdx.x & 7;
+    int token;
+    const int64_t slot = place(a, r.row, true, token);
+    for (int h0 = r.h0; h0 < r.h1; h0 += 4) {
+        unsigned codes[4], scale[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = static_cast<float>(x[j]);
-        Io8<T>::store(to, f);
+        for (int i = 0; i < 4; ++i) {
+            const int h = h0 + i;
+            if (h >= r.h1 || slot < 0) continue;
+            const bool is_v = h >= kv_heads;
+            const int64_t at = slot + (static_cast<int64_t>(h - (is_v ? kv_heads : 0)) << a.cache.page_shift);
+            codes[i] = *reinterpret_cast<const unsigned *>((is_v ? a.cache.v_codes : a.cache.k_codes) + at * 32 + 4 * c);
+            scale[i] = (is_v ? a.cache.v_scales : a.cache.k_scales)[at * 2 + (c >> 2)];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int h = h0 + i;
+            if (h >= r.h1) continue;
+            bf16x8 x = {};
+            if (slot >= 0) x = values8(codes[i], scale[i]);
+            T *to = (h >= kv_heads ? static_cast<T *>(a.v) + (h - kv_heads) * a.kv_head : static_cast<T *>(a.k) + h * a.kv_head) + r.row * a.kv_row + 8 * c;
+            if constexpr (sizeof(T) == 2) {
+                *reinterpret_cast<bf16x8 *>(to) = x;
+            } else {
+                float f[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] = static_cast<float>(x[j]);
+                Io8<T>::store(to, f);
+            }
+        }
     }
 }
 
@@ -335,25 +393,39 @@ template <typename T> hipError_t launch_cache_attn_t(const CacheArgs &a, bool fe
 
 }  // namespace
 
+namespace {
+
+// Heads that a wave takes in a row: as many, up to 16, as leave the card 8192 waves (eight for each of 1024 SIMDs).
+int run_of_heads(int64_t rows, int heads)
+{
+    int run = 1;
+    while (run < 16 && (rows + 7) / 8 * ((heads + 2 * run - 1) / (2 * run)) >= 8192) run *= 2;
+    return run;
+}
+
+}  // namespace
+
 hipError_t launch_cache_append(const CacheArgs &a, bool is_bf16, hipStream_t stream)
 {
-    const int64_t items = a.n_rows * (2 * a.cache.kv_heads + (a.q != nullptr ? a.heads : 0)), blocks = (items * 8 + 255) / 256;
+    const int heads = 2 * a.cache.kv_heads + (a.q != nullptr ? a.heads : 0), run = run_of_heads(a.n_rows, heads);
+    const int64_t blocks = ((a.n_rows + 7) / 8 * ((heads + run - 1) / run) + 3) / 4;
     if (!grid_ok(blocks)) return hipErrorInvalidValue;
     if (is_bf16)
-        hipLaunchKernelGGL(cache_append_kernel<bf16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL(cache_append_kernel<bf16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a, run);
     else
-        hipLaunchKernelGGL(cache_append_kernel<float>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL(cache_append_kernel<float>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a, run);
     return hipGetLastError();
 }
 
 hipError_t launch_cache_read(const CacheArgs &a, bool is_bf16, hipStream_t stream)
 {
-    const int64_t blocks = (a.n_rows * 2 * a.cache.kv_heads * 8 + 255) / 256;
+    const int heads = 2 * a.cache.kv_heads, run = run_of_heads(a.n_rows, heads);
+    const int64_t blocks = ((a.n_rows + 7) / 8 * ((heads + run - 1) / run) + 3) / 4;
     if (!grid_ok(blocks)) return hipErrorInvalidValue;
     if (is_bf16)
-        hipLaunchKernelGGL(cache_read_kernel<bf16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL(cache_read_kernel<bf16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a, run);
     else
-        hipLaunchKernelGGL(cache_read_kernel<float>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL(cache_read_kernel<float>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a, run);
     return hipGetLastError();
 }
 
