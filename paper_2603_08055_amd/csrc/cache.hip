@@ -220,135 +220,181 @@ template <typename T> __global__ __launch_bounds__(256) void cache_read_kernel(C
 
 // ---- attention -------------------------------------------------------------------------------------------
 
-// Units of 64 cached tokens: a lane has one token; of the four pieces of a unit (keys, values; 32 channels each) a thread brings one
-// (256 threads) or all (64).  In LDS they are bf16, which holds the values exactly.  Blocks of values that read as NaN are put as zeros and
-// told apart by a word per 32 channels, because only rows that see their token may become NaN.
+// Units of 64 cached tokens, a token for a lane.  In LDS they are bf16, which holds the values exactly.  Blocks of values that read as
+// NaN are put as zeros and told apart by a word per 32 channels, because only rows that see their token may become NaN.
 constexpr int kCacheStage = 2 * kPlane + 32;  // bf16 elements: keys, values, two 64-bit words and room to stay aligned
 
-template <int THREADS> struct PageUnits {
-    static constexpr int kPieces = 256 / THREADS;
+struct PageUnits {
     Cache cache;
     int seq, kv_head, len;
-    int64_t next;  // slot of the lane's token of the unit to be fetched next
-    uint4 codes[kPieces];
-    unsigned scale[kPieces];
-    bool there;
-
+    int64_t next;  // where the lane's token of the unit to be fetched next is; -1: nowhere
     __device__ __forceinline__ void find(int unit, int lane)
     {
         const int t = unit * kUnitRows + lane;
         next = t < len ? cache.slot(seq, t) : -1;
     }
-    __device__ __forceinline__ void fetch(int t, int lane)
+    __device__ __forceinline__ int64_t head_slot() const { return next + (static_cast<int64_t>(kv_head) << cache.page_shift); }
+};
+
+// 32 channels of a lane's token, as bf16 to a unit in LDS; not `ok`: zeros.
+__device__ __forceinline__ void put_block(bf16_t *unit, int row, int half, uint4 codes, unsigned scale, bool ok)
+{
+    if (!ok) { codes = uint4{0, 0, 0, 0}; scale = 127; }
+    *reinterpret_cast<bf16x8 *>(unit + unit_chunk(row, 4 * half + 0)) = values8(codes.x, scale);
+    *reinterpret_cast<bf16x8 *>(unit + unit_chunk(row, 4 * half + 1)) = values8(codes.y, scale);
+    *reinterpret_cast<bf16x8 *>(unit + unit_chunk(row, 4 * half + 2)) = values8(codes.z, scale);
+    *reinterpret_cast<bf16x8 *>(unit + unit_chunk(row, 4 * half + 3)) = values8(codes.w, scale);
+}
+
+// What a workgroup's rows of a sequence see.
+struct Sight {
+    int first, rows, len, sees, most;  // sees: tokens that the lane's row sees; most: that the last row of the tile sees
+    int64_t row;
+    int head;
+    bool ok;
+    __device__ __forceinline__ void find(const CacheArgs &a, const Share &sh, int tile, int item_in_tile)
     {
-        there = next >= 0;
-        if (!there) return;
-        const int64_t slot = next + (static_cast<int64_t>(kv_head) << cache.page_shift);
-#pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
-            const int id = THREADS == 256 ? t >> 6 : p, half = id & 1;
-            codes[p] = *reinterpret_cast<const uint4 *>((id >= 2 ? cache.v_codes : cache.k_codes) + slot * 32 + 16 * half);
-            scale[p] = ((id >= 2 ? cache.v_scales : cache.k_scales) + slot * 2)[half];
+        a.spans.of(sh.seq, first, rows);
+        len = a.cache.length(sh.seq);
+        const int64_t items = static_cast<int64_t>(rows) * a.per_row, item0 = static_cast<int64_t>(sh.tile) * tile, item = item0 + item_in_tile;
+        ok = item < items;
+        const int in_seq = static_cast<int>(item / a.per_row);
+        row = first + in_seq;
+        head = sh.kv_head * a.per_row + static_cast<int>(item - static_cast<int64_t>(in_seq) * a.per_row);
+        sees = most = len;
+        if (a.causal) {
+            sees = min(len, len - rows + in_seq + 1);
+            const int64_t last = (item0 + tile < items ? item0 + tile : items) - 1;
+            most = max(0, min(len, len - rows + static_cast<int>(last / a.per_row) + 1));
+            if (!ok) sees = most;
         }
-    }
-    __device__ __forceinline__ unsigned long long put(bf16_t *lds, int t, int lane)
-    {
-        unsigned long long *words = reinterpret_cast<unsigned long long *>(lds + 2 * kPlane);
-#pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
-            const int id = THREADS == 256 ? t >> 6 : p, half = id & 1;
-            uint4 x = codes[p];
-            unsigned s = scale[p];
-            const bool none = id >= 2 && there && s == 255u;
-            if (id >= 2) {
-                const unsigned long long w = __ballot(none);
-                if (lane == 0) words[half] = w;
-            }
-            if (!there || none) { x = uint4{0, 0, 0, 0}; s = 127; }
-            bf16_t *to = lds + (id >= 2 ? kPlane : 0);
-            *reinterpret_cast<bf16x8 *>(to + unit_chunk(lane, 4 * half + 0)) = values8(x.x, s);
-            *reinterpret_cast<bf16x8 *>(to + unit_chunk(lane, 4 * half + 1)) = values8(x.y, s);
-            *reinterpret_cast<bf16x8 *>(to + unit_chunk(lane, 4 * half + 2)) = values8(x.z, s);
-            *reinterpret_cast<bf16x8 *>(to + unit_chunk(lane, 4 * half + 3)) = values8(x.w, s);
-        }
-        return __ballot(there);
     }
 };
 
-template <int PQ>
-__device__ __forceinline__ void cache_unit(SoftRow<PQ> &soft, const bf16_t *lds, unsigned long long seen, float factor, int lane)
+// Many rows: four waves hold 32 rows each and share every unit; a wave brings 32 channels of its keys (waves 0, 1) or values (2, 3).
+template <typename T> __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a)
 {
-    soft.template unit<1>(lds, lds + kPlane, seen, factor, lane);
-    const unsigned long long *words = reinterpret_cast<const unsigned long long *>(lds + 2 * kPlane);
-#pragma unroll
-    for (int dt = 0; dt < 2; ++dt) {
-        const unsigned long long none = words[dt];
-        if (none != 0 && (none & seen) != 0)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) soft.o[dt][r] = NAN;
-    }
-}
-
-template <typename T, bool WIDE> __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheArgs a)
-{
-    constexpr int P = sizeof(T) == 4 ? 3 : 1, kRows = WIDE ? 32 : 128;
+    constexpr int P = sizeof(T) == 4 ? 3 : 1;
     extern __shared__ __align__(16) unsigned char smem[];
     bf16_t *lds = reinterpret_cast<bf16_t *>(smem);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = wave & 1;
+    const bool is_v = wave >= 2;
     Share sh;
-    if (!find_share(a.spans, a.per_row, kRows, a.tiles, a.n_split, a.cache.kv_heads, sh)) return;
-    int first, rows;
-    a.spans.of(sh.seq, first, rows);
-    const int len = a.cache.length(sh.seq);
-    const int64_t items = static_cast<int64_t>(rows) * a.per_row, item0 = static_cast<int64_t>(sh.tile) * kRows;
-    const int64_t item = item0 + (WIDE ? 0 : 32 * wave) + (lane & 31);
-    const bool ok = item < items;
-    const int in_seq = static_cast<int>(item / a.per_row);
-    const int64_t row = first + in_seq;
-    const int head = sh.kv_head * a.per_row + static_cast<int>(item - static_cast<int64_t>(in_seq) * a.per_row);
+    if (!find_share(a.spans, a.per_row, 128, a.tiles, a.n_split, a.cache.kv_heads, sh)) return;
+    Sight sight;
+    sight.find(a, sh, 128, 32 * wave + (lane & 31));
     SoftRow<P> soft;
     soft.clear();
-    soft.load(static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head, ok, lane);
-
-    // tokens that the lane's row sees, and the last row of the tile
-    int sees = len, most = len;
-    if (a.causal) {
-        sees = min(len, len - rows + in_seq + 1);
-        const int64_t last = (item0 + kRows < items ? item0 + kRows : items) - 1;
-        most = max(0, min(len, len - rows + static_cast<int>(last / a.per_row) + 1));
-        if (!ok) sees = most;
-    }
+    soft.load(static_cast<const T *>(a.q) + sight.row * a.q_row + sight.head * a.q_head, sight.ok, lane);
     int u0, u1;
-    piece((most + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
-    if constexpr (WIDE) {
-        PageUnits<64> units;
-        units.cache = a.cache; units.seq = sh.seq; units.kv_head = sh.kv_head; units.len = len;
-        bf16_t *mine = lds + wave * kCacheStage;
-        int u = u0 + wave;
-        if (u < u1) { units.find(u, lane); units.fetch(lane, lane); units.find(u + 4, lane); }
-        for (; u < u1; u += 4) {
-            const unsigned long long seen = units.put(mine, lane, lane) & low_bits(sees - u * kUnitRows);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            if (u + 4 < u1) { units.fetch(lane, lane); units.find(u + 8, lane); }
-            cache_unit(soft, mine, seen, a.factor, lane);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        }
+    piece((sight.most + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
+    PageUnits units{a.cache, sh.seq, sh.kv_head, sight.len, -1};
+    const uint8_t *codes = is_v ? a.cache.v_codes : a.cache.k_codes, *scales = is_v ? a.cache.v_scales : a.cache.k_scales;
+    uint4 code = {};
+    unsigned scale = 0;
+    bool there = false;
+    auto fetch = [&]() {
+        there = units.next >= 0;
+        if (!there) return;
+        code = *reinterpret_cast<const uint4 *>(codes + units.head_slot() * 32 + 16 * half);
+        scale = scales[units.head_slot() * 2 + half];
+    };
+    if (u0 < u1) { units.find(u0, lane); fetch(); units.find(u0 + 1, lane); }
+    for (int u = u0; u < u1; ++u) {
+        bf16_t *stage = lds + ((u - u0) & 1) * kCacheStage;
+        unsigned long long *words = reinterpret_cast<unsigned long long *>(stage + 2 * kPlane);
+        const bool none = is_v && there && scale == 255u;
+        put_block(stage + (is_v ? kPlane : 0), lane, half, code, scale, there && !none);
+        const unsigned long long w = __ballot(none);
+        if (is_v && lane == 0) words[half] = w;
+        const unsigned long long seen = __ballot(there) & low_bits(sight.sees - u * kUnitRows);
         __syncthreads();
-        join_waves<4>(soft, a.factor, reinterpret_cast<float *>(smem), wave, lane);
-        if (wave == 0) store_soft<T>(soft, a.factor, a.to, sh.split, row, head, ok, lane);
-    } else {
-        PageUnits<256> units;
-        units.cache = a.cache; units.seq = sh.seq; units.kv_head = sh.kv_head; units.len = len;
-        if (u0 < u1) { units.find(u0, lane); units.fetch(threadIdx.x, lane); units.find(u0 + 1, lane); }
-        for (int u = u0; u < u1; ++u) {
-            bf16_t *stage = lds + ((u - u0) & 1) * kCacheStage;
-            const unsigned long long seen = units.put(stage, threadIdx.x, lane) & low_bits(sees - u * kUnitRows);
-            __syncthreads();
-            if (u + 1 < u1) { units.fetch(threadIdx.x, lane); units.find(u + 2, lane); }
-            cache_unit(soft, stage, seen, a.factor, lane);
+        if (u + 1 < u1) { fetch(); units.find(u + 2, lane); }
+        soft.template unit<1>(stage, stage + kPlane, seen, a.factor, lane);
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt) {
+            const unsigned long long nan = words[dt];
+            if (nan != 0 && (nan & seen) != 0)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) soft.o[dt][r] = NAN;
         }
-        store_soft<T>(soft, a.factor, a.to, sh.split, row, head, ok, lane);
     }
+    store_soft<T>(soft, a.factor, a.to, sh.split, sight.row, sight.head, sight.ok, lane);
+}
+
+__device__ __forceinline__ int64_t lane_value(int64_t x, int lane)
+{
+    const unsigned lo = __builtin_amdgcn_readlane(static_cast<unsigned>(x), lane), hi = __builtin_amdgcn_readlane(static_cast<unsigned>(x >> 32), lane);
+    return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+
+// Few rows: WAVES waves with the same 16 rows take the units in turn.  Sixteen tokens of a unit lie on one page, so that a tile of keys
+// has one address for the wave.
+template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, 2) void cache_few_kernel(CacheArgs a)
+{
+    constexpr int P = sizeof(T) == 4 ? 3 : 1;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    bf16_t *mine = reinterpret_cast<bf16_t *>(smem) + wave * kPlane;
+    Share sh;
+    if (!find_share(a.spans, a.per_row, kFewRows, a.tiles, a.n_split, a.cache.kv_heads, sh)) return;
+    Sight sight;
+    sight.find(a, sh, kFewRows, lane & 15);
+    FewRows<P> few;
+    few.clear();
+    few.load(static_cast<const T *>(a.q) + sight.row * a.q_row + sight.head * a.q_head, sight.ok, lane);
+    int u0, u1;
+    piece((sight.most + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
+    PageUnits units{a.cache, sh.seq, sh.kv_head, sight.len, -1};
+    uint2 k[4] = {};
+    uint4 v[2] = {};
+    unsigned ks[4] = {}, vs = 0;
+    bool there = false;
+    auto fetch = [&]() {
+        there = units.next >= 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {  // a tile that is nowhere reads the first page instead, and counts for nothing
+            int64_t slot = lane_value(units.next, 16 * t);
+            slot = (slot < 0 ? 0 : slot) + (static_cast<int64_t>(sh.kv_head) << a.cache.page_shift);
+            k[t] = *reinterpret_cast<const uint2 *>(a.cache.k_codes + slot * 32 + ((lane & 15) * 32 + (lane >> 4) * 8));
+            ks[t] = (a.cache.k_scales + slot * 2)[(lane & 15) * 2 + (lane >> 5)];
+        }
+        if (!there) return;
+        const uint8_t *codes = a.cache.v_codes + units.head_slot() * 32;
+        v[0] = *reinterpret_cast<const uint4 *>(codes);
+        v[1] = *reinterpret_cast<const uint4 *>(codes + 16);
+        vs = *reinterpret_cast<const unsigned short *>(a.cache.v_scales + units.head_slot() * 2);
+    };
+    int u = u0 + wave;
+    if (u < u1) { units.find(u, lane); fetch(); units.find(u + WAVES, lane); }
+    for (; u < u1; u += WAVES) {
+        unsigned long long nan[2];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const unsigned scale = (vs >> (8 * half)) & 255u;
+            const bool none = there && scale == 255u;
+            put_block(mine, lane, half, v[half], scale, there && !none);
+            nan[half] = __ballot(none);
+        }
+        const unsigned long long seen = __ballot(there) & low_bits(sight.sees - u * kUnitRows);
+        bf16x8 kk[4][2];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            kk[t][0] = values8(k[t].x, ks[t]);
+            kk[t][1] = values8(k[t].y, ks[t]);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (u + WAVES < u1) { fetch(); units.find(u + 2 * WAVES, lane); }
+        few.template unit<1>([&](int t, int s, bf16x8(&to)[1]) { to[0] = kk[t][s]; }, mine, seen, a.factor, lane);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+            if (nan[half] != 0 && (nan[half] & seen) != 0)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) few.o[2 * half][r] = few.o[2 * half + 1][r] = NAN;
+    }
+    __syncthreads();
+    store_few<T, WAVES>(few, a.factor, a.to, sh.split, sight.row, sight.head, sight.ok, reinterpret_cast<float *>(smem), wave, lane);
 }
 
 // ---- faults of what a call was given ---------------------------------------------------------------------
@@ -380,20 +426,15 @@ template <typename T> hipError_t launch_cache_attn_t(const CacheArgs &a, bool fe
 {
     const int64_t n = xcd_padded(a.tiles * a.n_split * a.cache.kv_heads);
     if (!grid_ok(n)) return hipErrorInvalidValue;
-    constexpr size_t kStage = kCacheStage * sizeof(bf16_t);
     if (few_rows) {
-        const hipError_t e = allow_lds(&cache_attn_kernel<T, true>, 4 * kStage);
-        if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((cache_attn_kernel<T, true>), dim3(static_cast<unsigned>(n)), dim3(256), 4 * kStage, stream, a);
+        constexpr int kWaves = 4;
+        hipLaunchKernelGGL((cache_few_kernel<T, kWaves>), dim3(static_cast<unsigned>(n)), dim3(64 * kWaves), kWaves * kPlane * sizeof(bf16_t),
+                           stream, a);
     } else {
-        hipLaunchKernelGGL((cache_attn_kernel<T, false>), dim3(static_cast<unsigned>(n)), dim3(256), 2 * kStage, stream, a);
+        hipLaunchKernelGGL(cache_attn_kernel<T>, dim3(static_cast<unsigned>(n)), dim3(256), 2 * kCacheStage * sizeof(bf16_t), stream, a);
     }
     return hipGetLastError();
 }
-
-}  // namespace
-
-namespace {
 
 // Heads that a wave takes in a row: as many, up to 16, as leave the card 8192 waves (eight for each of 1024 SIMDs).
 int run_of_heads(int64_t rows, int heads)

@@ -12,82 +12,114 @@ namespace {
 
 constexpr int kTile = 128;  // held rows of a workgroup: 32 for each of four waves
 
-// LDS of a kernel that streams two tensors of `parts` planes: two stages where the operands are bf16 (32 KiB; one barrier per unit), one where
-// they are in three parts (48 KiB).
-template <typename T> struct Stages {
-    static constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
-    static constexpr int kCount = kParts == 1 ? 2 : 1;
-    static constexpr int kElems = 2 * kParts * kPlane;
-    static constexpr int kWideWaves = kParts == 1 ? 4 : 2;  // waves with an LDS stage each: 64 or 96 KiB
-};
-
-template <typename T, int THREADS>
-__device__ __forceinline__ RowUnits<T, THREADS> key_units(const CrossArgs &a, int kv_head, int first, int len)
+// Keys and values of a sequence, for a head of theirs.
+template <typename T>
+__device__ __forceinline__ UnitPairs<T> key_units(const CrossArgs &a, int kv_head, int first, int len, bf16_t *lds)
 {
-    RowUnits<T, THREADS> u;
-    u.a = static_cast<const T *>(a.k) + first * a.kv_row + kv_head * a.kv_head;
-    u.b = static_cast<const T *>(a.v) + first * a.kv_row + kv_head * a.kv_head;
-    u.a_row = u.b_row = a.kv_row;
-    u.a_head = u.b_head = 0;
-    u.mask = a.key_mask != nullptr ? a.key_mask + first : nullptr;
-    u.items = len;
-    u.per_row = 1;
-    return u;
+    const int64_t at = first * a.kv_row + kv_head * a.kv_head;
+    return UnitPairs<T>(static_cast<const T *>(a.k) + at, static_cast<const T *>(a.v) + at, len, a.kv_row, 0, a.kv_row, 0, 1, lds);
+}
+
+__device__ __forceinline__ CountedRows counted(const CrossArgs &a, int first, int len)
+{
+    return CountedRows{a.key_mask != nullptr ? a.key_mask + first : nullptr, len, 0};
 }
 
 // Many rows: four waves hold 32 rows each and share every unit.
-// Few rows (WIDE): the waves hold the same 32 rows and take the units in turn, each through an LDS stage of its own.
-template <typename T, bool WIDE> __global__ __launch_bounds__(256, WIDE && sizeof(T) == 4 ? 1 : 2) void cross_kernel(CrossArgs a)
+template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void cross_kernel(CrossArgs a)
 {
-    constexpr int P = Stages<T>::kParts;
-    constexpr int kStage = Stages<T>::kElems, kStages = Stages<T>::kCount, kWaves = Stages<T>::kWideWaves;
+    constexpr int P = UnitPairs<T>::kParts;
     extern __shared__ __align__(16) unsigned char smem[];
     bf16_t *lds = reinterpret_cast<bf16_t *>(smem);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Share sh;
-    if (!find_share(a.q_spans, a.per_row, WIDE ? 32 : kTile, a.tiles, a.n_split, a.kv_heads, sh)) return;
+    if (!find_share(a.q_spans, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, sh)) return;
     int q0, q_len, k0, k_len;
     a.q_spans.of(sh.seq, q0, q_len);
     a.kv_spans.of(sh.seq, k0, k_len);
-
-    const int64_t item = static_cast<int64_t>(sh.tile) * (WIDE ? 32 : kTile) + (WIDE ? 0 : 32 * wave) + (lane & 31);
+    const int64_t item = static_cast<int64_t>(sh.tile) * kTile + 32 * wave + (lane & 31);
     const bool ok = item < static_cast<int64_t>(q_len) * a.per_row;
     const int64_t row = q0 + item / a.per_row;
     const int head = sh.kv_head * a.per_row + static_cast<int>(item % a.per_row);
     SoftRow<P> soft;
     soft.clear();
     soft.load(static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head, ok, lane);
-
     int u0, u1;
     piece((k_len + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
-    if constexpr (WIDE) {
-        auto units = key_units<T, 64>(a, sh.kv_head, k0, k_len);
-        bf16_t *mine = lds + wave * kStage;
-        int u = u0 + wave;
-        if (u < u1) units.fetch(u, lane);
-        for (; u < u1; u += kWaves) {
-            const unsigned long long seen = units.put(mine, lane);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            if (u + kWaves < u1) units.fetch(u + kWaves, lane);
-            soft.template unit<P>(mine, mine + P * kPlane, seen, a.factor, lane);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        }
-        __syncthreads();
-        join_waves<kWaves>(soft, a.factor, reinterpret_cast<float *>(smem), wave, lane);
-        if (wave == 0) store_soft<T>(soft, a.factor, a.to, sh.split, row, head, ok, lane);
-    } else {
-        auto units = key_units<T, 256>(a, sh.kv_head, k0, k_len);
-        if (u0 < u1) units.fetch(u0, threadIdx.x);
-        for (int u = u0; u < u1; ++u) {
-            bf16_t *stage = lds + ((u - u0) % kStages) * kStage;
-            if (kStages == 1 && u > u0) __syncthreads();
-            const unsigned long long seen = units.put(stage, threadIdx.x);
-            __syncthreads();
-            if (u + 1 < u1) units.fetch(u + 1, threadIdx.x);
-            soft.template unit<P>(stage, stage + P * kPlane, seen, a.factor, lane);
-        }
-        store_soft<T>(soft, a.factor, a.to, sh.split, row, head, ok, lane);
+    auto units = key_units<T>(a, sh.kv_head, k0, k_len, lds);
+    auto rows = counted(a, k0, k_len);
+    unsigned long long seen = 0;
+    auto more = [&](int u) { rows.fetch(u, lane); };
+    units.begin(u0, u1, more);
+    for (int u = u0; u < u1; ++u) {
+        const bf16_t *k = units.step(u, u == u0, more, [&]() { return seen = rows.counts(); }, [](int) {});
+        soft.template unit<P>(k, k + P * kPlane, seen, a.factor, lane);
     }
+    store_soft<T>(soft, a.factor, a.to, sh.split, row, head, ok, lane);
+}
+
+// Few rows: WAVES waves with the same 16 rows take the units in turn, values through an LDS stage of their own (8 or 24 KiB).
+template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 ? 1 : 2) void cross_few_kernel(CrossArgs a)
+{
+    constexpr int P = UnitPairs<T>::kParts;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    bf16_t *mine = reinterpret_cast<bf16_t *>(smem) + wave * P * kPlane;
+    Share sh;
+    if (!find_share(a.q_spans, a.per_row, kFewRows, a.tiles, a.n_split, a.kv_heads, sh)) return;
+    int q0, q_len, k0, k_len;
+    a.q_spans.of(sh.seq, q0, q_len);
+    a.kv_spans.of(sh.seq, k0, k_len);
+    const int64_t item = static_cast<int64_t>(sh.tile) * kFewRows + (lane & 15);
+    const bool ok = item < static_cast<int64_t>(q_len) * a.per_row;
+    const int64_t row = q0 + item / a.per_row;
+    const int head = sh.kv_head * a.per_row + static_cast<int>(item % a.per_row);
+    FewRows<P> few;
+    few.clear();
+    few.load(static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head, ok, lane);
+    int u0, u1;
+    piece((k_len + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
+    const T *keys = static_cast<const T *>(a.k) + k0 * a.kv_row + sh.kv_head * a.kv_head + 16 * (lane >> 4);
+    RowUnits<T, 64> values(static_cast<const T *>(a.v) + k0 * a.kv_row + sh.kv_head * a.kv_head, k_len, a.kv_row, 0, 1, lane);
+    auto rows = counted(a, k0, k_len);
+    Io8<T> k[4][2];
+    auto fetch = [&](int u) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int r = u * kUnitRows + 16 * t + (lane & 15);
+            if (r < k_len) {
+                k[t][0].load(keys + r * a.kv_row);
+                k[t][1].load(keys + r * a.kv_row + 8);
+            }
+        }
+        values.fetch(u, lane);
+        rows.fetch(u, lane);
+    };
+    int u = u0 + wave;
+    if (u < u1) fetch(u);
+    for (; u < u1; u += WAVES) {
+        const unsigned long long seen = rows.counts();
+        values.put(mine, seen, lane);
+        bf16x8 kk[4][2][P];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                float x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = k[t][s].get(j);
+                split_parts<P>(x, kk[t][s]);
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (u + WAVES < u1) fetch(u + WAVES);
+        few.template unit<P>([&](int t, int s, bf16x8(&to)[P]) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) to[i] = kk[t][s][i];
+        }, mine, seen, a.factor, lane);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    __syncthreads();
+    store_few<T, WAVES>(few, a.factor, a.to, sh.split, row, head, ok, reinterpret_cast<float *>(smem), wave, lane);
 }
 
 // One result from the splits' normalised ones: weights 2^(lse_j - lse).  GROUPS x 16 threads for a row of a head: 16 take four
@@ -184,7 +216,7 @@ __device__ __forceinline__ float sum8(const bf16x8 &x)
 
 template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void grad_q_kernel(CrossArgs a)
 {
-    constexpr int P = Stages<T>::kParts, kStage = Stages<T>::kElems, kStages = Stages<T>::kCount;
+    constexpr int P = UnitPairs<T>::kParts;
     extern __shared__ __align__(16) unsigned char smem[];
     bf16_t *lds = reinterpret_cast<bf16_t *>(smem);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -207,14 +239,13 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     if (ok) { l2 = stats[0]; d = stats[1]; }
     int u0, u1;
     piece((k_len + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
-    auto units = key_units<T, 256>(a, sh.kv_head, k0, k_len);
-    if (u0 < u1) units.fetch(u0, threadIdx.x);
+    auto units = key_units<T>(a, sh.kv_head, k0, k_len, lds);
+    auto rows = counted(a, k0, k_len);
+    unsigned long long seen = 0;
+    auto more = [&](int u) { rows.fetch(u, lane); };
+    units.begin(u0, u1, more);
     for (int u = u0; u < u1; ++u) {
-        bf16_t *k = lds + ((u - u0) % kStages) * kStage, *v = k + P * kPlane;
-        if (kStages == 1 && u > u0) __syncthreads();
-        const unsigned long long seen = units.put(k, threadIdx.x);
-        __syncthreads();
-        if (u + 1 < u1) units.fetch(u + 1, threadIdx.x);
+        const bf16_t *k = units.step(u, u == u0, more, [&]() { return seen = rows.counts(); }, [](int) {}), *v = k + P * kPlane;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             floatx16 s = {}, dp = {};
@@ -223,22 +254,32 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
                 multiply<P>(s, held.q[i], [&](int part) { return unit_rows(k + part * kPlane, half, i, lane); });
                 multiply<P>(dp, grad.q[i], [&](int part) { return unit_rows(v + part * kPlane, half, i, lane); });
             }
-            const uint32_t bits = lane_bits(seen, half, lane);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[r] = fast_exp2(fmaf(s[r], a.factor, -l2));
+                dp[r] = s[r] * (dp[r] - d);
+            }
+            if (seen != ~0ull) {
+                const uint32_t out = left_out(seen, half, lane);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[r] = replace(s[r], 0.f, left_out_mask(out, r));
+                    dp[r] = replace(dp[r], 0.f, left_out_mask(out, r));
+                }
+            }
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
                 float x[8], y[8], sum = 0.f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const int r = 8 * w + j;
-                    const bool counts = lane_bit(bits, r);
-                    y[j] = counts ? fast_exp2(fmaf(s[r], a.factor, -l2)) : 0.f;
-                    x[j] = counts ? y[j] * (dp[r] - d) : 0.f;
+                    y[j] = s[8 * w + j];
+                    x[j] = dp[8 * w + j];
                     sum += x[j];
                 }
-                defect += sum;
                 bf16x8 ds[P], p[P];
                 split_parts<P>(x, ds);
                 if constexpr (kMendD<T>) {
+                    defect += sum;
                     split_parts<P>(y, p);
                     entered += sum8(ds[0]);
                 }
@@ -299,10 +340,10 @@ template <typename T> __global__ __launch_bounds__(256) void grad_q_combine_kern
 
 template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void grad_kv_kernel(CrossArgs a)
 {
-    constexpr int P = Stages<T>::kParts, kStage = Stages<T>::kElems, kStages = Stages<T>::kCount;
+    constexpr int P = UnitPairs<T>::kParts;
     extern __shared__ __align__(16) unsigned char smem[];
     bf16_t *lds = reinterpret_cast<bf16_t *>(smem);
-    float *row_stats = reinterpret_cast<float *>(smem + sizeof(bf16_t) * kStages * kStage);  // [stages][2][64]
+    float *row_stats = reinterpret_cast<float *>(smem + sizeof(bf16_t) * UnitPairs<T>::kStages * UnitPairs<T>::kStage);  // [stages][2][64]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Share sh;
     if (!find_share(a.kv_spans, 1, kTile, a.tiles, a.n_split, a.kv_heads, sh)) return;
@@ -319,19 +360,12 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     vv.load(static_cast<const T *>(a.v) + row * a.kv_row + sh.kv_head * a.kv_head, seen, lane);
 
     const int items = q_len * a.per_row, head0 = sh.kv_head * a.per_row;
-    RowUnits<T, 256> units;
-    units.a = static_cast<const T *>(a.q) + q0 * a.q_row + head0 * a.q_head;
-    units.a_row = a.q_row;
-    units.a_head = a.q_head;
-    units.b = static_cast<const T *>(a.d_out) + (static_cast<int64_t>(q0) * a.heads + head0) * 64;
-    units.b_row = static_cast<int64_t>(a.heads) * 64;
-    units.b_head = 64;
-    units.mask = nullptr;
-    units.items = items;
-    units.per_row = a.per_row;
+    UnitPairs<T, true> units(static_cast<const T *>(a.q) + q0 * a.q_row + head0 * a.q_head,
+                             static_cast<const T *>(a.d_out) + (static_cast<int64_t>(q0) * a.heads + head0) * 64, items, a.q_row, a.q_head,
+                             static_cast<int64_t>(a.heads) * 64, 64, a.per_row, lds);
     float st = 0.f;
     const int which = threadIdx.x >> 6;  // threads 0 .. 63 bring the rows' log-sums, 64 .. 127 their D
-    auto fetch_stats = [&](int u) {
+    auto more = [&](int u) {
         const int r = u * kUnitRows + lane;
         st = which == 0 ? INFINITY : 0.f;
         if (which < 2 && r < items) {
@@ -341,16 +375,14 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     };
     int u0, u1;
     piece((items + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
-    if (u0 < u1) { units.fetch(u0, threadIdx.x); fetch_stats(u0); }
+    units.begin(u0, u1, more);
+    const float *stats = row_stats;
     for (int u = u0; u < u1; ++u) {
-        const int n = (u - u0) % kStages;
-        bf16_t *q = lds + n * kStage, *g = q + P * kPlane;
-        float *stats = row_stats + n * 128;
-        if (kStages == 1 && u > u0) __syncthreads();
-        units.put(q, threadIdx.x);
-        if (which < 2) stats[which * 64 + lane] = st;
-        __syncthreads();
-        if (u + 1 < u1) { units.fetch(u + 1, threadIdx.x); fetch_stats(u + 1); }
+        const bf16_t *q = units.step(u, u == u0, more, [&]() { return low_bits(items - u * kUnitRows); }, [&](int stage) {
+            float *to = row_stats + stage * 128;
+            if (which < 2) to[which * 64 + lane] = st;
+            stats = to;
+        }), *g = q + P * kPlane;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             floatx16 s = {}, dp = {};
@@ -421,14 +453,15 @@ template <typename T> hipError_t launch_cross_t(const CrossArgs &a, bool few_row
 {
     const int64_t n = xcd_padded(a.tiles * a.n_split * a.kv_heads);
     if (!grid_ok(n)) return hipErrorInvalidValue;
-    constexpr size_t kStage = Stages<T>::kElems * sizeof(bf16_t);
     if (few_rows) {
-        const hipError_t e = allow_lds(&cross_kernel<T, true>, Stages<T>::kWideWaves * kStage);
+        constexpr int kWaves = 4;
+        constexpr size_t kLds = kWaves * UnitPairs<T>::kParts * kPlane * sizeof(bf16_t);
+        const hipError_t e = allow_lds(&cross_few_kernel<T, kWaves>, kLds);
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((cross_kernel<T, true>), dim3(static_cast<unsigned>(n)), dim3(64 * Stages<T>::kWideWaves),
-                           Stages<T>::kWideWaves * kStage, stream, a);
+        hipLaunchKernelGGL((cross_few_kernel<T, kWaves>), dim3(static_cast<unsigned>(n)), dim3(64 * kWaves), kLds, stream, a);
     } else {
-        hipLaunchKernelGGL((cross_kernel<T, false>), dim3(static_cast<unsigned>(n)), dim3(256), Stages<T>::kCount * kStage, stream, a);
+        constexpr size_t kLds = UnitPairs<T>::kStages * UnitPairs<T>::kStage * sizeof(bf16_t);
+        hipLaunchKernelGGL(cross_kernel<T>, dim3(static_cast<unsigned>(n)), dim3(256), kLds, stream, a);
     }
     return hipGetLastError();
 }
@@ -437,7 +470,7 @@ template <typename T> hipError_t launch_grad_t(const CrossArgs &a, bool of_keys,
 {
     const int64_t n = xcd_padded(a.tiles * a.n_split * a.kv_heads);
     if (!grid_ok(n)) return hipErrorInvalidValue;
-    const size_t lds = Stages<T>::kCount * (Stages<T>::kElems * sizeof(bf16_t) + (of_keys ? 128 * sizeof(float) : 0));
+    const size_t lds = UnitPairs<T>::kStages * (UnitPairs<T>::kStage * sizeof(bf16_t) + (of_keys ? 128 * sizeof(float) : 0));
     if (of_keys)
         hipLaunchKernelGGL(grad_kv_kernel<T>, dim3(static_cast<unsigned>(n)), dim3(256), lds, stream, a);
     else

@@ -294,7 +294,7 @@ struct CrossArgs {
     float *part_q, *part_pk, *part_defect, *part_k, *part_v;
 };
 
-// few_rows: a workgroup's waves divide the keys of 32 rows, and not 128 rows, among them.
+// few_rows: a workgroup's waves divide the keys of 16 rows, and not 128 rows, among them (tiles accordingly).
 hipError_t launch_cross(const CrossArgs &a, bool few_rows, bool is_bf16, hipStream_t stream);
 hipError_t launch_soft_combine(const SoftOut &to, const Spans &spans, int n_split, bool is_bf16, hipStream_t stream);
 // stats [heads][rows][2]: log-sum in log2 (+inf for a row without keys) and out . d_out

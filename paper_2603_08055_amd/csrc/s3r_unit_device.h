@@ -70,6 +70,18 @@ template <int PARTS> __device__ __forceinline__ void split_parts(const float (&x
     }
 }
 
+// The same for held rows.  A lower part of 0 would make NaN of an infinite key, whose score is -inf and counts for nothing: the
+// smallest normal number with the sign of x stands in, below every product's rounding.
+template <int PARTS> __device__ __forceinline__ void split_held(const float (&x)[8], bf16x8 (&p)[PARTS])
+{
+    split_parts<PARTS>(x, p);
+#pragma unroll
+    for (int i = 1; i < PARTS; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (static_cast<float>(p[i][j]) == 0.f && x[j] != 0.f) p[i][j] = static_cast<bf16_t>(copysignf(0x1p-126f, x[j]));
+}
+
 // acc += a b for an A operand that `fetch(part)` reads and a held operand of PB parts; A has PA.
 template <int PA, int PB, typename Fetch>
 __device__ __forceinline__ void multiply(floatx16 &acc, const bf16x8 (&b)[PB], Fetch &&fetch)
@@ -159,48 +171,44 @@ template <typename T> __device__ __forceinline__ void load8(const T *p, float (&
     for (int j = 0; j < 8; ++j) x[j] = v.get(j);
 }
 
-// Units of two tensors with the same rows (keys and values, or queries and output gradients), brought in by THREADS threads: item r of
-// a sequence is head r % per_row of its row r / per_row.  fetch() requests a unit's rows, put() writes them to LDS, with zeros in the
-// place of rows that do not count (behind the end, or masked: what stands there may be no number), and gives the 64 bits of those that do.
-template <typename T, int THREADS> struct RowUnits {
+// Units of one tensor, brought in by THREADS threads.  Item r of a sequence is its row r, or (GROUPED) head r % per_row of its row
+// r / per_row.  fetch() requests a unit's rows, put() writes them to LDS (`kParts` planes), with zeros in the place of rows that do not
+// count (behind the end, or masked: what stands there may be no number).
+template <typename T, int THREADS, bool GROUPED = false> struct RowUnits {
     static constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
     static constexpr int kChunks = 512 / THREADS;
-    const T *a, *b;                  // of item 0
-    int64_t a_row, a_head, b_row, b_head;
-    const uint8_t *mask;             // of row 0, or null
+    const T *base;  // item 0
+    int64_t row_stride, head_stride;
     int items, per_row;
-    Io8<T> ra[kChunks], rb[kChunks];
-    int seen;                        // of the lane's row of the unit
+    int64_t mine;   // of the thread's first chunk in a unit
+    Io8<T> r[kChunks];
 
+    __device__ __forceinline__ RowUnits(const T *base_, int items_, int64_t row_stride_, int64_t head_stride_, int per_row_, int t)
+        : base(base_), row_stride(row_stride_), head_stride(head_stride_), items(items_), per_row(per_row_), mine((t >> 3) * row_stride_ + (t & 7) * 8)
+    {
+    }
     __device__ __forceinline__ void fetch(int unit, int t)
     {
+        const T *from = base + unit * (kUnitRows * row_stride);
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
-            const int id = t + c * THREADS, r = unit * kUnitRows + (id >> 3);
-            if (r < items) {
-                const int row = per_row == 1 ? r : static_cast<int>(static_cast<unsigned>(r) / static_cast<unsigned>(per_row));
-                const int head = r - row * per_row;
-                ra[c].load(a + row * a_row + head * a_head + (id & 7) * 8);
-                rb[c].load(b + row * b_row + head * b_head + (id & 7) * 8);
+            const int id = t + c * THREADS, at = unit * kUnitRows + (id >> 3);
+            if (at >= items) continue;
+            if constexpr (GROUPED) {
+                const int row = static_cast<int>(static_cast<unsigned>(at) / static_cast<unsigned>(per_row));
+                r[c].load(base + row * row_stride + (at - row * per_row) * head_stride + (id & 7) * 8);
+            } else {
+                r[c].load(from + c * (THREADS / 8 * row_stride) + mine);
             }
         }
-        const int r = unit * kUnitRows + (t & 63);
-        seen = r < items;
-        if (mask != nullptr && seen) seen = mask[r];
     }
-    // lds: kParts planes of a, then kParts planes of b
-    __device__ __forceinline__ unsigned long long put(bf16_t *lds, int t)
+    __device__ __forceinline__ void put(bf16_t *lds, unsigned long long counts, int t) const
     {
-        const unsigned long long valid = __ballot(seen != 0);
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
             const int id = t + c * THREADS, row = id >> 3;
-            const bool ok = (valid >> row) & 1;
-            const int at = unit_chunk(row, id & 7);
-            put8(lds + at, ra[c], ok);
-            put8(lds + kParts * kPlane + at, rb[c], ok);
+            put8(lds + unit_chunk(row, id & 7), r[c], (counts >> row) & 1);
         }
-        return valid;
     }
     static __device__ __forceinline__ void put8(bf16_t *to, const Io8<T> &r, bool ok)
     {
@@ -220,14 +228,163 @@ template <typename T, int THREADS> struct RowUnits {
     }
 };
 
+// Which of a unit's 64 rows count, lane by lane: those before `items` that a mask (or null: all) does not leave out.
+struct CountedRows {
+    const uint8_t *mask;
+    int items, mine;
+    __device__ __forceinline__ void fetch(int unit, int lane)
+    {
+        const int r = unit * kUnitRows + lane;
+        mine = r < items;
+        if (mask != nullptr && mine) mine = mask[r];
+    }
+    __device__ __forceinline__ unsigned long long counts() const { return __ballot(mine != 0); }
+};
+
+// The same rows of a bf16 tensor brought to LDS without passing registers (256 threads): a wave requests two KiB of every unit, eight rows
+// each, lane by lane from where the chunk that belongs at its place of the unit lies.  Rows behind the end are the last one's, and made
+// zeros afterwards, as masked ones are (blank_rows): what stands there may be no number.
+template <bool GROUPED> struct DirectUnits {
+    const bf16_t *base;  // item 0
+    int64_t row_stride, head_stride;
+    int items, per_row;
+    unsigned off[2];     // bytes from the unit's first row; not GROUPED, and rows near enough for 32 bits
+    bool near;
+
+    __device__ __forceinline__ DirectUnits(const bf16_t *base_, int items_, int64_t row_stride_, int64_t head_stride_, int per_row_, int wave, int lane)
+        : base(base_), row_stride(row_stride_), head_stride(head_stride_), items(items_), per_row(per_row_)
+    {
+        near = row_stride < (int64_t(1) << 23);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) off[i] = 2 * (row_in_unit(wave, i, lane) * static_cast<unsigned>(row_stride) + 8 * chunk(wave, i, lane));
+    }
+    static __device__ __forceinline__ int row_in_unit(int wave, int i, int lane) { return 8 * (2 * wave + i) + (lane >> 3); }
+    static __device__ __forceinline__ int chunk(int wave, int i, int lane)
+    {
+        const int row = row_in_unit(wave, i, lane);
+        return (unit_chunk(row, lane & 7) - row * 64) >> 3;
+    }
+    // `lds`: byte address of the unit's place; wave and unit are the same for all lanes
+    __device__ __forceinline__ void request(int unit, unsigned lds, int wave, int lane) const
+    {
+        if (!GROUPED && near && (unit + 1) * kUnitRows <= items) {
+            const bf16_t *from = base + unit * (kUnitRows * row_stride);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) lds_dma_16_x1(from, off[i], lds + (2 * wave + i) * 1024);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = min(unit * kUnitRows + row_in_unit(wave, i, lane), items - 1);
+            const int row = GROUPED && per_row != 1 ? static_cast<int>(static_cast<unsigned>(at) / static_cast<unsigned>(per_row)) : at;
+            lds_dma_16(base + row * row_stride + (at - row * (GROUPED ? per_row : 1)) * head_stride + 8 * chunk(wave, i, lane), lds + (2 * wave + i) * 1024);
+        }
+    }
+};
+
+__device__ __forceinline__ void blank_rows(bf16_t *unit, unsigned long long counts, int t)
+{
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        const int id = t + c * 256;
+        if (((counts >> (id >> 3)) & 1) == 0) *reinterpret_cast<bf16x8 *>(unit + id * 8) = bf16x8{};
+    }
+}
+
+// Two tensors with the same rows, unit by unit, for 256 threads.  step(u) gives unit u's place in LDS, tensor a's planes and then b's, once
+// all of it is there, and sends for unit u + 1.
+//   bf16: straight to LDS, two stages, one barrier per unit (another where rows do not count);
+//   fp32: through registers, where values are cut into parts; one stage, two barriers.
+template <typename T, bool GROUPED = false> struct UnitPairs {
+    static constexpr int kParts = 3, kStages = 1, kStage = 2 * kParts * kPlane;  // bf16 elements
+    RowUnits<T, 256, GROUPED> a, b;
+    bf16_t *lds;
+    int end, t;
+    __device__ __forceinline__ UnitPairs(const T *a_, const T *b_, int items, int64_t a_row, int64_t a_head, int64_t b_row, int64_t b_head, int per_row,
+                                         bf16_t *lds_)
+        : a(a_, items, a_row, a_head, per_row, threadIdx.x), b(b_, items, b_row, b_head, per_row, threadIdx.x), lds(lds_), end(0), t(threadIdx.x)
+    {
+    }
+    template <typename More> __device__ __forceinline__ void begin(int u0, int u1, More &&more)
+    {
+        end = u1;
+        if (u0 < u1) { a.fetch(u0, t); b.fetch(u0, t); more(u0); }
+    }
+    // counts(): which of the unit's rows count, from what more(u) fetched; put(): what else goes to LDS for the unit
+    template <typename More, typename Counts, typename Put>
+    __device__ __forceinline__ bf16_t *step(int u, bool first, More &&more, Counts &&counts, Put &&put)
+    {
+        if (!first) __syncthreads();
+        const unsigned long long c = counts();
+        a.put(lds, c, t);
+        b.put(lds + kParts * kPlane, c, t);
+        put(0);
+        __syncthreads();
+        if (u + 1 < end) { a.fetch(u + 1, t); b.fetch(u + 1, t); more(u + 1); }
+        return lds;
+    }
+};
+
+template <bool GROUPED> struct UnitPairs<bf16_t, GROUPED> {
+    static constexpr int kParts = 1, kStages = 2, kStage = 2 * kPlane;
+    DirectUnits<GROUPED> a, b;
+    bf16_t *lds;
+    int end, wave, lane, stage;
+    __device__ __forceinline__ UnitPairs(const bf16_t *a_, const bf16_t *b_, int items, int64_t a_row, int64_t a_head, int64_t b_row, int64_t b_head,
+                                         int per_row, bf16_t *lds_)
+        : a(a_, items, a_row, a_head, per_row, threadIdx.x >> 6, threadIdx.x & 63),
+          b(b_, items, b_row, b_head, per_row, threadIdx.x >> 6, threadIdx.x & 63), lds(lds_), end(0),
+          wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63), stage(0)
+    {
+    }
+    __device__ __forceinline__ void send(int u, int to) const
+    {
+        const unsigned at = static_cast<unsigned>(reinterpret_cast<size_t>(lds)) + to * (kStage * 2);
+        a.request(u, at, wave, lane);
+        b.request(u, at + kPlane * 2, wave, lane);
+    }
+    template <typename More> __device__ __forceinline__ void begin(int u0, int u1, More &&more)
+    {
+        end = u1;
+        if (u0 < u1) { more(u0); send(u0, 0); }
+    }
+    template <typename More, typename Counts, typename Put>
+    __device__ __forceinline__ bf16_t *step(int u, bool first, More &&more, Counts &&counts, Put &&put)
+    {
+        wait_vmcnt<0>();
+        const unsigned long long c = counts();
+        bf16_t *here = lds + stage * kStage;
+        put(stage);
+        lds_barrier();
+        if (c != ~0ull) {
+            blank_rows(here, c, threadIdx.x);
+            blank_rows(here + kPlane, c, threadIdx.x);
+            lds_barrier();
+        }
+        stage ^= 1;
+        if (u + 1 < end) { more(u + 1); send(u + 1, stage); }
+        return here;
+    }
+};
+
 // ---- softmax over units -----------------------------------------------------------------------------------
 
-// Which of a half unit's 32 streamed rows a lane's 16 registers have, as bits 8 (r / 4) + r % 4.
-__device__ __forceinline__ uint32_t lane_bits(unsigned long long seen, int half, int lane)
+// Which of a half unit's 32 streamed rows, of those in a lane's 16 registers, do not count: bits 8 (r / 4) + r % 4.  Opaque to the
+// compiler, which would else make the masks of all registers ahead, for units that need none as well.
+__device__ __forceinline__ uint32_t left_out(unsigned long long seen, int half, int lane)
 {
-    return static_cast<uint32_t>(seen >> (32 * half)) >> (4 * (lane >> 5));
+    uint32_t bits = static_cast<uint32_t>(~seen >> (32 * half)) >> (4 * (lane >> 5));
+    asm volatile("" : "+v"(bits));
+    return bits;
 }
-__device__ __forceinline__ bool lane_bit(uint32_t bits, int r) { return (bits >> (8 * (r >> 2) + (r & 3))) & 1; }
+__device__ __forceinline__ uint32_t left_out_mask(uint32_t bits, int r)  // all ones: left out
+{
+    return static_cast<uint32_t>(__builtin_amdgcn_sbfe(static_cast<int>(bits), 8 * (r >> 2) + (r & 3), 1));
+}
+__device__ __forceinline__ float replace(float x, float by, uint32_t mask)  // bit by bit: x may be NaN
+{
+    return __uint_as_float((__float_as_uint(x) & ~mask) | (__float_as_uint(by) & mask));
+}
 
 // The lowest `n` of 64 bits.
 __device__ __forceinline__ unsigned long long low_bits(int n)
@@ -255,72 +412,87 @@ template <int PQ> struct SoftRow {
         for (int s = 0; s < 4; ++s) {
             float x[8] = {};
             if (ok) load8(row + 16 * s + 8 * (lane >> 5), x);
-            split_parts<PQ>(x, q[s]);
-            // A lower part of 0 would make NaN of an infinite key, whose score is -inf and counts for nothing: the smallest
-            // normal number with the sign of x stands in, below every product's rounding.
-            if constexpr (PQ == 3) {
-#pragma unroll
-                for (int i = 1; i < 3; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (static_cast<float>(q[s][i][j]) == 0.f && x[j] != 0.f) q[s][i][j] = static_cast<bf16_t>(copysignf(0x1p-126f, x[j]));
-            }
+            split_held<PQ>(x, q[s]);
         }
+        // they are waited for here: a wait in the loop would be one for the units on their way, too
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int i = 0; i < PQ; ++i) asm volatile("" : "+v"(q[s][i]));
     }
     // One unit of keys (PS planes) and values (PS planes); seen: the keys that count for the lane's row; factor: scale * log2(e).
+    // `top` need not be the largest score so far: it is raised only where a row's exponentials of a unit add up to more than 255, that is
+    // where one is above 2^8 times its like at `top`; the scores are then computed again.  That spares almost all units the search.
     template <int PS>
     __device__ __forceinline__ void unit(const bf16_t *k, const bf16_t *v, unsigned long long seen, float factor, int lane)
     {
+        const bool all = __all(seen == ~0ull);
         floatx16 s[2];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[half][r] = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                multiply<PS>(s[half], q[i], [&](int part) { return unit_rows(k + part * kPlane, half, i, lane); });
-        }
-        if (!__all(seen == ~0ull)) {
+        auto scores = [&]() {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const uint32_t bits = lane_bits(seen, half, lane);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[half][r] = lane_bit(bits, r) ? s[half][r] : -INFINITY;
+                for (int r = 0; r < 16; ++r) s[half][r] = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    multiply<PS>(s[half], q[i], [&](int part) { return unit_rows(k + part * kPlane, half, i, lane); });
             }
-        }
-        float most = s[0][0];
+            if (!all) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t out = left_out(seen, half, lane);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) most = fmaxf(most, s[half][r]);
-        most = max_with_other_half(most);
-        if (__any(most > top)) {
+                    for (int r = 0; r < 16; ++r) s[half][r] = replace(s[half][r], -INFINITY, left_out_mask(out, r));
+                }
+            }
+        };
+        auto raise = [&]() {
+            float most = s[0][0];
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) most = fmaxf(most, s[half][r]);
+            most = max_with_other_half(most);
             const float next = fmaxf(top, most);
             const float w = next == -INFINITY ? 1.f : fast_exp2((top - next) * factor);
             top = next;
             sum *= w;
 #pragma unroll
             for (int r = 0; r < 16; ++r) { o[0][r] *= w; o[1][r] *= w; }
+        };
+        float unit_sum;  // the unit's own sum first: a long row's chain of additions is a 32nd as long
+        auto exponentials = [&]() {
+            const float base = top == -INFINITY ? 0.f : top * factor;
+            unit_sum = 0.f;
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[half][r] = fast_exp2(fmaf(s[half][r], factor, -base));
+                    unit_sum += s[half][r];
+                }
+        };
+        for (bool look = !__all(top > -INFINITY);; look = true) {
+            scores();
+            if (look) raise();
+            exponentials();
+            if (look || __all(unit_sum <= kMaxUnitSum)) break;
         }
-        const float base = top == -INFINITY ? 0.f : top * factor;
-        float unit_sum = 0.f;  // the unit's own sum first: a long row's chain of additions is a 32nd as long
+        __builtin_amdgcn_sched_barrier(0);
+        sum += unit_sum;
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 float x[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    x[j] = fast_exp2(fmaf(s[half][8 * u + j], factor, -base));
-                    unit_sum += x[j];
-                }
+                for (int j = 0; j < 8; ++j) x[j] = s[half][8 * u + j];
                 bf16x8 p[PQ];
                 split_parts<PQ>(x, p);
 #pragma unroll
                 for (int dt = 0; dt < 2; ++dt)
                     multiply<PS>(o[dt], p, [&](int part) { return unit_channels(v + part * kPlane, half, u, dt, lane); });
             }
-        sum += unit_sum;
     }
     // The sum of exponentials over both half-waves, and its log2 (-inf: no keys).
     __device__ __forceinline__ void totals(float factor, float &total, float &log2_total) const
@@ -363,39 +535,173 @@ __device__ __forceinline__ void store_soft(const SoftRow<PQ> &soft, float factor
     }
 }
 
-// The joint result of WAVES waves that had a share of the keys each, for the same 32 rows.  lds: WAVES * kJoinFloats floats.
-constexpr int kJoinFloats = 2048 + 64;
-template <int WAVES, int PQ> __device__ __forceinline__ void join_waves(SoftRow<PQ> &soft, float factor, float *lds, int wave, int lane)
+// ---- few rows -----------------------------------------------------------------------------------------------
+// Up to 16 held rows, the same for all waves of a workgroup, each of which takes its own units (16x16x32 MFMAs; bound by the memory that
+// keys and values come from).  Keys go from memory to the A operand as they are: lane (key l % 16, channels 16 (l / 16) .. + 15) of each
+// 16-key tile; only values pass through LDS, to be transposed.  A lane has row l % 16 and, of every tile of 16 keys (or channels),
+// 4 (l / 16) + r.
+constexpr int kFewRows = 16;
+
+// A operand of the transposed unit: channels 16 ct .. + 15; keys 32 ks + 4 (lane / 16) + j, then 16 further.
+__device__ __forceinline__ bf16x8 few_channels(const bf16_t *unit, int ks, int ct, int lane)
 {
-    float *mine = lds + wave * kJoinFloats;
+    const int i = lane & 15, row = 32 * ks + 4 * (lane >> 4) + (i >> 2);
+    const int chunk = 2 * ct + ((i & 3) >> 1), in_chunk = 4 * (i & 1);
+    typedef short shortx8 __attribute__((ext_vector_type(8)));
+    const shortx4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4 *)(unit + unit_chunk(row, chunk) + in_chunk));
+    const shortx4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4 *)(unit + unit_chunk(row + 16, chunk) + in_chunk));
+    const shortx8 ab = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_bit_cast(bf16x8, ab);
+}
+
+__device__ __forceinline__ float max_over_groups(float x)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return max_with_other_half(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+
+__device__ __forceinline__ float sum_over_groups(float x)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return sum_with_other_half(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+template <int PQ> struct FewRows {
+    bf16x8 q[2][PQ];  // B operands: row l % 16, channels 16 (l / 16) + 8 s ..
+    floatx4 o[4];     // channels 16 ct + 4 (l / 16) + r
+    float top, sum;
+
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
-    for (int dt = 0; dt < 2; ++dt)
+        for (int ct = 0; ct < 4; ++ct) o[ct] = floatx4{0.f, 0.f, 0.f, 0.f};
+        top = -INFINITY;
+        sum = 0.f;
+    }
+    template <typename T> __device__ __forceinline__ void load(const T *row, bool ok, int lane)
+    {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) mine[(dt * 16 + r) * 64 + lane] = soft.o[dt][r];
-    const float both = sum_with_other_half(soft.sum);
-    if (lane < 32) { mine[2048 + lane] = soft.top; mine[2080 + lane] = both; }
+        for (int s = 0; s < 2; ++s) {
+            float x[8] = {};
+            if (ok) load8(row + 16 * (lane >> 4) + 8 * s, x);
+            split_held<PQ>(x, q[s]);
+        }
+    }
+    // key(t, s, parts): the A operand of key tile t, its PS parts; v: PS planes in LDS
+    template <int PS, typename Key>
+    __device__ __forceinline__ void unit(Key &&key, const bf16_t *v, unsigned long long seen, float factor, int lane)
+    {
+        floatx4 s[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                bf16x8 k[PS];
+                key(t, i, k);
+#pragma unroll
+                for (int a = 0; a < PS; ++a)
+#pragma unroll
+                    for (int b = 0; b < PQ; ++b)
+                        if (a + b < 3) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[a], q[i][b], s[t], 0, 0, 0);
+            }
+        }
+        if (!__all(seen == ~0ull)) {
+            const unsigned long long mine = seen >> (4 * (lane >> 4));
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[t][r] = (mine >> (16 * t + r)) & 1 ? s[t][r] : -INFINITY;
+        }
+        float most = s[0][0];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) most = fmaxf(most, s[t][r]);
+        most = max_over_groups(most);
+        if (__any(most > top)) {
+            const float next = fmaxf(top, most);
+            const float w = next == -INFINITY ? 1.f : fast_exp2((top - next) * factor);
+            top = next;
+            sum *= w;
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct) o[ct] *= w;
+        }
+        const float base = top == -INFINITY ? 0.f : top * factor;
+        float unit_sum = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                x[j] = fast_exp2(fmaf(s[2 * ks + (j >> 2)][j & 3], factor, -base));
+                unit_sum += x[j];
+            }
+            bf16x8 p[PQ];
+            split_parts<PQ>(x, p);
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+                for (int a = 0; a < PS; ++a) {
+                    const bf16x8 vt = few_channels(v + a * kPlane, ks, ct, lane);
+#pragma unroll
+                    for (int b = 0; b < PQ; ++b)
+                        if (a + b < 3) o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, p[b], o[ct], 0, 0, 0);
+                }
+        }
+        sum += unit_sum;
+    }
+};
+
+// The joint result of WAVES waves that had a share of the keys each, and its store: wave w < 4 takes channels 16 w .. + 15.
+// lds: WAVES * kFewJoin floats.
+constexpr int kFewJoin = 1024 + 32;
+template <typename T, int WAVES, int PQ>
+__device__ __forceinline__ void store_few(const FewRows<PQ> &few, float factor, const SoftOut &to, int split, int64_t row, int head, bool ok,
+                                          float *lds, int wave, int lane)
+{
+    float *mine = lds + wave * kFewJoin;
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mine[(ct * 4 + r) * 64 + lane] = few.o[ct][r];
+    const float all = sum_over_groups(few.sum);
+    if (lane < 16) { mine[1024 + lane] = few.top; mine[1040 + lane] = all; }
     __syncthreads();
-    if (wave != 0) return;
-    float top = -INFINITY, sum = 0.f, w[WAVES];
+    if (wave >= 4) return;
+    const int q = lane & 15;
+    float top = -INFINITY, sum = 0.f;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < WAVES; ++j) top = fmaxf(top, lds[j * kJoinFloats + 2048 + (lane & 31)]);
+    for (int j = 0; j < WAVES; ++j) top = fmaxf(top, lds[j * kFewJoin + 1024 + q]);
 #pragma unroll
     for (int j = 0; j < WAVES; ++j) {
-        const float t = lds[j * kJoinFloats + 2048 + (lane & 31)];
-        w[j] = t == top ? 1.f : (t == -INFINITY ? 0.f : fast_exp2((t - top) * factor));
-        sum += lds[j * kJoinFloats + 2080 + (lane & 31)] * w[j];
+        const float t = lds[j * kFewJoin + 1024 + q];
+        const float w = t == top ? 1.f : (t == -INFINITY ? 0.f : fast_exp2((t - top) * factor));
+        sum += lds[j * kFewJoin + 1040 + q] * w;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[r] += lds[j * kFewJoin + (wave * 4 + r) * 64 + lane] * w;
     }
+    if (!ok) return;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum, l2 = sum == 0.f ? -INFINITY : fmaf(top, factor, log2f(sum));
+    o *= inv;
+    const int64_t at = row * to.heads + head, part = split * to.rows * to.heads + at;
+    const int c = 16 * wave + 4 * (lane >> 4);
+    if (to.part_o != nullptr) {
+        *reinterpret_cast<floatx4 *>(to.part_o + part * 64 + c) = o;
+        if (wave == 0 && lane < 16) to.part_lse[part] = l2;
+    } else {
+        T *dst = static_cast<T *>(to.out) + at * 64 + c;
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<floatx4 *>(dst) = o;
+        } else {
+            bf16x4 x;
 #pragma unroll
-    for (int dt = 0; dt < 2; ++dt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            float x = 0.f;
-#pragma unroll
-            for (int j = 0; j < WAVES; ++j) x += lds[j * kJoinFloats + (dt * 16 + r) * 64 + lane] * w[j];
-            soft.o[dt][r] = x;
+            for (int r = 0; r < 4; ++r) x[r] = static_cast<bf16_t>(o[r]);
+            *reinterpret_cast<bf16x4 *>(dst) = x;
         }
-    soft.top = top;
-    soft.sum = lane < 32 ? sum : 0.f;
+        if (wave == 0 && lane < 16 && to.lse != nullptr) to.lse[head * to.rows + row] = l2 * kLn2;
+    }
 }
 
 // A thread of 1024's finding whether a list of spans is out of range or out of order.

@@ -1022,8 +1022,8 @@ s3r_status plan_cross(const s3r_cross_params *p, CrossPlan *out)
     if (p->n_q > kMaxRowHeads / p->heads || p->n_kv > kMaxRowHeads / p->kv_heads || c.batch > (1 << 22) / p->kv_heads)
         return fail(S3R_ERR_UNSUPPORTED, "rows * heads exceeds 2^28, or batch * kv_heads 2^22");
     const int64_t items = p->n_q * c.per_row, units = (p->n_kv / c.batch + 63) / 64;
-    c.few_rows = items <= int64_t(32) * c.batch;
-    c.tiles = s3r::most_tiles(p->n_q, c.per_row, c.few_rows ? 32 : 128, c.batch);
+    c.few_rows = items <= int64_t(16) * c.batch;
+    c.tiles = s3r::most_tiles(p->n_q, c.per_row, c.few_rows ? 16 : 128, c.batch);
     c.split = pieces(c.tiles * p->kv_heads, units, c.few_rows ? 8 : 4);
     c.q_tiles = s3r::most_tiles(p->n_q, c.per_row, 128, c.batch);
     c.split_q = pieces(c.q_tiles * p->kv_heads, units, 4);
@@ -1206,8 +1206,8 @@ s3r_status plan_cache(const s3r_cache_params *p, CachePlan *out)
     CachePlan c{};
     const int per_row = p->heads / p->kv_heads;
     const int64_t units = (int64_t(p->max_pages) * p->page + 63) / 64;
-    c.few_rows = p->n_rows * per_row <= int64_t(32) * p->batch;
-    c.tiles = s3r::most_tiles(p->n_rows, per_row, c.few_rows ? 32 : 128, p->batch);
+    c.few_rows = p->n_rows * per_row <= int64_t(16) * p->batch;
+    c.tiles = s3r::most_tiles(p->n_rows, per_row, c.few_rows ? 16 : 128, p->batch);
     c.split = pieces(c.tiles * p->kv_heads, units, c.few_rows ? 8 : 4);
     const size_t rows = static_cast<size_t>(p->n_rows) * p->heads;
     size_t off = 0;
