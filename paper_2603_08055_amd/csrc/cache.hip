@@ -299,6 +299,7 @@ template <typename T> __global__ __launch_bounds__(256, 2) void cache_attn_kerne
         code = *reinterpret_cast<const uint4 *>(codes + units.head_slot() * 32 + 16 * half);
         scale = scales[units.head_slot() * 2 + half];
     };
+    const UnitLanes at(lane);
     if (u0 < u1) { units.find(u0, lane); fetch(); units.find(u0 + 1, lane); }
     for (int u = u0; u < u1; ++u) {
         bf16_t *stage = lds + ((u - u0) & 1) * kCacheStage;
@@ -310,7 +311,7 @@ template <typename T> __global__ __launch_bounds__(256, 2) void cache_attn_kerne
         const unsigned long long seen = __ballot(there) & low_bits(sight.sees - u * kUnitRows);
         __syncthreads();
         if (u + 1 < u1) { fetch(); units.find(u + 2, lane); }
-        soft.template unit<1>(stage, stage + kPlane, seen, a.factor, lane);
+        soft.template unit<1>(stage, stage + kPlane, seen, a.factor, at, lane);
 #pragma unroll
         for (int dt = 0; dt < 2; ++dt) {
             const unsigned long long nan = words[dt];

@@ -26,7 +26,7 @@ __device__ __forceinline__ CountedRows counted(const CrossArgs &a, int first, in
 }
 
 // Many rows: four waves hold 32 rows each and share every unit.
-template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void cross_kernel(CrossArgs a)
+template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 4) void cross_kernel(CrossArgs a)
 {
     constexpr int P = UnitPairs<T>::kParts;
     extern __shared__ __align__(16) unsigned char smem[];
@@ -50,10 +50,11 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     auto rows = counted(a, k0, k_len);
     unsigned long long seen = 0;
     auto more = [&](int u) { rows.fetch(u, lane); };
+    const UnitLanes at(lane);
     units.begin(u0, u1, more);
     for (int u = u0; u < u1; ++u) {
         const bf16_t *k = units.step(u, u == u0, more, [&]() { return seen = rows.counts(); }, [](int) {});
-        soft.template unit<P>(k, k + P * kPlane, seen, a.factor, lane);
+        soft.template unit<P>(k, k + P * kPlane, seen, a.factor, at, lane);
     }
     store_soft<T>(soft, a.factor, a.to, sh.split, row, head, ok, lane);
 }
@@ -177,15 +178,15 @@ template <typename T, int GROUPS> __global__ __launch_bounds__(256) void soft_co
 
 // ---- gradient --------------------------------------------------------------------------------------------
 
-// D from the stored out: in bf16 it is off by the rounding of out, the same amount for all keys of a row, and
-// that would be most of the error of dq and dk (three times all other roundings together at 2748 rows over 10992 keys).  The sum of
-// a row's P (dP - D) over all keys, in fp32, is what D lacks: the query gradient adds it up and leaves D whole for the gradient of keys.
-// Its own result it mends by the sum of the dS as they entered the product, which should be 0: dS k - sum(dS) * P k.  That takes out
-// the lack of D and of the rounding of dS what all keys of the row have in common.  One product more of eight.
+// D from the stored out: in bf16 it is off by the rounding of out, the same amount for all keys of a row, and that would be most of the
+// error of dq and dk (three times all other roundings together at 2748 rows over 10992 keys).  The dS of a row add up to 0 over all
+// keys: what they do add up to in fp32 is what D lacks, and with it D is made whole for the gradient of keys.  What they add up to as they
+// enter the product has the roundings of dS in it as well; the query gradient takes that out of its own result, dS k - sum(dS) * P k.
+// One product more of eight (5.1e-3 -> 2.3e-3 against 64 bits).
 template <typename T> constexpr bool kMendD = sizeof(T) == 2;
 
 // What the gradient needs of every row of a head: its log-sum (in log2; +inf where it saw no keys, so that every probability is 0) and
-// D = out . d_out.  16 threads for a row of a head.
+// -D, D = out . d_out.  16 threads for a row of a head.
 template <typename T>
 __global__ __launch_bounds__(256) void row_stats_kernel(const T *__restrict__ out, const T *__restrict__ d_out,
                                                         const float *__restrict__ lse, float *__restrict__ stats, int64_t rows, int heads)
@@ -202,7 +203,7 @@ __global__ __launch_bounds__(256) void row_stats_kernel(const T *__restrict__ ou
     const int64_t row = at / heads, to = (at - row * heads) * rows + row;
     const float l = lse[to];
     stats[2 * to] = l == -INFINITY ? INFINITY : l * kLog2e;
-    stats[2 * to + 1] = d;
+    stats[2 * to + 1] = -d;
 }
 
 __device__ __forceinline__ float sum8(const bf16x8 &x)
@@ -234,7 +235,7 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     held.load(static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head, ok, lane);
     grad.clear();
     grad.load(static_cast<const T *>(a.d_out) + (row * a.heads + head) * 64, ok, lane);
-    float l2 = INFINITY, d = 0.f, defect = 0.f, entered = 0.f;
+    float l2 = INFINITY, d = 0.f, defect = 0.f, entered = 0.f;  // d: -D
     float *stats = a.stats + 2 * (head * a.n_q + row);
     if (ok) { l2 = stats[0]; d = stats[1]; }
     int u0, u1;
@@ -243,21 +244,36 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     auto rows = counted(a, k0, k_len);
     unsigned long long seen = 0;
     auto more = [&](int u) { rows.fetch(u, lane); };
+    const UnitLanes at(lane);
+    floatx16 minus_d;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) minus_d[r] = d;
+    asm volatile("" : "+v"(minus_d));  // sixteen registers to start from, and not a move for each of them in every product
     units.begin(u0, u1, more);
     for (int u = u0; u < u1; ++u) {
         const bf16_t *k = units.step(u, u == u0, more, [&]() { return seen = rows.counts(); }, [](int) {}), *v = k + P * kPlane;
+        // dP - D comes out of the product itself where it starts at -D
+        RowOperands<P> kr, vr;
+        kr.read(k, 0, at);
+        vr.read(v, 0, at);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            floatx16 s = {}, dp = {};
+            floatx16 s = {}, dp = minus_d;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                multiply<P>(s, held.q[i], [&](int part) { return unit_rows(k + part * kPlane, half, i, lane); });
-                multiply<P>(dp, grad.q[i], [&](int part) { return unit_rows(v + part * kPlane, half, i, lane); });
+                multiply<P>(s, held.q[i], [&](int part) { return kr.x[i][part]; });
+                multiply<P>(dp, grad.q[i], [&](int part) { return vr.x[i][part]; });
             }
+            if (half == 0) {
+                kr.read(k, 1, at);
+                vr.read(v, 1, at);
+            }
+            ChannelOperands<P> kt;
+            kt.read(k, half, at);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 s[r] = fast_exp2(fmaf(s[r], a.factor, -l2));
-                dp[r] = s[r] * (dp[r] - d);
+                dp[r] *= s[r];
             }
             if (seen != ~0ull) {
                 const uint32_t out = left_out(seen, half, lane);
@@ -269,30 +285,29 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
             }
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
-                float x[8], y[8], sum = 0.f;
+                float x[8], y[8], sum[2] = {0.f, 0.f};
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     y[j] = s[8 * w + j];
                     x[j] = dp[8 * w + j];
-                    sum += x[j];
+                    if constexpr (kMendD<T>) sum[j & 1] += x[j];
                 }
                 bf16x8 ds[P], p[P];
                 split_parts<P>(x, ds);
                 if constexpr (kMendD<T>) {
-                    defect += sum;
+                    defect += sum[0] + sum[1];
                     split_parts<P>(y, p);
                     entered += sum8(ds[0]);
                 }
 #pragma unroll
                 for (int dt = 0; dt < 2; ++dt) {
-                    multiply<P>(grad.o[dt], ds, [&](int part) { return unit_channels(k + part * kPlane, half, w, dt, lane); });
-                    if constexpr (kMendD<T>)
-                        multiply<P>(held.o[dt], p, [&](int part) { return unit_channels(k + part * kPlane, half, w, dt, lane); });
+                    multiply<P>(grad.o[dt], ds, [&](int part) { return kt.x[w][dt][part]; });
+                    if constexpr (kMendD<T>) multiply<P>(held.o[dt], p, [&](int part) { return kt.x[w][dt][part]; });
                 }
             }
         }
     }
-    const int64_t at = row * a.heads + head, part = sh.split * a.n_q * a.heads + at;
+    const int64_t to = row * a.heads + head, part = sh.split * a.n_q * a.heads + to;
     if constexpr (kMendD<T>) {
         defect = sum_with_other_half(defect);
         entered = sum_with_other_half(entered);
@@ -302,16 +317,16 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
                 grad.o[0][r] -= entered * held.o[0][r];
                 grad.o[1][r] -= entered * held.o[1][r];
             }
-            if (ok && lane < 32) stats[1] = d + defect;
+            if (ok && lane < 32) stats[1] = d - defect;
         } else {
             store_row(held.o, 1.f, a.part_pk + part * 64, ok, lane);
-            if (ok && lane < 32) { a.part_defect[2 * part] = defect; a.part_defect[2 * part + 1] = entered; }
+            if (ok && lane < 32) { a.part_sum[2 * part] = defect; a.part_sum[2 * part + 1] = entered; }
         }
     }
     if (a.part_q != nullptr)
         store_row(grad.o, 1.f, a.part_q + part * 64, ok, lane);
     else
-        store_row(grad.o, a.scale, static_cast<T *>(a.dq) + at * 64, ok, lane);
+        store_row(grad.o, a.scale, static_cast<T *>(a.dq) + to * 64, ok, lane);
 }
 
 // The query gradient from its pieces over keys.  16 threads for a row of a head.
@@ -328,14 +343,14 @@ template <typename T> __global__ __launch_bounds__(256) void grad_q_combine_kern
         g += *reinterpret_cast<const floatx4 *>(a.part_q + (j * share + at) * 64 + c);
         if constexpr (kMendD<T>) {
             pk += *reinterpret_cast<const floatx4 *>(a.part_pk + (j * share + at) * 64 + c);
-            defect += a.part_defect[2 * (j * share + at)];
-            entered += a.part_defect[2 * (j * share + at) + 1];
+            defect += a.part_sum[2 * (j * share + at)];
+            entered += a.part_sum[2 * (j * share + at) + 1];
         }
     }
     T *dst = static_cast<T *>(a.dq) + at * 64 + c;
 #pragma unroll
     for (int e = 0; e < 4; ++e) dst[e] = from_float<T>(a.scale * (g[e] - entered * pk[e]));
-    if (kMendD<T> && c == 0) a.stats[2 * ((at - row * a.heads) * a.n_q + row) + 1] += defect;
+    if (kMendD<T> && c == 0) a.stats[2 * ((at - row * a.heads) * a.n_q + row) + 1] -= defect;
 }
 
 template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void grad_kv_kernel(CrossArgs a)
@@ -375,6 +390,7 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     };
     int u0, u1;
     piece((items + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
+    const UnitLanes at(lane);
     units.begin(u0, u1, more);
     const float *stats = row_stats;
     for (int u = u0; u < u1; ++u) {
@@ -383,26 +399,42 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
             if (which < 2) to[which * 64 + lane] = st;
             stats = to;
         }), *g = q + P * kPlane;
+        RowOperands<P> qr, gr;
+        qr.read(q, 0, at);
+        gr.read(g, 0, at);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            floatx16 s = {}, dp = {};
+            floatx16 s = {}, dp;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const floatx4 d = *reinterpret_cast<const floatx4 *>(stats + 64 + 32 * half + 8 * b + 4 * (lane >> 5));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dp[4 * b + e] = d[e];
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                multiply<P>(s, kk.q[i], [&](int part) { return unit_rows(q + part * kPlane, half, i, lane); });
-                multiply<P>(dp, vv.q[i], [&](int part) { return unit_rows(g + part * kPlane, half, i, lane); });
+                multiply<P>(s, kk.q[i], [&](int part) { return qr.x[i][part]; });
+                multiply<P>(dp, vv.q[i], [&](int part) { return gr.x[i][part]; });
             }
+            if (half == 0) {
+                qr.read(q, 1, at);
+                gr.read(g, 1, at);
+            }
+            ChannelOperands<P> qt, gt;
+            gt.read(g, half, at);
+            qt.read(q, half, at);
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
                 float x[8], y[8];
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
                     const int r0 = 32 * half + 16 * w + 8 * b + 4 * (lane >> 5);
-                    const floatx4 l2 = *reinterpret_cast<const floatx4 *>(stats + r0), d = *reinterpret_cast<const floatx4 *>(stats + 64 + r0);
+                    const floatx4 l2 = *reinterpret_cast<const floatx4 *>(stats + r0);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int r = 8 * w + 4 * b + e;
                         x[4 * b + e] = fast_exp2(fmaf(s[r], a.factor, -l2[e]));
-                        y[4 * b + e] = x[4 * b + e] * (dp[r] - d[e]);
+                        y[4 * b + e] = x[4 * b + e] * dp[r];
                     }
                 }
                 bf16x8 p[P], ds[P];
@@ -410,8 +442,8 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
                 split_parts<P>(y, ds);
 #pragma unroll
                 for (int dt = 0; dt < 2; ++dt) {
-                    multiply<P>(vv.o[dt], p, [&](int part) { return unit_channels(g + part * kPlane, half, w, dt, lane); });
-                    multiply<P>(kk.o[dt], ds, [&](int part) { return unit_channels(q + part * kPlane, half, w, dt, lane); });
+                    multiply<P>(vv.o[dt], p, [&](int part) { return gt.x[w][dt][part]; });
+                    multiply<P>(kk.o[dt], ds, [&](int part) { return qt.x[w][dt][part]; });
                 }
             }
         }
@@ -419,13 +451,13 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     if (!seen)  // a masked key gets no gradient, whatever its lanes added up
 #pragma unroll
         for (int r = 0; r < 16; ++r) kk.o[0][r] = kk.o[1][r] = vv.o[0][r] = vv.o[1][r] = 0.f;
-    const int64_t at = (row * a.kv_heads + sh.kv_head) * 64, share = a.n_kv * a.kv_heads * 64;
+    const int64_t to = (row * a.kv_heads + sh.kv_head) * 64, share = a.n_kv * a.kv_heads * 64;
     if (a.part_k != nullptr) {
-        store_row(kk.o, a.scale, a.part_k + sh.split * share + at, ok, lane);
-        store_row(vv.o, 1.f, a.part_v + sh.split * share + at, ok, lane);
+        store_row(kk.o, a.scale, a.part_k + sh.split * share + to, ok, lane);
+        store_row(vv.o, 1.f, a.part_v + sh.split * share + to, ok, lane);
     } else {
-        store_row(kk.o, a.scale, static_cast<T *>(a.dk) + at, ok, lane);
-        store_row(vv.o, 1.f, static_cast<T *>(a.dv) + at, ok, lane);
+        store_row(kk.o, a.scale, static_cast<T *>(a.dk) + to, ok, lane);
+        store_row(vv.o, 1.f, static_cast<T *>(a.dv) + to, ok, lane);
     }
 }
 

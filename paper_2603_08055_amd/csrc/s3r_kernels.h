@@ -279,7 +279,7 @@ constexpr int kDiagPage = 4, kDiagSpans = 8, kDiagLength = 16, kDiagPosition = 3
 
 // q and d_out rows, k and v rows: element strides between rows and between heads.  per_row = heads / kv_heads.  factor = scale * log2(e).
 // tiles: most tiles of the held rows (most_tiles); n_split: pieces of the streamed rows.  stats: see launch_row_stats.  part_*: partial
-// sums [n_split][rows][heads][64] where n_split > 1, else null (part_defect: [n_split][rows][heads][2]; it and part_pk for bf16 alone).
+// sums [n_split][rows][heads][64] where n_split > 1, else null (part_sum: [n_split][rows][heads][2]; it and part_pk for bf16 alone).
 struct CrossArgs {
     const void *q, *k, *v, *d_out;
     int64_t q_row, q_head, kv_row, kv_head;
@@ -291,13 +291,13 @@ struct CrossArgs {
     SoftOut to;
     float *stats;
     void *dq, *dk, *dv;
-    float *part_q, *part_pk, *part_defect, *part_k, *part_v;
+    float *part_q, *part_pk, *part_sum, *part_k, *part_v;
 };
 
 // few_rows: a workgroup's waves divide the keys of 16 rows, and not 128 rows, among them (tiles accordingly).
 hipError_t launch_cross(const CrossArgs &a, bool few_rows, bool is_bf16, hipStream_t stream);
 hipError_t launch_soft_combine(const SoftOut &to, const Spans &spans, int n_split, bool is_bf16, hipStream_t stream);
-// stats [heads][rows][2]: log-sum in log2 (+inf for a row without keys) and out . d_out
+// stats [heads][rows][2]: log-sum in log2 (+inf for a row without keys) and -(out . d_out)
 hipError_t launch_row_stats(const void *out, const void *d_out, const float *lse, float *stats, int64_t rows, int heads, bool is_bf16,
                             hipStream_t stream);
 // bf16: D in stats is made whole, for launch_grad_kv, which comes after (n_split > 1: by the combine launch).

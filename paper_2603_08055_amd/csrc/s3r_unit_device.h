@@ -28,24 +28,75 @@ __device__ __forceinline__ int unit_chunk(int row, int c)
     return row * 64 + ((c ^ (((row & 2) << 1) | ((row >> 2) & 3))) << 3);
 }
 
-// A operand: rows 32 half .. + 31 of a unit, channels 16 s .. + 15.
-__device__ __forceinline__ bf16x8 unit_rows(const bf16_t *unit, int half, int s, int lane)
+// The same value, of which the compiler knows nothing: what is computed from it stays where it is written and holds no registers
+// through a loop that seldom comes by.
+__device__ __forceinline__ int opaque(int x)
 {
-    return *reinterpret_cast<const bf16x8 *>(unit + unit_chunk(32 * half + (lane & 31), 2 * s + (lane >> 5)));
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// Where a lane's pieces of the two kinds of A operand lie in a unit.  Rows 16, 32 and 48 further the chunks are permuted alike, so that
+// these few offsets serve a whole unit with constants added.
+struct UnitLanes {
+    int rows[4];   // channels 16 s + 8 (lane / 32) .. of row lane % 32
+    int tr[2][2];  // four channels of row 4 (lane / 32) + (lane % 16) / 4, of channels 32 dt + 16 ((lane / 16) % 2) .. + 15; row 8 further
+    __device__ __forceinline__ explicit UnitLanes(int lane)
+    {
+        const int i = lane & 15, row = 4 * (lane >> 5) + (i >> 2), in_chunk = 4 * (i & 1);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) rows[s] = unit_chunk(lane & 31, 2 * s + (lane >> 5));
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt) {
+            const int chunk = 4 * dt + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+            tr[dt][0] = unit_chunk(row, chunk) + in_chunk;
+            tr[dt][1] = unit_chunk(row + 8, chunk) + in_chunk;
+        }
+    }
+};
+
+// A operand: rows 32 half .. + 31 of a unit, channels 16 s .. + 15.
+__device__ __forceinline__ bf16x8 unit_rows(const bf16_t *unit, int half, int s, const UnitLanes &at)
+{
+    return *reinterpret_cast<const bf16x8 *>(unit + at.rows[s] + half * 2048);
 }
 
 // A operand of the transposed unit: channels 32 dt .. + 31, rows 32 half + 16 u + 8 (j / 4) + 4 (lane / 32) + j % 4, j = 0 .. 7.
 // Sixteen lanes fetch four rows of sixteen channels and get one channel of the four rows each.
-__device__ __forceinline__ bf16x8 unit_channels(const bf16_t *unit, int half, int u, int dt, int lane)
+__device__ __forceinline__ bf16x8 unit_channels(const bf16_t *unit, int half, int u, int dt, const UnitLanes &at)
 {
-    const int i = lane & 15, row = 32 * half + 16 * u + 4 * (lane >> 5) + (i >> 2);
-    const int chunk = 4 * dt + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1), in_chunk = 4 * (i & 1);
     typedef short shortx8 __attribute__((ext_vector_type(8)));
-    const shortx4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4 *)(unit + unit_chunk(row, chunk) + in_chunk));
-    const shortx4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4 *)(unit + unit_chunk(row + 8, chunk) + in_chunk));
+    const bf16_t *from = unit + (32 * half + 16 * u) * 64;
+    const shortx4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4 *)(from + at.tr[dt][0]));
+    const shortx4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4 *)(from + at.tr[dt][1]));
     const shortx8 ab = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     return __builtin_bit_cast(bf16x8, ab);
 }
+
+// All A operands of half a unit, sent for together.
+template <int PS> struct RowOperands {
+    bf16x8 x[4][PS];
+    __device__ __forceinline__ void read(const bf16_t *unit, int half, const UnitLanes &at)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int part = 0; part < PS; ++part) x[i][part] = unit_rows(unit + part * kPlane, half, i, at);
+    }
+};
+
+template <int PS> struct ChannelOperands {
+    bf16x8 x[2][2][PS];
+    __device__ __forceinline__ void read(const bf16_t *unit, int half, const UnitLanes &at)
+    {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+                for (int part = 0; part < PS; ++part) x[u][dt][part] = unit_channels(unit + part * kPlane, half, u, dt, at);
+    }
+};
 
 // The part of x that its upper 16 bits hold (a NaN stays one).
 __device__ __forceinline__ float upper_part(float x)
@@ -273,6 +324,7 @@ template <bool GROUPED> struct DirectUnits {
             for (int i = 0; i < 2; ++i) lds_dma_16_x1(from, off[i], lds + (2 * wave + i) * 1024);
             return;
         }
+        lane = opaque(lane);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int at = min(unit * kUnitRows + row_in_unit(wave, i, lane), items - 1);
@@ -284,6 +336,7 @@ template <bool GROUPED> struct DirectUnits {
 
 __device__ __forceinline__ void blank_rows(bf16_t *unit, unsigned long long counts, int t)
 {
+    t = opaque(t);
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
         const int id = t + c * 256;
@@ -373,9 +426,7 @@ template <bool GROUPED> struct UnitPairs<bf16_t, GROUPED> {
 // compiler, which would else make the masks of all registers ahead, for units that need none as well.
 __device__ __forceinline__ uint32_t left_out(unsigned long long seen, int half, int lane)
 {
-    uint32_t bits = static_cast<uint32_t>(~seen >> (32 * half)) >> (4 * (lane >> 5));
-    asm volatile("" : "+v"(bits));
-    return bits;
+    return static_cast<uint32_t>(opaque(static_cast<int>(static_cast<uint32_t>(~seen >> (32 * half)) >> (4 * (lane >> 5)))));
 }
 __device__ __forceinline__ uint32_t left_out_mask(uint32_t bits, int r)  // all ones: left out
 {
@@ -423,19 +474,22 @@ template <int PQ> struct SoftRow {
     // One unit of keys (PS planes) and values (PS planes); seen: the keys that count for the lane's row; factor: scale * log2(e).
     // `top` need not be the largest score so far: it is raised only where a row's exponentials of a unit add up to more than 255, that is
     // where one is above 2^8 times its like at `top`; the scores are then computed again.  That spares almost all units the search.
+    // All LDS reads of a product are sent for before its first MFMA.
     template <int PS>
-    __device__ __forceinline__ void unit(const bf16_t *k, const bf16_t *v, unsigned long long seen, float factor, int lane)
+    __device__ __forceinline__ void unit(const bf16_t *k, const bf16_t *v, unsigned long long seen, float factor, const UnitLanes &at, int lane)
     {
         const bool all = __all(seen == ~0ull);
         floatx16 s[2];
         auto scores = [&]() {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
+                RowOperands<PS> a;
+                a.read(k, half, at);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[half][r] = 0.f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    multiply<PS>(s[half], q[i], [&](int part) { return unit_rows(k + part * kPlane, half, i, lane); });
+                for (int i = 0; i < 4; ++i) multiply<PS>(s[half], q[i], [&](int part) { return a.x[i][part]; });
             }
             if (!all) {
 #pragma unroll
@@ -463,14 +517,15 @@ template <int PQ> struct SoftRow {
         float unit_sum;  // the unit's own sum first: a long row's chain of additions is a 32nd as long
         auto exponentials = [&]() {
             const float base = top == -INFINITY ? 0.f : top * factor;
-            unit_sum = 0.f;
+            float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     s[half][r] = fast_exp2(fmaf(s[half][r], factor, -base));
-                    unit_sum += s[half][r];
+                    part[r & 3] += s[half][r];
                 }
+            unit_sum = (part[0] + part[1]) + (part[2] + part[3]);
         };
         for (bool look = !__all(top > -INFINITY);; look = true) {
             scores();
@@ -478,20 +533,23 @@ template <int PQ> struct SoftRow {
             exponentials();
             if (look || __all(unit_sum <= kMaxUnitSum)) break;
         }
-        __builtin_amdgcn_sched_barrier(0);
         sum += unit_sum;
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
+                bf16x8 a[2][PS];
+#pragma unroll
+                for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+                    for (int part = 0; part < PS; ++part) a[dt][part] = unit_channels(v + part * kPlane, half, u, dt, at);
                 float x[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] = s[half][8 * u + j];
                 bf16x8 p[PQ];
                 split_parts<PQ>(x, p);
 #pragma unroll
-                for (int dt = 0; dt < 2; ++dt)
-                    multiply<PS>(o[dt], p, [&](int part) { return unit_channels(v + part * kPlane, half, u, dt, lane); });
+                for (int dt = 0; dt < 2; ++dt) multiply<PS>(o[dt], p, [&](int part) { return a[dt][part]; });
             }
     }
     // The sum of exponentials over both half-waves, and its log2 (-inf: no keys).

@@ -1003,7 +1003,7 @@ struct CrossPlan {
     int batch, per_row, split, split_q, split_kv;
     int64_t tiles, q_tiles, kv_tiles;
     size_t part_o, part_lse, forward;                   // workspace of the forward call
-    size_t stats, part_q, part_pk, part_defect, part_k, part_v, backward;     // of the gradient
+    size_t stats, part_q, part_pk, part_sum, part_k, part_v, backward;     // of the gradient
 };
 
 s3r_status plan_cross(const s3r_cross_params *p, CrossPlan *out)
@@ -1040,7 +1040,7 @@ s3r_status plan_cross(const s3r_cross_params *p, CrossPlan *out)
     c.part_q = take(c.split_q > 1 ? c.split_q * rows * 64 * sizeof(float) : 0);
     const bool mend = c.split_q > 1 && p->dtype == S3R_BF16;
     c.part_pk = take(mend ? c.split_q * rows * 64 * sizeof(float) : 0);
-    c.part_defect = take(mend ? c.split_q * rows * 2 * sizeof(float) : 0);
+    c.part_sum = take(mend ? c.split_q * rows * 2 * sizeof(float) : 0);
     c.part_k = take(c.split_kv > 1 ? c.split_kv * keys * 64 * sizeof(float) : 0);
     c.part_v = take(c.split_kv > 1 ? c.split_kv * keys * 64 * sizeof(float) : 0);
     c.backward = off;
@@ -1157,7 +1157,7 @@ s3r_status speed3r_cross_attn_backward(const s3r_cross_params *p)
         if (c.split_q > 1) {
             a.part_q = floats_at(p->workspace, c.part_q);
             a.part_pk = floats_at(p->workspace, c.part_pk);
-            a.part_defect = floats_at(p->workspace, c.part_defect);
+            a.part_sum = floats_at(p->workspace, c.part_sum);
         }
         S3R_HIP(s3r::launch_grad_q(a, bf16, s), "query gradient kernel launch");
         if (c.split_q > 1) S3R_HIP(s3r::launch_grad_q_combine(a, bf16, s), "query gradient combine kernel launch");
