@@ -989,13 +989,32 @@ s3r_status check_strides(const char *what, int64_t tok, int64_t head)
     return S3R_OK;
 }
 
-// Pieces of the streamed units, where the tiles alone would not fill 256 CUs twice: at least `least` units each.
-int pieces(int64_t workgroups, int64_t units, int64_t least)
+// Pieces that the streamed units are divided into, a workgroup for each, by a model of the launch in microseconds.  A CU works through
+// n = ceil(workgroups * pieces / 256) of them, `resident` at a time; one alone on a CU takes half as long again as its share
+// of a full one.  A workgroup takes `unit_us` for each unit and two units' time to start and end; more than one piece costs a launch that
+// joins them (3.5 us) and the partial results' way to memory and back at 5 TB/s (`part_bytes` each way for a piece).
+// Measured, 1374 rows over 27480 keys, 16 heads (176 tiles): PIECES_A; 2748 rows over 10992 keys: PIECES_B.
+struct Pace { double unit_us; int resident; };
+int pieces(int64_t workgroups, int64_t units, const Pace &pace, double part_bytes)
 {
-    int64_t s = (512 + workgroups - 1) / workgroups, most = units / least;
-    if (most > 64) most = 64;
-    if (s > most) s = most;
-    return s < 1 ? 1 : static_cast<int>(s);
+    int best = 1;
+    double least = 0;
+    for (int s = 1; s <= 64 && (s == 1 || units >= 4 * s); ++s) {
+        const int64_t n = (workgroups * s + 255) / 256, rest = n % pace.resident;
+        const double share = static_cast<double>(n) + (rest == 0 ? 0.0 : 0.5 - 0.5 * static_cast<double>(rest - 1) / pace.resident);
+        const double us = share * static_cast<double>((units + s - 1) / s + 2) * pace.unit_us + (s == 1 ? 0.0 : 3.5 + s * 2 * part_bytes / 5e6);
+        if (s == 1 || us < least) { least = us; best = s; }
+    }
+    return best;
+}
+
+// The same where a workgroup holds few rows and memory binds: as many as fill 256 CUs four times over, a unit at least for each of the
+// four waves.
+int pieces_few(int64_t workgroups, int64_t units)
+{
+    int64_t s = (1024 + workgroups - 1) / workgroups;
+    if (s > units / 4) s = units / 4;
+    return s < 1 ? 1 : (s > 64 ? 64 : static_cast<int>(s));
 }
 
 struct CrossPlan {
@@ -1024,11 +1043,14 @@ s3r_status plan_cross(const s3r_cross_params *p, CrossPlan *out)
     const int64_t items = p->n_q * c.per_row, units = (p->n_kv / c.batch + 63) / 64;
     c.few_rows = items <= int64_t(16) * c.batch;
     c.tiles = s3r::most_tiles(p->n_q, c.per_row, c.few_rows ? 16 : 128, c.batch);
-    c.split = pieces(c.tiles * p->kv_heads, units, c.few_rows ? 8 : 4);
+    const bool bf16 = p->dtype == S3R_BF16;
+    const double q_bytes = 256.0 * static_cast<double>(p->n_q) * p->heads, kv_bytes = 512.0 * static_cast<double>(p->n_kv) * p->kv_heads;
+    c.split = c.few_rows ? pieces_few(c.tiles * p->kv_heads, units)
+                         : pieces(c.tiles * p->kv_heads, units, bf16 ? Pace{0.67, 4} : Pace{2.2, 1}, q_bytes);
     c.q_tiles = s3r::most_tiles(p->n_q, c.per_row, 128, c.batch);
-    c.split_q = pieces(c.q_tiles * p->kv_heads, units, 4);
+    c.split_q = pieces(c.q_tiles * p->kv_heads, units, bf16 ? Pace{1.1, 2} : Pace{5.5, 1}, bf16 ? 2 * q_bytes : q_bytes);
     c.kv_tiles = s3r::most_tiles(p->n_kv, 1, 128, c.batch);
-    c.split_kv = pieces(c.kv_tiles * p->kv_heads, (items / c.batch + 63) / 64, 4);
+    c.split_kv = pieces(c.kv_tiles * p->kv_heads, (items / c.batch + 63) / 64, bf16 ? Pace{1.3, 2} : Pace{7.3, 1}, kv_bytes);
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
     const size_t rows = static_cast<size_t>(p->n_q) * p->heads, keys = static_cast<size_t>(p->n_kv) * p->kv_heads;
@@ -1038,7 +1060,7 @@ s3r_status plan_cross(const s3r_cross_params *p, CrossPlan *out)
     off = 0;
     c.stats = take(rows * 2 * sizeof(float));
     c.part_q = take(c.split_q > 1 ? c.split_q * rows * 64 * sizeof(float) : 0);
-    const bool mend = c.split_q > 1 && p->dtype == S3R_BF16;
+    const bool mend = c.split_q > 1 && bf16;
     c.part_pk = take(mend ? c.split_q * rows * 64 * sizeof(float) : 0);
     c.part_sum = take(mend ? c.split_q * rows * sizeof(float) : 0);
     c.part_k = take(c.split_kv > 1 ? c.split_kv * keys * 64 * sizeof(float) : 0);
@@ -1208,7 +1230,9 @@ s3r_status plan_cache(const s3r_cache_params *p, CachePlan *out)
     const int64_t units = (int64_t(p->max_pages) * p->page + 63) / 64;
     c.few_rows = p->n_rows * per_row <= int64_t(16) * p->batch;
     c.tiles = s3r::most_tiles(p->n_rows, per_row, c.few_rows ? 16 : 128, p->batch);
-    c.split = pieces(c.tiles * p->kv_heads, units, c.few_rows ? 8 : 4);
+    c.split = c.few_rows ? pieces_few(c.tiles * p->kv_heads, units)
+                         : pieces(c.tiles * p->kv_heads, units, p->dtype == S3R_BF16 ? Pace{0.9, 3} : Pace{2.0, 2},
+                                  256.0 * static_cast<double>(p->n_rows) * p->heads);
     const size_t rows = static_cast<size_t>(p->n_rows) * p->heads;
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
