@@ -254,8 +254,9 @@ struct Sight {
     bool ok;
     __device__ __forceinline__ void find(const CacheArgs &a, const Share &sh, int tile, int item_in_tile)
     {
-        a.spans.of(sh.seq, first, rows);
-        len = a.cache.length(sh.seq);
+        first = sh.of.first;
+        rows = sh.of.len;
+        len = a.cache.held_length(sh.of.entry);
         const int64_t items = static_cast<int64_t>(rows) * a.per_row, item0 = static_cast<int64_t>(sh.tile) * tile, item = item0 + item_in_tile;
         ok = item < items;
         const int in_seq = static_cast<int>(item / a.per_row);
@@ -280,7 +281,7 @@ template <typename T> __global__ __launch_bounds__(256, 2) void cache_attn_kerne
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = wave & 1;
     const bool is_v = wave >= 2;
     Share sh;
-    if (!find_share(a.spans, a.per_row, 128, a.tiles, a.n_split, a.cache.kv_heads, sh)) return;
+    if (!find_share(a.spans, a.cache.kv_len, a.per_row, 128, a.tiles, a.n_split, a.cache.kv_heads, sh)) return;
     Sight sight;
     sight.find(a, sh, 128, 32 * wave + (lane & 31));
     SoftRow<P> soft;
@@ -288,7 +289,7 @@ template <typename T> __global__ __launch_bounds__(256, 2) void cache_attn_kerne
     soft.load(static_cast<const T *>(a.q) + sight.row * a.q_row + sight.head * a.q_head, sight.ok, lane);
     int u0, u1;
     piece((sight.most + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
-    PageUnits units{a.cache, sh.seq, sh.kv_head, sight.len, -1};
+    PageUnits units{a.cache, sh.of.seq, sh.kv_head, sight.len, -1};
     const uint8_t *codes = is_v ? a.cache.v_codes : a.cache.k_codes, *scales = is_v ? a.cache.v_scales : a.cache.k_scales;
     uint4 code = {};
     unsigned scale = 0;
@@ -331,14 +332,14 @@ __device__ __forceinline__ int64_t lane_value(int64_t x, int lane)
 
 // Few rows: WAVES waves with the same 16 rows take the units in turn.  Sixteen tokens of a unit lie on one page, so that a tile of keys
 // has one address for the wave.
-template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, 2) void cache_few_kernel(CacheArgs a)
+template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void cache_few_kernel(CacheArgs a)
 {
     constexpr int P = sizeof(T) == 4 ? 3 : 1;
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     bf16_t *mine = reinterpret_cast<bf16_t *>(smem) + wave * kPlane;
     Share sh;
-    if (!find_share(a.spans, a.per_row, kFewRows, a.tiles, a.n_split, a.cache.kv_heads, sh)) return;
+    if (!find_few_share(a.spans, a.cache.kv_len, a.per_row, kFewRows, a.n_split, a.cache.kv_heads, sh)) return;
     Sight sight;
     sight.find(a, sh, kFewRows, lane & 15);
     FewRows<P> few;
@@ -346,7 +347,7 @@ template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, 2) voi
     few.load(static_cast<const T *>(a.q) + sight.row * a.q_row + sight.head * a.q_head, sight.ok, lane);
     int u0, u1;
     piece((sight.most + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
-    PageUnits units{a.cache, sh.seq, sh.kv_head, sight.len, -1};
+    PageUnits units{a.cache, sh.of.seq, sh.kv_head, sight.len, -1};
     uint2 k[4] = {};
     uint4 v[2] = {};
     unsigned ks[4] = {}, vs = 0;
@@ -423,14 +424,22 @@ __global__ __launch_bounds__(1024) void cache_status_kernel(CacheArgs a, bool ap
     if (threadIdx.x == 0) *status = all;
 }
 
+template <typename T, int WAVES> hipError_t launch_few(const CacheArgs &a, int64_t n, hipStream_t stream)
+{
+    constexpr size_t kLds = WAVES * kPlane * sizeof(bf16_t);
+    const hipError_t e = allow_lds(&cache_few_kernel<T, WAVES>, kLds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((cache_few_kernel<T, WAVES>), dim3(static_cast<unsigned>(n)), dim3(64 * WAVES), kLds, stream, a);
+    return hipGetLastError();
+}
+
 template <typename T> hipError_t launch_cache_attn_t(const CacheArgs &a, bool few_rows, hipStream_t stream)
 {
-    const int64_t n = xcd_padded(a.tiles * a.n_split * a.cache.kv_heads);
+    const int64_t shares = a.tiles * a.n_split * a.cache.kv_heads, n = few_rows ? shares : xcd_padded(shares);
     if (!grid_ok(n)) return hipErrorInvalidValue;
     if (few_rows) {
-        constexpr int kWaves = 4;
-        hipLaunchKernelGGL((cache_few_kernel<T, kWaves>), dim3(static_cast<unsigned>(n)), dim3(64 * kWaves), kWaves * kPlane * sizeof(bf16_t),
-                           stream, a);
+        if (a.n_split > 1) return launch_few<T, 4>(a, n, stream);
+        return launch_few<T, sizeof(T) == 4 ? 8 : 16>(a, n, stream);
     } else {
         hipLaunchKernelGGL(cache_attn_kernel<T>, dim3(static_cast<unsigned>(n)), dim3(256), 2 * kCacheStage * sizeof(bf16_t), stream, a);
     }

@@ -33,10 +33,10 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 4) 
     bf16_t *lds = reinterpret_cast<bf16_t *>(smem);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Share sh;
-    if (!find_share(a.q_spans, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, sh)) return;
-    int q0, q_len, k0, k_len;
-    a.q_spans.of(sh.seq, q0, q_len);
-    a.kv_spans.of(sh.seq, k0, k_len);
+    if (!find_share(a.q_spans, nullptr, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, sh)) return;
+    const int q0 = sh.of.first, q_len = sh.of.len;
+    int k0, k_len;
+    a.kv_spans.of(sh.of.seq, k0, k_len);
     const int64_t item = static_cast<int64_t>(sh.tile) * kTile + 32 * wave + (lane & 31);
     const bool ok = item < static_cast<int64_t>(q_len) * a.per_row;
     const int64_t row = q0 + item / a.per_row;
@@ -60,17 +60,17 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 4) 
 }
 
 // Few rows: WAVES waves with the same 16 rows take the units in turn, values through an LDS stage of their own (8 or 24 KiB).
-template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 ? 1 : 2) void cross_few_kernel(CrossArgs a)
+template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 || WAVES > 4 ? 1 : 2) void cross_few_kernel(CrossArgs a)
 {
     constexpr int P = UnitPairs<T>::kParts;
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     bf16_t *mine = reinterpret_cast<bf16_t *>(smem) + wave * P * kPlane;
     Share sh;
-    if (!find_share(a.q_spans, a.per_row, kFewRows, a.tiles, a.n_split, a.kv_heads, sh)) return;
-    int q0, q_len, k0, k_len;
-    a.q_spans.of(sh.seq, q0, q_len);
-    a.kv_spans.of(sh.seq, k0, k_len);
+    if (!find_few_share(a.q_spans, nullptr, a.per_row, kFewRows, a.n_split, a.kv_heads, sh)) return;
+    const int q0 = sh.of.first, q_len = sh.of.len;
+    int k0, k_len;
+    a.kv_spans.of(sh.of.seq, k0, k_len);
     const int64_t item = static_cast<int64_t>(sh.tile) * kFewRows + (lane & 15);
     const bool ok = item < static_cast<int64_t>(q_len) * a.per_row;
     const int64_t row = q0 + item / a.per_row;
@@ -144,20 +144,32 @@ template <typename T, int GROUPS> __global__ __launch_bounds__(256) void soft_co
         for (int j = 0; j < n_split; ++j) top = fmaxf(top, to.part_lse[j * share + at]);
     }
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    auto add = [&](int j, float l) {
-        if (j >= n_split || l == -INFINITY) return;  // no keys in this piece
-        const float w = l == top ? 1.f : exp2f(l - top);
-        const floatx4 o = *reinterpret_cast<const floatx4 *>(to.part_o + (j * share + at) * 64 + c);
-        total += w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] += w * o[e];
-    };
     if constexpr (GROUPS == 4) {
+        floatx4 o[16];  // all on their way at once
+#pragma unroll
+        for (int s = 0; s < 16; ++s) {
+            const int j = 4 * s + group;
+            if (4 * s < n_split) o[s] = *reinterpret_cast<const floatx4 *>(to.part_o + ((j < n_split ? j : 0) * share + at) * 64 + c);
+        }
 #pragma unroll
         for (int s = 0; s < 16; ++s)
-            if (4 * s < n_split) add(4 * s + group, __shfl(mine, 4 * s + group, 64));
+            if (4 * s < n_split) {
+                const float l = __shfl(mine, 4 * s + group, 64);  // -inf: no such split, or no keys in it
+                const float w = l == -INFINITY ? 0.f : (l == top ? 1.f : fast_exp2(l - top));
+                total += w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] += w == 0.f ? 0.f : w * o[s][e];
+            }
     } else {
-        for (int j = 0; j < n_split; ++j) add(j, to.part_lse[j * share + at]);
+        for (int j = 0; j < n_split; ++j) {
+            const float l = to.part_lse[j * share + at];
+            if (l == -INFINITY) continue;  // no keys in this piece
+            const float w = l == top ? 1.f : exp2f(l - top);
+            const floatx4 o = *reinterpret_cast<const floatx4 *>(to.part_o + (j * share + at) * 64 + c);
+            total += w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] += w * o[e];
+        }
     }
     if constexpr (GROUPS == 4) {
 #pragma unroll
@@ -223,10 +235,10 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     bf16_t *lds = reinterpret_cast<bf16_t *>(smem);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Share sh;
-    if (!find_share(a.q_spans, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, sh)) return;
-    int q0, q_len, k0, k_len;
-    a.q_spans.of(sh.seq, q0, q_len);
-    a.kv_spans.of(sh.seq, k0, k_len);
+    if (!find_share(a.q_spans, nullptr, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, sh)) return;
+    const int q0 = sh.of.first, q_len = sh.of.len;
+    int k0, k_len;
+    a.kv_spans.of(sh.of.seq, k0, k_len);
     const int64_t item = static_cast<int64_t>(sh.tile) * kTile + 32 * wave + (lane & 31);
     const bool ok = item < static_cast<int64_t>(q_len) * a.per_row;
     const int64_t row = q0 + item / a.per_row;
@@ -358,10 +370,10 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     float *row_stats = reinterpret_cast<float *>(smem + sizeof(bf16_t) * UnitPairs<T>::kStages * UnitPairs<T>::kStage);  // [stages][2][64]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Share sh;
-    if (!find_share(a.kv_spans, 1, kTile, a.tiles, a.n_split, a.kv_heads, sh)) return;
-    int q0, q_len, k0, k_len;
-    a.q_spans.of(sh.seq, q0, q_len);
-    a.kv_spans.of(sh.seq, k0, k_len);
+    if (!find_share(a.kv_spans, nullptr, 1, kTile, a.tiles, a.n_split, a.kv_heads, sh)) return;
+    const int k0 = sh.of.first, k_len = sh.of.len;
+    int q0, q_len;
+    a.q_spans.of(sh.of.seq, q0, q_len);
     const int key = sh.tile * kTile + 32 * wave + (lane & 31);
     const bool ok = key < k_len, seen = ok && (a.key_mask == nullptr || a.key_mask[k0 + key] != 0);
     const int64_t row = k0 + key;
@@ -478,16 +490,23 @@ __global__ __launch_bounds__(1024) void span_status_kernel(Spans q, Spans kv, in
     if (threadIdx.x == 0) *status = bad ? kDiagSpans : 0;
 }
 
+template <typename T, int WAVES> hipError_t launch_few(const CrossArgs &a, int64_t n, hipStream_t stream)
+{
+    constexpr size_t kLds = WAVES * UnitPairs<T>::kParts * kPlane * sizeof(bf16_t);
+    const hipError_t e = allow_lds(&cross_few_kernel<T, WAVES>, kLds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((cross_few_kernel<T, WAVES>), dim3(static_cast<unsigned>(n)), dim3(64 * WAVES), kLds, stream, a);
+    return hipGetLastError();
+}
+
 template <typename T> hipError_t launch_cross_t(const CrossArgs &a, bool few_rows, hipStream_t stream)
 {
-    const int64_t n = xcd_padded(a.tiles * a.n_split * a.kv_heads);
+    const int64_t shares = a.tiles * a.n_split * a.kv_heads, n = few_rows ? shares : xcd_padded(shares);
     if (!grid_ok(n)) return hipErrorInvalidValue;
     if (few_rows) {
-        constexpr int kWaves = 4;
-        constexpr size_t kLds = kWaves * UnitPairs<T>::kParts * kPlane * sizeof(bf16_t);
-        const hipError_t e = allow_lds(&cross_few_kernel<T, kWaves>, kLds);
-        if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((cross_few_kernel<T, kWaves>), dim3(static_cast<unsigned>(n)), dim3(64 * kWaves), kLds, stream, a);
+        if constexpr (sizeof(T) == 2)
+            if (a.n_split == 1) return launch_few<T, 8>(a, n, stream);
+        return launch_few<T, 4>(a, n, stream);
     } else {
         constexpr size_t kLds = UnitPairs<T>::kStages * UnitPairs<T>::kStage * sizeof(bf16_t);
         hipLaunchKernelGGL(cross_kernel<T>, dim3(static_cast<unsigned>(n)), dim3(256), kLds, stream, a);
@@ -537,7 +556,7 @@ hipError_t launch_grad_kv(const CrossArgs &a, bool is_bf16, hipStream_t stream)
 
 hipError_t launch_soft_combine(const SoftOut &to, const Spans &spans, int n_split, bool is_bf16, hipStream_t stream)
 {
-    const bool wide = n_split >= 8;  // at most 64
+    const bool wide = n_split >= 8 && to.rows * to.heads <= 4096;  // at most 64 splits
     const int64_t blocks = (to.rows * to.heads * (wide ? 64 : 16) + 255) / 256;
     if (!grid_ok(blocks) || n_split > 64) return hipErrorInvalidValue;
     auto kernel = is_bf16 ? (wide ? &soft_combine_kernel<bf16_t, 4> : &soft_combine_kernel<bf16_t, 1>)

@@ -316,9 +316,9 @@ struct Cache {
     const int32_t *kv_len;                             // [batch]
     int64_t n_pages;
     int max_pages, page_shift, kv_heads;
-    __device__ __forceinline__ int length(int b) const
+    __device__ __forceinline__ int length(int b) const { return held_length(kv_len[b]); }
+    __device__ __forceinline__ int held_length(int n) const
     {
-        const int n = kv_len[b];
         const int64_t most = static_cast<int64_t>(max_pages) << page_shift;
         return n < 0 ? 0 : (n > most ? static_cast<int>(most) : n);
     }

@@ -148,23 +148,27 @@ __device__ __forceinline__ void multiply(floatx16 &acc, const bf16x8 (&b)[PB], F
 
 // ---- sequences and tiles -----------------------------------------------------------------------------
 
+// A workgroup's sequence: its number, its rows, and its entry of another list (or 0).
+struct Sequence { int seq, first, len, entry; };
+
 // Tile `t` of the sequences' tiles of `tile` items in turn, a sequence having len * per_row items: its sequence and number
-// in it; false when there are fewer tiles.  All lanes of a wave call it.
-__device__ __forceinline__ bool find_tile(const Spans &spans, int per_row, int tile, int64_t t, int &b, int &in_seq)
+// in it; false when there are fewer tiles.  All lanes of a wave call it.  What is needed of a sequence is read for 64 of them at once,
+// and not when the number is known: one wait less before a short launch's first key.
+__device__ __forceinline__ bool find_tile(const Spans &spans, const int32_t *list, int per_row, int tile, int64_t t, Sequence &q, int &in_seq)
 {
     if (spans.batch == 1) {
-        int first, len;
-        spans.of(0, first, len);
-        b = 0;
+        q.seq = 0;
+        q.entry = list != nullptr ? list[0] : 0;
+        spans.of(0, q.first, q.len);
         in_seq = static_cast<int>(t);
-        return t * tile < static_cast<int64_t>(len) * per_row;
+        return t * tile < static_cast<int64_t>(q.len) * per_row;
     }
     const int lane = threadIdx.x & 63;
     int64_t before = 0;
     for (int b0 = 0; b0 < spans.batch; b0 += 64) {
-        int tiles = 0;
+        int tiles = 0, first = 0, len = 0, entry = 0;
         if (b0 + lane < spans.batch) {
-            int first, len;
+            if (list != nullptr) entry = list[b0 + lane];
             spans.of(b0 + lane, first, len);
             tiles = static_cast<int>((static_cast<int64_t>(len) * per_row + tile - 1) / tile);
         }
@@ -177,13 +181,14 @@ __device__ __forceinline__ bool find_tile(const Spans &spans, int per_row, int t
         const unsigned long long past = __ballot(before + upto > t);
         if (past != 0) {
             const int l = __ffsll(past) - 1;
-            b = b0 + l;
-            in_seq = static_cast<int>(t - before - (__shfl(upto, l, 64) - __shfl(tiles, l, 64)));
-            b = __builtin_amdgcn_readfirstlane(b);
-            in_seq = __builtin_amdgcn_readfirstlane(in_seq);
+            q.seq = b0 + l;
+            q.first = __builtin_amdgcn_readlane(first, l);
+            q.len = __builtin_amdgcn_readlane(len, l);
+            q.entry = __builtin_amdgcn_readlane(entry, l);
+            in_seq = static_cast<int>(t - before) - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(tiles, l));
             return true;
         }
-        before += __shfl(upto, 63, 64);
+        before += __builtin_amdgcn_readlane(upto, 63);
     }
     return false;
 }
@@ -193,15 +198,26 @@ __device__ __forceinline__ int64_t xcd_neighbours(int64_t bid, int64_t n) { retu
 inline int64_t xcd_padded(int64_t n) { return (n + 7) / 8 * 8; }
 
 // A workgroup's share of the grid: a tile of the held rows, a head of keys, one of n_split pieces of the streamed units.
-struct Share { int seq, tile, kv_head, split; };
+struct Share { Sequence of; int tile, kv_head, split; };
 
-__device__ __forceinline__ bool find_share(const Spans &spans, int per_row, int tile, int64_t tiles, int n_split, int kv_heads, Share &s)
+// Tiles of few rows share no keys with their neighbours, and may be a CU's only ones: those that `tiles` counts and the sequences do
+// not have come last, so that every XCD has as many real ones.
+__device__ __forceinline__ bool find_few_share(const Spans &spans, const int32_t *list, int per_row, int tile, int n_split, int kv_heads, Share &s)
+{
+    const unsigned each = static_cast<unsigned>(n_split) * static_cast<unsigned>(kv_heads), t = blockIdx.x / each, rest = blockIdx.x - t * each;
+    s.kv_head = static_cast<int>(rest / static_cast<unsigned>(n_split));
+    s.split = static_cast<int>(rest) - s.kv_head * n_split;
+    return find_tile(spans, list, per_row, tile, t, s.of, s.tile);
+}
+
+__device__ __forceinline__ bool find_share(const Spans &spans, const int32_t *list, int per_row, int tile, int64_t tiles, int n_split, int kv_heads,
+                                           Share &s)
 {
     const int64_t item = xcd_neighbours(blockIdx.x, tiles * n_split * kv_heads);
     const int64_t rest = item / tiles;
     s.split = static_cast<int>(rest % n_split);
     s.kv_head = static_cast<int>(rest / n_split);
-    return s.kv_head < kv_heads && find_tile(spans, per_row, tile, item - rest * tiles, s.seq, s.tile);
+    return s.kv_head < kv_heads && find_tile(spans, list, per_row, tile, item - rest * tiles, s.of, s.tile);
 }
 
 __device__ __forceinline__ void piece(int units, int n_split, int split, int &u0, int &u1)

@@ -1008,10 +1008,11 @@ int pieces(int64_t workgroups, int64_t units, const Pace &pace, double part_byte
     return best;
 }
 
-// The same where a workgroup holds few rows and memory binds: as many as fill 256 CUs four times over, a unit at least for each of the
-// four waves.
+// The same where a workgroup holds few rows and memory binds: none where there are workgroups for most CUs (the launch then takes more
+// waves in each), else as many as fill 256 CUs four times over, a unit at least for each of the four waves.
 int pieces_few(int64_t workgroups, int64_t units)
 {
+    if (workgroups >= 192) return 1;
     int64_t s = (1024 + workgroups - 1) / workgroups;
     if (s > units / 4) s = units / 4;
     return s < 1 ? 1 : (s > 64 ? 64 : static_cast<int>(s));
