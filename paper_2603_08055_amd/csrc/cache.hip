@@ -224,16 +224,38 @@ template <typename T> __global__ __launch_bounds__(256) void cache_read_kernel(C
 // NaN are put as zeros and told apart by a word per 32 channels, because only rows that see their token may become NaN.
 constexpr int kCacheStage = 2 * kPlane + 32;  // bf16 elements: keys, values, two 64-bit words and room to stay aligned
 
-struct PageUnits {
+// A page of 64 tokens and more (WIDE) holds whole units: its number and all addresses but a constant per lane are then scalars (one
+// token over 137400 cached 34.2 -> 32.3 us; with many rows, where the matrix and vector units bind, no difference).
+template <bool WIDE> struct PageUnits {
     Cache cache;
     int seq, kv_head, len;
-    int64_t next;  // where the lane's token of the unit to be fetched next is; -1: nowhere
+    int64_t next;  // of the unit to be fetched next: the lane's place in the cache, head 0's; WIDE: the unit's.  -1: nowhere
+    bool there;    // the lane's token of the unit that was fetched
     __device__ __forceinline__ void find(int unit, int lane)
     {
-        const int t = unit * kUnitRows + lane;
+        const int t = unit * kUnitRows + (WIDE ? 0 : lane);
         next = t < len ? cache.slot(seq, t) : -1;
     }
-    __device__ __forceinline__ int64_t head_slot() const { return next + (static_cast<int64_t>(kv_head) << cache.page_shift); }
+    // Byte offset of the unit's codes in the arrays of codes: from here a lane's are lane * 32 further (WIDE), or here.
+    __device__ __forceinline__ int64_t fetch(int unit, int lane)
+    {
+        there = next >= 0 && (!WIDE || unit * kUnitRows + lane < len);
+        return (next + (static_cast<int64_t>(kv_head) << cache.page_shift)) * 32;
+    }
+    // The same of 16 tokens, which lie on one page; a tile that is nowhere reads the first page instead, and counts for nothing.
+    __device__ __forceinline__ int64_t tile(int t) const
+    {
+        int64_t at = next;
+        if constexpr (WIDE) {
+            at = (at < 0 ? 0 : at) + 16 * t;
+        } else {
+            const unsigned lo = __builtin_amdgcn_readlane(static_cast<unsigned>(at), 16 * t), hi = __builtin_amdgcn_readlane(static_cast<unsigned>(at >> 32), 16 * t);
+            at = static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+            at = at < 0 ? 0 : at;
+        }
+        return (at + (static_cast<int64_t>(kv_head) << cache.page_shift)) * 32;
+    }
+    static __device__ __forceinline__ int lane_bytes(int lane) { return WIDE ? lane * 32 : 0; }
 };
 
 // 32 channels of a lane's token, as bf16 to a unit in LDS; not `ok`: zeros.
@@ -278,10 +300,10 @@ template <typename T> __global__ __launch_bounds__(256, 2) void cache_attn_kerne
     constexpr int P = sizeof(T) == 4 ? 3 : 1;
     extern __shared__ __align__(16) unsigned char smem[];
     bf16_t *lds = reinterpret_cast<bf16_t *>(smem);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = wave & 1;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = wave & 1;
     const bool is_v = wave >= 2;
     Share sh;
-    if (!find_share(a.spans, a.cache.kv_len, a.per_row, 128, a.tiles, a.n_split, a.cache.kv_heads, sh)) return;
+    if (!find_share(a.spans, a.cache.kv_len, a.per_row, 128, a.tiles, a.n_split, a.cache.kv_heads, sh, a.causal)) return;
     Sight sight;
     sight.find(a, sh, 128, 32 * wave + (lane & 31));
     SoftRow<P> soft;
@@ -289,29 +311,28 @@ template <typename T> __global__ __launch_bounds__(256, 2) void cache_attn_kerne
     soft.load(static_cast<const T *>(a.q) + sight.row * a.q_row + sight.head * a.q_head, sight.ok, lane);
     int u0, u1;
     piece((sight.most + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
-    PageUnits units{a.cache, sh.of.seq, sh.kv_head, sight.len, -1};
+    PageUnits<false> units{a.cache, sh.of.seq, sh.kv_head, sight.len, -1, false};
     const uint8_t *codes = is_v ? a.cache.v_codes : a.cache.k_codes, *scales = is_v ? a.cache.v_scales : a.cache.k_scales;
     uint4 code = {};
     unsigned scale = 0;
-    bool there = false;
-    auto fetch = [&]() {
-        there = units.next >= 0;
-        if (!there) return;
-        code = *reinterpret_cast<const uint4 *>(codes + units.head_slot() * 32 + 16 * half);
-        scale = scales[units.head_slot() * 2 + half];
+    auto fetch = [&](int u) {
+        const int64_t from = units.fetch(u, lane);
+        if (!units.there) return;
+        code = *reinterpret_cast<const uint4 *>(codes + from + (units.lane_bytes(lane) + 16 * half));
+        scale = (scales + from / 16)[units.lane_bytes(lane) / 16 + half];
     };
     const UnitLanes at(lane);
-    if (u0 < u1) { units.find(u0, lane); fetch(); units.find(u0 + 1, lane); }
+    if (u0 < u1) { units.find(u0, lane); fetch(u0); units.find(u0 + 1, lane); }
     for (int u = u0; u < u1; ++u) {
         bf16_t *stage = lds + ((u - u0) & 1) * kCacheStage;
         unsigned long long *words = reinterpret_cast<unsigned long long *>(stage + 2 * kPlane);
-        const bool none = is_v && there && scale == 255u;
-        put_block(stage + (is_v ? kPlane : 0), lane, half, code, scale, there && !none);
+        const bool none = is_v && units.there && scale == 255u;
+        put_block(stage + (is_v ? kPlane : 0), lane, half, code, scale, units.there && !none);
         const unsigned long long w = __ballot(none);
         if (is_v && lane == 0) words[half] = w;
-        const unsigned long long seen = __ballot(there) & low_bits(sight.sees - u * kUnitRows);
+        const unsigned long long seen = __ballot(units.there) & low_bits(sight.sees - u * kUnitRows);
         __syncthreads();
-        if (u + 1 < u1) { fetch(); units.find(u + 2, lane); }
+        if (u + 1 < u1) { fetch(u + 1); units.find(u + 2, lane); }
         soft.template unit<1>(stage, stage + kPlane, seen, a.factor, at, lane);
 #pragma unroll
         for (int dt = 0; dt < 2; ++dt) {
@@ -324,19 +345,12 @@ template <typename T> __global__ __launch_bounds__(256, 2) void cache_attn_kerne
     store_soft<T>(soft, a.factor, a.to, sh.split, sight.row, sight.head, sight.ok, lane);
 }
 
-__device__ __forceinline__ int64_t lane_value(int64_t x, int lane)
-{
-    const unsigned lo = __builtin_amdgcn_readlane(static_cast<unsigned>(x), lane), hi = __builtin_amdgcn_readlane(static_cast<unsigned>(x >> 32), lane);
-    return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
-}
-
-// Few rows: WAVES waves with the same 16 rows take the units in turn.  Sixteen tokens of a unit lie on one page, so that a tile of keys
-// has one address for the wave.
-template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void cache_few_kernel(CacheArgs a)
+// Few rows: WAVES waves with the same 16 rows take the units in turn.
+template <typename T, int WAVES, bool WIDE> __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void cache_few_kernel(CacheArgs a)
 {
     constexpr int P = sizeof(T) == 4 ? 3 : 1;
     extern __shared__ __align__(16) unsigned char smem[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     bf16_t *mine = reinterpret_cast<bf16_t *>(smem) + wave * kPlane;
     Share sh;
     if (!find_few_share(a.spans, a.cache.kv_len, a.per_row, kFewRows, a.n_split, a.cache.kv_heads, sh)) return;
@@ -347,38 +361,36 @@ template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, WAVES 
     few.load(static_cast<const T *>(a.q) + sight.row * a.q_row + sight.head * a.q_head, sight.ok, lane);
     int u0, u1;
     piece((sight.most + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
-    PageUnits units{a.cache, sh.of.seq, sh.kv_head, sight.len, -1};
+    PageUnits<WIDE> units{a.cache, sh.of.seq, sh.kv_head, sight.len, -1, false};
     uint2 k[4] = {};
     uint4 v[2] = {};
     unsigned ks[4] = {}, vs = 0;
-    bool there = false;
-    auto fetch = [&]() {
-        there = units.next >= 0;
+    auto fetch = [&](int u) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {  // a tile that is nowhere reads the first page instead, and counts for nothing
-            int64_t slot = lane_value(units.next, 16 * t);
-            slot = (slot < 0 ? 0 : slot) + (static_cast<int64_t>(sh.kv_head) << a.cache.page_shift);
-            k[t] = *reinterpret_cast<const uint2 *>(a.cache.k_codes + slot * 32 + ((lane & 15) * 32 + (lane >> 4) * 8));
-            ks[t] = (a.cache.k_scales + slot * 2)[(lane & 15) * 2 + (lane >> 5)];
+        for (int t = 0; t < 4; ++t) {
+            const int64_t from = units.tile(t);
+            k[t] = *reinterpret_cast<const uint2 *>(a.cache.k_codes + from + ((lane & 15) * 32 + (lane >> 4) * 8));
+            ks[t] = (a.cache.k_scales + from / 16)[(lane & 15) * 2 + (lane >> 5)];
         }
-        if (!there) return;
-        const uint8_t *codes = a.cache.v_codes + units.head_slot() * 32;
+        const int64_t from = units.fetch(u, lane);
+        if (!units.there) return;
+        const uint8_t *codes = a.cache.v_codes + from + units.lane_bytes(lane);
         v[0] = *reinterpret_cast<const uint4 *>(codes);
         v[1] = *reinterpret_cast<const uint4 *>(codes + 16);
-        vs = *reinterpret_cast<const unsigned short *>(a.cache.v_scales + units.head_slot() * 2);
+        vs = *reinterpret_cast<const unsigned short *>(a.cache.v_scales + from / 16 + units.lane_bytes(lane) / 16);
     };
     int u = u0 + wave;
-    if (u < u1) { units.find(u, lane); fetch(); units.find(u + WAVES, lane); }
+    if (u < u1) { units.find(u, lane); fetch(u); units.find(u + WAVES, lane); }
     for (; u < u1; u += WAVES) {
         unsigned long long nan[2];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const unsigned scale = (vs >> (8 * half)) & 255u;
-            const bool none = there && scale == 255u;
-            put_block(mine, lane, half, v[half], scale, there && !none);
+            const bool none = units.there && scale == 255u;
+            put_block(mine, lane, half, v[half], scale, units.there && !none);
             nan[half] = __ballot(none);
         }
-        const unsigned long long seen = __ballot(there) & low_bits(sight.sees - u * kUnitRows);
+        const unsigned long long seen = __ballot(units.there) & low_bits(sight.sees - u * kUnitRows);
         bf16x8 kk[4][2];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -386,7 +398,7 @@ template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, WAVES 
             kk[t][1] = values8(k[t].y, ks[t]);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (u + WAVES < u1) { fetch(); units.find(u + 2 * WAVES, lane); }
+        if (u + WAVES < u1) { fetch(u + WAVES); units.find(u + 2 * WAVES, lane); }
         few.template unit<1>([&](int t, int s, bf16x8(&to)[1]) { to[0] = kk[t][s]; }, mine, seen, a.factor, lane);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
@@ -424,12 +436,12 @@ __global__ __launch_bounds__(1024) void cache_status_kernel(CacheArgs a, bool ap
     if (threadIdx.x == 0) *status = all;
 }
 
-template <typename T, int WAVES> hipError_t launch_few(const CacheArgs &a, int64_t n, hipStream_t stream)
+template <typename T, int WAVES, bool WIDE> hipError_t launch_few(const CacheArgs &a, int64_t n, hipStream_t stream)
 {
     constexpr size_t kLds = WAVES * kPlane * sizeof(bf16_t);
-    const hipError_t e = allow_lds(&cache_few_kernel<T, WAVES>, kLds);
+    const hipError_t e = allow_lds(&cache_few_kernel<T, WAVES, WIDE>, kLds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((cache_few_kernel<T, WAVES>), dim3(static_cast<unsigned>(n)), dim3(64 * WAVES), kLds, stream, a);
+    hipLaunchKernelGGL((cache_few_kernel<T, WAVES, WIDE>), dim3(static_cast<unsigned>(n)), dim3(64 * WAVES), kLds, stream, a);
     return hipGetLastError();
 }
 
@@ -438,11 +450,12 @@ template <typename T> hipError_t launch_cache_attn_t(const CacheArgs &a, bool fe
     const int64_t shares = a.tiles * a.n_split * a.cache.kv_heads, n = few_rows ? shares : xcd_padded(shares);
     if (!grid_ok(n)) return hipErrorInvalidValue;
     if (few_rows) {
-        if (a.n_split > 1) return launch_few<T, 4>(a, n, stream);
-        return launch_few<T, sizeof(T) == 4 ? 8 : 16>(a, n, stream);
-    } else {
-        hipLaunchKernelGGL(cache_attn_kernel<T>, dim3(static_cast<unsigned>(n)), dim3(256), 2 * kCacheStage * sizeof(bf16_t), stream, a);
+        constexpr int kMany = sizeof(T) == 4 ? 8 : 16;
+        if (a.cache.page_shift >= 6)
+            return a.n_split > 1 ? launch_few<T, 4, true>(a, n, stream) : launch_few<T, kMany, true>(a, n, stream);
+        return a.n_split > 1 ? launch_few<T, 4, false>(a, n, stream) : launch_few<T, kMany, false>(a, n, stream);
     }
+    hipLaunchKernelGGL(cache_attn_kernel<T>, dim3(static_cast<unsigned>(n)), dim3(256), 2 * kCacheStage * sizeof(bf16_t), stream, a);
     return hipGetLastError();
 }
 

@@ -210,14 +210,16 @@ __device__ __forceinline__ bool find_few_share(const Spans &spans, const int32_t
     return find_tile(spans, list, per_row, tile, t, s.of, s.tile);
 }
 
+// last_first: a head's tiles from the last one on (causal rows: those that see most begin, and the short ones fill up the end).
 __device__ __forceinline__ bool find_share(const Spans &spans, const int32_t *list, int per_row, int tile, int64_t tiles, int n_split, int kv_heads,
-                                           Share &s)
+                                           Share &s, bool last_first = false)
 {
     const int64_t item = xcd_neighbours(blockIdx.x, tiles * n_split * kv_heads);
     const int64_t rest = item / tiles;
     s.split = static_cast<int>(rest % n_split);
     s.kv_head = static_cast<int>(rest / n_split);
-    return s.kv_head < kv_heads && find_tile(spans, list, per_row, tile, item - rest * tiles, s.of, s.tile);
+    const int64_t t = item - rest * tiles;
+    return s.kv_head < kv_heads && find_tile(spans, list, per_row, tile, last_first ? tiles - 1 - t : t, s.of, s.tile);
 }
 
 __device__ __forceinline__ void piece(int units, int n_split, int split, int &u0, int &u1)
