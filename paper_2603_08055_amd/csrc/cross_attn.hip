@@ -26,7 +26,7 @@ __device__ __forceinline__ CountedRows counted(const CrossArgs &a, int first, in
 }
 
 // Many rows: four waves hold 32 rows each and share every unit.
-template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 4) void cross_kernel(CrossArgs a)
+template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) void cross_kernel(CrossArgs a)
 {
     constexpr int P = UnitPairs<T>::kParts;
     extern __shared__ __align__(16) unsigned char smem[];
@@ -198,27 +198,6 @@ template <typename T, int GROUPS> __global__ __launch_bounds__(256) void soft_co
 // which the bound of a gradient's error has room for, and takes 10 % of the kernel (563 -> 624 us).
 template <typename T> constexpr bool kMendD = sizeof(T) == 2;
 
-// What the gradient needs of every row of a head: its log-sum (in log2; +inf where it saw no keys, so that every probability is 0) and
-// -D, D = out . d_out.  16 threads for a row of a head.
-template <typename T>
-__global__ __launch_bounds__(256) void row_stats_kernel(const T *__restrict__ out, const T *__restrict__ d_out,
-                                                        const float *__restrict__ lse, float *__restrict__ stats, int64_t rows, int heads)
-{
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, at = i >> 4;
-    if (at >= rows * heads) return;
-    const int c = static_cast<int>(i & 15) * 4;
-    float d = 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) d += to_float(out[at * 64 + c + e]) * to_float(d_out[at * 64 + c + e]);
-#pragma unroll
-    for (int m = 1; m < 16; m <<= 1) d += __shfl_xor(d, m, 64);
-    if (c != 0) return;
-    const int64_t row = at / heads, to = (at - row * heads) * rows + row;
-    const float l = lse[to];
-    stats[2 * to] = l == -INFINITY ? INFINITY : l * kLog2e;
-    stats[2 * to + 1] = -d;
-}
-
 __device__ __forceinline__ float sum8(const bf16x8 &x)
 {
     const bf16x2 one = {static_cast<bf16_t>(1.f), static_cast<bf16_t>(1.f)};
@@ -248,9 +227,25 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     held.load(static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head, ok, lane);
     grad.clear();
     grad.load(static_cast<const T *>(a.d_out) + (row * a.heads + head) * 64, ok, lane);
+    // What the gradient of keys needs of the row as well: its log-sum, in log2 (+inf where it saw no keys, so that every probability is
+    // 0), and -D, D = out . d_out.
     float l2 = INFINITY, d = 0.f, sum = 0.f;  // d: -D
     float *stats = a.stats + 2 * (head * a.n_q + row);
-    if (ok) { l2 = stats[0]; d = stats[1]; }
+    if (ok) {
+        const T *o = static_cast<const T *>(a.to.out) + (row * a.heads + head) * 64, *g = static_cast<const T *>(a.d_out) + (row * a.heads + head) * 64;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            float x[8], y[8];
+            load8(o + 16 * s + 8 * (lane >> 5), x);
+            load8(g + 16 * s + 8 * (lane >> 5), y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) d = fmaf(-x[j], y[j], d);
+        }
+        const float l = a.to.lse[head * a.n_q + row];
+        l2 = l == -INFINITY ? INFINITY : l * kLog2e;
+    }
+    d = sum_with_other_half(d);
+    if (ok && lane < 32 && sh.split == 0) { stats[0] = l2; stats[1] = d; }
     int u0, u1;
     piece((k_len + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
     auto units = key_units<T>(a, sh.kv_head, k0, k_len, lds);
@@ -470,15 +465,15 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     }
 }
 
-// out = the sum of n_split partial results, for the rows of the sequences.  16 threads for a row of a head.
-template <typename T>
-__global__ __launch_bounds__(256) void add_parts_kernel(const float *__restrict__ part, T *__restrict__ out, Spans spans, int64_t rows,
-                                                        int heads, int n_split)
+// dk and dv as the sums of their pieces over queries.  16 threads for a row of a head; blockIdx.y: dk or dv.
+template <typename T> __global__ __launch_bounds__(256) void grad_kv_combine_kernel(CrossArgs a)
 {
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, n = rows * heads * 16;
-    if (i >= n || !spans.covers(i / (heads * 16))) return;
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, n = a.n_kv * a.kv_heads * 16;
+    if (i >= n || !a.kv_spans.covers(i / (a.kv_heads * 16))) return;
+    const float *part = blockIdx.y == 0 ? a.part_k : a.part_v;
+    T *out = static_cast<T *>(blockIdx.y == 0 ? a.dk : a.dv);
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < n_split; ++j) acc += *reinterpret_cast<const floatx4 *>(part + (j * n + i) * 4);
+    for (int j = 0; j < a.n_split; ++j) acc += *reinterpret_cast<const floatx4 *>(part + (j * n + i) * 4);
 #pragma unroll
     for (int e = 0; e < 4; ++e) out[i * 4 + e] = from_float<T>(acc[e]);
 }
@@ -565,31 +560,15 @@ hipError_t launch_soft_combine(const SoftOut &to, const Spans &spans, int n_spli
     return hipGetLastError();
 }
 
-hipError_t launch_row_stats(const void *out, const void *d_out, const float *lse, float *stats, int64_t rows, int heads, bool is_bf16,
-                            hipStream_t stream)
+hipError_t launch_grad_kv_combine(const CrossArgs &a, bool is_bf16, hipStream_t stream)
 {
-    const int64_t blocks = (rows * heads * 16 + 255) / 256;
-    if (!grid_ok(blocks)) return hipErrorInvalidValue;
+    const int64_t blocks = (a.n_kv * a.kv_heads * 16 + 255) / 256;
+    if (!grid_ok(2 * blocks)) return hipErrorInvalidValue;
+    const dim3 grid(static_cast<unsigned>(blocks), 2);
     if (is_bf16)
-        hipLaunchKernelGGL(row_stats_kernel<bf16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
-                           static_cast<const bf16_t *>(out), static_cast<const bf16_t *>(d_out), lse, stats, rows, heads);
+        hipLaunchKernelGGL(grad_kv_combine_kernel<bf16_t>, grid, dim3(256), 0, stream, a);
     else
-        hipLaunchKernelGGL(row_stats_kernel<float>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
-                           static_cast<const float *>(out), static_cast<const float *>(d_out), lse, stats, rows, heads);
-    return hipGetLastError();
-}
-
-hipError_t launch_add_parts(const float *part, void *out, const Spans &spans, int64_t rows, int heads, int n_split, bool is_bf16,
-                            hipStream_t stream)
-{
-    const int64_t blocks = (rows * heads * 16 + 255) / 256;
-    if (!grid_ok(blocks)) return hipErrorInvalidValue;
-    if (is_bf16)
-        hipLaunchKernelGGL(add_parts_kernel<bf16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, part,
-                           static_cast<bf16_t *>(out), spans, rows, heads, n_split);
-    else
-        hipLaunchKernelGGL(add_parts_kernel<float>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, part,
-                           static_cast<float *>(out), spans, rows, heads, n_split);
+        hipLaunchKernelGGL(grad_kv_combine_kernel<float>, grid, dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 

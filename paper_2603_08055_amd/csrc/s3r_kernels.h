@@ -278,7 +278,7 @@ struct SoftOut {
 constexpr int kDiagPage = 4, kDiagSpans = 8, kDiagLength = 16, kDiagPosition = 32;
 
 // q and d_out rows, k and v rows: element strides between rows and between heads.  per_row = heads / kv_heads.  factor = scale * log2(e).
-// tiles: most tiles of the held rows (most_tiles); n_split: pieces of the streamed rows.  stats: see launch_row_stats.  part_*: partial
+// tiles: most tiles of the held rows (most_tiles); n_split: pieces of the streamed rows.  stats: see launch_grad_q.  part_*: partial
 // sums [n_split][rows][heads][64] where n_split > 1, else null (part_sum: [n_split][rows][heads]; it and part_pk for bf16 alone).
 struct CrossArgs {
     const void *q, *k, *v, *d_out;
@@ -297,15 +297,13 @@ struct CrossArgs {
 // few_rows: a workgroup's waves divide the keys of 16 rows, and not 128 rows, among them (tiles accordingly).
 hipError_t launch_cross(const CrossArgs &a, bool few_rows, bool is_bf16, hipStream_t stream);
 hipError_t launch_soft_combine(const SoftOut &to, const Spans &spans, int n_split, bool is_bf16, hipStream_t stream);
-// stats [heads][rows][2]: log-sum in log2 (+inf for a row without keys) and -(out . d_out)
-hipError_t launch_row_stats(const void *out, const void *d_out, const float *lse, float *stats, int64_t rows, int heads, bool is_bf16,
-                            hipStream_t stream);
-// bf16: D in stats is made whole, for launch_grad_kv, which comes after (n_split > 1: by the combine launch).
+// The gradient of queries comes first: it leaves stats [heads][n_q][2], of every row its log-sum in log2 (+inf for a row without keys)
+// and -(out . d_out), from to.out, to.lse and d_out.
+// bf16: D in stats is made whole there (n_split > 1: by the combine launch).
 hipError_t launch_grad_q(const CrossArgs &a, bool is_bf16, hipStream_t stream);
 hipError_t launch_grad_q_combine(const CrossArgs &a, bool is_bf16, hipStream_t stream);
 hipError_t launch_grad_kv(const CrossArgs &a, bool is_bf16, hipStream_t stream);
-hipError_t launch_add_parts(const float *part, void *out, const Spans &spans, int64_t rows, int heads, int n_split, bool is_bf16,
-                            hipStream_t stream);
+hipError_t launch_grad_kv_combine(const CrossArgs &a, bool is_bf16, hipStream_t stream);
 hipError_t launch_span_status(const Spans &q, const Spans &kv, int *status, hipStream_t stream);
 
 // A cache of keys and values in 4 bits: pages of `page` = 2^page_shift tokens; of every token and head 32 bytes of codes (64 channels of

@@ -992,20 +992,26 @@ s3r_status check_strides(const char *what, int64_t tok, int64_t head)
 // Pieces that the streamed units are divided into, a workgroup for each, by a model of the launch in microseconds.  A CU works through
 // n = ceil(workgroups * pieces / 256) of them, `resident` at a time; one alone on a CU takes half as long again as its share
 // of a full one.  A workgroup takes `unit_us` for each unit and two units' time to start and end; more than one piece costs a launch that
-// joins them (3.5 us) and the partial results' way to memory and back at 5 TB/s (`part_bytes` each way for a piece).
+// joins them (3.5 us, and `part_bytes` of partial results for a piece at 5 TB/s; their way out is under the work).  A piece has
+// `least` units or more.
 // Measured, 1374 rows over 27480 keys, 16 heads (176 tiles): PIECES_A; 2748 rows over 10992 keys: PIECES_B.
-struct Pace { double unit_us; int resident; };
+struct Pace { double unit_us; int resident, least; };
 int pieces(int64_t workgroups, int64_t units, const Pace &pace, double part_bytes)
 {
-    int best = 1;
-    double least = 0;
-    for (int s = 1; s <= 64 && (s == 1 || units >= 4 * s); ++s) {
+    auto time_us = [&](int s) {
         const int64_t n = (workgroups * s + 255) / 256, rest = n % pace.resident;
         const double share = static_cast<double>(n) + (rest == 0 ? 0.0 : 0.5 - 0.5 * static_cast<double>(rest - 1) / pace.resident);
-        const double us = share * static_cast<double>((units + s - 1) / s + 2) * pace.unit_us + (s == 1 ? 0.0 : 3.5 + s * 2 * part_bytes / 5e6);
-        if (s == 1 || us < least) { least = us; best = s; }
+        return share * static_cast<double>((units + s - 1) / s + 2) * pace.unit_us + (s == 1 ? 0.0 : 3.5 + s * part_bytes / 5e6);
+    };
+    int most = 1;
+    double shortest = time_us(1);
+    while (most < 64 && units >= static_cast<int64_t>(pace.least) * (most + 1)) {
+        const double us = time_us(++most);
+        if (us < shortest) shortest = us;
     }
-    return best;
+    for (int s = 1; s < most; ++s)
+        if (time_us(s) <= 1.01 * shortest) return s;  // the fewest that come within 1 %: their partial results take workspace
+    return most;
 }
 
 // The same where a workgroup holds few rows and memory binds: none where there are workgroups for most CUs (the launch then takes more
@@ -1041,17 +1047,18 @@ s3r_status plan_cross(const s3r_cross_params *p, CrossPlan *out)
     c.per_row = p->heads / p->kv_heads;
     if (p->n_q > kMaxRowHeads / p->heads || p->n_kv > kMaxRowHeads / p->kv_heads || c.batch > (1 << 22) / p->kv_heads)
         return fail(S3R_ERR_UNSUPPORTED, "rows * heads exceeds 2^28, or batch * kv_heads 2^22");
-    const int64_t items = p->n_q * c.per_row, units = (p->n_kv / c.batch + 63) / 64;
+    // (of ragged sequences the longest counts, and only their sum is known here)
+    const int64_t items = p->n_q * c.per_row, ragged = c.batch > 1 ? 2 : 1, units = (ragged * p->n_kv / c.batch + 63) / 64;
     c.few_rows = items <= int64_t(16) * c.batch;
     c.tiles = s3r::most_tiles(p->n_q, c.per_row, c.few_rows ? 16 : 128, c.batch);
     const bool bf16 = p->dtype == S3R_BF16;
     const double q_bytes = 256.0 * static_cast<double>(p->n_q) * p->heads, kv_bytes = 512.0 * static_cast<double>(p->n_kv) * p->kv_heads;
     c.split = c.few_rows ? pieces_few(c.tiles * p->kv_heads, units)
-                         : pieces(c.tiles * p->kv_heads, units, bf16 ? Pace{0.67, 4} : Pace{2.2, 1}, q_bytes);
+                         : pieces(c.tiles * p->kv_heads, units, bf16 ? Pace{0.67, 4, 4} : Pace{2.2, 2, 1}, q_bytes);
     c.q_tiles = s3r::most_tiles(p->n_q, c.per_row, 128, c.batch);
-    c.split_q = pieces(c.q_tiles * p->kv_heads, units, bf16 ? Pace{1.1, 2} : Pace{5.5, 1}, bf16 ? 2 * q_bytes : q_bytes);
+    c.split_q = pieces(c.q_tiles * p->kv_heads, units, bf16 ? Pace{1.1, 2, 4} : Pace{5.5, 1, 1}, bf16 ? 2 * q_bytes : q_bytes);
     c.kv_tiles = s3r::most_tiles(p->n_kv, 1, 128, c.batch);
-    c.split_kv = pieces(c.kv_tiles * p->kv_heads, (items / c.batch + 63) / 64, bf16 ? Pace{1.3, 2} : Pace{7.3, 1}, kv_bytes);
+    c.split_kv = pieces(c.kv_tiles * p->kv_heads, (ragged * items / c.batch + 63) / 64, bf16 ? Pace{1.3, 2, 4} : Pace{7.3, 1, 1}, kv_bytes);
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
     const size_t rows = static_cast<size_t>(p->n_q) * p->heads, keys = static_cast<size_t>(p->n_kv) * p->kv_heads;
@@ -1174,7 +1181,6 @@ s3r_status speed3r_cross_attn_backward(const s3r_cross_params *p)
     a.dq = p->dq; a.dk = p->dk; a.dv = p->dv;
     StageTimer tm(S3R_STAGE_DENSE, s);
     if (p->n_q > 0) {
-        S3R_HIP(s3r::launch_row_stats(p->out, p->d_out, p->lse, stats, p->n_q, p->heads, bf16, s), "row statistics kernel launch");
         a.tiles = c.q_tiles;
         a.n_split = c.split_q;
         if (c.split_q > 1) {
@@ -1193,10 +1199,7 @@ s3r_status speed3r_cross_attn_backward(const s3r_cross_params *p)
             a.part_v = floats_at(p->workspace, c.part_v);
         }
         S3R_HIP(s3r::launch_grad_kv(a, bf16, s), "key gradient kernel launch");
-        if (c.split_kv > 1) {
-            S3R_HIP(s3r::launch_add_parts(a.part_k, p->dk, a.kv_spans, p->n_kv, p->kv_heads, c.split_kv, bf16, s), "key gradient sum launch");
-            S3R_HIP(s3r::launch_add_parts(a.part_v, p->dv, a.kv_spans, p->n_kv, p->kv_heads, c.split_kv, bf16, s), "value gradient sum launch");
-        }
+        if (c.split_kv > 1) S3R_HIP(s3r::launch_grad_kv_combine(a, bf16, s), "key gradient combine kernel launch");
     }
     return S3R_OK;
 }
@@ -1232,7 +1235,7 @@ s3r_status plan_cache(const s3r_cache_params *p, CachePlan *out)
     c.few_rows = p->n_rows * per_row <= int64_t(16) * p->batch;
     c.tiles = s3r::most_tiles(p->n_rows, per_row, c.few_rows ? 16 : 128, p->batch);
     c.split = c.few_rows ? pieces_few(c.tiles * p->kv_heads, units)
-                         : pieces(c.tiles * p->kv_heads, units, p->dtype == S3R_BF16 ? Pace{0.9, 3} : Pace{2.0, 2},
+                         : pieces(c.tiles * p->kv_heads, units, p->dtype == S3R_BF16 ? Pace{0.85, 3, 4} : Pace{2.0, 2, 1},
                                   256.0 * static_cast<double>(p->n_rows) * p->heads);
     const size_t rows = static_cast<size_t>(p->n_rows) * p->heads;
     size_t off = 0;
