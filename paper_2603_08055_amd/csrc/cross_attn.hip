@@ -192,10 +192,10 @@ template <typename T, int GROUPS> __global__ __launch_bounds__(256) void soft_co
 
 // D from the stored out: in bf16 it is off by the rounding of out, the same amount for all keys of a row, and that would be most of the
 // error of dq and dk (three times all other roundings together at 2748 rows over 10992 keys).  The dS of a row add up to 0 over all
-// keys: what they do add up to, as they enter the product and in fp32, is what D lacks and what the roundings of dS have in common.
-// The query gradient takes it out of its own result, dS k - sum(dS) * P k, and puts it into D for the gradient of keys.  One product
-// more of eight (5.1e-3 -> 2.4e-3 against 64 bits).  A sum of dS before their rounding would leave D without the sum of the roundings,
-// which the bound of a gradient's error has room for, and takes 10 % of the kernel (563 -> 624 us).
+// keys: what they do add up to in fp32 is what D lacks, and goes into D for the gradient of keys.  What they add up to as they enter
+// the product, rounded, has the roundings in it as well; the query gradient takes that out of its own result, dS k - sum(dS) * P k.
+// One product more of eight.  Against 64 bits, dq of 2748 rows over 10992 keys: 5.1e-3 without, 3.1e-3 with the former sum, 2.3e-3 with
+// the latter; dk of short sequences with the latter in D 2.7e-3.  The former takes 10 % of the kernel (563 -> 624 us, 8192 rows and keys).
 template <typename T> constexpr bool kMendD = sizeof(T) == 2;
 
 __device__ __forceinline__ float sum8(const bf16x8 &x)
@@ -229,7 +229,7 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     grad.load(static_cast<const T *>(a.d_out) + (row * a.heads + head) * 64, ok, lane);
     // What the gradient of keys needs of the row as well: its log-sum, in log2 (+inf where it saw no keys, so that every probability is
     // 0), and -D, D = out . d_out.
-    float l2 = INFINITY, d = 0.f, sum = 0.f;  // d: -D
+    float l2 = INFINITY, d = 0.f, sum = 0.f, entered = 0.f;  // d: -D
     float *stats = a.stats + 2 * (head * a.n_q + row);
     if (ok) {
         const T *o = static_cast<const T *>(a.to.out) + (row * a.heads + head) * 64, *g = static_cast<const T *>(a.d_out) + (row * a.heads + head) * 64;
@@ -293,17 +293,19 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
             }
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
-                float x[8], y[8];
+                float x[8], y[8], add[2] = {0.f, 0.f};
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     y[j] = s[8 * w + j];
                     x[j] = dp[8 * w + j];
+                    if constexpr (kMendD<T>) add[j & 1] += x[j];
                 }
                 bf16x8 ds[P], p[P];
                 split_parts<P>(x, ds);
                 if constexpr (kMendD<T>) {
                     split_parts<P>(y, p);
-                    sum += sum8(ds[0]);
+                    sum += add[0] + add[1];
+                    entered += sum8(ds[0]);
                 }
 #pragma unroll
                 for (int dt = 0; dt < 2; ++dt) {
@@ -316,16 +318,17 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     const int64_t to = row * a.heads + head, part = sh.split * a.n_q * a.heads + to;
     if constexpr (kMendD<T>) {
         sum = sum_with_other_half(sum);
+        entered = sum_with_other_half(entered);
         if (a.part_q == nullptr) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                grad.o[0][r] -= sum * held.o[0][r];
-                grad.o[1][r] -= sum * held.o[1][r];
+                grad.o[0][r] -= entered * held.o[0][r];
+                grad.o[1][r] -= entered * held.o[1][r];
             }
             if (ok && lane < 32) stats[1] = d - sum;
         } else {
             store_row(held.o, 1.f, a.part_pk + part * 64, ok, lane);
-            if (ok && lane < 32) a.part_sum[part] = sum;
+            if (ok && lane < 32) { a.part_sum[2 * part] = sum; a.part_sum[2 * part + 1] = entered; }
         }
     }
     if (a.part_q != nullptr)
@@ -343,17 +346,18 @@ template <typename T> __global__ __launch_bounds__(256) void grad_q_combine_kern
     if (!a.q_spans.covers(row)) return;
     const int c = static_cast<int>(i & 15) * 4;
     floatx4 g = {0.f, 0.f, 0.f, 0.f}, pk = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
+    float sum = 0.f, entered = 0.f;
     for (int j = 0; j < a.n_split; ++j) {
         g += *reinterpret_cast<const floatx4 *>(a.part_q + (j * share + at) * 64 + c);
         if constexpr (kMendD<T>) {
             pk += *reinterpret_cast<const floatx4 *>(a.part_pk + (j * share + at) * 64 + c);
-            sum += a.part_sum[j * share + at];
+            sum += a.part_sum[2 * (j * share + at)];
+            entered += a.part_sum[2 * (j * share + at) + 1];
         }
     }
     T *dst = static_cast<T *>(a.dq) + at * 64 + c;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) dst[e] = from_float<T>(a.scale * (g[e] - sum * pk[e]));
+    for (int e = 0; e < 4; ++e) dst[e] = from_float<T>(a.scale * (g[e] - entered * pk[e]));
     if (kMendD<T> && c == 0) a.stats[2 * ((at - row * a.heads) * a.n_q + row) + 1] -= sum;
 }
 

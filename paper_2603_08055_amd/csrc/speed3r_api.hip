@@ -1070,7 +1070,7 @@ s3r_status plan_cross(const s3r_cross_params *p, CrossPlan *out)
     c.part_q = take(c.split_q > 1 ? c.split_q * rows * 64 * sizeof(float) : 0);
     const bool mend = c.split_q > 1 && bf16;
     c.part_pk = take(mend ? c.split_q * rows * 64 * sizeof(float) : 0);
-    c.part_sum = take(mend ? c.split_q * rows * sizeof(float) : 0);
+    c.part_sum = take(mend ? c.split_q * rows * 2 * sizeof(float) : 0);
     c.part_k = take(c.split_kv > 1 ? c.split_kv * keys * 64 * sizeof(float) : 0);
     c.part_v = take(c.split_kv > 1 ? c.split_kv * keys * 64 * sizeof(float) : 0);
     c.backward = off;

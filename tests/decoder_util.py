@@ -8,8 +8,8 @@ Bounds.  u = 2^-24 is half a step of fp32, h half a step of the tensors' type (b
   P        off by d P, and by h P where it enters a product in bf16 (fp32: parts hold it exactly).
   out      sum_j (d + h) P |v| from P, accumulation of n keys (n / 8 + 64) u sum_j P |v|, and h |out| for the store.
   dP       as the scores, with |d_out| |v|.   D: in fp32 sum_c |d_out| err(out) + 64 u sum |d_out out|; in bf16 the rounding of out
-           is taken out again, by the sum of dS over the keys, and what is left is (d + n u) sum_j P |dP - D| + sum_j P err(dP),
-           h times the rounding itself, from P k in bf16, and the roundings of the dS that were added up, h sum_j |dS|.
+           is taken out again, by the sum of dS over the keys, and what is left is (d + n u) sum_j P |dP - D| + sum_j P err(dP) and
+           h times the rounding itself, from P k in bf16.
            In bf16 dq is mended by the sum of the rounded dS: at most h sum_j |dS| more, through P |k|.
   dS       P ((d + h) |dP - D| + err(D) + err(dP)), which passes through |k| and |q|; dv: (d + h) P^T |d_out|.
 """
@@ -62,7 +62,6 @@ def attention(q, k, v, seen, scale, dtype, d_out=None):
     ds = p * (dp - delta)
     if not f32:
         d_err = hp * d_err + (d + chain + 4 * U) * ds.abs().sum(1, keepdim=True) + (p * dp_err).sum(1, keepdim=True)
-        d_err = d_err + hp * ds.abs().sum(1, keepdim=True)
         # the key gradient's D and the query gradient's dS, rounded with the D that lacks it
         d_err = d_err + hp * (g.abs() * out_tol).sum(1, keepdim=True)
     err = p * ((d + hp + 4 * U) * (dp - delta).abs() + d_err + dp_err) + hp * ds.abs() * 2 ** -7
