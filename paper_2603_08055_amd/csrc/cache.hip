@@ -303,14 +303,15 @@ template <typename T> __global__ __launch_bounds__(256, 2) void cache_attn_kerne
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = wave & 1;
     const bool is_v = wave >= 2;
     Share sh;
-    if (!find_share(a.spans, a.cache.kv_len, a.per_row, 128, a.tiles, a.n_split, a.cache.kv_heads, sh, a.causal)) return;
+    if (!find_share(a.spans, a.cache.kv_len, a.per_row, 128, a.tiles, a.n_split, a.cache.kv_heads, !a.uneven, false, sh)) return;
     Sight sight;
     sight.find(a, sh, 128, 32 * wave + (lane & 31));
+    int u0, u1;
+    piece((sight.most + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1);
+    if (a.to.part_o != nullptr && u0 == u1) return store_no_keys(a.to, sh.split, sight.row, sight.head, sight.ok && lane < 32);
     SoftRow<P> soft;
     soft.clear();
     soft.load(static_cast<const T *>(a.q) + sight.row * a.q_row + sight.head * a.q_head, sight.ok, lane);
-    int u0, u1;
-    piece((sight.most + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
     PageUnits<false> units{a.cache, sh.of.seq, sh.kv_head, sight.len, -1, false};
     const uint8_t *codes = is_v ? a.cache.v_codes : a.cache.k_codes, *scales = is_v ? a.cache.v_scales : a.cache.k_scales;
     uint4 code = {};
@@ -353,14 +354,15 @@ template <typename T, int WAVES, bool WIDE> __global__ __launch_bounds__(64 * WA
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     bf16_t *mine = reinterpret_cast<bf16_t *>(smem) + wave * kPlane;
     Share sh;
-    if (!find_few_share(a.spans, a.cache.kv_len, a.per_row, kFewRows, a.n_split, a.cache.kv_heads, sh)) return;
+    if (!find_share(a.spans, a.cache.kv_len, a.per_row, kFewRows, a.tiles, a.n_split, a.cache.kv_heads, false, true, sh)) return;
     Sight sight;
     sight.find(a, sh, kFewRows, lane & 15);
+    int u0, u1;
+    piece((sight.most + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1);
+    if (a.to.part_o != nullptr && u0 == u1) return store_no_keys(a.to, sh.split, sight.row, sight.head, sight.ok && threadIdx.x < 16);
     FewRows<P> few;
     few.clear();
     few.load(static_cast<const T *>(a.q) + sight.row * a.q_row + sight.head * a.q_head, sight.ok, lane);
-    int u0, u1;
-    piece((sight.most + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
     PageUnits<WIDE> units{a.cache, sh.of.seq, sh.kv_head, sight.len, -1, false};
     uint2 k[4] = {};
     uint4 v[2] = {};

@@ -33,7 +33,7 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) 
     bf16_t *lds = reinterpret_cast<bf16_t *>(smem);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Share sh;
-    if (!find_share(a.q_spans, nullptr, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, sh)) return;
+    if (!find_share(a.q_spans, nullptr, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, !a.uneven, true, sh)) return;
     const int q0 = sh.of.first, q_len = sh.of.len;
     int k0, k_len;
     a.kv_spans.of(sh.of.seq, k0, k_len);
@@ -41,11 +41,12 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) 
     const bool ok = item < static_cast<int64_t>(q_len) * a.per_row;
     const int64_t row = q0 + item / a.per_row;
     const int head = sh.kv_head * a.per_row + static_cast<int>(item % a.per_row);
+    int u0, u1;
+    piece((k_len + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1);
+    if (a.to.part_o != nullptr && u0 == u1) return store_no_keys(a.to, sh.split, row, head, ok && lane < 32);
     SoftRow<P> soft;
     soft.clear();
     soft.load(static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head, ok, lane);
-    int u0, u1;
-    piece((k_len + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
     auto units = key_units<T>(a, sh.kv_head, k0, k_len, lds);
     auto rows = counted(a, k0, k_len);
     unsigned long long seen = 0;
@@ -67,7 +68,7 @@ template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, sizeof
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     bf16_t *mine = reinterpret_cast<bf16_t *>(smem) + wave * P * kPlane;
     Share sh;
-    if (!find_few_share(a.q_spans, nullptr, a.per_row, kFewRows, a.n_split, a.kv_heads, sh)) return;
+    if (!find_share(a.q_spans, nullptr, a.per_row, kFewRows, a.tiles, a.n_split, a.kv_heads, false, true, sh)) return;
     const int q0 = sh.of.first, q_len = sh.of.len;
     int k0, k_len;
     a.kv_spans.of(sh.of.seq, k0, k_len);
@@ -75,11 +76,12 @@ template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, sizeof
     const bool ok = item < static_cast<int64_t>(q_len) * a.per_row;
     const int64_t row = q0 + item / a.per_row;
     const int head = sh.kv_head * a.per_row + static_cast<int>(item % a.per_row);
+    int u0, u1;
+    piece((k_len + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1);
+    if (a.to.part_o != nullptr && u0 == u1) return store_no_keys(a.to, sh.split, row, head, ok && threadIdx.x < 16);
     FewRows<P> few;
     few.clear();
     few.load(static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head, ok, lane);
-    int u0, u1;
-    piece((k_len + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
     const T *keys = static_cast<const T *>(a.k) + k0 * a.kv_row + sh.kv_head * a.kv_head + 16 * (lane >> 4);
     RowUnits<T, 64> values(static_cast<const T *>(a.v) + k0 * a.kv_row + sh.kv_head * a.kv_head, k_len, a.kv_row, 0, 1, lane);
     auto rows = counted(a, k0, k_len);
@@ -214,7 +216,7 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     bf16_t *lds = reinterpret_cast<bf16_t *>(smem);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Share sh;
-    if (!find_share(a.q_spans, nullptr, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, sh)) return;
+    if (!find_share(a.q_spans, nullptr, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, !a.uneven, true, sh)) return;
     const int q0 = sh.of.first, q_len = sh.of.len;
     int k0, k_len;
     a.kv_spans.of(sh.of.seq, k0, k_len);
@@ -222,6 +224,9 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     const bool ok = item < static_cast<int64_t>(q_len) * a.per_row;
     const int64_t row = q0 + item / a.per_row;
     const int head = sh.kv_head * a.per_row + static_cast<int>(item % a.per_row);
+    int u0, u1;
+    piece((k_len + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1);
+    if (sh.split > 0 && u0 == u1) return;
     SoftRow<P> held, grad;  // q, and d_out; held.o: P k, grad.o: the gradient
     held.clear();
     held.load(static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head, ok, lane);
@@ -246,8 +251,6 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     }
     d = sum_with_other_half(d);
     if (ok && lane < 32 && sh.split == 0) { stats[0] = l2; stats[1] = d; }
-    int u0, u1;
-    piece((k_len + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
     auto units = key_units<T>(a, sh.kv_head, k0, k_len, lds);
     auto rows = counted(a, k0, k_len);
     unsigned long long seen = 0;
@@ -337,6 +340,15 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
         store_row(grad.o, a.scale, static_cast<T *>(a.dq) + to * 64, ok, lane);
 }
 
+// Pieces that a sequence's streamed rows (items: rows * per_row) were divided into.
+__device__ __forceinline__ int pieces_of(const Spans &streamed, int seq, int per_row, const CrossArgs &a)
+{
+    int first, len;
+    streamed.of(seq, first, len);
+    const int units = (len * per_row + kUnitRows - 1) / kUnitRows, per = piece_units(units, a.n_split, a.least);
+    return (units + per - 1) / per;
+}
+
 // The query gradient from its pieces over keys.  16 threads for a row of a head.
 template <typename T> __global__ __launch_bounds__(256) void grad_q_combine_kernel(CrossArgs a)
 {
@@ -347,7 +359,8 @@ template <typename T> __global__ __launch_bounds__(256) void grad_q_combine_kern
     const int c = static_cast<int>(i & 15) * 4;
     floatx4 g = {0.f, 0.f, 0.f, 0.f}, pk = {0.f, 0.f, 0.f, 0.f};
     float sum = 0.f, entered = 0.f;
-    for (int j = 0; j < a.n_split; ++j) {
+    const int n = pieces_of(a.kv_spans, a.q_spans.find(row), 1, a);
+    for (int j = 0; j < n; ++j) {
         g += *reinterpret_cast<const floatx4 *>(a.part_q + (j * share + at) * 64 + c);
         if constexpr (kMendD<T>) {
             pk += *reinterpret_cast<const floatx4 *>(a.part_pk + (j * share + at) * 64 + c);
@@ -369,20 +382,23 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
     float *row_stats = reinterpret_cast<float *>(smem + sizeof(bf16_t) * UnitPairs<T>::kStages * UnitPairs<T>::kStage);  // [stages][2][64]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Share sh;
-    if (!find_share(a.kv_spans, nullptr, 1, kTile, a.tiles, a.n_split, a.kv_heads, sh)) return;
+    if (!find_share(a.kv_spans, nullptr, 1, kTile, a.tiles, a.n_split, a.kv_heads, !a.uneven, true, sh)) return;
     const int k0 = sh.of.first, k_len = sh.of.len;
     int q0, q_len;
     a.q_spans.of(sh.of.seq, q0, q_len);
     const int key = sh.tile * kTile + 32 * wave + (lane & 31);
     const bool ok = key < k_len, seen = ok && (a.key_mask == nullptr || a.key_mask[k0 + key] != 0);
     const int64_t row = k0 + key;
+    const int items = q_len * a.per_row, head0 = sh.kv_head * a.per_row;
+    int u0, u1;
+    piece((items + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1);
+    if (sh.split > 0 && u0 == u1) return;
     SoftRow<P> kk, vv;  // k and v; .o: their gradients
     kk.clear();
     vv.clear();
     kk.load(static_cast<const T *>(a.k) + row * a.kv_row + sh.kv_head * a.kv_head, seen, lane);
     vv.load(static_cast<const T *>(a.v) + row * a.kv_row + sh.kv_head * a.kv_head, seen, lane);
 
-    const int items = q_len * a.per_row, head0 = sh.kv_head * a.per_row;
     UnitPairs<T, true> units(static_cast<const T *>(a.q) + q0 * a.q_row + head0 * a.q_head,
                              static_cast<const T *>(a.d_out) + (static_cast<int64_t>(q0) * a.heads + head0) * 64, items, a.q_row, a.q_head,
                              static_cast<int64_t>(a.heads) * 64, 64, a.per_row, lds);
@@ -396,8 +412,6 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
             st = a.stats[2 * ((head0 + r - i * a.per_row) * a.n_q + q0 + i) + which];
         }
     };
-    int u0, u1;
-    piece((items + kUnitRows - 1) / kUnitRows, a.n_split, sh.split, u0, u1);
     const UnitLanes at(lane);
     units.begin(u0, u1, more);
     const float *stats = row_stats;
@@ -477,7 +491,8 @@ template <typename T> __global__ __launch_bounds__(256) void grad_kv_combine_ker
     const float *part = blockIdx.y == 0 ? a.part_k : a.part_v;
     T *out = static_cast<T *>(blockIdx.y == 0 ? a.dk : a.dv);
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < a.n_split; ++j) acc += *reinterpret_cast<const floatx4 *>(part + (j * n + i) * 4);
+    const int pieces = pieces_of(a.q_spans, a.kv_spans.find(i / (a.kv_heads * 16)), a.per_row, a);
+    for (int j = 0; j < pieces; ++j) acc += *reinterpret_cast<const floatx4 *>(part + (j * n + i) * 4);
 #pragma unroll
     for (int e = 0; e < 4; ++e) out[i * 4 + e] = from_float<T>(acc[e]);
 }
@@ -555,7 +570,7 @@ hipError_t launch_grad_kv(const CrossArgs &a, bool is_bf16, hipStream_t stream)
 
 hipError_t launch_soft_combine(const SoftOut &to, const Spans &spans, int n_split, bool is_bf16, hipStream_t stream)
 {
-    const bool wide = n_split >= 8 && to.rows * to.heads <= 4096;  // at most 64 splits
+    const bool wide = n_split >= 8 && to.rows * to.heads <= 8192;  // at most 64 splits
     const int64_t blocks = (to.rows * to.heads * (wide ? 64 : 16) + 255) / 256;
     if (!grid_ok(blocks) || n_split > 64) return hipErrorInvalidValue;
     auto kernel = is_bf16 ? (wide ? &soft_combine_kernel<bf16_t, 4> : &soft_combine_kernel<bf16_t, 1>)

@@ -278,7 +278,7 @@ struct SoftOut {
 constexpr int kDiagPage = 4, kDiagSpans = 8, kDiagLength = 16, kDiagPosition = 32;
 
 // q and d_out rows, k and v rows: element strides between rows and between heads.  per_row = heads / kv_heads.  factor = scale * log2(e).
-// tiles: most tiles of the held rows (most_tiles); n_split: pieces of the streamed rows.  stats: see launch_grad_q.  part_*: partial
+// tiles: most tiles of the held rows (most_tiles); n_split: most pieces of a tile's streamed rows, of `least` units or more each.  stats: see launch_grad_q.  part_*: partial
 // sums [n_split][rows][heads][64] where n_split > 1, else null (part_sum: [n_split][rows][heads][2]; it and part_pk for bf16 alone).
 struct CrossArgs {
     const void *q, *k, *v, *d_out;
@@ -286,7 +286,8 @@ struct CrossArgs {
     const uint8_t *key_mask;
     Spans q_spans, kv_spans;
     int64_t n_q, n_kv, tiles;
-    int heads, kv_heads, per_row, n_split;
+    int heads, kv_heads, per_row, n_split, least;
+    bool uneven;  // sequences of several lengths, or causal rows
     float scale, factor;
     SoftOut to;
     float *stats;
@@ -344,7 +345,8 @@ struct CacheArgs {
     const void *q;
     void *k, *v;      // rows to append, or room for rows read
     int64_t q_row, q_head, kv_row, kv_head, n_rows;
-    int heads, per_row, n_split;
+    int heads, per_row, n_split, least;
+    bool uneven;
     int64_t tiles;
     bool causal;
     float factor;

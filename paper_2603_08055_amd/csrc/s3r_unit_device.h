@@ -200,31 +200,34 @@ inline int64_t xcd_padded(int64_t n) { return (n + 7) / 8 * 8; }
 // A workgroup's share of the grid: a tile of the held rows, a head of keys, one of n_split pieces of the streamed units.
 struct Share { Sequence of; int tile, kv_head, split; };
 
-// Tiles of few rows share no keys with their neighbours, and may be a CU's only ones: those that `tiles` counts and the sequences do
-// not have come last, so that every XCD has as many real ones.
-__device__ __forceinline__ bool find_few_share(const Spans &spans, const int32_t *list, int per_row, int tile, int n_split, int kv_heads, Share &s)
-{
-    const unsigned each = static_cast<unsigned>(n_split) * static_cast<unsigned>(kv_heads), t = blockIdx.x / each, rest = blockIdx.x - t * each;
-    s.kv_head = static_cast<int>(rest / static_cast<unsigned>(n_split));
-    s.split = static_cast<int>(rest) - s.kv_head * n_split;
-    return find_tile(spans, list, per_row, tile, t, s.of, s.tile);
-}
-
-// last_first: a head's tiles from the last one on (causal rows: those that see most begin, and the short ones fill up the end).
+// Two orders of the workgroups.  together: neighbouring tiles, which read the same keys, on one XCD and its L2, the heads and pieces one
+// after the other.  Else tile by tile, each with its heads and pieces side by side over the XCDs, the last tile first (causal rows:
+// those that see most begin) or, `first_first`, the last one last: with sequences of several lengths, or causal rows, the later pieces
+// are short or empty, and an XCD with several heads' later pieces would have less to do than its neighbours.  Tiles that `tiles` counts
+// and the sequences do not have are found here as well.
 __device__ __forceinline__ bool find_share(const Spans &spans, const int32_t *list, int per_row, int tile, int64_t tiles, int n_split, int kv_heads,
-                                           Share &s, bool last_first = false)
+                                           bool together, bool first_first, Share &s)
 {
-    const int64_t item = xcd_neighbours(blockIdx.x, tiles * n_split * kv_heads);
-    const int64_t rest = item / tiles;
-    s.split = static_cast<int>(rest % n_split);
-    s.kv_head = static_cast<int>(rest / n_split);
-    const int64_t t = item - rest * tiles;
-    return s.kv_head < kv_heads && find_tile(spans, list, per_row, tile, last_first ? tiles - 1 - t : t, s.of, s.tile);
+    int64_t t;
+    if (together) {
+        const int64_t item = xcd_neighbours(blockIdx.x, tiles * n_split * kv_heads), rest = item / tiles;
+        s.split = static_cast<int>(rest % n_split);
+        s.kv_head = static_cast<int>(rest / n_split);
+        t = item - rest * tiles;
+    } else {
+        const unsigned each = static_cast<unsigned>(n_split) * static_cast<unsigned>(kv_heads), u = blockIdx.x / each, rest = blockIdx.x - u * each;
+        s.split = static_cast<int>(rest / static_cast<unsigned>(kv_heads));
+        s.kv_head = static_cast<int>(rest) - s.split * kv_heads;
+        t = first_first ? u : tiles - 1 - u;
+    }
+    return t >= 0 && t < tiles && s.kv_head < kv_heads && find_tile(spans, list, per_row, tile, t, s.of, s.tile);
 }
 
-__device__ __forceinline__ void piece(int units, int n_split, int split, int &u0, int &u1)
+// Units of a piece: the same for all pieces of a tile but the last ones, which may be shorter or empty; short sequences have fewer pieces.
+__device__ __forceinline__ int piece_units(int units, int n_split, int least) { return max((units + n_split - 1) / n_split, least); }
+__device__ __forceinline__ void piece(int units, int n_split, int least, int split, int &u0, int &u1)
 {
-    const int per = (units + n_split - 1) / n_split;
+    const int per = piece_units(units, n_split, least);
     u0 = min(split * per, units);
     u1 = min(u0 + per, units);
 }
@@ -591,6 +594,12 @@ template <typename T> __device__ __forceinline__ void store_row(const floatx16 (
             join_runs_32(x, y, z);
             if (ok) Io8<T>::store(to + 32 * dt + 8 * (b + (lane >> 5)), z);
         }
+}
+
+// A piece without keys leaves its rows' log-sums only, by which it is known.
+__device__ __forceinline__ void store_no_keys(const SoftOut &to, int split, int64_t row, int head, bool ok)
+{
+    if (ok) to.part_lse[split * to.rows * to.heads + row * to.heads + head] = -INFINITY;
 }
 
 template <typename T, int PQ>

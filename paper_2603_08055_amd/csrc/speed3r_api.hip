@@ -993,16 +993,27 @@ s3r_status check_strides(const char *what, int64_t tok, int64_t head)
 // n = ceil(workgroups * pieces / 256) of them, `resident` at a time; one alone on a CU takes half as long again as its share
 // of a full one.  A workgroup takes `unit_us` for each unit and two units' time to start and end; more than one piece costs a launch that
 // joins them (3.5 us, and `part_bytes` of partial results for a piece at 5 TB/s; their way out is under the work).  A piece has
-// `least` units or more.
+// `least` units or more.  uneven: sequences of several lengths, or causal rows, of which only the longest is known here; then pieces for
+// two workgroups on every CU (one where no more fit), were all as long as that.
 // Measured, 1374 rows over 27480 keys, 16 heads (176 tiles): PIECES_A; 2748 rows over 10992 keys: PIECES_B.
 struct Pace { double unit_us; int resident, least; };
-int pieces(int64_t workgroups, int64_t units, const Pace &pace, double part_bytes)
+constexpr Pace kCrossPace[2] = {{2.2, 2, 3}, {0.67, 4, 4}};  // [bf16]
+constexpr Pace kGradQPace[2] = {{5.5, 1, 3}, {1.1, 2, 4}};
+constexpr Pace kGradKvPace[2] = {{7.3, 1, 3}, {1.3, 2, 4}};
+constexpr Pace kCachePace[2] = {{2.0, 2, 3}, {0.85, 3, 4}};
+constexpr int kFewLeast = 4;
+int pieces(int64_t workgroups, int64_t units, const Pace &pace, double part_bytes, bool uneven)
 {
     auto time_us = [&](int s) {
         const int64_t n = (workgroups * s + 255) / 256, rest = n % pace.resident;
         const double share = static_cast<double>(n) + (rest == 0 ? 0.0 : 0.5 - 0.5 * static_cast<double>(rest - 1) / pace.resident);
         return share * static_cast<double>((units + s - 1) / s + 2) * pace.unit_us + (s == 1 ? 0.0 : 3.5 + s * part_bytes / 5e6);
     };
+    if (uneven) {
+        int64_t s = (256 * (pace.resident < 2 ? 1 : 2) + workgroups - 1) / workgroups;
+        if (s > units / pace.least) s = units / pace.least;
+        return s < 1 ? 1 : (s > 64 ? 64 : static_cast<int>(s));
+    }
     int most = 1;
     double shortest = time_us(1);
     while (most < 64 && units >= static_cast<int64_t>(pace.least) * (most + 1)) {
@@ -1026,7 +1037,7 @@ int pieces_few(int64_t workgroups, int64_t units)
 
 struct CrossPlan {
     bool few_rows;
-    int batch, per_row, split, split_q, split_kv;
+    int batch, per_row, split, least, split_q, split_kv;
     int64_t tiles, q_tiles, kv_tiles;
     size_t part_o, part_lse, forward;                   // workspace of the forward call
     size_t stats, part_q, part_pk, part_sum, part_k, part_v, backward;     // of the gradient
@@ -1047,18 +1058,20 @@ s3r_status plan_cross(const s3r_cross_params *p, CrossPlan *out)
     c.per_row = p->heads / p->kv_heads;
     if (p->n_q > kMaxRowHeads / p->heads || p->n_kv > kMaxRowHeads / p->kv_heads || c.batch > (1 << 22) / p->kv_heads)
         return fail(S3R_ERR_UNSUPPORTED, "rows * heads exceeds 2^28, or batch * kv_heads 2^22");
-    // (of ragged sequences the longest counts, and only their sum is known here)
-    const int64_t items = p->n_q * c.per_row, ragged = c.batch > 1 ? 2 : 1, units = (ragged * p->n_kv / c.batch + 63) / 64;
+    const int bf16 = p->dtype == S3R_BF16;
+    const bool uneven = c.batch > 1;
+    // (the longest of several sequences counts, and only their sum is known: four times their mean, if there is that much)
+    auto units_of = [&](int64_t rows) { return ((uneven ? (4 * rows / c.batch < rows ? 4 * rows / c.batch : rows) : rows) + 63) / 64; };
+    const int64_t items = p->n_q * c.per_row, units = units_of(p->n_kv);
+    const double q_bytes = 256.0 * static_cast<double>(p->n_q) * p->heads, kv_bytes = 512.0 * static_cast<double>(p->n_kv) * p->kv_heads;
     c.few_rows = items <= int64_t(16) * c.batch;
     c.tiles = s3r::most_tiles(p->n_q, c.per_row, c.few_rows ? 16 : 128, c.batch);
-    const bool bf16 = p->dtype == S3R_BF16;
-    const double q_bytes = 256.0 * static_cast<double>(p->n_q) * p->heads, kv_bytes = 512.0 * static_cast<double>(p->n_kv) * p->kv_heads;
-    c.split = c.few_rows ? pieces_few(c.tiles * p->kv_heads, units)
-                         : pieces(c.tiles * p->kv_heads, units, bf16 ? Pace{0.67, 4, 4} : Pace{2.2, 2, 1}, q_bytes);
+    c.split = c.few_rows ? pieces_few(c.tiles * p->kv_heads, units) : pieces(c.tiles * p->kv_heads, units, kCrossPace[bf16], q_bytes, uneven);
+    c.least = c.few_rows ? kFewLeast : kCrossPace[bf16].least;
     c.q_tiles = s3r::most_tiles(p->n_q, c.per_row, 128, c.batch);
-    c.split_q = pieces(c.q_tiles * p->kv_heads, units, bf16 ? Pace{1.1, 2, 4} : Pace{5.5, 1, 1}, bf16 ? 2 * q_bytes : q_bytes);
+    c.split_q = pieces(c.q_tiles * p->kv_heads, units, kGradQPace[bf16], bf16 ? 2 * q_bytes : q_bytes, uneven);
     c.kv_tiles = s3r::most_tiles(p->n_kv, 1, 128, c.batch);
-    c.split_kv = pieces(c.kv_tiles * p->kv_heads, (ragged * items / c.batch + 63) / 64, bf16 ? Pace{1.3, 2, 4} : Pace{7.3, 1, 1}, kv_bytes);
+    c.split_kv = pieces(c.kv_tiles * p->kv_heads, units_of(items), kGradKvPace[bf16], kv_bytes, uneven);
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
     const size_t rows = static_cast<size_t>(p->n_q) * p->heads, keys = static_cast<size_t>(p->n_kv) * p->kv_heads;
@@ -1109,7 +1122,7 @@ s3r_status cross_args(const s3r_cross_params *p, const CrossPlan &c, s3r::CrossA
     a.q_spans = s3r::Spans{p->q_start, c.batch, p->n_q};
     a.kv_spans = s3r::Spans{p->kv_start, c.batch, p->n_kv};
     a.n_q = p->n_q; a.n_kv = p->n_kv;
-    a.heads = p->heads; a.kv_heads = p->kv_heads; a.per_row = c.per_row;
+    a.heads = p->heads; a.kv_heads = p->kv_heads; a.per_row = c.per_row; a.uneven = c.batch > 1;
     a.scale = resolve_scale(p->softmax_scale, 64);
     a.factor = a.scale * 1.4426950408889634f;
     a.to.out = p->out; a.to.lse = p->lse; a.to.rows = p->n_q; a.to.heads = p->heads;
@@ -1144,6 +1157,7 @@ s3r_status speed3r_cross_attn(const s3r_cross_params *p)
     if (p->n_q == 0) return S3R_OK;
     a.tiles = c.tiles;
     a.n_split = c.split;
+    a.least = c.least;
     if (c.split > 1) {
         a.to.part_o = floats_at(p->workspace, c.part_o);
         a.to.part_lse = floats_at(p->workspace, c.part_lse);
@@ -1183,6 +1197,7 @@ s3r_status speed3r_cross_attn_backward(const s3r_cross_params *p)
     if (p->n_q > 0) {
         a.tiles = c.q_tiles;
         a.n_split = c.split_q;
+        a.least = kGradQPace[bf16].least;
         if (c.split_q > 1) {
             a.part_q = floats_at(p->workspace, c.part_q);
             a.part_pk = floats_at(p->workspace, c.part_pk);
@@ -1194,6 +1209,7 @@ s3r_status speed3r_cross_attn_backward(const s3r_cross_params *p)
     if (p->n_kv > 0) {
         a.tiles = c.kv_tiles;
         a.n_split = c.split_kv;
+        a.least = kGradKvPace[bf16].least;
         if (c.split_kv > 1) {
             a.part_k = floats_at(p->workspace, c.part_k);
             a.part_v = floats_at(p->workspace, c.part_v);
@@ -1209,7 +1225,7 @@ namespace {
 
 struct CachePlan {
     bool few_rows;
-    int split;
+    int split, least;
     int64_t tiles;
     size_t part_o, part_lse, total;
 };
@@ -1234,9 +1250,10 @@ s3r_status plan_cache(const s3r_cache_params *p, CachePlan *out)
     const int64_t units = (int64_t(p->max_pages) * p->page + 63) / 64;
     c.few_rows = p->n_rows * per_row <= int64_t(16) * p->batch;
     c.tiles = s3r::most_tiles(p->n_rows, per_row, c.few_rows ? 16 : 128, p->batch);
+    const Pace &pace = kCachePace[p->dtype == S3R_BF16];
     c.split = c.few_rows ? pieces_few(c.tiles * p->kv_heads, units)
-                         : pieces(c.tiles * p->kv_heads, units, p->dtype == S3R_BF16 ? Pace{0.85, 3, 4} : Pace{2.0, 2, 1},
-                                  256.0 * static_cast<double>(p->n_rows) * p->heads);
+                         : pieces(c.tiles * p->kv_heads, units, pace, 256.0 * static_cast<double>(p->n_rows) * p->heads, p->batch > 1 || p->causal);
+    c.least = c.few_rows ? kFewLeast : pace.least;
     const size_t rows = static_cast<size_t>(p->n_rows) * p->heads;
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
@@ -1271,6 +1288,7 @@ s3r_status cache_args(const s3r_cache_params *p, s3r::CacheArgs *out)
     a.kv_head = p->kv_stride_head ? p->kv_stride_head : 64;
     a.n_rows = p->n_rows; a.heads = p->heads; a.per_row = p->heads / p->kv_heads;
     a.causal = p->causal != 0;
+    a.uneven = p->batch > 1 || a.causal;
     a.factor = resolve_scale(p->softmax_scale, 64) * 1.4426950408889634f;
     a.to.out = p->out; a.to.lse = p->lse; a.to.rows = p->n_rows; a.to.heads = p->heads;
     *out = a;
@@ -1349,6 +1367,7 @@ s3r_status speed3r_cache_attn(const s3r_cache_params *p)
     if (p->n_rows == 0) return S3R_OK;
     a.tiles = c.tiles;
     a.n_split = c.split;
+    a.least = c.least;
     if (c.split > 1) {
         a.to.part_o = floats_at(p->workspace, c.part_o);
         a.to.part_lse = floats_at(p->workspace, c.part_lse);
