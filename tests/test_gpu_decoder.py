@@ -70,6 +70,48 @@ def test_cross_and_its_gradient(s3r, dtype, n, m, heads, kv_heads):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,m,heads,kv_heads", [(0, 70, 4, 2), (0, 0, 1, 1), (1, 700, 32, 1), (2, 90, 16, 1), (300, 9000, 32, 32)])
+def test_cross_without_rows_with_many_heads_and_many_pieces(s3r, dtype, n, m, heads, kv_heads):
+    g = gen(n + m + heads)
+    q, k, v = (normal(g, r, h, 64, dtype=dtype) for r, h in ((n, heads), (m, kv_heads), (m, kv_heads)))
+    d_out = normal(g, n, heads, 64, dtype=dtype)
+    compare(run_cross(s3r, q, k, v, d_out), cross_reference(q, k, v, [(0, n, 0, m)], None, SCALE, d_out))
+
+
+BATCHES = {"130 of few rows": ([1, 2, 3] * 43 + [1], 40), "one long among many": ([1] * 70 + [300] + [1] * 30, 100), "100 single rows": ([1] * 100, 150)}
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("which", list(BATCHES))
+def test_cross_batches_of_more_than_a_wave(s3r, dtype, which):
+    rows, most = BATCHES[which]
+    g = gen(len(rows))
+    keys = torch.randint(0, most, (len(rows),), generator=g, device="cuda").tolist()
+    q, k, v = normal(g, sum(rows), 4, 64, dtype=dtype), normal(g, sum(keys), 2, 64, dtype=dtype), normal(g, sum(keys), 2, 64, dtype=dtype)
+    d_out = normal(g, sum(rows), 4, 64, dtype=dtype)
+    a, b = starts(rows), starts(keys)
+    spans = [(int(x), r, int(y), c) for x, y, r, c in zip(a, b, rows, keys)]
+    compare(run_cross(s3r, q, k, v, d_out, q_start=a, kv_start=b), cross_reference(q, k, v, spans, None, SCALE, d_out))
+
+
+@pytest.mark.parametrize("stride", [1 << 22, 1 << 24])
+def test_rows_far_apart(s3r, stride):
+    """Rows of k and v further than 2^32 bytes from the first, and further apart than a 32-bit offset within a unit reaches."""
+    g = gen(77)
+    m = (5 << 30) // (2 * stride)
+    room = torch.zeros(m * stride, dtype=BF16, device="cuda")
+    k, v = (room.as_strided((m, 1, 64), (stride, 64, 1), at) for at in (0, 64))
+    k.copy_(normal(g, m, 1, 64, dtype=BF16)), v.copy_(normal(g, m, 1, 64, dtype=BF16))
+    for n in (1, 100):
+        q, d_out = normal(g, n, 1, 64, dtype=BF16), normal(g, n, 1, 64, dtype=BF16)
+        got = {"out": nan_like(q), "lse": torch.empty((1, n), device="cuda"), "dq": nan_like(q),
+               "dk": torch.empty((m, 1, 64), dtype=BF16, device="cuda"), "dv": torch.empty((m, 1, 64), dtype=BF16, device="cuda")}
+        s3r.speed3r_cross_attn(q, k, v, got["out"], lse=got["lse"])
+        s3r.speed3r_cross_attn_backward(q, k, v, got["out"], got["lse"], d_out, got["dq"], got["dk"], got["dv"])
+        compare(got, cross_reference(q, k, v, [(0, n, 0, m)], None, SCALE, d_out))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("heads,kv_heads", [(2, 2), (6, 2)])
 def test_ragged_batches_masks_and_what_must_not_matter(s3r, dtype, heads, kv_heads):
     """Sequences without rows or keys, a sequence whose keys are all masked, rows before the first and behind the last
@@ -333,6 +375,58 @@ def test_cache_attention(s3r, dtype, causal, page, heads, kv_heads, rows, length
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("which", list(BATCHES))
+def test_cache_batches_of_more_than_a_wave(s3r, dtype, page, which):
+    rows, most = BATCHES[which]
+    g = gen(len(rows) + page)
+    lengths = [r + int(x) for r, x in zip(rows, torch.randint(0, 2 * most, (len(rows),), generator=g, device="cuda"))]
+    width = max(lengths) // page + 1
+    cache = filled_cache(s3r, g, width * len(rows), 2, page)
+    pt = table(g, len(rows), width, width * len(rows))
+    q = normal(g, sum(rows), 4, 64, dtype=dtype)
+    for causal in (True, False):
+        compare(run_attend(s3r, cache, q, pt, lengths, rows, causal), attend_reference(cache, q, pt, lengths, rows, causal))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_cache_rows_in_larger_tensors(s3r, dtype):
+    """k, v and q as slices of one projection; rows read back into slices, and what lies between them left alone."""
+    g = gen(91)
+    n, page = 50, 32
+    packed_rows = normal(g, n, 8, 64, dtype=dtype)
+    q, k, v = packed_rows[:, :4], packed_rows[:, 4:6], packed_rows[:, 6:]
+    cos, sin = tables_of_angles(n, 32)
+    pt, kv_len = table(g, 1, 2, 3), torch.tensor([n], dtype=torch.int32, device="cuda")
+    one, two = s3r.PagedCache.empty(3, 2, page), s3r.PagedCache.empty(3, 2, page)
+    turned, again = torch.empty((n, 4, 64), dtype=dtype, device="cuda"), torch.empty((n, 4, 64), dtype=dtype, device="cuda")
+    s3r.speed3r_cache_append(one, k, v, pt, kv_len, q=q, q_out=turned, cos=cos, sin=sin)
+    s3r.speed3r_cache_append(two, k.contiguous(), v.contiguous(), pt, kv_len, q=q.contiguous(), q_out=again, cos=cos, sin=sin)
+    assert torch.equal(turned, again) and all(torch.equal(a, b) for a, b in zip(one, two))
+    room = torch.full((n, 3, 2, 64), 7.0, dtype=dtype, device="cuda")
+    s3r.speed3r_cache_read(one, room[:, 0], room[:, 2], pt, kv_len)
+    ko, vo = torch.empty((n, 2, 64), dtype=dtype, device="cuda"), torch.empty((n, 2, 64), dtype=dtype, device="cuda")
+    s3r.speed3r_cache_read(one, ko, vo, pt, kv_len)
+    assert torch.equal(room[:, 0], ko) and torch.equal(room[:, 2], vo) and bool((room[:, 1] == 7.0).all())
+    wide = torch.empty((n, 2, 4, 64), dtype=dtype, device="cuda")
+    wide[:, 1] = turned
+    a, b = torch.empty_like(turned), torch.empty_like(turned)
+    s3r.speed3r_cache_attn(one, wide[:, 1], a, pt, kv_len)
+    s3r.speed3r_cache_attn(one, turned, b, pt, kv_len)
+    assert torch.equal(a, b)
+
+
+def test_no_rows_at_all(s3r):
+    cache, pt = s3r.PagedCache.empty(2, 1, 16), torch.zeros((1, 2), dtype=torch.int32, device="cuda")
+    kv_len, none = torch.tensor([5], dtype=torch.int32, device="cuda"), torch.empty((0, 1, 64), dtype=BF16, device="cuda")
+    status = torch.full((1,), -1, dtype=torch.int32, device="cuda")
+    s3r.speed3r_cache_append(cache, none, none, pt, kv_len, status=status)
+    s3r.speed3r_cache_read(cache, none, none.clone(), pt, kv_len)
+    s3r.speed3r_cache_attn(cache, none, none.clone(), pt, kv_len)
+    assert int(status) == 0 and all(int(t.max()) == 0 for t in cache)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("rows", [3, 200])
 def test_nan_in_the_cache_reaches_only_rows_that_see_it(s3r, dtype, rows):
     g = gen(31)
@@ -411,30 +505,32 @@ def test_offsets_past_32_bits(s3r):
 
 # ---- as they are used -------------------------------------------------------------------------------------
 
-def test_a_decoder_over_a_scene_captured_and_replayed(s3r):
+@pytest.mark.parametrize("dtype,batch", [(BF16, 3), (F32, 3), (BF16, 100)])
+def test_a_decoder_over_a_scene_captured_and_replayed(s3r, dtype, batch):
     """Sparse global attention gives a scene's states; a decoder layer appends a token at a time, attends its cache and the scene.  The
     step is captured once (lengths and tokens in device memory) and replayed with the program's own work between; every
     replay equals the eager call, and two graphs with workspaces of their own do not disturb each other."""
     g = gen(61)
-    views, tokens, H, KH, page, batch = 2, 300, 4, 2, 16, 3
+    views, tokens, H, KH, page, width = 2, 300, 4, 2, 16, 14
     n = views * tokens
     q, k, v = (normal(g, n, H, 64, dtype=BF16) for _ in range(3))
     states = torch.empty_like(q)
     s3r.speed3r_sparse_global_attn(q, k, v, states, 64, 4)
+    states = states.to(dtype)
     scene_k, scene_v = states[:, :KH], states[:, KH:]
-    kv_start = torch.tensor([0, n, n, n], dtype=torch.int32, device="cuda")          # the first sequence has the scene, the others none
+    kv_start = starts([n] + [0] * (batch - 1))                                       # the first sequence has the scene, the others none
     cos, sin = tables_of_angles(256, 32)
 
     class Step:
         def __init__(self):
-            self.cache = s3r.PagedCache.empty(3 * 16, KH, page)
-            self.pt = torch.arange(48, dtype=torch.int32, device="cuda").reshape(3, 16)
-            self.len = torch.tensor([1, 5, 200], dtype=torch.int32, device="cuda")
+            self.cache = s3r.PagedCache.empty(batch * width, KH, page)
+            self.pt = torch.arange(batch * width, dtype=torch.int32, device="cuda").reshape(batch, width)
+            self.len = torch.tensor(([1, 5, 200] * batch)[:batch], dtype=torch.int32, device="cuda")
             self.start = starts([1] * batch)
-            self.q, self.k, self.v = (torch.zeros((batch, h, 64), dtype=BF16, device="cuda") for h in (H, KH, KH))
+            self.q, self.k, self.v = (torch.zeros((batch, h, 64), dtype=dtype, device="cuda") for h in (H, KH, KH))
             self.turned, self.own, self.out = (torch.zeros_like(self.q) for _ in range(3))
-            dt = s3r.S3R_BF16
-            need = max(s3r.speed3r_cache_workspace_bytes(self.cache, batch, H, dt, batch, 16),
+            dt = s3r.S3R_BF16 if dtype == BF16 else s3r.S3R_F32
+            need = max(s3r.speed3r_cache_workspace_bytes(self.cache, batch, H, dt, batch, width),
                        s3r.speed3r_cross_workspace_bytes(self.q, scene_k, q_start=self.start), 1)
             self.ws = torch.empty(need, dtype=torch.uint8, device="cuda")
 
@@ -446,7 +542,7 @@ def test_a_decoder_over_a_scene_captured_and_replayed(s3r):
         def feed(self, i):
             x = gen(100 + i)
             for t in (self.q, self.k, self.v):
-                t.copy_(normal(x, *t.shape, dtype=BF16))
+                t.copy_(normal(x, *t.shape, dtype=dtype))
 
     eager, one, two = Step(), Step(), Step()
     side = torch.cuda.Stream()
@@ -507,6 +603,36 @@ def test_views_one_after_another_match_all_at_once(s3r):
     for name, got in (("cache", attended), ("cross", crossed), ("dense", dense)):
         check(name, got, want["out"], want["out_tol"])
     assert torch.isfinite(out.float()).all()
+
+
+def test_gradient_captured_and_replayed(s3r):
+    """A training step's calls in a graph, with the inputs changed and the program's own work between replays."""
+    g = gen(101)
+    q, k, v, d_out = (normal(g, n, 4, 64, dtype=BF16) for n in (200, 900, 900, 200))
+    names = ("out", "lse", "dq", "dk", "dv")
+    buffers = (torch.empty_like(q), torch.empty((4, 200), device="cuda"), torch.empty_like(q), torch.empty_like(k), torch.empty_like(v))
+    ws = torch.empty(max(s3r.speed3r_cross_workspace_bytes(q, k), s3r.speed3r_cross_workspace_bytes(q, k, backward=True)), dtype=torch.uint8, device="cuda")
+
+    def step():
+        out, lse, dq, dk, dv = buffers
+        s3r.speed3r_cross_attn(q, k, v, out, lse=lse, workspace=ws)
+        s3r.speed3r_cross_attn_backward(q, k, v, out, lse, d_out, dq, dk, dv, workspace=ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        for t in (q, k, v, d_out):
+            t.copy_(normal(g, *t.shape, dtype=BF16))
+        want = run_cross(s3r, q, k, v, d_out)
+        graph.replay()
+        torch.cuda.synchronize()
+        for name, t in zip(names, buffers):
+            assert torch.equal(t, want[name]), (i, name)
 
 
 def test_another_stream(s3r):
