@@ -127,8 +127,9 @@ template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, sizeof
 
 // One result from the splits' normalised ones: weights 2^(lse_j - lse).  GROUPS x 16 threads for a row of a head: 16 take four
 // channels each, the groups every GROUPS-th split.  With one group, the splits follow one another; with four (a wave for a row of a
-// head), the log-sums of up to 64 splits are one load, and a row's partial results come in a sixteenth of the steps.  64 splits of 16
-// rows: 22.4 us with one group, 5.2 with four; 2 splits of 22 thousand rows take 6.2 us with one.
+// head), the log-sums of 64 splits are one load, and 64 splits' partial results are requested at once.  64 splits of 16 rows: 22.4 us
+// with one group, 4.6 with four; 13 splits of 22 thousand rows 16 with one, 19 with four.
+constexpr int kSplitChunks = kMostSplits / 64;
 template <typename T, int GROUPS> __global__ __launch_bounds__(256) void soft_combine_kernel(SoftOut to, Spans spans, int n_split)
 {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, at = i / (16 * GROUPS), share = to.rows * to.heads;
@@ -136,44 +137,35 @@ template <typename T, int GROUPS> __global__ __launch_bounds__(256) void soft_co
     const int64_t row = at / to.heads;
     if (!spans.covers(row)) return;
     const int c = static_cast<int>(i & 15) * 4, group = static_cast<int>(i >> 4) % GROUPS, lane = threadIdx.x & 63;
-    float top = -INFINITY, total = 0.f, mine = -INFINITY;
+    float top = -INFINITY, total = 0.f;
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+    auto weight = [&](float l) { return l == -INFINITY ? 0.f : (l == top ? 1.f : fast_exp2(l - top)); };  // -inf: no keys in the piece
+    auto add = [&](float w, const floatx4 &o) {
+        total += w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += w == 0.f ? 0.f : w * o[e];  // a piece without keys left no result
+    };
     if constexpr (GROUPS == 4) {
-        if (lane < n_split) mine = to.part_lse[lane * share + at];
-        top = mine;
+        float l[kSplitChunks];
+#pragma unroll
+        for (int k = 0; k < kSplitChunks; ++k) l[k] = 64 * k + lane < n_split ? to.part_lse[(64 * k + lane) * share + at] : -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kSplitChunks; ++k) top = fmaxf(top, l[k]);
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
-    } else {
-        for (int j = 0; j < n_split; ++j) top = fmaxf(top, to.part_lse[j * share + at]);
-    }
-    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    if constexpr (GROUPS == 4) {
-        floatx4 o[16];  // all on their way at once
 #pragma unroll
-        for (int s = 0; s < 16; ++s) {
-            const int j = 4 * s + group;
-            if (4 * s < n_split) o[s] = *reinterpret_cast<const floatx4 *>(to.part_o + ((j < n_split ? j : 0) * share + at) * 64 + c);
-        }
+        for (int k = 0; k < kSplitChunks; ++k) {
+            if (64 * k >= n_split) break;
+            floatx4 o[16];
 #pragma unroll
-        for (int s = 0; s < 16; ++s)
-            if (4 * s < n_split) {
-                const float l = __shfl(mine, 4 * s + group, 64);  // -inf: no such split, or no keys in it
-                const float w = l == -INFINITY ? 0.f : (l == top ? 1.f : fast_exp2(l - top));
-                total += w;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] += w == 0.f ? 0.f : w * o[s][e];
+            for (int s = 0; s < 16; ++s) {
+                const int j = 64 * k + 4 * s + group;
+                if (64 * k + 4 * s < n_split) o[s] = *reinterpret_cast<const floatx4 *>(to.part_o + ((j < n_split ? j : 0) * share + at) * 64 + c);
             }
-    } else {
-        for (int j = 0; j < n_split; ++j) {
-            const float l = to.part_lse[j * share + at];
-            if (l == -INFINITY) continue;  // no keys in this piece
-            const float w = l == top ? 1.f : exp2f(l - top);
-            const floatx4 o = *reinterpret_cast<const floatx4 *>(to.part_o + (j * share + at) * 64 + c);
-            total += w;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[e] += w * o[e];
+            for (int s = 0; s < 16; ++s)
+                if (64 * k + 4 * s < n_split) add(weight(__shfl(l[k], 4 * s + group, 64)), o[s]);
         }
-    }
-    if constexpr (GROUPS == 4) {
 #pragma unroll
         for (int m = 16; m < 64; m <<= 1) {
             total += __shfl_xor(total, m, 64);
@@ -181,6 +173,12 @@ template <typename T, int GROUPS> __global__ __launch_bounds__(256) void soft_co
             for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], m, 64);
         }
         if (group != 0) return;
+    } else {
+        for (int j = 0; j < n_split; ++j) top = fmaxf(top, to.part_lse[j * share + at]);
+        for (int j = 0; j < n_split; ++j) {
+            const float w = weight(to.part_lse[j * share + at]);
+            if (w != 0.f) add(w, *reinterpret_cast<const floatx4 *>(to.part_o + (j * share + at) * 64 + c));
+        }
     }
     const float w = total == 0.f ? 0.f : 1.f / total;
     T *dst = static_cast<T *>(to.out) + at * 64 + c;
@@ -570,9 +568,9 @@ hipError_t launch_grad_kv(const CrossArgs &a, bool is_bf16, hipStream_t stream)
 
 hipError_t launch_soft_combine(const SoftOut &to, const Spans &spans, int n_split, bool is_bf16, hipStream_t stream)
 {
-    const bool wide = n_split >= 8 && to.rows * to.heads <= 8192;  // at most 64 splits
+    const bool wide = n_split >= 8 && to.rows * to.heads <= 8192;
     const int64_t blocks = (to.rows * to.heads * (wide ? 64 : 16) + 255) / 256;
-    if (!grid_ok(blocks) || n_split > 64) return hipErrorInvalidValue;
+    if (!grid_ok(blocks) || n_split > kMostSplits) return hipErrorInvalidValue;
     auto kernel = is_bf16 ? (wide ? &soft_combine_kernel<bf16_t, 4> : &soft_combine_kernel<bf16_t, 1>)
                           : (wide ? &soft_combine_kernel<float, 4> : &soft_combine_kernel<float, 1>);
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, to, spans, n_split);

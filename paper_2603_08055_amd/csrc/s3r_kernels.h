@@ -297,6 +297,8 @@ struct CrossArgs {
 
 // few_rows: a workgroup's waves divide the keys of 16 rows, and not 128 rows, among them (tiles accordingly).
 hipError_t launch_cross(const CrossArgs &a, bool few_rows, bool is_bf16, hipStream_t stream);
+// n_split: at most kMostSplits
+constexpr int kMostSplits = 256;
 hipError_t launch_soft_combine(const SoftOut &to, const Spans &spans, int n_split, bool is_bf16, hipStream_t stream);
 // The gradient of queries comes first: it leaves stats [heads][n_q][2], of every row its log-sum in log2 (+inf for a row without keys)
 // and -(out . d_out), from to.out, to.lse and d_out.

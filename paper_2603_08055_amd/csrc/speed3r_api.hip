@@ -1012,11 +1012,11 @@ int pieces(int64_t workgroups, int64_t units, const Pace &pace, double part_byte
     if (uneven) {
         int64_t s = (256 * (pace.resident < 2 ? 1 : 2) + workgroups - 1) / workgroups;
         if (s > units / pace.least) s = units / pace.least;
-        return s < 1 ? 1 : (s > 64 ? 64 : static_cast<int>(s));
+        return s < 1 ? 1 : (s > s3r::kMostSplits ? s3r::kMostSplits : static_cast<int>(s));
     }
     int most = 1;
     double shortest = time_us(1);
-    while (most < 64 && units >= static_cast<int64_t>(pace.least) * (most + 1)) {
+    while (most < s3r::kMostSplits && units >= static_cast<int64_t>(pace.least) * (most + 1)) {
         const double us = time_us(++most);
         if (us < shortest) shortest = us;
     }
@@ -1032,7 +1032,7 @@ int pieces_few(int64_t workgroups, int64_t units)
     if (workgroups >= 192) return 1;
     int64_t s = (1024 + workgroups - 1) / workgroups;
     if (s > units / 4) s = units / 4;
-    return s < 1 ? 1 : (s > 64 ? 64 : static_cast<int>(s));
+    return s < 1 ? 1 : (s > s3r::kMostSplits ? s3r::kMostSplits : static_cast<int>(s));
 }
 
 struct CrossPlan {
@@ -1064,7 +1064,11 @@ s3r_status plan_cross(const s3r_cross_params *p, CrossPlan *out)
     auto units_of = [&](int64_t rows) { return ((uneven ? (4 * rows / c.batch < rows ? 4 * rows / c.batch : rows) : rows) + 63) / 64; };
     const int64_t items = p->n_q * c.per_row, units = units_of(p->n_kv);
     const double q_bytes = 256.0 * static_cast<double>(p->n_q) * p->heads, kv_bytes = 512.0 * static_cast<double>(p->n_kv) * p->kv_heads;
-    c.few_rows = items <= int64_t(16) * c.batch;
+    // Few rows for a sequence: tiles of 16, which bring the keys in once each, in place of one of 128, whose waves are mostly idle.  Up to
+    // two tiles where keys and values stay in the L2s (us, one of 128 / two of 16: 2000 keys of 16 heads 11.9 / 9.3, 20000 of 4 heads 14.6 /
+    // 15.3, 10992 of 16 heads (45 MB) 19.7 / 21.9; fp32 2000 keys 23 / 16, 20000 of 4 heads 30 / 44).
+    const int64_t kv_tensors = p->n_kv * p->kv_heads * (bf16 ? 256 : 512);
+    c.few_rows = items <= int64_t(kv_tensors <= (24 << 20) ? 32 : 16) * c.batch;
     c.tiles = s3r::most_tiles(p->n_q, c.per_row, c.few_rows ? 16 : 128, c.batch);
     c.split = c.few_rows ? pieces_few(c.tiles * p->kv_heads, units) : pieces(c.tiles * p->kv_heads, units, kCrossPace[bf16], q_bytes, uneven);
     c.least = c.few_rows ? kFewLeast : kCrossPace[bf16].least;
@@ -1248,7 +1252,10 @@ s3r_status plan_cache(const s3r_cache_params *p, CachePlan *out)
     CachePlan c{};
     const int per_row = p->heads / p->kv_heads;
     const int64_t units = (int64_t(p->max_pages) * p->page + 63) / 64;
-    c.few_rows = p->n_rows * per_row <= int64_t(16) * p->batch;
+    // Few rows for a sequence: tiles of 16 in place of one of 128.  Codes are a quarter of bf16 keys, and three tiles still take less than
+    // one mostly idle one (us, one of 128 / tiles of 16: 48 rows over 10992 tokens of 16 heads 23.4 / 16.1, over 137400 122 / 87, 64
+    // sequences of 1500 tokens 34.9 / 31.1; 64 rows 25 / 20, 123 / 123, 36 / 40).
+    c.few_rows = p->n_rows * per_row <= int64_t(48) * p->batch;
     c.tiles = s3r::most_tiles(p->n_rows, per_row, c.few_rows ? 16 : 128, p->batch);
     const Pace &pace = kCachePace[p->dtype == S3R_BF16];
     c.split = c.few_rows ? pieces_few(c.tiles * p->kv_heads, units)
