@@ -362,6 +362,10 @@ hipError_t launch_cache_attn(const CacheArgs &a, bool few_rows, bool is_bf16, hi
 hipError_t launch_cache_status(const CacheArgs &a, bool appends, int *status, hipStream_t stream);
 
 // Most tiles that `batch` sequences of n rows together can have.
-inline int64_t most_tiles(int64_t n, int per_row, int tile, int batch) { return n * per_row / tile + batch; }
+inline int64_t most_tiles(int64_t n, int per_row, int tile, int batch)
+{
+    const int64_t most = batch == 1 ? (n * per_row + tile - 1) / tile : n * per_row / tile + batch;
+    return most < 1 ? 1 : most;
+}
 
 }  // namespace s3r

@@ -995,7 +995,8 @@ s3r_status check_strides(const char *what, int64_t tok, int64_t head)
 // joins them (3.5 us, and `part_bytes` of partial results for a piece at 5 TB/s; their way out is under the work).  A piece has
 // `least` units or more.  uneven: sequences of several lengths, or causal rows, of which only the longest is known here; then pieces for
 // two workgroups on every CU (one where no more fit), were all as long as that.
-// Measured, 1374 rows over 27480 keys, 16 heads (176 tiles): PIECES_A; 2748 rows over 10992 keys: PIECES_B.
+// Measured, 16 heads: 1374 rows over 27480 keys (176 workgroups) in 3 pieces 300 us, in 10 215-238 and 13 to join them; gradient of q,
+// 2748 rows over 10992 keys (352), in 2 pieces 335, in 4 255 and 16.
 struct Pace { double unit_us; int resident, least; };
 constexpr Pace kCrossPace[2] = {{2.2, 2, 3}, {0.67, 4, 4}};  // [bf16]
 constexpr Pace kGradQPace[2] = {{5.5, 1, 3}, {1.1, 2, 4}};
@@ -1231,10 +1232,11 @@ struct CachePlan {
     bool few_rows;
     int split, least;
     int64_t tiles;
-    size_t part_o, part_lse, total;
+    size_t part_o, part_lse, need, total;
 };
 
-s3r_status plan_cache(const s3r_cache_params *p, CachePlan *out)
+// attends: the attention's pieces as well.  Either order of its rows, causal or not, has room in the workspace of the larger.
+s3r_status plan_cache(const s3r_cache_params *p, bool attends, CachePlan *out)
 {
     if (!p) return fail(S3R_ERR_INVALID_ARG, "params is null");
     s3r_status st = check_heads(p->heads, p->kv_heads, p->head_dim, p->dtype);
@@ -1257,16 +1259,23 @@ s3r_status plan_cache(const s3r_cache_params *p, CachePlan *out)
     // sequences of 1500 tokens 34.9 / 31.1; 64 rows 25 / 20, 123 / 123, 36 / 40).
     c.few_rows = p->n_rows * per_row <= int64_t(48) * p->batch;
     c.tiles = s3r::most_tiles(p->n_rows, per_row, c.few_rows ? 16 : 128, p->batch);
-    const Pace &pace = kCachePace[p->dtype == S3R_BF16];
-    c.split = c.few_rows ? pieces_few(c.tiles * p->kv_heads, units)
-                         : pieces(c.tiles * p->kv_heads, units, pace, 256.0 * static_cast<double>(p->n_rows) * p->heads, p->batch > 1 || p->causal);
-    c.least = c.few_rows ? kFewLeast : pace.least;
-    const size_t rows = static_cast<size_t>(p->n_rows) * p->heads;
-    size_t off = 0;
-    auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
-    c.part_o = take(c.split > 1 ? c.split * rows * 64 * sizeof(float) : 0);
-    c.part_lse = take(c.split > 1 ? c.split * rows * sizeof(float) : 0);
-    c.total = off;
+    if (attends) {
+        const Pace &pace = kCachePace[p->dtype == S3R_BF16];
+        const int64_t workgroups = c.tiles * p->kv_heads;
+        const size_t rows = static_cast<size_t>(p->n_rows) * p->heads;
+        auto layout = [&](bool uneven) {
+            c.split = c.few_rows ? pieces_few(workgroups, units) : pieces(workgroups, units, pace, 256.0 * static_cast<double>(rows), uneven);
+            const size_t parts = c.split > 1 ? c.split * rows : 0;
+            c.part_o = 0;
+            c.part_lse = align_up(parts * 64 * sizeof(float));
+            return c.part_lse + align_up(parts * sizeof(float));
+        };
+        c.least = c.few_rows ? kFewLeast : pace.least;
+        const bool uneven = p->batch > 1 || p->causal;
+        const size_t other = layout(!uneven), need = layout(uneven);
+        c.need = need;
+        c.total = need > other ? need : other;
+    }
     *out = c;
     return S3R_OK;
 }
@@ -1307,13 +1316,13 @@ s3r_status cache_args(const s3r_cache_params *p, s3r::CacheArgs *out)
 size_t speed3r_cache_workspace_bytes(const s3r_cache_params *p)
 {
     CachePlan c;
-    return plan_cache(p, &c) == S3R_OK ? c.total : SIZE_MAX;
+    return plan_cache(p, true, &c) == S3R_OK ? c.total : SIZE_MAX;
 }
 
 s3r_status speed3r_cache_append(const s3r_cache_params *p)
 {
     CachePlan c;
-    s3r_status st = plan_cache(p, &c);
+    s3r_status st = plan_cache(p, false, &c);
     if (st != S3R_OK) return st;
     s3r::CacheArgs a;
     st = cache_args(p, &a);
@@ -1341,7 +1350,7 @@ s3r_status speed3r_cache_append(const s3r_cache_params *p)
 s3r_status speed3r_cache_read(const s3r_cache_params *p)
 {
     CachePlan c;
-    s3r_status st = plan_cache(p, &c);
+    s3r_status st = plan_cache(p, false, &c);
     if (st != S3R_OK) return st;
     s3r::CacheArgs a;
     st = cache_args(p, &a);
@@ -1358,7 +1367,7 @@ s3r_status speed3r_cache_read(const s3r_cache_params *p)
 s3r_status speed3r_cache_attn(const s3r_cache_params *p)
 {
     CachePlan c;
-    s3r_status st = plan_cache(p, &c);
+    s3r_status st = plan_cache(p, true, &c);
     if (st != S3R_OK) return st;
     s3r::CacheArgs a;
     st = cache_args(p, &a);
@@ -1366,7 +1375,7 @@ s3r_status speed3r_cache_attn(const s3r_cache_params *p)
     if (p->n_rows > 0 && (!p->q || !p->out)) return fail(S3R_ERR_INVALID_ARG, "q and out must be non-null");
     if (p->n_rows > 0 && p->q == p->out) return fail(S3R_ERR_INVALID_ARG, "out must not alias an input");
     if (p->causal != 0 && p->causal != 1) return fail(S3R_ERR_INVALID_ARG, "causal (%d) must be 0 or 1", p->causal);
-    st = check_workspace(p->workspace, p->workspace_bytes, c.total);
+    st = check_workspace(p->workspace, p->workspace_bytes, c.need);
     if (st != S3R_OK) return st;
     hipStream_t s = static_cast<hipStream_t>(p->stream);
     const bool bf16 = p->dtype == S3R_BF16;

@@ -148,6 +148,29 @@ def test_workspaces(s3r):
         s3r.speed3r_cache_workspace_bytes(c, 1, 6, s3r.S3R_BF16, 1, 4)
 
 
+@pytest.mark.parametrize("rows", [0, 1, 40, 100, 1374, 8192])
+@pytest.mark.parametrize("batch", [1, 3])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_cache_workspace_serves_causal_rows_and_others(s3r, rows, batch, dtype):
+    need = []
+    for causal in (0, 1):
+        p = cache(s3r, n_rows=rows, batch=batch, row_start=P, max_pages=700, page=64, causal=causal, dtype=dtype)
+        need.append(s3r.load().speed3r_cache_workspace_bytes(ctypes.byref(p)))
+        if need[-1] and rows:
+            p.workspace, p.workspace_bytes = 0x1000000 + 16, need[-1]      # refused for its alignment, and not for its size
+            assert s3r.load().speed3r_cache_attn(ctypes.byref(p)) == INVALID and "256" in s3r.speed3r_last_error()
+    assert need[0] == need[1] < 1 << 40
+
+
+@pytest.mark.parametrize("n_q,n_kv", [(0, 0), (0, 5000), (5000, 0), (1, 1), (1 << 20, 1 << 20)])
+@pytest.mark.parametrize("batch", [1, 7])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_cross_workspace_of_any_size(s3r, n_q, n_kv, batch, dtype):
+    p = cross(s3r, n_q=n_q, n_kv=n_kv, batch=batch, q_start=P, kv_start=P, dtype=dtype)
+    for backward in (0, 1):
+        assert s3r.load().speed3r_cross_workspace_bytes(ctypes.byref(p), backward) < 1 << 40
+
+
 def test_binding_refuses_what_it_can_see(s3r):
     q, kv = torch.zeros((4, 2, 64), dtype=torch.bfloat16), torch.zeros((8, 2, 64), dtype=torch.bfloat16)
     with pytest.raises(TypeError, match="GPU"):
