@@ -255,7 +255,8 @@ s3r_status speed3r_select_attn(const void *q, const void *k, const void *v, cons
  *   this is reported through `status`; the call then runs on entries held into range (memory-safe).  Rows outside all sequences are
  *   left as they were, in outputs and gradients alike.
  *   Mask: keys with key_mask 0 take no part, whatever their k and v hold (padding, invalid patches); their gradients are 0.
- *   A query row without any key gets out = 0, lse = -inf and gradient 0.
+ *   A query row without any key, or whose scores are all -inf, gets out = 0 and lse = -inf; without any key its gradient is 0.
+ *   Limits: 65536 sequences, batch * kv_heads 2^19, rows * heads 2^28 (the cache calls: rows * (heads + 2 kv_heads)).
  *   Sums, maxima and log-sums are fp32.  bf16 data: probabilities (and dS, in the gradient) enter the second product rounded to
  *   bf16.  fp32 data: products in bf16 parts, to fp32 precision (an infinity in v or
  *   d_out may come out as NaN).
@@ -337,7 +338,7 @@ typedef struct s3r_cache_params {
 s3r_status speed3r_cache_append(const s3r_cache_params *p);
 /* The rows' tokens as values: what the cache holds for them, exactly (to k and v). */
 s3r_status speed3r_cache_read(const s3r_cache_params *p);
-/* out = softmax(scale q . k) v over the cached tokens that a row sees; a row that sees none gets out = 0, lse = -inf.  q is taken as it is
+/* out = softmax(scale q . k) v over the cached tokens that a row sees; a row that sees none (or only scores of -inf) gets out = 0, lse = -inf.  q is taken as it is
  * (rotated by append).  NaNs in the cache reach only the rows that see them.  Sums, maxima and log-sums are fp32; cached values enter
  * exactly; bf16 rows: probabilities enter the second product rounded to bf16. */
 s3r_status speed3r_cache_attn(const s3r_cache_params *p);

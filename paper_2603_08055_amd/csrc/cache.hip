@@ -450,7 +450,7 @@ template <typename T, int WAVES, bool WIDE> hipError_t launch_few(const CacheArg
 template <typename T> hipError_t launch_cache_attn_t(const CacheArgs &a, bool few_rows, hipStream_t stream)
 {
     const int64_t shares = a.tiles * a.n_split * a.cache.kv_heads, n = few_rows ? shares : xcd_padded(shares);
-    if (!grid_ok(n)) return hipErrorInvalidValue;
+    if (!grid_ok(few_rows ? 4 * n : n)) return hipErrorInvalidValue;  // (up to 1024 threads)
     if (few_rows) {
         constexpr int kMany = sizeof(T) == 4 ? 8 : 16;
         if (a.cache.page_shift >= 6)

@@ -140,10 +140,11 @@ template <typename T, int GROUPS> __global__ __launch_bounds__(256) void soft_co
     float top = -INFINITY, total = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
     auto weight = [&](float l) { return l == -INFINITY ? 0.f : (l == top ? 1.f : fast_exp2(l - top)); };  // -inf: no keys in the piece
-    auto add = [&](float w, const floatx4 &o) {
+    auto add = [&](float l, const floatx4 &o) {
+        const float w = weight(l);
         total += w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] += w == 0.f ? 0.f : w * o[e];  // a piece without keys left no result
+        for (int e = 0; e < 4; ++e) acc[e] += l == -INFINITY ? 0.f : w * o[e];  // a piece without keys left no result
     };
     if constexpr (GROUPS == 4) {
         float l[kSplitChunks];
@@ -164,7 +165,7 @@ template <typename T, int GROUPS> __global__ __launch_bounds__(256) void soft_co
             }
 #pragma unroll
             for (int s = 0; s < 16; ++s)
-                if (64 * k + 4 * s < n_split) add(weight(__shfl(l[k], 4 * s + group, 64)), o[s]);
+                if (64 * k + 4 * s < n_split) add(__shfl(l[k], 4 * s + group, 64), o[s]);
         }
 #pragma unroll
         for (int m = 16; m < 64; m <<= 1) {
@@ -176,8 +177,8 @@ template <typename T, int GROUPS> __global__ __launch_bounds__(256) void soft_co
     } else {
         for (int j = 0; j < n_split; ++j) top = fmaxf(top, to.part_lse[j * share + at]);
         for (int j = 0; j < n_split; ++j) {
-            const float w = weight(to.part_lse[j * share + at]);
-            if (w != 0.f) add(w, *reinterpret_cast<const floatx4 *>(to.part_o + (j * share + at) * 64 + c));
+            const float l = to.part_lse[j * share + at];
+            if (l != -INFINITY) add(l, *reinterpret_cast<const floatx4 *>(to.part_o + (j * share + at) * 64 + c));
         }
     }
     const float w = total == 0.f ? 0.f : 1.f / total;
@@ -514,7 +515,7 @@ template <typename T, int WAVES> hipError_t launch_few(const CrossArgs &a, int64
 template <typename T> hipError_t launch_cross_t(const CrossArgs &a, bool few_rows, hipStream_t stream)
 {
     const int64_t shares = a.tiles * a.n_split * a.kv_heads, n = few_rows ? shares : xcd_padded(shares);
-    if (!grid_ok(n)) return hipErrorInvalidValue;
+    if (!grid_ok(few_rows ? 2 * n : n)) return hipErrorInvalidValue;  // (up to 512 threads)
     if (few_rows) {
         if constexpr (sizeof(T) == 2)
             if (a.n_split == 1) return launch_few<T, 8>(a, n, stream);

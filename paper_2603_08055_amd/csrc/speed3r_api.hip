@@ -981,6 +981,15 @@ s3r_status check_heads(int heads, int kv_heads, int head_dim, int dtype)
     return S3R_OK;
 }
 
+// A workgroup looks for its sequence 64 at a time, and a launch of few rows has up to four workgroups of 1024 threads for a sequence
+// and head.
+s3r_status check_batch(int batch, int kv_heads)
+{
+    if (batch > 65536 || batch > (1 << 19) / kv_heads)
+        return fail(S3R_ERR_UNSUPPORTED, "batch (%d) exceeds 65536, or batch * kv_heads 2^19", batch);
+    return S3R_OK;
+}
+
 s3r_status check_strides(const char *what, int64_t tok, int64_t head)
 {
     if (tok < 0 || head < 0 || tok % 8 != 0 || head % 8 != 0)
@@ -1057,8 +1066,9 @@ s3r_status plan_cross(const s3r_cross_params *p, CrossPlan *out)
     CrossPlan c{};
     c.batch = p->batch == 0 ? 1 : p->batch;
     c.per_row = p->heads / p->kv_heads;
-    if (p->n_q > kMaxRowHeads / p->heads || p->n_kv > kMaxRowHeads / p->kv_heads || c.batch > (1 << 22) / p->kv_heads)
-        return fail(S3R_ERR_UNSUPPORTED, "rows * heads exceeds 2^28, or batch * kv_heads 2^22");
+    if (p->n_q > kMaxRowHeads / p->heads || p->n_kv > kMaxRowHeads / p->kv_heads) return fail(S3R_ERR_UNSUPPORTED, "rows * heads exceeds 2^28");
+    st = check_batch(c.batch, p->kv_heads);
+    if (st != S3R_OK) return st;
     const int bf16 = p->dtype == S3R_BF16;
     const bool uneven = c.batch > 1;
     // (the longest of several sequences counts, and only their sum is known: four times their mean, if there is that much)
@@ -1249,8 +1259,9 @@ s3r_status plan_cache(const s3r_cache_params *p, bool attends, CachePlan *out)
     if (p->batch > 1 && !p->row_start) return fail(S3R_ERR_INVALID_ARG, "batch (%d) must be 1 without row_start", p->batch);
     if (int64_t(p->max_pages) * p->page > 0x7fffffffLL - 4096 || p->n_pages > 0x7fffffffLL)
         return fail(S3R_ERR_UNSUPPORTED, "max_pages * page exceeds 2^31 - 4097 tokens, or n_pages 2^31 - 1");
-    if (p->n_rows > kMaxRowHeads / (p->heads + 2 * p->kv_heads) || p->batch > (1 << 22) / p->kv_heads)
-        return fail(S3R_ERR_UNSUPPORTED, "rows * (heads + 2 kv_heads) exceeds 2^28, or batch * kv_heads 2^22");
+    if (p->n_rows > kMaxRowHeads / (p->heads + 2 * p->kv_heads)) return fail(S3R_ERR_UNSUPPORTED, "rows * (heads + 2 kv_heads) exceeds 2^28");
+    st = check_batch(p->batch, p->kv_heads);
+    if (st != S3R_OK) return st;
     CachePlan c{};
     const int per_row = p->heads / p->kv_heads;
     const int64_t units = (int64_t(p->max_pages) * p->page + 63) / 64;
@@ -1328,6 +1339,7 @@ s3r_status speed3r_cache_append(const s3r_cache_params *p)
     st = cache_args(p, &a);
     if (st != S3R_OK) return st;
     if (p->n_rows > 0 && (!p->k || !p->v)) return fail(S3R_ERR_INVALID_ARG, "k and v must be non-null");
+    if (p->k_codes == p->v_codes || p->k_scales == p->v_scales) return fail(S3R_ERR_INVALID_ARG, "keys and values must not share an array");
     if ((p->cos != nullptr) != (p->sin != nullptr)) return fail(S3R_ERR_INVALID_ARG, "cos and sin must be given together");
     if (p->n_rows > 0 && (p->q != nullptr) != (p->out != nullptr)) return fail(S3R_ERR_INVALID_ARG, "q and out must be given together");
     if (p->q && !p->cos) return fail(S3R_ERR_INVALID_ARG, "q is given to be rotated: cos and sin are needed");

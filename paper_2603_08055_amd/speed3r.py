@@ -393,10 +393,22 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i:
 
 
 def _stream_of(stream, index):
+    if isinstance(stream, torch.cuda.Stream) and stream.device_index != index:
+        raise ValueError(f"stream belongs to GPU {stream.device_index}, the tensors to GPU {index}")
     return _raw_stream(index) if stream is None else _stream(stream)
 
 
-def _call(fn, p, need, workspace, index):
+def _empty_on(need, stream, index):
+    """`need` bytes of the allocator's memory for the stream that uses them: it may be given to nothing else before that is done."""
+    if stream is None:
+        return torch.empty(need, dtype=torch.uint8, device=f"cuda:{index}")
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=index) if int(stream) else torch.cuda.default_stream(index)
+    with torch.cuda.stream(stream):
+        return torch.empty(need, dtype=torch.uint8, device=f"cuda:{index}")
+
+
+def _call(fn, p, need, workspace, index, stream=None):
     """The call with a workspace of `need` bytes (2^64 - 1: its arguments are wrong and the call says why), the caller's where there
     is one.  Returns the workspace."""
     if workspace is not None:
@@ -404,7 +416,7 @@ def _call(fn, p, need, workspace, index):
                 or not workspace.is_contiguous():
             raise TypeError(f"workspace must be a contiguous uint8 tensor on GPU {index}")
     elif 0 < need < 1 << 62:
-        workspace = torch.empty(need, dtype=torch.uint8, device=f"cuda:{index}")
+        workspace = _empty_on(need, stream, index)
     if workspace is not None:
         p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel()
     if index == torch.cuda.current_device():
@@ -458,7 +470,7 @@ def speed3r_cross_attn(q, k, v, out, *, lse=None, q_start=None, kv_start=None, k
     used (None: none was needed)."""
     index, lib = _gpu(q, "q"), load()
     p = _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, status, stream, index)
-    return _call(lib.speed3r_cross_attn, p, lib.speed3r_cross_workspace_bytes(ctypes.byref(p), 0), workspace, index)
+    return _call(lib.speed3r_cross_attn, p, lib.speed3r_cross_workspace_bytes(ctypes.byref(p), 0), workspace, index, stream)
 
 
 def speed3r_cross_attn_backward(q, k, v, out, lse, d_out, dq, dk, dv, *, q_start=None, kv_start=None, key_mask=None,
@@ -469,7 +481,7 @@ def speed3r_cross_attn_backward(q, k, v, out, lse, d_out, dq, dk, dv, *, q_start
     p = _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, status, stream, index)
     p.d_out, p.dq = _arg(d_out, "d_out", index, q.dtype, q.shape), _arg(dq, "dq", index, q.dtype, q.shape)
     p.dk, p.dv = _arg(dk, "dk", index, q.dtype, k.shape), _arg(dv, "dv", index, q.dtype, k.shape)
-    return _call(lib.speed3r_cross_attn_backward, p, lib.speed3r_cross_workspace_bytes(ctypes.byref(p), 1), workspace, index)
+    return _call(lib.speed3r_cross_attn_backward, p, lib.speed3r_cross_workspace_bytes(ctypes.byref(p), 1), workspace, index, stream)
 
 
 class PagedCache(NamedTuple):
@@ -566,7 +578,7 @@ def speed3r_cache_attn(cache, q, out, page_table, kv_len, row_start=None, *, cau
     index, lib = _gpu(cache[0], "the cache"), load()
     p = _cache_params(cache, q, page_table, kv_len, row_start, status, stream, index, q=q, out=out, causal=int(bool(causal)),
                       softmax_scale=softmax_scale, lse=lse)
-    return _call(lib.speed3r_cache_attn, p, lib.speed3r_cache_workspace_bytes(ctypes.byref(p)), workspace, index)
+    return _call(lib.speed3r_cache_attn, p, lib.speed3r_cache_workspace_bytes(ctypes.byref(p)), workspace, index, stream)
 
 
 def speed3r_probe_select_loads(q, k, v, idx, out, block, ring_stages=0, wg_per_cu=0, stream=None):

@@ -65,6 +65,7 @@ INVALID, UNSUPPORTED, WORKSPACE = 1, 2, 3
     (dict(heads=0), INVALID, "heads"), (dict(kv_heads=0), INVALID, "kv_heads"), (dict(n_q=-1), INVALID, "n_q"),
     (dict(n_kv=-1), INVALID, "n_kv"), (dict(batch=2), INVALID, "batch"), (dict(batch=-1), INVALID, "batch"),
     (dict(q_start=P), INVALID, "together"), (dict(q_start=P, kv_start=P, batch=0), INVALID, "batch"),
+    (dict(q_start=P, kv_start=P, batch=65537), UNSUPPORTED, "65536"), (dict(q_start=P, kv_start=P, batch=32769, heads=16, kv_heads=16), UNSUPPORTED, "2^19"),
     (dict(n_q=1 << 27), UNSUPPORTED, "2^28"), (dict(n_kv=1 << 40), UNSUPPORTED, "2^28"), (dict(heads=1 << 17, kv_heads=1), UNSUPPORTED, "heads"),
     (dict(q=None), INVALID, "null"), (dict(out=None), INVALID, "null"), (dict(k=None), INVALID, "null"), (dict(v=None), INVALID, "null"),
     (dict(q=P + 2), INVALID, "aligned"), (dict(out=0x20008), INVALID, "aligned"), (dict(lse=0x30002), INVALID, "aligned"),
@@ -112,7 +113,8 @@ def cache(s3r, **change):
     (dict(n_pages=1 << 31), UNSUPPORTED, "n_pages"), (dict(k_codes=None), INVALID, "null"), (dict(v_scales=None), INVALID, "null"),
     (dict(page_table=None), INVALID, "null"), (dict(kv_len=None), INVALID, "null"), (dict(v_codes=P + 8), INVALID, "aligned"),
     (dict(k_scales=P + 1), INVALID, "aligned"), (dict(out=0x400008), INVALID, "aligned"), (dict(kv_stride_tok=12), INVALID, "stride"),
-    (dict(q_stride_head=-8), INVALID, "stride"),
+    (dict(q_stride_head=-8), INVALID, "stride"), (dict(row_start=P, batch=65537), UNSUPPORTED, "65536"),
+    (dict(row_start=P, batch=32769, heads=16, kv_heads=16), UNSUPPORTED, "2^19"),
 ])
 def test_cache_refusals(s3r, change, status, word):
     p, lib = cache(s3r, **change), s3r.load()
@@ -124,6 +126,7 @@ def test_cache_refusals(s3r, change, status, word):
     ("append", dict(k=None), INVALID, "null"), ("append", dict(cos=None), INVALID, "together"), ("append", dict(out=None), INVALID, "together"),
     ("append", dict(cos=None, sin=None), INVALID, "rotated"), ("append", dict(rot_axes=3), INVALID, "rot_axes"),
     ("append", dict(rot_axes=2), INVALID, "positions"), ("append", dict(rot_neighbours=2), INVALID, "rot_neighbours"),
+    ("append", dict(v_codes=P), INVALID, "share"), ("append", dict(v_scales=P * 3), INVALID, "share"),
     ("append", dict(n_positions=0), INVALID, "n_positions"), ("append", dict(out=0x100000), INVALID, "alias"),
     ("read", dict(v=None), INVALID, "null"), ("read", dict(v=0x200000), INVALID, "apart"),
     ("attn", dict(q=None), INVALID, "null"), ("attn", dict(out=0x100000), INVALID, "alias"), ("attn", dict(causal=2), INVALID, "causal"),

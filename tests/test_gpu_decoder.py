@@ -206,6 +206,17 @@ def test_infinities_and_nan_that_count(s3r):
     compare(run_cross(s3r, q, k, v), cross_reference(q, k, v, [(0, 40, 0, 100)], keep, SCALE))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows", [5, 150])
+def test_rows_whose_scores_are_all_minus_infinity(s3r, dtype, rows):
+    g = gen(7)
+    q, k, v = normal(g, rows, 2, 64, dtype=dtype).abs() + 1, normal(g, 700, 2, 64, dtype=dtype), normal(g, 700, 2, 64, dtype=dtype)
+    k[:, 1] = -math.inf
+    got = run_cross(s3r, q, k, v)
+    assert bool((got["out"][:, 1] == 0).all()) and bool((got["lse"][1] == -math.inf).all())
+    assert torch.isfinite(got["out"][:, 0]).all() and torch.isfinite(got["lse"][0]).all()
+
+
 def test_broken_starts_are_reported_and_stay_in_range(s3r):
     g = gen(8)
     q, k, v = (normal(g, n, 1, 64, dtype=BF16) for n in (50, 80, 80))
@@ -444,6 +455,19 @@ def test_nan_in_the_cache_reaches_only_rows_that_see_it(s3r, dtype, rows):
     assert torch.isnan(run_attend(s3r, cache, q, pt, [length], [rows], False)["out"][:, 0, 32:]).all()
 
 
+@pytest.mark.parametrize("rows", [3, 200])
+def test_nan_that_a_row_sees_counts_however_little_it_weighs(s3r, rows):
+    """A value of NaN under a weight of e^-512, which is 0 in 32 bits; with few rows it is in a piece of its own that weighs e^-256."""
+    length, page = 2000, 64
+    cache, pt = s3r.PagedCache.empty(32, 1, page), torch.arange(32, dtype=torch.int32, device="cuda")[None]
+    k, v = torch.zeros((length, 1, 64), dtype=BF16, device="cuda"), torch.ones((length, 1, 64), dtype=BF16, device="cuda")
+    k[5], k[1900], v[5, 0, 40] = -4.0, 4.0, math.nan
+    kv_len = torch.tensor([length], dtype=torch.int32, device="cuda")
+    s3r.speed3r_cache_append(cache, k, v, pt, kv_len)
+    out = run_attend(s3r, cache, torch.full((rows, 1, 64), 8.0, dtype=BF16, device="cuda"), pt, [length], [rows], False)["out"]
+    assert torch.isnan(out[:, 0, 32:]).all() and bool((out[:, 0, :32] == 1).all())
+
+
 def test_broken_lists_are_reported_and_stay_in_range(s3r):
     g = gen(41)
     page, batch, width = 16, 3, 4
@@ -645,3 +669,21 @@ def test_another_stream(s3r):
     s3r.speed3r_cross_attn(q, k, v, got, stream=side)
     side.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_workspace_belongs_to_the_stream_of_the_call(s3r, raw):
+    """What a call allocates for itself must not go to the program's own stream while the call's may still be at work."""
+    g = gen(82)
+    q, k, v = normal(g, 8, 2, 64, dtype=BF16), normal(g, 4000, 2, 64, dtype=BF16), normal(g, 4000, 2, 64, dtype=BF16)
+    out, side = torch.empty_like(q), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    workspace = s3r.speed3r_cross_attn(q, k, v, out, stream=side.cuda_stream if raw else side)
+    place, size = workspace.data_ptr(), workspace.numel()
+    del workspace
+    mine = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(3)]
+    assert place not in [t.data_ptr() for t in mine]
+    side.synchronize()
+    want = torch.empty_like(q)
+    s3r.speed3r_cross_attn(q, k, v, want)
+    assert torch.equal(out, want)
