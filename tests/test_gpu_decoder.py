@@ -400,6 +400,21 @@ def test_cache_batches_of_more_than_a_wave(s3r, dtype, page, which):
         compare(run_attend(s3r, cache, q, pt, lengths, rows, causal), attend_reference(cache, q, pt, lengths, rows, causal))
 
 
+@pytest.mark.parametrize("rows", [2, 150])
+def test_pages_that_sequences_share(s3r, rows):
+    """Two sequences with the same first pages, one that has a page twice: the same as with pages of their own."""
+    g = gen(32)
+    page, lengths = 64, [300, 290, 200]
+    cache = filled_cache(s3r, g, 24, 2, page)
+    shared = torch.tensor([[3, 7, 5, 2, 11], [3, 7, 5, 9, 0], [6, 6, 4, 6, 1]], dtype=torch.int32, device="cuda")
+    own = s3r.PagedCache(*(t[shared.flatten().long()].contiguous() for t in cache))
+    apart = torch.arange(15, dtype=torch.int32, device="cuda").reshape(3, 5)
+    q = normal(g, 3 * rows, 4, 64, dtype=BF16)
+    for causal in (True, False):
+        a, b = (run_attend(s3r, c, q, pt, lengths, [rows] * 3, causal) for c, pt in ((cache, shared), (own, apart)))
+        assert torch.equal(a["out"], b["out"]) and torch.equal(a["lse"], b["lse"])
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_cache_rows_in_larger_tensors(s3r, dtype):
     """k, v and q as slices of one projection; rows read back into slices, and what lies between them left alone."""
@@ -525,6 +540,24 @@ def test_offsets_past_32_bits(s3r):
         q = normal(g, rows, 16, 64, dtype=BF16)
         compare(run_attend(s3r, cache, q, pt, [1500], [rows], True), attend_reference(cache, q, pt, [1500], [rows], True))
     assert int(cache.k_codes[: n_pages - 12].max()) == 0
+
+
+def test_more_than_2_to_the_31_elements(s3r):
+    """Rows whose offset in q, out and the gradients passes 32 bits, in elements and in bytes: the last ones, and a whole head."""
+    g = gen(52)
+    n, m, heads = 600_000, 70, 64
+    q, d_out = (torch.empty((n, heads, 64), dtype=BF16, device="cuda").normal_(generator=g) for _ in range(2))
+    k, v = normal(g, m, heads, 64, dtype=BF16), normal(g, m, heads, 64, dtype=BF16)
+    got = run_cross(s3r, q, k, v, d_out)
+    tail = slice(n - 300, n)
+    for h in range(heads):
+        want = attention(q[tail, h], k[:, h], v[:, h], torch.ones((1, m), dtype=torch.bool, device="cuda"), SCALE, BF16, d_out[tail, h])
+        for name in ("out", "dq"):
+            check(name, got[name][tail, h], want[name], want[name + "_tol"])
+        check("lse", got["lse"][h, tail], want["lse"], want["lse_tol"])
+    want = attention(q[:, 63], k[:, 63], v[:, 63], torch.ones((1, m), dtype=torch.bool, device="cuda"), SCALE, BF16, d_out[:, 63])
+    for name in ("out", "dq", "dk", "dv"):
+        check(name, got[name][:, 63], want[name], want[name + "_tol"])
 
 
 # ---- as they are used -------------------------------------------------------------------------------------
@@ -687,3 +720,24 @@ def test_workspace_belongs_to_the_stream_of_the_call(s3r, raw):
     want = torch.empty_like(q)
     s3r.speed3r_cross_attn(q, k, v, want)
     assert torch.equal(out, want)
+
+
+def test_two_calls_at_once(s3r):
+    """Calls of two streams that overlap, each with a workspace that the binding allocates."""
+    g = gen(83)
+    work = []
+    for n, m in ((700, 5000), (3, 20000)):
+        q, k, v, d_out = (normal(g, x, 4, 64, dtype=BF16) for x in (n, m, m, n))
+        work.append((torch.cuda.Stream(), (q, k, v, d_out), run_cross(s3r, q, k, v, d_out)))
+    results = []
+    for _ in range(6):
+        for stream, (q, k, v, d_out), want in work:
+            out, lse, dq, dk, dv = (torch.empty_like(want[x]) for x in ("out", "lse", "dq", "dk", "dv"))
+            stream.wait_stream(torch.cuda.current_stream())
+            s3r.speed3r_cross_attn(q, k, v, out, lse=lse, stream=stream)
+            s3r.speed3r_cross_attn_backward(q, k, v, out, lse, d_out, dq, dk, dv, stream=stream)
+            results.append((want, dict(out=out, lse=lse, dq=dq, dk=dk, dv=dv)))
+    torch.cuda.synchronize()
+    for want, got in results:
+        for name in got:
+            assert torch.equal(got[name], want[name]), name
