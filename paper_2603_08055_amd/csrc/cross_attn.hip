@@ -569,8 +569,11 @@ hipError_t launch_grad_kv(const CrossArgs &a, bool is_bf16, hipStream_t stream)
 
 hipError_t launch_soft_combine(const SoftOut &to, const Spans &spans, int n_split, bool is_bf16, hipStream_t stream)
 {
-    const bool wide = n_split >= 8 && to.rows * to.heads <= 8192;
-    const int64_t blocks = (to.rows * to.heads * (wide ? 64 : 16) + 255) / 256;
+    // (us, wide or not: 5 splits of 4800 rows 17.7 / 19.2 with the attention, 4 of 8192 23.5 / 21.6, 10 of 2048 15.7 / 20.0, 6 of 256 9.8 / 12.8,
+    // 2 of 16 9.0 / 8.5)
+    const int64_t share = to.rows * to.heads;
+    const bool wide = n_split >= 3 && share <= 1024 * (n_split < 8 ? n_split : 8);
+    const int64_t blocks = (share * (wide ? 64 : 16) + 255) / 256;
     if (!grid_ok(blocks) || n_split > kMostSplits) return hipErrorInvalidValue;
     auto kernel = is_bf16 ? (wide ? &soft_combine_kernel<bf16_t, 4> : &soft_combine_kernel<bf16_t, 1>)
                           : (wide ? &soft_combine_kernel<float, 4> : &soft_combine_kernel<float, 1>);

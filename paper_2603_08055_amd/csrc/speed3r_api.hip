@@ -1035,14 +1035,43 @@ int pieces(int64_t workgroups, int64_t units, const Pace &pace, double part_byte
     return most;
 }
 
-// The same where a workgroup holds few rows and memory binds: none where there are workgroups for most CUs (the launch then takes more
-// waves in each), else as many as fill 256 CUs four times over, a unit at least for each of the four waves.
-int pieces_few(int64_t workgroups, int64_t units)
+// The same where a workgroup holds few rows and its waves take the units in turn.  Undivided, it has `waves` of them, takes `whole_us` for
+// a round and `start` rounds' time to start and end; divided, it has four, and takes `unit_us` for a round as one of `resident` on a
+// CU, half as long again as its share alone, and up to 40 % less where few CUs are busy, a round and a quarter to start and end; joining
+// takes `join_us` and 0.03 for a piece.  Only as many pieces are looked at as fill the CUs once, twice .. and 64 and 128, with a unit at
+// least for each wave.  `workgroups`: were the sequences all as long as their mean.
+// Measured / by this model, us, one row for a head (workgroups, units): cross bf16 (16, 172) in 43 pieces 17.0, 16 15.2 / 15.5; (64, 94) 16
+// 26, 4 23 / 23; (1, 2147) 256 21.4, 128 19.8 / 21; (16, 10) 2 9.5 / 9.6, 1 7.4 / 7.5; fp32 (64, 94) 16 80, 4 55 / 53; (128, 24) 2 35 / 33, 1
+// 48 / 49; cache bf16 (128, 94) 8 20 / 20, 2 27, 1 23 / 22; (16, 2147) 64 38 / 42, 16 58; (64, 24) 6 9.8 / 9.7, 1 9.7 / 9.3; fp32 (128, 94) 6
+// 25 / 26, 1 36 / 34.
+struct FewPace { double unit_us; int resident; double join_us, whole_us, start; int waves; };
+constexpr FewPace kCrossFew[2] = {{6.7, 1, 4.0, 6.7, 1.25, 4}, {2.6, 1, 4.0, 3.0, 1.25, 8}};  // [bf16]
+constexpr FewPace kCacheFew[2] = {{1.33, 3, 5.0, 2.45, 2.1, 8}, {0.85, 4, 5.0, 3.0, 1.6, 16}};
+int pieces_few(int64_t workgroups, int64_t units, const FewPace &pace)
 {
-    if (workgroups >= 192) return 1;
-    int64_t s = (1024 + workgroups - 1) / workgroups;
-    if (s > units / 4) s = units / 4;
-    return s < 1 ? 1 : (s > s3r::kMostSplits ? s3r::kMostSplits : static_cast<int>(s));
+    int best = 1;
+    double shortest = static_cast<double>((workgroups + 255) / 256) * (static_cast<double>(units) / pace.waves + pace.start) * pace.whole_us;
+    auto look = [&](int64_t s) {
+        if (s > units / 4) s = units / 4;
+        if (s < 2) return;
+        const int64_t all = workgroups * s, n = (all + 255) / 256, rest = n % pace.resident, rounds = ((units + s - 1) / s + 3) / 4;
+        const double share = static_cast<double>(n) + (rest == 0 ? 0.0 : 0.5 - 0.5 * static_cast<double>(rest - 1) / pace.resident);
+        const double busy = all < 256 ? 0.6 + 0.4 * static_cast<double>(all) / 256 : 1.0;
+        const double us = share * busy * (static_cast<double>(rounds) + 1.25) * pace.unit_us + pace.join_us + 0.03 * static_cast<double>(s);
+        if (us < shortest) {
+            shortest = us;
+            best = static_cast<int>(s);
+        }
+    };
+    for (int n = 1; n <= pace.resident; ++n) look(256 * n / workgroups);
+    look(64);
+    look(128);
+    return best;
+}
+int64_t mean_tiles(int64_t n, int per_row, int tile, int batch)
+{
+    const int64_t some = n < batch ? (n < 1 ? 1 : n) : batch, each = (n * per_row + some - 1) / some;
+    return some * (each < 1 ? 1 : (each + tile - 1) / tile);
 }
 
 struct CrossPlan {
@@ -1075,13 +1104,15 @@ s3r_status plan_cross(const s3r_cross_params *p, CrossPlan *out)
     auto units_of = [&](int64_t rows) { return ((uneven ? (4 * rows / c.batch < rows ? 4 * rows / c.batch : rows) : rows) + 63) / 64; };
     const int64_t items = p->n_q * c.per_row, units = units_of(p->n_kv);
     const double q_bytes = 256.0 * static_cast<double>(p->n_q) * p->heads, kv_bytes = 512.0 * static_cast<double>(p->n_kv) * p->kv_heads;
-    // Few rows for a sequence: tiles of 16, which bring the keys in once each, in place of one of 128, whose waves are mostly idle.  Up to
-    // two tiles where keys and values stay in the L2s (us, one of 128 / two of 16: 2000 keys of 16 heads 11.9 / 9.3, 20000 of 4 heads 14.6 /
-    // 15.3, 10992 of 16 heads (45 MB) 19.7 / 21.9; fp32 2000 keys 23 / 16, 20000 of 4 heads 30 / 44).
+    // Few rows for a sequence: tiles of 16, which bring the keys in once each, in place of one of 128, whose waves are mostly idle: more of
+    // them the smaller keys and values are beside the L2s (us, one of 128 / tiles of 16: 64 rows over 2000 keys of 16 heads 12.6 / 10.6, 48
+    // over 20000 of 4 heads 15.1 / 16.0; 32 over 10992 of 16 heads (45 MB) 19.9 / 19.0, over 137400 of 16 122 / 168; fp32 64 over 2000
+    // 23.7 / 22.5, 32 over 10992 (90 MB) 43.8 / 50.5).
     const int64_t kv_tensors = p->n_kv * p->kv_heads * (bf16 ? 256 : 512);
-    c.few_rows = items <= int64_t(kv_tensors <= (24 << 20) ? 32 : 16) * c.batch;
+    c.few_rows = items <= int64_t(kv_tensors <= (16 << 20) ? 64 : (kv_tensors <= (48 << 20) ? 32 : 16)) * c.batch;
     c.tiles = s3r::most_tiles(p->n_q, c.per_row, c.few_rows ? 16 : 128, c.batch);
-    c.split = c.few_rows ? pieces_few(c.tiles * p->kv_heads, units) : pieces(c.tiles * p->kv_heads, units, kCrossPace[bf16], q_bytes, uneven);
+    c.split = c.few_rows ? pieces_few(mean_tiles(p->n_q, c.per_row, 16, c.batch) * p->kv_heads, units, kCrossFew[bf16])
+                         : pieces(c.tiles * p->kv_heads, units, kCrossPace[bf16], q_bytes, uneven);
     c.least = c.few_rows ? kFewLeast : kCrossPace[bf16].least;
     c.q_tiles = s3r::most_tiles(p->n_q, c.per_row, 128, c.batch);
     c.split_q = pieces(c.q_tiles * p->kv_heads, units, kGradQPace[bf16], bf16 ? 2 * q_bytes : q_bytes, uneven);
@@ -1266,16 +1297,17 @@ s3r_status plan_cache(const s3r_cache_params *p, bool attends, CachePlan *out)
     const int per_row = p->heads / p->kv_heads;
     const int64_t units = (int64_t(p->max_pages) * p->page + 63) / 64;
     // Few rows for a sequence: tiles of 16 in place of one of 128.  Codes are a quarter of bf16 keys, and three tiles still take less than
-    // one mostly idle one (us, one of 128 / tiles of 16: 48 rows over 10992 tokens of 16 heads 23.4 / 16.1, over 137400 122 / 87, 64
-    // sequences of 1500 tokens 34.9 / 31.1; 64 rows 25 / 20, 123 / 123, 36 / 40).
-    c.few_rows = p->n_rows * per_row <= int64_t(48) * p->batch;
+    // one mostly idle one; five where there are too few of those for the card (us, one of 128 / tiles of 16: 80 rows over 10992 tokens of 16
+    // heads 26.1 / 21.1, over 137400 131 / 133, 16 sequences of 1500 tokens and 4 heads 20.3 / 17.5; 64 of these, 48 rows 31 / 31, 64 rows 36 / 40).
+    c.few_rows = p->n_rows * per_row <= int64_t(p->batch * p->kv_heads <= 64 ? 80 : 48) * p->batch;
     c.tiles = s3r::most_tiles(p->n_rows, per_row, c.few_rows ? 16 : 128, p->batch);
     if (attends) {
         const Pace &pace = kCachePace[p->dtype == S3R_BF16];
         const int64_t workgroups = c.tiles * p->kv_heads;
         const size_t rows = static_cast<size_t>(p->n_rows) * p->heads;
         auto layout = [&](bool uneven) {
-            c.split = c.few_rows ? pieces_few(workgroups, units) : pieces(workgroups, units, pace, 256.0 * static_cast<double>(rows), uneven);
+            c.split = c.few_rows ? pieces_few(mean_tiles(p->n_rows, per_row, 16, p->batch) * p->kv_heads, units, kCacheFew[p->dtype == S3R_BF16])
+                                 : pieces(workgroups, units, pace, 256.0 * static_cast<double>(rows), uneven);
             const size_t parts = c.split > 1 ? c.split * rows : 0;
             c.part_o = 0;
             c.part_lse = align_up(parts * 64 * sizeof(float));
@@ -1283,7 +1315,7 @@ s3r_status plan_cache(const s3r_cache_params *p, bool attends, CachePlan *out)
         };
         c.least = c.few_rows ? kFewLeast : pace.least;
         const bool uneven = p->batch > 1 || p->causal;
-        const size_t other = layout(!uneven), need = layout(uneven);
+        const size_t other = c.few_rows ? 0 : layout(!uneven), need = layout(uneven);
         c.need = need;
         c.total = need > other ? need : other;
     }
