@@ -1002,28 +1002,22 @@ s3r_status check_strides(const char *what, int64_t tok, int64_t head)
 // n = ceil(workgroups * pieces / 256) of them, `resident` at a time; one alone on a CU takes half as long again as its share
 // of a full one.  A workgroup takes `unit_us` for each unit and two units' time to start and end; more than one piece costs a launch that
 // joins them (3.5 us, and `part_bytes` of partial results for a piece at 5 TB/s; their way out is under the work).  A piece has
-// `least` units or more.  uneven: sequences of several lengths, or causal rows, of which only the longest is known here; then pieces for
-// two workgroups on every CU (one where no more fit), were all as long as that.
+// `least` units or more.
 // Measured, 16 heads: 1374 rows over 27480 keys (176 workgroups) in 3 pieces 300 us, in 10 215-238 and 13 to join them; gradient of q,
 // 2748 rows over 10992 keys (352), in 2 pieces 335, in 4 255 and 16.
-struct Pace { double unit_us; int resident, least; };
-constexpr Pace kCrossPace[2] = {{2.2, 2, 3}, {0.67, 4, 4}};  // [bf16]
-constexpr Pace kGradQPace[2] = {{5.5, 1, 3}, {1.1, 2, 4}};
-constexpr Pace kGradKvPace[2] = {{7.3, 1, 3}, {1.3, 2, 4}};
-constexpr Pace kCachePace[2] = {{2.0, 2, 3}, {0.85, 3, 4}};
+struct Pace { double unit_us; int resident, least, uneven; };
+constexpr Pace kCrossPace[2] = {{2.2, 2, 3, 256}, {0.67, 4, 4, 512}};  // [bf16]
+constexpr Pace kGradQPace[2] = {{5.5, 1, 3, 256}, {1.1, 2, 4, 512}};
+constexpr Pace kGradKvPace[2] = {{7.3, 1, 3, 256}, {1.3, 2, 4, 512}};
+constexpr Pace kCachePace[2] = {{2.0, 2, 3, 256}, {0.85, 3, 4, 512}};
 constexpr int kFewLeast = 4;
-int pieces(int64_t workgroups, int64_t units, const Pace &pace, double part_bytes, bool uneven)
+int pieces(int64_t workgroups, int64_t units, const Pace &pace, double part_bytes)
 {
     auto time_us = [&](int s) {
         const int64_t n = (workgroups * s + 255) / 256, rest = n % pace.resident;
         const double share = static_cast<double>(n) + (rest == 0 ? 0.0 : 0.5 - 0.5 * static_cast<double>(rest - 1) / pace.resident);
         return share * static_cast<double>((units + s - 1) / s + 2) * pace.unit_us + (s == 1 ? 0.0 : 3.5 + s * part_bytes / 5e6);
     };
-    if (uneven) {
-        int64_t s = (256 * (pace.resident < 2 ? 1 : 2) + workgroups - 1) / workgroups;
-        if (s > units / pace.least) s = units / pace.least;
-        return s < 1 ? 1 : (s > s3r::kMostSplits ? s3r::kMostSplits : static_cast<int>(s));
-    }
     int most = 1;
     double shortest = time_us(1);
     while (most < s3r::kMostSplits && units >= static_cast<int64_t>(pace.least) * (most + 1)) {
@@ -1033,6 +1027,21 @@ int pieces(int64_t workgroups, int64_t units, const Pace &pace, double part_byte
     for (int s = 1; s < most; ++s)
         if (time_us(s) <= 1.01 * shortest) return s;  // the fewest that come within 1 %: their partial results take workspace
     return most;
+}
+
+// The same for sequences of several lengths, or causal rows, of which only the mean (or the longest) is known here: the longer they are, the
+// further apart they can be, and the more workgroups level that out.  16 of them for every unit, up to five for each CU, and at least
+// `uneven`; short ones are left whole where most CUs have a workgroup.  `most`: units of the longest.  Measured, us, forward / gradient
+// (workgroups, units): bf16, 16 times 200 rows over 500 keys (256, 8) in 1 14 / 36, in 2 24 / 51; 17 rows over 28 to 4329 keys (119, 16) gradient
+// in 3 72, in 5 65; 2000, 700 and 100 rows over 4000, 1000 and 9000 keys (360, 73) in 2 109 / 285, 4 95 / 268; 4 times 1374 over 2748 (704, 43)
+// in 1 91 / 291, 2 103 / 319; 5000 and 300 over 9000 and 700 (672, 76) in 1 249 / 848, 2 231 / 810; fp32 300, 20, 900 and 64 over 3000, 8000,
+// 100 and 600 (48, 47) in 9 61 / 235, 16 49 / 188; 500, 1 and 129 over 1369, 700 and 64 (42, 11) in 6 29 / 83, 12 33 / 93.
+int pieces_uneven(int64_t workgroups, int64_t units, int64_t most, const Pace &pace)
+{
+    const int64_t least = workgroups >= 192 ? 256 : pace.uneven, all = 16 * units < least ? least : (units >= 80 ? 1280 : 16 * units);
+    int64_t s = (all + workgroups - 1) / workgroups;
+    if (s > most / pace.least) s = most / pace.least;
+    return s < 1 ? 1 : (s > s3r::kMostSplits ? s3r::kMostSplits : static_cast<int>(s));
 }
 
 // The same where a workgroup holds few rows and its waves take the units in turn.  Undivided, it has `waves` of them, takes `whole_us` for
@@ -1068,6 +1077,7 @@ int pieces_few(int64_t workgroups, int64_t units, const FewPace &pace)
     look(128);
     return best;
 }
+// Tiles, were the sequences all as long as their mean.
 int64_t mean_tiles(int64_t n, int per_row, int tile, int batch)
 {
     const int64_t some = n < batch ? (n < 1 ? 1 : n) : batch, each = (n * per_row + some - 1) / some;
@@ -1102,6 +1112,10 @@ s3r_status plan_cross(const s3r_cross_params *p, CrossPlan *out)
     const bool uneven = c.batch > 1;
     // (the longest of several sequences counts, and only their sum is known: four times their mean, if there is that much)
     auto units_of = [&](int64_t rows) { return ((uneven ? (4 * rows / c.batch < rows ? 4 * rows / c.batch : rows) : rows) + 63) / 64; };
+    auto split_of = [&](int64_t tiles, int64_t held, int per_row, int64_t streamed, const Pace &pace, double part_bytes) {
+        if (!uneven) return pieces(tiles * p->kv_heads, units_of(streamed), pace, part_bytes);
+        return pieces_uneven(mean_tiles(held, per_row, 128, c.batch) * p->kv_heads, streamed / c.batch / 64 + 1, units_of(streamed), pace);
+    };
     const int64_t items = p->n_q * c.per_row, units = units_of(p->n_kv);
     const double q_bytes = 256.0 * static_cast<double>(p->n_q) * p->heads, kv_bytes = 512.0 * static_cast<double>(p->n_kv) * p->kv_heads;
     // Few rows for a sequence: tiles of 16, which bring the keys in once each, in place of one of 128, whose waves are mostly idle: more of
@@ -1112,12 +1126,12 @@ s3r_status plan_cross(const s3r_cross_params *p, CrossPlan *out)
     c.few_rows = items <= int64_t(kv_tensors <= (16 << 20) ? 64 : (kv_tensors <= (48 << 20) ? 32 : 16)) * c.batch;
     c.tiles = s3r::most_tiles(p->n_q, c.per_row, c.few_rows ? 16 : 128, c.batch);
     c.split = c.few_rows ? pieces_few(mean_tiles(p->n_q, c.per_row, 16, c.batch) * p->kv_heads, units, kCrossFew[bf16])
-                         : pieces(c.tiles * p->kv_heads, units, kCrossPace[bf16], q_bytes, uneven);
+                         : split_of(c.tiles, p->n_q, c.per_row, p->n_kv, kCrossPace[bf16], q_bytes);
     c.least = c.few_rows ? kFewLeast : kCrossPace[bf16].least;
     c.q_tiles = s3r::most_tiles(p->n_q, c.per_row, 128, c.batch);
-    c.split_q = pieces(c.q_tiles * p->kv_heads, units, kGradQPace[bf16], bf16 ? 2 * q_bytes : q_bytes, uneven);
+    c.split_q = split_of(c.q_tiles, p->n_q, c.per_row, p->n_kv, kGradQPace[bf16], bf16 ? 2 * q_bytes : q_bytes);
     c.kv_tiles = s3r::most_tiles(p->n_kv, 1, 128, c.batch);
-    c.split_kv = pieces(c.kv_tiles * p->kv_heads, units_of(items), kGradKvPace[bf16], kv_bytes, uneven);
+    c.split_kv = split_of(c.kv_tiles, p->n_kv, 1, items, kGradKvPace[bf16], kv_bytes);
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
     const size_t rows = static_cast<size_t>(p->n_q) * p->heads, keys = static_cast<size_t>(p->n_kv) * p->kv_heads;
@@ -1303,11 +1317,18 @@ s3r_status plan_cache(const s3r_cache_params *p, bool attends, CachePlan *out)
     c.tiles = s3r::most_tiles(p->n_rows, per_row, c.few_rows ? 16 : 128, p->batch);
     if (attends) {
         const Pace &pace = kCachePace[p->dtype == S3R_BF16];
-        const int64_t workgroups = c.tiles * p->kv_heads;
         const size_t rows = static_cast<size_t>(p->n_rows) * p->heads;
         auto layout = [&](bool uneven) {
-            c.split = c.few_rows ? pieces_few(mean_tiles(p->n_rows, per_row, 16, p->batch) * p->kv_heads, units, kCacheFew[p->dtype == S3R_BF16])
-                                 : pieces(workgroups, units, pace, 256.0 * static_cast<double>(rows), uneven);
+            if (c.few_rows)
+                c.split = pieces_few(mean_tiles(p->n_rows, per_row, 16, p->batch) * p->kv_heads, units, kCacheFew[p->dtype == S3R_BF16]);
+            else if (uneven) {
+                // Only the longest is known, and counts.  A sequence alone is uneven by what its own rows do not see: two workgroups on a CU (us,
+                // 600 causal rows over 5000 in 7 pieces 46, 16 51; 2748 over 10992 in 1 287, 2 198).
+                const int64_t mean = p->batch > 1 || units < 32 ? units : 32;
+                c.split = pieces_uneven(mean_tiles(p->n_rows, per_row, 128, p->batch) * p->kv_heads, mean, units, pace);
+            }
+            else
+                c.split = pieces(c.tiles * p->kv_heads, units, pace, 256.0 * static_cast<double>(rows));
             const size_t parts = c.split > 1 ? c.split * rows : 0;
             c.part_o = 0;
             c.part_lse = align_up(parts * 64 * sizeof(float));
