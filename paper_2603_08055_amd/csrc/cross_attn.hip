@@ -269,11 +269,10 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             floatx16 s = {}, dp = minus_d;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                multiply<P>(s, held.q[i], [&](int part) { return kr.x[i][part]; });
-                multiply<P>(dp, grad.q[i], [&](int part) { return vr.x[i][part]; });
-            }
+            each_part<P, P, 4>([&](int step, int i, int j) {
+                s = mfma(kr.x[step][i], held.q[step][j], s);
+                dp = mfma(vr.x[step][i], grad.q[step][j], dp);
+            });
             if (half == 0) {
                 kr.read(k, 1, at);
                 vr.read(v, 1, at);
@@ -432,11 +431,10 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
 #pragma unroll
                 for (int e = 0; e < 4; ++e) dp[4 * b + e] = d[e];
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                multiply<P>(s, kk.q[i], [&](int part) { return qr.x[i][part]; });
-                multiply<P>(dp, vv.q[i], [&](int part) { return gr.x[i][part]; });
-            }
+            each_part<P, P, 4>([&](int step, int i, int j) {
+                s = mfma(qr.x[step][i], kk.q[step][j], s);
+                dp = mfma(gr.x[step][i], vv.q[step][j], dp);
+            });
             if (half == 0) {
                 qr.read(q, 1, at);
                 gr.read(g, 1, at);
