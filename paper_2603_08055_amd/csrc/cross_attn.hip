@@ -372,7 +372,8 @@ template <typename T> __global__ __launch_bounds__(256) void grad_q_combine_kern
     if (kMendD<T> && c == 0) a.stats[2 * ((at - row * a.heads) * a.n_q + row) + 1] -= sum;
 }
 
-template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void grad_kv_kernel(CrossArgs a)
+// PX: bf16 parts in which probabilities and dS enter the products.
+template <typename T, int PX> __global__ __launch_bounds__(256, PX == 1 ? 2 : 1) void grad_kv_kernel(CrossArgs a)
 {
     constexpr int P = UnitPairs<T>::kParts;
     extern __shared__ __align__(16) unsigned char smem[];
@@ -456,9 +457,9 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
                         y[4 * b + e] = x[4 * b + e] * dp[r];
                     }
                 }
-                bf16x8 p[P], ds[P];
-                split_parts<P>(x, p);
-                split_parts<P>(y, ds);
+                bf16x8 p[PX], ds[PX];
+                split_parts<PX>(x, p);
+                split_parts<PX>(y, ds);
 #pragma unroll
                 for (int dt = 0; dt < 2; ++dt) {
                     multiply<P>(vv.o[dt], p, [&](int part) { return gt.x[w][dt][part]; });
@@ -525,15 +526,19 @@ template <typename T> hipError_t launch_cross_t(const CrossArgs &a, bool few_row
     return hipGetLastError();
 }
 
+// Sums of few terms: probabilities and dS rounded to bf16 would be most of the error of dk and dv (2.4e-3 and more, against 1.66e-3 by
+// the rounding of the results themselves, which is what two parts leave).  Longer sums stay at 2.35e-3.  Gradient of 16 heads in bf16, us,
+// one part / two: 1 row over 10992 keys 55 / 59, 64 over 2000 24.8 / 25.7; 128 over 10992 71 / 80; 512 over 10992 137 / 163.
+constexpr int kFewItems = kUnitRows;
 template <typename T> hipError_t launch_grad_t(const CrossArgs &a, bool of_keys, hipStream_t stream)
 {
     const int64_t n = xcd_padded(a.tiles * a.n_split * a.kv_heads);
     if (!grid_ok(n)) return hipErrorInvalidValue;
     const size_t lds = UnitPairs<T>::kStages * (UnitPairs<T>::kStage * sizeof(bf16_t) + (of_keys ? 128 * sizeof(float) : 0));
-    if (of_keys)
-        hipLaunchKernelGGL(grad_kv_kernel<T>, dim3(static_cast<unsigned>(n)), dim3(256), lds, stream, a);
-    else
-        hipLaunchKernelGGL(grad_q_kernel<T>, dim3(static_cast<unsigned>(n)), dim3(256), lds, stream, a);
+    auto kernel = of_keys ? &grad_kv_kernel<T, UnitPairs<T>::kParts> : &grad_q_kernel<T>;
+    if constexpr (sizeof(T) == 2)
+        if (of_keys && a.n_q * a.per_row <= kFewItems * a.q_spans.batch) kernel = &grad_kv_kernel<T, 2>;
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(n)), dim3(256), lds, stream, a);
     return hipGetLastError();
 }
 

@@ -104,13 +104,14 @@ __device__ __forceinline__ float upper_part(float x)
     return __uint_as_float((__float_as_uint(x) & 0xffff0000u) | (x != x ? 0x00400000u : 0u));
 }
 
-// x = p[0] + p[1] + p[2] (parts 3), or p[0] = x rounded to bf16 (parts 1).
+// x = p[0] + p[1] + p[2] (parts 3), or p[0] = x rounded to bf16 (parts 1), p[1] what is left, rounded (parts 2).
 template <int PARTS> __device__ __forceinline__ void split_parts(const float (&x)[8], bf16x8 (&p)[PARTS])
 {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        if constexpr (PARTS == 1) {
+        if constexpr (PARTS <= 2) {
             p[0][j] = static_cast<bf16_t>(x[j]);
+            if constexpr (PARTS == 2) p[1][j] = static_cast<bf16_t>(x[j] - static_cast<float>(p[0][j]));
         } else {
             const float h = upper_part(x[j]), rest = __builtin_isfinite(x[j]) ? x[j] - h : 0.f;
             const float m = __uint_as_float(__float_as_uint(rest) & 0xffff0000u), l = rest - m;

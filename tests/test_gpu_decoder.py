@@ -159,6 +159,34 @@ def test_strided_views(s3r, dtype, n, m):
     compare(got, cross_reference(q, k, v, [(0, n, 0, m)], None, 0.3, d_out))
 
 
+@pytest.mark.parametrize("n,m,heads,kv_heads", [(1, 64, 4, 1), (16, 300, 8, 2), (60, 2000, 2, 2)])
+def test_key_gradients_of_few_rows_are_rounded_once(s3r, n, m, heads, kv_heads):
+    """bf16, up to 64 rows of the heads that share one: P and dS enter in two bf16 parts (2^-16 and 2^-17 for the part that is
+    left out and for its truncation: 2^-15 covers both), D is what the dS lack of 0, and one rounding is left, that of dk and dv."""
+    g = gen(21)
+    q, k, v, d_out = (normal(g, x, h, 64, dtype=BF16) for x, h in ((n, heads), (m, kv_heads), (m, kv_heads), (n, heads)))
+    got = run_cross(s3r, q, k, v, d_out)
+    share, u, h = heads // kv_heads, 2.0 ** -24, 2.0 ** -8
+    chain = (m / 8 + 64 + share * n) * u
+    for kv in range(kv_heads):
+        dk, dv, dk_tol, dv_tol = 0.0, 0.0, 0.0, 0.0
+        for head in range(kv * share, (kv + 1) * share):
+            x, y, gd, vd = q[:, head].double(), k[:, kv].double(), d_out[:, head].double(), v[:, kv].double()
+            s = x @ y.t() * SCALE
+            p = torch.softmax(s, 1)
+            err = 2 * (64 * u * (x.abs() @ y.abs().t()) * SCALE + (s.abs() + 8) * u).amax(1, keepdim=True) + chain        # of P, relative
+            dp, out = gd @ vd.t(), p @ vd
+            ds = p * (dp - (gd * out).sum(1, keepdim=True))
+            size = (dp.abs() + (gd.abs() * out.abs()).sum(1, keepdim=True)) * (1 + h)
+            off_d = (chain + err) * (p * size).sum(1, keepdim=True) + 64 * u * (gd.abs() @ vd.abs().t()).amax(1, keepdim=True)
+            ds_tol = (err + 2.0 ** -15) * p * size + p * off_d + p * 64 * u * (gd.abs() @ vd.abs().t())
+            dk, dv = dk + SCALE * ds.t() @ x, dv + p.t() @ gd
+            dk_tol = dk_tol + SCALE * (ds_tol + chain * ds.abs()).t() @ x.abs()
+            dv_tol = dv_tol + (p * (err + 2.0 ** -15 + chain)).t() @ gd.abs()
+        check("dk", got["dk"][:, kv], dk, dk_tol + h * dk.abs())
+        check("dv", got["dv"][:, kv], dv, dv_tol + h * dv.abs())
+
+
 def test_gradient_against_differences(s3r):
     """fp32: (f(x + t d) - f(x - t d)) / 2 t of f = sum(out * d_out), computed by the forward kernel in fp32 and summed in
     64 bits, against the gradient's product with d.  Cancellation leaves err(out) sqrt(n) / t; the cubic term is t^2: with t = 2^-4
