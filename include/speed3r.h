@@ -338,8 +338,8 @@ typedef struct s3r_cache_params {
 s3r_status speed3r_cache_append(const s3r_cache_params *p);
 /* The rows' tokens as values: what the cache holds for them, exactly (to k and v). */
 s3r_status speed3r_cache_read(const s3r_cache_params *p);
-/* out = softmax(scale q . k) v over the cached tokens that a row sees; a row that sees none (or only scores of -inf) gets out = 0, lse = -inf.  q is taken as it is
- * (rotated by append).  NaNs in the cache reach only the rows that see them.  Sums, maxima and log-sums are fp32; cached values enter
+/* out = softmax(scale q . k) v over the cached tokens that a row sees; a row that sees none (or only scores of -inf) gets out = 0,
+ * lse = -inf.  q is taken as it is (rotated by append).  NaNs in the cache reach only the rows that see them.  Sums, maxima and log-sums are fp32; cached values enter
  * exactly; bf16 rows: probabilities enter the second product rounded to bf16. */
 s3r_status speed3r_cache_attn(const s3r_cache_params *p);
 /* Bytes of device scratch of speed3r_cache_attn; only the shape fields are read.  May be 0; SIZE_MAX on invalid arguments. */

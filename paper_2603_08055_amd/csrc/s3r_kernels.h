@@ -278,8 +278,8 @@ struct SoftOut {
 constexpr int kDiagPage = 4, kDiagSpans = 8, kDiagLength = 16, kDiagPosition = 32;
 
 // q and d_out rows, k and v rows: element strides between rows and between heads.  per_row = heads / kv_heads.  factor = scale * log2(e).
-// tiles: most tiles of the held rows (most_tiles); n_split: most pieces of a tile's streamed rows, of `least` units or more each.  stats: see launch_grad_q.  part_*: partial
-// sums [n_split][rows][heads][64] where n_split > 1, else null (part_sum: [n_split][rows][heads][2]; it and part_pk for bf16 alone).
+// tiles: most tiles of the held rows (most_tiles); n_split: most pieces of a tile's streamed rows, of `least` units or more each.  stats: see
+// launch_grad_q.  part_*: partial sums [n_split][rows][heads][64] where n_split > 1, else null (part_sum: [n_split][rows][heads][2]; it and part_pk for bf16 alone).
 struct CrossArgs {
     const void *q, *k, *v, *d_out;
     int64_t q_row, q_head, kv_row, kv_head;

@@ -173,6 +173,20 @@ template <int PA, int PB, int STEPS, typename Product> __device__ __forceinline_
 // A workgroup's sequence: its number, its rows, and its entry of another list (or 0).
 struct Sequence { int seq, first, len, entry; };
 
+// The sum over the lanes up to this one.  Shifts by 1, 2, 4 and 8 within sixteen lanes, then the last of each sixteen to the next, and of
+// the lower half to the upper: vector instructions, no trips to LDS.
+__device__ __forceinline__ int sum_up_to(int x)
+{
+    constexpr int kShift = 0x110, kLastOf16 = 0x142, kLastOf32 = 0x143;
+    x += __builtin_amdgcn_update_dpp(0, x, kShift + 1, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, kShift + 2, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, kShift + 4, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, kShift + 8, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, kLastOf16, 0xa, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, kLastOf32, 0xc, 0xf, false);
+    return x;
+}
+
 // Tile `t` of the sequences' tiles of `tile` items in turn, a sequence having len * per_row items: its sequence and number
 // in it; false when there are fewer tiles.  All lanes of a wave call it.  What is needed of a sequence is read for 64 of them at once,
 // and not when the number is known: one wait less before a short launch's first key.
@@ -194,12 +208,7 @@ __device__ __forceinline__ bool find_tile(const Spans &spans, const int32_t *lis
             spans.of(b0 + lane, first, len);
             tiles = static_cast<int>((static_cast<int64_t>(len) * per_row + tile - 1) / tile);
         }
-        int upto = tiles;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int v = __shfl_up(upto, d, 64);
-            if (lane >= d) upto += v;
-        }
+        const int upto = sum_up_to(tiles);
         const unsigned long long past = __ballot(before + upto > t);
         if (past != 0) {
             const int l = __ffsll(past) - 1;
