@@ -258,7 +258,7 @@ s3r_status speed3r_select_attn(const void *q, const void *k, const void *v, cons
  *   A query row without any key, or whose scores are all -inf, gets out = 0 and lse = -inf; without any key its gradient is 0.
  *   Limits: 65536 sequences, batch * kv_heads 2^19, rows * heads 2^28 (the cache calls: rows * (heads + 2 kv_heads)).
  *   Sums, maxima and log-sums are fp32.  bf16 data: probabilities (and dS, in the gradient) enter the second product rounded to
- *   bf16, for dk and dv of up to 64 rows (of all heads that share one) in two bf16 parts.  fp32 data: products in bf16 parts, to fp32
+ *   bf16; in the gradient of up to 64 rows (of all heads that share one) in two bf16 parts.  fp32 data: products in bf16 parts, to fp32
  *   precision (an infinity in v or d_out may come out as NaN).
  *   The gradient takes out and lse as the forward call left them; the gradients of shared heads are summed.  Its results do not
  *   depend on the order in which workgroups run. */

@@ -60,6 +60,10 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) 
     store_soft<T>(soft, a.factor, a.to, sh.split, row, head, ok, lane);
 }
 
+// Probabilities of few bf16 rows enter in two parts, which the memory that binds hides (16 rows over 10992 keys of 16 heads 15.4 us with one,
+// 15.6 with two): the error of out is the rounding of its store, also where few keys count (rows over 17 keys, up to 2.4e-3 with one).
+template <typename T> constexpr int kFewParts = sizeof(T) == 4 ? 3 : 2;
+
 // Few rows: WAVES waves with the same 16 rows take the units in turn, values through an LDS stage of their own (8 or 24 KiB).
 template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 || WAVES > 4 ? 1 : 2) void cross_few_kernel(CrossArgs a)
 {
@@ -115,7 +119,7 @@ template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, sizeof
             }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         if (u + WAVES < u1) fetch(u + WAVES);
-        few.template unit<P>([&](int t, int s, bf16x8(&to)[P]) {
+        few.template unit<P, kFewParts<T>>([&](int t, int s, bf16x8(&to)[P]) {
 #pragma unroll
             for (int i = 0; i < P; ++i) to[i] = kk[t][s][i];
         }, mine, seen, a.factor, lane);
@@ -208,7 +212,8 @@ __device__ __forceinline__ float sum8(const bf16x8 &x)
     return s;
 }
 
-template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void grad_q_kernel(CrossArgs a)
+// PX: bf16 parts in which dS enters its product.
+template <typename T, int PX> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void grad_q_kernel(CrossArgs a)
 {
     constexpr int P = UnitPairs<T>::kParts;
     extern __shared__ __align__(16) unsigned char smem[];
@@ -301,12 +306,13 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) 
                     x[j] = dp[8 * w + j];
                     if constexpr (kMendD<T>) add[j & 1] += x[j];
                 }
-                bf16x8 ds[P], p[P];
-                split_parts<P>(x, ds);
+                bf16x8 ds[PX], p[P];
+                split_parts<PX>(x, ds);
                 if constexpr (kMendD<T>) {
                     split_parts<P>(y, p);
                     sum += add[0] + add[1];
                     entered += sum8(ds[0]);
+                    if constexpr (PX == 2) entered += sum8(ds[1]);
                 }
 #pragma unroll
                 for (int dt = 0; dt < 2; ++dt) {
@@ -373,7 +379,7 @@ template <typename T> __global__ __launch_bounds__(256) void grad_q_combine_kern
 }
 
 // PX: bf16 parts in which probabilities and dS enter the products.
-template <typename T, int PX> __global__ __launch_bounds__(256, PX == 1 ? 2 : 1) void grad_kv_kernel(CrossArgs a)
+template <typename T, int PX> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void grad_kv_kernel(CrossArgs a)
 {
     constexpr int P = UnitPairs<T>::kParts;
     extern __shared__ __align__(16) unsigned char smem[];
@@ -526,18 +532,19 @@ template <typename T> hipError_t launch_cross_t(const CrossArgs &a, bool few_row
     return hipGetLastError();
 }
 
-// Sums of few terms: probabilities and dS rounded to bf16 would be most of the error of dk and dv (2.4e-3 and more, against 1.66e-3 by
-// the rounding of the results themselves, which is what two parts leave).  Longer sums stay at 2.35e-3.  Gradient of 16 heads in bf16, us,
-// one part / two: 1 row over 10992 keys 55 / 59, 64 over 2000 24.8 / 25.7; 128 over 10992 71 / 80; 512 over 10992 137 / 163.
+// Few rows: probabilities and dS rounded to bf16 would be most of the error of dk and dv, whose sums have few terms, and now and then of
+// dq, where a few dS count (2.4e-3 to 2.9e-3, against 1.66e-3 by the rounding of the results themselves, which is what two parts leave).
+// With many rows 2.35e-3 and 2.2e-3.  Gradient of 16 heads in bf16, us, one part / two: 1 row over 10992 keys 55 / 61, 64 over 2000 24.8 /
+// 26.3; dk and dv alone: 128 over 10992 71 / 80, 512 over 10992 137 / 163.
 constexpr int kFewItems = kUnitRows;
 template <typename T> hipError_t launch_grad_t(const CrossArgs &a, bool of_keys, hipStream_t stream)
 {
     const int64_t n = xcd_padded(a.tiles * a.n_split * a.kv_heads);
     if (!grid_ok(n)) return hipErrorInvalidValue;
     const size_t lds = UnitPairs<T>::kStages * (UnitPairs<T>::kStage * sizeof(bf16_t) + (of_keys ? 128 * sizeof(float) : 0));
-    auto kernel = of_keys ? &grad_kv_kernel<T, UnitPairs<T>::kParts> : &grad_q_kernel<T>;
+    auto kernel = of_keys ? &grad_kv_kernel<T, UnitPairs<T>::kParts> : &grad_q_kernel<T, UnitPairs<T>::kParts>;
     if constexpr (sizeof(T) == 2)
-        if (of_keys && a.n_q * a.per_row <= kFewItems * a.q_spans.batch) kernel = &grad_kv_kernel<T, 2>;
+        if (a.n_q * a.per_row <= kFewItems * a.q_spans.batch) kernel = of_keys ? &grad_kv_kernel<T, 2> : &grad_q_kernel<T, 2>;
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(n)), dim3(256), lds, stream, a);
     return hipGetLastError();
 }

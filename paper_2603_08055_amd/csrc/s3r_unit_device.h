@@ -702,8 +702,8 @@ template <int PQ> struct FewRows {
             split_held<PQ>(x, q[s]);
         }
     }
-    // key(t, s, parts): the A operand of key tile t, its PS parts; v: PS planes in LDS
-    template <int PS, typename Key>
+    // key(t, s, parts): the A operand of key tile t, its PS parts; v: PS planes in LDS; PP: parts in which probabilities enter the product
+    template <int PS, int PP, typename Key>
     __device__ __forceinline__ void unit(Key &&key, const bf16_t *v, unsigned long long seen, float factor, int lane)
     {
         floatx4 s[4];
@@ -748,15 +748,15 @@ template <int PQ> struct FewRows {
                 x[j] = fast_exp2(fmaf(s[2 * ks + (j >> 2)][j & 3], factor, -base));
                 unit_sum += x[j];
             }
-            bf16x8 p[PQ];
-            split_parts<PQ>(x, p);
+            bf16x8 p[PP];
+            split_parts<PP>(x, p);
 #pragma unroll
             for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
                 for (int a = 0; a < PS; ++a) {
                     const bf16x8 vt = few_channels(v + a * kPlane, ks, ct, lane);
 #pragma unroll
-                    for (int b = 0; b < PQ; ++b)
+                    for (int b = 0; b < PP; ++b)
                         if (a + b < 3) o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, p[b], o[ct], 0, 0, 0);
                 }
         }
