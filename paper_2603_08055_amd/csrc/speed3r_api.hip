@@ -1062,6 +1062,7 @@ int pieces_few(int64_t workgroups, int64_t units, const FewPace &pace)
     double shortest = static_cast<double>((workgroups + 255) / 256) * (static_cast<double>(units) / pace.waves + pace.start) * pace.whole_us;
     auto look = [&](int64_t s) {
         if (s > units / 4) s = units / 4;
+        if (s > s3r::kMostSplits) s = s3r::kMostSplits;
         if (s < 2) return;
         const int64_t all = workgroups * s, n = (all + 255) / 256, rest = n % pace.resident, rounds = ((units + s - 1) / s + 3) / 4;
         const double share = static_cast<double>(n) + (rest == 0 ? 0.0 : 0.5 - 0.5 * static_cast<double>(rest - 1) / pace.resident);

@@ -165,6 +165,19 @@ def test_cache_workspace_serves_causal_rows_and_others(s3r, rows, batch, dtype):
     assert need[0] == need[1] < 1 << 40
 
 
+@pytest.mark.parametrize("rows", [1, 16, 200])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_pieces_of_very_long_sequences_are_as_many_as_can_be_joined(s3r, rows, dtype):
+    most = 256 * rows * 65 * 4 + 2 * 256                                     # partial results and log-sums of 256 pieces
+    for heads in (1, 2, 3, 7):
+        for pages in (10_000, 100_000, 1_000_000, 16_000_000):
+            p = cache(s3r, n_rows=rows, max_pages=pages, page=128, n_pages=1 << 20, heads=heads, kv_heads=heads, dtype=dtype)
+            assert 0 < s3r.load().speed3r_cache_workspace_bytes(ctypes.byref(p)) <= most * heads
+        for keys in (1_000_000, 30_000_000):
+            p = cross(s3r, n_q=rows, n_kv=keys, heads=heads, kv_heads=heads, batch=1, dtype=dtype)
+            assert 0 < s3r.load().speed3r_cross_workspace_bytes(ctypes.byref(p), 0) <= most * heads
+
+
 @pytest.mark.parametrize("n_q,n_kv", [(0, 0), (0, 5000), (5000, 0), (1, 1), (1 << 20, 1 << 20)])
 @pytest.mark.parametrize("batch", [1, 7])
 @pytest.mark.parametrize("dtype", [0, 1])

@@ -570,6 +570,20 @@ def test_offsets_past_32_bits(s3r):
     assert int(cache.k_codes[: n_pages - 12].max()) == 0
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows", [1, 20, 100])
+def test_millions_of_tokens(s3r, dtype, rows):
+    """A sequence that is divided into as many pieces as can be joined."""
+    g = gen(53)
+    page, length = 128, 1_500_000
+    n_pages = (length + page - 1) // page
+    cache, pt = filled_cache(s3r, g, n_pages, 1, page), torch.randperm(n_pages, generator=g, device="cuda").to(torch.int32)[None].contiguous()
+    q = normal(g, rows, 1, 64, dtype=dtype)
+    compare(run_attend(s3r, cache, q, pt, [length], [rows], True), attend_reference(cache, q, pt, [length], [rows], True))
+    k, v = normal(g, 400_000, 1, 64, dtype=dtype), normal(g, 400_000, 1, 64, dtype=dtype)
+    compare(run_cross(s3r, q, k, v), cross_reference(q, k, v, [(0, rows, 0, 400_000)], None, SCALE))
+
+
 def test_more_than_2_to_the_31_elements(s3r):
     """Rows whose offset in q, out and the gradients passes 32 bits, in elements and in bytes: the last ones, and a whole head."""
     g = gen(52)
