@@ -333,7 +333,7 @@ typedef struct s3r_cache_params {
     void *stream;
 } s3r_cache_params;
 
-/* Keys and values of the rows go to the cache, k rotated; q rotated goes to out.  One launch.  Two rows of a call must not be the
+/* Keys and values of the rows go to the cache, k rotated; q rotated goes to out, which must not be q, k or v.  One launch.  Two rows of a call must not be the
  * same token of the same page (which of them is kept is not specified). */
 s3r_status speed3r_cache_append(const s3r_cache_params *p);
 /* The rows' tokens as values: what the cache holds for them, exactly (to k and v). */

@@ -1397,7 +1397,8 @@ s3r_status speed3r_cache_append(const s3r_cache_params *p)
     if ((p->cos != nullptr) != (p->sin != nullptr)) return fail(S3R_ERR_INVALID_ARG, "cos and sin must be given together");
     if (p->n_rows > 0 && (p->q != nullptr) != (p->out != nullptr)) return fail(S3R_ERR_INVALID_ARG, "q and out must be given together");
     if (p->q && !p->cos) return fail(S3R_ERR_INVALID_ARG, "q is given to be rotated: cos and sin are needed");
-    if (p->q && p->q == p->out) return fail(S3R_ERR_INVALID_ARG, "out must not alias an input");
+    // (waves have rows' queries, keys and values apart: one may write over what another is still to read)
+    if (p->q && (p->out == p->q || p->out == p->k || p->out == p->v)) return fail(S3R_ERR_INVALID_ARG, "out must not alias an input");
     if (p->cos) {
         if (p->rot_axes != 1 && p->rot_axes != 2) return fail(S3R_ERR_INVALID_ARG, "rot_axes (%d) must be 1 or 2", p->rot_axes);
         if (p->rot_axes == 2 && !p->positions) return fail(S3R_ERR_INVALID_ARG, "two axes need positions");

@@ -137,6 +137,14 @@ def test_cache_refusals_of_one_call(s3r, fn, change, status, word):
     assert getattr(s3r.load(), "speed3r_cache_" + fn)(ctypes.byref(p)) == status and word in s3r.speed3r_last_error()
 
 
+@pytest.mark.parametrize("where", ["q", "k", "v"])
+def test_rotated_queries_do_not_go_where_an_input_is(s3r, where):
+    """Waves that have a row's keys or values may still be about to read what another, with its queries, would write over."""
+    p = cache(s3r, heads=2, kv_heads=2)                                       # rows of q, k and v alike, so that the shapes fit
+    p.out = getattr(p, where)
+    assert s3r.load().speed3r_cache_append(ctypes.byref(p)) == INVALID and "alias" in s3r.speed3r_last_error()
+
+
 def test_workspaces(s3r):
     q, kv = torch.empty((1, 16, 64), dtype=torch.bfloat16, device="meta"), torch.empty((100000, 16, 64), dtype=torch.bfloat16, device="meta")
     assert s3r.speed3r_cross_workspace_bytes(q, kv) > 0                               # one row over many keys: split along them
