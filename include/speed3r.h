@@ -259,7 +259,9 @@ s3r_status speed3r_select_attn(const void *q, const void *k, const void *v, cons
  *   Limits: 65536 sequences, batch * kv_heads 2^19, rows * heads 2^28 (the cache calls: rows * (heads + 2 kv_heads)).
  *   Sums, maxima and log-sums are fp32.  bf16 data: probabilities (and dS, in the gradient) enter the second product rounded to
  *   bf16; in the gradient of up to 64 rows (of all heads that share one) in two bf16 parts.  fp32 data: products in bf16 parts, to fp32
- *   precision (an infinity in v or d_out may come out as NaN).
+ *   precision.
+ *   Infinities: bf16 v and d_out: one in v reaches out, and one in d_out reaches dv, as an infinity, where its weight is above 2^-100; dq
+ *   and dk are then infinities or NaN.  fp32 v and d_out: it may come out as NaN.
  *   The gradient takes out and lse as the forward call left them; the gradients of shared heads are summed.  Its results do not
  *   depend on the order in which workgroups run. */
 typedef struct s3r_cross_params {

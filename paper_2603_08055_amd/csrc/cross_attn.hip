@@ -61,7 +61,7 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) 
 }
 
 // Probabilities of few bf16 rows enter in two parts, which the memory that binds hides (16 rows over 10992 keys of 16 heads 15.4 us with one,
-// 15.6 with two): the error of out is the rounding of its store, also where few keys count (rows over 17 keys, up to 2.4e-3 with one).
+// 16.0 with two): the error of out is the rounding of its store, also where few keys count (rows over 17 keys, up to 2.4e-3 with one).
 template <typename T> constexpr int kFewParts = sizeof(T) == 4 ? 3 : 2;
 
 // Few rows: WAVES waves with the same 16 rows take the units in turn, values through an LDS stage of their own (8 or 24 KiB).

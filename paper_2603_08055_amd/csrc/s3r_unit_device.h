@@ -104,14 +104,19 @@ __device__ __forceinline__ float upper_part(float x)
     return __uint_as_float((__float_as_uint(x) & 0xffff0000u) | (x != x ? 0x00400000u : 0u));
 }
 
-// x = p[0] + p[1] + p[2] (parts 3), or p[0] = x rounded to bf16 (parts 1), p[1] what is left, rounded (parts 2).
+// x = p[0] + p[1] + p[2] (parts 3), p[0] = x rounded to bf16 (parts 1), or p[0] = x cut to bf16 and p[1] what is left, rounded (parts 2: off by
+// 2^-16 of x at most).  Of two parts both have the sign of x, and neither is 0 unless x is (2^-24 of x goes to the second): their products
+// with an infinity are that of x, where a part of 0 or of the other sign would make NaN of it.
 template <int PARTS> __device__ __forceinline__ void split_parts(const float (&x)[8], bf16x8 (&p)[PARTS])
 {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        if constexpr (PARTS <= 2) {
+        if constexpr (PARTS == 1) {
             p[0][j] = static_cast<bf16_t>(x[j]);
-            if constexpr (PARTS == 2) p[1][j] = static_cast<bf16_t>(x[j] - static_cast<float>(p[0][j]));
+        } else if constexpr (PARTS == 2) {
+            const float h = __uint_as_float(__float_as_uint(x[j]) & 0xffff0000u);  // (of a NaN: p[1] is one)
+            p[0][j] = __builtin_bit_cast(bf16_t, static_cast<unsigned short>(__float_as_uint(x[j]) >> 16));
+            p[1][j] = static_cast<bf16_t>(fmaf(x[j], 0x1p-24f, x[j] - h));
         } else {
             const float h = upper_part(x[j]), rest = __builtin_isfinite(x[j]) ? x[j] - h : 0.f;
             const float m = __uint_as_float(__float_as_uint(rest) & 0xffff0000u), l = rest - m;
