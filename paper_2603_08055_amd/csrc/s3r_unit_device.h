@@ -637,13 +637,17 @@ __device__ __forceinline__ void store_no_keys(const SoftOut &to, int split, int6
     if (ok) to.part_lse[split * to.rows * to.heads + row * to.heads + head] = -INFINITY;
 }
 
+// A row without a weight above 0 is 0, also where its product with v is not: 0 times an infinity or NaN.
 template <typename T, int PQ>
-__device__ __forceinline__ void store_soft(const SoftRow<PQ> &soft, float factor, const SoftOut &to, int split, int64_t row,
+__device__ __forceinline__ void store_soft(SoftRow<PQ> &soft, float factor, const SoftOut &to, int split, int64_t row,
                                            int head, bool ok, int lane)
 {
     float total, l2;
     soft.totals(factor, total, l2);
     const float w = total == 0.f ? 0.f : 1.f / total;
+    if (total == 0.f)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) soft.o[0][r] = soft.o[1][r] = 0.f;
     const int64_t at = row * to.heads + head;
     if (to.part_o != nullptr) {
         const int64_t part = split * to.rows * to.heads + at;
@@ -799,8 +803,9 @@ __device__ __forceinline__ void store_few(const FewRows<PQ> &few, float factor, 
         for (int r = 0; r < 4; ++r) o[r] += lds[j * kFewJoin + (wave * 4 + r) * 64 + lane] * w;
     }
     if (!ok) return;
-    const float inv = sum == 0.f ? 0.f : 1.f / sum, l2 = sum == 0.f ? -INFINITY : fmaf(top, factor, log2f(sum));
-    o *= inv;
+    const float inv = 1.f / sum, l2 = sum == 0.f ? -INFINITY : fmaf(top, factor, log2f(sum));
+#pragma unroll
+    for (int r = 0; r < 4; ++r) o[r] = sum == 0.f ? 0.f : o[r] * inv;  // (see store_soft)
     const int64_t at = row * to.heads + head, part = split * to.rows * to.heads + at;
     const int c = 16 * wave + 4 * (lane >> 4);
     if (to.part_o != nullptr) {
