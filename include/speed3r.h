@@ -258,8 +258,10 @@ s3r_status speed3r_select_attn(const void *q, const void *k, const void *v, cons
  *   A query row without any key, or whose scores are all -inf, gets out = 0 and lse = -inf; without any key its gradient is 0.
  *   Limits: 65536 sequences, batch * kv_heads 2^19, rows * heads 2^28 (the cache calls: rows * (heads + 2 kv_heads)).
  *   Sums, maxima and log-sums are fp32.  bf16 data: probabilities (and dS, in the gradient) enter the second product rounded to
- *   bf16; in the gradient of up to 64 rows (of all heads that share one) in two bf16 parts.  fp32 data: products in bf16 parts, to fp32
- *   precision.
+ *   bf16 (errors of the results up to about 1.4 times that of rounding them); those of few rows in two bf16 parts (errors of the rounding
+ *   alone): in the forward call of up to 64 (keys and values of up to 16 MiB together), 32 (48 MiB) or 16 rows, in the gradient of up to 64,
+ *   counting those of all heads that share one, on average over the batch.  A sequence's last bits thus depend on the lengths in its batch.
+ *   fp32 data: products in bf16 parts, each off by up to 2^-21 of its magnitude.
  *   Infinities: bf16 v and d_out: one in v reaches out, and one in d_out reaches dv, as an infinity, where its weight is above 2^-100; dq
  *   and dk are then infinities or NaN.  fp32 v and d_out: it may come out as NaN.
  *   The gradient takes out and lse as the forward call left them; the gradients of shared heads are summed.  Its results do not
