@@ -261,7 +261,7 @@ s3r_status speed3r_select_attn(const void *q, const void *k, const void *v, cons
  *   bf16 (errors of the results up to about 1.4 times that of rounding them); those of few rows in two bf16 parts (errors of the rounding
  *   alone): in the forward call of up to 64 (keys and values of up to 16 MiB together), 32 (48 MiB) or 16 rows, in the gradient of up to 64,
  *   counting those of all heads that share one, on average over the batch.  A sequence's last bits thus depend on the lengths in its batch.
- *   fp32 data: products in bf16 parts, each off by up to 2^-21 of its magnitude.
+ *   fp32 data: products in bf16 parts, each off by up to 2^-21 of its magnitude (operands below 2^-102 keep fewer bits).
  *   Infinities: bf16 v and d_out: one in v reaches out, and one in d_out reaches dv, as an infinity, where its weight is above 2^-100; dq
  *   and dk are then infinities or NaN.  fp32 v and d_out: it may come out as NaN.
  *   The gradient takes out and lse as the forward call left them; the gradients of shared heads are summed.  Its results do not

@@ -129,7 +129,8 @@ template <int PARTS> __device__ __forceinline__ void split_parts(const float (&x
 }
 
 // The same for held rows.  A lower part of 0 would make NaN of an infinite key, whose score is -inf and counts for nothing: the
-// smallest normal number with the sign of x stands in, below every product's rounding.
+// smallest normal number with the sign of x stands in, for x of 2^-102 and more below every product's rounding.  (Rows of 2^-108 over keys
+// of 2^108: out off by 1.2e-5, at 2^-100 by 2e-7 as ever.)
 template <int PARTS> __device__ __forceinline__ void split_held(const float (&x)[8], bf16x8 (&p)[PARTS])
 {
     split_parts<PARTS>(x, p);
