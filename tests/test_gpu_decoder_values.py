@@ -1,12 +1,13 @@
 """GPU tests of cross attention, its gradient and the 4-bit cache on values that are rare or that tell a mistake: infinities that count, scores
-that are all -inf."""
+that are all -inf, rotated rows next to a border of their rounding."""
 import math
 
 import pytest
 import torch
 
-from tests.decoder_util import check, cross_reference
-from tests.test_gpu_decoder import BF16, F32, SCALE, compare, gen, normal, run_cross, s3r  # noqa: F401 (s3r: the fixture)
+from tests.decoder_once import next_to_ties, to_bf16_once
+from tests.decoder_util import check, cross_reference, four_bits, packed, rotated
+from tests.test_gpu_decoder import BF16, F32, SCALE, compare, gen, new_cache, normal, run_cross, s3r, tables_of_angles  # noqa: F401 (s3r: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +53,49 @@ def test_rows_whose_scores_are_all_minus_infinity_whatever_the_values(s3r, dtype
     assert bool((got["out"][:, 1] == 0).all()) and bool((got["lse"][1] == -math.inf).all())
     want = cross_reference(q[:, :1], k[:, :1], v[:, :1], [(0, rows, 0, m)], None, SCALE)
     compare({"out": got["out"][:, :1], "lse": got["lse"][:1]}, want)
+
+
+def append_one_sequence(s3r, k, v, page, **kw):  # noqa: F811
+    """The rows as a sequence of their own; codes and exponents of the keys, row by row."""
+    n, heads = k.shape[:2]
+    width = (n + page - 1) // page
+    cache, pt = new_cache(s3r, width, heads, page), torch.arange(width, dtype=torch.int32, device="cuda")[None]
+    s3r.speed3r_cache_append(cache, k, v, pt, torch.tensor([n], dtype=torch.int32, device="cuda"), **kw)
+    return tuple(t.permute(0, 2, 1, 3).reshape(width * page, heads, -1)[:n] for t in (cache.k_codes, cache.k_scales))
+
+
+@pytest.mark.parametrize("axes", [1, 2])
+@pytest.mark.parametrize("pairs", ["halves", "neighbours"])
+@pytest.mark.parametrize("n,heads,kv_heads", [(1, 1, 1), (777, 6, 2)])
+def test_rotated_bf16_queries_are_rounded_once(s3r, n, heads, kv_heads, axes, pairs):  # noqa: F811
+    """Bit by bit: random rows, and powers of two whose exact results lie next to the middle of two bf16 numbers, nearer than fp32 can tell."""
+    g = gen(n + axes)
+    at = torch.arange(n, device="cuda")[:, None].expand(n, axes)
+    kw = {"positions": at.int().contiguous(), "pairs": pairs}
+    tied, cos_t, sin_t = next_to_ties(n, heads, axes, g, "cuda")
+    for q, (cos, sin) in ((normal(g, n, heads, 64, dtype=BF16), tables_of_angles(n, 32 // axes)), (tied, (cos_t, sin_t))):
+        k, out = normal(g, n, kv_heads, 64, dtype=BF16), torch.full_like(q, math.nan)
+        append_one_sequence(s3r, k, k, 32, q=q, q_out=out, cos=cos, sin=sin, **kw)
+        assert torch.equal(out, to_bf16_once(rotated(q.double(), at, cos, sin, pairs == "neighbours")))
+
+
+@pytest.mark.parametrize("axes", [1, 2])
+@pytest.mark.parametrize("pairs", ["halves", "neighbours"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_codes_next_to_a_border_in_every_order_of_pairs(s3r, dtype, axes, pairs):  # noqa: F811
+    """Channels at a tie of the 4-bit form or at a change of exponent, turned by cosines of 1 and sines of 2^-30 to 2^-45 (the
+    exact value is off the border by less than fp32 can tell), and fp32 rows that a turn brings next to one."""
+    n = 1000
+    g = gen(23)
+    at = torch.arange(n, device="cuda")[:, None].expand(n, axes)
+    border = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0], device="cuda")
+    want = border[torch.randint(0, 8, (n, 2, 64), generator=g, device="cuda")] * torch.where(torch.rand((n, 2, 64), generator=g, device="cuda") < 0.5, -1, 1)
+    _, _, sin = next_to_ties(n, 1, axes, g, "cuda")
+    cases = [(want.to(dtype), torch.ones_like(sin), sin)]
+    if dtype == F32:
+        cos, sin = tables_of_angles(n, 32 // axes)
+        cases.append((rotated(want.double(), at, cos, -sin, pairs == "neighbours").float(), cos, sin))
+    for k, cos, sin in cases:
+        codes, scales = append_one_sequence(s3r, k, k, 64, cos=cos, sin=sin, positions=at.int().contiguous(), pairs=pairs)
+        code, scale = four_bits(rotated(k.double(), at, cos, sin, pairs == "neighbours"))
+        assert torch.equal(codes, packed(code)) and torch.equal(scales, scale)
