@@ -37,7 +37,8 @@ template <int BIT> __device__ __forceinline__ unsigned other_lane(unsigned x)
 // channels, and a run of heads: what a row needs (its sequence, its place, the angles) is found once for them, and the 32 bytes of
 // codes of neighbouring tokens, which lie side by side in a page, are written together.  The products of the rotation are exact in 64
 // bits and their sum is rounded once, so that the codes are those of the exact values.
-// 100 views of 1374 tokens, 16 heads: append 172 us, without rotation 145, read 148; a plain copy of as many bytes 133.  The rotation is
+// 100 views of 1374 tokens, 16 heads: append 166 us, without rotation 135, read 138; a plain copy of as many bytes 140 (each on end; append and
+// read in turn 180 and 124).  The rotation is
 // what memory does not hide: 101 registers, four waves on a SIMD; held to 96 they spill (200 us).
 
 // The rows of a wave and its heads: `octets` of rows, and for each heads h0 .. h1 - 1 of `heads`, `run` at a time.

@@ -196,11 +196,11 @@ template <typename T, int GROUPS> __global__ __launch_bounds__(256) void soft_co
 // ---- gradient --------------------------------------------------------------------------------------------
 
 // D from the stored out: in bf16 it is off by the rounding of out, the same amount for all keys of a row, and that would be most of the
-// error of dq and dk (three times all other roundings together at 2748 rows over 10992 keys).  The dS of a row add up to 0 over all
-// keys: what they do add up to in fp32 is what D lacks, and goes into D for the gradient of keys.  What they add up to as they enter
-// the product, rounded, has the roundings in it as well; the query gradient takes that out of its own result, dS k - sum(dS) * P k.
-// One product more of eight.  Against 64 bits, dq of 2748 rows over 10992 keys: 5.1e-3 without, 3.1e-3 with the former sum, 2.3e-3 with
-// the latter; dk of short sequences with the latter in D 2.7e-3.  The former takes 10 % of the kernel (563 -> 624 us, 8192 rows and keys).
+// error of dq and dk.  The dS of a row add up to 0 over all keys: what they do add up to in fp32 is what D lacks, and goes into D for the
+// gradient of keys.  What they add up to as they enter the product, rounded, has the roundings in it as well; the query gradient takes that
+// out of its own result, dS k - sum(dS) * P k.  One product more of four.  Against 64 bits, 2748 rows over 10992 keys of which a few channels
+// are large: dq 4.0e-3 without, 2.2e-3 so, dk 2.7e-3 and 2.3e-3; 300 normal rows over 700 keys dq 2.8e-3 and 2.2e-3, dk 2.5e-3 and 2.3e-3.  The
+// kernel of 2748 rows, 16 heads: 208 us without, 281 so.
 template <typename T> constexpr bool kMendD = sizeof(T) == 2;
 
 __device__ __forceinline__ float sum8(const bf16x8 &x)
