@@ -39,17 +39,19 @@ def plant(q, k, v, heads_of):
     return at
 
 
-def planted_reference(q, k, v, scale, dtype, pieces, left_out=None):
+def planted_reference(q, k, v, scale, dtype, pieces, left_out=None, seen=None):
     """One head in 64 bits, and its bounds: the score's error d (64 products, for fp32 in parts 400 u of their magnitudes; the exponential's
     argument; twice, for the row's maximum and sum), h for a probability rounded to bf16, h |out| for the store.  Sums: a wave adds the
     keys of its piece one after the other, m / pieces of them, 16 waves are joined and 256 pieces: that many roundings, no more.
-    left_out: tokens that a mistake leaves out."""
+    left_out: tokens that a mistake leaves out; seen [n, m]: what each row sees, None: all."""
     q, k, v = q.double(), k.double(), v.double()
     m, f32 = k.shape[0], dtype == torch.float32
     h = half_step(dtype)
     s = (q @ k.t()) * scale
     if left_out is not None:
         s[:, left_out] = -math.inf
+    if seen is not None:
+        s = s.masked_fill(~seen, -math.inf)
     size = float(((q.abs() @ k.abs().t()) * scale).max())
     d = 2 * ((400 if f32 else 64) * U * size + (size + 4) * U)
     chain = (math.ceil(m / pieces / UNIT) * UNIT + 16 + 256) * U

@@ -4,7 +4,7 @@ import torch
 
 from tests.decoder_util import attention, check
 from tests.pieces_util import UNIT, plant, planted_reference
-from tests.test_gpu_decoder import BF16, F32, SCALE, cached, gen, normal, run_attend, run_cross, s3r  # noqa: F401 (s3r: the fixture)
+from tests.test_gpu_decoder import BF16, F32, SCALE, cached, gen, normal, run_attend, run_cross, s3r, starts, table  # noqa: F401 (s3r: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -81,3 +81,51 @@ def test_every_piece_of_a_gradient_counts(s3r, dtype, n, m, heads, kv_heads):  #
                 sums[name] = sums[name] + want[name]
         for name in ("dk", "dv"):
             check(name, got[name][:, kv], sums[name], sums[name + "_tol"])
+
+
+RAGGED = {"few rows": ([3, 1, 2, 5], [9000, 65, 1, 30_000]), "many rows": ([300, 40, 1, 129], [9000, 700, 20_000, 64]),
+          "single rows, one long": ([1] * 20, [500] * 19 + [40_000])}
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("which", list(RAGGED))
+def test_every_piece_of_ragged_keys_counts(s3r, dtype, which):  # noqa: F811
+    rows, keys = RAGGED[which]
+    g = gen(len(rows))
+    q, k, v = (normal(g, r, h, 64, dtype=dtype) for r, h in ((sum(rows), 4), (sum(keys), 2), (sum(keys), 2)))
+    at = [(sum(rows[:b]), n, sum(keys[:b]), m) for b, (n, m) in enumerate(zip(rows, keys))]
+    for q0, n, k0, m in at:
+        plant(q[q0:q0 + n], k[k0:k0 + m], v[k0:k0 + m], 2)
+    got = run_cross(s3r, q, k, v, q_start=starts(rows), kv_start=starts(keys))
+    for q0, n, k0, m in at:
+        for h in range(4):
+            want = planted_reference(q[q0:q0 + n, h], k[k0:k0 + m, h // 2], v[k0:k0 + m, h // 2], SCALE, dtype, 1)
+            for name, x in (("out", got["out"][q0:q0 + n, h]), ("lse", got["lse"][h, q0:q0 + n])):
+                check(name, x, want[name], want[name + "_tol"])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("which", list(RAGGED))
+@pytest.mark.parametrize("page", [16, 128])
+def test_every_piece_of_a_ragged_cache_counts(s3r, dtype, causal, which, page):  # noqa: F811
+    rows, keys = RAGGED[which]
+    keys = [max(n, m) for n, m in zip(rows, keys)]
+    g = gen(len(rows) + page)
+    q, k, v = (normal(g, r, h, 64, dtype=BF16) for r, h in ((sum(rows), 4), (sum(keys), 2), (sum(keys), 2)))
+    at = [(sum(rows[:b]), n, sum(keys[:b]), m) for b, (n, m) in enumerate(zip(rows, keys))]
+    for q0, n, k0, m in at:
+        plant(q[q0:q0 + n], k[k0:k0 + m], v[k0:k0 + m], 2)
+    width = max((m + page - 1) // page for m in keys)
+    cache, pt = s3r.PagedCache.empty(width * len(keys), 2, page), table(g, len(keys), width, width * len(keys))
+    s3r.speed3r_cache_append(cache, k, v, pt, torch.tensor(keys, dtype=torch.int32, device="cuda"), starts(keys))
+    q = q.to(dtype)
+    got = run_attend(s3r, cache, q, pt, keys, rows, causal)
+    for b, (q0, n, k0, m) in enumerate(at):
+        last = torch.arange(m - n, m, device="cuda") if causal else torch.full((n,), m - 1, device="cuda")
+        seen = torch.arange(m, device="cuda")[None] <= last[:, None]
+        for h in range(4):
+            kc, vc = cached(cache, pt, b, m, h // 2)
+            want = planted_reference(q[q0:q0 + n, h], kc, vc, SCALE, dtype, 1, seen=seen)
+            for name, x in (("out", got["out"][q0:q0 + n, h]), ("lse", got["lse"][h, q0:q0 + n])):
+                check(name, x, want[name], want[name + "_tol"])
