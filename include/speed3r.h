@@ -65,7 +65,8 @@ typedef enum { S3R_F32 = 0, S3R_BF16 = 1 } s3r_dtype;
 enum { S3R_DIAG_FORCED_RANGE = 1, S3R_DIAG_FORCED_ORDER = 2 };
 /* Bits of the status word of the cache and cross attention calls: a page number outside [0, n_pages); a list of row
  * starts that is out of range or not ascending; a length outside the page table (for append and read also one below the
- * sequence's rows); a position outside the tables. */
+ * sequence's rows); a position outside the tables.  Asking for it is one more launch, which takes the cache calls half a microsecond for each
+ * sequence. */
 enum { S3R_DIAG_PAGE = 4, S3R_DIAG_SPANS = 8, S3R_DIAG_LENGTH = 16, S3R_DIAG_POSITION = 32 };
 
 /* Stages of the path, for speed3r_get_stage_ms(). */
