@@ -534,7 +534,7 @@ template <typename T> hipError_t launch_cross_t(const CrossArgs &a, bool few_row
 
 // Few rows: probabilities and dS rounded to bf16 would be most of the error of dk and dv, whose sums have few terms, and now and then of
 // dq, where a few dS count (2.4e-3 to 2.9e-3, against 1.66e-3 by the rounding of the results themselves, which is what two parts leave).
-// With many rows the errors are 2.35e-3 and 2.3e-3 and the matrix pipe binds.  Gradient of 16 heads in bf16, us, one part / two: 1 row over 10992
+// With many rows the errors are 2.35e-3 and 2.3e-3 and no memory hides the products.  Gradient of 16 heads in bf16, us, one part / two: 1 row over 10992
 // keys 55 / 60, 64 over 2000 24.8 / 26.6, 2748 over 10992 588 / 795, 8192 over 8192 1129 / 1554; dk and dv alone: 128 over 10992 71 / 80, 512 over
 // 10992 137 / 163.
 constexpr int kFewItems = kUnitRows;
