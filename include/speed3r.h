@@ -350,6 +350,96 @@ s3r_status speed3r_cache_attn(const s3r_cache_params *p);
 /* Bytes of device scratch of speed3r_cache_attn; only the shape fields are read.  May be 0; SIZE_MAX on invalid arguments. */
 size_t speed3r_cache_workspace_bytes(const s3r_cache_params *p);
 
+/* ---- rotary positions with the norm of a head ------------------------------------------------- */
+
+typedef enum { S3R_NORM_NONE = 0, S3R_NORM_RMS = 1, S3R_NORM_LAYER = 2 } s3r_norm;
+typedef enum { S3R_PAIRS_HALVES = 0, S3R_PAIRS_NEIGHBOURS = 1, S3R_PAIRS_WHOLE = 2 } s3r_pairs;
+
+/* What q and k go through before any of the attentions: every head's 64 channels are normed (or not), n = norm(x) weight + bias, and
+ * pairs of channels turned by the angles of the row's positions, one for each axis (time or view, row, column):
+ *   out_a = n_a cos - n_b sin,  out_b = n_b cos + n_a sin.
+ *   Axes: axis x has axis_pairs[x] pairs, P = their sum <= 32; pair p of all (those of axis 0 first) takes
+ *   cos[position of its axis][p].  Channels that are in no pair are not turned.
+ *   Pairs: S3R_PAIRS_HALVES: the channels of an axis are a group of 2 axis_pairs[x], of which i and i + axis_pairs[x] are a pair;
+ *   S3R_PAIRS_NEIGHBOURS: channels 2 p and 2 p + 1;  S3R_PAIRS_WHOLE: channels p and P + p.
+ *   Norm: over a head's channels, S3R_NORM_LAYER (x - mean) / sqrt(variance + eps) or S3R_NORM_RMS x / sqrt(mean of squares + eps), for
+ *   magnitudes up to 2^56; everything is computed in fp32 and rounded once.
+ * Either of q and k may be absent (heads or kv_heads 0); heads need not be a multiple of kv_heads.
+ * The gradient takes those of q_out and k_out and, with a norm, q and k again.  The gradients of weights are sums over all rows and heads, in
+ * an order that does not depend on that of the workgroups.  Without a norm q, k, and weights are not read. */
+typedef struct s3r_rotary_params {
+    const void *q, *k;            /* in  [n_rows][heads][64], [n_rows][kv_heads][64] (or *_stride_*)     */
+    void *q_out, *k_out;          /* out, packed; must not alias inputs                                  */
+    const void *d_q_out, *d_k_out; /* gradient: in, packed                                               */
+    void *dq, *dk;                /* gradient: out (or d*_stride_*: parts of one gradient of a projection) */
+    const void *q_weight, *q_bias, *k_weight, *k_bias;     /* in, optional [64] of weight_dtype (1 and 0) */
+    void *dq_weight, *dq_bias, *dk_weight, *dk_bias;       /* gradient: out, optional, of weight_dtype    */
+    const float *cos, *sin;       /* [n_positions][P], 16-byte aligned; NULL with axes 0: no rotation    */
+    const int32_t *positions;     /* [n_rows][axes]; NULL (axes 1): the row's number.  Held into [0, n_positions) */
+    int32_t *status;              /* out, optional: one device word, 0 or S3R_DIAG_POSITION              */
+    int64_t n_rows, n_positions;  /* n_rows may be 0; rows * (heads + kv_heads) at most 2^28             */
+    int64_t q_stride_tok, q_stride_head, k_stride_tok, k_stride_head;     /* elements, 0: packed; multiples of 8 */
+    int64_t dq_stride_tok, dq_stride_head, dk_stride_tok, dk_stride_head;
+    int heads, kv_heads, head_dim;
+    s3r_dtype dtype, weight_dtype;
+    int axes;                     /* 0 .. 3                                                              */
+    int axis_pairs[3];
+    s3r_pairs pairs;
+    s3r_norm norm;
+    float eps;                    /* with a norm: positive                                               */
+    void *workspace;              /* gradient: caller-owned device scratch, 256-byte aligned             */
+    size_t workspace_bytes;       /* >= speed3r_rotary_workspace_bytes(...)                              */
+    void *stream;
+} s3r_rotary_params;
+
+s3r_status speed3r_rotary(const s3r_rotary_params *p);
+s3r_status speed3r_rotary_backward(const s3r_rotary_params *p);
+/* Bytes of device scratch of the gradient.  May be 0; SIZE_MAX on invalid arguments. */
+size_t speed3r_rotary_workspace_bytes(const s3r_rotary_params *p);
+
+/* ---- the residual stream with the norms around a block ------------------------------------------ */
+
+/* The end of one block and the start of the next:
+ *   r = x + residual_scale * scale * gate * u,  u = post-norm(f) post_weight + post_bias (or f);   y = norm(r) weight + bias
+ * for rows of `width` channels: x is the residual stream, f what the block adds to it, scale a learned factor for each channel, gate one
+ * for each channel of each sequence.  Only x is required: without f, r is x; y, r, and every weight may be absent (NULL).
+ *   Norms: as in s3r_rotary_params, over the `width` channels, for magnitudes up to 2^56.  Everything is computed in fp32 and rounded once:
+ *   y is the norm of r before its rounding.
+ *   Sequences: with gates, those of sequence b are the rows row_start[b] .. row_start[b+1] - 1 (DEVICE memory; broken lists as in
+ *   s3r_cross_params); rows outside all sequences are left as they were, in r, y, dx and df.  row_start NULL: one sequence of all rows.
+ *   Types: the stream (x, r and their gradients) is of x_dtype: dtype, or fp32 with everything else in bf16.  weights, biases and scale
+ *   are of weight_dtype, gates of dtype.
+ * The gradient takes those of y and r (either may be NULL: 0), x and f again, and gives
+ * those of x, f and of every weight that is asked for, sums in an order that does not depend on that of the workgroups. */
+typedef struct s3r_residual_params {
+    const void *x, *f;            /* in  [n_rows][width] (or *_stride)                                   */
+    void *r, *y;                  /* out, packed; r may be x itself where x is packed                    */
+    const void *weight, *bias, *post_weight, *post_bias, *scale;   /* in, optional [width]               */
+    const void *gate;             /* in, optional [batch][width] (or gate_stride)                        */
+    const int32_t *row_start;     /* in, optional [batch + 1]; with gates                                */
+    const void *d_r, *d_y;        /* gradient: in, packed                                                */
+    void *dx, *df;                /* gradient: out, packed; df with f                                    */
+    void *d_weight, *d_bias, *d_post_weight, *d_post_bias, *d_scale; /* gradient: out, optional [width]  */
+    void *d_gate;                 /* gradient: out, optional [batch][width], packed                      */
+    int32_t *status;              /* out, optional: one device word, 0 or S3R_DIAG_SPANS                 */
+    int64_t n_rows;               /* 0 .. 2^28                                                           */
+    int64_t x_stride, f_stride, gate_stride; /* elements between rows, 0: packed; multiples of 8         */
+    int width;                    /* a multiple of 8 up to 8192                                          */
+    int batch;                    /* sequences; 1 (or 0) without row_start; at most 65536                */
+    s3r_dtype x_dtype, dtype, weight_dtype;
+    s3r_norm norm, post_norm;     /* of r (needed for y), and of f                                       */
+    float eps;                    /* with a norm: positive                                               */
+    float residual_scale;         /* finite; 0: 1                                                        */
+    void *workspace;              /* gradient: caller-owned device scratch, 256-byte aligned             */
+    size_t workspace_bytes;       /* >= speed3r_residual_workspace_bytes(...)                            */
+    void *stream;
+} s3r_residual_params;
+
+s3r_status speed3r_residual_norm(const s3r_residual_params *p);
+s3r_status speed3r_residual_norm_backward(const s3r_residual_params *p);
+/* Bytes of device scratch of the gradient (those of weights count where their pointers are given).  May be 0; SIZE_MAX on invalid arguments. */
+size_t speed3r_residual_workspace_bytes(const s3r_residual_params *p);
+
 /* ---- utilities ------------------------------------------------------------------------------ */
 
 /* Measurement of what the data movement of the selection stage (eq. 6 / Alg. 2) costs by itself: the

@@ -361,6 +361,61 @@ hipError_t launch_cache_attn(const CacheArgs &a, bool few_rows, bool is_bf16, hi
 // appends: the rows' tokens have to be in the sequences, and positions in the table.
 hipError_t launch_cache_status(const CacheArgs &a, bool appends, int *status, hipStream_t stream);
 
+// ---- rotary positions, and the residual stream with its norms -----------------------------------------
+
+// S3R_NORM_* and S3R_PAIRS_* of the public header.
+constexpr int kNormNone = 0, kNormRms = 1, kNormLayer = 2;
+constexpr int kPairsHalves = 0, kPairsNeighbours = 1, kPairsWhole = 2;
+
+// q or k: rows [n_rows][heads][64] by element strides.  in: what is rotated (the gradient through a norm: x, and grad that of the result,
+// packed); out: the result.
+struct RotarySide {
+    const void *in, *grad;
+    void *out;
+    int64_t in_row, in_head, out_row, out_head;
+    int heads;  // 0: none
+    const void *weight, *bias;
+    void *d_weight, *d_bias;
+};
+
+// cos, sin [places][n_pairs], or null: no rotation; axis_pairs: pairs of each axis, n_pairs their sum.  sign: -1 turns back.  part:
+// [kRotaryGradGroups][2][64], or null: no gradients of weights.
+constexpr int kRotaryGradGroups = 1024;
+struct RotaryArgs {
+    RotarySide side[2];
+    const float *cos, *sin;
+    const int32_t *positions;
+    int64_t n_rows, places;
+    int axes, n_pairs, axis_pairs[3], pairing, norm;
+    bool w_bf16;
+    float eps, sign;
+    float *part;
+};
+hipError_t launch_rotary(const RotaryArgs &a, bool is_bf16, hipStream_t stream);
+hipError_t launch_rotary_norm_grad(const RotaryArgs &a, bool is_bf16, hipStream_t stream);
+hipError_t launch_rotary_status(const RotaryArgs &a, int *status, hipStream_t stream);
+
+// x_row, f_row, gate_row: elements between rows; all others are packed.  rows_per_block: rows of a workgroup, which follow one another.
+// part: [5][workgroups][width], part_gate: [workgroups + batch - 1][width], or null.
+struct ResidualArgs {
+    const void *x, *f, *gate;
+    int64_t x_row, f_row, gate_row;
+    void *r, *y;
+    const void *weight, *bias, *post_weight, *post_bias, *scale;
+    const void *d_r, *d_y;
+    void *dx, *df, *d_weight, *d_bias, *d_post_weight, *d_post_bias, *d_scale, *d_gate;
+    Spans spans;
+    int64_t n;
+    int width, norm, post, rows_per_block;
+    bool w_bf16;
+    float eps, residual_scale;
+    float *part, *part_gate;
+};
+hipError_t launch_residual(const ResidualArgs &a, bool x_bf16, bool is_bf16, hipStream_t stream);
+hipError_t launch_residual_grad(const ResidualArgs &a, bool x_bf16, bool is_bf16, hipStream_t stream);
+// Rows that a workgroup has at a time.
+inline int residual_rows(int width) { return width <= 128 ? 16 : (width <= 1024 ? 4 : 1); }
+
 // Most tiles that `batch` sequences of n rows together can have, at least 1.  A sequence's items are a multiple of per_row, so that its
 // last tile lacks at most tile - gcd(per_row, tile) of them, and at most n sequences have any.  (64 sequences of a row, four heads
 // of which share keys: 64 tiles of 16 for each head of keys, 6.3 us over short sequences; with 16 more that found nothing to do 7.4.)

@@ -6,7 +6,10 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <initializer_list>
 #include <mutex>
+#include <tuple>
+#include <utility>
 #include <vector>
 
 // Scratch of speed3r_sparse_global_attn_noalloc: device memory that exists from the moment the code object
@@ -1458,6 +1461,303 @@ s3r_status speed3r_cache_attn(const s3r_cache_params *p)
     StageTimer tm(S3R_STAGE_DENSE, s);
     S3R_HIP(s3r::launch_cache_attn(a, c.few_rows, bf16, s), "cache attention kernel launch");
     if (c.split > 1) S3R_HIP(s3r::launch_soft_combine(a.to, a.spans, c.split, bf16, s), "cache attention combine kernel launch");
+    return S3R_OK;
+}
+
+// ---- rotary positions with the norm of a head ------------------------------------------------------------
+namespace {
+
+s3r_status check_eps(float eps)
+{
+    if (!(eps >= 1.17549435e-38f) || !std::isfinite(eps)) return fail(S3R_ERR_INVALID_ARG, "eps (%g) must be positive and finite", static_cast<double>(eps));
+    return S3R_OK;
+}
+
+s3r_status check_norm(const char *what, int norm)
+{
+    if (norm < S3R_NORM_NONE || norm > S3R_NORM_LAYER) return fail(S3R_ERR_INVALID_ARG, "%s (%d) must be one of S3R_NORM_*", what, norm);
+    return S3R_OK;
+}
+
+// Checks of what the shape fields hold.
+s3r_status check_rotary(const s3r_rotary_params *p)
+{
+    if (!p) return fail(S3R_ERR_INVALID_ARG, "params is null");
+    if (p->heads < 0 || p->kv_heads < 0 || p->heads + static_cast<int64_t>(p->kv_heads) == 0)
+        return fail(S3R_ERR_INVALID_ARG, "heads (%d) and kv_heads (%d) must not be negative, nor both 0", p->heads, p->kv_heads);
+    if (p->heads > 65535 || p->kv_heads > 65535) return fail(S3R_ERR_UNSUPPORTED, "heads %d, %d unsupported (max 65535)", p->heads, p->kv_heads);
+    if (p->head_dim != 64) return fail(S3R_ERR_UNSUPPORTED, "head_dim %d unsupported (must be 64)", p->head_dim);
+    if (p->dtype != S3R_F32 && p->dtype != S3R_BF16) return fail(S3R_ERR_UNSUPPORTED, "unknown dtype %d", p->dtype);
+    if (p->weight_dtype != S3R_F32 && p->weight_dtype != S3R_BF16) return fail(S3R_ERR_UNSUPPORTED, "unknown weight_dtype %d", p->weight_dtype);
+    if (p->n_rows < 0) return fail(S3R_ERR_INVALID_ARG, "n_rows must not be negative");
+    if (p->n_rows > kMaxRowHeads / (p->heads + p->kv_heads)) return fail(S3R_ERR_UNSUPPORTED, "rows * heads exceeds 2^28");
+    s3r_status st = check_norm("norm", p->norm);
+    if (st != S3R_OK) return st;
+    if (p->axes < 0 || p->axes > 3) return fail(S3R_ERR_INVALID_ARG, "axes (%d) must be 0 to 3", p->axes);
+    if (p->axes == 0 && p->norm == S3R_NORM_NONE) return fail(S3R_ERR_INVALID_ARG, "neither axes nor a norm: nothing to do");
+    int pairs = 0;
+    for (int x = 0; x < p->axes; ++x) {
+        if (p->axis_pairs[x] < 1 || p->axis_pairs[x] > 32) return fail(S3R_ERR_INVALID_ARG, "axis_pairs[%d] (%d) must be 1 to 32", x, p->axis_pairs[x]);
+        pairs += p->axis_pairs[x];
+    }
+    if (pairs > 32) return fail(S3R_ERR_INVALID_ARG, "axis_pairs add up to %d, more than the 32 pairs of a head", pairs);
+    if (p->pairs < S3R_PAIRS_HALVES || p->pairs > S3R_PAIRS_WHOLE) return fail(S3R_ERR_INVALID_ARG, "pairs (%d) must be one of S3R_PAIRS_*", p->pairs);
+    if (p->norm != S3R_NORM_NONE) return check_eps(p->eps);
+    if (p->q_weight || p->q_bias || p->k_weight || p->k_bias || p->dq_weight || p->dq_bias || p->dk_weight || p->dk_bias)
+        return fail(S3R_ERR_INVALID_ARG, "weights and biases need a norm");
+    return S3R_OK;
+}
+
+// What the two calls have in common; the tensors' pointers and strides are theirs.
+s3r_status rotary_args(const s3r_rotary_params *p, s3r::RotaryArgs *out)
+{
+    s3r_status st = check_rotary(p);
+    if (st != S3R_OK) return st;
+    if ((p->axes > 0) != (p->cos != nullptr) || (p->axes > 0) != (p->sin != nullptr))
+        return fail(S3R_ERR_INVALID_ARG, "cos, sin and axes must be given together");
+    if (!aligned16(p->cos) || !aligned16(p->sin) || !aligned(p->positions, 4) || !aligned(p->status, 4))
+        return fail(S3R_ERR_INVALID_ARG, "cos and sin must be 16-byte aligned, positions and status 4-byte");
+    if (p->axes > 0 && p->n_positions <= 0) return fail(S3R_ERR_INVALID_ARG, "n_positions must be positive");
+    if (p->axes > 1 && !p->positions && p->n_rows > 0) return fail(S3R_ERR_INVALID_ARG, "positions must be given for %d axes", p->axes);
+    if (p->axes == 0 && p->positions) return fail(S3R_ERR_INVALID_ARG, "positions need axes");
+    for (const void *t : {p->q, p->k, static_cast<const void *>(p->q_out), static_cast<const void *>(p->k_out), p->d_q_out, p->d_k_out,
+                          static_cast<const void *>(p->dq), static_cast<const void *>(p->dk), p->q_weight, p->q_bias, p->k_weight, p->k_bias,
+                          static_cast<const void *>(p->dq_weight), static_cast<const void *>(p->dq_bias), static_cast<const void *>(p->dk_weight),
+                          static_cast<const void *>(p->dk_bias)})
+        if (!aligned16(t)) return fail(S3R_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+    for (auto [what, tok, head] : {std::make_tuple("q", p->q_stride_tok, p->q_stride_head), std::make_tuple("k", p->k_stride_tok, p->k_stride_head),
+                                   std::make_tuple("dq", p->dq_stride_tok, p->dq_stride_head), std::make_tuple("dk", p->dk_stride_tok, p->dk_stride_head)}) {
+        st = check_strides(what, tok, head);
+        if (st != S3R_OK) return st;
+    }
+    s3r::RotaryArgs a{};
+    a.cos = p->cos; a.sin = p->sin; a.positions = p->positions;
+    a.n_rows = p->n_rows; a.places = p->n_positions;
+    a.axes = p->axes; a.pairing = p->pairs; a.norm = p->norm;
+    for (int x = 0; x < p->axes; ++x) {
+        a.axis_pairs[x] = p->axis_pairs[x];
+        a.n_pairs += p->axis_pairs[x];
+    }
+    a.w_bf16 = p->weight_dtype == S3R_BF16;
+    a.eps = p->eps;
+    a.sign = 1.f;
+    a.side[0].heads = p->heads; a.side[0].weight = p->q_weight; a.side[0].bias = p->q_bias;
+    a.side[1].heads = p->kv_heads; a.side[1].weight = p->k_weight; a.side[1].bias = p->k_bias;
+    *out = a;
+    return S3R_OK;
+}
+
+int64_t or_else(int64_t given, int64_t packed) { return given ? given : packed; }
+
+bool same_as_any(const void *t, std::initializer_list<const void *> others)
+{
+    for (const void *o : others)
+        if (t && t == o) return true;
+    return false;
+}
+
+}  // namespace
+
+size_t speed3r_rotary_workspace_bytes(const s3r_rotary_params *p)
+{
+    if (check_rotary(p) != S3R_OK) return SIZE_MAX;
+    return p->norm != S3R_NORM_NONE && (p->dq_weight || p->dq_bias || p->dk_weight || p->dk_bias)
+               ? align_up(static_cast<size_t>(s3r::kRotaryGradGroups) * 128 * sizeof(float)) : 0;
+}
+
+s3r_status speed3r_rotary(const s3r_rotary_params *p)
+{
+    s3r::RotaryArgs a;
+    s3r_status st = rotary_args(p, &a);
+    if (st != S3R_OK) return st;
+    if (p->n_rows > 0 && ((p->heads > 0 && (!p->q || !p->q_out)) || (p->kv_heads > 0 && (!p->k || !p->k_out))))
+        return fail(S3R_ERR_INVALID_ARG, "q, k, q_out and k_out must be non-null");
+    if (same_as_any(p->q_out, {p->q, p->k, p->k_out}) || same_as_any(p->k_out, {p->q, p->k}))
+        return fail(S3R_ERR_INVALID_ARG, "q_out and k_out must not alias inputs or each other");
+    const int64_t q_row = int64_t(p->heads) * 64, k_row = int64_t(p->kv_heads) * 64;
+    s3r::RotarySide &q = a.side[0], &k = a.side[1];
+    q.in = p->q; q.out = p->q_out; q.in_row = or_else(p->q_stride_tok, q_row); q.in_head = or_else(p->q_stride_head, 64); q.out_row = q_row; q.out_head = 64;
+    k.in = p->k; k.out = p->k_out; k.in_row = or_else(p->k_stride_tok, k_row); k.in_head = or_else(p->k_stride_head, 64); k.out_row = k_row; k.out_head = 64;
+    hipStream_t s = static_cast<hipStream_t>(p->stream);
+    if (p->status) S3R_HIP(s3r::launch_rotary_status(a, p->status, s), "status kernel launch");
+    if (p->n_rows == 0) return S3R_OK;
+    StageTimer tm(S3R_STAGE_POOL, s);
+    S3R_HIP(s3r::launch_rotary(a, p->dtype == S3R_BF16, s), "rotary kernel launch");
+    return S3R_OK;
+}
+
+s3r_status speed3r_rotary_backward(const s3r_rotary_params *p)
+{
+    s3r::RotaryArgs a;
+    s3r_status st = rotary_args(p, &a);
+    if (st != S3R_OK) return st;
+    const bool norm = p->norm != S3R_NORM_NONE;
+    if (p->n_rows > 0 && ((p->heads > 0 && (!p->d_q_out || !p->dq || (norm && !p->q))) || (p->kv_heads > 0 && (!p->d_k_out || !p->dk || (norm && !p->k)))))
+        return fail(S3R_ERR_INVALID_ARG, "d_q_out, d_k_out, dq and dk (and, with a norm, q and k) must be non-null");
+    if (same_as_any(p->dq, {p->q, p->k, p->d_q_out, p->d_k_out, p->dk}) || same_as_any(p->dk, {p->q, p->k, p->d_q_out, p->d_k_out}))
+        return fail(S3R_ERR_INVALID_ARG, "gradients must not alias inputs or each other");
+    const size_t need = speed3r_rotary_workspace_bytes(p);
+    st = check_workspace(p->workspace, p->workspace_bytes, need);
+    if (st != S3R_OK) return st;
+    const int64_t q_row = int64_t(p->heads) * 64, k_row = int64_t(p->kv_heads) * 64;
+    s3r::RotarySide &q = a.side[0], &k = a.side[1];
+    q.out = p->dq; q.out_row = or_else(p->dq_stride_tok, q_row); q.out_head = or_else(p->dq_stride_head, 64);
+    k.out = p->dk; k.out_row = or_else(p->dk_stride_tok, k_row); k.out_head = or_else(p->dk_stride_head, 64);
+    q.in = norm ? p->q : p->d_q_out; q.in_row = norm ? or_else(p->q_stride_tok, q_row) : q_row; q.in_head = norm ? or_else(p->q_stride_head, 64) : 64;
+    k.in = norm ? p->k : p->d_k_out; k.in_row = norm ? or_else(p->k_stride_tok, k_row) : k_row; k.in_head = norm ? or_else(p->k_stride_head, 64) : 64;
+    q.grad = p->d_q_out; q.d_weight = p->dq_weight; q.d_bias = p->dq_bias;
+    k.grad = p->d_k_out; k.d_weight = p->dk_weight; k.d_bias = p->dk_bias;
+    a.part = need > 0 ? static_cast<float *>(p->workspace) : nullptr;
+    hipStream_t s = static_cast<hipStream_t>(p->stream);
+    if (p->status) S3R_HIP(s3r::launch_rotary_status(a, p->status, s), "status kernel launch");
+    if (p->n_rows == 0 && a.part == nullptr) return S3R_OK;
+    StageTimer tm(S3R_STAGE_POOL, s);
+    if (norm) {
+        S3R_HIP(s3r::launch_rotary_norm_grad(a, p->dtype == S3R_BF16, s), "rotary gradient kernel launch");
+    } else {
+        a.sign = -1.f;
+        S3R_HIP(s3r::launch_rotary(a, p->dtype == S3R_BF16, s), "rotary gradient kernel launch");
+    }
+    return S3R_OK;
+}
+
+// ---- the residual stream with the norms around a block -----------------------------------------------------
+namespace {
+
+struct ResidualPlan {
+    int batch, rows_per_block;
+    int64_t blocks;
+    size_t part, part_gate, need;  // workspace of the gradient
+};
+
+// Workgroups: as many as the card holds at once, or fewer; their rows follow one another, a multiple of what they have at a time.
+constexpr int kResidualBlocks = 2048, kResidualGradBlocks = 512;
+
+s3r_status plan_residual(const s3r_residual_params *p, bool backward, ResidualPlan *out)
+{
+    if (!p) return fail(S3R_ERR_INVALID_ARG, "params is null");
+    if (p->width < 8 || p->width > 8192 || p->width % 8 != 0) return fail(S3R_ERR_UNSUPPORTED, "width %d unsupported (must be a multiple of 8 up to 8192)", p->width);
+    if (p->n_rows < 0) return fail(S3R_ERR_INVALID_ARG, "n_rows must not be negative");
+    if (p->n_rows > kMaxRowHeads) return fail(S3R_ERR_UNSUPPORTED, "n_rows exceeds 2^28");
+    if (p->dtype != S3R_F32 && p->dtype != S3R_BF16) return fail(S3R_ERR_UNSUPPORTED, "unknown dtype %d", p->dtype);
+    if (p->x_dtype != S3R_F32 && p->x_dtype != p->dtype) return fail(S3R_ERR_UNSUPPORTED, "x_dtype must be dtype or fp32");
+    if (p->weight_dtype != S3R_F32 && p->weight_dtype != S3R_BF16) return fail(S3R_ERR_UNSUPPORTED, "unknown weight_dtype %d", p->weight_dtype);
+    if (p->batch < 0 || (p->batch > 1 && !p->row_start)) return fail(S3R_ERR_INVALID_ARG, "batch (%d) must be 1 without row_start, and never negative", p->batch);
+    if (p->row_start && (p->batch == 0 || !p->gate)) return fail(S3R_ERR_INVALID_ARG, "row_start needs gates and a positive batch");
+    if (p->batch > 65536) return fail(S3R_ERR_UNSUPPORTED, "batch (%d) exceeds 65536", p->batch);
+    s3r_status st = check_norm("norm", p->norm);
+    if (st != S3R_OK) return st;
+    st = check_norm("post_norm", p->post_norm);
+    if (st != S3R_OK) return st;
+    if (p->norm != S3R_NORM_NONE || p->post_norm != S3R_NORM_NONE) {
+        st = check_eps(p->eps);
+        if (st != S3R_OK) return st;
+    }
+    if (!std::isfinite(p->residual_scale)) return fail(S3R_ERR_INVALID_ARG, "residual_scale must be finite");
+    if (p->norm == S3R_NORM_NONE && (p->weight || p->bias || p->d_weight || p->d_bias)) return fail(S3R_ERR_INVALID_ARG, "weight and bias need a norm");
+    if (p->post_norm == S3R_NORM_NONE && (p->post_weight || p->post_bias || p->d_post_weight || p->d_post_bias))
+        return fail(S3R_ERR_INVALID_ARG, "post_weight and post_bias need a post_norm");
+    if (p->n_rows > 0 && !p->f && (p->post_norm != S3R_NORM_NONE || p->scale || p->gate || p->d_scale || p->d_gate))
+        return fail(S3R_ERR_INVALID_ARG, "a post_norm, scale and gate need f");
+    if (p->d_gate && !p->gate) return fail(S3R_ERR_INVALID_ARG, "d_gate needs a gate");
+    ResidualPlan c{};
+    c.batch = p->batch == 0 ? 1 : p->batch;
+    const int64_t at_once = s3r::residual_rows(p->width), most = backward ? kResidualGradBlocks : kResidualBlocks;
+    const int64_t rows = ((p->n_rows + most - 1) / most + at_once - 1) / at_once * at_once;
+    c.rows_per_block = static_cast<int>(rows < at_once ? at_once : rows);
+    c.blocks = (p->n_rows + c.rows_per_block - 1) / c.rows_per_block;
+    const size_t row = static_cast<size_t>(p->width) * sizeof(float);
+    size_t off = 0;
+    c.part = off;
+    if (p->d_weight || p->d_bias || p->d_scale || p->d_post_weight || p->d_post_bias) off += align_up(5 * static_cast<size_t>(c.blocks) * row);
+    c.part_gate = off;
+    if (p->d_gate) off += align_up((static_cast<size_t>(c.blocks) + c.batch) * row);
+    c.need = off;
+    *out = c;
+    return S3R_OK;
+}
+
+s3r_status residual_args(const s3r_residual_params *p, const ResidualPlan &c, s3r::ResidualArgs *out)
+{
+    if (p->n_rows > 0 && !p->x) return fail(S3R_ERR_INVALID_ARG, "x must be non-null");
+    for (const void *t : {p->x, p->f, static_cast<const void *>(p->r), static_cast<const void *>(p->y), p->weight, p->bias, p->post_weight, p->post_bias,
+                          p->scale, p->gate, p->d_r, p->d_y, static_cast<const void *>(p->dx), static_cast<const void *>(p->df),
+                          static_cast<const void *>(p->d_weight), static_cast<const void *>(p->d_bias), static_cast<const void *>(p->d_post_weight),
+                          static_cast<const void *>(p->d_post_bias), static_cast<const void *>(p->d_scale), static_cast<const void *>(p->d_gate)})
+        if (!aligned16(t)) return fail(S3R_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+    if (!aligned(p->row_start, 4) || !aligned(p->status, 4)) return fail(S3R_ERR_INVALID_ARG, "row_start and status must be 4-byte aligned");
+    for (auto [what, stride] : {std::make_pair("x", p->x_stride), std::make_pair("f", p->f_stride), std::make_pair("gate", p->gate_stride)}) {
+        s3r_status st = check_strides(what, stride, 0);
+        if (st != S3R_OK) return st;
+    }
+    s3r::ResidualArgs a{};
+    a.x = p->x; a.f = p->f; a.gate = p->gate;
+    a.x_row = or_else(p->x_stride, p->width); a.f_row = or_else(p->f_stride, p->width); a.gate_row = or_else(p->gate_stride, p->width);
+    a.weight = p->weight; a.bias = p->bias; a.post_weight = p->post_weight; a.post_bias = p->post_bias; a.scale = p->scale;
+    a.spans = s3r::Spans{p->row_start, c.batch, p->n_rows};
+    a.n = p->n_rows; a.width = p->width; a.norm = p->norm; a.post = p->post_norm; a.rows_per_block = c.rows_per_block;
+    a.w_bf16 = p->weight_dtype == S3R_BF16;
+    a.eps = p->eps;
+    a.residual_scale = p->residual_scale == 0.f ? 1.f : p->residual_scale;
+    *out = a;
+    return S3R_OK;
+}
+
+}  // namespace
+
+size_t speed3r_residual_workspace_bytes(const s3r_residual_params *p)
+{
+    ResidualPlan c;
+    if (plan_residual(p, true, &c) != S3R_OK) return SIZE_MAX;
+    return c.need;
+}
+
+s3r_status speed3r_residual_norm(const s3r_residual_params *p)
+{
+    ResidualPlan c;
+    s3r_status st = plan_residual(p, false, &c);
+    if (st != S3R_OK) return st;
+    s3r::ResidualArgs a;
+    st = residual_args(p, c, &a);
+    if (st != S3R_OK) return st;
+    if (p->n_rows > 0 && !p->r && !p->y) return fail(S3R_ERR_INVALID_ARG, "r and y must not both be null");
+    if (p->y && p->norm == S3R_NORM_NONE) return fail(S3R_ERR_INVALID_ARG, "y needs a norm");
+    if (same_as_any(p->y, {p->x, p->f, p->r, p->gate}) || same_as_any(p->r, {p->f, p->gate}) || (p->r && p->r == p->x && a.x_row != p->width))
+        return fail(S3R_ERR_INVALID_ARG, "outputs must not alias inputs or each other (but r may be a packed x)");
+    a.r = p->r; a.y = p->y;
+    hipStream_t s = static_cast<hipStream_t>(p->stream);
+    if (p->status) S3R_HIP(s3r::launch_span_status(a.spans, a.spans, p->status, s), "status kernel launch");
+    if (p->n_rows == 0) return S3R_OK;
+    StageTimer tm(S3R_STAGE_POOL, s);
+    S3R_HIP(s3r::launch_residual(a, p->x_dtype == S3R_BF16, p->dtype == S3R_BF16, s), "residual norm kernel launch");
+    return S3R_OK;
+}
+
+s3r_status speed3r_residual_norm_backward(const s3r_residual_params *p)
+{
+    ResidualPlan c;
+    s3r_status st = plan_residual(p, true, &c);
+    if (st != S3R_OK) return st;
+    s3r::ResidualArgs a;
+    st = residual_args(p, c, &a);
+    if (st != S3R_OK) return st;
+    if (p->n_rows > 0 && !p->dx) return fail(S3R_ERR_INVALID_ARG, "dx must be non-null");
+    if (p->n_rows > 0 && (p->f != nullptr) != (p->df != nullptr)) return fail(S3R_ERR_INVALID_ARG, "f and df must be given together");
+    if (p->n_rows > 0 && !p->d_r && !p->d_y) return fail(S3R_ERR_INVALID_ARG, "d_r and d_y must not both be null");
+    if (p->d_y && p->norm == S3R_NORM_NONE) return fail(S3R_ERR_INVALID_ARG, "d_y needs a norm");
+    if (same_as_any(p->dx, {p->x, p->f, p->d_r, p->d_y, p->df, p->gate}) || same_as_any(p->df, {p->x, p->f, p->d_r, p->d_y, p->gate}))
+        return fail(S3R_ERR_INVALID_ARG, "gradients must not alias inputs or each other");
+    st = check_workspace(p->workspace, p->workspace_bytes, c.need);
+    if (st != S3R_OK) return st;
+    a.d_r = p->d_r; a.d_y = p->d_y; a.dx = p->dx; a.df = p->df;
+    a.d_weight = p->d_weight; a.d_bias = p->d_bias; a.d_post_weight = p->d_post_weight; a.d_post_bias = p->d_post_bias;
+    a.d_scale = p->d_scale; a.d_gate = p->d_gate;
+    if (c.part_gate > c.part) a.part = floats_at(p->workspace, c.part);
+    if (p->d_gate) a.part_gate = floats_at(p->workspace, c.part_gate);
+    hipStream_t s = static_cast<hipStream_t>(p->stream);
+    if (p->status) S3R_HIP(s3r::launch_span_status(a.spans, a.spans, p->status, s), "status kernel launch");
+    StageTimer tm(S3R_STAGE_POOL, s);
+    S3R_HIP(s3r::launch_residual_grad(a, p->x_dtype == S3R_BF16, p->dtype == S3R_BF16, s), "residual norm gradient kernel launch");
     return S3R_OK;
 }
 

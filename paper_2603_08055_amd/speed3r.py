@@ -15,6 +15,8 @@ LIB_PATH = os.path.join(_HERE, "libspeed3r.so")
 
 S3R_OK, S3R_ERR_INVALID_ARG, S3R_ERR_UNSUPPORTED, S3R_ERR_WORKSPACE, S3R_ERR_HIP = range(5)
 S3R_F32, S3R_BF16 = 0, 1
+S3R_NORM_NONE, S3R_NORM_RMS, S3R_NORM_LAYER = range(3)
+S3R_PAIRS_HALVES, S3R_PAIRS_NEIGHBOURS, S3R_PAIRS_WHOLE = range(3)
 S3R_DIAG_FORCED_RANGE, S3R_DIAG_FORCED_ORDER = 1, 2
 S3R_DIAG_PAGE, S3R_DIAG_SPANS, S3R_DIAG_LENGTH, S3R_DIAG_POSITION = 4, 8, 16, 32
 STAGES = ("pool", "split", "compress", "topk", "select", "dense")
@@ -57,6 +59,27 @@ class s3r_cache_params(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_size_t), ("stream", _vp)]
 
 
+class s3r_rotary_params(ctypes.Structure):
+    _fields_ = [("q", _vp), ("k", _vp), ("q_out", _vp), ("k_out", _vp), ("d_q_out", _vp), ("d_k_out", _vp), ("dq", _vp),
+                ("dk", _vp), ("q_weight", _vp), ("q_bias", _vp), ("k_weight", _vp), ("k_bias", _vp), ("dq_weight", _vp),
+                ("dq_bias", _vp), ("dk_weight", _vp), ("dk_bias", _vp), ("cos", _vp), ("sin", _vp), ("positions", _vp),
+                ("status", _vp), ("n_rows", _i64), ("n_positions", _i64), ("q_stride_tok", _i64), ("q_stride_head", _i64),
+                ("k_stride_tok", _i64), ("k_stride_head", _i64), ("dq_stride_tok", _i64), ("dq_stride_head", _i64),
+                ("dk_stride_tok", _i64), ("dk_stride_head", _i64), ("heads", _int), ("kv_heads", _int), ("head_dim", _int),
+                ("dtype", _int), ("weight_dtype", _int), ("axes", _int), ("axis_pairs", _int * 3), ("pairs", _int),
+                ("norm", _int), ("eps", _flt), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t), ("stream", _vp)]
+
+
+class s3r_residual_params(ctypes.Structure):
+    _fields_ = [("x", _vp), ("f", _vp), ("r", _vp), ("y", _vp), ("weight", _vp), ("bias", _vp), ("post_weight", _vp),
+                ("post_bias", _vp), ("scale", _vp), ("gate", _vp), ("row_start", _vp), ("d_r", _vp), ("d_y", _vp), ("dx", _vp),
+                ("df", _vp), ("d_weight", _vp), ("d_bias", _vp), ("d_post_weight", _vp), ("d_post_bias", _vp), ("d_scale", _vp),
+                ("d_gate", _vp), ("status", _vp), ("n_rows", _i64), ("x_stride", _i64), ("f_stride", _i64),
+                ("gate_stride", _i64), ("width", _int), ("batch", _int), ("x_dtype", _int), ("dtype", _int),
+                ("weight_dtype", _int), ("norm", _int), ("post_norm", _int), ("eps", _flt), ("residual_scale", _flt),
+                ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t), ("stream", _vp)]
+
+
 EXPORTS = {
     "speed3r_workspace_bytes": (ctypes.c_size_t, [_i64, _int, _int, _int, _int, _int, _int]),
     "speed3r_workspace_bytes_ex": (ctypes.c_size_t, [ctypes.POINTER(s3r_params)]),
@@ -80,6 +103,12 @@ EXPORTS = {
     "speed3r_cache_read": (_int, [ctypes.POINTER(s3r_cache_params)]),
     "speed3r_cache_attn": (_int, [ctypes.POINTER(s3r_cache_params)]),
     "speed3r_cache_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(s3r_cache_params)]),
+    "speed3r_rotary": (_int, [ctypes.POINTER(s3r_rotary_params)]),
+    "speed3r_rotary_backward": (_int, [ctypes.POINTER(s3r_rotary_params)]),
+    "speed3r_rotary_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(s3r_rotary_params)]),
+    "speed3r_residual_norm": (_int, [ctypes.POINTER(s3r_residual_params)]),
+    "speed3r_residual_norm_backward": (_int, [ctypes.POINTER(s3r_residual_params)]),
+    "speed3r_residual_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(s3r_residual_params)]),
     "speed3r_probe_select_loads": (_int, [_vp, _vp, _vp, _vp, _vp, _i64, _int, _int, _int, _int, _int, _int, _vp]),
     "speed3r_set_profiling": (_int, [_int]),
     "speed3r_get_stage_ms": (_int, [ctypes.POINTER(_flt), ctypes.POINTER(_int)]),
@@ -579,6 +608,210 @@ def speed3r_cache_attn(cache, q, out, page_table, kv_len, row_start=None, *, cau
     p = _cache_params(cache, q, page_table, kv_len, row_start, status, stream, index, q=q, out=out, causal=int(bool(causal)),
                       softmax_scale=softmax_scale, lse=lse)
     return _call(lib.speed3r_cache_attn, p, lib.speed3r_cache_workspace_bytes(ctypes.byref(p)), workspace, index, stream)
+
+
+# ---- rotary positions, and the residual stream with its norms ------------------------------------------------
+_NORMS = {None: S3R_NORM_NONE, "rms": S3R_NORM_RMS, "layer": S3R_NORM_LAYER}
+_PAIRS = {"halves": S3R_PAIRS_HALVES, "neighbours": S3R_PAIRS_NEIGHBOURS, "whole": S3R_PAIRS_WHOLE}
+
+
+def _weight_type(dtype, *weights):
+    """The type that the weights given have in common (none: that of the rows)."""
+    for w in weights:
+        if w is not None:
+            return w.dtype
+    return dtype
+
+
+_CODES = {torch.float32: S3R_F32, torch.bfloat16: S3R_BF16}
+
+
+def _code(dtype, name):
+    code = _CODES.get(dtype)
+    if code is None:
+        raise TypeError(f"{name} has unsupported dtype {dtype}")
+    return code
+
+
+def _rotary_params(like_q, like_k, cos, sin, positions, axis_pairs, pairs, norm, eps, weights, status, stream, index):
+    """weights: q_weight, q_bias, k_weight, k_bias and their gradients."""
+    dtype = None
+    p = s3r_rotary_params()
+    for t, name in ((like_q, "q"), (like_k, "k")):
+        if t is None:
+            continue
+        if t.dim() != 3:
+            raise ValueError(f"{name} must be [n_rows, heads, head_dim]")
+        if dtype is not None and (t.dtype is not dtype or t.shape[0] != p.n_rows or t.shape[2] != p.head_dim):
+            raise ValueError("q and k must share dtype, rows and head_dim")
+        dtype = t.dtype
+        p.n_rows, heads, p.head_dim = t.shape
+        if name == "q":
+            p.heads = heads
+        else:
+            p.kv_heads = heads
+    p.dtype = _code(dtype, "q or k")
+    if pairs not in _PAIRS:
+        raise ValueError(f"pairs must be one of {list(_PAIRS)}")
+    if norm not in _NORMS:
+        raise ValueError(f"norm must be one of {list(_NORMS)}")
+    p.pairs, p.norm, p.eps = _PAIRS[pairs], _NORMS[norm], eps
+    if cos is not None:
+        axis_pairs = (32,) if axis_pairs is None else tuple(axis_pairs)
+        if not 1 <= len(axis_pairs) <= 3:
+            raise ValueError("axis_pairs must name 1 to 3 axes")
+        p.axes = len(axis_pairs)
+        total = 0
+        for i, n in enumerate(axis_pairs):
+            p.axis_pairs[i] = n
+            total += n
+        if cos.dim() != 2:
+            raise ValueError("cos and sin must be [n_positions, pairs]")
+        p.n_positions = cos.shape[0]
+        table = (cos.shape[0], total)
+        p.cos, p.sin = _arg(cos, "cos", index, torch.float32, table), _arg(sin, "sin", index, torch.float32, table)
+        if positions is not None:
+            if p.axes == 1 and positions.dim() == 1:
+                positions = positions[:, None]
+            p.positions = _arg(positions, "positions", index, torch.int32, (p.n_rows, p.axes))
+    elif sin is not None or positions is not None or axis_pairs is not None:
+        raise ValueError("sin, positions and axis_pairs need cos")
+    w_dtype = _weight_type(dtype, *weights.values())
+    p.weight_dtype = _code(w_dtype, "a weight")
+    for name, w in weights.items():
+        if w is not None:
+            setattr(p, name, _arg(w, name, index, w_dtype, (p.head_dim,)))
+    p.status, p.stream = _arg(status, "status", index, torch.int32, (1,)), _stream_of(stream, index)
+    return p
+
+
+def speed3r_rotary(q, k, q_out, k_out, cos=None, sin=None, positions=None, *, axis_pairs=None, pairs="halves", norm=None, eps=1e-6,
+                   q_weight=None, q_bias=None, k_weight=None, k_bias=None, status=None, stream=None):
+    """q [n_rows, heads, 64] and k [n_rows, kv_heads, 64] (either may be None), normed head by head (norm: None, "rms" or "layer";
+    weights and biases: [64], all fp32 or all bf16) and rotated, into q_out and k_out (contiguous).  axis_pairs: channel pairs of each
+    of up to three axes, by default (32,); cos, sin: fp32 [n_positions, pairs of all axes]; positions: int32 [n_rows, axes] (one axis: may be
+    [n_rows], or None: row numbers); pairs: "halves" of an axis' channels, "neighbours", or "whole": halves of all axes' channels
+    together.  Without cos nothing is rotated.  status: int32 [1], receives 0 or S3R_DIAG_POSITION.  q and k may be strided views."""
+    index, lib = _gpu(k if q is None else q, "q" if k is None else "k"), load()
+    p = _rotary_params(q, k, cos, sin, positions, axis_pairs, pairs, norm, eps,
+                       {"q_weight": q_weight, "q_bias": q_bias, "k_weight": k_weight, "k_bias": k_bias}, status, stream, index)
+    if q is not None:
+        p.q, p.q_stride_tok, p.q_stride_head = _rows_arg(q, "q", index, q.dtype, q.shape)
+        p.q_out = _arg(q_out, "q_out", index, q.dtype, q.shape)
+    if k is not None:
+        p.k, p.k_stride_tok, p.k_stride_head = _rows_arg(k, "k", index, k.dtype, k.shape)
+        p.k_out = _arg(k_out, "k_out", index, k.dtype, k.shape)
+    _call(lib.speed3r_rotary, p, 0, None, index)
+
+
+def speed3r_rotary_backward(q, k, d_q_out, d_k_out, dq, dk, cos=None, sin=None, positions=None, *, axis_pairs=None, pairs="halves",
+                            norm=None, eps=1e-6, q_weight=None, k_weight=None, dq_weight=None, dq_bias=None, dk_weight=None,
+                            dk_bias=None, workspace=None, status=None, stream=None):
+    """Gradients of speed3r_rotary from those of q_out and k_out (contiguous) into dq and dk (which may be strided views: parts of the
+    gradient of a packed projection), and those of weights and biases that are given.  Without a norm q and k are not
+    read and may be None.  The other arguments are those of the forward call.  Returns the workspace used (None: none was needed)."""
+    like_q, like_k = d_q_out, d_k_out
+    index, lib = _gpu(like_k if like_q is None else like_q, "d_q_out" if like_k is None else "d_k_out"), load()
+    p = _rotary_params(like_q, like_k, cos, sin, positions, axis_pairs, pairs, norm, eps,
+                       {"q_weight": q_weight, "k_weight": k_weight, "dq_weight": dq_weight, "dq_bias": dq_bias, "dk_weight": dk_weight,
+                        "dk_bias": dk_bias}, status, stream, index)
+    if like_q is not None:
+        if q is not None:
+            p.q, p.q_stride_tok, p.q_stride_head = _rows_arg(q, "q", index, like_q.dtype, like_q.shape)
+        p.d_q_out = _arg(d_q_out, "d_q_out", index, like_q.dtype, like_q.shape)
+        p.dq, p.dq_stride_tok, p.dq_stride_head = _rows_arg(dq, "dq", index, like_q.dtype, like_q.shape)
+    if like_k is not None:
+        if k is not None:
+            p.k, p.k_stride_tok, p.k_stride_head = _rows_arg(k, "k", index, like_k.dtype, like_k.shape)
+        p.d_k_out = _arg(d_k_out, "d_k_out", index, like_k.dtype, like_k.shape)
+        p.dk, p.dk_stride_tok, p.dk_stride_head = _rows_arg(dk, "dk", index, like_k.dtype, like_k.shape)
+    return _call(lib.speed3r_rotary_backward, p, lib.speed3r_rotary_workspace_bytes(ctypes.byref(p)), workspace, index, stream)
+
+
+def _matrix_arg(t, name, index, dtype, shape):
+    """data_ptr and row stride of a tensor [rows, width] with contiguous channels."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != index:
+        raise TypeError(f"{name} must be a tensor on GPU {index}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
+    row = shape[1]
+    if not t.is_contiguous():
+        if t.stride(1) != 1:
+            raise TypeError(f"the channels of {name} must be contiguous")
+        if shape[0] > 1:
+            row = t.stride(0)
+        if row == 0:
+            raise TypeError(f"{name} must not be broadcast along its rows")
+    return t.data_ptr(), row
+
+
+def _residual_params(x, like, f, norm, post_norm, eps, weights, gate, row_start, residual_scale, status, stream, index):
+    """like: a tensor of the type that all but the stream have, or None: that of x."""
+    if x.dim() != 2:
+        raise ValueError("x must be [n_rows, width]")
+    if norm not in _NORMS or post_norm not in _NORMS:
+        raise ValueError(f"norm and post_norm must be among {list(_NORMS)}")
+    if residual_scale == 0:
+        raise ValueError("residual_scale must not be 0")
+    shape = n_rows, width = x.shape
+    dtype = x.dtype if like is None else like.dtype
+    p = s3r_residual_params()
+    p.n_rows, p.width, p.x_dtype, p.dtype = n_rows, width, _code(x.dtype, "x"), _code(dtype, "f or y")
+    p.x, p.x_stride = _matrix_arg(x, "x", index, x.dtype, shape)
+    if f is not None:
+        p.f, p.f_stride = _matrix_arg(f, "f", index, dtype, shape)
+    w_dtype = _weight_type(dtype, *weights.values())
+    p.weight_dtype = _code(w_dtype, "a weight")
+    for name, w in weights.items():
+        if w is not None:
+            setattr(p, name, _arg(w, name, index, w_dtype, (width,)))
+    p.batch = 1 if row_start is None else row_start.numel() - 1
+    if gate is not None:
+        p.gate, p.gate_stride = _matrix_arg(gate, "gate", index, dtype, (p.batch, width))
+    p.row_start = _arg(row_start, "row_start", index, torch.int32, (p.batch + 1,))
+    p.norm, p.post_norm, p.eps, p.residual_scale = _NORMS[norm], _NORMS[post_norm], eps, residual_scale
+    p.status, p.stream = _arg(status, "status", index, torch.int32, (1,)), _stream_of(stream, index)
+    return p
+
+
+def speed3r_residual_norm(x, y=None, *, f=None, r=None, norm=None, weight=None, bias=None, eps=1e-6, post_norm=None, post_weight=None,
+                          post_bias=None, scale=None, gate=None, row_start=None, residual_scale=1.0, status=None, stream=None):
+    """r = x + residual_scale * scale * gate * (f, normed by post_norm or not), and y = norm(r), for x and f [n_rows, width]; without f
+    r is x.  r (of x's type; may be x itself) and y (of f's type) are contiguous, either may be None.  norm, post_norm: None, "rms" or
+    "layer"; weights, biases and scale: [width], all fp32 or all bf16; gate: [batch, width], of f's type, for the sequences whose rows
+    start at row_start (int32 [batch + 1]; None: one sequence).  x may be fp32 where f and y are bf16.  x, f and gate may have strides
+    between rows.  status: int32 [1], receives 0 or S3R_DIAG_SPANS."""
+    index, lib = _gpu(x, "x"), load()
+    p = _residual_params(x, y if f is None else f, f, norm, post_norm, eps,
+                         {"weight": weight, "bias": bias, "post_weight": post_weight, "post_bias": post_bias, "scale": scale},
+                         gate, row_start, residual_scale, status, stream, index)
+    if r is not None:
+        p.r = _arg(r, "r", index, x.dtype, x.shape)
+    if y is not None:
+        p.y = _arg(y, "y", index, y.dtype if f is None else f.dtype, x.shape)
+    _call(lib.speed3r_residual_norm, p, 0, None, index)
+
+
+def speed3r_residual_norm_backward(x, d_y, dx, *, f=None, d_r=None, df=None, norm=None, weight=None, eps=1e-6, post_norm=None,
+                                   post_weight=None, post_bias=None, scale=None, gate=None, row_start=None, residual_scale=1.0,
+                                   d_weight=None, d_bias=None, d_post_weight=None, d_post_bias=None, d_scale=None, d_gate=None,
+                                   workspace=None, status=None, stream=None):
+    """Gradients of speed3r_residual_norm from those of y and r (d_y, d_r; contiguous, either may be None) into dx and df, and into
+    those of weights, scale and gate that are given (each like its tensor).  The other arguments are those of the forward call.  Returns the
+    workspace used (None: none was needed)."""
+    index, lib = _gpu(x, "x"), load()
+    p = _residual_params(x, d_y if f is None else f, f, norm, post_norm, eps,
+                         {"weight": weight, "post_weight": post_weight, "post_bias": post_bias, "scale": scale, "d_weight": d_weight,
+                          "d_bias": d_bias, "d_post_weight": d_post_weight, "d_post_bias": d_post_bias, "d_scale": d_scale},
+                         gate, row_start, residual_scale, status, stream, index)
+    dtype = x.dtype if d_y is None and f is None else (d_y if f is None else f).dtype
+    p.d_y, p.d_r = _arg(d_y, "d_y", index, dtype, x.shape), _arg(d_r, "d_r", index, x.dtype, x.shape)
+    p.dx, p.df = _arg(dx, "dx", index, x.dtype, x.shape), _arg(df, "df", index, dtype, x.shape)
+    if d_gate is not None:
+        p.d_gate = _arg(d_gate, "d_gate", index, dtype, (p.batch, x.shape[1]))
+    return _call(lib.speed3r_residual_norm_backward, p, lib.speed3r_residual_workspace_bytes(ctypes.byref(p)), workspace, index, stream)
 
 
 def speed3r_probe_select_loads(q, k, v, idx, out, block, ring_stages=0, wg_per_cu=0, stream=None):

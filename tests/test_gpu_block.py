@@ -1,0 +1,523 @@
+"""GPU tests of rotary positions with head norms and of the residual stream with its norms, through the binding, against plain 64-bit forms
+(tests/block_util.py, which derives the bounds)."""
+import math
+
+import pytest
+import torch
+
+from tests.block_util import check, residual, rotary
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def s3r():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2603_08055_amd import speed3r
+    speed3r.load()
+    return speed3r
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def normal(g, *shape, dtype=F32, scale=1.0, shift=0.0):
+    return (torch.randn(shape, generator=g, device="cuda") * scale + shift).to(dtype)
+
+
+def nan(*shape, dtype=F32):
+    return torch.full(shape, math.nan, dtype=dtype, device="cuda")
+
+
+def nan_like(t):
+    return None if t is None else torch.full(t.shape, math.nan, dtype=t.dtype, device="cuda")
+
+
+def starts(lengths, first=0):
+    s = [first]
+    for n in lengths:
+        s.append(s[-1] + n)
+    return torch.tensor(s, dtype=torch.int32, device="cuda")
+
+
+# ---- rotary ---------------------------------------------------------------------------------------------------
+
+def table(g, places, pairs):
+    angle = torch.rand((places, pairs), generator=g, device="cuda").double() * 7
+    return torch.cos(angle).float(), torch.sin(angle).float()
+
+
+def rotary_case(seed, n, heads, kv_heads, dtype, axis_pairs, norm, w_dtype=F32, bias=True, places=50):
+    g = gen(seed)
+    c = {"q": normal(g, n, heads, 64, dtype=dtype, scale=2.0, shift=0.5) if heads else None,
+         "k": normal(g, n, kv_heads, 64, dtype=dtype, scale=0.5) if kv_heads else None}
+    for x in "qk":
+        c["d_" + x] = None if c[x] is None else normal(g, *c[x].shape, dtype=dtype)
+        c[x + "_weight"] = normal(g, 64, dtype=w_dtype, shift=1.0) if norm and c[x] is not None else None
+        c[x + "_bias"] = normal(g, 64, dtype=w_dtype) if norm and bias and c[x] is not None else None
+    c["cos"], c["sin"] = table(g, places, sum(axis_pairs)) if axis_pairs else (None, None)
+    c["positions"] = torch.randint(0, places, (n, len(axis_pairs)), generator=g, device="cuda").int() if axis_pairs else None
+    return c
+
+
+def run_rotary(s3r, c, axis_pairs, pairs, norm, eps=1e-6, status=None, **kw):
+    """Forward and gradient into buffers full of NaN: results by name."""
+    q, k = c["q"], c["k"]
+    how = dict(axis_pairs=axis_pairs or None, pairs=pairs, norm=norm, eps=eps, q_weight=c["q_weight"], k_weight=c["k_weight"], status=status, **kw)
+    r = {"q_out": nan_like(c["d_q"]), "k_out": nan_like(c["d_k"]), "dq": nan_like(c["d_q"]), "dk": nan_like(c["d_k"])}
+    s3r.speed3r_rotary(q, k, r["q_out"], r["k_out"], c["cos"], c["sin"], c["positions"], q_bias=c["q_bias"], k_bias=c["k_bias"], **how)
+    for x in "qk":
+        if norm and c[x] is not None:
+            like = c[x + "_weight"] if c[x + "_weight"] is not None else c[x][0, 0]
+            r[f"d{x}_weight"], r[f"d{x}_bias"] = nan_like(like), nan_like(like)
+    grads = {n: t for n, t in r.items() if n.endswith("_weight") or n.endswith("_bias")}
+    s3r.speed3r_rotary_backward(q, k, c["d_q"], c["d_k"], r["dq"], r["dk"], c["cos"], c["sin"], c["positions"], **grads, **how)
+    torch.cuda.synchronize()
+    return r
+
+
+def compare_rotary(r, c, axis_pairs, pairs, norm, eps=1e-6):
+    for x in "qk":
+        if c[x] is None:
+            continue
+        want = rotary(c[x], c[x + "_weight"], c[x + "_bias"], c["cos"], c["sin"], c["positions"], axis_pairs, pairs, norm, eps, c["d_" + x])
+        for name, of in ((x + "_out", "out"), ("d" + x, "dx"), (f"d{x}_weight", "d_weight"), (f"d{x}_bias", "d_bias")):
+            if r.get(name) is not None:
+                check(name, r[name], want[of])
+
+
+AXES = [(32,), (16, 16), (16, 8, 8), (10, 11, 11), (12, 20), (8, 4, 4), (3, 1, 5), (1,), (24,)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("pairs", ["halves", "neighbours", "whole"])
+@pytest.mark.parametrize("axis_pairs", AXES)
+def test_rotary_axes_and_pairs(s3r, dtype, pairs, axis_pairs):
+    for norm in (None, "rms", "layer"):
+        c = rotary_case(len(axis_pairs) * 100 + axis_pairs[0], 21, 3, 2, dtype, axis_pairs, norm)
+        print(pairs, axis_pairs, norm, flush=True)
+        compare_rotary(run_rotary(s3r, c, axis_pairs, pairs, norm), c, axis_pairs, pairs, norm)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("norm", [None, "rms", "layer"])
+@pytest.mark.parametrize("n,heads,kv_heads", [(1, 1, 1), (1, 16, 2), (7, 5, 5), (8, 2, 0), (9, 0, 3), (64, 16, 4), (300, 17, 1), (1374, 16, 16), (5000, 2, 1)])
+def test_rotary_rows_and_heads(s3r, dtype, norm, n, heads, kv_heads):
+    c = rotary_case(n + heads, n, heads, kv_heads, dtype, (16, 16), norm, w_dtype=BF16 if heads % 2 else F32, bias=kv_heads != 1)
+    compare_rotary(run_rotary(s3r, c, (16, 16), "halves", norm), c, (16, 16), "halves", norm)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rotary_without_rotation_or_weights(s3r, dtype):
+    for norm in ("rms", "layer"):
+        c = rotary_case(5, 40, 4, 2, dtype, (), norm)
+        compare_rotary(run_rotary(s3r, c, (), "halves", norm), c, (), "halves", norm)
+        c = {**rotary_case(6, 40, 4, 2, dtype, (32,), norm), "q_weight": None, "q_bias": None, "k_weight": None, "k_bias": None}
+        compare_rotary(run_rotary(s3r, c, (32,), "whole", norm), c, (32,), "whole", norm)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("norm", [None, "layer"])
+def test_rotary_views_of_a_packed_projection(s3r, dtype, norm):
+    """q and k as views of one tensor, their gradients as parts of another, of which nothing else is touched."""
+    n, H = 70, 6
+    c = rotary_case(8, n, H, H, dtype, (10, 11, 11), norm)
+    packed = nan(n, 3, H, 64, dtype=dtype)
+    packed[:, 0], packed[:, 1] = c["q"], c["k"]
+    d_packed = nan(n, 3, H, 64, dtype=dtype)
+    want = run_rotary(s3r, c, (10, 11, 11), "halves", norm)
+    how = dict(axis_pairs=(10, 11, 11), norm=norm, q_weight=c["q_weight"], k_weight=c["k_weight"])
+    q_out, k_out = nan_like(c["q"]), nan_like(c["k"])
+    s3r.speed3r_rotary(packed[:, 0], packed[:, 1], q_out, k_out, c["cos"], c["sin"], c["positions"], q_bias=c["q_bias"], k_bias=c["k_bias"], **how)
+    s3r.speed3r_rotary_backward(packed[:, 0], packed[:, 1], c["d_q"], c["d_k"], d_packed[:, 0], d_packed[:, 1], c["cos"], c["sin"], c["positions"], **how)
+    heads_first = c["q"].transpose(0, 1).contiguous().transpose(0, 1)          # another order of rows and heads
+    again = nan_like(c["q"])
+    s3r.speed3r_rotary(heads_first, None, again, None, c["cos"], c["sin"], c["positions"], axis_pairs=(10, 11, 11), norm=norm, q_weight=c["q_weight"],
+                       q_bias=c["q_bias"])
+    torch.cuda.synchronize()
+    for a, b in ((q_out, want["q_out"]), (k_out, want["k_out"]), (d_packed[:, 0], want["dq"]), (d_packed[:, 1], want["dk"]), (again, want["q_out"])):
+        assert torch.equal(a, b)
+    assert torch.isnan(d_packed[:, 2]).all()
+
+
+def test_rotary_positions_of_one_axis_and_outside_the_table(s3r):
+    c = rotary_case(9, 30, 2, 2, BF16, (32,), None, places=40)
+    status = torch.full((1,), 77, dtype=torch.int32, device="cuda")
+    r = run_rotary(s3r, c, (32,), "halves", None, status=status)
+    assert int(status) == 0
+    flat = run_rotary(s3r, {**c, "positions": c["positions"][:, 0]}, (32,), "halves", None)
+    assert all(torch.equal(r[x], flat[x]) for x in r)
+    numbers = torch.arange(30, dtype=torch.int32, device="cuda")
+    assert all(torch.equal(a, b) for a, b in zip(run_rotary(s3r, {**c, "positions": None}, (32,), "halves", None, status=status).values(),
+                                                 run_rotary(s3r, {**c, "positions": numbers}, (32,), "halves", None).values()))
+    assert int(status) == 0
+    far = c["positions"].clone()
+    far[3], far[17], far[29] = -5, 40, 2 ** 31 - 1
+    got = run_rotary(s3r, {**c, "positions": far}, (32,), "halves", None, status=status)
+    assert int(status) == s3r.S3R_DIAG_POSITION
+    compare_rotary(got, {**c, "positions": far}, (32,), "halves", None)
+    c = rotary_case(9, 50, 2, 2, BF16, (32,), None, places=40)
+    run_rotary(s3r, {**c, "positions": None}, (32,), "halves", None, status=status)
+    assert int(status) == s3r.S3R_DIAG_POSITION
+
+
+@pytest.mark.parametrize("norm", [None, "rms"])
+def test_rotary_without_rows(s3r, norm):
+    c = rotary_case(10, 0, 2, 1, BF16, (32,), norm)
+    r = run_rotary(s3r, c, (32,), "halves", norm)
+    for name, t in r.items():
+        assert not torch.isnan(t).any() and float(t.float().abs().sum()) == 0, name
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("pairs,axis_pairs", [("neighbours", (32,)), ("halves", (16, 16)), ("whole", (10, 11, 5))])
+def test_rotary_infinities_and_nan_stay_in_their_pairs_and_heads(s3r, dtype, pairs, axis_pairs):
+    c = rotary_case(11, 20, 3, 2, dtype, axis_pairs, None)
+    c["q"][4, 1, 7], c["q"][5, 2, 60], c["k"][19, 0, 33] = math.inf, -math.inf, math.nan
+    c["d_q"][6, 0, 1] = math.inf
+    compare_rotary(run_rotary(s3r, c, axis_pairs, pairs, None), c, axis_pairs, pairs, None)
+    c = rotary_case(12, 20, 3, 2, dtype, axis_pairs, "layer")
+    c["q"][4, 1, 7] = math.nan
+    r, c["q"][4, 1, 7] = run_rotary(s3r, c, axis_pairs, pairs, "layer"), 0.0
+    want = run_rotary(s3r, c, axis_pairs, pairs, "layer")
+    for name in ("q_out", "dq"):
+        assert torch.isnan(r[name][4, 1]).all()
+        r[name][4, 1] = want[name][4, 1]
+        assert torch.equal(r[name], want[name])
+    assert torch.isnan(r["dq_weight"]).all() and torch.equal(r["dk_weight"], want["dk_weight"]) and torch.equal(r["dk"], want["dk"])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_head_norms_of_constant_tiny_large_and_shifted_rows(s3r, dtype):
+    c = rotary_case(13, 6, 4, 1, dtype, (32,), "layer")
+    c["q"][0], c["q"][1], c["q"][2] = 0.0, 3.0, c["q"][2] * 2.0 ** -70
+    c["q"][3], c["q"][4] = c["q"][3] * 2.0 ** 50, c["q"][4] + 1000.0
+    compare_rotary(run_rotary(s3r, c, (32,), "halves", "layer"), c, (32,), "halves", "layer")
+    compare_rotary(run_rotary(s3r, c, (32,), "halves", "rms"), c, (32,), "halves", "rms")
+    compare_rotary(run_rotary(s3r, c, (32,), "halves", "layer", eps=0.1), c, (32,), "halves", "layer", 0.1)
+
+
+def test_rotary_agrees_with_the_cache(s3r):
+    """fp32 queries that the cache rotates in 64 bits, and these."""
+    n, H = 100, 4
+    c = rotary_case(14, n, H, H, F32, (32,), None, places=n)
+    cache = s3r.PagedCache.empty(n_pages=2, kv_heads=H, page=64)
+    page_table, kv_len = torch.tensor([[0, 1]], dtype=torch.int32, device="cuda"), torch.tensor([n], dtype=torch.int32, device="cuda")
+    for pairs in ("halves", "neighbours"):
+        want, got = nan_like(c["q"]), nan_like(c["q"])
+        s3r.speed3r_cache_append(cache, c["k"], c["k"].clone(), page_table, kv_len, q=c["q"], q_out=want, cos=c["cos"], sin=c["sin"], pairs=pairs)
+        s3r.speed3r_rotary(c["q"], None, got, None, c["cos"], c["sin"], pairs=pairs)
+        # (`want` is rounded once, `got` off by up to 3 * 2^-24)
+        assert float(((got - want).abs() / want.abs().clamp(min=1e-30)).max()) <= 4 * 2.0 ** -24
+
+
+def test_rotary_far_rows(s3r):
+    """Rows past 2^32 bytes, and results past 2^31 elements."""
+    rows, stride = 40, (5 << 30) // (2 * 40) // 8 * 8
+    room = torch.zeros(rows * stride, dtype=BF16, device="cuda")
+    c = rotary_case(15, rows, 1, 0, BF16, (16, 16), "rms")
+    view = room.as_strided((rows, 1, 64), (stride, 64, 1))
+    view.copy_(c["q"])
+    want = run_rotary(s3r, c, (16, 16), "halves", "rms")
+    out, dq = nan_like(c["q"]), room.as_strided((rows, 1, 64), (stride, 64, 1), 128)
+    how = dict(axis_pairs=(16, 16), norm="rms", q_weight=c["q_weight"])
+    s3r.speed3r_rotary(view, None, out, None, c["cos"], c["sin"], c["positions"], q_bias=c["q_bias"], **how)
+    s3r.speed3r_rotary_backward(view, None, c["d_q"], None, dq, None, c["cos"], c["sin"], c["positions"], **how)
+    assert torch.equal(out, want["q_out"]) and torch.equal(dq, want["dq"])
+    del room, view, dq
+    n = (1 << 31) // (64 * 16) + 9
+    q = torch.ones((n, 16, 64), dtype=BF16, device="cuda")
+    q[-20:] = normal(gen(1), 20, 16, 64, dtype=BF16)
+    out = torch.empty_like(q)
+    cos, sin = table(gen(2), 50, 32)
+    at = torch.zeros((n, 1), dtype=torch.int32, device="cuda")
+    at[-20:] = 7
+    s3r.speed3r_rotary(q, None, out, None, cos, sin, at)
+    check("last rows", out[-20:], rotary(q[-20:], None, None, cos, sin, at[-20:], (32,), "halves", None, 1e-6)["out"])
+
+
+# ---- the residual stream -----------------------------------------------------------------------------------------
+
+def residual_case(seed, n, width, x_dtype=BF16, dtype=BF16, w_dtype=F32, norm="layer", post=None, f=True, scale=True, rows=None, bias=True):
+    g = gen(seed)
+    c = {"x": normal(g, n, width, dtype=x_dtype, scale=1.5, shift=0.3), "f": normal(g, n, width, dtype=dtype, scale=2.0, shift=-0.2) if f else None,
+         "norm": norm, "post_norm": post}
+    for name, there in (("weight", norm), ("bias", norm and bias), ("post_weight", post), ("post_bias", post and bias), ("scale", f and scale)):
+        c[name] = normal(g, width, dtype=w_dtype, shift=0.0 if "bias" in name else 1.0) if there else None
+    c["gate"] = normal(g, len(rows), width, dtype=dtype) if rows else None
+    c["row_start"] = starts(rows) if rows else None
+    c["d_r"], c["d_y"] = normal(g, n, width, dtype=x_dtype), normal(g, n, width, dtype=dtype) if norm else None
+    c["dtype"], c["w_dtype"] = dtype, w_dtype
+    return c
+
+
+CALL = ("f", "norm", "weight", "post_norm", "post_weight", "post_bias", "scale", "gate", "row_start")
+
+
+def run_residual(s3r, c, eps=1e-6, residual_scale=0.75, gradient=True, **kw):
+    n, width = c["x"].shape
+    how = {**{name: c[name] for name in CALL}, "eps": eps, "residual_scale": residual_scale, **kw}
+    r = {"r": nan_like(c["x"])}
+    if c["norm"]:
+        r["y"] = nan(n, width, dtype=c["dtype"])
+    s3r.speed3r_residual_norm(c["x"], r.get("y"), r=r["r"], bias=c["bias"], **how)
+    if gradient:
+        grads = {}
+        for name, there in (("d_weight", c["norm"]), ("d_bias", c["norm"]), ("d_post_weight", c["post_norm"]), ("d_post_bias", c["post_norm"]),
+                            ("d_scale", c["scale"] is not None)):
+            if there:
+                grads[name] = nan(width, dtype=c["w_dtype"])
+        if c["gate"] is not None:
+            grads["d_gate"] = nan(*c["gate"].shape, dtype=c["dtype"])
+        r["dx"] = nan_like(c["x"])
+        if c["f"] is not None:
+            r["df"] = nan_like(c["f"])
+        s3r.speed3r_residual_norm_backward(c["x"], c["d_y"], r["dx"], d_r=c["d_r"], df=r.get("df"), **grads, **how)
+        r.update(grads)
+    torch.cuda.synchronize()
+    return r
+
+
+def compare_residual(got, c, eps=1e-6, residual_scale=0.75, rows=None):
+    seq = None
+    if c["gate"] is not None:
+        lengths = rows or [c["x"].shape[0]]
+        seq = torch.repeat_interleave(torch.arange(len(lengths), device="cuda"), torch.tensor(lengths, device="cuda"))
+    want = residual(c["x"], c["f"], c["norm"], c["weight"], c["bias"], eps, c["post_norm"], c["post_weight"], c["post_bias"], c["scale"], c["gate"], seq,
+                    residual_scale, c["d_r"] if "dx" in got else None, c["d_y"] if "dx" in got else None, c["dtype"], c["w_dtype"])
+    for name in got:
+        check(name, got[name], want[name])
+
+
+TYPES = [(BF16, BF16, F32), (F32, F32, F32), (F32, BF16, BF16)]
+WIDTHS = [8, 64, 120, 128, 136, 512, 520, 1000, 1024, 1032, 2048, 4096, 4104, 5000, 8192]
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("width", WIDTHS)
+def test_residual_widths(s3r, types, width):
+    for norm, post, rows in (("layer", None, None), ("rms", "layer", [20, 1, 16]), ("layer", "rms", None)):
+        print(width, norm, post, rows, flush=True)
+        c = residual_case(width, 37, width, *types, norm=norm, post=post, rows=rows)
+        compare_residual(run_residual(s3r, c), c, rows=rows)
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("n", [1, 2, 5, 16, 17, 700, 5001])
+def test_residual_rows(s3r, types, n):
+    for width, post in ((64, "rms"), (1024, None), (1024, "layer"), (4096, None)):
+        c = residual_case(n, n, width, *types, post=post)
+        compare_residual(run_residual(s3r, c), c)
+
+
+@pytest.mark.parametrize("types", TYPES)
+def test_residual_parts_that_are_absent(s3r, types):
+    base = dict(x_dtype=types[0], dtype=types[1], w_dtype=types[2])
+    for change in (dict(f=False), dict(norm=None), dict(norm=None, post="rms"), dict(scale=False), dict(bias=False, post="layer"), dict(f=False, norm="rms")):
+        print(change, flush=True)
+        c = residual_case(3, 50, 520, **base, **change)
+        compare_residual(run_residual(s3r, c), c)
+    c = residual_case(4, 50, 520, **base, post="rms")
+    c.update(weight=None, bias=None, post_weight=None, post_bias=None)
+    compare_residual(run_residual(s3r, c), c)
+    c = residual_case(5, 50, 520, **base)
+    for gone in ("d_r", "d_y"):
+        got = run_residual(s3r, {**c, gone: None})
+        if gone == "d_y":
+            assert float(got.pop("d_weight").float().abs().sum()) == 0 and float(got.pop("d_bias").float().abs().sum()) == 0
+        compare_residual(got, {**c, gone: None})
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("rows", [[300], [1] * 64, [0, 5, 0, 0, 100, 1, 0], [2, 1] * 100, [700, 3, 900]])
+@pytest.mark.parametrize("width", [64, 1000, 4096])
+def test_residual_gates_of_ragged_sequences(s3r, types, rows, width):
+    c = residual_case(len(rows) + width, sum(rows), width, *types, norm="rms", post="rms", rows=rows)
+    got = run_residual(s3r, c)
+    for b, n in enumerate(rows):
+        if n == 0:
+            assert float(got["d_gate"][b].float().abs().sum()) == 0
+    compare_residual(got, c, rows=rows)
+
+
+def test_residual_many_short_sequences(s3r):
+    g = gen(5)
+    rows = torch.randint(0, 3, (5000,), generator=g, device="cuda").tolist()
+    c = residual_case(6, sum(rows), 64, rows=rows)
+    got = run_residual(s3r, c)
+    seq = torch.repeat_interleave(torch.arange(len(rows), device="cuda"), torch.tensor(rows, device="cuda"))
+    want = residual(c["x"], c["f"], "layer", c["weight"], c["bias"], 1e-6, scale=c["scale"], gate=c["gate"], seq=seq, residual_scale=0.75,
+                    d_r=c["d_r"], d_y=c["d_y"], w_dtype=F32)
+    for name in got:
+        check(name, got[name], want[name])
+
+
+@pytest.mark.parametrize("width", [64, 1024, 4096])
+def test_residual_rows_outside_and_broken_lists(s3r, width):
+    """Rows before the first and behind the last sequence are left as they were, and their contents count for nothing; a list out of order or
+    range is reported and stays in memory."""
+    rows = [40, 0, 25]
+    whole = residual_case(7, 65, width, rows=rows, post="rms")
+    want = run_residual(s3r, whole)
+    c = dict(whole)
+    for name in ("x", "f", "d_r", "d_y"):
+        c[name] = torch.cat((nan(10, width, dtype=whole[name].dtype), whole[name], nan(9, width, dtype=whole[name].dtype)))
+    c["row_start"] = starts(rows, first=10)
+    status = torch.full((1,), 77, dtype=torch.int32, device="cuda")
+    got = run_residual(s3r, c, status=status)
+    assert int(status) == 0
+    for name in got:
+        if got[name].shape[0] == 84:
+            assert torch.isnan(got[name][:10]).all() and torch.isnan(got[name][75:]).all(), name
+            assert torch.equal(got[name][10:75], want[name]), name
+    seq = torch.repeat_interleave(torch.arange(3, device="cuda"), torch.tensor(rows, device="cuda"))
+    ref = residual(whole["x"], whole["f"], "layer", whole["weight"], whole["bias"], 1e-6, "rms", whole["post_weight"], whole["post_bias"], whole["scale"],
+                   whole["gate"], seq, 0.75, whole["d_r"], whole["d_y"], BF16, F32)
+    for name in ("d_weight", "d_bias", "d_post_weight", "d_post_bias", "d_scale", "d_gate"):
+        check(name, got[name], ref[name])
+    for broken in ([50, 10, 60, 84], [-3, 10, 20, 84], [0, 20, 10, 2 ** 30], [2 ** 31 - 1, 0, 5, -7]):
+        c["row_start"] = torch.tensor(broken, dtype=torch.int32, device="cuda")
+        run_residual(s3r, c, status=status)
+        assert int(status) == s3r.S3R_DIAG_SPANS
+
+
+def test_residual_in_place_strides_and_gates_of_a_wider_tensor(s3r):
+    n, width, rows = 60, 520, [31, 29]
+    c = residual_case(8, n, width, rows=rows)
+    want = run_residual(s3r, c, gradient=False)
+    wide_x, wide_f, wide_gate = nan(n, 3 * width, dtype=BF16), nan(n, 2 * width, dtype=BF16), nan(2, 6 * width, dtype=BF16)
+    wide_x[:, width:2 * width], wide_f[:, :width], wide_gate[:, 5 * width:] = c["x"], c["f"], c["gate"]
+    strided = {**c, "x": wide_x[:, width:2 * width], "f": wide_f[:, :width], "gate": wide_gate[:, 5 * width:]}
+    got = run_residual(s3r, strided, gradient=False)
+    assert torch.equal(got["r"], want["r"]) and torch.equal(got["y"], want["y"])
+    grads, strided_grads = run_residual(s3r, c), run_residual(s3r, strided)
+    assert all(torch.equal(grads[name], strided_grads[name]) for name in grads)
+    x, y = c["x"].clone(), nan_like(c["f"])
+    s3r.speed3r_residual_norm(x, y, r=x, bias=c["bias"], eps=1e-6, residual_scale=0.75, **{name: c[name] for name in CALL})
+    assert torch.equal(x, want["r"]) and torch.equal(y, want["y"])
+
+
+def test_residual_without_rows(s3r):
+    c = residual_case(9, 0, 64, rows=[0, 0], post="rms")
+    for name, t in run_residual(s3r, c).items():
+        assert not torch.isnan(t).any() and float(t.float().abs().sum()) == 0, name
+
+
+@pytest.mark.parametrize("width", [64, 1024, 4096])
+def test_residual_nan_stays_in_its_row(s3r, width):
+    c = residual_case(10, 50, width, rows=[20, 30], post="layer")
+    bad = {**c, "x": c["x"].clone(), "f": c["f"].clone()}
+    bad["x"][7, 3], bad["f"][33, 5] = math.nan, math.inf
+    want, got = run_residual(s3r, c), run_residual(s3r, bad)
+    keep = [i for i in range(50) if i not in (7, 33)]
+    for name in ("r", "y", "dx", "df"):
+        assert torch.equal(got[name][keep], want[name][keep]), name
+    assert torch.isnan(got["y"][[7, 33]].float()).all() and torch.isnan(got["r"][33].float()).all()
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+def test_residual_constant_tiny_large_and_shifted_rows(s3r, types, norm):
+    c = residual_case(11, 8, 1024, *types, norm=norm, f=False)
+    x = c["x"]
+    x[0], x[1], x[2], x[3], x[4] = 0.0, 2.5, x[2] * 2.0 ** -70, x[3] * 2.0 ** 50, x[4] + 500.0
+    x[5, 100] = 3000.0
+    compare_residual(run_residual(s3r, c), c)
+    c = residual_case(12, 8, 1024, *types, norm=norm, post=norm)
+    f = c["f"]
+    f[0], f[1], f[2], f[3] = 0.0, 2.5, f[2] * 2.0 ** -70, f[3] + 500.0
+    compare_residual(run_residual(s3r, c, eps=1e-5), c, eps=1e-5)
+
+
+def test_residual_far_rows(s3r):
+    """Rows past 2^32 bytes."""
+    n, width, stride = 50, 64, (5 << 30) // (2 * 50) // 8 * 8
+    c = residual_case(13, n, width)
+    room = torch.zeros(n * stride, dtype=BF16, device="cuda")
+    far = {**c}
+    for i, name in enumerate(("x", "f")):
+        far[name] = room.as_strided((n, width), (stride, 1), 64 * i)
+        far[name].copy_(c[name])
+    want, got = run_residual(s3r, c), run_residual(s3r, far)
+    assert all(torch.equal(got[name], want[name]) for name in want)
+
+
+def test_residual_many_elements(s3r):
+    n, width = (1 << 31) // 8192 + 100, 8192
+    x, f = torch.zeros((n, width), dtype=BF16, device="cuda"), torch.zeros((n, width), dtype=BF16, device="cuda")
+    c = residual_case(14, 30, width, norm="rms", bias=False)
+    x[-30:], f[-30:] = c["x"], c["f"]
+    r, y = torch.empty_like(x), torch.empty_like(x)
+    s3r.speed3r_residual_norm(x, y, f=f, r=r, norm="rms", weight=c["weight"], scale=c["scale"], residual_scale=0.75)
+    compare_residual({"r": r[-30:], "y": y[-30:]}, c)
+
+
+# ---- how the calls are made -----------------------------------------------------------------------------------------
+
+def test_calls_repeat_overlap_and_replay(s3r):
+    """The same bits on every call, on two streams at once, and when replayed from a graph with other contents, between eager calls."""
+    a, b = rotary_case(20, 3000, 4, 2, BF16, (16, 16), "layer"), residual_case(21, 3000, 1024, rows=[1000, 1500, 500], post="rms")
+    want_a, want_b = run_rotary(s3r, a, (16, 16), "halves", "layer"), run_residual(s3r, b)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        got = []
+        for i, s in enumerate(streams):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                got.append((run_rotary(s3r, a, (16, 16), "halves", "layer"), run_residual(s3r, b)))
+        torch.cuda.synchronize()
+        for ra, rb in got:
+            assert all(torch.equal(ra[n], want_a[n]) for n in want_a) and all(torch.equal(rb[n], want_b[n]) for n in want_b)
+
+    names = ("q_weight", "k_weight")
+    out_a = {n: torch.zeros_like(want_a[n]) for n in want_a}
+    out_b = {n: torch.zeros_like(want_b[n]) for n in want_b}
+
+    def step():
+        how = dict(axis_pairs=(16, 16), norm="layer", **{n: a[n] for n in names})
+        s3r.speed3r_rotary(a["q"], a["k"], out_a["q_out"], out_a["k_out"], a["cos"], a["sin"], a["positions"], q_bias=a["q_bias"], k_bias=a["k_bias"], **how)
+        s3r.speed3r_rotary_backward(a["q"], a["k"], a["d_q"], a["d_k"], out_a["dq"], out_a["dk"], a["cos"], a["sin"], a["positions"],
+                                    **{n: out_a[n] for n in ("dq_weight", "dq_bias", "dk_weight", "dk_bias")}, **how)
+        how = {**{n: b[n] for n in CALL}, "residual_scale": 0.75}
+        s3r.speed3r_residual_norm(b["x"], out_b["y"], r=out_b["r"], bias=b["bias"], **how)
+        s3r.speed3r_residual_norm_backward(b["x"], b["d_y"], out_b["dx"], d_r=b["d_r"], df=out_b["df"],
+                                           **{n: out_b[n] for n in out_b if n.startswith("d_")}, **how)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for turn in range(4):
+        g = gen(100 + turn)
+        for t in (a["q"], a["d_k"], b["x"], b["f"], b["d_y"], b["gate"]):
+            t.copy_(normal(g, *t.shape, dtype=t.dtype))
+        b["row_start"].copy_(starts([[1000, 1500, 500], [0, 3000, 0], [1, 2, 2997], [2000, 0, 1000]][turn]))
+        for t in (*out_a.values(), *out_b.values()):
+            t.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        want_a, want_b = run_rotary(s3r, a, (16, 16), "halves", "layer"), run_residual(s3r, b)
+        assert all(torch.equal(out_a[n], want_a[n]) for n in want_a), turn
+        assert all(torch.equal(out_b[n], want_b[n]) for n in want_b), turn
+
+
+def test_a_workspace_of_the_callers_and_its_refusal(s3r):
+    c = rotary_case(22, 100, 2, 2, BF16, (32,), "rms")
+    dq, dk, dw = nan_like(c["q"]), nan_like(c["k"]), nan_like(c["q_weight"])
+    args = (c["q"], c["k"], c["d_q"], c["d_k"], dq, dk, c["cos"], c["sin"], c["positions"])
+    how = dict(norm="rms", q_weight=c["q_weight"], k_weight=c["k_weight"], dq_weight=dw)
+    ws = s3r.speed3r_rotary_backward(*args, **how)
+    assert ws.numel() > 0 and s3r.speed3r_rotary_backward(*args, workspace=ws, **how) is ws
+    with pytest.raises(s3r.Speed3rError) as e:
+        s3r.speed3r_rotary_backward(*args, workspace=ws[:256], **how)
+    assert e.value.status == s3r.S3R_ERR_WORKSPACE
+    assert s3r.speed3r_rotary_backward(*args, norm="rms", q_weight=c["q_weight"], k_weight=c["k_weight"]) is None
+    with pytest.raises(TypeError, match="dtype"):
+        s3r.speed3r_rotary(c["q"], c["k"], dq, dk, c["cos"], c["sin"], c["positions"], norm="rms", q_weight=c["q_weight"], k_weight=c["k_weight"].bfloat16())
+    with pytest.raises(ValueError, match="shape"):
+        s3r.speed3r_rotary(c["q"], c["k"], dq, dk, c["cos"], c["sin"], c["positions"], axis_pairs=(16, 8))
+    with pytest.raises(TypeError, match="broadcast"):
+        s3r.speed3r_rotary(c["q"][:1].expand(100, 2, 64), c["k"], dq, dk, c["cos"], c["sin"], c["positions"])
