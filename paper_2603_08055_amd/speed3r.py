@@ -704,6 +704,14 @@ def speed3r_rotary(q, k, q_out, k_out, cos=None, sin=None, positions=None, *, ax
     _call(lib.speed3r_rotary, p, 0, None, index)
 
 
+def speed3r_rotary_workspace_bytes(weight_gradients=True) -> int:
+    """Bytes of workspace of speed3r_rotary_backward, with gradients of weights or without (the same for all shapes)."""
+    p = s3r_rotary_params()
+    p.heads, p.head_dim, p.norm, p.eps, p.dtype = 1, HEAD_DIM, S3R_NORM_RMS, 1.0, S3R_BF16
+    p.dq_weight = 16 if weight_gradients else None                   # only whether it is given counts here
+    return load().speed3r_rotary_workspace_bytes(ctypes.byref(p))
+
+
 def speed3r_rotary_backward(q, k, d_q_out, d_k_out, dq, dk, cos=None, sin=None, positions=None, *, axis_pairs=None, pairs="halves",
                             norm=None, eps=1e-6, q_weight=None, k_weight=None, dq_weight=None, dq_bias=None, dk_weight=None,
                             dk_bias=None, workspace=None, status=None, stream=None):
@@ -792,6 +800,18 @@ def speed3r_residual_norm(x, y=None, *, f=None, r=None, norm=None, weight=None, 
     if y is not None:
         p.y = _arg(y, "y", index, y.dtype if f is None else f.dtype, x.shape)
     _call(lib.speed3r_residual_norm, p, 0, None, index)
+
+
+def speed3r_residual_workspace_bytes(n_rows, width, *, batch=1, weight_gradients=True, gate_gradients=False) -> int:
+    """Bytes of workspace of speed3r_residual_norm_backward; weight_gradients: of any of weights, biases and scale."""
+    p = s3r_residual_params()
+    p.n_rows, p.width, p.batch, p.norm, p.eps = n_rows, width, batch, S3R_NORM_RMS, 1.0
+    p.f = p.gate = p.row_start = 16                                  # only whether they are given counts here
+    p.d_weight, p.d_gate = 16 if weight_gradients else None, 16 if gate_gradients else None
+    need = load().speed3r_residual_workspace_bytes(ctypes.byref(p))
+    if need >= 1 << 62:
+        raise Speed3rError(S3R_ERR_INVALID_ARG, speed3r_last_error())
+    return need
 
 
 def speed3r_residual_norm_backward(x, d_y, dx, *, f=None, d_r=None, df=None, norm=None, weight=None, eps=1e-6, post_norm=None,

@@ -157,6 +157,14 @@ def test_workspaces_and_null_parameters(s3r):
     assert 0 < lib.speed3r_residual_workspace_bytes(ctypes.byref(residual_params(s3r, n_rows=1 << 28, width=8192))) < 1 << 30
 
 
+def test_workspaces_by_the_binding(s3r):
+    assert s3r.speed3r_rotary_workspace_bytes(False) == 0 < s3r.speed3r_rotary_workspace_bytes()
+    plain, gates = s3r.speed3r_residual_workspace_bytes(1000, 512), s3r.speed3r_residual_workspace_bytes(1000, 512, batch=7, gate_gradients=True)
+    assert 0 < plain < gates and s3r.speed3r_residual_workspace_bytes(1000, 512, weight_gradients=False) == 0
+    with pytest.raises(s3r.Speed3rError, match="width"):
+        s3r.speed3r_residual_workspace_bytes(10, 12)
+
+
 def test_the_binding_refuses(s3r):
     x = torch.zeros((4, 2, 64))
     with pytest.raises(TypeError, match="GPU"):
