@@ -295,6 +295,16 @@ size_t speed3r_cross_workspace_bytes(const s3r_cross_params *p, int backward);
 s3r_status speed3r_cross_attn(const s3r_cross_params *p);
 s3r_status speed3r_cross_attn_backward(const s3r_cross_params *p);
 
+/* The same over packed sequences whose rows are their LAST tokens (of n rows and m keys, row i is token m - n + i; all m are those of the
+ * sequence, n = m: a prompt over itself, n < m: new tokens over earlier ones): a row sees the tokens of its own view of tokens_per_view
+ * tokens and of the views before.  tokens_per_view 1: causal by token, up to the row itself; a view's tokens see one another otherwise, as views that arrive
+ * one after another do.  Everything else, p's fields, masks, broken lists, workspaces and arithmetic, is as above.  A row before the first key (n > m)
+ * sees none.  What stands in k and v of tokens that a row does not see, or in q and d_out of rows that do not see a key, does not matter to
+ * it, infinities and NaN included. */
+size_t speed3r_causal_workspace_bytes(const s3r_cross_params *p, int tokens_per_view, int backward);
+s3r_status speed3r_causal_attn(const s3r_cross_params *p, int tokens_per_view);
+s3r_status speed3r_causal_attn_backward(const s3r_cross_params *p, int tokens_per_view);
+
 /* ---- a cache of keys and values in 4 bits ------------------------------------------------------ */
 
 /* Views (or tokens) that arrive one after another: keys and values of earlier rows are kept in pages, 34 bytes for the 64 channels of a

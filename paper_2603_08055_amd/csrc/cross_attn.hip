@@ -25,15 +25,50 @@ __device__ __forceinline__ CountedRows counted(const CrossArgs &a, int first, in
     return CountedRows{a.key_mask != nullptr ? a.key_mask + first : nullptr, len, 0};
 }
 
+// Causal rows: the n rows of a sequence are its last tokens of m, and each sees the tokens of its own view of `view` tokens and of those
+// before (view 1: the tokens up to itself).  Keys that row i sees, and the first row that sees a key.
+__device__ __forceinline__ int keys_seen(int i, int n, int m, int view)
+{
+    const int t = m - n + i;
+    return t < 0 ? 0 : (view == 1 ? t + 1 : min(m, (t / view + 1) * view));
+}
+__device__ __forceinline__ int first_seer(int key, int n, int m, int view) { return max(0, (view == 1 ? key : key / view * view) - (m - n)); }
+
+// Keys that the last of a tile's items sees; `items`: of the sequence.
+__device__ __forceinline__ int tile_sees(int64_t end, int64_t items, int per_row, int n, int m, int view)
+{
+    return keys_seen(static_cast<int>((end < items ? end : items) - 1) / per_row, n, m, view);
+}
+
+// What a tile of kTile items, a wave of it and the lane's row see; `tile` keys are walked.  Without CAUSAL: all.
+template <bool CAUSAL> struct CausalTile {
+    int tile, mine, wave, all;  // all: keys that all of the tile's rows see
+    __device__ __forceinline__ CausalTile(const CrossArgs &a, int t, int n, int m, int64_t item, bool ok, int w) : tile(m), mine(m), wave(m), all(m)
+    {
+        if constexpr (CAUSAL) {
+            const int64_t items = static_cast<int64_t>(n) * a.per_row, item0 = static_cast<int64_t>(t) * kTile + 32 * w;
+            tile = tile_sees(static_cast<int64_t>(t + 1) * kTile, items, a.per_row, n, m, a.view);
+            wave = __builtin_amdgcn_readfirstlane(item0 < items ? tile_sees(item0 + 32, items, a.per_row, n, m, a.view) : 0);
+            mine = ok ? keys_seen(static_cast<int>(item) / a.per_row, n, m, a.view) : wave;
+            all = keys_seen(t * kTile / a.per_row, n, m, a.view);
+        }
+    }
+    __device__ __forceinline__ bool sees(int unit) const { return !CAUSAL || unit * kUnitRows < wave; }
+    __device__ __forceinline__ unsigned long long of(unsigned long long seen, int unit) const
+    {
+        return CAUSAL ? seen & low_bits(mine - unit * kUnitRows) : seen;
+    }
+};
+
 // Many rows: four waves hold 32 rows each and share every unit.
-template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) void cross_kernel(CrossArgs a)
+template <typename T, bool CAUSAL> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) void cross_kernel(CrossArgs a)
 {
     constexpr int P = UnitPairs<T>::kParts;
     extern __shared__ __align__(16) unsigned char smem[];
     bf16_t *lds = reinterpret_cast<bf16_t *>(smem);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Share sh;
-    if (!find_share(a.q_spans, nullptr, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, !a.uneven, true, sh)) return;
+    if (!find_share(a.q_spans, nullptr, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, !CAUSAL && !a.uneven, !CAUSAL, sh)) return;
     const int q0 = sh.of.first, q_len = sh.of.len;
     int k0, k_len;
     a.kv_spans.of(sh.of.seq, k0, k_len);
@@ -41,8 +76,9 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) 
     const bool ok = item < static_cast<int64_t>(q_len) * a.per_row;
     const int64_t row = q0 + item / a.per_row;
     const int head = sh.kv_head * a.per_row + static_cast<int>(item % a.per_row);
+    const CausalTile<CAUSAL> sight(a, sh.tile, q_len, k_len, item, ok, wave);
     int u0, u1;
-    piece((k_len + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1);
+    piece((sight.tile + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1);
     if (a.to.part_o != nullptr && u0 == u1) return store_no_keys(a.to, sh.split, row, head, ok && lane < 32);
     SoftRow<P> soft;
     soft.clear();
@@ -54,8 +90,15 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) 
     const UnitLanes at(lane);
     units.begin(u0, u1, more);
     for (int u = u0; u < u1; ++u) {
-        const bf16_t *k = units.step(u, u == u0, more, [&]() { return seen = rows.counts(); }, [](int) {});
-        soft.template unit<P>(k, k + P * kPlane, seen, a.factor, at, lane);
+        bf16_t *k = units.step(u, u == u0, more, [&]() { return seen = rows.counts(); }, [](int) {});
+        if constexpr (CAUSAL)
+            if ((u + 1) * kUnitRows > sight.all && unit_is_wild(k + P * kPlane, lane)) {  // (all waves find the same)
+                add_wild(soft.o, k + P * kPlane, sight.of(seen, u), lane);
+                lds_barrier();
+                tame_unit(k + P * kPlane, threadIdx.x);
+                lds_barrier();
+            }
+        if (sight.sees(u)) soft.template unit<P, CAUSAL>(k, k + P * kPlane, sight.of(seen, u), a.factor, at, lane);
     }
     store_soft<T>(soft, a.factor, a.to, sh.split, row, head, ok, lane);
 }
@@ -65,7 +108,7 @@ template <typename T> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) 
 template <typename T> constexpr int kFewParts = sizeof(T) == 4 ? 3 : 2;
 
 // Few rows: WAVES waves with the same 16 rows take the units in turn, values through an LDS stage of their own (8 or 24 KiB).
-template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 || WAVES > 4 ? 1 : 2) void cross_few_kernel(CrossArgs a)
+template <typename T, int WAVES, bool CAUSAL> __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 || WAVES > 4 ? 1 : 2) void cross_few_kernel(CrossArgs a)
 {
     constexpr int P = UnitPairs<T>::kParts;
     extern __shared__ __align__(16) unsigned char smem[];
@@ -80,8 +123,13 @@ template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, sizeof
     const bool ok = item < static_cast<int64_t>(q_len) * a.per_row;
     const int64_t row = q0 + item / a.per_row;
     const int head = sh.kv_head * a.per_row + static_cast<int>(item % a.per_row);
+    int sees = k_len, walked = k_len;
+    if constexpr (CAUSAL) {
+        walked = tile_sees(static_cast<int64_t>(sh.tile + 1) * kFewRows, static_cast<int64_t>(q_len) * a.per_row, a.per_row, q_len, k_len, a.view);
+        sees = ok ? keys_seen(static_cast<int>(item) / a.per_row, q_len, k_len, a.view) : walked;
+    }
     int u0, u1;
-    piece((k_len + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1);
+    piece((walked + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1);
     if (a.to.part_o != nullptr && u0 == u1) return store_no_keys(a.to, sh.split, row, head, ok && threadIdx.x < 16);
     FewRows<P> few;
     few.clear();
@@ -119,10 +167,10 @@ template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES, sizeof
             }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         if (u + WAVES < u1) fetch(u + WAVES);
-        few.template unit<P, kFewParts<T>>([&](int t, int s, bf16x8(&to)[P]) {
+        few.template unit<P, kFewParts<T>, CAUSAL>([&](int t, int s, bf16x8(&to)[P]) {
 #pragma unroll
             for (int i = 0; i < P; ++i) to[i] = kk[t][s][i];
-        }, mine, seen, a.factor, lane);
+        }, mine, CAUSAL ? seen & low_bits(sees - u * kUnitRows) : seen, a.factor, lane);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
     __syncthreads();
@@ -213,14 +261,14 @@ __device__ __forceinline__ float sum8(const bf16x8 &x)
 }
 
 // PX: bf16 parts in which dS enters its product.
-template <typename T, int PX> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void grad_q_kernel(CrossArgs a)
+template <typename T, int PX, bool CAUSAL> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void grad_q_kernel(CrossArgs a)
 {
     constexpr int P = UnitPairs<T>::kParts;
     extern __shared__ __align__(16) unsigned char smem[];
     bf16_t *lds = reinterpret_cast<bf16_t *>(smem);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Share sh;
-    if (!find_share(a.q_spans, nullptr, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, !a.uneven, true, sh)) return;
+    if (!find_share(a.q_spans, nullptr, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, !CAUSAL && !a.uneven, !CAUSAL, sh)) return;
     const int q0 = sh.of.first, q_len = sh.of.len;
     int k0, k_len;
     a.kv_spans.of(sh.of.seq, k0, k_len);
@@ -228,8 +276,9 @@ template <typename T, int PX> __global__ __launch_bounds__(256, sizeof(T) == 4 ?
     const bool ok = item < static_cast<int64_t>(q_len) * a.per_row;
     const int64_t row = q0 + item / a.per_row;
     const int head = sh.kv_head * a.per_row + static_cast<int>(item % a.per_row);
+    const CausalTile<CAUSAL> sight(a, sh.tile, q_len, k_len, item, ok, wave);
     int u0, u1;
-    piece((k_len + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1);
+    piece((sight.tile + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1);
     if (sh.split > 0 && u0 == u1) return;
     SoftRow<P> held, grad;  // q, and d_out; held.o: P k, grad.o: the gradient
     held.clear();
@@ -267,6 +316,9 @@ template <typename T, int PX> __global__ __launch_bounds__(256, sizeof(T) == 4 ?
     units.begin(u0, u1, more);
     for (int u = u0; u < u1; ++u) {
         const bf16_t *k = units.step(u, u == u0, more, [&]() { return seen = rows.counts(); }, [](int) {}), *v = k + P * kPlane;
+        if (!sight.sees(u)) continue;
+        seen = sight.of(seen, u);
+        const bool some = CAUSAL ? __any(seen != ~0ull) : seen != ~0ull, wild = CAUSAL && some && unit_is_wild(k, lane);
         // dP - D comes out of the product itself where it starts at -D
         RowOperands<P> kr, vr;
         kr.read(k, 0, at);
@@ -284,12 +336,13 @@ template <typename T, int PX> __global__ __launch_bounds__(256, sizeof(T) == 4 ?
             }
             ChannelOperands<P> kt;
             kt.read(k, half, at);
+            if (CAUSAL && wild) kt.tame_all();
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 s[r] = fast_exp2(fmaf(s[r], a.factor, -l2));
                 dp[r] *= s[r];
             }
-            if (seen != ~0ull) {
+            if (some) {
                 const uint32_t out = left_out(seen, half, lane);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
@@ -321,6 +374,7 @@ template <typename T, int PX> __global__ __launch_bounds__(256, sizeof(T) == 4 ?
                 }
             }
         }
+        if (CAUSAL && wild) add_wild(grad.o, k, seen, lane);
     }
     const int64_t to = row * a.heads + head, part = sh.split * a.n_q * a.heads + to;
     if constexpr (kMendD<T>) {
@@ -353,6 +407,35 @@ __device__ __forceinline__ int pieces_of(const Spans &streamed, int seq, int per
     return (units + per - 1) / per;
 }
 
+// The same for causal rows, whose tiles walk as many units as they see: for a row and head of the queries, and for a key.
+__device__ __forceinline__ int causal_pieces_q(const CrossArgs &a, int64_t row, int head)
+{
+    const int seq = a.q_spans.find(row);
+    int q0, q_len, k0, k_len;
+    a.q_spans.of(seq, q0, q_len);
+    a.kv_spans.of(seq, k0, k_len);
+    const int64_t item = (row - q0) * a.per_row + head % a.per_row, items = static_cast<int64_t>(q_len) * a.per_row;
+    const int units = (tile_sees((item / kTile + 1) * kTile, items, a.per_row, q_len, k_len, a.view) + kUnitRows - 1) / kUnitRows;
+    const int per = piece_units(units, a.n_split, a.least);
+    return (units + per - 1) / per;
+}
+// Units of a tile of keys: those from the first that sees its first key.
+__device__ __forceinline__ void seeing_units(const CrossArgs &a, int tile, int q_len, int k_len, int &from, int &end)
+{
+    end = (q_len * a.per_row + kUnitRows - 1) / kUnitRows;
+    from = min(end, first_seer(tile * kTile, q_len, k_len, a.view) * a.per_row / kUnitRows);
+}
+__device__ __forceinline__ int causal_pieces_kv(const CrossArgs &a, int64_t row)
+{
+    const int seq = a.kv_spans.find(row);
+    int q0, q_len, k0, k_len, from, end;
+    a.q_spans.of(seq, q0, q_len);
+    a.kv_spans.of(seq, k0, k_len);
+    seeing_units(a, static_cast<int>(row - k0) / kTile, q_len, k_len, from, end);
+    const int per = piece_units(end - from, a.n_split, a.least);
+    return (end - from + per - 1) / per;
+}
+
 // The query gradient from its pieces over keys.  16 threads for a row of a head.
 template <typename T> __global__ __launch_bounds__(256) void grad_q_combine_kernel(CrossArgs a)
 {
@@ -363,7 +446,7 @@ template <typename T> __global__ __launch_bounds__(256) void grad_q_combine_kern
     const int c = static_cast<int>(i & 15) * 4;
     floatx4 g = {0.f, 0.f, 0.f, 0.f}, pk = {0.f, 0.f, 0.f, 0.f};
     float sum = 0.f, entered = 0.f;
-    const int n = pieces_of(a.kv_spans, a.q_spans.find(row), 1, a);
+    const int n = a.view > 0 ? causal_pieces_q(a, row, static_cast<int>(at - row * a.heads)) : pieces_of(a.kv_spans, a.q_spans.find(row), 1, a);
     for (int j = 0; j < n; ++j) {
         g += *reinterpret_cast<const floatx4 *>(a.part_q + (j * share + at) * 64 + c);
         if constexpr (kMendD<T>) {
@@ -379,7 +462,7 @@ template <typename T> __global__ __launch_bounds__(256) void grad_q_combine_kern
 }
 
 // PX: bf16 parts in which probabilities and dS enter the products.
-template <typename T, int PX> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void grad_kv_kernel(CrossArgs a)
+template <typename T, int PX, bool CAUSAL> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void grad_kv_kernel(CrossArgs a)
 {
     constexpr int P = UnitPairs<T>::kParts;
     extern __shared__ __align__(16) unsigned char smem[];
@@ -395,8 +478,18 @@ template <typename T, int PX> __global__ __launch_bounds__(256, sizeof(T) == 4 ?
     const bool ok = key < k_len, seen = ok && (a.key_mask == nullptr || a.key_mask[k0 + key] != 0);
     const int64_t row = k0 + key;
     const int items = q_len * a.per_row, head0 = sh.kv_head * a.per_row;
-    int u0, u1;
-    piece((items + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1);
+    int u0, u1, from = 0, wave_from = 0;  // causal: the first item that sees the lane's key, and the wave's first
+    if constexpr (CAUSAL) {
+        int begin, end;
+        seeing_units(a, sh.tile, q_len, k_len, begin, end);
+        piece(end - begin, a.n_split, a.least, sh.split, u0, u1);
+        u0 += begin;
+        u1 += begin;
+        from = first_seer(key, q_len, k_len, a.view) * a.per_row;
+        wave_from = __builtin_amdgcn_readfirstlane(from);
+    } else {
+        piece((items + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1);
+    }
     if (sh.split > 0 && u0 == u1) return;
     SoftRow<P> kk, vv;  // k and v; .o: their gradients
     kk.clear();
@@ -426,6 +519,14 @@ template <typename T, int PX> __global__ __launch_bounds__(256, sizeof(T) == 4 ?
             if (which < 2) to[which * 64 + lane] = st;
             stats = to;
         }), *g = q + P * kPlane;
+        unsigned long long items_seen = ~0ull;
+        bool some = false, wild = false;
+        if constexpr (CAUSAL) {
+            if ((u + 1) * kUnitRows <= wave_from) continue;
+            items_seen = ~low_bits(from - u * kUnitRows);
+            some = __any(items_seen != ~0ull);
+            wild = some && (unit_is_wild(q, lane) || unit_is_wild(g, lane));
+        }
         RowOperands<P> qr, gr;
         qr.read(q, 0, at);
         gr.read(g, 0, at);
@@ -449,6 +550,11 @@ template <typename T, int PX> __global__ __launch_bounds__(256, sizeof(T) == 4 ?
             ChannelOperands<P> qt, gt;
             gt.read(g, half, at);
             qt.read(q, half, at);
+            if (CAUSAL && wild) {
+                gt.tame_all();
+                qt.tame_all();
+            }
+            const uint32_t out = CAUSAL && some ? left_out(items_seen, half, lane) : 0u;
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
                 float x[8], y[8];
@@ -463,6 +569,12 @@ template <typename T, int PX> __global__ __launch_bounds__(256, sizeof(T) == 4 ?
                         y[4 * b + e] = x[4 * b + e] * dp[r];
                     }
                 }
+                if (CAUSAL && some)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        x[j] = replace(x[j], 0.f, left_out_mask(out, 8 * w + j));
+                        y[j] = replace(y[j], 0.f, left_out_mask(out, 8 * w + j));
+                    }
                 bf16x8 p[PX], ds[PX];
                 split_parts<PX>(x, p);
                 split_parts<PX>(y, ds);
@@ -472,6 +584,11 @@ template <typename T, int PX> __global__ __launch_bounds__(256, sizeof(T) == 4 ?
                     multiply<P>(kk.o[dt], ds, [&](int part) { return qt.x[w][dt][part]; });
                 }
             }
+        }
+        if (CAUSAL && wild) {
+            add_wild(vv.o, g, items_seen, lane);
+            add_wild(kk.o, q, items_seen, lane);
+            add_wild(kk.o, g, items_seen, lane);
         }
     }
     if (!seen)  // a masked key gets no gradient, whatever its lanes added up
@@ -495,7 +612,8 @@ template <typename T> __global__ __launch_bounds__(256) void grad_kv_combine_ker
     const float *part = blockIdx.y == 0 ? a.part_k : a.part_v;
     T *out = static_cast<T *>(blockIdx.y == 0 ? a.dk : a.dv);
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    const int pieces = pieces_of(a.q_spans, a.kv_spans.find(i / (a.kv_heads * 16)), a.per_row, a);
+    const int64_t row = i / (a.kv_heads * 16);
+    const int pieces = a.view > 0 ? causal_pieces_kv(a, row) : pieces_of(a.q_spans, a.kv_spans.find(row), a.per_row, a);
     for (int j = 0; j < pieces; ++j) acc += *reinterpret_cast<const floatx4 *>(part + (j * n + i) * 4);
 #pragma unroll
     for (int e = 0; e < 4; ++e) out[i * 4 + e] = from_float<T>(acc[e]);
@@ -511,9 +629,10 @@ __global__ __launch_bounds__(1024) void span_status_kernel(Spans q, Spans kv, in
 template <typename T, int WAVES> hipError_t launch_few(const CrossArgs &a, int64_t n, hipStream_t stream)
 {
     constexpr size_t kLds = WAVES * UnitPairs<T>::kParts * kPlane * sizeof(bf16_t);
-    const hipError_t e = allow_lds(&cross_few_kernel<T, WAVES>, kLds);
+    auto kernel = a.view > 0 ? &cross_few_kernel<T, WAVES, true> : &cross_few_kernel<T, WAVES, false>;
+    const hipError_t e = allow_lds(kernel, kLds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((cross_few_kernel<T, WAVES>), dim3(static_cast<unsigned>(n)), dim3(64 * WAVES), kLds, stream, a);
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(n)), dim3(64 * WAVES), kLds, stream, a);
     return hipGetLastError();
 }
 
@@ -527,7 +646,8 @@ template <typename T> hipError_t launch_cross_t(const CrossArgs &a, bool few_row
         return launch_few<T, 4>(a, n, stream);
     } else {
         constexpr size_t kLds = UnitPairs<T>::kStages * UnitPairs<T>::kStage * sizeof(bf16_t);
-        hipLaunchKernelGGL(cross_kernel<T>, dim3(static_cast<unsigned>(n)), dim3(256), kLds, stream, a);
+        auto kernel = a.view > 0 ? &cross_kernel<T, true> : &cross_kernel<T, false>;
+        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(n)), dim3(256), kLds, stream, a);
     }
     return hipGetLastError();
 }
@@ -538,14 +658,19 @@ template <typename T> hipError_t launch_cross_t(const CrossArgs &a, bool few_row
 // keys 55 / 60, 64 over 2000 24.8 / 26.6, 2748 over 10992 588 / 795, 8192 over 8192 1129 / 1554; dk and dv alone: 128 over 10992 71 / 80, 512 over
 // 10992 137 / 163.
 constexpr int kFewItems = kUnitRows;
+template <typename T, int PX> auto grad_kernel(bool of_keys, bool causal)
+{
+    return of_keys ? (causal ? &grad_kv_kernel<T, PX, true> : &grad_kv_kernel<T, PX, false>)
+                   : (causal ? &grad_q_kernel<T, PX, true> : &grad_q_kernel<T, PX, false>);
+}
 template <typename T> hipError_t launch_grad_t(const CrossArgs &a, bool of_keys, hipStream_t stream)
 {
     const int64_t n = xcd_padded(a.tiles * a.n_split * a.kv_heads);
     if (!grid_ok(n)) return hipErrorInvalidValue;
     const size_t lds = UnitPairs<T>::kStages * (UnitPairs<T>::kStage * sizeof(bf16_t) + (of_keys ? 128 * sizeof(float) : 0));
-    auto kernel = of_keys ? &grad_kv_kernel<T, UnitPairs<T>::kParts> : &grad_q_kernel<T, UnitPairs<T>::kParts>;
+    auto kernel = grad_kernel<T, UnitPairs<T>::kParts>(of_keys, a.view > 0);
     if constexpr (sizeof(T) == 2)
-        if (a.n_q * a.per_row <= kFewItems * a.q_spans.batch) kernel = of_keys ? &grad_kv_kernel<T, 2> : &grad_q_kernel<T, 2>;
+        if (a.n_q * a.per_row <= kFewItems * a.q_spans.batch) kernel = grad_kernel<T, 2>(of_keys, a.view > 0);
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(n)), dim3(256), lds, stream, a);
     return hipGetLastError();
 }

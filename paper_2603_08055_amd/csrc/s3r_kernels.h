@@ -288,6 +288,7 @@ struct CrossArgs {
     int64_t n_q, n_kv, tiles;
     int heads, kv_heads, per_row, n_split, least;
     bool uneven;  // sequences of several lengths, or causal rows
+    int view;     // causal rows: tokens of a view, else 0
     float scale, factor;
     SoftOut to;
     float *stats;

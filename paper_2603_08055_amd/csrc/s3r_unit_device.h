@@ -86,6 +86,16 @@ template <int PS> struct RowOperands {
     }
 };
 
+// An infinity or NaN, and what is left without them (see unit_is_wild).
+__device__ __forceinline__ bool is_wild(bf16_t x) { return (__builtin_bit_cast(unsigned short, x) & 0x7f80) == 0x7f80; }
+__device__ __forceinline__ bf16x8 tame(bf16x8 x)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (is_wild(x[j])) x[j] = static_cast<bf16_t>(0.f);
+    return x;
+}
+
 template <int PS> struct ChannelOperands {
     bf16x8 x[2][2][PS];
     __device__ __forceinline__ void read(const bf16_t *unit, int half, const UnitLanes &at)
@@ -96,6 +106,15 @@ template <int PS> struct ChannelOperands {
             for (int dt = 0; dt < 2; ++dt)
 #pragma unroll
                 for (int part = 0; part < PS; ++part) x[u][dt][part] = unit_channels(unit + part * kPlane, half, u, dt, at);
+    }
+    __device__ __forceinline__ void tame_all()
+    {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+                for (int part = 0; part < PS; ++part) x[u][dt][part] = tame(x[u][dt][part]);
     }
 };
 
@@ -479,6 +498,55 @@ template <bool GROUPED> struct UnitPairs<bf16_t, GROUPED> {
     }
 };
 
+// ---- numbers that are none, in rows that only some of the held rows see -----------------------------------
+// A streamed row that a held row does not see enters their products with a weight of 0, and 0 times an infinity or NaN would be NaN.  Where
+// whole rows are left out they are zeros in LDS; causal rows leave out other rows each.  Units that all of a wave's rows see are as they
+// are; the others (a tile of 128 rows has two or three) are searched, and the rare unit with such numbers is multiplied without them,
+// which are then added to the rows that do see them: what these get is an infinity or NaN in any case.
+// Whether a unit (its upper parts) has such a number: all lanes of a wave look.
+__device__ __forceinline__ bool unit_is_wild(const bf16_t *unit, int lane)
+{
+    unsigned found = 0;
+    lane = opaque(lane);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(unit + (i * 64 + lane) * 8);
+        // (a full exponent, and only that, carries into the sign's place)
+        found |= ((x.x & 0x7f807f80u) + 0x00800080u) | ((x.y & 0x7f807f80u) + 0x00800080u) | ((x.z & 0x7f807f80u) + 0x00800080u) |
+                 ((x.w & 0x7f807f80u) + 0x00800080u);
+    }
+    return __any((found & 0x80008000u) != 0);
+}
+
+// All threads (256) of a workgroup take them out of a unit in LDS (of its upper parts; where those are none, the lower ones are 0).
+__device__ __forceinline__ void tame_unit(bf16_t *unit, int t)
+{
+    t = opaque(t);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        bf16x8 *at = reinterpret_cast<bf16x8 *>(unit + (i * 256 + t) * 8);
+        *at = tame(*at);
+    }
+}
+
+// To a held row's channels (32 dt + acc_row(lane, r)) what is no number in the rows it sees.
+__device__ __forceinline__ void add_wild(floatx16 (&o)[2], const bf16_t *unit, unsigned long long seen, int lane)
+{
+#pragma unroll 1
+    for (int row = 0; row < kUnitRows; ++row) {
+        if (((seen >> row) & 1) == 0) continue;
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const bf16x4 x = *reinterpret_cast<const bf16x4 *>(unit + unit_chunk(row, 4 * dt + b) + 4 * (lane >> 5));
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (is_wild(x[e])) o[dt][4 * b + e] += static_cast<float>(x[e]);
+            }
+    }
+}
+
 // ---- softmax over units -----------------------------------------------------------------------------------
 
 // Which of a half unit's 32 streamed rows, of those in a lane's 16 registers, do not count: bits 8 (r / 4) + r % 4.  Opaque to the
@@ -537,7 +605,8 @@ template <int PQ> struct SoftRow {
     // bf16: probabilities enter the product with v rounded to bf16, as in the library's dense attention.  Two parts would leave of the error of
     // out its own rounding alone (2.2e-3 -> 1.66e-3 against 64 bits, 2748 rows over 10992 keys) and take 24 matrix instructions for a unit in place of 16: us,
     // one part / two, 1374 rows over 27480 keys of 16 heads 203 / 297, 8192 over 8192 317 / 469, over cached tokens of 4 bits 402 / 517.
-    template <int PS>
+    // CAUSAL: o may hold infinities before the first score (add_wild).
+    template <int PS, bool CAUSAL = false>
     __device__ __forceinline__ void unit(const bf16_t *k, const bf16_t *v, unsigned long long seen, float factor, const UnitLanes &at, int lane)
     {
         const bool all = __all(seen == ~0ull);
@@ -569,7 +638,7 @@ template <int PQ> struct SoftRow {
                 for (int r = 0; r < 16; ++r) most = fmaxf(most, s[half][r]);
             most = max_with_other_half(most);
             const float next = fmaxf(top, most);
-            const float w = next == -INFINITY ? 1.f : fast_exp2((top - next) * factor);
+            const float w = (CAUSAL ? top : next) == -INFINITY ? 1.f : fast_exp2((top - next) * factor);
             top = next;
             sum *= w;
 #pragma unroll
@@ -717,7 +786,8 @@ template <int PQ> struct FewRows {
         }
     }
     // key(t, s, parts): the A operand of key tile t, its PS parts; v: PS planes in LDS; PP: parts in which probabilities enter the product
-    template <int PS, int PP, typename Key>
+    // CAUSAL: rows see other keys each (unit_is_wild).
+    template <int PS, int PP, bool CAUSAL = false, typename Key>
     __device__ __forceinline__ void unit(Key &&key, const bf16_t *v, unsigned long long seen, float factor, int lane)
     {
         floatx4 s[4];
@@ -754,6 +824,7 @@ template <int PQ> struct FewRows {
         }
         const float base = top == -INFINITY ? 0.f : top * factor;
         float unit_sum = 0.f;
+        const bool wild = CAUSAL && !__all(seen == ~0ull) && unit_is_wild(v, lane);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             float x[8];
@@ -768,12 +839,26 @@ template <int PQ> struct FewRows {
             for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
                 for (int a = 0; a < PS; ++a) {
-                    const bf16x8 vt = few_channels(v + a * kPlane, ks, ct, lane);
+                    bf16x8 vt = few_channels(v + a * kPlane, ks, ct, lane);
+                    if (CAUSAL && wild) vt = tame(vt);
 #pragma unroll
                     for (int b = 0; b < PP; ++b)
                         if (a + b < 3) o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, p[b], o[ct], 0, 0, 0);
                 }
         }
+        if (CAUSAL && wild)
+#pragma unroll 1
+            for (int row = 0; row < kUnitRows; ++row) {
+                if (((seen >> row) & 1) == 0) continue;
+#pragma unroll
+                for (int ct = 0; ct < 4; ++ct) {
+                    const int c = 16 * ct + 4 * (lane >> 4);
+                    const bf16x4 x = *reinterpret_cast<const bf16x4 *>(v + unit_chunk(row, c >> 3) + (c & 7));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (is_wild(x[e])) o[ct][e] += static_cast<float>(x[e]);
+                }
+            }
         sum += unit_sum;
     }
 };

@@ -1096,7 +1096,8 @@ struct CrossPlan {
     size_t stats, part_q, part_pk, part_sum, part_k, part_v, backward;     // of the gradient
 };
 
-s3r_status plan_cross(const s3r_cross_params *p, CrossPlan *out)
+// view: tokens of a view whose rows see those of their own and of earlier ones, 0: all rows see all keys.
+s3r_status plan_cross(const s3r_cross_params *p, int view, CrossPlan *out)
 {
     if (!p) return fail(S3R_ERR_INVALID_ARG, "params is null");
     s3r_status st = check_heads(p->heads, p->kv_heads, p->head_dim, p->dtype);
@@ -1113,12 +1114,14 @@ s3r_status plan_cross(const s3r_cross_params *p, CrossPlan *out)
     st = check_batch(c.batch, p->kv_heads);
     if (st != S3R_OK) return st;
     const int bf16 = p->dtype == S3R_BF16;
-    const bool uneven = c.batch > 1;
+    const bool uneven = c.batch > 1 || view > 0;
     // (the longest of several sequences counts, and only their sum is known: four times their mean, if there is that much)
     auto units_of = [&](int64_t rows) { return ((uneven ? (4 * rows / c.batch < rows ? 4 * rows / c.batch : rows) : rows) + 63) / 64; };
     auto split_of = [&](int64_t tiles, int64_t held, int per_row, int64_t streamed, const Pace &pace, double part_bytes) {
         if (!uneven) return pieces(tiles * p->kv_heads, units_of(streamed), pace, part_bytes);
-        return pieces_uneven(mean_tiles(held, per_row, 128, c.batch) * p->kv_heads, streamed / c.batch / 64 + 1, units_of(streamed), pace);
+        // (a causal sequence alone is uneven by what its own rows do not see: two workgroups on a CU)
+        const int64_t mean = streamed / c.batch / 64 + 1, level = c.batch > 1 || mean < 32 ? mean : 32;
+        return pieces_uneven(mean_tiles(held, per_row, 128, c.batch) * p->kv_heads, level, units_of(streamed), pace);
     };
     const int64_t items = p->n_q * c.per_row, units = units_of(p->n_kv);
     const double q_bytes = 256.0 * static_cast<double>(p->n_q) * p->heads, kv_bytes = 512.0 * static_cast<double>(p->n_kv) * p->kv_heads;
@@ -1164,7 +1167,7 @@ s3r_status check_workspace(const void *ws, size_t have, size_t need)
 }
 
 // Checks and arguments that the forward call and the gradient have in common.
-s3r_status cross_args(const s3r_cross_params *p, const CrossPlan &c, s3r::CrossArgs *out)
+s3r_status cross_args(const s3r_cross_params *p, const CrossPlan &c, int view, s3r::CrossArgs *out)
 {
     if (p->n_q > 0 && (!p->q || !p->out)) return fail(S3R_ERR_INVALID_ARG, "q and out must be non-null");
     if (p->n_kv > 0 && (!p->k || !p->v)) return fail(S3R_ERR_INVALID_ARG, "k and v must be non-null");
@@ -1186,7 +1189,8 @@ s3r_status cross_args(const s3r_cross_params *p, const CrossPlan &c, s3r::CrossA
     a.q_spans = s3r::Spans{p->q_start, c.batch, p->n_q};
     a.kv_spans = s3r::Spans{p->kv_start, c.batch, p->n_kv};
     a.n_q = p->n_q; a.n_kv = p->n_kv;
-    a.heads = p->heads; a.kv_heads = p->kv_heads; a.per_row = c.per_row; a.uneven = c.batch > 1;
+    a.heads = p->heads; a.kv_heads = p->kv_heads; a.per_row = c.per_row; a.uneven = c.batch > 1 || view > 0;
+    a.view = view;
     a.scale = resolve_scale(p->softmax_scale, 64);
     a.factor = a.scale * 1.4426950408889634f;
     a.to.out = p->out; a.to.lse = p->lse; a.to.rows = p->n_q; a.to.heads = p->heads;
@@ -1196,22 +1200,13 @@ s3r_status cross_args(const s3r_cross_params *p, const CrossPlan &c, s3r::CrossA
 
 float *floats_at(void *base, size_t off) { return reinterpret_cast<float *>(at(base, off)); }
 
-}  // namespace
-
-size_t speed3r_cross_workspace_bytes(const s3r_cross_params *p, int backward)
+s3r_status cross_forward(const s3r_cross_params *p, int view)
 {
     CrossPlan c;
-    if (plan_cross(p, &c) != S3R_OK) return SIZE_MAX;
-    return backward ? c.backward : c.forward;
-}
-
-s3r_status speed3r_cross_attn(const s3r_cross_params *p)
-{
-    CrossPlan c;
-    s3r_status st = plan_cross(p, &c);
+    s3r_status st = plan_cross(p, view, &c);
     if (st != S3R_OK) return st;
     s3r::CrossArgs a;
-    st = cross_args(p, c, &a);
+    st = cross_args(p, c, view, &a);
     if (st != S3R_OK) return st;
     st = check_workspace(p->workspace, p->workspace_bytes, c.forward);
     if (st != S3R_OK) return st;
@@ -1232,13 +1227,13 @@ s3r_status speed3r_cross_attn(const s3r_cross_params *p)
     return S3R_OK;
 }
 
-s3r_status speed3r_cross_attn_backward(const s3r_cross_params *p)
+s3r_status cross_backward(const s3r_cross_params *p, int view)
 {
     CrossPlan c;
-    s3r_status st = plan_cross(p, &c);
+    s3r_status st = plan_cross(p, view, &c);
     if (st != S3R_OK) return st;
     s3r::CrossArgs a;
-    st = cross_args(p, c, &a);
+    st = cross_args(p, c, view, &a);
     if (st != S3R_OK) return st;
     if (p->n_q > 0 && (!p->lse || !p->d_out || !p->dq)) return fail(S3R_ERR_INVALID_ARG, "lse, d_out and dq must be non-null");
     if (p->n_kv > 0 && (!p->dk || !p->dv)) return fail(S3R_ERR_INVALID_ARG, "dk and dv must be non-null");
@@ -1282,6 +1277,50 @@ s3r_status speed3r_cross_attn_backward(const s3r_cross_params *p)
         if (c.split_kv > 1) S3R_HIP(s3r::launch_grad_kv_combine(a, bf16, s), "key gradient combine kernel launch");
     }
     return S3R_OK;
+}
+
+// Tokens of a view that a causal call is given, held to the keys there are (a larger view sees all of them).
+s3r_status causal_view(const s3r_cross_params *p, int tokens_per_view, int *view)
+{
+    if (!p) return fail(S3R_ERR_INVALID_ARG, "params is null");
+    if (tokens_per_view <= 0) return fail(S3R_ERR_INVALID_ARG, "tokens_per_view (%d) must be positive", tokens_per_view);
+    const int64_t most = p->n_kv < 1 ? 1 : (p->n_kv > kMaxRowHeads ? kMaxRowHeads : p->n_kv);
+    *view = tokens_per_view < most ? tokens_per_view : static_cast<int>(most);
+    return S3R_OK;
+}
+
+}  // namespace
+
+size_t speed3r_cross_workspace_bytes(const s3r_cross_params *p, int backward)
+{
+    CrossPlan c;
+    if (plan_cross(p, 0, &c) != S3R_OK) return SIZE_MAX;
+    return backward ? c.backward : c.forward;
+}
+
+s3r_status speed3r_cross_attn(const s3r_cross_params *p) { return cross_forward(p, 0); }
+s3r_status speed3r_cross_attn_backward(const s3r_cross_params *p) { return cross_backward(p, 0); }
+
+size_t speed3r_causal_workspace_bytes(const s3r_cross_params *p, int tokens_per_view, int backward)
+{
+    CrossPlan c;
+    int view;
+    if (causal_view(p, tokens_per_view, &view) != S3R_OK || plan_cross(p, view, &c) != S3R_OK) return SIZE_MAX;
+    return backward ? c.backward : c.forward;
+}
+
+s3r_status speed3r_causal_attn(const s3r_cross_params *p, int tokens_per_view)
+{
+    int view;
+    const s3r_status st = causal_view(p, tokens_per_view, &view);
+    return st != S3R_OK ? st : cross_forward(p, view);
+}
+
+s3r_status speed3r_causal_attn_backward(const s3r_cross_params *p, int tokens_per_view)
+{
+    int view;
+    const s3r_status st = causal_view(p, tokens_per_view, &view);
+    return st != S3R_OK ? st : cross_backward(p, view);
 }
 
 // ---- a cache in 4 bits ---------------------------------------------------------------------------------

@@ -99,6 +99,9 @@ EXPORTS = {
     "speed3r_cross_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(s3r_cross_params), _int]),
     "speed3r_cross_attn": (_int, [ctypes.POINTER(s3r_cross_params)]),
     "speed3r_cross_attn_backward": (_int, [ctypes.POINTER(s3r_cross_params)]),
+    "speed3r_causal_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(s3r_cross_params), _int, _int]),
+    "speed3r_causal_attn": (_int, [ctypes.POINTER(s3r_cross_params), _int]),
+    "speed3r_causal_attn_backward": (_int, [ctypes.POINTER(s3r_cross_params), _int]),
     "speed3r_cache_append": (_int, [ctypes.POINTER(s3r_cache_params)]),
     "speed3r_cache_read": (_int, [ctypes.POINTER(s3r_cache_params)]),
     "speed3r_cache_attn": (_int, [ctypes.POINTER(s3r_cache_params)]),
@@ -437,9 +440,9 @@ def _empty_on(need, stream, index):
         return torch.empty(need, dtype=torch.uint8, device=f"cuda:{index}")
 
 
-def _call(fn, p, need, workspace, index, stream=None):
+def _call(fn, p, need, workspace, index, stream=None, *more):
     """The call with a workspace of `need` bytes (2^64 - 1: its arguments are wrong and the call says why), the caller's where there
-    is one.  Returns the workspace."""
+    is one, and with `more` arguments behind p.  Returns the workspace."""
     if workspace is not None:
         if not isinstance(workspace, torch.Tensor) or workspace.get_device() != index or workspace.dtype is not torch.uint8 \
                 or not workspace.is_contiguous():
@@ -449,10 +452,10 @@ def _call(fn, p, need, workspace, index, stream=None):
     if workspace is not None:
         p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel()
     if index == torch.cuda.current_device():
-        status = fn(ctypes.byref(p))
+        status = fn(ctypes.byref(p), *more)
     else:
         with torch.cuda.device(index):
-            status = fn(ctypes.byref(p))
+            status = fn(ctypes.byref(p), *more)
     if status != S3R_OK:
         raise Speed3rError(status, speed3r_last_error())
     return workspace
@@ -511,6 +514,44 @@ def speed3r_cross_attn_backward(q, k, v, out, lse, d_out, dq, dk, dv, *, q_start
     p.d_out, p.dq = _arg(d_out, "d_out", index, q.dtype, q.shape), _arg(dq, "dq", index, q.dtype, q.shape)
     p.dk, p.dv = _arg(dk, "dk", index, q.dtype, k.shape), _arg(dv, "dv", index, q.dtype, k.shape)
     return _call(lib.speed3r_cross_attn_backward, p, lib.speed3r_cross_workspace_bytes(ctypes.byref(p), 1), workspace, index, stream)
+
+
+def speed3r_causal_workspace_bytes(q, k, *, q_start=None, tokens_per_view=1, backward=False) -> int:
+    """Bytes of workspace that speed3r_causal_attn, or its gradient, needs for these shapes (tensors, or anything
+    with their `shape` and `dtype`)."""
+    p = s3r_cross_params()
+    p.n_q, p.heads, p.head_dim = q.shape
+    p.n_kv, p.kv_heads = k.shape[0], k.shape[1]
+    p.dtype = _dtype_code(q)
+    p.batch = 1 if q_start is None else q_start.numel() - 1
+    p.q_start = p.kv_start = None if q_start is None else 4          # only whether they are given counts here
+    need = load().speed3r_causal_workspace_bytes(ctypes.byref(p), tokens_per_view, int(bool(backward)))
+    if need >= 1 << 62:
+        raise Speed3rError(S3R_ERR_INVALID_ARG, speed3r_last_error())
+    return need
+
+
+def speed3r_causal_attn(q, k, v, out, *, tokens_per_view=1, lse=None, q_start=None, kv_start=None, key_mask=None, softmax_scale=0.0,
+                        workspace=None, status=None, stream=None):
+    """speed3r_cross_attn where the rows of a sequence are its last tokens, and each sees the tokens of its own view and of earlier ones
+    (tokens_per_view 1: the tokens up to itself).  The other arguments are the same; q_start and kv_start are the same list where rows
+    and keys are of the same tokens.  Returns the workspace used (None: none was needed)."""
+    index, lib = _gpu(q, "q"), load()
+    p = _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, status, stream, index)
+    need = lib.speed3r_causal_workspace_bytes(ctypes.byref(p), tokens_per_view, 0)
+    return _call(lib.speed3r_causal_attn, p, need, workspace, index, stream, tokens_per_view)
+
+
+def speed3r_causal_attn_backward(q, k, v, out, lse, d_out, dq, dk, dv, *, tokens_per_view=1, q_start=None, kv_start=None, key_mask=None,
+                                 softmax_scale=0.0, workspace=None, status=None, stream=None):
+    """Gradients of speed3r_causal_attn into dq, dk, dv (contiguous, like q, k, v), from its out and lse and the gradient
+    d_out of out.  The other arguments are those of the forward call.  Returns the workspace used."""
+    index, lib = _gpu(q, "q"), load()
+    p = _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, status, stream, index)
+    p.d_out, p.dq = _arg(d_out, "d_out", index, q.dtype, q.shape), _arg(dq, "dq", index, q.dtype, q.shape)
+    p.dk, p.dv = _arg(dk, "dk", index, q.dtype, k.shape), _arg(dv, "dv", index, q.dtype, k.shape)
+    need = lib.speed3r_causal_workspace_bytes(ctypes.byref(p), tokens_per_view, 1)
+    return _call(lib.speed3r_causal_attn_backward, p, need, workspace, index, stream, tokens_per_view)
 
 
 class PagedCache(NamedTuple):

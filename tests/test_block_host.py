@@ -157,7 +157,35 @@ def test_workspaces_and_null_parameters(s3r):
     assert 0 < lib.speed3r_residual_workspace_bytes(ctypes.byref(residual_params(s3r, n_rows=1 << 28, width=8192))) < 1 << 30
 
 
+def causal_params(s3r, **change):
+    p = fill(s3r.s3r_cross_params(), ("q", "k", "v", "out", "lse", "d_out", "dq", "dk", "dv"))
+    p.n_q, p.n_kv, p.batch, p.heads, p.kv_heads, p.head_dim, p.dtype = 10, 20, 1, 4, 2, 64, s3r.S3R_BF16
+    for f, x in change.items():
+        setattr(p, f, x)
+    return p
+
+
+@pytest.mark.parametrize("change,view,status,word", [
+    (dict(), 0, INVALID, "tokens_per_view"), (dict(), -5, INVALID, "tokens_per_view"), (dict(head_dim=32), 1, UNSUPPORTED, "head_dim"),
+    (dict(n_kv=-1), 1, INVALID, "n_kv"), (dict(n_kv=1 << 40), 7, UNSUPPORTED, "2^28"), (dict(heads=3), 1, INVALID, "multiple"),
+    (dict(q_start=P), 1, INVALID, "together"), (dict(q=None), 1, INVALID, "null"), (dict(out=P), 1, INVALID, "alias"), (dict(k=P + 2), 1, INVALID, "aligned"),
+])
+def test_causal_refusals(s3r, change, view, status, word):
+    lib, p = s3r.load(), causal_params(s3r, **change)
+    for fn in (lib.speed3r_causal_attn, lib.speed3r_causal_attn_backward):
+        assert fn(ctypes.byref(p), view) == status and word in s3r.speed3r_last_error()
+        assert fn(None, 1) == INVALID and "null" in s3r.speed3r_last_error()
+    assert lib.speed3r_causal_workspace_bytes(None, 1, 0) == 2 ** 64 - 1
+    assert lib.speed3r_causal_workspace_bytes(ctypes.byref(causal_params(s3r)), 0, 0) == 2 ** 64 - 1
+    p = causal_params(s3r)
+    assert lib.speed3r_causal_attn_backward(ctypes.byref(p), 1) == WORKSPACE and "workspace" in s3r.speed3r_last_error()
+
+
 def test_workspaces_by_the_binding(s3r):
+    q = torch.empty((10000, 4, 64), dtype=torch.bfloat16, device="meta")
+    assert s3r.speed3r_causal_workspace_bytes(q, q, backward=True) >= 10000 * 4 * 8
+    with pytest.raises(s3r.Speed3rError, match="tokens_per_view"):
+        s3r.speed3r_causal_workspace_bytes(q, q, tokens_per_view=0)
     assert s3r.speed3r_rotary_workspace_bytes(False) == 0 < s3r.speed3r_rotary_workspace_bytes()
     plain, gates = s3r.speed3r_residual_workspace_bytes(1000, 512), s3r.speed3r_residual_workspace_bytes(1000, 512, batch=7, gate_gradients=True)
     assert 0 < plain < gates and s3r.speed3r_residual_workspace_bytes(1000, 512, weight_gradients=False) == 0
