@@ -21,7 +21,7 @@ constexpr int threads_of(int w) { return w > 4 ? 64 * w : 256; }
 
 // A thread's part of a row, and sums over rows of channels.
 template <int L, int W, int CH> struct RowPart {
-    static constexpr int kRows = W == 1 ? 4 * (64 / L) : threads_of(W) / (64 * W);  // of a workgroup at a time
+    static constexpr int kRows = threads_of(W) / (L * W);  // of a workgroup at a time
     int sub, chunk0;
     bool has[CH];
     float *lds;   // [2][waves][2]
@@ -30,11 +30,19 @@ template <int L, int W, int CH> struct RowPart {
     {
         const int t = threadIdx.x;
         sub = t / (L * W);
+        if constexpr (L == 64) sub = __builtin_amdgcn_readfirstlane(sub);  // rows and their addresses are scalars then
         chunk0 = t % (L * W);
 #pragma unroll
         for (int i = 0; i < CH; ++i) has[i] = at(i) < width;
     }
     __device__ __forceinline__ int at(int i) const { return 8 * (chunk0 + L * W * i); }
+    // The thread's i-th chunk of a row (`anyway`: the first chunk where there is none): the row's address, a scalar where a wave has one row, and
+    // an offset of 32 bits.
+    template <typename T> __device__ __forceinline__ T *chunk(T *row, int i, bool anyway) const
+    {
+        const unsigned offset = anyway && !has[i] ? 0u : static_cast<unsigned>(at(i)) * static_cast<unsigned>(sizeof(T));
+        return reinterpret_cast<T *>(reinterpret_cast<uintptr_t>(row) + offset);
+    }
     // Sums of a and b over the row, to all of its threads.  One barrier: a wave writes a buffer again only two sums on.
     __device__ __forceinline__ void sum2(float &a, float &b)
     {
@@ -53,13 +61,13 @@ template <int L, int W, int CH> struct RowPart {
     }
 };
 
+// A thread's chunks of a row as they come from memory; those behind the row's end are the row's first (no lane is left out of a load).
 template <typename T, int CH> struct Raw {
     Io8<T> v[CH];
-    template <typename Part> __device__ __forceinline__ void load(const T *row, const Part &part, bool ok)
+    template <typename Part> __device__ __forceinline__ void load(const T *row, const Part &part)
     {
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
-            if (ok && part.has[i]) v[i].load(row + part.at(i));
+        for (int i = 0; i < CH; ++i) v[i].load(part.chunk(row, i, true));
     }
     template <typename Part> __device__ __forceinline__ void get(float (&x)[CH][8], const Part &part) const
     {
@@ -74,7 +82,7 @@ template <typename T, int CH, typename Part> __device__ __forceinline__ void sto
 {
 #pragma unroll
     for (int i = 0; i < CH; ++i)
-        if (ok && part.has[i]) Io8<T>::store(row + part.at(i), x[i]);
+        if (ok && part.has[i]) Io8<T>::store(part.chunk(row, i, false), x[i]);
 }
 
 template <int CH, typename Part> __device__ __forceinline__ void channel_weights(const void *from, bool is_bf16, const Part &part, float none, float (&w)[CH][8])
@@ -169,14 +177,16 @@ template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ _
     int64_t lo = 0, hi = a.n;
     Raw<TX, CH> x;
     Raw<T, CH> f, gate;
-    auto request = [&](int64_t row, bool ok) {
-        x.load(x_at + row * a.x_row, part, ok);
-        if (f_at != nullptr) f.load(f_at + row * a.f_row, part, ok);
+    // (rows that there are not: the last)
+    auto request = [&](int64_t row) {
+        row = min(row, r1 - 1);
+        x.load(x_at + row * a.x_row, part);
+        if (f_at != nullptr) f.load(f_at + row * a.f_row, part);
         if constexpr (FULL)
             if (gate_at != nullptr) {
                 if (a.spans.start != nullptr)
-                    while (ok && seq + 1 < a.spans.batch && a.spans.start[seq + 1] <= row) ++seq;
-                gate.load(gate_at + seq * a.gate_row, part, ok);
+                    while (seq + 1 < a.spans.batch && a.spans.start[seq + 1] <= row) ++seq;
+                gate.load(gate_at + seq * a.gate_row, part);
             }
     };
     if constexpr (FULL)
@@ -186,7 +196,7 @@ template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ _
             hi = a.spans.start[a.spans.batch];
         }
     auto counts = [&](int64_t row) { return row < r1 && row >= lo && row < hi; };
-    request(r0 + part.sub, counts(r0 + part.sub));
+    request(r0 + part.sub);
     channel_weights<CH>(a.weight, a.w_bf16, part, 1.f, w);
     channel_weights<CH>(a.bias, a.w_bf16, part, 0.f, b);
     channel_weights<CH>(a.scale, a.w_bf16, part, 1.f, scale);
@@ -204,7 +214,7 @@ template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ _
             float g[CH][8];
             if constexpr (FULL)
                 if (gate_at != nullptr) gate.get(g, part);
-            request(row + part.kRows, counts(row + part.kRows));
+            request(row + part.kRows);
             if constexpr (FULL)
                 if (a.post != kNormNone) {
                     row_norm<CH>(a.post, a.eps, of_width, part, u);
@@ -223,7 +233,7 @@ template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ _
                     z[i][j] = fmaf(s, u[i][j], z[i][j]);
                 }
         } else {
-            request(row + part.kRows, counts(row + part.kRows));
+            request(row + part.kRows);
         }
         if (a.r != nullptr) store_row<TX, CH>(static_cast<TX *>(a.r) + row * a.width, z, part, ok);
         if (a.y == nullptr) continue;
@@ -265,77 +275,154 @@ template <int L, int W, int CH, typename Part> __device__ __forceinline__ void s
     }
 }
 
+// A thread's channels of two sums, in places of its own in LDS.
+template <int THREADS, int CH> struct OwnSums {
+    floatx4 *at;  // [CH][2][THREADS]
+    __device__ __forceinline__ OwnSums(float *lds, int which) : at(reinterpret_cast<floatx4 *>(lds) + which * (2 * CH * THREADS) + threadIdx.x)
+    {
+#pragma unroll
+        for (int i = 0; i < 2 * CH; ++i) at[i * THREADS] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    __device__ __forceinline__ void add(const float (&x)[CH][8], const float (&w)[CH][8])
+    {
+#pragma unroll
+        for (int i = 0; i < 2 * CH; ++i) {
+            floatx4 t = at[i * THREADS];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] = fmaf(x[i / 2][4 * (i & 1) + e], w[i / 2][4 * (i & 1) + e], t[e]);
+            at[i * THREADS] = t;
+        }
+    }
+    __device__ __forceinline__ void add(const float (&x)[CH][8])
+    {
+#pragma unroll
+        for (int i = 0; i < 2 * CH; ++i) {
+            floatx4 t = at[i * THREADS];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] += x[i / 2][4 * (i & 1) + e];
+            at[i * THREADS] = t;
+        }
+    }
+    __device__ __forceinline__ void get(float (&x)[CH][8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 2 * CH; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[i / 2][4 * (i & 1) + e] = at[i * THREADS][e];
+    }
+};
+// Sums of a gradient that are in LDS: GA and GB, and where registers run out those of dy n and dy.
+template <int W, int CH, bool FULL> constexpr int kOwnSums = !FULL ? 0 : (W * CH >= 16 ? 4 : 2);
+
+// A thread's part of the rows of a gradient.
+template <typename TX, typename T, int CH> struct GradRows {
+    Raw<TX, CH> x, dr;
+    Raw<T, CH> f, dy;
+    template <typename Part> __device__ __forceinline__ void load(const ResidualArgs &a, int64_t row, int64_t end, const Part &part)
+    {
+        row = min(row, end - 1);  // (rows that there are not: the last)
+        x.load(static_cast<const TX *>(a.x) + row * a.x_row, part);
+        if (a.f != nullptr) f.load(static_cast<const T *>(a.f) + row * a.f_row, part);
+        if (a.d_y != nullptr) dy.load(static_cast<const T *>(a.d_y) + row * a.width, part);
+        if (a.d_r != nullptr) dr.load(static_cast<const TX *>(a.d_r) + row * a.width, part);
+    }
+};
+
+// FULL: with a post-norm or gates.  What scale, gate and post weights multiply is the same for all rows of a sequence, so that their
+// gradients are made of two sums over these, A = sum dr' n' (n': f normed, or f) and B = sum dr':
+//   d gate = residual_scale scale (post_weight A + post_bias B), and, with GA and GB the sums of gate A and gate B over the sequences,
+//   d scale = residual_scale (post_weight GA + post_bias GB),  d post_weight = residual_scale scale GA,  d post_bias = residual_scale scale GB.
+// A row needs of the weights their products r = x + fw n' + fb alone: fw = s post_weight, fb = s post_bias.
 template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ __launch_bounds__(threads_of(W)) void residual_grad_kernel(ResidualArgs a)
 {
     using Part = RowPart<L, W, CH>;
     __shared__ float lds[2 * 2 * (threads_of(W) / 64)];
     __shared__ float join[Part::kRows > 1 ? Part::kRows * 8 * L * W : 1];
+    extern __shared__ __align__(16) float own_sums[];  // FULL: GA and GB
     Part part(a.width, lds);
     const float of_width = 1.f / static_cast<float>(a.width);
     const int64_t r0 = static_cast<int64_t>(blockIdx.x) * a.rows_per_block, r1 = min(r0 + a.rows_per_block, a.n);
-    float w[CH][8], scale[CH][8], pw[CH][8], pb[CH][8], gate[CH][8];
+    float w[CH][8], fw[CH][8], fb[CH][8], dw[CH][8], db[CH][8], sa[CH][8], sb[CH][8];
     channel_weights<CH>(a.weight, a.w_bf16, part, 1.f, w);
-    channel_weights<CH>(a.scale, a.w_bf16, part, 1.f, scale);
-    if constexpr (FULL) {
-        channel_weights<CH>(a.post_weight, a.w_bf16, part, 1.f, pw);
-        channel_weights<CH>(a.post_bias, a.w_bf16, part, 0.f, pb);
-    }
-    float dw[CH][8], db[CH][8], ds[CH][8], dpw[CH][8], dpb[CH][8], dg[CH][8];
 #pragma unroll
     for (int i = 0; i < CH; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) dw[i][j] = db[i][j] = ds[i][j] = dpw[i][j] = dpb[i][j] = dg[i][j] = 0.f, gate[i][j] = 1.f;
-    const TX *x_at = static_cast<const TX *>(a.x), *dr_at = static_cast<const TX *>(a.d_r);
-    const T *f_at = static_cast<const T *>(a.f), *dy_at = static_cast<const T *>(a.d_y);
-    auto rows_of = [&](int64_t from, int64_t to) {
-        Raw<TX, CH> x, dr;
-        Raw<T, CH> f, dy;
-        auto request = [&](int64_t row) {
-            const bool ok = row < to;
-            x.load(x_at + row * a.x_row, part, ok);
-            if (f_at != nullptr) f.load(f_at + row * a.f_row, part, ok);
-            if (dy_at != nullptr) dy.load(dy_at + row * a.width, part, ok);
-            if (dr_at != nullptr) dr.load(dr_at + row * a.width, part, ok);
+        for (int j = 0; j < 8; ++j) dw[i][j] = db[i][j] = sa[i][j] = sb[i][j] = 0.f;
+    constexpr int kOwn = kOwnSums<W, CH, FULL>;
+    OwnSums<threads_of(W), kOwn >= 2 ? CH : 0> ga(own_sums, 0), gb(own_sums, 1);
+    OwnSums<threads_of(W), kOwn >= 4 ? CH : 0> own_dw(own_sums, 2), own_db(own_sums, 3);
+    const bool gated = FULL && a.gate != nullptr, with_f = a.f != nullptr;
+    // Sequence by sequence (without gates: all rows at once).
+    for (int seq = gated ? find_sequence(a.spans, r0) : 0; seq < a.spans.batch; ++seq) {
+        int first_row = 0, len = 0;
+        if (gated) a.spans.of(seq, first_row, len);
+        if (first_row >= r1) break;
+        const int64_t from = gated ? max(r0, static_cast<int64_t>(first_row)) : r0, to = gated ? min(r1, static_cast<int64_t>(first_row) + len) : r1;
+        if (from >= to) continue;
+        GradRows<TX, T, CH> ahead;
+        constexpr bool kAhead = W * CH < 16 || (!FULL && sizeof(TX) == 2);  // (the widest rows leave no registers for the next one)
+        if (kAhead) ahead.load(a, from + part.sub, to, part);
+        auto get_gate = [&](float (&gate)[CH][8]) {
+            Raw<T, CH> raw;
+            raw.load(static_cast<const T *>(a.gate) + seq * a.gate_row, part);
+            raw.get(gate, part);
         };
-        request(from + part.sub);
+        channel_weights<CH>(a.scale, a.w_bf16, part, 1.f, fw);
+        if constexpr (FULL) {
+            float gate[CH][8], pw[CH][8];
+            if (gated) get_gate(gate);
+            channel_weights<CH>(a.post_weight, a.w_bf16, part, 1.f, pw);
+            channel_weights<CH>(a.post_bias, a.w_bf16, part, 0.f, fb);
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float s = a.residual_scale * fw[i][j];
+                    if (gated) s *= gate[i][j];
+                    fw[i][j] = s * pw[i][j];
+                    fb[i][j] *= s;
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) fw[i][j] *= a.residual_scale;
+        }
         for (int64_t first = from; first < to; first += Part::kRows) {
             const int64_t row = first + part.sub;
             const bool ok = row < to;
-            float z[CH][8], u[CH][8], g[CH][8], d[CH][8];
-            x.get(z, part);
-            if (f_at != nullptr) f.get(u, part);
-            if (dy_at != nullptr) dy.get(g, part);
-            if (dr_at != nullptr) dr.get(d, part);
-            request(row + Part::kRows);
+            float z[CH][8], n[CH][8], g[CH][8], d[CH][8];
+            GradRows<TX, T, CH> here;
+            if (kAhead) here = ahead; else here.load(a, row, to, part);
+            here.x.get(z, part);
+            if (with_f) here.f.get(n, part);
+            if (a.d_y != nullptr) here.dy.get(g, part);
+            if (a.d_r != nullptr) here.dr.get(d, part);
+            if (kAhead) ahead.load(a, row + Part::kRows, to, part);
             float post_inv = 0.f;
             if constexpr (FULL)
-                if (a.post != kNormNone) post_inv = row_norm<CH>(a.post, a.eps, of_width, part, u);
-            auto branch = [&](int i, int j) {  // u of the formulas
-                if constexpr (FULL) return fmaf(u[i][j], pw[i][j], pb[i][j]);
-                return u[i][j];
-            };
-            auto factor = [&](int i, int j) {
-                float s = a.residual_scale * scale[i][j];
-                if constexpr (FULL) s *= gate[i][j];
-                return s;
-            };
-            if (dr_at == nullptr)
+                if (a.post != kNormNone) post_inv = row_norm<CH>(a.post, a.eps, of_width, part, n);
+            if (a.d_r == nullptr)
 #pragma unroll
                 for (int i = 0; i < CH; ++i)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) d[i][j] = 0.f;
-            if (dy_at != nullptr) {
-                if (f_at != nullptr)
+            if (a.d_y != nullptr) {
+                if (with_f)
 #pragma unroll
                     for (int i = 0; i < CH; ++i)
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) z[i][j] = fmaf(factor(i, j), branch(i, j), z[i][j]);
+                        for (int j = 0; j < 8; ++j) z[i][j] += FULL ? fmaf(fw[i][j], n[i][j], fb[i][j]) : fw[i][j] * n[i][j];
                 const float inv = row_norm<CH>(a.norm, a.eps, of_width, part, z);
+                if constexpr (kOwn >= 4) {  // (one row at a time)
+                    own_dw.add(g, z);
+                    own_db.add(g);
+                }
 #pragma unroll
                 for (int i = 0; i < CH; ++i)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        if (ok) {
+                        if (kOwn < 4 && ok) {
                             dw[i][j] = fmaf(g[i][j], z[i][j], dw[i][j]);
                             db[i][j] += g[i][j];
                         }
@@ -348,122 +435,187 @@ template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ _
                     for (int j = 0; j < 8; ++j) d[i][j] += g[i][j];
             }
             store_row<TX, CH>(static_cast<TX *>(a.dx) + row * a.width, d, part, ok);
-            if (f_at == nullptr) continue;
+            if (!with_f) continue;
 #pragma unroll
             for (int i = 0; i < CH; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float t = d[i][j] * branch(i, j);
-                    d[i][j] *= factor(i, j);
-                    if (!ok) continue;
-                    if constexpr (FULL) {
-                        ds[i][j] = fmaf(gate[i][j], t, ds[i][j]);
-                        dg[i][j] += t;
-                        dpw[i][j] = fmaf(d[i][j], u[i][j], dpw[i][j]);
-                        dpb[i][j] += d[i][j];
-                    } else {
-                        ds[i][j] += t;
+                    if (ok) {
+                        sa[i][j] = fmaf(d[i][j], n[i][j], sa[i][j]);
+                        if constexpr (FULL) sb[i][j] += d[i][j];
                     }
+                    d[i][j] *= fw[i][j];
                 }
             if constexpr (FULL)
-                if (a.post != kNormNone) {
-#pragma unroll
-                    for (int i = 0; i < CH; ++i)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) d[i][j] *= pw[i][j];
-                    row_norm_back<CH>(a.post, of_width, post_inv, u, part, d);
-                }
+                if (a.post != kNormNone) row_norm_back<CH>(a.post, of_width, post_inv, n, part, d);
             store_row<T, CH>(static_cast<T *>(a.df) + row * a.width, d, part, ok);
         }
-    };
-    if (FULL && a.gate != nullptr) {
-        // sequence by sequence; what a workgroup's rows of sequence b give goes to place blockIdx.x + b, which no other pair has
-        int seq = find_sequence(a.spans, r0);
-        for (; seq < a.spans.batch; ++seq) {
-            int first, len;
-            a.spans.of(seq, first, len);
-            if (first >= r1) break;
-            const int64_t from = max(r0, static_cast<int64_t>(first)), to = min(r1, static_cast<int64_t>(first) + len);
-            if (from >= to) continue;
-            Raw<T, CH> raw;
-            raw.load(static_cast<const T *>(a.gate) + seq * a.gate_row, part, true);
-            raw.get(gate, part);
-            rows_of(from, to);
-            if (a.part_gate != nullptr)
-                store_sums<L, W, CH>(dg, a.part_gate + (static_cast<int64_t>(blockIdx.x) + seq) * a.width, a.width, part, join);
+        if constexpr (FULL) {
+            if (!gated) break;
+            float gate[CH][8], sums[CH][8];
+            get_gate(gate);
+            ga.add(sa, gate);
+            gb.add(sb, gate);
+            if (a.part_gate != nullptr) {  // at place blockIdx.x + seq, which no other pair has
+                channel_weights<CH>(a.post_weight, a.w_bf16, part, 1.f, sums);
+                channel_weights<CH>(a.post_bias, a.w_bf16, part, 0.f, gate);
+#pragma unroll
+                for (int i = 0; i < CH; ++i)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sums[i][j] = fmaf(sums[i][j], sa[i][j], gate[i][j] * sb[i][j]);
+                store_sums<L, W, CH>(sums, a.part_gate + (static_cast<int64_t>(blockIdx.x) + seq) * a.width, a.width, part, join);
+            }
 #pragma unroll
             for (int i = 0; i < CH; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) dg[i][j] = 0.f;
+                for (int j = 0; j < 8; ++j) sa[i][j] = sb[i][j] = 0.f;
+        } else {
+            break;
         }
-    } else {
-        rows_of(r0, r1);
     }
+    if (a.part == nullptr) return;
     const int64_t share = static_cast<int64_t>(gridDim.x) * a.width;
     float *to = a.part + blockIdx.x * static_cast<int64_t>(a.width);
-    if (a.part == nullptr) return;
-    if (a.d_weight != nullptr) store_sums<L, W, CH>(dw, to, a.width, part, join);
-    if (a.d_bias != nullptr) store_sums<L, W, CH>(db, to + share, a.width, part, join);
-    if (a.d_scale != nullptr) store_sums<L, W, CH>(ds, to + 2 * share, a.width, part, join);
+    if (a.d_weight != nullptr || a.d_bias != nullptr) {
+        if constexpr (kOwn >= 4) {
+            own_dw.get(dw);
+            own_db.get(db);
+        }
+        store_sums<L, W, CH>(dw, to, a.width, part, join);
+        store_sums<L, W, CH>(db, to + share, a.width, part, join);
+    }
+    if (a.d_scale == nullptr && a.d_post_weight == nullptr && a.d_post_bias == nullptr) return;
     if constexpr (FULL) {
-        if (a.d_post_weight != nullptr) store_sums<L, W, CH>(dpw, to + 3 * share, a.width, part, join);
-        if (a.d_post_bias != nullptr) store_sums<L, W, CH>(dpb, to + 4 * share, a.width, part, join);
+        if (gated) {
+            ga.get(sa);
+            gb.get(sb);
+        }
+        store_sums<L, W, CH>(sb, to + 3 * share, a.width, part, join);
+    }
+    store_sums<L, W, CH>(sa, to + 2 * share, a.width, part, join);
+}
+
+// The sums of `count` partial results, `stride` floats apart, of 16 channels (channel = the thread's, ok: there is one), of N tensors that
+// are `gap` apart: 64 groups of a workgroup take every 64th, in 64 bits (sums of hundreds, which cost nothing here).  To the threads of group 0.
+template <int N> __device__ __forceinline__ void sum_parts(const float *from, int64_t count, int64_t stride, int64_t gap, bool ok, double (&lds)[N][64][16], double (&s)[N])
+{
+    const int c = threadIdx.x & 15, group = threadIdx.x >> 4;
+#pragma unroll
+    for (int n = 0; n < N; ++n) s[n] = 0.0;
+    if (ok) {
+        constexpr int kAtOnce = 8;
+        for (int64_t i = group; i < count; i += 64 * kAtOnce) {
+            float x[N][kAtOnce];
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) x[n][k] = i + 64 * k < count ? from[n * gap + (i + 64 * k) * stride] : 0.f;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) s[n] += x[n][k];
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) lds[n][group][c] = s[n];
+    __syncthreads();
+    if (group != 0) return;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        s[n] = 0.0;
+#pragma unroll
+        for (int i = 0; i < 64; ++i) s[n] += lds[n][i][c];
     }
 }
 
-// Sums over the workgroups, 32 channels of one tensor (blockIdx.y) for a workgroup of eight groups.
-__global__ __launch_bounds__(256) void residual_sums_kernel(ResidualArgs a, int blocks)
+__device__ __forceinline__ float weight_at(const void *w, bool is_bf16, int c, float none)
 {
-    const int which = blockIdx.y, c = threadIdx.x & 31, group = threadIdx.x >> 5, channel = blockIdx.x * 32 + c;
-    void *to = which == 0 ? a.d_weight : (which == 1 ? a.d_bias : (which == 2 ? a.d_scale : (which == 3 ? a.d_post_weight : a.d_post_bias)));
-    if (to == nullptr) return;
-    __shared__ float sums[8][32];
-    float s = 0.f;
-    if (channel < a.width)
-        for (int i = group; i < blocks; i += 8) s += a.part[(static_cast<int64_t>(which) * blocks + i) * a.width + channel];
-    sums[group][c] = s;
-    __syncthreads();
-    if (group != 0 || channel >= a.width) return;
-    s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s += sums[i][c];
-    store_weight(to, a.w_bf16, channel, which == 2 ? s * a.residual_scale : s);
+    if (w == nullptr) return none;
+    return is_bf16 ? static_cast<float>(static_cast<const bf16_t *>(w)[c]) : static_cast<const float *>(w)[c];
 }
 
-// The gradient of a sequence's gate: the sum over the workgroups that had rows of it.
-template <typename T> __global__ __launch_bounds__(256) void residual_gate_kernel(ResidualArgs a)
+// What is made of the workgroups' sums, 16 channels for a workgroup; blockIdx.y: d weight and d bias (of_norm), then GA and GB and
+// what comes of them (of_branch), then the gates, sequence by sequence.
+__global__ __launch_bounds__(1024) void residual_sums_kernel(ResidualArgs a, int blocks, bool of_norm, bool of_branch, bool is_bf16)
+{
+    __shared__ double lds[2][64][16];
+    const int c = blockIdx.x * 16 + (threadIdx.x & 15), seq = static_cast<int>(blockIdx.y) - (of_norm + of_branch);
+    const bool first = of_norm && blockIdx.y == 0, ok = c < a.width, mine = threadIdx.x < 16 && ok;
+    const double scale = a.residual_scale * static_cast<double>(ok ? weight_at(a.scale, a.w_bf16, c, 1.f) : 0.f);
+    double s[2];
+    if (seq >= 0) {
+        int row, len;
+        a.spans.of(seq, row, len);
+        const int64_t from = row / a.rows_per_block, count = len > 0 ? (static_cast<int64_t>(row) + len - 1) / a.rows_per_block - from + 1 : 0;
+        sum_parts<1>(a.part_gate + (from + seq) * a.width + c, count, a.width, 0, ok, reinterpret_cast<double(&)[1][64][16]>(lds), reinterpret_cast<double(&)[1]>(s));
+        if (mine) store_weight(a.d_gate, is_bf16, static_cast<int64_t>(seq) * a.width + c, static_cast<float>(scale * s[0]));
+        return;
+    }
+    const int64_t gap = static_cast<int64_t>(blocks) * a.width;
+    sum_parts<2>(a.part + (first ? 0 : 2 * gap) + c, blocks, a.width, first || a.post != kNormNone || a.gate != nullptr ? gap : 0, ok, lds, s);
+    if (!mine) return;
+    if (first) {
+        if (a.d_weight != nullptr) store_weight(a.d_weight, a.w_bf16, c, static_cast<float>(s[0]));
+        if (a.d_bias != nullptr) store_weight(a.d_bias, a.w_bf16, c, static_cast<float>(s[1]));
+        return;
+    }
+    if (a.d_scale != nullptr)
+        store_weight(a.d_scale, a.w_bf16, c, static_cast<float>(a.residual_scale * (weight_at(a.post_weight, a.w_bf16, c, 1.f) * s[0] +
+                                                                                   weight_at(a.post_bias, a.w_bf16, c, 0.f) * s[1])));
+    if (a.d_post_weight != nullptr) store_weight(a.d_post_weight, a.w_bf16, c, static_cast<float>(scale * s[0]));
+    if (a.d_post_bias != nullptr) store_weight(a.d_post_bias, a.w_bf16, c, static_cast<float>(scale * s[1]));
+}
+
+// The gates of sequences that few workgroups had rows of each: a thread for a channel.
+__global__ __launch_bounds__(256) void residual_gate_kernel(ResidualArgs a, bool is_bf16)
 {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    const int64_t seq = i / a.width;
+    const int seq = static_cast<int>(i / a.width), c = static_cast<int>(i % a.width);
     if (seq >= a.spans.batch) return;
-    const int c = static_cast<int>(i - seq * a.width);
-    int first, len;
-    a.spans.of(static_cast<int>(seq), first, len);
-    float s = 0.f;
-    if (len > 0)
-        for (int64_t g = first / a.rows_per_block; g <= (static_cast<int64_t>(first) + len - 1) / a.rows_per_block; ++g)
-            s += a.part_gate[(g + seq) * a.width + c];
-    s *= a.residual_scale;
-    if (a.scale != nullptr) s *= a.w_bf16 ? static_cast<float>(static_cast<const bf16_t *>(a.scale)[c]) : static_cast<const float *>(a.scale)[c];
-    static_cast<T *>(a.d_gate)[i] = from_float<T>(s);
+    int row, len;
+    a.spans.of(seq, row, len);
+    const int64_t from = row / a.rows_per_block, count = len > 0 ? (static_cast<int64_t>(row) + len - 1) / a.rows_per_block - from + 1 : 0;
+    const float *part = a.part_gate + (from + seq) * a.width + c;
+    double s = 0.0;
+    for (int64_t g = 0; g < count; ++g) s += part[g * a.width];
+    store_weight(a.d_gate, is_bf16, i, static_cast<float>(s * a.residual_scale * weight_at(a.scale, a.w_bf16, c, 1.f)));
 }
 
-// Rows of up to 128, 512, 1024, 4096 and 8192 channels.
-template <typename TX, typename T, bool FULL, typename Launch> hipError_t by_width(int width, Launch &&launch)
-{
-    if (width <= 128) return launch(&residual_kernel<TX, T, 16, 1, 1, FULL>, &residual_grad_kernel<TX, T, 16, 1, 1, FULL>, 256);
-    if (width <= 512) return launch(&residual_kernel<TX, T, 64, 1, 1, FULL>, &residual_grad_kernel<TX, T, 64, 1, 1, FULL>, 256);
-    if (width <= 1024) return launch(&residual_kernel<TX, T, 64, 1, 2, FULL>, &residual_grad_kernel<TX, T, 64, 1, 2, FULL>, 256);
-    if (width <= 4096) return launch(&residual_kernel<TX, T, 64, 4, 2, FULL>, &residual_grad_kernel<TX, T, 64, 4, 2, FULL>, 256);
-    return launch(&residual_kernel<TX, T, 64, 8, 2, FULL>, &residual_grad_kernel<TX, T, 64, 8, 2, FULL>, 512);
-}
+// Kernels for rows of up to 64, 128, 256 .. channels: lanes, waves and chunks of a row.
+template <typename TX, typename T, bool FULL> struct Kernels {
+    struct { void (*kernel)(ResidualArgs); int threads; size_t lds; } forward, grad;
+    template <int L, int W, int CH> void set_forward() { forward = {&residual_kernel<TX, T, L, W, CH, FULL>, threads_of(W), 0}; }
+    template <int L, int W, int CH> void set_grad()
+    {
+        grad = {&residual_grad_kernel<TX, T, L, W, CH, FULL>, threads_of(W), kOwnSums<W, CH, FULL> * 8 * CH * threads_of(W) * sizeof(float)};
+    }
+    template <int L, int W, int CH> void set() { set_forward<L, W, CH>(); set_grad<L, W, CH>(); }
+    explicit Kernels(int width)
+    {
+        if (width <= 64) set<8, 1, 1>();
+        else if (width <= 128) set<16, 1, 1>();
+        else if (width <= 256) set<32, 1, 1>();
+        else if (width <= 512) set<64, 1, 1>();
+        else if constexpr (FULL) {
+            if (width <= 1024) set<64, 2, 1>();
+            else if (width <= 2048) set<64, 4, 1>();
+            else if (width <= 4096) set<64, 8, 1>();
+            else { set_forward<64, 16, 1>(); set_grad<64, 8, 2>(); }
+        } else {
+            if (width <= 1024) set<64, 1, 2>();
+            else if (width <= 2048) set<64, 2, 2>();
+            else if (width <= 4096) set<64, 4, 2>();
+            else set<64, 8, 2>();
+        }
+    }
+};
 
 template <typename Launch> hipError_t by_type(const ResidualArgs &a, bool x_bf16, bool is_bf16, Launch &&launch)
 {
     const bool full = a.post != kNormNone || a.gate != nullptr;
-    if (!is_bf16) return full ? by_width<float, float, true>(a.width, launch) : by_width<float, float, false>(a.width, launch);
-    if (x_bf16) return full ? by_width<bf16_t, bf16_t, true>(a.width, launch) : by_width<bf16_t, bf16_t, false>(a.width, launch);
-    return full ? by_width<float, bf16_t, true>(a.width, launch) : by_width<float, bf16_t, false>(a.width, launch);
+    if (!is_bf16) return full ? launch(Kernels<float, float, true>(a.width)) : launch(Kernels<float, float, false>(a.width));
+    if (x_bf16) return full ? launch(Kernels<bf16_t, bf16_t, true>(a.width)) : launch(Kernels<bf16_t, bf16_t, false>(a.width));
+    return full ? launch(Kernels<float, bf16_t, true>(a.width)) : launch(Kernels<float, bf16_t, false>(a.width));
 }
 
 }  // namespace
@@ -471,8 +623,8 @@ template <typename Launch> hipError_t by_type(const ResidualArgs &a, bool x_bf16
 hipError_t launch_residual(const ResidualArgs &a, bool x_bf16, bool is_bf16, hipStream_t stream)
 {
     const int64_t blocks = (a.n + a.rows_per_block - 1) / a.rows_per_block;
-    return by_type(a, x_bf16, is_bf16, [&](auto kernel, auto, int threads) {
-        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(threads), 0, stream, a);
+    return by_type(a, x_bf16, is_bf16, [&](auto kernels) {
+        hipLaunchKernelGGL(kernels.forward.kernel, dim3(static_cast<unsigned>(blocks)), dim3(kernels.forward.threads), 0, stream, a);
         return hipGetLastError();
     });
 }
@@ -481,23 +633,26 @@ hipError_t launch_residual_grad(const ResidualArgs &a, bool x_bf16, bool is_bf16
 {
     const int64_t blocks = (a.n + a.rows_per_block - 1) / a.rows_per_block;
     if (blocks > 0) {
-        const hipError_t e = by_type(a, x_bf16, is_bf16, [&](auto, auto kernel, int threads) {
-            hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(threads), 0, stream, a);
+        const hipError_t e = by_type(a, x_bf16, is_bf16, [&](auto kernels) {
+            const hipError_t allowed = allow_lds(kernels.grad.kernel, kernels.grad.lds);
+            if (allowed != hipSuccess) return allowed;
+            hipLaunchKernelGGL(kernels.grad.kernel, dim3(static_cast<unsigned>(blocks)), dim3(kernels.grad.threads), kernels.grad.lds, stream, a);
             return hipGetLastError();
         });
         if (e != hipSuccess) return e;
     }
-    if (a.d_weight != nullptr || a.d_bias != nullptr || a.d_scale != nullptr || a.d_post_weight != nullptr || a.d_post_bias != nullptr) {
-        hipLaunchKernelGGL(residual_sums_kernel, dim3((a.width + 31) / 32, 5), dim3(256), 0, stream, a, static_cast<int>(blocks));
+    const bool of_norm = a.d_weight != nullptr || a.d_bias != nullptr, of_branch = a.d_scale != nullptr || a.d_post_weight != nullptr || a.d_post_bias != nullptr;
+    // (more than eight workgroups for a sequence: 64 groups add them up; 40 us where a thread does, for 6 sequences of 501 workgroups, 4 so)
+    const bool spread = a.d_gate != nullptr && blocks > 8 * static_cast<int64_t>(a.spans.batch);
+    const unsigned rows = of_norm + of_branch + (spread ? a.spans.batch : 0);
+    if (rows > 0) {
+        hipLaunchKernelGGL(residual_sums_kernel, dim3((a.width + 15) / 16, rows), dim3(1024), 0, stream, a, static_cast<int>(blocks), of_norm, of_branch, is_bf16);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (a.d_gate == nullptr) return hipSuccess;
+    if (a.d_gate == nullptr || spread) return hipSuccess;
     const int64_t gates = (static_cast<int64_t>(a.spans.batch) * a.width + 255) / 256;
-    if (is_bf16)
-        hipLaunchKernelGGL(residual_gate_kernel<bf16_t>, dim3(static_cast<unsigned>(gates)), dim3(256), 0, stream, a);
-    else
-        hipLaunchKernelGGL(residual_gate_kernel<float>, dim3(static_cast<unsigned>(gates)), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(residual_gate_kernel, dim3(static_cast<unsigned>(gates)), dim3(256), 0, stream, a, is_bf16);
     return hipGetLastError();
 }
 

@@ -314,23 +314,29 @@ template <typename T, Mode MODE> __global__ __launch_bounds__(256) void rotary_n
             (exchange[threadIdx.x] + exchange[512 + threadIdx.x]) + (exchange[1024 + threadIdx.x] + exchange[1536 + threadIdx.x]);
 }
 
-// The gradients of weight and bias (blockIdx.x % 2) of q or k (blockIdx.x / 2) as sums over the workgroups, sixteen at a time.
+// The gradients of weight and bias of q and of k as sums over the workgroups, in 64 bits: 16 of the 64 channels of one of the four for a
+// workgroup, whose 64 groups take every 64th.
 __global__ __launch_bounds__(1024) void rotary_weight_grad_kernel(RotaryArgs a, int wgs_q, int wgs)
 {
-    const int side = blockIdx.x >> 1, which = blockIdx.x & 1, c = threadIdx.x & 63, group = threadIdx.x >> 6;
+    const int side = blockIdx.x >> 3, which = (blockIdx.x >> 2) & 1, c = threadIdx.x & 15, group = threadIdx.x >> 4, channel = (blockIdx.x & 3) * 16 + c;
     const int first = side == 0 ? 0 : wgs_q, end = side == 0 ? wgs_q : wgs;
     void *to = which == 0 ? a.side[side].d_weight : a.side[side].d_bias;
     if (to == nullptr) return;
-    __shared__ float sums[16][64];
-    float s = 0.f;
-    for (int i = first + group; i < end; i += 16) s += a.part[static_cast<int64_t>(i) * 128 + which * 64 + c];
+    __shared__ double sums[64][16];
+    constexpr int kMost = kRotaryGradGroups / 64;
+    float x[kMost];
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) x[i] = first + group + 64 * i < end ? a.part[static_cast<int64_t>(first + group + 64 * i) * 128 + which * 64 + channel] : 0.f;
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) s += x[i];
     sums[group][c] = s;
     __syncthreads();
     if (group != 0) return;
-    s = 0.f;
+    s = 0.0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s += sums[i][c];
-    store_weight(to, a.w_bf16, c, s);
+    for (int i = 0; i < 64; ++i) s += sums[i][c];
+    store_weight(to, a.w_bf16, channel, static_cast<float>(s));
 }
 
 // Whether a position is outside the table.  One workgroup.
@@ -408,7 +414,7 @@ hipError_t launch_rotary_norm_grad(const RotaryArgs &a, bool is_bf16, hipStream_
     hipError_t e = hipSuccess;
     if (wgs > 0) e = is_bf16 ? launch_norm_grad_t<bf16_t>(a, run, wgs_q, wgs, stream) : launch_norm_grad_t<float>(a, run, wgs_q, wgs, stream);
     if (e != hipSuccess || a.part == nullptr) return e;
-    hipLaunchKernelGGL(rotary_weight_grad_kernel, dim3(4), dim3(1024), 0, stream, a, wgs_q, wgs);
+    hipLaunchKernelGGL(rotary_weight_grad_kernel, dim3(16), dim3(1024), 0, stream, a, wgs_q, wgs);
     return hipGetLastError();
 }
 

@@ -27,6 +27,13 @@ __device__ __forceinline__ float sum_with_other_half(float x)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// More than 64 KiB of LDS have to be allowed to a kernel first.
+template <typename Kernel> hipError_t allow_lds(Kernel kernel, size_t bytes)
+{
+    if (bytes <= size_t(64) << 10) return hipSuccess;
+    return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+}
+
 // One LDS-direct load: 64 lanes x 16 bytes from `src` (per-lane address) to LDS byte address
 // `lds_byte` (wave-uniform) + 16 * lane.  Counted by vmcnt like any vector memory load.
 __device__ __forceinline__ void lds_dma_16(const void *src, unsigned lds_byte)

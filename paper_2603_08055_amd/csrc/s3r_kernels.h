@@ -397,7 +397,7 @@ hipError_t launch_rotary_norm_grad(const RotaryArgs &a, bool is_bf16, hipStream_
 hipError_t launch_rotary_status(const RotaryArgs &a, int *status, hipStream_t stream);
 
 // x_row, f_row, gate_row: elements between rows; all others are packed.  rows_per_block: rows of a workgroup, which follow one another.
-// part: [5][workgroups][width], part_gate: [workgroups + batch - 1][width], or null.
+// part: [4][workgroups][width], part_gate: [workgroups + batch - 1][width], or null.
 struct ResidualArgs {
     const void *x, *f, *gate;
     int64_t x_row, f_row, gate_row;
@@ -414,8 +414,11 @@ struct ResidualArgs {
 };
 hipError_t launch_residual(const ResidualArgs &a, bool x_bf16, bool is_bf16, hipStream_t stream);
 hipError_t launch_residual_grad(const ResidualArgs &a, bool x_bf16, bool is_bf16, hipStream_t stream);
-// Rows that a workgroup has at a time.
-inline int residual_rows(int width) { return width <= 128 ? 16 : (width <= 1024 ? 4 : 1); }
+// Rows that a workgroup has at a time (full: with a post-norm or gates).
+inline int residual_rows(int width, bool full)
+{
+    return width <= 64 ? 32 : (width <= 128 ? 16 : (width <= 256 ? 8 : (width <= 512 ? 4 : (width <= 1024 ? (full ? 2 : 4) : (width <= 2048 && !full ? 2 : 1)))));
+}
 
 // Most tiles that `batch` sequences of n rows together can have, at least 1.  A sequence's items are a multiple of per_row, so that its
 // last tile lacks at most tile - gcd(per_row, tile) of them, and at most n sequences have any.  (64 sequences of a row, four heads

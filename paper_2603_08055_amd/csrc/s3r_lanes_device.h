@@ -53,7 +53,7 @@ __device__ __forceinline__ void load_weights(const void *from, bool is_bf16, int
     }
 }
 
-__device__ __forceinline__ void store_weight(void *to, bool is_bf16, int at, float x)
+__device__ __forceinline__ void store_weight(void *to, bool is_bf16, int64_t at, float x)
 {
     if (is_bf16)
         static_cast<bf16_t *>(to)[at] = static_cast<bf16_t>(x);

@@ -930,11 +930,4 @@ __device__ __forceinline__ bool spans_bad(const Spans &s)
 // A launch's threads must stay below 2^32.
 inline bool grid_ok(int64_t blocks_of_256) { return blocks_of_256 > 0 && blocks_of_256 <= 0xffffff; }
 
-// More than 64 KiB of LDS have to be allowed to a kernel first.
-template <typename Kernel> hipError_t allow_lds(Kernel kernel, size_t bytes)
-{
-    if (bytes <= size_t(64) << 10) return hipSuccess;
-    return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
-}
-
 }  // namespace s3r

@@ -1701,14 +1701,14 @@ s3r_status plan_residual(const s3r_residual_params *p, bool backward, ResidualPl
     if (p->d_gate && !p->gate) return fail(S3R_ERR_INVALID_ARG, "d_gate needs a gate");
     ResidualPlan c{};
     c.batch = p->batch == 0 ? 1 : p->batch;
-    const int64_t at_once = s3r::residual_rows(p->width), most = backward ? kResidualGradBlocks : kResidualBlocks;
+    const int64_t at_once = s3r::residual_rows(p->width, p->gate || p->post_norm != S3R_NORM_NONE), most = backward ? kResidualGradBlocks : kResidualBlocks;
     const int64_t rows = ((p->n_rows + most - 1) / most + at_once - 1) / at_once * at_once;
     c.rows_per_block = static_cast<int>(rows < at_once ? at_once : rows);
     c.blocks = (p->n_rows + c.rows_per_block - 1) / c.rows_per_block;
     const size_t row = static_cast<size_t>(p->width) * sizeof(float);
     size_t off = 0;
     c.part = off;
-    if (p->d_weight || p->d_bias || p->d_scale || p->d_post_weight || p->d_post_bias) off += align_up(5 * static_cast<size_t>(c.blocks) * row);
+    if (p->d_weight || p->d_bias || p->d_scale || p->d_post_weight || p->d_post_bias) off += align_up(4 * static_cast<size_t>(c.blocks) * row);
     c.part_gate = off;
     if (p->d_gate) off += align_up((static_cast<size_t>(c.blocks) + c.batch) * row);
     c.need = off;

@@ -9,6 +9,8 @@ additions that a term of a sum over channels can pass through (8 or 16 in a lane
   turn     x c + p with the rounding of p = o s made up for: 3 u |y|, and the operands' errors times |c| and |s|.
   back     g = dn, err(g) given:  mean g is off by mean err(g) + depth u mean|g|, mean(g n) by mean(|g| err(n) + |n| err(g)) + (depth + 1) u mean|g n|;
            dz = (g - mean g - n mean(g n)) / sigma  by the sum of these, 3 u of each term, and (depth / 2 + 4) u of itself.
+  scale    and gate: dr' (n w + b) is summed as w (sum dr' n) + b (sum dr'), r is x + (s w) n + s b: the parts |n w| and |b| count each, with
+           up to three roundings more.
   sums     over rows: the terms' errors, and `chain` u times the sum of their magnitudes: rows of a wave one after the other (at most a
            512th of all, those of 16 heads), rows side by side (16), workgroups (128 in a row) and eight groups of them.
 """
@@ -70,10 +72,12 @@ def affine(n, weight, bias):
     return n if bias is None else n + given(bias)
 
 
-def sum_rows(v, rows):
-    """Over all axes but the last; rows: how many rows (of 16 heads and less) there are."""
+def sum_rows(v, rows, size=None):
+    """Over all axes but the last; rows: how many rows (of 16 heads and less) there are; size: the terms' magnitudes, where they are made
+    of parts that are summed apart."""
     flat, err = v.x.reshape(-1, v.x.shape[-1]), v.err.reshape(-1, v.x.shape[-1])
-    return Value(flat.sum(0), err.sum(0) + (170 + 16 * rows / 512) * U * flat.abs().sum(0))
+    size = flat.abs() if size is None else size.reshape(flat.shape)
+    return Value(flat.sum(0), err.sum(0) + (170 + 16 * rows / 512) * U * size.sum(0))
 
 
 # ---- rotary ----------------------------------------------------------------------------------------------
@@ -130,6 +134,9 @@ def residual(x, f=None, kind=None, weight=None, bias=None, eps=1e-6, post=None, 
     if f is not None:
         n_post, inv_post = norm(given(f), post, eps) if post else (given(f), None)
         u = affine(n_post, post_weight, post_bias)
+        n_part = n_post.x.abs() if post_weight is None else (n_post.x * post_weight.double()).abs()
+        b_part = torch.zeros_like(n_part) if post_bias is None else post_bias.double().abs().expand_as(n_part)
+        u.err = u.err + 2 * U * (n_part + b_part)
         s = Value(torch.full((1, width), residual_scale, dtype=torch.float64, device=x.device))
         s = s if scale is None else s * given(scale)
         gates = None if gate is None else Value(gate[seq])
@@ -151,11 +158,13 @@ def residual(x, f=None, kind=None, weight=None, bias=None, eps=1e-6, post=None, 
     if f is None:
         return out
     t, du = d * u, d * s
+    t.err = t.err + 3 * U * d.x.abs() * (n_part + b_part)
+    t_size = d.x.abs() * (n_part + b_part)
     few = Value(torch.full((1, 1), residual_scale, dtype=torch.float64, device=x.device))
-    out["d_scale"] = (sum_rows(t if gate is None else t * gates, rows) * few).stored(w_dtype)
+    out["d_scale"] = (sum_rows(t if gate is None else t * gates, rows, t_size if gate is None else t_size * gates.x.abs()) * few).stored(w_dtype)
     if gate is not None:
         by_scale = few if scale is None else few * given(scale)
-        parts = [sum_rows(Value(t.x[seq == b], t.err[seq == b]), rows) * by_scale for b in range(gate.shape[0])]
+        parts = [sum_rows(Value(t.x[seq == b], t.err[seq == b]), rows, t_size[seq == b]) * by_scale for b in range(gate.shape[0])]
         x_, e_ = torch.cat([p.x.reshape(1, -1) for p in parts]), torch.cat([p.err.reshape(1, -1) for p in parts])
         out["d_gate"] = Value(x_, e_).stored(dtype)
     if post:
