@@ -12,9 +12,10 @@ namespace s3r {
 
 namespace {
 
-// Where a channel's partner is: in the same lane (neighbours, axes of multiples of four pairs), at the same place of another of the
-// eight lanes (axes of multiples of eight pairs), or anywhere: then through LDS.
-enum Mode { kInLane, kAcross, kAnywhere };
+// Where a channel's partner is: in the same lane (neighbours, axes of multiples of four pairs); at the same place of the lane whose number
+// differs by 2 or 4 (all axes of 16 pairs, or one of 32), or of another of the eight (axes of multiples of eight); or anywhere: then
+// through LDS.
+enum Mode { kInLane, kAcross2, kAcross4, kAcross, kAnywhere };
 
 struct Channel { int pair, partner, axis; bool turned, second; };
 __device__ __forceinline__ Channel channel_of(const RotaryArgs &a, int c)
@@ -40,9 +41,16 @@ __device__ __forceinline__ Channel channel_of(const RotaryArgs &a, int c)
     return r;
 }
 
-// Cosines and sines of a lane's eight channels of a row, the sines with the sign that the channel's half of the pair takes (times
-// `sign`), and where its partners are.
-template <Mode MODE> struct Turn {
+// The value of the lane whose number differs by BIT (2 or 4), without a trip to LDS.
+template <int BIT> __device__ __forceinline__ float other_lane(float x)
+{
+    if constexpr (BIT == 2) return lane_moved<0x4e>(x);
+    return lane_moved<0x1b>(lane_moved<0x141>(x));  // the mirror of eight lanes, and that of four
+}
+
+// Cosines and sines of a lane's eight channels of a row, the sines with the sign that the channel's half of the pair takes times
+// that of the rotation, and where its partners are.
+template <typename T, Mode MODE> struct Turn {
     float co[8], si[8];
     int from;            // kAcross: lane of the partners, times 4
     int at[8];           // kAnywhere: of the partners in LDS; -1: not turned
@@ -61,7 +69,7 @@ template <Mode MODE> struct Turn {
             from = 4 * ((lane & 56) + (channel_of(a, 8 * c).partner >> 3));
         }
     }
-    __device__ __forceinline__ void load(const RotaryArgs &a, int64_t row, int lane)
+    __device__ __forceinline__ void load(const RotaryArgs &a, int64_t row, int lane, float sign)
     {
         const int c = lane & 7;
         int64_t where[3];
@@ -77,56 +85,58 @@ template <Mode MODE> struct Turn {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const Channel ch = channel_of(a, 8 * c + j);
-                co[j] = 1.f;
-                si[j] = 0.f;
-                if (!ch.turned) continue;
+                // (channels that are not turned take another's angle, which goes unused)
                 const int64_t i = (ch.axis == 0 ? where[0] : (ch.axis == 1 ? where[1] : where[2])) + ch.pair;
-                co[j] = a.cos[i];
-                si[j] = ch.second ? a.sin[i] : -a.sin[i];
+                co[j] = a.cos[ch.turned ? i : where[0]];
+                si[j] = a.sin[ch.turned ? i : where[0]] * (ch.second ? sign : -sign);
             }
         } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) { co[j] = 1.f; si[j] = 0.f; }
-            if (!turned) return;
-            const int64_t i = (first.axis == 0 ? where[0] : (first.axis == 1 ? where[1] : where[2])) + first.pair;
+            const int64_t i = turned ? (first.axis == 0 ? where[0] : (first.axis == 1 ? where[1] : where[2])) + first.pair : where[0];
             if constexpr (MODE == kInLane) {
                 const floatx4 x = *reinterpret_cast<const floatx4 *>(a.cos + i), y = *reinterpret_cast<const floatx4 *>(a.sin + i);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) { co[j] = x[j >> 1]; si[j] = (j & 1) != 0 ? y[j >> 1] : -y[j >> 1]; }
+                for (int j = 0; j < 8; ++j) { co[j] = x[j >> 1]; si[j] = y[j >> 1] * ((j & 1) != 0 ? sign : -sign); }
             } else {
                 Io8<float> x, y;
                 x.load(a.cos + i);
                 y.load(a.sin + i);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) { co[j] = x.get(j); si[j] = first.second ? y.get(j) : -y.get(j); }
+                for (int j = 0; j < 8; ++j) { co[j] = x.get(j); si[j] = y.get(j) * (first.second ? sign : -sign); }
             }
         }
     }
-    // x cos + (partner) sin, with the rounding of the second product made up for (a sum of products that cancel keeps its bits; where an
-    // infinity makes that NaN, the sum as it is).  sign: 1, or -1 to turn back.  lds: 512 floats of the wave's own.
-    __device__ __forceinline__ void apply(const float (&x)[8], float (&y)[8], float sign, float *lds, int lane) const
+    // x cos + (partner) sin.  fp32: with the rounding of the second product made up for (a sum of products that cancel keeps its bits; where
+    // an infinity makes that NaN, the sum as it is).  lds: 512 floats of the wave's own.
+    __device__ __forceinline__ void apply(const RotaryArgs &a, const float (&x)[8], float (&y)[8], float *lds, int lane) const
     {
         float other[8];
-        if constexpr (MODE == kInLane) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) other[j] = x[j ^ 1];
-        } else if constexpr (MODE == kAcross) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) other[j] = __uint_as_float(static_cast<unsigned>(__builtin_amdgcn_ds_bpermute(from, static_cast<int>(__float_as_uint(x[j])))));
-        } else {
+        if constexpr (MODE == kAnywhere) {
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
             for (int j = 0; j < 8; ++j) lds[64 * j + lane] = x[j];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-            for (int j = 0; j < 8; ++j) other[j] = lds[at[j] < 0 ? 0 : at[j]];
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float s = sign * si[j], p = other[j] * s, rest = fmaf(other[j], s, -p), sum = fmaf(x[j], co[j], p), whole = sum + rest;
-            const bool is_turned = MODE == kAnywhere ? at[j] >= 0 : turned;
-            y[j] = !is_turned ? x[j] : (whole == whole ? whole : sum);
+            if constexpr (MODE == kInLane) other[j] = x[j ^ 1];
+            if constexpr (MODE == kAcross2) other[j] = other_lane<2>(x[j]);
+            if constexpr (MODE == kAcross4) other[j] = other_lane<4>(x[j]);
+            if constexpr (MODE == kAcross)
+                other[j] = __uint_as_float(static_cast<unsigned>(__builtin_amdgcn_ds_bpermute(from, static_cast<int>(__float_as_uint(x[j])))));
+            if constexpr (MODE == kAnywhere) other[j] = lds[at[j] < 0 ? 0 : at[j]];
         }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float p = other[j] * si[j];
+            y[j] = fmaf(x[j], co[j], p);
+            if constexpr (sizeof(T) == 4) {
+                const float whole = y[j] + fmaf(other[j], si[j], -p);
+                y[j] = whole == whole ? whole : y[j];
+            }
+        }
+        if (a.n_pairs < 32)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = (MODE == kAnywhere ? at[j] >= 0 : turned) ? y[j] : x[j];
     }
 };
 
@@ -149,15 +159,11 @@ __device__ __forceinline__ float head_norm(const RotaryArgs &a, const float (&x)
         s2 = fmaf(n[j], n[j], s2);
     }
     s2 = sum_over_lanes<8>(s2) * (1.f / 64);
-    if (a.norm == kNormLayer) {
-        s1 = sum_over_lanes<8>(s1) * (1.f / 64);
-        s2 = fmaxf(fmaf(-s1, s1, s2), 0.f) + 0.f * s2;  // (a NaN stays one)
+    s1 = a.norm == kNormLayer ? sum_over_lanes<8>(s1) * (1.f / 64) : 0.f;
+    const float inv = inverse_root(fmaxf(fmaf(-s1, s1, s2), 0.f) + 0.f * s2 + a.eps);  // (a NaN stays one)
+    s1 *= -inv;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) n[j] -= s1;
-    }
-    const float inv = inverse_root(s2 + a.eps);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) n[j] *= inv;
+    for (int j = 0; j < 8; ++j) n[j] = fmaf(n[j], inv, s1);
     return inv;
 }
 
@@ -193,10 +199,10 @@ template <typename T, Mode MODE, bool NORM> __global__ __launch_bounds__(256) vo
     const RotarySide s = side == 0 ? a.side[0] : a.side[1];
     const int c = lane & 7;
     const int64_t row = r.ok ? r.row : 0;
-    Turn<MODE> turn;
+    Turn<T, MODE> turn;
     const bool turns = a.cos != nullptr;
     turn.place(a, lane);
-    if (turns) turn.load(a, row, lane);
+    if (turns) turn.load(a, row, lane, a.sign);
     float w[8], b[8];
     if constexpr (NORM) {
         load_weights(s.weight, a.w_bf16, 8 * c, true, 1.f, w);
@@ -221,7 +227,7 @@ template <typename T, Mode MODE, bool NORM> __global__ __launch_bounds__(256) vo
                 for (int j = 0; j < 8; ++j) x[j] = fmaf(y[j], w[j], b[j]);
             }
             if (turns) {
-                turn.apply(x, y, a.sign, lds, lane);
+                turn.apply(a, x, y, lds, lane);
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) y[j] = x[j];
@@ -242,7 +248,7 @@ template <typename T, Mode MODE> __global__ __launch_bounds__(256) void rotary_n
     const RotarySide s = side == 0 ? a.side[0] : a.side[1];
     const int64_t items = (a.n_rows + 7) / 8 * ((s.heads + run - 1) / run);
     const int c = lane & 7;
-    Turn<MODE> turn;
+    Turn<T, MODE> turn;
     const bool turns = a.cos != nullptr;
     turn.place(a, lane);
     float w[8], dw[8], db[8];
@@ -252,7 +258,7 @@ template <typename T, Mode MODE> __global__ __launch_bounds__(256) void rotary_n
     for (int64_t item = (static_cast<int64_t>(blockIdx.x) - first) * 4 + wave; item < items; item += 4 * wgs) {
         const HeadRun r = head_run(a, item, side, run, lane);
         const int64_t row = r.ok ? r.row : 0;
-        if (turns) turn.load(a, row, lane);
+        if (turns) turn.load(a, row, lane, -1.f);
         const T *in = static_cast<const T *>(s.in) + row * s.in_row + 8 * c, *grad = static_cast<const T *>(s.grad) + row * s.heads * 64 + 8 * c;
         T *out = static_cast<T *>(s.out) + row * s.out_row + 8 * c;
         for (int h0 = r.h0; h0 < r.h1; h0 += kAhead<T>) {
@@ -270,7 +276,7 @@ template <typename T, Mode MODE> __global__ __launch_bounds__(256) void rotary_n
 #pragma unroll
                 for (int j = 0; j < 8; ++j) { x[j] = raw[i].get(j); n[j] = raw_g[i].get(j); }
                 if (turns) {
-                    turn.apply(n, g, -1.f, lds, lane);
+                    turn.apply(a, n, g, lds, lane);
                 } else {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) g[j] = n[j];
@@ -287,10 +293,10 @@ template <typename T, Mode MODE> __global__ __launch_bounds__(256) void rotary_n
                     s1 += g[j];
                     s2 = fmaf(g[j], n[j], s2);
                 }
-                s1 = a.norm == kNormLayer ? sum_over_lanes<8>(s1) * (1.f / 64) : 0.f;
-                s2 = sum_over_lanes<8>(s2) * (1.f / 64);
+                s1 = a.norm == kNormLayer ? sum_over_lanes<8>(s1) * (-inv / 64) : 0.f;
+                s2 = sum_over_lanes<8>(s2) * (-inv / 64);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = inv * (g[j] - s1 - n[j] * s2);
+                for (int j = 0; j < 8; ++j) x[j] = fmaf(n[j], s2, fmaf(g[j], inv, s1));
                 if (r.ok) Io8<T>::store(out + (h0 + i) * s.out_head, x);
             }
         }
@@ -358,38 +364,59 @@ Mode mode_of(const RotaryArgs &a)
         while (a.axis_pairs[x] % common != 0) common /= 2;
     if (a.axes == 0) return kInLane;
     if (a.pairing == kPairsNeighbours) return common >= 4 ? kInLane : kAnywhere;
-    return common == 8 ? kAcross : kAnywhere;
+    if (common < 8) return kAnywhere;
+    const int half = a.pairing == kPairsWhole ? a.n_pairs : a.axis_pairs[0];  // channels from one of a pair to the other
+    for (int x = 1; x < a.axes; ++x)
+        if (a.pairing == kPairsHalves && a.axis_pairs[x] != half) return kAcross;
+    return half == 16 ? kAcross2 : (half == 32 ? kAcross4 : kAcross);
 }
 
-// Heads that a wave takes in a row: as many, up to 16, as leave the card 8192 waves (eight for each of 1024 SIMDs).
-int run_of_heads(const RotaryArgs &a)
+// Heads that a wave takes in a row: as many as leave the card 2048 waves, up to 4, 8 through a norm's gradient (more to be read for the
+// same angles), 16 where partners are looked up (whose places take longest to find).  us, 1 / 2 / 4 / 8 / 16 of them: 27480 rows of 16 + 16
+// heads, norm and rotation 67 / 41 / 36 / 37 / 38, with the gradient 209 / 139 / 118 / 114 / 114, axes of 10, 11 and 11 pairs 370 / 229 /
+// 168 / - / 133; 3001 rows of 15 + 5 heads in fp32 with the gradient 45 / 36 / 34 / 34 / 38.
+int run_of_heads(const RotaryArgs &a, Mode mode, bool grad)
 {
+    const int most = mode == kAnywhere ? 16 : (grad ? 8 : 4);
     int run = 1;
-    while (run < 16 && (a.n_rows + 7) / 8 * ((a.side[0].heads + a.side[1].heads + 2 * run - 1) / (2 * run)) >= 8192) run *= 2;
+    auto waves = [&](int r) { return (a.n_rows + 7) / 8 * ((a.side[0].heads + r - 1) / r + (a.side[1].heads + r - 1) / r); };
+    while (run < most && waves(2 * run) >= 2048) run *= 2;
     return run;
 }
 
 int64_t items_of(const RotaryArgs &a, int side, int run) { return (a.n_rows + 7) / 8 * ((a.side[side].heads + run - 1) / run); }
 
+template <typename T, Mode MODE> auto rotary_kernel_of(bool norm) { return norm ? &rotary_kernel<T, MODE, true> : &rotary_kernel<T, MODE, false>; }
+
 template <typename T> hipError_t launch_rotary_t(const RotaryArgs &a, hipStream_t stream)
 {
-    const int run = run_of_heads(a);
+    const Mode mode = mode_of(a);
+    const int run = run_of_heads(a, mode, false);
     const int64_t blocks = (items_of(a, 0, run) + items_of(a, 1, run) + 3) / 4;
     if (blocks <= 0 || blocks > 0xffffff) return hipErrorInvalidValue;
-    const Mode mode = mode_of(a);
     const bool norm = a.norm != kNormNone;
-    auto kernel = mode == kInLane ? (norm ? &rotary_kernel<T, kInLane, true> : &rotary_kernel<T, kInLane, false>)
-                : mode == kAcross ? (norm ? &rotary_kernel<T, kAcross, true> : &rotary_kernel<T, kAcross, false>)
-                                  : (norm ? &rotary_kernel<T, kAnywhere, true> : &rotary_kernel<T, kAnywhere, false>);
+    auto kernel = rotary_kernel_of<T, kAnywhere>(norm);
+    switch (mode) {
+    case kInLane: kernel = rotary_kernel_of<T, kInLane>(norm); break;
+    case kAcross2: kernel = rotary_kernel_of<T, kAcross2>(norm); break;
+    case kAcross4: kernel = rotary_kernel_of<T, kAcross4>(norm); break;
+    case kAcross: kernel = rotary_kernel_of<T, kAcross>(norm); break;
+    case kAnywhere: break;
+    }
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a, run);
     return hipGetLastError();
 }
 
-template <typename T> hipError_t launch_norm_grad_t(const RotaryArgs &a, int run, int wgs_q, int wgs, hipStream_t stream)
+template <typename T> hipError_t launch_norm_grad_t(const RotaryArgs &a, Mode mode, int run, int wgs_q, int wgs, hipStream_t stream)
 {
-    const Mode mode = mode_of(a);
-    auto kernel = mode == kInLane ? &rotary_norm_grad_kernel<T, kInLane>
-                : mode == kAcross ? &rotary_norm_grad_kernel<T, kAcross> : &rotary_norm_grad_kernel<T, kAnywhere>;
+    auto kernel = &rotary_norm_grad_kernel<T, kAnywhere>;
+    switch (mode) {
+    case kInLane: kernel = &rotary_norm_grad_kernel<T, kInLane>; break;
+    case kAcross2: kernel = &rotary_norm_grad_kernel<T, kAcross2>; break;
+    case kAcross4: kernel = &rotary_norm_grad_kernel<T, kAcross4>; break;
+    case kAcross: kernel = &rotary_norm_grad_kernel<T, kAcross>; break;
+    case kAnywhere: break;
+    }
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(wgs)), dim3(256), 0, stream, a, run, wgs_q);
     return hipGetLastError();
 }
@@ -403,16 +430,17 @@ hipError_t launch_rotary(const RotaryArgs &a, bool is_bf16, hipStream_t stream)
 
 hipError_t launch_rotary_norm_grad(const RotaryArgs &a, bool is_bf16, hipStream_t stream)
 {
-    const int run = run_of_heads(a);
+    const Mode mode = mode_of(a);
+    const int run = run_of_heads(a, mode, true);
     const int64_t of_q = items_of(a, 0, run), of_k = items_of(a, 1, run);
-    // workgroups of q and of k by their share of the work, at least one for either that has any
-    const int64_t most_q = (of_q + 3) / 4, most_k = (of_k + 3) / 4;
-    int64_t q = of_q + of_k > 0 ? kRotaryGradGroups * of_q / (of_q + of_k) : 0, k = kRotaryGradGroups - q;
-    if (of_q > 0 && q == 0) { q = 1; k -= 1; }
-    if (of_k > 0 && k == 0) { k = 1; q -= 1; }
-    const int wgs_q = static_cast<int>(q < most_q ? q : most_q), wgs = wgs_q + static_cast<int>(k < most_k ? k : most_k);
+    // the same number of items for every wave, or one less, in as many workgroups as there is room for (27480 rows of 16 + 16 heads 114 us, in
+    // 1024 122; axes of 10, 11 and 11 pairs 133, in 512 127)
+    int64_t each = 1;
+    const int most = mode == kAnywhere ? 512 : kRotaryGradGroups;
+    while ((of_q + 4 * each - 1) / (4 * each) + (of_k + 4 * each - 1) / (4 * each) > most) ++each;
+    const int wgs_q = static_cast<int>((of_q + 4 * each - 1) / (4 * each)), wgs = wgs_q + static_cast<int>((of_k + 4 * each - 1) / (4 * each));
     hipError_t e = hipSuccess;
-    if (wgs > 0) e = is_bf16 ? launch_norm_grad_t<bf16_t>(a, run, wgs_q, wgs, stream) : launch_norm_grad_t<float>(a, run, wgs_q, wgs, stream);
+    if (wgs > 0) e = is_bf16 ? launch_norm_grad_t<bf16_t>(a, mode, run, wgs_q, wgs, stream) : launch_norm_grad_t<float>(a, mode, run, wgs_q, wgs, stream);
     if (e != hipSuccess || a.part == nullptr) return e;
     hipLaunchKernelGGL(rotary_weight_grad_kernel, dim3(16), dim3(1024), 0, stream, a, wgs_q, wgs);
     return hipGetLastError();

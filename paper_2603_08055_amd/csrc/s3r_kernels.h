@@ -381,7 +381,7 @@ struct RotarySide {
 
 // cos, sin [places][n_pairs], or null: no rotation; axis_pairs: pairs of each axis, n_pairs their sum.  sign: -1 turns back.  part:
 // [kRotaryGradGroups][2][64], or null: no gradients of weights.
-constexpr int kRotaryGradGroups = 1024;
+constexpr int kRotaryGradGroups = 2048;
 struct RotaryArgs {
     RotarySide side[2];
     const float *cos, *sin;

@@ -6,7 +6,7 @@ additions that a term of a sum over channels can pass through (8 or 16 in a lane
   norm     The mean is taken twice: what is left of its error is that of the sum of the centred values, depth u mean|d|, and of the subtraction,
            u |d|, u more for the second.  The sum of squares is off by (depth + 2) u of itself, its inverse root by half of that and 3 u.  With
            mean|d| <= sigma:  err(n) = u ((depth / 2 + 8) |n| + depth + 3).  An error e of z itself adds (e + mean e + |n| mean(|n| e)) / sigma.
-  turn     x c + p with the rounding of p = o s made up for: 3 u |y|, and the operands' errors times |c| and |s|.
+  turn     x c + p, in fp32 with the rounding of p = o s made up for: 3 u |y|, in bf16 u |o s| more, and the operands' errors times |c| and |s|.
   back     g = dn, err(g) given:  mean g is off by mean err(g) + depth u mean|g|, mean(g n) by mean(|g| err(n) + |n| err(g)) + (depth + 1) u mean|g n|;
            dz = (g - mean g - n mean(g n)) / sigma  by the sum of these, 3 u of each term, and (depth / 2 + 4) u of itself.
   scale    and gate: dr' (n w + b) is summed as w (sum dr' n) + b (sum dr'), r is x + (s w) n + s b: the parts |n w| and |b| count each, with
@@ -93,14 +93,18 @@ def pair_channels(axis_pairs, pairs):
     return out
 
 
-def turn(v, cos, sin, at, axis_pairs, pairs, sign=1.0):
+def turn(v, cos, sin, at, axis_pairs, pairs, dtype, sign=1.0):
     """v [n, heads, 64]; at [n, axes]: rows of the tables, held into them."""
     x, err = v.x.clone(), v.err.clone()
     at = at.long().clamp(0, cos.shape[0] - 1)
     for j, (a, b, axis) in enumerate(pair_channels(axis_pairs, pairs)):
         c, s = cos[at[:, axis], j].double()[:, None], sign * sin[at[:, axis], j].double()[:, None]
         x[..., a], x[..., b] = v.x[..., a] * c - v.x[..., b] * s, v.x[..., b] * c + v.x[..., a] * s
+        size = v.x[..., a].abs() * c.abs() + v.x[..., b].abs() * s.abs(), v.x[..., b].abs() * c.abs() + v.x[..., a].abs() * s.abs()
         err[..., a], err[..., b] = v.err[..., a] * c.abs() + v.err[..., b] * s.abs(), v.err[..., b] * c.abs() + v.err[..., a] * s.abs()
+        if dtype != torch.float32:
+            err[..., a] += U * size[0]
+            err[..., b] += U * size[1]
     return Value(x, err + 3 * U * x.abs())
 
 
@@ -109,12 +113,12 @@ def rotary(x, weight, bias, cos, sin, at, axis_pairs, pairs, kind, eps, d_out=No
     turns = cos is not None
     n, inv = norm(given(x), kind, eps) if kind else (given(x), None)
     y = affine(n, weight, bias)
-    y = turn(y, cos, sin, at, axis_pairs, pairs) if turns else y
+    y = turn(y, cos, sin, at, axis_pairs, pairs, x.dtype) if turns else y
     r = {"out": y.stored(x.dtype)}
     if d_out is None:
         return r
     g = given(d_out)
-    g = turn(g, cos, sin, at, axis_pairs, pairs, -1.0) if turns else g
+    g = turn(g, cos, sin, at, axis_pairs, pairs, x.dtype, -1.0) if turns else g
     w_dtype = x.dtype if weight is None else weight.dtype
     if kind:
         rows = x.shape[0]
