@@ -301,6 +301,8 @@ hipError_t launch_cross(const CrossArgs &a, bool few_rows, bool is_bf16, hipStre
 // n_split: at most kMostSplits
 constexpr int kMostSplits = 256;
 hipError_t launch_soft_combine(const SoftOut &to, const Spans &spans, int n_split, bool is_bf16, hipStream_t stream);
+// Of causal rows, many of them (few: the above).
+hipError_t launch_causal_combine(const CrossArgs &a, bool is_bf16, hipStream_t stream);
 // The gradient of queries comes first: it leaves stats [heads][n_q][2], of every row its log-sum in log2 (+inf for a row without keys)
 // and -(out . d_out), from to.out, to.lse and d_out.
 // bf16: D in stats is made whole there (n_split > 1: by the combine launch).

@@ -1088,6 +1088,33 @@ int64_t mean_tiles(int64_t n, int per_row, int tile, int batch)
     return some * (each < 1 ? 1 : (each + tile - 1) / tile);
 }
 
+// The same for causal rows: `tiles` (heads counted) walk from `shortest` to `longest` units, as many of each, and all are divided alike.  They
+// are taken the longest first, so that the short ones fill the CUs up.  The work takes its time at the pace of as many workgroups as a CU
+// has (alone half as long again), and the longest piece twice its share at the pace of a full CU, or 1.6 times where two fill it; joining
+// 9 us and `tile_bytes` of a tile's piece, out and in again.
+// Measured (1, 2, 3, 4 .. pieces), us: forward, bf16, 4096 rows of 16 heads that share 4 87 / 75 / 79 / 87, 1374 of 16 38 / 31 / 32 / 33, 512 over
+// 16384 285 / 156 / 112 / 93, 8 69, 12 67, 16 66, 32 75, 8192 in three sequences 93 / 108 / 119 / 134; the whole step with gradients of keys
+// in these: 8192 in three sequences 599 / 437 / 398 / 385, 6 391, 8 420; 4096 568 / 388 / 337 / 310, 6 293, 8 302.
+int causal_pieces(double tiles, double shortest, double longest, const Pace &pace, double tile_bytes)
+{
+    const double all = tiles * (shortest + longest) / 2 / 256 * pace.unit_us, alone = pace.resident > 2 ? 2.0 : (pace.resident > 1 ? 1.6 : 1.1);
+    auto time_us = [&](int n) {
+        const double on_a_cu = tiles * n / 256, k = on_a_cu < 1 ? 1 : (on_a_cu > pace.resident ? pace.resident : on_a_cu);
+        const double work = all * (pace.resident > 1 ? 1.5 - 0.5 * (k - 1) / (pace.resident - 1) : 1.0), piece = alone * longest / n * pace.unit_us;
+        return (work > piece ? work : piece) + (n == 1 ? 0.0 : 9.0 + tiles * n * tile_bytes * 2 / 5e6);
+    };
+    int best = 1;
+    double least_us = time_us(1);
+    for (int n = 2; n <= s3r::kMostSplits && longest >= static_cast<double>(pace.least) * n; ++n) {
+        const double us = time_us(n);
+        if (us < 0.99 * least_us) {
+            least_us = us;
+            best = n;
+        }
+    }
+    return best;
+}
+
 struct CrossPlan {
     bool few_rows;
     int batch, per_row, split, least, split_q, split_kv;
@@ -1119,9 +1146,7 @@ s3r_status plan_cross(const s3r_cross_params *p, int view, CrossPlan *out)
     auto units_of = [&](int64_t rows) { return ((uneven ? (4 * rows / c.batch < rows ? 4 * rows / c.batch : rows) : rows) + 63) / 64; };
     auto split_of = [&](int64_t tiles, int64_t held, int per_row, int64_t streamed, const Pace &pace, double part_bytes) {
         if (!uneven) return pieces(tiles * p->kv_heads, units_of(streamed), pace, part_bytes);
-        // (a causal sequence alone is uneven by what its own rows do not see: two workgroups on a CU)
-        const int64_t mean = streamed / c.batch / 64 + 1, level = c.batch > 1 || mean < 32 ? mean : 32;
-        return pieces_uneven(mean_tiles(held, per_row, 128, c.batch) * p->kv_heads, level, units_of(streamed), pace);
+        return pieces_uneven(mean_tiles(held, per_row, 128, c.batch) * p->kv_heads, streamed / c.batch / 64 + 1, units_of(streamed), pace);
     };
     const int64_t items = p->n_q * c.per_row, units = units_of(p->n_kv);
     const double q_bytes = 256.0 * static_cast<double>(p->n_q) * p->heads, kv_bytes = 512.0 * static_cast<double>(p->n_kv) * p->kv_heads;
@@ -1139,6 +1164,18 @@ s3r_status plan_cross(const s3r_cross_params *p, int view, CrossPlan *out)
     c.split_q = split_of(c.q_tiles, p->n_q, c.per_row, p->n_kv, kGradQPace[bf16], bf16 ? 2 * q_bytes : q_bytes);
     c.kv_tiles = s3r::most_tiles(p->n_kv, 1, 128, c.batch);
     c.split_kv = split_of(c.kv_tiles, p->n_kv, 1, items, kGradKvPace[bf16], kv_bytes);
+    if (view > 0) {
+        // Of several sequences only the sums of their lengths are known: the longest is taken to be 1.75 times their mean.
+        const double n = static_cast<double>(p->n_q) / c.batch, m = static_cast<double>(p->n_kv) / c.batch, v = view < m ? view : m;
+        const double spread = c.batch > 1 ? 1.75 : 1.0, first = m > n ? m - n + v : v;
+        const double most = m * spread / 64 + 0.5, least = first < m ? first / 64 + 0.5 : most;
+        const double q_tiles = static_cast<double>(mean_tiles(p->n_q, c.per_row, 128, c.batch)) * p->kv_heads, tile_bytes = 128.0 * 256;
+        if (!c.few_rows) c.split = causal_pieces(q_tiles, least, most, kCrossPace[bf16], tile_bytes);
+        c.split_q = causal_pieces(q_tiles, least, most, kGradQPace[bf16], bf16 ? 2 * tile_bytes : tile_bytes);
+        // Keys: the first ones are seen by all rows, the last ones by a view's, or by all where there are earlier tokens.
+        const double rows = n * c.per_row / 64, kv_tiles = static_cast<double>(mean_tiles(p->n_kv, 1, 128, c.batch)) * p->kv_heads;
+        c.split_kv = causal_pieces(kv_tiles, (m > n ? rows * (m - n) / m : 0.0) + 0.5, rows * spread + 0.5, kGradKvPace[bf16], 2 * tile_bytes);
+    }
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
     const size_t rows = static_cast<size_t>(p->n_q) * p->heads, keys = static_cast<size_t>(p->n_kv) * p->kv_heads;
@@ -1223,7 +1260,9 @@ s3r_status cross_forward(const s3r_cross_params *p, int view)
     }
     StageTimer tm(S3R_STAGE_DENSE, s);
     S3R_HIP(s3r::launch_cross(a, c.few_rows, bf16, s), "cross attention kernel launch");
-    if (c.split > 1) S3R_HIP(s3r::launch_soft_combine(a.to, a.q_spans, c.split, bf16, s), "cross attention combine kernel launch");
+    if (c.split > 1)
+        S3R_HIP(view > 0 && !c.few_rows ? s3r::launch_causal_combine(a, bf16, s) : s3r::launch_soft_combine(a.to, a.q_spans, c.split, bf16, s),
+                "cross attention combine kernel launch");
     return S3R_OK;
 }
 
