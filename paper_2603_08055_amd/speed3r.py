@@ -656,12 +656,7 @@ _NORMS = {None: S3R_NORM_NONE, "rms": S3R_NORM_RMS, "layer": S3R_NORM_LAYER}
 _PAIRS = {"halves": S3R_PAIRS_HALVES, "neighbours": S3R_PAIRS_NEIGHBOURS, "whole": S3R_PAIRS_WHOLE}
 
 
-def _weight_type(dtype, *weights):
-    """The type that the weights given have in common (none: that of the rows)."""
-    for w in weights:
-        if w is not None:
-            return w.dtype
-    return dtype
+_ONE_AXIS = (32,)
 
 
 _CODES = {torch.float32: S3R_F32, torch.bfloat16: S3R_BF16}
@@ -674,55 +669,61 @@ def _code(dtype, name):
     return code
 
 
+def _weight_args(p, weights, dtype, index, shape):
+    """Puts weights (by name) and the type that they have in common (none given: that of the rows) into p."""
+    w_dtype = None
+    for name, w in weights.items():
+        if w is not None:
+            if w_dtype is None:
+                w_dtype = w.dtype
+            setattr(p, name, _arg(w, name, index, w_dtype, shape))
+    p.weight_dtype = _code(w_dtype or dtype, "a weight")
+
+
 def _rotary_params(like_q, like_k, cos, sin, positions, axis_pairs, pairs, norm, eps, weights, status, stream, index):
-    """weights: q_weight, q_bias, k_weight, k_bias and their gradients."""
-    dtype = None
-    p = s3r_rotary_params()
-    for t, name in ((like_q, "q"), (like_k, "k")):
-        if t is None:
-            continue
-        if t.dim() != 3:
-            raise ValueError(f"{name} must be [n_rows, heads, head_dim]")
-        if dtype is not None and (t.dtype is not dtype or t.shape[0] != p.n_rows or t.shape[2] != p.head_dim):
+    """weights: q_weight, q_bias, k_weight, k_bias and their gradients, by name."""
+    like, heads, kv_heads = like_k if like_q is None else like_q, 0, 0
+    if like.dim() != 3 or (like_k is not None and like_k.dim() != 3):
+        raise ValueError("q and k must be [n_rows, heads, head_dim]")
+    n_rows, heads, head_dim = like.shape
+    dtype = like.dtype
+    if like_q is None:
+        heads, kv_heads = 0, heads
+    elif like_k is not None:
+        k_rows, kv_heads, k_dim = like_k.shape
+        if k_rows != n_rows or k_dim != head_dim or like_k.dtype is not dtype:
             raise ValueError("q and k must share dtype, rows and head_dim")
-        dtype = t.dtype
-        p.n_rows, heads, p.head_dim = t.shape
-        if name == "q":
-            p.heads = heads
-        else:
-            p.kv_heads = heads
-    p.dtype = _code(dtype, "q or k")
     if pairs not in _PAIRS:
         raise ValueError(f"pairs must be one of {list(_PAIRS)}")
     if norm not in _NORMS:
         raise ValueError(f"norm must be one of {list(_NORMS)}")
-    p.pairs, p.norm, p.eps = _PAIRS[pairs], _NORMS[norm], eps
+    p = s3r_rotary_params()
+    p.n_rows, p.heads, p.kv_heads, p.head_dim, p.dtype, p.pairs = n_rows, heads, kv_heads, head_dim, _code(dtype, "q or k"), _PAIRS[pairs]
     if cos is not None:
-        axis_pairs = (32,) if axis_pairs is None else tuple(axis_pairs)
+        if axis_pairs is None:
+            axis_pairs = _ONE_AXIS
         if not 1 <= len(axis_pairs) <= 3:
             raise ValueError("axis_pairs must name 1 to 3 axes")
-        p.axes = len(axis_pairs)
-        total = 0
+        p.axes, total, sizes = len(axis_pairs), 0, p.axis_pairs
         for i, n in enumerate(axis_pairs):
-            p.axis_pairs[i] = n
+            sizes[i] = n
             total += n
         if cos.dim() != 2:
             raise ValueError("cos and sin must be [n_positions, pairs]")
-        p.n_positions = cos.shape[0]
         table = (cos.shape[0], total)
-        p.cos, p.sin = _arg(cos, "cos", index, torch.float32, table), _arg(sin, "sin", index, torch.float32, table)
+        p.n_positions, p.cos, p.sin = table[0], _arg(cos, "cos", index, torch.float32, table), _arg(sin, "sin", index, torch.float32, table)
         if positions is not None:
             if p.axes == 1 and positions.dim() == 1:
                 positions = positions[:, None]
-            p.positions = _arg(positions, "positions", index, torch.int32, (p.n_rows, p.axes))
+            p.positions = _arg(positions, "positions", index, torch.int32, (n_rows, p.axes))
     elif sin is not None or positions is not None or axis_pairs is not None:
         raise ValueError("sin, positions and axis_pairs need cos")
-    w_dtype = _weight_type(dtype, *weights.values())
-    p.weight_dtype = _code(w_dtype, "a weight")
-    for name, w in weights.items():
-        if w is not None:
-            setattr(p, name, _arg(w, name, index, w_dtype, (p.head_dim,)))
-    p.status, p.stream = _arg(status, "status", index, torch.int32, (1,)), _stream_of(stream, index)
+    if norm is not None:
+        p.norm, p.eps = _NORMS[norm], eps
+    _weight_args(p, weights, dtype, index, (head_dim,))
+    if status is not None:
+        p.status = _arg(status, "status", index, torch.int32, (1,))
+    p.stream = _stream_of(stream, index)
     return p
 
 
@@ -811,17 +812,16 @@ def _residual_params(x, like, f, norm, post_norm, eps, weights, gate, row_start,
     p.x, p.x_stride = _matrix_arg(x, "x", index, x.dtype, shape)
     if f is not None:
         p.f, p.f_stride = _matrix_arg(f, "f", index, dtype, shape)
-    w_dtype = _weight_type(dtype, *weights.values())
-    p.weight_dtype = _code(w_dtype, "a weight")
-    for name, w in weights.items():
-        if w is not None:
-            setattr(p, name, _arg(w, name, index, w_dtype, (width,)))
+    _weight_args(p, weights, dtype, index, (width,))
     p.batch = 1 if row_start is None else row_start.numel() - 1
     if gate is not None:
         p.gate, p.gate_stride = _matrix_arg(gate, "gate", index, dtype, (p.batch, width))
-    p.row_start = _arg(row_start, "row_start", index, torch.int32, (p.batch + 1,))
+    if row_start is not None:
+        p.row_start = _arg(row_start, "row_start", index, torch.int32, (p.batch + 1,))
     p.norm, p.post_norm, p.eps, p.residual_scale = _NORMS[norm], _NORMS[post_norm], eps, residual_scale
-    p.status, p.stream = _arg(status, "status", index, torch.int32, (1,)), _stream_of(stream, index)
+    if status is not None:
+        p.status = _arg(status, "status", index, torch.int32, (1,))
+    p.stream = _stream_of(stream, index)
     return p
 
 
