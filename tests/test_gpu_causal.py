@@ -139,6 +139,25 @@ def test_packed_sequences_and_masks(s3r, dtype, which, view):
         compare(got, reference(q, k, v, spans, view, d_out, mask))
 
 
+def lengths(seed, count, lo, hi):
+    return torch.randint(lo, hi, (count,), generator=torch.Generator().manual_seed(seed)).tolist()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("view", [1, 90])
+@pytest.mark.parametrize("count,lo,hi,earlier,heads,kv_heads", [
+    (70, 70, 150, 0, 2, 2),          # more sequences than a wave has lanes, 128 rows and fewer in each
+    (64, 1, 300, 0, 3, 1), (65, 40, 200, 300, 2, 1), (5, 300, 1200, 0, 2, 1), (3, 129, 700, 2000, 4, 4), (2, 1, 2, 5000, 8, 1), (40, 0, 400, 100, 1, 1)])
+def test_many_rows_of_many_sequences(s3r, dtype, view, count, lo, hi, earlier, heads, kv_heads):
+    """Tiles by their lengths over all sequences, in one piece and in several."""
+    rows = lengths(count, count, lo, hi)
+    keys = [r + x for r, x in zip(rows, lengths(count + 1, count, 0, earlier + 1))]
+    q, k, v, d_out = inputs(count + view, sum(rows), sum(keys), heads, kv_heads, dtype)
+    a, b = starts(rows), starts(keys)
+    spans = [(int(x), r, int(y), c) for x, y, r, c in zip(a, b, rows, keys)]
+    compare(run(s3r, q, k, v, d_out, view, q_start=a, kv_start=b), reference(q, k, v, spans, view, d_out))
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("n,m,view,heads,kv_heads", [(300, 300, 1, 2, 1), (300, 300, 100, 2, 2), (12, 80, 1, 2, 2), (30, 30, 1, 4, 1), (700, 900, 1, 4, 4)])
 def test_what_is_not_seen_may_hold_anything(s3r, dtype, n, m, view, heads, kv_heads):
@@ -246,6 +265,29 @@ def test_gradient_against_differences(s3r):
         slope, want = (f(*up) - f(*down)) / (2 * t), float(r[name].double().norm())
         print(name, slope, want, flush=True)
         assert abs(slope - want) <= 5e-3 * want
+
+
+def test_rows_past_2_31_elements(s3r):
+    """Keys whose rows lie further than 2^32 bytes apart, and rows of q that start past 2^31 elements."""
+    g = gen(21)
+    n, m, H = 150, 400, 2
+    stride = (5 << 30) // (2 * m) // 8 * 8
+    room = torch.zeros(m * stride, dtype=BF16, device="cuda")
+    k, v = (room.as_strided((m, 1, 64), (stride, 64, 1), at) for at in (0, 64))
+    q = room.as_strided((n, H, 64), (stride, 64, 1), room.numel() - (n - 1) * stride - 64 * H - 128)
+    for t in (k, v, q):
+        t.copy_(normal(g, *t.shape, dtype=BF16))
+    d_out = normal(g, n, H, 64, dtype=BF16)
+    got = {"out": torch.full((n, H, 64), math.nan, dtype=BF16, device="cuda"), "lse": torch.empty((H, n), device="cuda")}
+    s3r.speed3r_causal_attn(q, k, v, got["out"], lse=got["lse"])
+    got.update(dq=nan_like(d_out), dk=torch.full((m, 1, 64), math.nan, dtype=BF16, device="cuda"), dv=torch.full((m, 1, 64), math.nan, dtype=BF16, device="cuda"))
+    s3r.speed3r_causal_attn_backward(q, k, v, got["out"], got["lse"], d_out, got["dq"], got["dk"], got["dv"])
+    compare(got, reference(q.contiguous(), k.contiguous(), v.contiguous(), [(0, n, 0, m)], 1, d_out))
+
+
+def test_keys_that_are_their_own_values(s3r):
+    q, k, _, d_out = inputs(22, 300, 300, 2, 2, BF16)
+    compare(run(s3r, q, k, k, d_out), reference(q, k, k, [(0, 300, 0, 300)], 1, d_out))
 
 
 def test_large_scores_and_rising_maxima(s3r):
