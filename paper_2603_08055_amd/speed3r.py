@@ -516,6 +516,11 @@ def speed3r_cross_attn_backward(q, k, v, out, lse, d_out, dq, dk, dv, *, q_start
     return _call(lib.speed3r_cross_attn_backward, p, lib.speed3r_cross_workspace_bytes(ctypes.byref(p), 1), workspace, index, stream)
 
 
+def _view_arg(tokens_per_view):
+    # (one that 32 bits cannot hold is longer than every sequence; ctypes would cut it down)
+    return max(-1, min(tokens_per_view, 2 ** 31 - 1))
+
+
 def speed3r_causal_workspace_bytes(q, k, *, q_start=None, tokens_per_view=1, backward=False) -> int:
     """Bytes of workspace that speed3r_causal_attn, or its gradient, needs for these shapes (tensors, or anything
     with their `shape` and `dtype`)."""
@@ -525,7 +530,7 @@ def speed3r_causal_workspace_bytes(q, k, *, q_start=None, tokens_per_view=1, bac
     p.dtype = _dtype_code(q)
     p.batch = 1 if q_start is None else q_start.numel() - 1
     p.q_start = p.kv_start = None if q_start is None else 4          # only whether they are given counts here
-    need = load().speed3r_causal_workspace_bytes(ctypes.byref(p), tokens_per_view, int(bool(backward)))
+    need = load().speed3r_causal_workspace_bytes(ctypes.byref(p), _view_arg(tokens_per_view), int(bool(backward)))
     if need >= 1 << 62:
         raise Speed3rError(S3R_ERR_INVALID_ARG, speed3r_last_error())
     return need
@@ -538,8 +543,9 @@ def speed3r_causal_attn(q, k, v, out, *, tokens_per_view=1, lse=None, q_start=No
     and keys are of the same tokens.  Returns the workspace used (None: none was needed)."""
     index, lib = _gpu(q, "q"), load()
     p = _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, status, stream, index)
-    need = lib.speed3r_causal_workspace_bytes(ctypes.byref(p), tokens_per_view, 0)
-    return _call(lib.speed3r_causal_attn, p, need, workspace, index, stream, tokens_per_view)
+    view = _view_arg(tokens_per_view)
+    need = lib.speed3r_causal_workspace_bytes(ctypes.byref(p), view, 0)
+    return _call(lib.speed3r_causal_attn, p, need, workspace, index, stream, view)
 
 
 def speed3r_causal_attn_backward(q, k, v, out, lse, d_out, dq, dk, dv, *, tokens_per_view=1, q_start=None, kv_start=None, key_mask=None,
@@ -550,8 +556,9 @@ def speed3r_causal_attn_backward(q, k, v, out, lse, d_out, dq, dk, dv, *, tokens
     p = _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, status, stream, index)
     p.d_out, p.dq = _arg(d_out, "d_out", index, q.dtype, q.shape), _arg(dq, "dq", index, q.dtype, q.shape)
     p.dk, p.dv = _arg(dk, "dk", index, q.dtype, k.shape), _arg(dv, "dv", index, q.dtype, k.shape)
-    need = lib.speed3r_causal_workspace_bytes(ctypes.byref(p), tokens_per_view, 1)
-    return _call(lib.speed3r_causal_attn_backward, p, need, workspace, index, stream, tokens_per_view)
+    view = _view_arg(tokens_per_view)
+    need = lib.speed3r_causal_workspace_bytes(ctypes.byref(p), view, 1)
+    return _call(lib.speed3r_causal_attn_backward, p, need, workspace, index, stream, view)
 
 
 class PagedCache(NamedTuple):

@@ -193,6 +193,17 @@ def test_workspaces_by_the_binding(s3r):
         s3r.speed3r_residual_workspace_bytes(10, 12)
 
 
+def test_a_view_longer_than_32_bits_hold(s3r):
+    """It is held to what they do, and not cut down to another one."""
+    q = torch.empty((10000, 4, 64), dtype=torch.bfloat16, device="meta")
+    largest = s3r.speed3r_causal_workspace_bytes(q, q, tokens_per_view=2 ** 31 - 1, backward=True)
+    assert largest != s3r.speed3r_causal_workspace_bytes(q, q, tokens_per_view=1, backward=True)
+    for view in (2 ** 31, 2 ** 32 + 1, 2 ** 63 - 1):
+        assert s3r.speed3r_causal_workspace_bytes(q, q, tokens_per_view=view, backward=True) == largest
+    with pytest.raises(s3r.Speed3rError, match="tokens_per_view"):
+        s3r.speed3r_causal_workspace_bytes(q, q, tokens_per_view=1 - 2 ** 32)
+
+
 def test_the_binding_refuses(s3r):
     x = torch.zeros((4, 2, 64))
     with pytest.raises(TypeError, match="GPU"):

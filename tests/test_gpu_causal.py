@@ -227,6 +227,14 @@ def test_a_view_of_all_tokens_is_cross_attention(s3r, dtype):
     assert torch.equal(one["out"], cross)
 
 
+def test_a_view_longer_than_32_bits_hold(s3r):
+    q, k, v, d_out = inputs(6, 200, 200, 4, 2, torch.bfloat16)
+    want = run(s3r, q, k, v, d_out, 200)
+    for view in (2 ** 31 - 1, 2 ** 32 + 1):
+        got = run(s3r, q, k, v, d_out, view)
+        assert all(torch.equal(got[name], want[name]) for name in want)
+
+
 def test_the_cache_gives_the_same(s3r):
     """A prompt over itself by the cache (keys and values that 4 bits hold exactly) and without it, in fp32."""
     g = gen(6)
