@@ -275,6 +275,7 @@ template <typename T, int WAVES, bool CAUSAL> __global__ __launch_bounds__(64 * 
 // head), the log-sums of 64 splits are one load, and 64 splits' partial results are requested at once.  64 splits of 16 rows: 22.4 us
 // with one group, 4.6 with four; 13 splits of 22 thousand rows 16 with one, 19 with four.
 constexpr int kSplitChunks = kMostSplits / 64;
+constexpr int kJoinAtOnce = 4;  // pieces whose loads are under way together where a thread goes through them
 template <typename T, int GROUPS> __device__ __forceinline__ void soft_combine(const SoftOut &to, int64_t row, int64_t at, int n_split)
 {
     const int64_t share = to.rows * to.heads;
@@ -317,10 +318,25 @@ template <typename T, int GROUPS> __device__ __forceinline__ void soft_combine(c
         }
         if (group != 0) return;
     } else {
-        for (int j = 0; j < n_split; ++j) top = fmaxf(top, to.part_lse[j * share + at]);
-        for (int j = 0; j < n_split; ++j) {
-            const float l = to.part_lse[j * share + at];
-            if (l != -INFINITY) add(l, *reinterpret_cast<const floatx4 *>(to.part_o + (j * share + at) * 64 + c));
+        for (int j0 = 0; j0 < n_split; j0 += kJoinAtOnce) {
+            float l[kJoinAtOnce];
+#pragma unroll
+            for (int k = 0; k < kJoinAtOnce; ++k) l[k] = to.part_lse[min(j0 + k, n_split - 1) * share + at];
+#pragma unroll
+            for (int k = 0; k < kJoinAtOnce; ++k) top = fmaxf(top, l[k]);
+        }
+        for (int j0 = 0; j0 < n_split; j0 += kJoinAtOnce) {
+            float l[kJoinAtOnce];
+            floatx4 o[kJoinAtOnce];
+#pragma unroll
+            for (int k = 0; k < kJoinAtOnce; ++k) {
+                const int64_t from = min(j0 + k, n_split - 1) * share + at;
+                l[k] = to.part_lse[from];
+                o[k] = *reinterpret_cast<const floatx4 *>(to.part_o + from * 64 + c);
+            }
+#pragma unroll
+            for (int k = 0; k < kJoinAtOnce; ++k)
+                if (j0 + k < n_split && l[k] != -INFINITY) add(l[k], o[k]);
         }
     }
     const float w = total == 0.f ? 0.f : 1.f / total;
@@ -548,12 +564,28 @@ template <typename T> __device__ __forceinline__ void grad_q_combine(const Cross
     const int c = static_cast<int>(threadIdx.x & 15) * 4;
     floatx4 g = {0.f, 0.f, 0.f, 0.f}, pk = {0.f, 0.f, 0.f, 0.f};
     float sum = 0.f, entered = 0.f;
-    for (int j = 0; j < n; ++j) {
-        g += *reinterpret_cast<const floatx4 *>(a.part_q + (j * share + at) * 64 + c);
-        if constexpr (kMendD<T>) {
-            pk += *reinterpret_cast<const floatx4 *>(a.part_pk + (j * share + at) * 64 + c);
-            sum += a.part_sum[2 * (j * share + at)];
-            entered += a.part_sum[2 * (j * share + at) + 1];
+    for (int j0 = 0; j0 < n; j0 += kJoinAtOnce) {
+        floatx4 q[kJoinAtOnce], p[kJoinAtOnce];
+        float s[kJoinAtOnce][2];
+#pragma unroll
+        for (int k = 0; k < kJoinAtOnce; ++k) {
+            const int64_t from = min(j0 + k, n - 1) * share + at;
+            q[k] = *reinterpret_cast<const floatx4 *>(a.part_q + from * 64 + c);
+            if constexpr (kMendD<T>) {
+                p[k] = *reinterpret_cast<const floatx4 *>(a.part_pk + from * 64 + c);
+                s[k][0] = a.part_sum[2 * from];
+                s[k][1] = a.part_sum[2 * from + 1];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kJoinAtOnce; ++k) {
+            if (j0 + k >= n) break;
+            g += q[k];
+            if constexpr (kMendD<T>) {
+                pk += p[k];
+                sum += s[k][0];
+                entered += s[k][1];
+            }
         }
     }
     T *dst = static_cast<T *>(a.dq) + at * 64 + c;
@@ -737,7 +769,14 @@ template <typename T> __device__ __forceinline__ void grad_kv_combine(const Cros
     const float *part = blockIdx.y == 0 ? a.part_k : a.part_v;
     T *out = static_cast<T *>(blockIdx.y == 0 ? a.dk : a.dv);
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < pieces; ++j) acc += *reinterpret_cast<const floatx4 *>(part + (j * n + i) * 4);
+    for (int j0 = 0; j0 < pieces; j0 += kJoinAtOnce) {
+        floatx4 x[kJoinAtOnce];
+#pragma unroll
+        for (int k = 0; k < kJoinAtOnce; ++k) x[k] = *reinterpret_cast<const floatx4 *>(part + (min(j0 + k, pieces - 1) * n + i) * 4);
+#pragma unroll
+        for (int k = 0; k < kJoinAtOnce; ++k)
+            if (j0 + k < pieces) acc += x[k];
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) out[i * 4 + e] = from_float<T>(acc[e]);
 }
