@@ -13,7 +13,7 @@
 // fixed order.
 // Rows of 1024: 137400 with an fp32 stream beside bf16, channel scale and LayerNorm, 337 us, 5.0 TB/s, the rate of a copy of as much (4.97);
 // 41220 all in bf16 60 us, 5.7 TB/s, their gradient 109 us, 4.65 TB/s (six tensors at once), and 8 us for the sums.  3001 rows of 1000 in
-// fp32 with a post-norm and gates: 13 us (3.7 TB/s) and 27 + 8 (2.7 TB/s): four sums over a row, one after the other, and three rows for a workgroup.
+// fp32 with a post-norm and gates: 13 us (3.7 TB/s) and 27 + 8 (2.7 TB/s): four sums over a row, one after the other, and six rows for a workgroup, two at a time.
 #include "s3r_lanes_device.h"
 
 namespace s3r {

@@ -377,15 +377,18 @@ template <bool GROUPED> struct DirectUnits {
     const bf16_t *base;  // item 0
     int64_t row_stride, head_stride;
     int items, per_row;
-    unsigned off[2];     // bytes from the unit's first row; not GROUPED, and rows near enough for 32 bits
+    unsigned off[2];     // bytes from the unit's first row, where rows are near enough for 32 bits (GROUPED: and a unit is whole rows)
     bool near;
 
     __device__ __forceinline__ DirectUnits(const bf16_t *base_, int items_, int64_t row_stride_, int64_t head_stride_, int per_row_, int wave, int lane)
         : base(base_), row_stride(row_stride_), head_stride(head_stride_), items(items_), per_row(per_row_)
     {
-        near = row_stride < (int64_t(1) << 23);
+        near = row_stride < (int64_t(1) << 23) && (!GROUPED || (kUnitRows % per_row == 0 && head_stride < (int64_t(1) << 23)));
 #pragma unroll
-        for (int i = 0; i < 2; ++i) off[i] = 2 * (row_in_unit(wave, i, lane) * static_cast<unsigned>(row_stride) + 8 * chunk(wave, i, lane));
+        for (int i = 0; i < 2; ++i) {
+            const unsigned at = row_in_unit(wave, i, lane), row = GROUPED ? at / static_cast<unsigned>(per_row) : at;
+            off[i] = 2 * (row * static_cast<unsigned>(row_stride) + (GROUPED ? (at - row * per_row) * static_cast<unsigned>(head_stride) : 0u) + 8 * chunk(wave, i, lane));
+        }
     }
     static __device__ __forceinline__ int row_in_unit(int wave, int i, int lane) { return 8 * (2 * wave + i) + (lane >> 3); }
     static __device__ __forceinline__ int chunk(int wave, int i, int lane)
@@ -396,8 +399,8 @@ template <bool GROUPED> struct DirectUnits {
     // `lds`: byte address of the unit's place; wave and unit are the same for all lanes
     __device__ __forceinline__ void request(int unit, unsigned lds, int wave, int lane) const
     {
-        if (!GROUPED && near && (unit + 1) * kUnitRows <= items) {
-            const bf16_t *from = base + unit * (kUnitRows * row_stride);
+        if (near && (unit + 1) * kUnitRows <= items) {
+            const bf16_t *from = base + unit * ((GROUPED ? kUnitRows / per_row : kUnitRows) * row_stride);
 #pragma unroll
             for (int i = 0; i < 2; ++i) lds_dma_16_x1(from, off[i], lds + (2 * wave + i) * 1024);
             return;
