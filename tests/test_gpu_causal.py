@@ -215,6 +215,44 @@ def test_strides_scale_and_sums_of_shared_heads(s3r, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("layout", ["projection", "head by head", "far heads", "far rows"])
+@pytest.mark.parametrize("heads,kv_heads", [(8, 2), (6, 2), (64, 1)])
+def test_layouts_of_shared_heads(s3r, dtype, layout, heads, kv_heads):
+    """Rows of q anywhere give the bits of packed ones, by token and in cross attention: units of whole rows (64 is a multiple of the heads that
+    share one) and others, rows and heads near enough for offsets of 32 bits and not."""
+    n, m = 150, 200
+    q, k, v, d_out = inputs(heads, n, m, heads, kv_heads, dtype)
+    if layout == "projection":
+        there = torch.zeros((n, heads + 5, 64), dtype=dtype, device="cuda")[:, 3:3 + heads]
+    elif layout == "head by head":
+        there = torch.zeros((heads, n, 64), dtype=dtype, device="cuda").transpose(0, 1)
+    else:
+        far = 2 ** 23 + 64                                       # elements; room for the last row of the last head, no more
+        row, head = (64, far) if layout == "far heads" else (far, 64)
+        there = torch.zeros((n - 1) * row + (heads - 1) * head + 64, dtype=dtype, device="cuda").as_strided((n, heads, 64), (row, head, 1))
+    there.copy_(q)
+    got, want = run(s3r, there, k, v, d_out), run(s3r, q, k, v, d_out)
+    assert all(torch.equal(got[name], want[name]) for name in want)
+    results = []
+    for x in (there, q):
+        out, lse, dq, dk, dv = torch.empty_like(d_out), torch.empty((heads, n), device="cuda"), torch.empty_like(d_out), torch.empty_like(k), torch.empty_like(v)
+        s3r.speed3r_cross_attn(x, k, v, out, lse=lse)
+        s3r.speed3r_cross_attn_backward(x, k, v, out, lse, d_out, dq, dk, dv)
+        results.append((out, lse, dq, dk, dv))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,m", [(0, 200), (0, 0), (90, 0)])
+def test_calls_without_rows_or_keys(s3r, dtype, n, m):
+    """Keys that no row sees have gradients of 0."""
+    q, k, v, d_out = inputs(n + m, n, m, 4, 2, dtype)
+    got = run(s3r, q, k, v, d_out)
+    assert not got["dk"].any() and not got["dv"].any() and not got["dq"].any() and not got["out"].any()
+    assert (got["lse"] == -math.inf).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_a_view_of_all_tokens_is_cross_attention(s3r, dtype):
     """And the last token alone sees all."""
     q, k, v, d_out = inputs(5, 200, 200, 4, 2, dtype)
