@@ -47,6 +47,8 @@ __device__ __forceinline__ int tile_sees(int64_t end, int64_t items, int per_row
 
 // Pieces of a causal tile: n_split alike of `least` units or more, or fewer (so that they differ in length as the tiles do, and the CUs that are
 // done first find short ones), none of them empty where there are units; a tile of one piece goes straight to the results.
+// (Pieces of one length for all tiles, by the longest: 4096 rows of 16 heads that share 4 with gradients 273 us so, 330 by length; 8192 in three
+// sequences 370 and 364.)
 __device__ __forceinline__ int causal_pieces(int units, int n_split, int least)
 {
     const int per = max(1, piece_units(units, n_split, least));
