@@ -498,39 +498,6 @@ template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ _
     store_sums<L, W, CH>(sa, to + 2 * share, a.width, part, join);
 }
 
-// The sums of `count` partial results, `stride` floats apart, of 16 channels (channel = the thread's, ok: there is one), of N tensors that
-// are `gap` apart: 64 groups of a workgroup take every 64th, in 64 bits (sums of hundreds, which cost nothing here).  To the threads of group 0.
-template <int N> __device__ __forceinline__ void sum_parts(const float *from, int64_t count, int64_t stride, int64_t gap, bool ok, double (&lds)[N][64][16], double (&s)[N])
-{
-    const int c = threadIdx.x & 15, group = threadIdx.x >> 4;
-#pragma unroll
-    for (int n = 0; n < N; ++n) s[n] = 0.0;
-    if (ok) {
-        constexpr int kAtOnce = 8;
-        for (int64_t i = group; i < count; i += 64 * kAtOnce) {
-            float x[N][kAtOnce];
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) x[n][k] = i + 64 * k < count ? from[n * gap + (i + 64 * k) * stride] : 0.f;
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) s[n] += x[n][k];
-        }
-    }
-#pragma unroll
-    for (int n = 0; n < N; ++n) lds[n][group][c] = s[n];
-    __syncthreads();
-    if (group != 0) return;
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-        s[n] = 0.0;
-#pragma unroll
-        for (int i = 0; i < 64; ++i) s[n] += lds[n][i][c];
-    }
-}
-
 __device__ __forceinline__ float weight_at(const void *w, bool is_bf16, int c, float none)
 {
     if (w == nullptr) return none;
@@ -541,21 +508,21 @@ __device__ __forceinline__ float weight_at(const void *w, bool is_bf16, int c, f
 // what comes of them (of_branch), then the gates, sequence by sequence.
 __global__ __launch_bounds__(1024) void residual_sums_kernel(ResidualArgs a, int blocks, bool of_norm, bool of_branch, bool is_bf16)
 {
-    __shared__ double lds[2][64][16];
-    const int c = blockIdx.x * 16 + (threadIdx.x & 15), seq = static_cast<int>(blockIdx.y) - (of_norm + of_branch);
-    const bool first = of_norm && blockIdx.y == 0, ok = c < a.width, mine = threadIdx.x < 16 && ok;
-    const double scale = a.residual_scale * static_cast<double>(ok ? weight_at(a.scale, a.w_bf16, c, 1.f) : 0.f);
+    __shared__ union { PartSums<2> two; PartSums<1> one; } lds;
+    const int c = blockIdx.x * 16 + (threadIdx.x & 15), four = blockIdx.x * 16 + 4 * (threadIdx.x & 3), seq = static_cast<int>(blockIdx.y) - (of_norm + of_branch);
+    const bool first = of_norm && blockIdx.y == 0, ok = four < a.width, mine = threadIdx.x < 16 && c < a.width;
+    const double scale = a.residual_scale * static_cast<double>(mine ? weight_at(a.scale, a.w_bf16, c, 1.f) : 0.f);
     double s[2];
     if (seq >= 0) {
         int row, len;
         a.spans.of(seq, row, len);
         const int64_t from = row / a.rows_per_block, count = len > 0 ? (static_cast<int64_t>(row) + len - 1) / a.rows_per_block - from + 1 : 0;
-        sum_parts<1>(a.part_gate + (from + seq) * a.width + c, count, a.width, 0, ok, reinterpret_cast<double(&)[1][64][16]>(lds), reinterpret_cast<double(&)[1]>(s));
+        sum_parts<1, 2>(a.part_gate + (from + seq) * a.width + four, count, a.width, 0, ok, lds.one, reinterpret_cast<double(&)[1]>(s));
         if (mine) store_weight(a.d_gate, is_bf16, static_cast<int64_t>(seq) * a.width + c, static_cast<float>(scale * s[0]));
         return;
     }
     const int64_t gap = static_cast<int64_t>(blocks) * a.width;
-    sum_parts<2>(a.part + (first ? 0 : 2 * gap) + c, blocks, a.width, first || a.post != kNormNone || a.gate != nullptr ? gap : 0, ok, lds, s);
+    sum_parts<2, 2>(a.part + (first ? 0 : 2 * gap) + four, blocks, a.width, first || a.post != kNormNone || a.gate != nullptr ? gap : 0, ok, lds.two, s);
     if (!mine) return;
     if (first) {
         if (a.d_weight != nullptr) store_weight(a.d_weight, a.w_bf16, c, static_cast<float>(s[0]));

@@ -323,29 +323,17 @@ template <typename T, Mode MODE> __global__ __launch_bounds__(256) void rotary_n
             (exchange[threadIdx.x] + exchange[512 + threadIdx.x]) + (exchange[1024 + threadIdx.x] + exchange[1536 + threadIdx.x]);
 }
 
-// The gradients of weight and bias of q and of k as sums over the workgroups, in 64 bits: 16 of the 64 channels of one of the four for a
-// workgroup, whose 64 groups take every 64th.
+// The gradients of weight and bias of q and of k as sums over the workgroups: 16 of the 64 channels of one of the four for a workgroup.
 __global__ __launch_bounds__(1024) void rotary_weight_grad_kernel(RotaryArgs a, int wgs_q, int wgs)
 {
-    const int side = blockIdx.x >> 3, which = (blockIdx.x >> 2) & 1, c = threadIdx.x & 15, group = threadIdx.x >> 4, channel = (blockIdx.x & 3) * 16 + c;
+    __shared__ PartSums<1> lds;
+    const int side = blockIdx.x >> 3, which = (blockIdx.x >> 2) & 1, channels = (blockIdx.x & 3) * 16;
     const int first = side == 0 ? 0 : wgs_q, end = side == 0 ? wgs_q : wgs;
     void *to = which == 0 ? a.side[side].d_weight : a.side[side].d_bias;
     if (to == nullptr) return;
-    __shared__ double sums[64][16];
-    constexpr int kMost = kRotaryGradGroups / 64;
-    float x[kMost];
-#pragma unroll
-    for (int i = 0; i < kMost; ++i) x[i] = first + group + 64 * i < end ? a.part[static_cast<int64_t>(first + group + 64 * i) * 128 + which * 64 + channel] : 0.f;
-    double s = 0.0;
-#pragma unroll
-    for (int i = 0; i < kMost; ++i) s += x[i];
-    sums[group][c] = s;
-    __syncthreads();
-    if (group != 0) return;
-    s = 0.0;
-#pragma unroll
-    for (int i = 0; i < 64; ++i) s += sums[i][c];
-    store_weight(to, a.w_bf16, channel, static_cast<float>(s));
+    double s[1];
+    sum_parts<1, kRotaryGradGroups / 256>(a.part + static_cast<int64_t>(first) * 128 + which * 64 + channels + 4 * (threadIdx.x & 3), end - first, 128, 0, true, lds, s);
+    if (threadIdx.x < 16) store_weight(to, a.w_bf16, channels + threadIdx.x, static_cast<float>(s[0]));
 }
 
 // Whether a position is outside the table.  One workgroup.

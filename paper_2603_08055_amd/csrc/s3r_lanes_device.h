@@ -61,4 +61,51 @@ __device__ __forceinline__ void store_weight(void *to, bool is_bf16, int64_t at,
         static_cast<float *>(to)[at] = x;
 }
 
+// Sums of N tensors' rows `stride` floats apart, `count` of them, the tensors `gap` apart, of 16 channels, by a workgroup of 1024 threads: a thread
+// takes four channels (from: the first of its own, 4 (thread mod 4); ok: they are there) of every 256th row, AT_ONCE of them requested together.  In
+// 64 bits, which cost nothing here, in a fixed order.  To threads 0 .. 15, a channel each.
+template <int N> struct PartSums { double rows[N][128][16], groups[N][16][16]; };
+template <int N, int AT_ONCE> __device__ __forceinline__ void sum_parts(const float *from, int64_t count, int64_t stride, int64_t gap, bool ok, PartSums<N> &lds, double (&s)[N])
+{
+    const int t = threadIdx.x, lane = t & 63;
+    double own[N][4] = {};
+    if (ok)
+        for (int64_t i = t >> 2; i < count; i += 256 * AT_ONCE) {
+            floatx4 x[N][AT_ONCE];
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k)
+                    x[n][k] = i + 256 * k < count ? *reinterpret_cast<const floatx4 *>(from + n * gap + (i + 256 * k) * stride) : floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) own[n][e] += x[n][k][e];
+        }
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            own[n][e] += __shfl_xor(own[n][e], 32, 64);
+            if (lane < 32) lds.rows[n][(t >> 6) * 8 + (lane >> 2)][4 * (t & 3) + e] = own[n][e];
+        }
+    __syncthreads();
+    if (t < 256 * N) {
+        double x = 0.0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x += lds.rows[t >> 8][8 * ((t >> 4) & 15) + i][t & 15];
+        lds.groups[t >> 8][(t >> 4) & 15][t & 15] = x;
+    }
+    __syncthreads();
+    if (t >= 16) return;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        s[n] = 0.0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[n] += lds.groups[n][i][t];
+    }
+}
+
 }  // namespace s3r
