@@ -8,7 +8,7 @@
 // heads, so that a row's cosines and sines stay in registers for the heads in turn, and the sums over a head are three lane moves.
 // 27480 rows of 16 + 16 heads in bf16, LayerNorm and two axes of 16 pairs: 42 us, 5.4 TB/s of what is read and written (a copy of as much: 5.2 to
 // 5.4); the gradient, which reads q and k again beside the gradients, 73 us, 4.6 TB/s, and 8 us for adding up those of the weights.  3001 rows of
-// 15 + 5 heads in fp32, axes of 10, 11 and 11 pairs: 11.7 us (2.6 TB/s) and 19.2 + 3.9: too few rows to hide the way through LDS.
+// 15 + 5 heads in fp32, axes of 10, 11 and 11 pairs: 10.5 us (2.9 TB/s) and 14.4 + 3.8.
 #include "s3r_lanes_device.h"
 
 namespace s3r {
@@ -16,9 +16,10 @@ namespace s3r {
 namespace {
 
 // Where a channel's partner is: in the same lane (neighbours, axes of multiples of four pairs); at the same place of the lane whose number
-// differs by 2 or 4 (all axes of 16 pairs, or one of 32), or of another of the eight (axes of multiples of eight); or anywhere: then
-// through LDS.
-enum Mode { kInLane, kAcross2, kAcross4, kAcross, kAnywhere };
+// differs by 2 or 4 (all axes of 16 pairs, or one of 32, or halves of 32 pairs whatever their axes: the angles of a lane's channels then lie apart),
+// or of another of the eight (axes of multiples of eight); or anywhere: then through LDS.
+enum Mode { kInLane, kAcross2, kAcross4, kAcross4Apart, kAcross, kAnywhere };
+constexpr bool angles_apart(Mode mode) { return mode == kAcross4Apart || mode == kAnywhere; }
 
 struct Channel { int pair, partner, axis; bool turned, second; };
 __device__ __forceinline__ Channel channel_of(const RotaryArgs &a, int c)
@@ -84,7 +85,7 @@ template <typename T, Mode MODE> struct Turn {
         }
         const Channel first = channel_of(a, 8 * c);
         turned = first.turned;
-        if constexpr (MODE == kAnywhere) {
+        if constexpr (angles_apart(MODE)) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const Channel ch = channel_of(a, 8 * c + j);
@@ -123,7 +124,7 @@ template <typename T, Mode MODE> struct Turn {
         for (int j = 0; j < 8; ++j) {
             if constexpr (MODE == kInLane) other[j] = x[j ^ 1];
             if constexpr (MODE == kAcross2) other[j] = other_lane<2>(x[j]);
-            if constexpr (MODE == kAcross4) other[j] = other_lane<4>(x[j]);
+            if constexpr (MODE == kAcross4 || MODE == kAcross4Apart) other[j] = other_lane<4>(x[j]);
             if constexpr (MODE == kAcross)
                 other[j] = __uint_as_float(static_cast<unsigned>(__builtin_amdgcn_ds_bpermute(from, static_cast<int>(__float_as_uint(x[j])))));
             if constexpr (MODE == kAnywhere) other[j] = lds[at[j] < 0 ? 0 : at[j]];
@@ -355,6 +356,7 @@ Mode mode_of(const RotaryArgs &a)
         while (a.axis_pairs[x] % common != 0) common /= 2;
     if (a.axes == 0) return kInLane;
     if (a.pairing == kPairsNeighbours) return common >= 4 ? kInLane : kAnywhere;
+    if (a.pairing == kPairsWhole && a.n_pairs == 32 && common < 8) return kAcross4Apart;
     if (common < 8) return kAnywhere;
     const int half = a.pairing == kPairsWhole ? a.n_pairs : a.axis_pairs[0];  // channels from one of a pair to the other
     for (int x = 1; x < a.axes; ++x)
@@ -363,12 +365,12 @@ Mode mode_of(const RotaryArgs &a)
 }
 
 // Heads that a wave takes in a row: as many as leave the card 2048 waves, up to 4, 8 through a norm's gradient (more to be read for the
-// same angles), 16 where partners are looked up (whose places take longest to find).  us, 1 / 2 / 4 / 8 / 16 of them: 27480 rows of 16 + 16
-// heads, norm and rotation 67 / 41 / 36 / 37 / 38, with the gradient 209 / 139 / 118 / 114 / 114, axes of 10, 11 and 11 pairs 370 / 229 /
-// 168 / - / 133; 3001 rows of 15 + 5 heads in fp32 with the gradient 45 / 36 / 34 / 34 / 38.
+// same angles), twice as many where a lane's angles lie apart, 16 where partners are looked up (whose places take longest to find).  us,
+// 1 / 2 / 4 / 8 / 16 of them: 27480 rows of 16 + 16 heads, norm and rotation 67 / 41 / 36 / 37 / 38, with the gradient 209 / 139 / 118 / 114 / 114; axes of
+// 10, 11 and 11 pairs 100 / 58 / 40 / 38 / 40, with the gradient 280 / 178 / 134 / 119 / 115, with partners looked up 370 / 229 / 168 / - / 133.
 int run_of_heads(const RotaryArgs &a, Mode mode, bool grad)
 {
-    const int most = mode == kAnywhere ? 16 : (grad ? 8 : 4);
+    const int most = mode == kAnywhere || (mode == kAcross4Apart && grad) ? 16 : (mode == kAcross4Apart || grad ? 8 : 4);
     int run = 1;
     auto waves = [&](int r) { return (a.n_rows + 7) / 8 * ((a.side[0].heads + r - 1) / r + (a.side[1].heads + r - 1) / r); };
     while (run < most && waves(2 * run) >= 2048) run *= 2;
@@ -391,6 +393,7 @@ template <typename T> hipError_t launch_rotary_t(const RotaryArgs &a, hipStream_
     case kInLane: kernel = rotary_kernel_of<T, kInLane>(norm); break;
     case kAcross2: kernel = rotary_kernel_of<T, kAcross2>(norm); break;
     case kAcross4: kernel = rotary_kernel_of<T, kAcross4>(norm); break;
+    case kAcross4Apart: kernel = rotary_kernel_of<T, kAcross4Apart>(norm); break;
     case kAcross: kernel = rotary_kernel_of<T, kAcross>(norm); break;
     case kAnywhere: break;
     }
@@ -405,6 +408,7 @@ template <typename T> hipError_t launch_norm_grad_t(const RotaryArgs &a, Mode mo
     case kInLane: kernel = &rotary_norm_grad_kernel<T, kInLane>; break;
     case kAcross2: kernel = &rotary_norm_grad_kernel<T, kAcross2>; break;
     case kAcross4: kernel = &rotary_norm_grad_kernel<T, kAcross4>; break;
+    case kAcross4Apart: kernel = &rotary_norm_grad_kernel<T, kAcross4Apart>; break;
     case kAcross: kernel = &rotary_norm_grad_kernel<T, kAcross>; break;
     case kAnywhere: break;
     }

@@ -102,6 +102,17 @@ def test_rotary_axes_and_pairs(s3r, dtype, pairs, axis_pairs):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("pairs,axis_pairs", [("whole", (8, 12, 12)), ("whole", (10, 11, 11)), ("halves", (10, 11, 11)), ("halves", (16, 8, 8)), ("neighbours", (12, 20)),
+                                              ("whole", (9, 15)), ("whole", (32,))])
+def test_rotary_runs_of_heads(s3r, dtype, pairs, axis_pairs):
+    """Rows enough for a wave to take several heads."""
+    for norm in (None, "rms"):
+        c = rotary_case(sum(axis_pairs) + axis_pairs[0], 2501, 9, 4, dtype, axis_pairs, norm)
+        print(pairs, axis_pairs, norm, flush=True)
+        compare_rotary(run_rotary(s3r, c, axis_pairs, pairs, norm), c, axis_pairs, pairs, norm)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("norm", [None, "rms", "layer"])
 @pytest.mark.parametrize("n,heads,kv_heads", [(1, 1, 1), (1, 16, 2), (7, 5, 5), (8, 2, 0), (9, 0, 3), (64, 16, 4), (300, 17, 1), (1374, 16, 16), (5000, 2, 1)])
 def test_rotary_rows_and_heads(s3r, dtype, norm, n, heads, kv_heads):
