@@ -12,8 +12,8 @@
 // registers for the rows of a workgroup, which follow one another; what the workgroups have is added up by another launch in a
 // fixed order.
 // Rows of 1024: 137400 with an fp32 stream beside bf16, channel scale and LayerNorm, 337 us, 5.0 TB/s, the rate of a copy of as much (4.97);
-// 41220 all in bf16 60 us, 5.7 TB/s, their gradient 109 us, 4.65 TB/s (six tensors at once), and 8 us for the sums.  3001 rows of 1000 in
-// fp32 with a post-norm and gates: 13 us (3.7 TB/s) and 27 + 8 (2.7 TB/s): four sums over a row, one after the other, and six rows for a workgroup, two at a time.
+// 41220 all in bf16 60 us, 5.7 TB/s, their gradient 109 us, 4.65 TB/s (six tensors at once), and 6 us for the sums.  3001 rows of 1000 in
+// fp32 with a post-norm and gates: 13 us (3.7 TB/s) and 27 + 7 (2.7 TB/s): four sums over a row, one after the other, and six rows for a workgroup, two at a time.
 #include "s3r_lanes_device.h"
 
 namespace s3r {
@@ -612,7 +612,7 @@ hipError_t launch_residual_grad(const ResidualArgs &a, bool x_bf16, bool is_bf16
         if (e != hipSuccess) return e;
     }
     const bool of_norm = a.d_weight != nullptr || a.d_bias != nullptr, of_branch = a.d_scale != nullptr || a.d_post_weight != nullptr || a.d_post_bias != nullptr;
-    // (more than eight workgroups for a sequence: 64 groups add them up; 40 us where a thread does, for 6 sequences of 501 workgroups, 4 so)
+    // (more than eight workgroups for a sequence: a workgroup adds them up; 40 us where a thread does, for 6 sequences of 501 workgroups, 4 so)
     const bool spread = a.d_gate != nullptr && blocks > 8 * static_cast<int64_t>(a.spans.batch);
     const unsigned rows = of_norm + of_branch + (spread ? a.spans.batch : 0);
     if (rows > 0) {

@@ -7,7 +7,7 @@
 // Bound by HBM: a row of a head is read and written once.  Eight lanes have a head's 64 channels, a wave eight rows and a run of
 // heads, so that a row's cosines and sines stay in registers for the heads in turn, and the sums over a head are three lane moves.
 // 27480 rows of 16 + 16 heads in bf16, LayerNorm and two axes of 16 pairs: 42 us, 5.4 TB/s of what is read and written (a copy of as much: 5.2 to
-// 5.4); the gradient, which reads q and k again beside the gradients, 73 us, 4.6 TB/s, and 8 us for adding up those of the weights.  3001 rows of
+// 5.4); the gradient, which reads q and k again beside the gradients, 73 us, 4.6 TB/s, and 5 us for adding up those of the weights.  3001 rows of
 // 15 + 5 heads in fp32, axes of 10, 11 and 11 pairs: 10.5 us (2.9 TB/s) and 14.4 + 3.8.
 #include "s3r_lanes_device.h"
 
