@@ -45,6 +45,45 @@ __device__ __forceinline__ int tile_sees(int64_t end, int64_t items, int per_row
     return keys_seen(static_cast<int>((end < items ? end : items) - 1) / per_row, n, m, view);
 }
 
+// Pieces of causal tiles, n_split of them or fewer, by the lengths of up to 64 sequences, of which the host knows the sums alone: a lane for a
+// sequence, then one for a number of pieces, by the host's model of the launch (causal_us).  The kernels of a call have to find the same: sums
+// are those of integers, and no product of floats is added to anything, which the compiler might round once or twice.
+// bf16, forward and gradients, us with the number that the host guesses / so: 17 sequences of up to 220 rows, one over 4075 keys 142 / 73, 17 of up to 203
+// over up to 1160 100 / 72, 64 of up to 64 rows, one over 2026 keys 87 / 65; what it costs where it finds no use: 17 of 60 rows over 500 keys 59 / 68.
+template <bool OF_KEYS> __device__ __forceinline__ int causal_split(const CrossArgs &a)
+{
+    if (a.resident == 0) return a.n_split;
+    const int lane = threadIdx.x & 63;
+    int tiles = 0, work = 0, longest = 0;  // work: twice the units of all tiles
+    if (lane < a.q_spans.batch) {
+        int at, n, m;
+        a.q_spans.of(lane, at, n);
+        a.kv_spans.of(lane, at, m);
+        if (n > 0 && m > 0) {
+            const int items = n * a.per_row, before = max(m - n, 0), last = OF_KEYS ? items : m;
+            const int first = OF_KEYS ? static_cast<int>(static_cast<float>(items) * (static_cast<float>(before) / static_cast<float>(m))) : min(before + a.view, m);
+            tiles = ((OF_KEYS ? m : items) + kTile - 1) / kTile;
+            work = static_cast<int>(min(static_cast<int64_t>(tiles) * (first / kUnitRows + last / kUnitRows + 1), int64_t(1) << 24));
+            longest = (last + kUnitRows - 1) / kUnitRows;
+        }
+    }
+    for (int x = 1; x < 64; x <<= 1) {
+        tiles += __shfl_xor(tiles, x, 64);
+        work += __shfl_xor(work, x, 64);
+        longest = max(longest, __shfl_xor(longest, x, 64));
+    }
+    tiles = min(tiles, 1 << 10) * a.kv_heads;
+    const int n = lane + 1, others = a.resident - 1, on_cus = min(max(tiles * n, 256), 256 * a.resident);
+    const float alone = others > 1 ? 2000.f : (others > 0 ? 1600.f : 1100.f);
+    const float pace = others > 0 ? static_cast<float>(3 * 256 * others - (on_cus - 256)) / static_cast<float>(2 * 256 * others) : 1.f;
+    const float all = static_cast<float>(work) * static_cast<float>(a.kv_heads) * a.unit_us * pace * (1000.f / 512), piece = static_cast<float>(longest) * a.unit_us * alone / static_cast<float>(n);
+    int ns = static_cast<int>(fminf(fmaxf(all, piece), 1e9f)) + (lane == 0 ? 0 : a.join_ns + tiles * n * a.tile_ns);
+    if (lane >= a.n_split || (lane > 0 && longest < a.least * n)) ns = 0x7fffffff;
+    int least = ns;
+    for (int x = 1; x < 64; x <<= 1) least = min(least, __shfl_xor(least, x, 64));
+    return __builtin_amdgcn_readfirstlane(static_cast<int>(__ffsll(__ballot(ns - least <= least / 100))));
+}
+
 // Pieces of a causal tile: n_split alike of `least` units or more, or fewer (so that they differ in length as the tiles do, and the CUs that are
 // done first find short ones), none of them empty where there are units; a tile of one piece goes straight to the results.
 // (Pieces of one length for all tiles, by the longest: 4096 rows of 16 heads that share 4 with gradients 273 us so, 330 by length; 8192 in three
@@ -91,9 +130,9 @@ template <bool OF_KEYS> __device__ __forceinline__ int tiles_of_units(const Cros
 // first take short ones last; of up to 64 sequences, a lane for each: the number of units by bisection, then the tile among those that walk as
 // many.  (More sequences: one after the other, the longest tile of each first.)  8192 rows in three sequences, 16 heads that share 4, sequence by
 // sequence / so: forward 108 / 90 us, query gradient 157 / 131.
-template <bool OF_KEYS> __device__ __forceinline__ bool find_causal_share(const CrossArgs &a, Share &s)
+template <bool OF_KEYS> __device__ __forceinline__ bool find_causal_share(const CrossArgs &a, int n_split, Share &s)
 {
-    const int each = a.n_split * a.kv_heads, u = static_cast<int>(blockIdx.x) / each, rest = static_cast<int>(blockIdx.x) - u * each;
+    const int each = n_split * a.kv_heads, u = static_cast<int>(blockIdx.x) / each, rest = static_cast<int>(blockIdx.x) - u * each;
     s.split = rest / a.kv_heads;
     s.kv_head = rest - s.split * a.kv_heads;
     const Spans &held = OF_KEYS ? a.kv_spans : a.q_spans, &other = OF_KEYS ? a.q_spans : a.kv_spans;
@@ -160,8 +199,13 @@ template <typename T, bool CAUSAL> __global__ __launch_bounds__(256, sizeof(T) =
     bf16_t *lds = reinterpret_cast<bf16_t *>(smem);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Share sh;
-    if (CAUSAL ? !find_causal_share<false>(a, sh)
-               : !find_share(a.q_spans, nullptr, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, !a.uneven, true, sh)) return;
+    int pieces;  // causal: of a tile, at most
+    if constexpr (CAUSAL) {
+        pieces = causal_split<false>(a);
+        if (!find_causal_share<false>(a, pieces, sh)) return;
+    } else {
+        if (!find_share(a.q_spans, nullptr, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, !a.uneven, true, sh)) return;
+    }
     const int q0 = sh.of.first, q_len = sh.of.len;
     int k0, k_len;
     a.kv_spans.of(sh.of.seq, k0, k_len);
@@ -174,7 +218,7 @@ template <typename T, bool CAUSAL> __global__ __launch_bounds__(256, sizeof(T) =
     SoftOut to = a.to;
     if constexpr (CAUSAL) {
         bool whole;
-        if (!causal_piece((sight.tile + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1, whole)) return;
+        if (!causal_piece((sight.tile + kUnitRows - 1) / kUnitRows, pieces, a.least, sh.split, u0, u1, whole)) return;
         if (whole) to.part_o = nullptr;
     } else {
         piece((sight.tile + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1);
@@ -382,7 +426,7 @@ template <typename T, int GROUPS> __global__ __launch_bounds__(256) void causal_
     int k0, k_len;
     a.kv_spans.of(t.of.of.seq, k0, k_len);
     const int64_t items = static_cast<int64_t>(t.of.of.len) * a.per_row, tile0 = static_cast<int64_t>(t.of.tile) * kTile;
-    const int n = causal_pieces((tile_sees(tile0 + kTile, items, a.per_row, t.of.of.len, k_len, a.view) + kUnitRows - 1) / kUnitRows, a.n_split, a.least);
+    const int n = causal_pieces((tile_sees(tile0 + kTile, items, a.per_row, t.of.of.len, k_len, a.view) + kUnitRows - 1) / kUnitRows, causal_split<false>(a), a.least);
     if (n == 1) return;
     for (int i = threadIdx.x / (16 * GROUPS); i < kItems; i += 256 / (16 * GROUPS)) {
         const int64_t item = tile0 + t.item0 + i, in_seq = item / a.per_row, row = t.of.of.first + in_seq;
@@ -417,8 +461,13 @@ template <typename T, int PX, bool CAUSAL> __global__ __launch_bounds__(256, siz
     bf16_t *lds = reinterpret_cast<bf16_t *>(smem);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Share sh;
-    if (CAUSAL ? !find_causal_share<false>(a, sh)
-               : !find_share(a.q_spans, nullptr, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, !a.uneven, true, sh)) return;
+    int pieces;  // causal: of a tile, at most
+    if constexpr (CAUSAL) {
+        pieces = causal_split<false>(a);
+        if (!find_causal_share<false>(a, pieces, sh)) return;
+    } else {
+        if (!find_share(a.q_spans, nullptr, a.per_row, kTile, a.tiles, a.n_split, a.kv_heads, !a.uneven, true, sh)) return;
+    }
     const int q0 = sh.of.first, q_len = sh.of.len;
     int k0, k_len;
     a.kv_spans.of(sh.of.seq, k0, k_len);
@@ -431,7 +480,7 @@ template <typename T, int PX, bool CAUSAL> __global__ __launch_bounds__(256, siz
     float *part_q = a.part_q;
     if constexpr (CAUSAL) {
         bool whole;
-        if (!causal_piece((sight.tile + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1, whole)) return;
+        if (!causal_piece((sight.tile + kUnitRows - 1) / kUnitRows, pieces, a.least, sh.split, u0, u1, whole)) return;
         if (whole) part_q = nullptr;
     } else {
         piece((sight.tile + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1);
@@ -614,7 +663,7 @@ template <typename T> __global__ __launch_bounds__(256) void causal_grad_q_combi
     int k0, k_len;
     a.kv_spans.of(t.of.of.seq, k0, k_len);
     const int64_t items = static_cast<int64_t>(t.of.of.len) * a.per_row, tile0 = static_cast<int64_t>(t.of.tile) * kTile;
-    const int n = causal_pieces((tile_sees(tile0 + kTile, items, a.per_row, t.of.of.len, k_len, a.view) + kUnitRows - 1) / kUnitRows, a.n_split, a.least);
+    const int n = causal_pieces((tile_sees(tile0 + kTile, items, a.per_row, t.of.of.len, k_len, a.view) + kUnitRows - 1) / kUnitRows, causal_split<false>(a), a.least);
     if (n == 1) return;
     for (int i = threadIdx.x / 16; i < kJoinItems<1>; i += 16) {
         const int64_t item = tile0 + t.item0 + i, in_seq = item / a.per_row, row = t.of.of.first + in_seq;
@@ -631,8 +680,13 @@ template <typename T, int PX, bool CAUSAL> __global__ __launch_bounds__(256, siz
     float *row_stats = reinterpret_cast<float *>(smem + sizeof(bf16_t) * UnitPairs<T>::kStages * UnitPairs<T>::kStage);  // [stages][2][64]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Share sh;
-    if (CAUSAL ? !find_causal_share<true>(a, sh)
-               : !find_share(a.kv_spans, nullptr, 1, kTile, a.tiles, a.n_split, a.kv_heads, !a.uneven, true, sh)) return;
+    int pieces;  // causal: of a tile, at most
+    if constexpr (CAUSAL) {
+        pieces = causal_split<true>(a);
+        if (!find_causal_share<true>(a, pieces, sh)) return;
+    } else {
+        if (!find_share(a.kv_spans, nullptr, 1, kTile, a.tiles, a.n_split, a.kv_heads, !a.uneven, true, sh)) return;
+    }
     const int k0 = sh.of.first, k_len = sh.of.len;
     int q0, q_len;
     a.q_spans.of(sh.of.seq, q0, q_len);
@@ -646,7 +700,7 @@ template <typename T, int PX, bool CAUSAL> __global__ __launch_bounds__(256, siz
         int begin, end;
         seeing_units(a, sh.tile, q_len, k_len, begin, end);
         bool whole;
-        if (!causal_piece(end - begin, a.n_split, a.least, sh.split, u0, u1, whole)) return;
+        if (!causal_piece(end - begin, pieces, a.least, sh.split, u0, u1, whole)) return;
         if (whole) part_k = nullptr;
         u0 += begin;
         u1 += begin;
@@ -800,7 +854,7 @@ template <typename T> __global__ __launch_bounds__(256) void causal_grad_kv_comb
     int q0, q_len, from, end;
     a.q_spans.of(t.of.of.seq, q0, q_len);
     seeing_units(a, t.of.tile, q_len, t.of.of.len, from, end);
-    const int n = causal_pieces(end - from, a.n_split, a.least);
+    const int n = causal_pieces(end - from, causal_split<true>(a), a.least);
     if (n == 1) return;
     for (int i = threadIdx.x / 16; i < kJoinItems<1>; i += 16) {
         const int key = t.of.tile * kTile + t.item0 + i;

@@ -6,6 +6,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <algorithm>
 #include <initializer_list>
 #include <mutex>
 #include <tuple>
@@ -1088,25 +1089,27 @@ int64_t mean_tiles(int64_t n, int per_row, int tile, int batch)
     return some * (each < 1 ? 1 : (each + tile - 1) / tile);
 }
 
-// The same for causal rows: `tiles` (heads counted) walk from `shortest` to `longest` units, as many of each, and all are divided alike.  They
+// The same for causal rows: `tiles` (heads counted) walk `units` units on average, the longest of them `longest`, and all are divided alike.  They
 // are taken the longest first, so that the short ones fill the CUs up.  The work takes its time at the pace of as many workgroups as a CU
 // has (alone half as long again), and the longest piece twice its share at the pace of a full CU, or 1.6 times where two fill it; joining
-// 9 us and `tile_bytes` of a tile's piece, out and in again.
+// 9 us and `tile_us` for each tile's piece, out and in again.
 // Measured (1, 2, 3, 4 .. pieces), us: forward, bf16, 4096 rows of 16 heads that share 4 87 / 75 / 79 / 87, 1374 of 16 38 / 31 / 32 / 33, 512 over
 // 16384 285 / 156 / 112 / 93, 8 69, 12 67, 16 66, 32 75, 8192 in three sequences 93 / 108 / 119 / 134; the whole step with gradients of keys
 // in these: 8192 in three sequences 599 / 437 / 398 / 385, 6 391, 8 420; 4096 568 / 388 / 337 / 310, 6 293, 8 302.
-int causal_pieces(double tiles, double shortest, double longest, const Pace &pace, double tile_bytes)
+double causal_us(int n, double tiles, double units, double longest, const Pace &pace, double join_us, double tile_us)
 {
-    const double all = tiles * (shortest + longest) / 2 / 256 * pace.unit_us, alone = pace.resident > 2 ? 2.0 : (pace.resident > 1 ? 1.6 : 1.1);
-    auto time_us = [&](int n) {
-        const double on_a_cu = tiles * n / 256, k = on_a_cu < 1 ? 1 : (on_a_cu > pace.resident ? pace.resident : on_a_cu);
-        const double work = all * (pace.resident > 1 ? 1.5 - 0.5 * (k - 1) / (pace.resident - 1) : 1.0), piece = alone * longest / n * pace.unit_us;
-        return (work > piece ? work : piece) + (n == 1 ? 0.0 : 9.0 + tiles * n * tile_bytes * 2 / 5e6);
-    };
+    const double all = tiles * units / 256 * pace.unit_us, alone = pace.resident > 2 ? 2.0 : (pace.resident > 1 ? 1.6 : 1.1);
+    const double on_a_cu = tiles * n / 256, k = on_a_cu < 1 ? 1 : (on_a_cu > pace.resident ? pace.resident : on_a_cu);
+    const double work = all * (pace.resident > 1 ? 1.5 - 0.5 * (k - 1) / (pace.resident - 1) : 1.0), piece = alone * longest / n * pace.unit_us;
+    return (work > piece ? work : piece) + (n == 1 ? 0.0 : join_us + tiles * n * tile_us);
+}
+constexpr double kJoinUs = 9.0;
+int causal_pieces(double tiles, double units, double longest, const Pace &pace, double tile_bytes)
+{
     int best = 1;
-    double least_us = time_us(1);
+    double least_us = causal_us(1, tiles, units, longest, pace, kJoinUs, tile_bytes * 2 / 5e6);
     for (int n = 2; n <= s3r::kMostSplits && longest >= static_cast<double>(pace.least) * n; ++n) {
-        const double us = time_us(n);
+        const double us = causal_us(n, tiles, units, longest, pace, kJoinUs, tile_bytes * 2 / 5e6);
         if (us < 0.99 * least_us) {
             least_us = us;
             best = n;
@@ -1114,9 +1117,18 @@ int causal_pieces(double tiles, double shortest, double longest, const Pace &pac
     }
     return best;
 }
+// Of 2 to 64 sequences: the most pieces that their lengths may ask for, where one of them may have all the `longest` units.  What is left over of the
+// grid, and a launch that may find nothing to join, cost some us for each kernel: as many as make 1024 workgroups, 8 at most, and
+// only where that promises half the time.  (The kernels find the number that the lengths do ask for, causal_split.)
+int causal_most_pieces(int guess, double tiles, double units, double longest, const Pace &pace, double tile_bytes)
+{
+    const int n = std::min({causal_pieces(tiles, units, longest, pace, tile_bytes), 8, static_cast<int>(1024 / tiles)});
+    auto us = [&](int k) { return causal_us(k, tiles, units, longest, pace, kJoinUs, tile_bytes * 2 / 5e6); };
+    return n > guess && us(guess) > 2 * us(n) ? n : guess;
+}
 
 struct CrossPlan {
-    bool few_rows;
+    bool few_rows, adapts, adapts_q, adapts_kv;  // causal: kernels take fewer pieces by the sequences' lengths
     int batch, per_row, split, least, split_q, split_kv;
     int64_t tiles, q_tiles, kv_tiles;
     size_t part_o, part_lse, forward;                   // workspace of the forward call
@@ -1165,16 +1177,24 @@ s3r_status plan_cross(const s3r_cross_params *p, int view, CrossPlan *out)
     c.kv_tiles = s3r::most_tiles(p->n_kv, 1, 128, c.batch);
     c.split_kv = split_of(c.kv_tiles, p->n_kv, 1, items, kGradKvPace[bf16], kv_bytes);
     if (view > 0) {
-        // Of several sequences only the sums of their lengths are known: the longest is taken to be 1.75 times their mean.
+        // Of several sequences only the sums of their lengths are known: the longest is taken to be 1.75 times their mean.  (Where there are few
+        // tiles, and it may be far longer, the kernels are given room for more pieces, and find how many by themselves.)
         const double n = static_cast<double>(p->n_q) / c.batch, m = static_cast<double>(p->n_kv) / c.batch, v = view < m ? view : m;
         const double spread = c.batch > 1 ? 1.75 : 1.0, first = m > n ? m - n + v : v;
         const double most = m * spread / 64 + 0.5, least = first < m ? first / 64 + 0.5 : most;
         const double q_tiles = static_cast<double>(mean_tiles(p->n_q, c.per_row, 128, c.batch)) * p->kv_heads, tile_bytes = 128.0 * 256;
-        if (!c.few_rows) c.split = causal_pieces(q_tiles, least, most, kCrossPace[bf16], tile_bytes);
-        c.split_q = causal_pieces(q_tiles, least, most, kGradQPace[bf16], bf16 ? 2 * tile_bytes : tile_bytes);
         // Keys: the first ones are seen by all rows, the last ones by a view's, or by all where there are earlier tokens.
-        const double rows = n * c.per_row / 64, kv_tiles = static_cast<double>(mean_tiles(p->n_kv, 1, 128, c.batch)) * p->kv_heads;
-        c.split_kv = causal_pieces(kv_tiles, (m > n ? rows * (m - n) / m : 0.0) + 0.5, rows * spread + 0.5, kGradKvPace[bf16], 2 * tile_bytes);
+        const double rows = n * c.per_row / 64, kv_tiles = static_cast<double>(mean_tiles(p->n_kv, 1, 128, c.batch)) * p->kv_heads, few = (m > n ? rows * (m - n) / m : 0.0) + 0.5;
+        const double mean_q = ((first < m ? first : m) + m) / 128 + 0.5, mean_k = (rows + few) / 2 + 0.5;
+        auto split = [&](double tiles, double shortest, double longest, double mean, double total, const Pace &pace, double bytes, bool *adapts) {
+            const int guess = causal_pieces(tiles, (shortest + longest) / 2, longest, pace, bytes);
+            const int n = c.batch > 1 && c.batch <= 64 ? causal_most_pieces(guess, tiles, mean, total, pace, bytes) : guess;
+            *adapts = n > guess;
+            return n;
+        };
+        if (!c.few_rows) c.split = split(q_tiles, least, most, mean_q, m * c.batch / 64 + 0.5, kCrossPace[bf16], tile_bytes, &c.adapts);
+        c.split_q = split(q_tiles, least, most, mean_q, m * c.batch / 64 + 0.5, kGradQPace[bf16], bf16 ? 2 * tile_bytes : tile_bytes, &c.adapts_q);
+        c.split_kv = split(kv_tiles, few, rows * spread + 0.5, mean_k, rows * c.batch + 0.5, kGradKvPace[bf16], 2 * tile_bytes, &c.adapts_kv);
     }
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
@@ -1237,6 +1257,15 @@ s3r_status cross_args(const s3r_cross_params *p, const CrossPlan &c, int view, s
 
 float *floats_at(void *base, size_t off) { return reinterpret_cast<float *>(at(base, off)); }
 
+// What the kernels divide tiles by.  (A launch that joins is there in any case: 2 us of it remain.)
+void set_pace(s3r::CrossArgs *a, bool adapts, const Pace &pace, double tile_bytes)
+{
+    a->resident = adapts ? pace.resident : 0;
+    a->unit_us = static_cast<float>(pace.unit_us);
+    a->join_ns = 2000;
+    a->tile_ns = static_cast<int>(tile_bytes * 2 / 5e3);
+}
+
 s3r_status cross_forward(const s3r_cross_params *p, int view)
 {
     CrossPlan c;
@@ -1254,6 +1283,7 @@ s3r_status cross_forward(const s3r_cross_params *p, int view)
     a.tiles = c.tiles;
     a.n_split = c.split;
     a.least = c.least;
+    if (!c.few_rows) set_pace(&a, c.adapts, kCrossPace[bf16], 128.0 * 256);
     if (c.split > 1) {
         a.to.part_o = floats_at(p->workspace, c.part_o);
         a.to.part_lse = floats_at(p->workspace, c.part_lse);
@@ -1296,6 +1326,7 @@ s3r_status cross_backward(const s3r_cross_params *p, int view)
         a.tiles = c.q_tiles;
         a.n_split = c.split_q;
         a.least = kGradQPace[bf16].least;
+        set_pace(&a, c.adapts_q, kGradQPace[bf16], bf16 ? 2 * 128.0 * 256 : 128.0 * 256);
         if (c.split_q > 1) {
             a.part_q = floats_at(p->workspace, c.part_q);
             a.part_pk = floats_at(p->workspace, c.part_pk);
@@ -1308,6 +1339,7 @@ s3r_status cross_backward(const s3r_cross_params *p, int view)
         a.tiles = c.kv_tiles;
         a.n_split = c.split_kv;
         a.least = kGradKvPace[bf16].least;
+        set_pace(&a, c.adapts_kv, kGradKvPace[bf16], 2 * 128.0 * 256);
         if (c.split_kv > 1) {
             a.part_k = floats_at(p->workspace, c.part_k);
             a.part_v = floats_at(p->workspace, c.part_v);

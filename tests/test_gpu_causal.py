@@ -159,6 +159,27 @@ def test_many_rows_of_many_sequences(s3r, dtype, view, count, lo, hi, earlier, h
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("seed", range(12))
+def test_batches_with_a_long_sequence(s3r, dtype, seed):
+    """Batches whose tiles take more pieces than the mean length asks for: all launches of a call find the same number."""
+    g = torch.Generator().manual_seed(seed)
+    pick = lambda lo, hi: int(torch.randint(lo, hi + 1, (1,), generator=g))
+    count, heads = (2, 5, 17, 40, 64, 65)[seed % 6], (1, 2, 4, 8)[pick(0, 3)]
+    kv_heads = heads // (1, 2, 4, 8)[pick(0, (1, 2, 4, 8).index(heads))]
+    rows = [max(1, int(2 ** (pick(0, 80) / 10))) for _ in range(count)]
+    keys = [r + (int(2 ** (pick(0, 90) / 10)) if pick(0, 2) == 0 else 0) for r in rows]
+    rows[seed % count], keys[seed % count] = (700, 700) if seed % 3 == 0 else (150, 2500 + 100 * seed)
+    q, k, v, d_out = inputs(seed, sum(rows), sum(keys), heads, kv_heads, dtype)
+    a, b = starts(rows), starts(keys)
+    spans = [(int(x), r, int(y), c) for x, y, r, c in zip(a, b, rows, keys)]
+    view = (1, 1, 37)[pick(0, 2)]
+    got = run(s3r, q, k, v, d_out, view, q_start=a, kv_start=b)
+    compare(got, reference(q, k, v, spans, view, d_out))
+    again = run(s3r, q, k, v, d_out, view, q_start=a, kv_start=b)
+    assert all(torch.equal(got[name], again[name]) for name in got)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("n,m,view,heads,kv_heads", [(300, 300, 1, 2, 1), (300, 300, 100, 2, 2), (12, 80, 1, 2, 2), (30, 30, 1, 4, 1), (700, 900, 1, 4, 4)])
 def test_what_is_not_seen_may_hold_anything(s3r, dtype, n, m, view, heads, kv_heads):
     """Infinities and NaN in keys and values of later tokens do not reach earlier rows, nor those of earlier rows later keys; who does see them
