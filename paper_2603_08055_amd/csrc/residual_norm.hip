@@ -334,7 +334,8 @@ template <typename TX, typename T, int CH> struct GradRows {
 // FULL: with a post-norm or gates.  What scale, gate and post weights multiply is the same for all rows of a sequence, so that their
 // gradients are made of two sums over these, A = sum dr' n' (n': f normed, or f) and B = sum dr':
 //   d gate = residual_scale scale (post_weight A + post_bias B), and, with GA and GB the sums of gate A and gate B over the sequences,
-//   d scale = residual_scale (post_weight GA + post_bias GB),  d post_weight = residual_scale scale GA,  d post_bias = residual_scale scale GB.
+//   d scale = residual_scale (post_weight GA + post_bias GB),  d post_weight = residual_scale scale GA,  d post_bias = residual_scale scale GB
+// (without a post_bias nothing of B: 0 times an infinite sum would be NaN).
 // A row needs of the weights their products r = x + fw n' + fb alone: fw = s post_weight, fb = s post_bias.
 template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ __launch_bounds__(threads_of(W)) void residual_grad_kernel(ResidualArgs a)
 {
@@ -465,7 +466,10 @@ template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ _
 #pragma unroll
                 for (int i = 0; i < CH; ++i)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) sums[i][j] = fmaf(sums[i][j], sa[i][j], gate[i][j] * sb[i][j]);
+                    for (int j = 0; j < 8; ++j) {
+                        sums[i][j] *= sa[i][j];
+                        if (a.post_bias != nullptr) sums[i][j] = fmaf(gate[i][j], sb[i][j], sums[i][j]);
+                    }
                 store_sums<L, W, CH>(sums, a.part_gate + (static_cast<int64_t>(blockIdx.x) + seq) * a.width, a.width, part, join);
             }
 #pragma unroll
@@ -531,7 +535,7 @@ __global__ __launch_bounds__(1024) void residual_sums_kernel(ResidualArgs a, int
     }
     if (a.d_scale != nullptr)
         store_weight(a.d_scale, a.w_bf16, c, static_cast<float>(a.residual_scale * (weight_at(a.post_weight, a.w_bf16, c, 1.f) * s[0] +
-                                                                                   weight_at(a.post_bias, a.w_bf16, c, 0.f) * s[1])));
+                                                                                   (a.post_bias != nullptr ? weight_at(a.post_bias, a.w_bf16, c, 0.f) * s[1] : 0.0))));
     if (a.d_post_weight != nullptr) store_weight(a.d_post_weight, a.w_bf16, c, static_cast<float>(scale * s[0]));
     if (a.d_post_bias != nullptr) store_weight(a.d_post_bias, a.w_bf16, c, static_cast<float>(scale * s[1]));
 }
