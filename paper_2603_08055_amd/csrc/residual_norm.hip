@@ -21,6 +21,9 @@ namespace s3r {
 namespace {
 
 constexpr int threads_of(int w) { return w > 4 ? 64 * w : 256; }
+// The sums of a gradient over the rows of a workgroup, in the workspace: of dy n, of dy, and (see residual_grad_kernel) C, A and B.
+enum { kPartWeight, kPartBias, kPartC, kPartA, kPartB };
+static_assert(kPartB + 1 == kResidualParts, "");
 
 // A thread's part of a row, and sums over rows of channels.
 template <int L, int W, int CH> struct RowPart {
@@ -278,23 +281,13 @@ template <int L, int W, int CH, typename Part> __device__ __forceinline__ void s
     }
 }
 
-// A thread's channels of two sums, in places of its own in LDS.
-template <int THREADS, int CH> struct OwnSums {
-    floatx4 *at;  // [CH][2][THREADS]
-    __device__ __forceinline__ OwnSums(float *lds, int which) : at(reinterpret_cast<floatx4 *>(lds) + which * (2 * CH * THREADS) + threadIdx.x)
+// A thread's channels of a sum, or of a weight, in places of its own in LDS.
+template <int THREADS, int CH> struct OwnSum {
+    floatx4 *at;  // [2 CH][THREADS]
+    __device__ __forceinline__ OwnSum(float *lds, int which) : at(reinterpret_cast<floatx4 *>(lds) + which * (2 * CH * THREADS) + threadIdx.x)
     {
 #pragma unroll
         for (int i = 0; i < 2 * CH; ++i) at[i * THREADS] = floatx4{0.f, 0.f, 0.f, 0.f};
-    }
-    __device__ __forceinline__ void add(const float (&x)[CH][8], const float (&w)[CH][8])
-    {
-#pragma unroll
-        for (int i = 0; i < 2 * CH; ++i) {
-            floatx4 t = at[i * THREADS];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) t[e] = fmaf(x[i / 2][4 * (i & 1) + e], w[i / 2][4 * (i & 1) + e], t[e]);
-            at[i * THREADS] = t;
-        }
     }
     __device__ __forceinline__ void add(const float (&x)[CH][8])
     {
@@ -306,6 +299,23 @@ template <int THREADS, int CH> struct OwnSums {
             at[i * THREADS] = t;
         }
     }
+    __device__ __forceinline__ void add(const float (&x)[CH][8], const float (&w)[CH][8])
+    {
+#pragma unroll
+        for (int i = 0; i < 2 * CH; ++i) {
+            floatx4 t = at[i * THREADS];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] = fmaf(x[i / 2][4 * (i & 1) + e], w[i / 2][4 * (i & 1) + e], t[e]);
+            at[i * THREADS] = t;
+        }
+    }
+    __device__ __forceinline__ void set(const float (&x)[CH][8])
+    {
+#pragma unroll
+        for (int i = 0; i < 2 * CH; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) at[i * THREADS][e] = x[i / 2][4 * (i & 1) + e];
+    }
     __device__ __forceinline__ void get(float (&x)[CH][8]) const
     {
 #pragma unroll
@@ -314,8 +324,12 @@ template <int THREADS, int CH> struct OwnSums {
             for (int e = 0; e < 4; ++e) x[i / 2][4 * (i & 1) + e] = at[i * THREADS][e];
     }
 };
-// Sums of a gradient that are in LDS: GA and GB, and where registers run out those of dy n and dy.
-template <int W, int CH, bool FULL> constexpr int kOwnSums = !FULL ? 0 : (W * CH >= 16 ? 4 : 2);
+
+// Rows over 4096 channels with a post-norm or gates: registers run out, and the sums of dy n and dy and the post weights and biases are in LDS, the sums over
+// sequences in the workgroup's place of the workspace, which is for its threads alone.
+template <int W, int CH, bool FULL> constexpr bool kWidest = FULL && W * CH >= 16;
+// LDS of a gradient: GA, GB and GC, or those four.
+template <int W, int CH, bool FULL> constexpr size_t kGradLds = !FULL ? 0 : (kWidest<W, CH, FULL> ? 4 : 3) * 8 * CH * threads_of(W) * sizeof(float);
 
 // A thread's part of the rows of a gradient.
 template <typename TX, typename T, int CH> struct GradRows {
@@ -332,30 +346,52 @@ template <typename TX, typename T, int CH> struct GradRows {
 };
 
 // FULL: with a post-norm or gates.  What scale, gate and post weights multiply is the same for all rows of a sequence, so that their
-// gradients are made of two sums over these, A = sum dr' n' (n': f normed, or f) and B = sum dr':
-//   d gate = residual_scale scale (post_weight A + post_bias B), and, with GA and GB the sums of gate A and gate B over the sequences,
-//   d scale = residual_scale (post_weight GA + post_bias GB),  d post_weight = residual_scale scale GA,  d post_bias = residual_scale scale GB
-// (without a post_bias nothing of B: 0 times an infinite sum would be NaN).
-// A row needs of the weights their products r = x + fw n' + fb alone: fw = s post_weight, fb = s post_bias.
+// gradients are made of sums over these, A = sum dr' n' (n': f normed, or f), B = sum dr' and C = sum dr' u:
+//   d gate = residual_scale scale C,  and with GA, GB and GC the sums of gate A, gate B and gate C over the sequences,
+//   d scale = residual_scale GC,  d post_weight = residual_scale scale GA,  d post_bias = residual_scale scale GB.
+// (C is post_weight A + post_bias B, but u may be far smaller than these parts, and then that loses what a sum of its own keeps.)
 template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ __launch_bounds__(threads_of(W)) void residual_grad_kernel(ResidualArgs a)
 {
     using Part = RowPart<L, W, CH>;
-    __shared__ float lds[2 * 2 * (threads_of(W) / 64)];
+    constexpr int kThreads = threads_of(W);
+    constexpr bool kWide = kWidest<W, CH, FULL>;
+    __shared__ float lds[2 * 2 * (kThreads / 64)];
     __shared__ float join[Part::kRows > 1 ? Part::kRows * 8 * L * W : 1];
-    extern __shared__ __align__(16) float own_sums[];  // FULL: GA and GB
+    extern __shared__ __align__(16) float own_sums[];  // FULL: see kGradLds
     Part part(a.width, lds);
     const float of_width = 1.f / static_cast<float>(a.width);
     const int64_t r0 = static_cast<int64_t>(blockIdx.x) * a.rows_per_block, r1 = min(r0 + a.rows_per_block, a.n);
-    float w[CH][8], fw[CH][8], fb[CH][8], dw[CH][8], db[CH][8], sa[CH][8], sb[CH][8];
+    const int64_t share = static_cast<int64_t>(gridDim.x) * a.width;
+    float *to_part = a.part + blockIdx.x * static_cast<int64_t>(a.width);
+    float w[CH][8], factor[CH][8], pw[CH][8], pb[CH][8], dw[CH][8], db[CH][8], sa[CH][8], sb[CH][8], sc[CH][8];  // (not FULL: A is C)
     channel_weights<CH>(a.weight, a.w_bf16, part, 1.f, w);
+    constexpr int kOwn = FULL && !kWide ? CH : 0, kAside = kWide ? CH : 0;
+    OwnSum<kThreads, kOwn> ga(own_sums, 0), gb(own_sums, 1), gc(own_sums, 2);
+    OwnSum<kThreads, kAside> own_dw(own_sums, 0), own_db(own_sums, 1), own_pw(own_sums, 2), own_pb(own_sums, 3);
+    if constexpr (FULL) {
+        channel_weights<CH>(a.post_weight, a.w_bf16, part, 1.f, pw);
+        channel_weights<CH>(a.post_bias, a.w_bf16, part, 0.f, pb);
+        if constexpr (kWide) {
+            own_pw.set(pw);
+            own_pb.set(pb);
+        }
+    }
+    auto get_post = [&]() {
+        if constexpr (kWide) {
+            own_pw.get(pw);
+            own_pb.get(pb);
+        }
+    };
 #pragma unroll
     for (int i = 0; i < CH; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) dw[i][j] = db[i][j] = sa[i][j] = sb[i][j] = 0.f;
-    constexpr int kOwn = kOwnSums<W, CH, FULL>;
-    OwnSums<threads_of(W), kOwn >= 2 ? CH : 0> ga(own_sums, 0), gb(own_sums, 1);
-    OwnSums<threads_of(W), kOwn >= 4 ? CH : 0> own_dw(own_sums, 2), own_db(own_sums, 3);
+        for (int j = 0; j < 8; ++j) dw[i][j] = db[i][j] = sa[i][j] = sb[i][j] = sc[i][j] = 0.f;
     const bool gated = FULL && a.gate != nullptr, with_f = a.f != nullptr;
+    const bool of_scale = a.part != nullptr && a.d_scale != nullptr, of_post_weight = a.part != nullptr && a.d_post_weight != nullptr,
+               of_post_bias = a.part != nullptr && a.d_post_bias != nullptr;
+    // What the workgroup has of a sum over sequences, to its place.
+    auto store_part = [&](int which, const float (&x)[CH][8]) { store_sums<L, W, CH>(x, to_part + which * share, a.width, part, join); };
+    bool fresh = true;  // no sequence yet
     // Sequence by sequence (without gates: all rows at once).
     for (int seq = gated ? find_sequence(a.spans, r0) : 0; seq < a.spans.batch; ++seq) {
         int first_row = 0, len = 0;
@@ -371,30 +407,21 @@ template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ _
             raw.load(static_cast<const T *>(a.gate) + seq * a.gate_row, part);
             raw.get(gate, part);
         };
-        channel_weights<CH>(a.scale, a.w_bf16, part, 1.f, fw);
-        if constexpr (FULL) {
-            float gate[CH][8], pw[CH][8];
+        channel_weights<CH>(a.scale, a.w_bf16, part, 1.f, factor);
+        {
+            float gate[CH][8];
             if (gated) get_gate(gate);
-            channel_weights<CH>(a.post_weight, a.w_bf16, part, 1.f, pw);
-            channel_weights<CH>(a.post_bias, a.w_bf16, part, 0.f, fb);
 #pragma unroll
             for (int i = 0; i < CH; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    float s = a.residual_scale * fw[i][j];
-                    if (gated) s *= gate[i][j];
-                    fw[i][j] = s * pw[i][j];
-                    fb[i][j] *= s;
+                    factor[i][j] *= a.residual_scale;
+                    if (gated) factor[i][j] *= gate[i][j];
                 }
-        } else {
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) fw[i][j] *= a.residual_scale;
         }
         for (int64_t first = from; first < to; first += Part::kRows) {
             const int64_t row = first + part.sub;
-            const bool ok = row < to;
+            const bool ok = Part::kRows == 1 || row < to;
             float z[CH][8], n[CH][8], g[CH][8], d[CH][8];
             GradRows<TX, T, CH> here;
             if (kAhead) here = ahead; else here.load(a, row, to, part);
@@ -412,13 +439,15 @@ template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ _
 #pragma unroll
                     for (int j = 0; j < 8; ++j) d[i][j] = 0.f;
             if (a.d_y != nullptr) {
-                if (with_f)
+                if (with_f) {
+                    get_post();
 #pragma unroll
                     for (int i = 0; i < CH; ++i)
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) z[i][j] += FULL ? fmaf(fw[i][j], n[i][j], fb[i][j]) : fw[i][j] * n[i][j];
+                        for (int j = 0; j < 8; ++j) z[i][j] = fmaf(factor[i][j], FULL ? fmaf(n[i][j], pw[i][j], pb[i][j]) : n[i][j], z[i][j]);
+                }
                 const float inv = row_norm<CH>(a.norm, a.eps, of_width, part, z);
-                if constexpr (kOwn >= 4) {  // (one row at a time)
+                if constexpr (kWide) {  // (one row at a time)
                     own_dw.add(g, z);
                     own_db.add(g);
                 }
@@ -426,7 +455,7 @@ template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ _
                 for (int i = 0; i < CH; ++i)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        if (kOwn < 4 && ok) {
+                        if (!kWide && ok) {
                             dw[i][j] = fmaf(g[i][j], z[i][j], dw[i][j]);
                             db[i][j] += g[i][j];
                         }
@@ -440,15 +469,19 @@ template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ _
             }
             store_row<TX, CH>(static_cast<TX *>(a.dx) + row * a.width, d, part, ok);
             if (!with_f) continue;
+            if constexpr (FULL) get_post();
 #pragma unroll
             for (int i = 0; i < CH; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     if (ok) {
-                        sa[i][j] = fmaf(d[i][j], n[i][j], sa[i][j]);
-                        if constexpr (FULL) sb[i][j] += d[i][j];
+                        if constexpr (FULL) {
+                            sa[i][j] = fmaf(d[i][j], n[i][j], sa[i][j]);
+                            sb[i][j] += d[i][j];
+                        }
+                        sc[i][j] = fmaf(d[i][j], FULL ? fmaf(n[i][j], pw[i][j], pb[i][j]) : n[i][j], sc[i][j]);
                     }
-                    d[i][j] *= fw[i][j];
+                    d[i][j] *= FULL ? factor[i][j] * pw[i][j] : factor[i][j];
                 }
             if constexpr (FULL)
                 if (a.post != kNormNone) row_norm_back<CH>(a.post, of_width, post_inv, n, part, d);
@@ -456,50 +489,61 @@ template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ _
         }
         if constexpr (FULL) {
             if (!gated) break;
-            float gate[CH][8], sums[CH][8];
+            float gate[CH][8];
             get_gate(gate);
-            ga.add(sa, gate);
-            gb.add(sb, gate);
-            if (a.part_gate != nullptr) {  // at place blockIdx.x + seq, which no other pair has
-                channel_weights<CH>(a.post_weight, a.w_bf16, part, 1.f, sums);
-                channel_weights<CH>(a.post_bias, a.w_bf16, part, 0.f, gate);
+            if (a.part_gate != nullptr)  // at place blockIdx.x + seq, which no other pair has
+                store_sums<L, W, CH>(sc, a.part_gate + (static_cast<int64_t>(blockIdx.x) + seq) * a.width, a.width, part, join);
+            // times the gate to the sums over sequences
+            auto add = [&](float (&sums)[CH][8], int which, OwnSum<kThreads, kOwn> &own) {
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    if constexpr (kWide) {
+                        if (!part.has[i]) continue;
+                        float *at = to_part + which * share + part.at(i);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) sums[i][j] *= gate[i][j];
+                        if (!fresh) {
+                            Io8<float> x;
+                            x.load(at);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) sums[i][j] += x.get(j);
+                        }
+                        Io8<float>::store(at, sums[i]);
+                    }
+                }
+                if constexpr (!kWide) own.add(sums, gate);
 #pragma unroll
                 for (int i = 0; i < CH; ++i)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        sums[i][j] *= sa[i][j];
-                        if (a.post_bias != nullptr) sums[i][j] = fmaf(gate[i][j], sb[i][j], sums[i][j]);
-                    }
-                store_sums<L, W, CH>(sums, a.part_gate + (static_cast<int64_t>(blockIdx.x) + seq) * a.width, a.width, part, join);
-            }
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) sa[i][j] = sb[i][j] = 0.f;
+                    for (int j = 0; j < 8; ++j) sums[i][j] = 0.f;
+            };
+            if (of_scale || !kWide) add(sc, kPartC, gc);
+            if (of_post_weight || !kWide) add(sa, kPartA, ga);
+            if (of_post_bias || !kWide) add(sb, kPartB, gb);
+            fresh = false;
         } else {
             break;
         }
     }
     if (a.part == nullptr) return;
-    const int64_t share = static_cast<int64_t>(gridDim.x) * a.width;
-    float *to = a.part + blockIdx.x * static_cast<int64_t>(a.width);
     if (a.d_weight != nullptr || a.d_bias != nullptr) {
-        if constexpr (kOwn >= 4) {
+        if constexpr (kWide) {
             own_dw.get(dw);
             own_db.get(db);
         }
-        store_sums<L, W, CH>(dw, to, a.width, part, join);
-        store_sums<L, W, CH>(db, to + share, a.width, part, join);
+        store_part(kPartWeight, dw);
+        store_part(kPartBias, db);
     }
-    if (a.d_scale == nullptr && a.d_post_weight == nullptr && a.d_post_bias == nullptr) return;
-    if constexpr (FULL) {
+    if (kWide && gated && !fresh) return;
+    if constexpr (kOwn > 0)
         if (gated) {
             ga.get(sa);
             gb.get(sb);
+            gc.get(sc);
         }
-        store_sums<L, W, CH>(sb, to + 3 * share, a.width, part, join);
-    }
-    store_sums<L, W, CH>(sa, to + 2 * share, a.width, part, join);
+    if (of_scale) store_part(kPartC, sc);
+    if (of_post_weight) store_part(kPartA, sa);
+    if (of_post_bias) store_part(kPartB, sb);
 }
 
 __device__ __forceinline__ float weight_at(const void *w, bool is_bf16, int c, float none)
@@ -508,14 +552,17 @@ __device__ __forceinline__ float weight_at(const void *w, bool is_bf16, int c, f
     return is_bf16 ? static_cast<float>(static_cast<const bf16_t *>(w)[c]) : static_cast<const float *>(w)[c];
 }
 
-// What is made of the workgroups' sums, 16 channels for a workgroup; blockIdx.y: d weight and d bias (of_norm), then GA and GB and
-// what comes of them (of_branch), then the gates, sequence by sequence.
-__global__ __launch_bounds__(1024) void residual_sums_kernel(ResidualArgs a, int blocks, bool of_norm, bool of_branch, bool is_bf16)
+// What is made of the workgroups' sums, 16 channels for a workgroup; blockIdx.y: d weight and d bias (of_norm), then d scale (of_scale), then d post
+// weight and d post bias (of_post), then the gates, sequence by sequence.
+__global__ __launch_bounds__(1024) void residual_sums_kernel(ResidualArgs a, int blocks, bool of_norm, bool of_scale, bool of_post, bool is_bf16)
 {
     __shared__ union { PartSums<2> two; PartSums<1> one; } lds;
-    const int c = blockIdx.x * 16 + (threadIdx.x & 15), four = blockIdx.x * 16 + 4 * (threadIdx.x & 3), seq = static_cast<int>(blockIdx.y) - (of_norm + of_branch);
-    const bool first = of_norm && blockIdx.y == 0, ok = four < a.width, mine = threadIdx.x < 16 && c < a.width;
+    const int c = blockIdx.x * 16 + (threadIdx.x & 15), four = blockIdx.x * 16 + 4 * (threadIdx.x & 3);
+    const int y = static_cast<int>(blockIdx.y), seq = y - (of_norm + of_scale + of_post);
+    const bool ok = four < a.width, mine = threadIdx.x < 16 && c < a.width;
     const double scale = a.residual_scale * static_cast<double>(mine ? weight_at(a.scale, a.w_bf16, c, 1.f) : 0.f);
+    const int64_t gap = static_cast<int64_t>(blocks) * a.width;
+    const bool first = of_norm && y == 0;
     double s[2];
     if (seq >= 0) {
         int row, len;
@@ -523,21 +570,17 @@ __global__ __launch_bounds__(1024) void residual_sums_kernel(ResidualArgs a, int
         const int64_t from = row / a.rows_per_block, count = len > 0 ? (static_cast<int64_t>(row) + len - 1) / a.rows_per_block - from + 1 : 0;
         sum_parts<1, 2>(a.part_gate + (from + seq) * a.width + four, count, a.width, 0, ok, lds.one, reinterpret_cast<double(&)[1]>(s));
         if (mine) store_weight(a.d_gate, is_bf16, static_cast<int64_t>(seq) * a.width + c, static_cast<float>(scale * s[0]));
-        return;
+    } else if (of_scale && y == of_norm) {
+        sum_parts<1, 2>(a.part + kPartC * gap + four, blocks, a.width, 0, ok, lds.one, reinterpret_cast<double(&)[1]>(s));
+        if (mine) store_weight(a.d_scale, a.w_bf16, c, static_cast<float>(a.residual_scale * s[0]));
+    } else {
+        // (a sum that is not asked for may not be there: the other one in its place)
+        const int at = first ? kPartWeight : (a.d_post_weight != nullptr ? kPartA : kPartB);
+        sum_parts<2, 2>(a.part + at * gap + four, blocks, a.width, first || (a.d_post_weight != nullptr && a.d_post_bias != nullptr) ? gap : 0, ok, lds.two, s);
+        void *const one = first ? a.d_weight : a.d_post_weight, *const two = first ? a.d_bias : a.d_post_bias;
+        if (mine && one != nullptr) store_weight(one, a.w_bf16, c, static_cast<float>(first ? s[0] : scale * s[0]));
+        if (mine && two != nullptr) store_weight(two, a.w_bf16, c, static_cast<float>(first ? s[1] : scale * s[1]));
     }
-    const int64_t gap = static_cast<int64_t>(blocks) * a.width;
-    sum_parts<2, 2>(a.part + (first ? 0 : 2 * gap) + four, blocks, a.width, first || a.post != kNormNone || a.gate != nullptr ? gap : 0, ok, lds.two, s);
-    if (!mine) return;
-    if (first) {
-        if (a.d_weight != nullptr) store_weight(a.d_weight, a.w_bf16, c, static_cast<float>(s[0]));
-        if (a.d_bias != nullptr) store_weight(a.d_bias, a.w_bf16, c, static_cast<float>(s[1]));
-        return;
-    }
-    if (a.d_scale != nullptr)
-        store_weight(a.d_scale, a.w_bf16, c, static_cast<float>(a.residual_scale * (weight_at(a.post_weight, a.w_bf16, c, 1.f) * s[0] +
-                                                                                   (a.post_bias != nullptr ? weight_at(a.post_bias, a.w_bf16, c, 0.f) * s[1] : 0.0))));
-    if (a.d_post_weight != nullptr) store_weight(a.d_post_weight, a.w_bf16, c, static_cast<float>(scale * s[0]));
-    if (a.d_post_bias != nullptr) store_weight(a.d_post_bias, a.w_bf16, c, static_cast<float>(scale * s[1]));
 }
 
 // The gates of sequences that few workgroups had rows of each: a thread for a channel.
@@ -561,7 +604,7 @@ template <typename TX, typename T, bool FULL> struct Kernels {
     template <int L, int W, int CH> void set_forward() { forward = {&residual_kernel<TX, T, L, W, CH, FULL>, threads_of(W), 0}; }
     template <int L, int W, int CH> void set_grad()
     {
-        grad = {&residual_grad_kernel<TX, T, L, W, CH, FULL>, threads_of(W), kOwnSums<W, CH, FULL> * 8 * CH * threads_of(W) * sizeof(float)};
+        grad = {&residual_grad_kernel<TX, T, L, W, CH, FULL>, threads_of(W), kGradLds<W, CH, FULL>};
     }
     template <int L, int W, int CH> void set() { set_forward<L, W, CH>(); set_grad<L, W, CH>(); }
     explicit Kernels(int width)
@@ -615,12 +658,12 @@ hipError_t launch_residual_grad(const ResidualArgs &a, bool x_bf16, bool is_bf16
         });
         if (e != hipSuccess) return e;
     }
-    const bool of_norm = a.d_weight != nullptr || a.d_bias != nullptr, of_branch = a.d_scale != nullptr || a.d_post_weight != nullptr || a.d_post_bias != nullptr;
+    const bool of_norm = a.d_weight != nullptr || a.d_bias != nullptr, of_scale = a.d_scale != nullptr, of_post = a.d_post_weight != nullptr || a.d_post_bias != nullptr;
     // (more than eight workgroups for a sequence: a workgroup adds them up; 40 us where a thread does, for 6 sequences of 501 workgroups, 4 so)
     const bool spread = a.d_gate != nullptr && blocks > 8 * static_cast<int64_t>(a.spans.batch);
-    const unsigned rows = of_norm + of_branch + (spread ? a.spans.batch : 0);
+    const unsigned rows = of_norm + of_scale + of_post + (spread ? a.spans.batch : 0);
     if (rows > 0) {
-        hipLaunchKernelGGL(residual_sums_kernel, dim3((a.width + 15) / 16, rows), dim3(1024), 0, stream, a, static_cast<int>(blocks), of_norm, of_branch, is_bf16);
+        hipLaunchKernelGGL(residual_sums_kernel, dim3((a.width + 15) / 16, rows), dim3(1024), 0, stream, a, static_cast<int>(blocks), of_norm, of_scale, of_post, is_bf16);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

@@ -402,7 +402,8 @@ hipError_t launch_rotary_norm_grad(const RotaryArgs &a, bool is_bf16, hipStream_
 hipError_t launch_rotary_status(const RotaryArgs &a, int *status, hipStream_t stream);
 
 // x_row, f_row, gate_row: elements between rows; all others are packed.  rows_per_block: rows of a workgroup, which follow one another.
-// part: [4][workgroups][width], part_gate: [workgroups + batch - 1][width], or null.
+// part: [kResidualParts][workgroups][width], part_gate: [workgroups + batch - 1][width], or null.
+constexpr int kResidualParts = 5;
 struct ResidualArgs {
     const void *x, *f, *gate;
     int64_t x_row, f_row, gate_row;

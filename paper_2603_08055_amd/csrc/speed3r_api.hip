@@ -1779,7 +1779,7 @@ s3r_status plan_residual(const s3r_residual_params *p, bool backward, ResidualPl
     const size_t row = static_cast<size_t>(p->width) * sizeof(float);
     size_t off = 0;
     c.part = off;
-    if (p->d_weight || p->d_bias || p->d_scale || p->d_post_weight || p->d_post_bias) off += align_up(4 * static_cast<size_t>(c.blocks) * row);
+    if (p->d_weight || p->d_bias || p->d_scale || p->d_post_weight || p->d_post_bias) off += align_up(s3r::kResidualParts * static_cast<size_t>(c.blocks) * row);
     c.part_gate = off;
     if (p->d_gate) off += align_up((static_cast<size_t>(c.blocks) + c.batch) * row);
     c.need = off;

@@ -32,3 +32,48 @@ def test_an_infinite_gradient_without_a_post_bias(s3r, types, width, post):
     want = residual(c["x"], c["f"], "layer", c["weight"], None, 1e-6, post, c["post_weight"], None, c["scale"], None, None, 0.75, c["d_r"], c["d_y"],
                     c["dtype"], c["w_dtype"])
     check("d_scale", got["d_scale"], want["d_scale"])
+
+
+@pytest.mark.parametrize("x_dtype,dtype", [(F32, F32), (BF16, BF16), (F32, BF16)])
+@pytest.mark.parametrize("n,width,lengths", [
+    (800, 64, None), (100000, 64, None), (800, 64, [500, 1, 0, 299]), (800, 128, [800]), (800, 256, None), (800, 520, [700, 100]), (3000, 1000, None),
+    (800, 1024, [500, 1, 299]), (800, 2048, [800]), (800, 4096, [1, 799]), (800, 8192, None), (800, 8192, [300, 0, 77, 423]), (1500, 64, [1] * 1500)])
+def test_products_that_cancel_before_they_are_summed(s3r, x_dtype, dtype, n, width, lengths):
+    """Rows of one number, so that the post-norm leaves the same nu of all, and u = nu w + b with w = 1.5, b = -w nu (1 - 2^-16): of the gradients of scale
+    and gate, sums of dr' u, each part, w sum dr' nu and b sum dr', is 2^16 times the whole, and a rounding of one of them to fp32 is 2^-8 of it.
+
+    nu is known to 6 u alone (u = 2^-24), but is the same for all rows and channels, as is the rounding of nu w + b: a gradient over the exact sum of its
+    channel's d_r (y is not asked for, so that dr' is d_r) has to be the same for all channels but for the roundings of sums of terms of one sign: up to 8 rows
+    of a thread, 32 rows side by side and, where sequences are single rows, 32 of these, the products with the gate and with scale, and the store: 44 u, 76 u
+    for single rows, either way."""
+    g = gen(width)
+    exact_nu = 1.625 / math.sqrt(1.625 ** 2 + 0.3)
+    f, w = torch.full((n, width), 1.625, dtype=dtype, device="cuda"), torch.full((width,), 1.5, device="cuda")
+    b, scale = (-w.double() * exact_nu * (1 - 2.0 ** -16)).float(), torch.full((width,), 0.5, device="cuda")
+    d_r = (1 + torch.rand((n, width), generator=g, device="cuda")).to(x_dtype)
+    gate = torch.ones((len(lengths), width), dtype=dtype, device="cuda") if lengths else None
+    x = torch.zeros((n, width), dtype=x_dtype, device="cuda")
+    grads = {"d_scale": torch.full((width,), math.nan, device="cuda")}
+    if lengths:
+        grads["d_gate"] = torch.full(gate.shape, math.nan, dtype=dtype, device="cuda")
+    s3r.speed3r_residual_norm_backward(x, None, torch.empty_like(x), d_r=d_r, df=torch.empty_like(f), f=f, post_norm="rms", post_weight=w, post_bias=b, scale=scale,
+                                       gate=gate, row_start=starts(lengths) if lengths else None, eps=0.3, **grads)
+    u = 2.0 ** -24
+    nu_err = 7 * u * 2.0 ** 16                                        # of what nu w + b is, and a rounding of b
+
+    def same(name, got, size, factor, store):
+        ratio = got.double() / size / (1.5 * exact_nu * factor * 2.0 ** -16)
+        mean = float(ratio.mean())
+        off = float((ratio - mean).abs().max()) / mean
+        bound = (76 if lengths and len(lengths) > 300 else 44) * u + store
+        print(f"{name}: {mean:.6f}, {off / bound:.3f} of its bound", flush=True)
+        assert abs(mean - 1) <= nu_err + store and off <= 2 * bound
+
+    same("d_scale", grads["d_scale"], d_r.double().sum(0), 1.0, 0.0)
+    if lengths:
+        store = torch.finfo(dtype).eps / 2 if dtype != F32 else 0.0
+        for i, part in enumerate(d_r.double().split(lengths)):
+            if lengths[i] == 0:
+                assert not grads["d_gate"][i].any()
+            elif i < 10:
+                same(f"d_gate {i}", grads["d_gate"][i], part.sum(0), 0.5, store)
