@@ -420,7 +420,8 @@ size_t speed3r_rotary_workspace_bytes(const s3r_rotary_params *p);
  *   Types: the stream (x, r and their gradients) is of x_dtype: dtype, or fp32 with everything else in bf16.  weights, biases and scale
  *   are of weight_dtype, gates of dtype.
  * The gradient takes those of y and r (either may be NULL: 0), x and f again, and gives
- * those of x, f and of every weight that is asked for, sums in an order that does not depend on that of the workgroups. */
+ * those of x, f and of every weight that is asked for, sums in an order that does not depend on that of the workgroups, of which at most
+ * 256 terms and 32 sums of these are added one after the other in fp32, and all beyond that in 64 bits. */
 typedef struct s3r_residual_params {
     const void *x, *f;            /* in  [n_rows][width] (or *_stride)                                   */
     void *r, *y;                  /* out, packed; r may be x itself where x is packed                    */

@@ -10,11 +10,13 @@
 // Bound by HBM: every row is read once and written once.  A row is in the registers of L lanes of one wave, or of W waves, CH
 // chunks of eight channels in each; sums over a row are lane moves, and a trip through LDS where waves share one.  Sums over rows stay in
 // registers for the rows of a workgroup, which follow one another; what the workgroups have is added up by another launch in a
-// fixed order.
+// fixed order.  256 terms and fewer are added in fp32 by a thread, then those of the workgroup's rows side by side; the rest in 64 bits.
 // Rows of 1024: 137400 with an fp32 stream beside bf16, channel scale and LayerNorm, 337 us, 5.0 TB/s, the rate of a copy of as much (4.97);
 // 41220 all in bf16 60 us, 5.7 TB/s, their gradient 109 us, 4.65 TB/s (six tensors at once), and 6 us for the sums.  3001 rows of 1000 in
 // fp32 with a post-norm and gates: 13 us (3.7 TB/s) and 27 + 7 (2.7 TB/s): four sums over a row, one after the other, and six rows for a workgroup, two at a time.
 #include "s3r_lanes_device.h"
+
+#include <type_traits>
 
 namespace s3r {
 
@@ -252,15 +254,35 @@ template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ _
     }
 }
 
-// A workgroup's sums over rows, of each of its threads' channels, to `to` [width].  Rows of a workgroup side by side are added up in LDS.
-template <int L, int W, int CH, typename Part> __device__ __forceinline__ void store_sums(const float (&s)[CH][8], float *to, int width, const Part &part, float *lds)
+// A place [width] for a workgroup's sums: fp32, or (WIDE) 64 bits, where they come in shares (see ResidualArgs::turns), which all but the first are added to it.
+template <bool WIDE> struct Place {
+    std::conditional_t<WIDE, double, float> *at;
+    bool add;
+    __device__ __forceinline__ Place(void *base, int64_t offset, bool add_) : at(static_cast<decltype(at)>(base) + offset), add(add_) {}
+    __device__ __forceinline__ void put(int channel, float x) const
+    {
+        if constexpr (WIDE)
+            at[channel] = (add ? at[channel] : 0.0) + static_cast<double>(x);
+        else
+            at[channel] = x;
+    }
+};
+
+// A workgroup's sums over rows, of each of its threads' channels.  Rows of a workgroup side by side are added up in LDS.
+template <int L, int W, int CH, bool WIDE, typename Part> __device__ __forceinline__ void store_sums(const float (&s)[CH][8], const Place<WIDE> &to, int width, const Part &part, float *lds)
 {
     constexpr int kRows = Part::kRows;
     if constexpr (kRows == 1) {
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
-            if (part.has[i]) Io8<float>::store(to + part.at(i), s[i]);
-        return;
+        for (int i = 0; i < CH; ++i) {
+            if (!part.has[i]) continue;
+            if constexpr (WIDE) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) to.put(part.at(i) + j, s[i][j]);
+            } else {
+                Io8<float>::store(to.at + part.at(i), s[i]);
+            }
+        }
     } else {
         constexpr int kWidth = 8 * L * W;   // channels of one chunk of all threads of a row
 #pragma unroll
@@ -275,7 +297,7 @@ template <int L, int W, int CH, typename Part> __device__ __forceinline__ void s
                 float sum = 0.f;
 #pragma unroll
                 for (int r = 0; r < kRows; ++r) sum += lds[r * kWidth + c];
-                to[channel] = sum;
+                to.put(channel, sum);
             }
         }
     }
@@ -285,6 +307,10 @@ template <int L, int W, int CH, typename Part> __device__ __forceinline__ void s
 template <int THREADS, int CH> struct OwnSum {
     floatx4 *at;  // [2 CH][THREADS]
     __device__ __forceinline__ OwnSum(float *lds, int which) : at(reinterpret_cast<floatx4 *>(lds) + which * (2 * CH * THREADS) + threadIdx.x)
+    {
+        clear();
+    }
+    __device__ __forceinline__ void clear()
     {
 #pragma unroll
         for (int i = 0; i < 2 * CH; ++i) at[i * THREADS] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -350,7 +376,8 @@ template <typename TX, typename T, int CH> struct GradRows {
 //   d gate = residual_scale scale C,  and with GA, GB and GC the sums of gate A, gate B and gate C over the sequences,
 //   d scale = residual_scale GC,  d post_weight = residual_scale scale GA,  d post_bias = residual_scale scale GB.
 // (C is post_weight A + post_bias B, but u may be far smaller than these parts, and then that loses what a sum of its own keeps.)
-template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ __launch_bounds__(threads_of(W)) void residual_grad_kernel(ResidualArgs a)
+// WIDE: in shares (a.wide), of which each starts with sums of 0.
+template <typename TX, typename T, int L, int W, int CH, bool FULL, bool WIDE> __global__ __launch_bounds__(threads_of(W)) void residual_grad_kernel(ResidualArgs a)
 {
     using Part = RowPart<L, W, CH>;
     constexpr int kThreads = threads_of(W);
@@ -362,7 +389,6 @@ template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ _
     const float of_width = 1.f / static_cast<float>(a.width);
     const int64_t r0 = static_cast<int64_t>(blockIdx.x) * a.rows_per_block, r1 = min(r0 + a.rows_per_block, a.n);
     const int64_t share = static_cast<int64_t>(gridDim.x) * a.width;
-    float *to_part = a.part + blockIdx.x * static_cast<int64_t>(a.width);
     float w[CH][8], factor[CH][8], pw[CH][8], pb[CH][8], dw[CH][8], db[CH][8], sa[CH][8], sb[CH][8], sc[CH][8];  // (not FULL: A is C)
     channel_weights<CH>(a.weight, a.w_bf16, part, 1.f, w);
     constexpr int kOwn = FULL && !kWide ? CH : 0, kAside = kWide ? CH : 0;
@@ -389,161 +415,205 @@ template <typename TX, typename T, int L, int W, int CH, bool FULL> __global__ _
     const bool gated = FULL && a.gate != nullptr, with_f = a.f != nullptr;
     const bool of_scale = a.part != nullptr && a.d_scale != nullptr, of_post_weight = a.part != nullptr && a.d_post_weight != nullptr,
                of_post_bias = a.part != nullptr && a.d_post_bias != nullptr;
-    // What the workgroup has of a sum over sequences, to its place.
-    auto store_part = [&](int which, const float (&x)[CH][8]) { store_sums<L, W, CH>(x, to_part + which * share, a.width, part, join); };
-    bool fresh = true;  // no sequence yet
-    // Sequence by sequence (without gates: all rows at once).
-    for (int seq = gated ? find_sequence(a.spans, r0) : 0; seq < a.spans.batch; ++seq) {
-        int first_row = 0, len = 0;
-        if (gated) a.spans.of(seq, first_row, len);
-        if (first_row >= r1) break;
-        const int64_t from = gated ? max(r0, static_cast<int64_t>(first_row)) : r0, to = gated ? min(r1, static_cast<int64_t>(first_row) + len) : r1;
-        if (from >= to) continue;
-        GradRows<TX, T, CH> ahead;
-        constexpr bool kAhead = W * CH < 16 || (!FULL && sizeof(TX) == 2);  // (the widest rows leave no registers for the next one)
-        if (kAhead) ahead.load(a, from + part.sub, to, part);
-        auto get_gate = [&](float (&gate)[CH][8]) {
-            Raw<T, CH> raw;
-            raw.load(static_cast<const T *>(a.gate) + seq * a.gate_row, part);
-            raw.get(gate, part);
-        };
-        channel_weights<CH>(a.scale, a.w_bf16, part, 1.f, factor);
-        {
-            float gate[CH][8];
-            if (gated) get_gate(gate);
+    auto place = [&](int which, bool add) { return Place<WIDE>(a.part, which * share + blockIdx.x * static_cast<int64_t>(a.width), add); };
+    auto clear = [&](float (&x)[CH][8]) {
 #pragma unroll
-            for (int i = 0; i < CH; ++i)
+        for (int i = 0; i < CH; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    factor[i][j] *= a.residual_scale;
-                    if (gated) factor[i][j] *= gate[i][j];
-                }
-        }
-        for (int64_t first = from; first < to; first += Part::kRows) {
-            const int64_t row = first + part.sub;
-            const bool ok = Part::kRows == 1 || row < to;
-            float z[CH][8], n[CH][8], g[CH][8], d[CH][8];
-            GradRows<TX, T, CH> here;
-            if (kAhead) here = ahead; else here.load(a, row, to, part);
-            here.x.get(z, part);
-            if (with_f) here.f.get(n, part);
-            if (a.d_y != nullptr) here.dy.get(g, part);
-            if (a.d_r != nullptr) here.dr.get(d, part);
-            if (kAhead) ahead.load(a, row + Part::kRows, to, part);
-            float post_inv = 0.f;
-            if constexpr (FULL)
-                if (a.post != kNormNone) post_inv = row_norm<CH>(a.post, a.eps, of_width, part, n);
-            if (a.d_r == nullptr)
-#pragma unroll
-                for (int i = 0; i < CH; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) d[i][j] = 0.f;
-            if (a.d_y != nullptr) {
-                if (with_f) {
-                    get_post();
-#pragma unroll
-                    for (int i = 0; i < CH; ++i)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) z[i][j] = fmaf(factor[i][j], FULL ? fmaf(n[i][j], pw[i][j], pb[i][j]) : n[i][j], z[i][j]);
-                }
-                const float inv = row_norm<CH>(a.norm, a.eps, of_width, part, z);
-                if constexpr (kWide) {  // (one row at a time)
-                    own_dw.add(g, z);
-                    own_db.add(g);
-                }
+            for (int j = 0; j < 8; ++j) x[i][j] = 0.f;
+    };
+    bool fresh = true;  // nothing in the places of the sums over sequences yet
+    // In shares of `turns` rows of a thread (and sequences), as many as are added up in fp32; sequence by sequence (without gates: all rows at once).
+    int seq = gated ? find_sequence(a.spans, r0) : 0;
+    int64_t next = r0;  // of a sequence that a share ended in
+    bool more = true;
+    for (bool first_share = true; more; first_share = false) {
+        more = false;
+        int turns = a.turns;
+        for (; seq < a.spans.batch; ++seq) {
+            int first_row = 0, len = 0;
+            if (gated) a.spans.of(seq, first_row, len);
+            if (first_row >= r1) break;
+            const int64_t begin = gated ? max(r0, static_cast<int64_t>(first_row)) : r0, end = gated ? min(r1, static_cast<int64_t>(first_row) + len) : r1;
+            const int64_t from = WIDE ? max(begin, next) : begin, to = WIDE ? min(end, from + static_cast<int64_t>(turns) * Part::kRows) : end;
+            if (from >= end) continue;
+            if constexpr (WIDE) {
+                more = turns <= 0;
+                if (more) break;
+                turns -= static_cast<int>((to - from + Part::kRows - 1) / Part::kRows);
+            }
+            GradRows<TX, T, CH> ahead;
+            constexpr bool kAhead = W * CH < 16 || (!FULL && sizeof(TX) == 2);  // (the widest rows leave no registers for the next one)
+            if (kAhead) ahead.load(a, from + part.sub, to, part);
+            auto get_gate = [&](float (&gate)[CH][8]) {
+                Raw<T, CH> raw;
+                raw.load(static_cast<const T *>(a.gate) + seq * a.gate_row, part);
+                raw.get(gate, part);
+            };
+            channel_weights<CH>(a.scale, a.w_bf16, part, 1.f, factor);
+            {
+                float gate[CH][8];
+                if (gated) get_gate(gate);
 #pragma unroll
                 for (int i = 0; i < CH; ++i)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        if (!kWide && ok) {
-                            dw[i][j] = fmaf(g[i][j], z[i][j], dw[i][j]);
-                            db[i][j] += g[i][j];
-                        }
-                        g[i][j] *= w[i][j];
+                        factor[i][j] *= a.residual_scale;
+                        if (gated) factor[i][j] *= gate[i][j];
                     }
-                row_norm_back<CH>(a.norm, of_width, inv, z, part, g);
-#pragma unroll
-                for (int i = 0; i < CH; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) d[i][j] += g[i][j];
             }
-            store_row<TX, CH>(static_cast<TX *>(a.dx) + row * a.width, d, part, ok);
-            if (!with_f) continue;
-            if constexpr (FULL) get_post();
+            for (int64_t first = from; first < to; first += Part::kRows) {
+                const int64_t row = first + part.sub;
+                const bool ok = Part::kRows == 1 || row < to;
+                float z[CH][8], n[CH][8], g[CH][8], d[CH][8];
+                GradRows<TX, T, CH> here;
+                if (kAhead) here = ahead; else here.load(a, row, to, part);
+                here.x.get(z, part);
+                if (with_f) here.f.get(n, part);
+                if (a.d_y != nullptr) here.dy.get(g, part);
+                if (a.d_r != nullptr) here.dr.get(d, part);
+                if (kAhead) ahead.load(a, row + Part::kRows, to, part);
+                float post_inv = 0.f;
+                if constexpr (FULL)
+                    if (a.post != kNormNone) post_inv = row_norm<CH>(a.post, a.eps, of_width, part, n);
+                if (a.d_r == nullptr)
 #pragma unroll
-            for (int i = 0; i < CH; ++i)
+                    for (int i = 0; i < CH; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    if (ok) {
-                        if constexpr (FULL) {
-                            sa[i][j] = fmaf(d[i][j], n[i][j], sa[i][j]);
-                            sb[i][j] += d[i][j];
-                        }
-                        sc[i][j] = fmaf(d[i][j], FULL ? fmaf(n[i][j], pw[i][j], pb[i][j]) : n[i][j], sc[i][j]);
+                        for (int j = 0; j < 8; ++j) d[i][j] = 0.f;
+                if (a.d_y != nullptr) {
+                    if (with_f) {
+                        get_post();
+#pragma unroll
+                        for (int i = 0; i < CH; ++i)
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) z[i][j] = fmaf(factor[i][j], FULL ? fmaf(n[i][j], pw[i][j], pb[i][j]) : n[i][j], z[i][j]);
                     }
-                    d[i][j] *= FULL ? factor[i][j] * pw[i][j] : factor[i][j];
-                }
-            if constexpr (FULL)
-                if (a.post != kNormNone) row_norm_back<CH>(a.post, of_width, post_inv, n, part, d);
-            store_row<T, CH>(static_cast<T *>(a.df) + row * a.width, d, part, ok);
-        }
-        if constexpr (FULL) {
-            if (!gated) break;
-            float gate[CH][8];
-            get_gate(gate);
-            if (a.part_gate != nullptr)  // at place blockIdx.x + seq, which no other pair has
-                store_sums<L, W, CH>(sc, a.part_gate + (static_cast<int64_t>(blockIdx.x) + seq) * a.width, a.width, part, join);
-            // times the gate to the sums over sequences
-            auto add = [&](float (&sums)[CH][8], int which, OwnSum<kThreads, kOwn> &own) {
-#pragma unroll
-                for (int i = 0; i < CH; ++i) {
-                    if constexpr (kWide) {
-                        if (!part.has[i]) continue;
-                        float *at = to_part + which * share + part.at(i);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) sums[i][j] *= gate[i][j];
-                        if (!fresh) {
-                            Io8<float> x;
-                            x.load(at);
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) sums[i][j] += x.get(j);
-                        }
-                        Io8<float>::store(at, sums[i]);
+                    const float inv = row_norm<CH>(a.norm, a.eps, of_width, part, z);
+                    if constexpr (kWide) {  // (one row at a time)
+                        own_dw.add(g, z);
+                        own_db.add(g);
                     }
+#pragma unroll
+                    for (int i = 0; i < CH; ++i)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            if (!kWide && ok) {
+                                dw[i][j] = fmaf(g[i][j], z[i][j], dw[i][j]);
+                                db[i][j] += g[i][j];
+                            }
+                            g[i][j] *= w[i][j];
+                        }
+                    row_norm_back<CH>(a.norm, of_width, inv, z, part, g);
+#pragma unroll
+                    for (int i = 0; i < CH; ++i)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) d[i][j] += g[i][j];
                 }
-                if constexpr (!kWide) own.add(sums, gate);
+                store_row<TX, CH>(static_cast<TX *>(a.dx) + row * a.width, d, part, ok);
+                if (!with_f) continue;
+                if constexpr (FULL) get_post();
 #pragma unroll
                 for (int i = 0; i < CH; ++i)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) sums[i][j] = 0.f;
-            };
-            if (of_scale || !kWide) add(sc, kPartC, gc);
-            if (of_post_weight || !kWide) add(sa, kPartA, ga);
-            if (of_post_bias || !kWide) add(sb, kPartB, gb);
-            fresh = false;
-        } else {
-            break;
+                    for (int j = 0; j < 8; ++j) {
+                        if (ok) {
+                            if constexpr (FULL) {
+                                sa[i][j] = fmaf(d[i][j], n[i][j], sa[i][j]);
+                                sb[i][j] += d[i][j];
+                            }
+                            sc[i][j] = fmaf(d[i][j], FULL ? fmaf(n[i][j], pw[i][j], pb[i][j]) : n[i][j], sc[i][j]);
+                        }
+                        d[i][j] *= FULL ? factor[i][j] * pw[i][j] : factor[i][j];
+                    }
+                if constexpr (FULL)
+                    if (a.post != kNormNone) row_norm_back<CH>(a.post, of_width, post_inv, n, part, d);
+                store_row<T, CH>(static_cast<T *>(a.df) + row * a.width, d, part, ok);
+            }
+            if constexpr (FULL)
+                if (gated) {
+                    float gate[CH][8];
+                    get_gate(gate);
+                    if (a.part_gate != nullptr)  // at place blockIdx.x + seq, which no other pair has
+                        store_sums<L, W, CH>(sc, Place<WIDE>(a.part_gate, (static_cast<int64_t>(blockIdx.x) + seq) * a.width, from > begin), a.width, part, join);
+                    // times the gate to the sums over sequences
+                    auto add = [&](float (&sums)[CH][8], int which, OwnSum<kThreads, kOwn> &own) {
+                        if constexpr (kWide) {
+                            const Place<WIDE> to = place(which, !fresh);
+#pragma unroll
+                            for (int i = 0; i < CH; ++i) {
+                                if (!part.has[i]) continue;
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) sums[i][j] *= gate[i][j];
+                                if constexpr (!WIDE)
+                                    if (!fresh) {
+                                        Io8<float> x;
+                                        x.load(to.at + part.at(i));
+#pragma unroll
+                                        for (int j = 0; j < 8; ++j) sums[i][j] += x.get(j);
+                                    }
+                            }
+                            store_sums<L, W, CH>(sums, to, a.width, part, join);
+                        } else {
+                            own.add(sums, gate);
+                        }
+                        clear(sums);
+                    };
+                    if (of_scale || !kWide) add(sc, kPartC, gc);
+                    if (of_post_weight || !kWide) add(sa, kPartA, ga);
+                    if (of_post_bias || !kWide) add(sb, kPartB, gb);
+                    fresh = false;
+                }
+            if constexpr (WIDE) {
+                next = to < end ? to : r0;
+                more = to < end;
+                if (more) break;
+            }
+            if (!gated) break;
         }
+        if (a.part == nullptr) {
+            if constexpr (WIDE) continue;
+            return;
+        }
+        if (a.d_weight != nullptr || a.d_bias != nullptr) {
+            if constexpr (kWide) {
+                own_dw.get(dw);
+                own_db.get(db);
+                if constexpr (WIDE) {
+                    own_dw.clear();
+                    own_db.clear();
+                }
+            }
+            store_sums<L, W, CH>(dw, place(kPartWeight, !first_share), a.width, part, join);
+            store_sums<L, W, CH>(db, place(kPartBias, !first_share), a.width, part, join);
+            if constexpr (WIDE) {
+                clear(dw);
+                clear(db);
+            }
+        }
+        if (kWide && gated && !fresh) {
+            if constexpr (WIDE) continue;
+            return;
+        }
+        if constexpr (kOwn > 0)
+            if (gated) {
+                ga.get(sa);
+                gb.get(sb);
+                gc.get(sc);
+                if constexpr (WIDE) {
+                    ga.clear();
+                    gb.clear();
+                    gc.clear();
+                }
+            }
+        if (of_scale) store_sums<L, W, CH>(sc, place(kPartC, !first_share), a.width, part, join);
+        if (of_post_weight) store_sums<L, W, CH>(sa, place(kPartA, !first_share), a.width, part, join);
+        if (of_post_bias) store_sums<L, W, CH>(sb, place(kPartB, !first_share), a.width, part, join);
+        if constexpr (!WIDE) return;
+        clear(sa);
+        clear(sb);
+        clear(sc);
     }
-    if (a.part == nullptr) return;
-    if (a.d_weight != nullptr || a.d_bias != nullptr) {
-        if constexpr (kWide) {
-            own_dw.get(dw);
-            own_db.get(db);
-        }
-        store_part(kPartWeight, dw);
-        store_part(kPartBias, db);
-    }
-    if (kWide && gated && !fresh) return;
-    if constexpr (kOwn > 0)
-        if (gated) {
-            ga.get(sa);
-            gb.get(sb);
-            gc.get(sc);
-        }
-    if (of_scale) store_part(kPartC, sc);
-    if (of_post_weight) store_part(kPartA, sa);
-    if (of_post_bias) store_part(kPartB, sb);
 }
 
 __device__ __forceinline__ float weight_at(const void *w, bool is_bf16, int c, float none)
@@ -554,7 +624,7 @@ __device__ __forceinline__ float weight_at(const void *w, bool is_bf16, int c, f
 
 // What is made of the workgroups' sums, 16 channels for a workgroup; blockIdx.y: d weight and d bias (of_norm), then d scale (of_scale), then d post
 // weight and d post bias (of_post), then the gates, sequence by sequence.
-__global__ __launch_bounds__(1024) void residual_sums_kernel(ResidualArgs a, int blocks, bool of_norm, bool of_scale, bool of_post, bool is_bf16)
+template <typename P> __global__ __launch_bounds__(1024) void residual_sums_kernel(ResidualArgs a, int blocks, bool of_norm, bool of_scale, bool of_post, bool is_bf16)
 {
     __shared__ union { PartSums<2> two; PartSums<1> one; } lds;
     const int c = blockIdx.x * 16 + (threadIdx.x & 15), four = blockIdx.x * 16 + 4 * (threadIdx.x & 3);
@@ -563,20 +633,21 @@ __global__ __launch_bounds__(1024) void residual_sums_kernel(ResidualArgs a, int
     const double scale = a.residual_scale * static_cast<double>(mine ? weight_at(a.scale, a.w_bf16, c, 1.f) : 0.f);
     const int64_t gap = static_cast<int64_t>(blocks) * a.width;
     const bool first = of_norm && y == 0;
+    const P *part = static_cast<const P *>(a.part);
     double s[2];
     if (seq >= 0) {
         int row, len;
         a.spans.of(seq, row, len);
         const int64_t from = row / a.rows_per_block, count = len > 0 ? (static_cast<int64_t>(row) + len - 1) / a.rows_per_block - from + 1 : 0;
-        sum_parts<1, 2>(a.part_gate + (from + seq) * a.width + four, count, a.width, 0, ok, lds.one, reinterpret_cast<double(&)[1]>(s));
+        sum_parts<1, 2>(static_cast<const P *>(a.part_gate) + (from + seq) * a.width + four, count, a.width, 0, ok, lds.one, reinterpret_cast<double(&)[1]>(s));
         if (mine) store_weight(a.d_gate, is_bf16, static_cast<int64_t>(seq) * a.width + c, static_cast<float>(scale * s[0]));
     } else if (of_scale && y == of_norm) {
-        sum_parts<1, 2>(a.part + kPartC * gap + four, blocks, a.width, 0, ok, lds.one, reinterpret_cast<double(&)[1]>(s));
+        sum_parts<1, 2>(part + kPartC * gap + four, blocks, a.width, 0, ok, lds.one, reinterpret_cast<double(&)[1]>(s));
         if (mine) store_weight(a.d_scale, a.w_bf16, c, static_cast<float>(a.residual_scale * s[0]));
     } else {
         // (a sum that is not asked for may not be there: the other one in its place)
         const int at = first ? kPartWeight : (a.d_post_weight != nullptr ? kPartA : kPartB);
-        sum_parts<2, 2>(a.part + at * gap + four, blocks, a.width, first || (a.d_post_weight != nullptr && a.d_post_bias != nullptr) ? gap : 0, ok, lds.two, s);
+        sum_parts<2, 2>(part + at * gap + four, blocks, a.width, first || (a.d_post_weight != nullptr && a.d_post_bias != nullptr) ? gap : 0, ok, lds.two, s);
         void *const one = first ? a.d_weight : a.d_post_weight, *const two = first ? a.d_bias : a.d_post_bias;
         if (mine && one != nullptr) store_weight(one, a.w_bf16, c, static_cast<float>(first ? s[0] : scale * s[0]));
         if (mine && two != nullptr) store_weight(two, a.w_bf16, c, static_cast<float>(first ? s[1] : scale * s[1]));
@@ -584,7 +655,7 @@ __global__ __launch_bounds__(1024) void residual_sums_kernel(ResidualArgs a, int
 }
 
 // The gates of sequences that few workgroups had rows of each: a thread for a channel.
-__global__ __launch_bounds__(256) void residual_gate_kernel(ResidualArgs a, bool is_bf16)
+template <typename P> __global__ __launch_bounds__(256) void residual_gate_kernel(ResidualArgs a, bool is_bf16)
 {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     const int seq = static_cast<int>(i / a.width), c = static_cast<int>(i % a.width);
@@ -592,7 +663,7 @@ __global__ __launch_bounds__(256) void residual_gate_kernel(ResidualArgs a, bool
     int row, len;
     a.spans.of(seq, row, len);
     const int64_t from = row / a.rows_per_block, count = len > 0 ? (static_cast<int64_t>(row) + len - 1) / a.rows_per_block - from + 1 : 0;
-    const float *part = a.part_gate + (from + seq) * a.width + c;
+    const P *part = static_cast<const P *>(a.part_gate) + (from + seq) * a.width + c;
     double s = 0.0;
     for (int64_t g = 0; g < count; ++g) s += part[g * a.width];
     store_weight(a.d_gate, is_bf16, i, static_cast<float>(s * a.residual_scale * weight_at(a.scale, a.w_bf16, c, 1.f)));
@@ -601,13 +672,14 @@ __global__ __launch_bounds__(256) void residual_gate_kernel(ResidualArgs a, bool
 // Kernels for rows of up to 64, 128, 256 .. channels: lanes, waves and chunks of a row.
 template <typename TX, typename T, bool FULL> struct Kernels {
     struct { void (*kernel)(ResidualArgs); int threads; size_t lds; } forward, grad;
+    bool wide;
     template <int L, int W, int CH> void set_forward() { forward = {&residual_kernel<TX, T, L, W, CH, FULL>, threads_of(W), 0}; }
     template <int L, int W, int CH> void set_grad()
     {
-        grad = {&residual_grad_kernel<TX, T, L, W, CH, FULL>, threads_of(W), kGradLds<W, CH, FULL>};
+        grad = {wide ? &residual_grad_kernel<TX, T, L, W, CH, FULL, true> : &residual_grad_kernel<TX, T, L, W, CH, FULL, false>, threads_of(W), kGradLds<W, CH, FULL>};
     }
     template <int L, int W, int CH> void set() { set_forward<L, W, CH>(); set_grad<L, W, CH>(); }
-    explicit Kernels(int width)
+    Kernels(int width, bool wide_) : wide(wide_)
     {
         if (width <= 64) set<8, 1, 1>();
         else if (width <= 128) set<16, 1, 1>();
@@ -630,9 +702,9 @@ template <typename TX, typename T, bool FULL> struct Kernels {
 template <typename Launch> hipError_t by_type(const ResidualArgs &a, bool x_bf16, bool is_bf16, Launch &&launch)
 {
     const bool full = a.post != kNormNone || a.gate != nullptr;
-    if (!is_bf16) return full ? launch(Kernels<float, float, true>(a.width)) : launch(Kernels<float, float, false>(a.width));
-    if (x_bf16) return full ? launch(Kernels<bf16_t, bf16_t, true>(a.width)) : launch(Kernels<bf16_t, bf16_t, false>(a.width));
-    return full ? launch(Kernels<float, bf16_t, true>(a.width)) : launch(Kernels<float, bf16_t, false>(a.width));
+    if (!is_bf16) return full ? launch(Kernels<float, float, true>(a.width, a.wide)) : launch(Kernels<float, float, false>(a.width, a.wide));
+    if (x_bf16) return full ? launch(Kernels<bf16_t, bf16_t, true>(a.width, a.wide)) : launch(Kernels<bf16_t, bf16_t, false>(a.width, a.wide));
+    return full ? launch(Kernels<float, bf16_t, true>(a.width, a.wide)) : launch(Kernels<float, bf16_t, false>(a.width, a.wide));
 }
 
 }  // namespace
@@ -663,13 +735,13 @@ hipError_t launch_residual_grad(const ResidualArgs &a, bool x_bf16, bool is_bf16
     const bool spread = a.d_gate != nullptr && blocks > 8 * static_cast<int64_t>(a.spans.batch);
     const unsigned rows = of_norm + of_scale + of_post + (spread ? a.spans.batch : 0);
     if (rows > 0) {
-        hipLaunchKernelGGL(residual_sums_kernel, dim3((a.width + 15) / 16, rows), dim3(1024), 0, stream, a, static_cast<int>(blocks), of_norm, of_scale, of_post, is_bf16);
+        hipLaunchKernelGGL(a.wide ? &residual_sums_kernel<double> : &residual_sums_kernel<float>, dim3((a.width + 15) / 16, rows), dim3(1024), 0, stream, a, static_cast<int>(blocks), of_norm, of_scale, of_post, is_bf16);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     if (a.d_gate == nullptr || spread) return hipSuccess;
     const int64_t gates = (static_cast<int64_t>(a.spans.batch) * a.width + 255) / 256;
-    hipLaunchKernelGGL(residual_gate_kernel, dim3(static_cast<unsigned>(gates)), dim3(256), 0, stream, a, is_bf16);
+    hipLaunchKernelGGL(a.wide ? &residual_gate_kernel<double> : &residual_gate_kernel<float>, dim3(static_cast<unsigned>(gates)), dim3(256), 0, stream, a, is_bf16);
     return hipGetLastError();
 }
 

@@ -402,7 +402,8 @@ hipError_t launch_rotary_norm_grad(const RotaryArgs &a, bool is_bf16, hipStream_
 hipError_t launch_rotary_status(const RotaryArgs &a, int *status, hipStream_t stream);
 
 // x_row, f_row, gate_row: elements between rows; all others are packed.  rows_per_block: rows of a workgroup, which follow one another.
-// part: [kResidualParts][workgroups][width], part_gate: [workgroups + batch - 1][width], or null.
+// part: [kResidualParts][workgroups][width], part_gate: [workgroups + batch - 1][width], or null.  turns: rows of a thread, and sequences with gates, that are
+// added up in fp32 before they go there; wide: a workgroup may have more, and these are 64 bits, to which it adds (else fp32).
 constexpr int kResidualParts = 5;
 struct ResidualArgs {
     const void *x, *f, *gate;
@@ -416,7 +417,9 @@ struct ResidualArgs {
     int width, norm, post, rows_per_block;
     bool w_bf16;
     float eps, residual_scale;
-    float *part, *part_gate;
+    void *part, *part_gate;
+    int turns;
+    bool wide;
 };
 hipError_t launch_residual(const ResidualArgs &a, bool x_bf16, bool is_bf16, hipStream_t stream);
 hipError_t launch_residual_grad(const ResidualArgs &a, bool x_bf16, bool is_bf16, hipStream_t stream);

@@ -61,22 +61,23 @@ __device__ __forceinline__ void store_weight(void *to, bool is_bf16, int64_t at,
         static_cast<float *>(to)[at] = x;
 }
 
-// Sums of N tensors' rows `stride` floats apart, `count` of them, the tensors `gap` apart, of 16 channels, by a workgroup of 1024 threads: a thread
+// Sums of N tensors' rows (fp32 or 64 bits) `stride` apart, `count` of them, the tensors `gap` apart, of 16 channels, by a workgroup of 1024 threads: a thread
 // takes four channels (from: the first of its own, 4 (thread mod 4); ok: they are there) of every 256th row, AT_ONCE of them requested together.  In
 // 64 bits, which cost nothing here, in a fixed order.  To threads 0 .. 15, a channel each.
 template <int N> struct PartSums { double rows[N][128][16], groups[N][16][16]; };
-template <int N, int AT_ONCE> __device__ __forceinline__ void sum_parts(const float *from, int64_t count, int64_t stride, int64_t gap, bool ok, PartSums<N> &lds, double (&s)[N])
+template <int N, int AT_ONCE, typename P> __device__ __forceinline__ void sum_parts(const P *from, int64_t count, int64_t stride, int64_t gap, bool ok, PartSums<N> &lds, double (&s)[N])
 {
+    typedef P P4 __attribute__((ext_vector_type(4)));
     const int t = threadIdx.x, lane = t & 63;
     double own[N][4] = {};
     if (ok)
         for (int64_t i = t >> 2; i < count; i += 256 * AT_ONCE) {
-            floatx4 x[N][AT_ONCE];
+            P4 x[N][AT_ONCE];
 #pragma unroll
             for (int n = 0; n < N; ++n)
 #pragma unroll
                 for (int k = 0; k < AT_ONCE; ++k)
-                    x[n][k] = i + 256 * k < count ? *reinterpret_cast<const floatx4 *>(from + n * gap + (i + 256 * k) * stride) : floatx4{0.f, 0.f, 0.f, 0.f};
+                    x[n][k] = i + 256 * k < count ? *reinterpret_cast<const P4 *>(from + n * gap + (i + 256 * k) * stride) : P4{};
 #pragma unroll
             for (int n = 0; n < N; ++n)
 #pragma unroll

@@ -3,6 +3,7 @@
 #include "../../include/speed3r.h"
 #include "s3r_kernels.h"
 
+#include <climits>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -1737,11 +1738,15 @@ namespace {
 struct ResidualPlan {
     int batch, rows_per_block;
     int64_t blocks;
+    bool wide;                     // sums of the gradient in 64 bits between shares of kResidualTurns
     size_t part, part_gate, need;  // workspace of the gradient
 };
 
 // Workgroups: as many as the card holds at once, or fewer; their rows follow one another, a multiple of what they have at a time.
 constexpr int kResidualBlocks = 2048, kResidualGradBlocks = 512;
+// Terms of a gradient that a thread adds up in fp32, one after the other: off by up to 2^-16 of the sum of their magnitudes.  (512 workgroups reach it at
+// 131072 rows of 2048 channels and more, four million of 64.)
+constexpr int kResidualTurns = 256;
 
 s3r_status plan_residual(const s3r_residual_params *p, bool backward, ResidualPlan *out)
 {
@@ -1776,7 +1781,8 @@ s3r_status plan_residual(const s3r_residual_params *p, bool backward, ResidualPl
     const int64_t rows = ((p->n_rows + most - 1) / most + at_once - 1) / at_once * at_once;
     c.rows_per_block = static_cast<int>(rows < at_once ? at_once : rows);
     c.blocks = (p->n_rows + c.rows_per_block - 1) / c.rows_per_block;
-    const size_t row = static_cast<size_t>(p->width) * sizeof(float);
+    c.wide = c.rows_per_block / at_once + (p->gate ? std::min<int64_t>(c.batch, c.rows_per_block) : 0) > kResidualTurns;
+    const size_t row = static_cast<size_t>(p->width) * (c.wide ? sizeof(double) : sizeof(float));
     size_t off = 0;
     c.part = off;
     if (p->d_weight || p->d_bias || p->d_scale || p->d_post_weight || p->d_post_bias) off += align_up(s3r::kResidualParts * static_cast<size_t>(c.blocks) * row);
@@ -1862,8 +1868,10 @@ s3r_status speed3r_residual_norm_backward(const s3r_residual_params *p)
     a.d_r = p->d_r; a.d_y = p->d_y; a.dx = p->dx; a.df = p->df;
     a.d_weight = p->d_weight; a.d_bias = p->d_bias; a.d_post_weight = p->d_post_weight; a.d_post_bias = p->d_post_bias;
     a.d_scale = p->d_scale; a.d_gate = p->d_gate;
-    if (c.part_gate > c.part) a.part = floats_at(p->workspace, c.part);
-    if (p->d_gate) a.part_gate = floats_at(p->workspace, c.part_gate);
+    a.wide = c.wide;
+    a.turns = c.wide ? kResidualTurns : INT_MAX;
+    if (c.part_gate > c.part) a.part = at(p->workspace, c.part);
+    if (p->d_gate) a.part_gate = at(p->workspace, c.part_gate);
     hipStream_t s = static_cast<hipStream_t>(p->stream);
     if (p->status) S3R_HIP(s3r::launch_span_status(a.spans, a.spans, p->status, s), "status kernel launch");
     StageTimer tm(S3R_STAGE_POOL, s);

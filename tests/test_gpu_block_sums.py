@@ -77,3 +77,58 @@ def test_products_that_cancel_before_they_are_summed(s3r, x_dtype, dtype, n, wid
                 assert not grads["d_gate"][i].any()
             elif i < 10:
                 same(f"d_gate {i}", grads["d_gate"][i], part.sum(0), 0.5, store)
+
+
+ALIKE = 1 + 2.0 ** -13 + 2.0 ** -21    # 1024 to 4096 of them added in fp32, each to the sum of those before, end 2^-14 of the sum too high
+
+
+def close_to(name, got, want, bound):
+    off = float((got.double() / want - 1).abs().max())
+    print(f"{name}: {off / bound:.3f} of its bound", flush=True)
+    assert off <= bound, name
+
+
+@pytest.mark.parametrize("post,lengths", [(None, None), ("rms", None), ("rms", [2 ** 26 - 5, 1, 4]), (None, [2 ** 26])])
+def test_millions_of_terms_of_one_sign(s3r, post, lengths):
+    """2^26 rows of eight channels, whose terms are all the same: a thread has 4096 of them.  At most 256 are added in fp32, 32 rows side by side are,
+    and beyond that 64 bits: 288 u of the sum, and 8 u for n and u (the norm of ones), gate, scale and the store."""
+    n, width, u = 2 ** 26, 8, 2.0 ** -24
+    ones = torch.ones((n, width), device="cuda")
+    d = torch.full((n, width), ALIKE, device="cuda")
+    weight = torch.ones(width, device="cuda")
+    names = ["d_scale", "d_post_weight", "d_post_bias"] if post else ["d_scale"]
+    grads = {name: torch.full((width,), math.nan, device="cuda") for name in names}
+    gate = torch.ones((len(lengths), width), device="cuda") if lengths else None
+    if lengths:
+        grads["d_gate"] = torch.full_like(gate, math.nan)
+    s3r.speed3r_residual_norm_backward(ones, None, torch.empty_like(ones), d_r=d, f=ones.clone(), df=torch.empty_like(ones), post_norm=post, eps=2.0 ** -40,
+                                       post_weight=weight if post else None, scale=weight, gate=gate, row_start=starts(lengths) if lengths else None, **grads)
+    for name in names:
+        close_to(name, grads[name], n * d[0, 0].double(), 296 * u)
+    for b, length in enumerate(lengths or []):
+        close_to(f"d_gate {b}", grads["d_gate"][b], length * d[0, 0].double(), 296 * u)
+    if lengths is None:
+        grads = {name: torch.full((width,), math.nan, device="cuda") for name in ("d_weight", "d_bias")}
+        s3r.speed3r_residual_norm_backward(ones, d, torch.empty_like(ones), norm="rms", weight=weight, eps=2.0 ** -40, **grads,
+                                           **(dict(f=torch.zeros_like(ones), df=torch.empty_like(ones), post_norm=post, post_weight=weight) if post else {}))
+        for name in grads:
+            close_to(name, grads[name], n * d[0, 0].double(), 296 * u)
+
+
+@pytest.mark.parametrize("width", [64, 8192])
+def test_many_sequences_of_a_row_in_one_workgroup(s3r, width):
+    """60000 sequences of a row before a long one, so that some workgroups have hundreds of sequences (or thousands) to add up: terms that are all the
+    same, as above."""
+    n, u = (2 ** 23, 2.0 ** -24) if width == 64 else (2 ** 17, 2.0 ** -24)
+    lengths = [1] * 60000 + [n - 60000]
+    ones = torch.ones((n, width), device="cuda")
+    d = torch.full((n, width), ALIKE, device="cuda")
+    weight, gate = torch.ones(width, device="cuda"), torch.ones((len(lengths), width), device="cuda")
+    grads = {name: torch.full((width,), math.nan, device="cuda") for name in ("d_scale", "d_post_weight", "d_post_bias")}
+    grads["d_gate"] = torch.full_like(gate, math.nan)
+    s3r.speed3r_residual_norm_backward(ones, None, torch.empty_like(ones), d_r=d, f=ones.clone(), df=torch.empty_like(ones), post_norm="rms", eps=2.0 ** -40,
+                                       post_weight=weight, scale=weight, gate=gate, row_start=starts(lengths), **grads)
+    for name in ("d_scale", "d_post_weight", "d_post_bias"):
+        close_to(name, grads[name], n * d[0, 0].double(), 296 * u)
+    close_to("d_gate of a row", grads["d_gate"][:60000], d[0, 0].double(), 10 * u)
+    close_to("d_gate of many", grads["d_gate"][60000], lengths[-1] * d[0, 0].double(), 296 * u)
