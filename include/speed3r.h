@@ -376,7 +376,7 @@ typedef enum { S3R_PAIRS_HALVES = 0, S3R_PAIRS_NEIGHBOURS = 1, S3R_PAIRS_WHOLE =
  *   magnitudes up to 2^56; everything is computed in fp32 and rounded once.
  * Either of q and k may be absent (heads or kv_heads 0); heads need not be a multiple of kv_heads.
  * The gradient takes those of q_out and k_out and, with a norm, q and k again.  The gradients of weights are sums over all rows and heads, in
- * an order that does not depend on that of the workgroups.  Without a norm q, k, and weights are not read. */
+ * an order that does not depend on that of the workgroups, up to 16 terms in fp32 and the rest in 64 bits.  Without a norm q, k, and weights are not read. */
 typedef struct s3r_rotary_params {
     const void *q, *k;            /* in  [n_rows][heads][64], [n_rows][kv_heads][64] (or *_stride_*)     */
     void *q_out, *k_out;          /* out, packed; must not alias inputs                                  */

@@ -186,6 +186,8 @@ __device__ __forceinline__ HeadRun head_run(const RotaryArgs &a, int64_t item, i
     return r;
 }
 
+typedef double doublex2 __attribute__((ext_vector_type(2)));
+
 template <typename T> constexpr int kAhead = sizeof(T) == 4 ? 2 : 4;  // heads whose rows are requested at once: 64 bytes of a lane
 
 template <typename T, Mode MODE, bool NORM> __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int run)
@@ -241,11 +243,13 @@ template <typename T, Mode MODE, bool NORM> __global__ __launch_bounds__(256) vo
     }
 }
 
-// Gradient through a norm.  A workgroup stays with q or with k and adds up what its rows give to the gradients of weight and bias;
-// another launch adds up the workgroups.
+// Gradient through a norm.  A workgroup stays with q or with k and adds up what its rows give to the gradients of weight and bias, a run of heads in
+// fp32 and runs, of which a lane may have thousands, in 64 bits; another launch adds up the workgroups.  (Those totals are in LDS: 32 registers more
+// cost a wave on a SIMD where a lane's angles lie apart, 27480 rows, forward and gradient 114 -> 121 us; from LDS 115.)
 template <typename T, Mode MODE> __global__ __launch_bounds__(256) void rotary_norm_grad_kernel(RotaryArgs a, int run, int wgs_q)
 {
     __shared__ float exchange[4 * 512];
+    __shared__ doublex2 totals[8][256];  // of each thread's channels: dw, db
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     float *lds = exchange + wave * 512;
     const int side = static_cast<int>(blockIdx.x) >= wgs_q ? 1 : 0, first = side == 0 ? 0 : wgs_q, wgs = side == 0 ? wgs_q : static_cast<int>(gridDim.x) - wgs_q;
@@ -255,16 +259,17 @@ template <typename T, Mode MODE> __global__ __launch_bounds__(256) void rotary_n
     Turn<T, MODE> turn;
     const bool turns = a.cos != nullptr;
     turn.place(a, lane);
-    float w[8], dw[8], db[8];
+    float w[8];
     load_weights(s.weight, a.w_bf16, 8 * c, true, 1.f, w);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) dw[j] = db[j] = 0.f;
+    for (int j = 0; j < 8; ++j) totals[j][threadIdx.x] = doublex2{0.0, 0.0};
     for (int64_t item = (static_cast<int64_t>(blockIdx.x) - first) * 4 + wave; item < items; item += 4 * wgs) {
         const HeadRun r = head_run(a, item, side, run, lane);
         const int64_t row = r.ok ? r.row : 0;
         if (turns) turn.load(a, row, lane, -1.f);
         const T *in = static_cast<const T *>(s.in) + row * s.in_row + 8 * c, *grad = static_cast<const T *>(s.grad) + row * s.heads * 64 + 8 * c;
         T *out = static_cast<T *>(s.out) + row * s.out_row + 8 * c;
+        float dw[8] = {}, db[8] = {};
         for (int h0 = r.h0; h0 < r.h1; h0 += kAhead<T>) {
             Io8<T> raw[kAhead<T>], raw_g[kAhead<T>];
 #pragma unroll
@@ -289,10 +294,8 @@ template <typename T, Mode MODE> __global__ __launch_bounds__(256) void rotary_n
                 float s1 = 0.f, s2 = 0.f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    if (r.ok) {
-                        dw[j] = fmaf(g[j], n[j], dw[j]);
-                        db[j] += g[j];
-                    }
+                    dw[j] = fmaf(g[j], n[j], dw[j]);
+                    db[j] += g[j];
                     g[j] *= w[j];
                     s1 += g[j];
                     s2 = fmaf(g[j], n[j], s2);
@@ -304,18 +307,22 @@ template <typename T, Mode MODE> __global__ __launch_bounds__(256) void rotary_n
                 if (r.ok) Io8<T>::store(out + (h0 + i) * s.out_head, x);
             }
         }
+        if (r.ok)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) totals[j][threadIdx.x] += doublex2{static_cast<double>(dw[j]), static_cast<double>(db[j])};
     }
     if (a.part == nullptr) return;
     // the wave's eight rows, then the workgroup's waves
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
+        double dw = totals[j][threadIdx.x][0], db = totals[j][threadIdx.x][1];
         for (int m = 8; m < 64; m <<= 1) {
-            dw[j] += __shfl_xor(dw[j], m, 64);
-            db[j] += __shfl_xor(db[j], m, 64);
+            dw += __shfl_xor(dw, m, 64);
+            db += __shfl_xor(db, m, 64);
         }
         if (lane < 8) {
-            lds[8 * c + j] = dw[j];
-            lds[64 + 8 * c + j] = db[j];
+            lds[8 * c + j] = static_cast<float>(dw);
+            lds[64 + 8 * c + j] = static_cast<float>(db);
         }
     }
     __syncthreads();

@@ -132,3 +132,43 @@ def test_many_sequences_of_a_row_in_one_workgroup(s3r, width):
         close_to(name, grads[name], n * d[0, 0].double(), 296 * u)
     close_to("d_gate of a row", grads["d_gate"][:60000], d[0, 0].double(), 10 * u)
     close_to("d_gate of many", grads["d_gate"][60000], lengths[-1] * d[0, 0].double(), 296 * u)
+
+
+def test_millions_of_rotated_rows_of_one_sign(s3r):
+    """2^26 heads of rows, whose terms are all the same in the channels that are turned (by a cosine of that value): a lane has 4096 of them.  At most the 16
+    heads of a run are added in fp32, four waves at the end, with 5 u for n (the norm of ones), and three roundings: 28 u."""
+    n, heads, u = 2 ** 22, 16, 2.0 ** -24
+    ones = torch.ones((n, heads, 64), dtype=BF16, device="cuda")
+    cos, sin = torch.full((1, 11), ALIKE, device="cuda"), torch.zeros((1, 11), device="cuda")
+    weight = torch.ones(64, device="cuda")
+    grads = {name: torch.full((64,), math.nan, device="cuda") for name in ("dq_weight", "dq_bias")}
+    s3r.speed3r_rotary_backward(ones, None, ones, None, torch.empty_like(ones), None, cos, sin, axis_pairs=(11,), norm="rms", eps=2.0 ** -40, q_weight=weight, **grads)
+    for name in grads:
+        close_to(name, grads[name][:22], n * heads * cos[0, 0].double(), 28 * u)
+        close_to(name + " of others", grads[name][22:], torch.tensor(float(n * heads), dtype=torch.float64, device="cuda"), 28 * u)
+
+
+def multiples(g, bits, *shape):
+    """Random multiples of 2^-bits in [0, 1)."""
+    return torch.randint(0, 2 ** bits, shape, generator=g, device="cuda") * 2.0 ** -bits
+
+
+@pytest.mark.parametrize("n,width,bits", [(2 ** 14, 64, 19), (2048, 1024, 22), (512, 8192, 24), (2 ** 23, 64, 11), (2 ** 18, 2048, 14)])
+def test_workgroups_are_added_up_in_64_bits(s3r, n, width, bits):
+    """Gradients of a bias whose sums are exact in fp32 within a workgroup (24 bits: 5, 2, 0, 13 and 9 for the rows of one, of which those beyond 256 for a thread
+    are added in 64 bits) and take more bits together: the result is the exact sum, rounded once."""
+    d = multiples(gen(n), bits, n, width)
+    x = torch.ones_like(d)
+    d_bias = torch.full((width,), math.nan, device="cuda")
+    s3r.speed3r_residual_norm_backward(x, d, torch.empty_like(x), norm="rms", d_bias=d_bias)
+    assert torch.equal(d_bias, d.sum(0, dtype=torch.float64).float())
+
+
+@pytest.mark.parametrize("n,heads,bits", [(2 ** 16, 1, 19), (2 ** 16, 16, 14)])
+def test_workgroups_of_rotated_rows_are_added_up_in_64_bits(s3r, n, heads, bits):
+    """As above: 32 rows for a workgroup of 2048, or 512 heads of rows."""
+    d = multiples(gen(n + heads), bits, n, heads, 64)
+    q = torch.ones_like(d)
+    dq_bias = torch.full((64,), math.nan, device="cuda")
+    s3r.speed3r_rotary_backward(q, None, d, None, torch.empty_like(q), None, norm="rms", dq_bias=dq_bias)
+    assert torch.equal(dq_bias, d.sum((0, 1), dtype=torch.float64).float())
