@@ -318,7 +318,7 @@ template <typename T, int WAVES, bool CAUSAL> __global__ __launch_bounds__(64 * 
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
     __syncthreads();
-    store_few<T, WAVES>(few, a.factor, a.to, sh.split, row, head, ok, reinterpret_cast<float *>(smem), wave, lane);
+    store_few<T, WAVES, CAUSAL>(few, a.factor, a.to, sh.split, row, head, ok, reinterpret_cast<float *>(smem), wave, lane);
 }
 
 // One result from the splits' normalised ones: weights 2^(lse_j - lse).  GROUPS x 16 threads for a row of a head: 16 take four
@@ -327,13 +327,13 @@ template <typename T, int WAVES, bool CAUSAL> __global__ __launch_bounds__(64 * 
 // with one group, 4.6 with four; 13 splits of 22 thousand rows 16 with one, 19 with four.
 constexpr int kSplitChunks = kMostSplits / 64;
 constexpr int kJoinAtOnce = 4;  // pieces whose loads are under way together where a thread goes through them
-template <typename T, int GROUPS> __device__ __forceinline__ void soft_combine(const SoftOut &to, int64_t row, int64_t at, int n_split)
+template <typename T, int GROUPS, bool CAUSAL> __device__ __forceinline__ void soft_combine(const SoftOut &to, int64_t row, int64_t at, int n_split)
 {
     const int64_t share = to.rows * to.heads;
     const int c = static_cast<int>(threadIdx.x & 15) * 4, group = static_cast<int>(threadIdx.x >> 4) % GROUPS, lane = threadIdx.x & 63;
     float top = -INFINITY, total = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    auto weight = [&](float l) { return l == -INFINITY ? 0.f : (l == top ? 1.f : fast_exp2(l - top)); };  // -inf: no keys in the piece
+    auto weight = [&](float l) { return l == -INFINITY ? 0.f : (l == top ? 1.f : (CAUSAL ? held_weight(l - top) : fast_exp2(l - top))); };  // -inf: no keys in the piece
     auto add = [&](float l, const floatx4 &o) {
         const float w = weight(l);
         total += w;
@@ -398,12 +398,12 @@ template <typename T, int GROUPS> __device__ __forceinline__ void soft_combine(c
         to.lse[(at - row * to.heads) * to.rows + row] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
 }
 
-template <typename T, int GROUPS> __global__ __launch_bounds__(256) void soft_combine_kernel(SoftOut to, Spans spans, int n_split)
+template <typename T, int GROUPS, bool CAUSAL> __global__ __launch_bounds__(256) void soft_combine_kernel(SoftOut to, Spans spans, int n_split)
 {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, at = i / (16 * GROUPS);
     if (at >= to.rows * to.heads) return;
     const int64_t row = at / to.heads;
-    if (spans.covers(row)) soft_combine<T, GROUPS>(to, row, at, n_split);
+    if (spans.covers(row)) soft_combine<T, GROUPS, CAUSAL>(to, row, at, n_split);
 }
 
 // What causal tiles left in pieces is joined tile by tile: kItems items of a tile of kTile for a workgroup, which is done at once where the
@@ -430,7 +430,7 @@ template <typename T, int GROUPS> __global__ __launch_bounds__(256) void causal_
     if (n == 1) return;
     for (int i = threadIdx.x / (16 * GROUPS); i < kItems; i += 256 / (16 * GROUPS)) {
         const int64_t item = tile0 + t.item0 + i, in_seq = item / a.per_row, row = t.of.of.first + in_seq;
-        if (item < items) soft_combine<T, GROUPS>(a.to, row, row * a.heads + t.of.kv_head * a.per_row + (item - in_seq * a.per_row), n);
+        if (item < items) soft_combine<T, GROUPS, true>(a.to, row, row * a.heads + t.of.kv_head * a.per_row + (item - in_seq * a.per_row), n);
     }
 }
 
@@ -949,7 +949,9 @@ hipError_t launch_grad_kv(const CrossArgs &a, bool is_bf16, hipStream_t stream)
     return is_bf16 ? launch_grad_t<bf16_t>(a, true, stream) : launch_grad_t<float>(a, true, stream);
 }
 
-hipError_t launch_soft_combine(const SoftOut &to, const Spans &spans, int n_split, bool is_bf16, hipStream_t stream)
+template <int GROUPS, bool CAUSAL> auto soft_combine_of(bool is_bf16) { return is_bf16 ? &soft_combine_kernel<bf16_t, GROUPS, CAUSAL> : &soft_combine_kernel<float, GROUPS, CAUSAL>; }
+
+hipError_t launch_soft_combine(const SoftOut &to, const Spans &spans, int n_split, bool causal, bool is_bf16, hipStream_t stream)
 {
     // (us, wide or not: 5 splits of 4800 rows 17.7 / 19.2 with the attention, 4 of 8192 23.5 / 21.6, 10 of 2048 15.7 / 20.0, 6 of 256 9.8 / 12.8,
     // 2 of 16 9.0 / 8.5)
@@ -957,8 +959,8 @@ hipError_t launch_soft_combine(const SoftOut &to, const Spans &spans, int n_spli
     const bool wide = n_split >= 3 && share <= 1024 * (n_split < 8 ? n_split : 8);
     const int64_t blocks = (share * (wide ? 64 : 16) + 255) / 256;
     if (!grid_ok(blocks) || n_split > kMostSplits) return hipErrorInvalidValue;
-    auto kernel = is_bf16 ? (wide ? &soft_combine_kernel<bf16_t, 4> : &soft_combine_kernel<bf16_t, 1>)
-                          : (wide ? &soft_combine_kernel<float, 4> : &soft_combine_kernel<float, 1>);
+    auto kernel = causal ? (wide ? soft_combine_of<4, true>(is_bf16) : soft_combine_of<1, true>(is_bf16))
+                         : (wide ? soft_combine_of<4, false>(is_bf16) : soft_combine_of<1, false>(is_bf16));
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, to, spans, n_split);
     return hipGetLastError();
 }

@@ -303,7 +303,8 @@ struct CrossArgs {
 hipError_t launch_cross(const CrossArgs &a, bool few_rows, bool is_bf16, hipStream_t stream);
 // n_split: at most kMostSplits
 constexpr int kMostSplits = 256;
-hipError_t launch_soft_combine(const SoftOut &to, const Spans &spans, int n_split, bool is_bf16, hipStream_t stream);
+// causal: infinities stay whatever their piece's weight.
+hipError_t launch_soft_combine(const SoftOut &to, const Spans &spans, int n_split, bool causal, bool is_bf16, hipStream_t stream);
 // Of causal rows, many of them (few: the above).
 hipError_t launch_causal_combine(const CrossArgs &a, bool is_bf16, hipStream_t stream);
 // The gradient of queries comes first: it leaves stats [heads][n_q][2], of every row its log-sum in log2 (+inf for a row without keys)

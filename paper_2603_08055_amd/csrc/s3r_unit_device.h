@@ -532,6 +532,14 @@ __device__ __forceinline__ void tame_unit(bf16_t *unit, int t)
     }
 }
 
+// The weight of earlier sums where the maximum has risen, or of a piece: one that underflows is held at 2^-126, so that an infinity in them stays
+// one (0 times it is NaN) and numbers come to 2^-126 of what they were, less than the rounding of any sum that is not as small.
+__device__ __forceinline__ float held_weight(float x)
+{
+    const float w = fast_exp2(x);
+    return w < 1.17549435e-38f ? 1.17549435e-38f : w;  // (not fmaxf: a NaN stays one)
+}
+
 // To a held row's channels (32 dt + acc_row(lane, r)) what is no number in the rows it sees.
 __device__ __forceinline__ void add_wild(floatx16 (&o)[2], const bf16_t *unit, unsigned long long seen, int lane)
 {
@@ -608,7 +616,7 @@ template <int PQ> struct SoftRow {
     // bf16: probabilities enter the product with v rounded to bf16, as in the library's dense attention.  Two parts would leave of the error of
     // out its own rounding alone (2.2e-3 -> 1.66e-3 against 64 bits, 2748 rows over 10992 keys) and take 24 matrix instructions for a unit in place of 16: us,
     // one part / two, 1374 rows over 27480 keys of 16 heads 203 / 297, 8192 over 8192 317 / 469, over cached tokens of 4 bits 402 / 517.
-    // CAUSAL: o may hold infinities before the first score (add_wild).
+    // CAUSAL: o may hold infinities before the first score (add_wild), and they stay whatever the maximum rises to.
     template <int PS, bool CAUSAL = false>
     __device__ __forceinline__ void unit(const bf16_t *k, const bf16_t *v, unsigned long long seen, float factor, const UnitLanes &at, int lane)
     {
@@ -641,7 +649,7 @@ template <int PQ> struct SoftRow {
                 for (int r = 0; r < 16; ++r) most = fmaxf(most, s[half][r]);
             most = max_with_other_half(most);
             const float next = fmaxf(top, most);
-            const float w = (CAUSAL ? top : next) == -INFINITY ? 1.f : fast_exp2((top - next) * factor);
+            const float w = (CAUSAL ? top : next) == -INFINITY ? 1.f : (CAUSAL ? held_weight((top - next) * factor) : fast_exp2((top - next) * factor));
             top = next;
             sum *= w;
 #pragma unroll
@@ -819,7 +827,7 @@ template <int PQ> struct FewRows {
         most = max_over_groups(most);
         if (__any(most > top)) {
             const float next = fmaxf(top, most);
-            const float w = next == -INFINITY ? 1.f : fast_exp2((top - next) * factor);
+            const float w = (CAUSAL ? top : next) == -INFINITY ? 1.f : (CAUSAL ? held_weight((top - next) * factor) : fast_exp2((top - next) * factor));
             top = next;
             sum *= w;
 #pragma unroll
@@ -869,7 +877,7 @@ template <int PQ> struct FewRows {
 // The joint result of WAVES waves that had a share of the keys each, and its store: wave w < 4 takes channels 16 w .. + 15.
 // lds: WAVES * kFewJoin floats.
 constexpr int kFewJoin = 1024 + 32;
-template <typename T, int WAVES, int PQ>
+template <typename T, int WAVES, bool CAUSAL = false, int PQ>
 __device__ __forceinline__ void store_few(const FewRows<PQ> &few, float factor, const SoftOut &to, int split, int64_t row, int head, bool ok,
                                           float *lds, int wave, int lane)
 {
@@ -890,7 +898,7 @@ __device__ __forceinline__ void store_few(const FewRows<PQ> &few, float factor, 
 #pragma unroll
     for (int j = 0; j < WAVES; ++j) {
         const float t = lds[j * kFewJoin + 1024 + q];
-        const float w = t == top ? 1.f : (t == -INFINITY ? 0.f : fast_exp2((t - top) * factor));
+        const float w = t == top ? 1.f : (t == -INFINITY ? 0.f : (CAUSAL ? held_weight((t - top) * factor) : fast_exp2((t - top) * factor)));
         sum += lds[j * kFewJoin + 1040 + q] * w;
 #pragma unroll
         for (int r = 0; r < 4; ++r) o[r] += lds[j * kFewJoin + (wave * 4 + r) * 64 + lane] * w;

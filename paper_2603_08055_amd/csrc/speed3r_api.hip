@@ -1292,7 +1292,7 @@ s3r_status cross_forward(const s3r_cross_params *p, int view)
     StageTimer tm(S3R_STAGE_DENSE, s);
     S3R_HIP(s3r::launch_cross(a, c.few_rows, bf16, s), "cross attention kernel launch");
     if (c.split > 1)
-        S3R_HIP(view > 0 && !c.few_rows ? s3r::launch_causal_combine(a, bf16, s) : s3r::launch_soft_combine(a.to, a.q_spans, c.split, bf16, s),
+        S3R_HIP(view > 0 && !c.few_rows ? s3r::launch_causal_combine(a, bf16, s) : s3r::launch_soft_combine(a.to, a.q_spans, c.split, view > 0, bf16, s),
                 "cross attention combine kernel launch");
     return S3R_OK;
 }
@@ -1571,7 +1571,7 @@ s3r_status speed3r_cache_attn(const s3r_cache_params *p)
     }
     StageTimer tm(S3R_STAGE_DENSE, s);
     S3R_HIP(s3r::launch_cache_attn(a, c.few_rows, bf16, s), "cache attention kernel launch");
-    if (c.split > 1) S3R_HIP(s3r::launch_soft_combine(a.to, a.spans, c.split, bf16, s), "cache attention combine kernel launch");
+    if (c.split > 1) S3R_HIP(s3r::launch_soft_combine(a.to, a.spans, c.split, false, bf16, s), "cache attention combine kernel launch");
     return S3R_OK;
 }
 
