@@ -671,6 +671,16 @@ template <typename T> __global__ __launch_bounds__(256) void causal_grad_q_combi
     }
 }
 
+// Few rows: probabilities and dS rounded to bf16 would be most of the error of dk and dv, whose sums have few terms, and now and then of
+// dq, where a few dS count (2.4e-3 to 2.9e-3, against 1.66e-3 by the rounding of the results themselves, which is what two parts leave).
+// With many rows the errors are 2.35e-3 and 2.3e-3 and no memory hides the products.  Gradient of 16 heads in bf16, us, one part / two: 1 row over 10992
+// keys 55 / 60, 64 over 2000 24.8 / 26.6, 2748 over 10992 588 / 795, 8192 over 8192 1129 / 1554; dk and dv alone: 128 over 10992 71 / 80, 512 over
+// 10992 137 / 163.
+// CAUSAL: of many rows, too, the last keys are seen by few, and so the last tile of a sequence takes its last kFewItems items in two parts (errors of the last 16 keys
+// of 2048 2.9e-3 with one).
+constexpr int kFewItems = kUnitRows;
+template <int N> struct Parts { static constexpr int value = N; };
+
 // PX: bf16 parts in which probabilities and dS enter the products.
 template <typename T, int PX, bool CAUSAL> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void grad_kv_kernel(CrossArgs a)
 {
@@ -696,6 +706,7 @@ template <typename T, int PX, bool CAUSAL> __global__ __launch_bounds__(256, siz
     const int items = q_len * a.per_row, head0 = sh.kv_head * a.per_row;
     float *part_k = a.part_k;
     int u0, u1, from = 0, wave_from = 0;  // causal: the first item that sees the lane's key, and the wave's first
+    int two_from = 0x7fffffff;            // units from here on enter in two parts
     if constexpr (CAUSAL) {
         int begin, end;
         seeing_units(a, sh.tile, q_len, k_len, begin, end);
@@ -706,6 +717,8 @@ template <typename T, int PX, bool CAUSAL> __global__ __launch_bounds__(256, siz
         u1 += begin;
         from = first_seer(key, q_len, k_len, a.view) * a.per_row;
         wave_from = __builtin_amdgcn_readfirstlane(from);
+        const int few = max(0, items - kFewItems);
+        if (PX == 1 && first_seer(min(k_len, (sh.tile + 1) * kTile) - 1, q_len, k_len, a.view) * a.per_row >= few) two_from = few / kUnitRows;
     } else {
         piece((items + kUnitRows - 1) / kUnitRows, a.n_split, a.least, sh.split, u0, u1);
     }
@@ -732,7 +745,8 @@ template <typename T, int PX, bool CAUSAL> __global__ __launch_bounds__(256, siz
     const UnitLanes at(lane);
     units.begin(u0, u1, more);
     const float *stats = row_stats;
-    for (int u = u0; u < u1; ++u) {
+    auto walk = [&](auto parts, int u) {
+        constexpr int kParts = parts.value;
         const bf16_t *q = units.step(u, u == u0, more, [&]() { return low_bits(items - u * kUnitRows); }, [&](int stage) {
             float *to = row_stats + stage * 128;
             if (which < 2) to[which * 64 + lane] = st;
@@ -741,7 +755,7 @@ template <typename T, int PX, bool CAUSAL> __global__ __launch_bounds__(256, siz
         unsigned long long items_seen = ~0ull;
         bool some = false, wild = false;
         if constexpr (CAUSAL) {
-            if ((u + 1) * kUnitRows <= wave_from) continue;
+            if ((u + 1) * kUnitRows <= wave_from) return;
             items_seen = ~low_bits(from - u * kUnitRows);
             some = __any(items_seen != ~0ull);
             wild = some && (unit_is_wild(q, lane) || unit_is_wild(g, lane));
@@ -794,9 +808,9 @@ template <typename T, int PX, bool CAUSAL> __global__ __launch_bounds__(256, siz
                         x[j] = replace(x[j], 0.f, left_out_mask(out, 8 * w + j));
                         y[j] = replace(y[j], 0.f, left_out_mask(out, 8 * w + j));
                     }
-                bf16x8 p[PX], ds[PX];
-                split_parts<PX>(x, p);
-                split_parts<PX>(y, ds);
+                bf16x8 p[kParts], ds[kParts];
+                split_parts<kParts>(x, p);
+                split_parts<kParts>(y, ds);
 #pragma unroll
                 for (int dt = 0; dt < 2; ++dt) {
                     multiply<P>(vv.o[dt], p, [&](int part) { return gt.x[w][dt][part]; });
@@ -809,7 +823,11 @@ template <typename T, int PX, bool CAUSAL> __global__ __launch_bounds__(256, siz
             add_wild(kk.o, q, items_seen, lane);
             add_wild(kk.o, g, items_seen, lane);
         }
-    }
+    };
+    int u = u0;
+    for (const int to = min(u1, two_from); u < to; ++u) walk(Parts<PX>(), u);
+    if constexpr (CAUSAL && PX == 1)
+        for (; u < u1; ++u) walk(Parts<2>(), u);
     if (!seen)  // a masked key gets no gradient, whatever its lanes added up
 #pragma unroll
         for (int r = 0; r < 16; ++r) kk.o[0][r] = kk.o[1][r] = vv.o[0][r] = vv.o[1][r] = 0.f;
@@ -895,12 +913,6 @@ template <typename T> hipError_t launch_cross_t(const CrossArgs &a, bool few_row
     return hipGetLastError();
 }
 
-// Few rows: probabilities and dS rounded to bf16 would be most of the error of dk and dv, whose sums have few terms, and now and then of
-// dq, where a few dS count (2.4e-3 to 2.9e-3, against 1.66e-3 by the rounding of the results themselves, which is what two parts leave).
-// With many rows the errors are 2.35e-3 and 2.3e-3 and no memory hides the products.  Gradient of 16 heads in bf16, us, one part / two: 1 row over 10992
-// keys 55 / 60, 64 over 2000 24.8 / 26.6, 2748 over 10992 588 / 795, 8192 over 8192 1129 / 1554; dk and dv alone: 128 over 10992 71 / 80, 512 over
-// 10992 137 / 163.
-constexpr int kFewItems = kUnitRows;
 template <typename T, int PX> auto grad_kernel(bool of_keys, bool causal)
 {
     return of_keys ? (causal ? &grad_kv_kernel<T, PX, true> : &grad_kv_kernel<T, PX, false>)

@@ -1,4 +1,4 @@
-"""GPU tests of what causal attention makes of rare values and of rows that see few keys, against the plain 64-bit form of tests/decoder_util.py."""
+"""GPU tests of what causal attention makes of rare values and of keys that few rows see, against the plain 64-bit form of tests/decoder_util.py."""
 import math
 
 import pytest
@@ -55,3 +55,72 @@ def test_a_score_that_is_none_is_seen_in_results_and_log_sums(s3r, dtype, n, m, 
     assert torch.isnan(got["out"][sees, 0].float()).all() and torch.isnan(got["lse"][0, sees]).all()
     assert torch.isfinite(got["out"][~sees, 0].float()).all() and torch.isfinite(got["lse"][0, ~sees]).all()
     assert torch.isfinite(got["out"][:, 1].float()).all() and torch.isfinite(got["lse"][1]).all()
+
+
+def attention_of_two_parts(q, k, v, seen, scale, d_out):
+    """As attention() of tests/decoder_util.py, bounds where probabilities and dS of bf16 rows enter their products in two bf16 parts, off by h^2 (h = 2^-8)
+    and not by h.  u = 2^-24.
+      out   (d + h^2 + chain) sum P |v| and h |out| for the store.
+      D     of the stored out is off by up to |d_out| err(out), which is taken out again: of dk by the fp32 sum of dS, (d + chain + 4 u) sum |dS| + sum P err(dP)
+            are left; of dq by that of the parts of dS as they enter, times P k with P in one part: h (|d_out| err(out) + h^2 sum |dS|) sum P |k| as well.
+      dS    P ((d + h^2 + 4 u) |dP - D| + err(D) + err(dP)), through |k| and |q|;  dv: (d + h^2) P^T |d_out|."""
+    u, h = 2.0 ** -24, 2.0 ** -8
+    q, k, v, g = q.double(), k.double(), v.double(), d_out.double()
+    n, m = seen.shape
+    s = ((q @ k.t()) * scale).masked_fill(~seen, -math.inf)
+    size = (q.abs() @ k.abs().t()) * scale
+    lse = torch.logsumexp(s, 1)
+    p = torch.where(seen, torch.exp(s - lse[:, None]), 0.0)
+    d = (64 * u * size + (torch.where(seen, s, 0.0).abs() + 4) * u).masked_fill(~seen, 0.0).amax(1, keepdim=True) * 2
+    chain, pairs = (m / 8 + 64) * u, (max(n, m) / 8 + 64) * u
+    out = p @ v
+    out_tol = (d + h * h + chain) * (p @ v.abs()) + h * out.abs()
+    dp, delta = g @ v.t(), (g * out).sum(1, keepdim=True)
+    dp_err = 64 * u * (g.abs() @ v.abs().t())
+    ds = p * (dp - delta)
+    first = (g.abs() * out_tol).sum(1, keepdim=True) + 64 * u * (g * out).abs().sum(1, keepdim=True)
+    d_err = (d + chain + 4 * u) * ds.abs().sum(1, keepdim=True) + (p * dp_err).sum(1, keepdim=True)
+    err = p * ((d + h * h + 4 * u) * (dp - delta).abs() + d_err + dp_err)
+    r = {"out": out, "out_tol": out_tol}
+    for name, a, b, e in (("dq", ds, k, err + p * h * (first + h * h * ds.abs().sum(1, keepdim=True))), ("dk", ds.t(), q, err.t()), ("dv", p.t(), g, (p * (d + h * h)).t())):
+        f = 1.0 if name == "dv" else scale
+        x = f * (a @ b)
+        r[name], r[name + "_tol"] = x, f * (e @ b.abs() + pairs * (a.abs() @ b.abs())) + h * x.abs()
+    return r
+
+
+@pytest.mark.parametrize("n,m,view,heads,kv_heads", [(700, 700, 1, 2, 2), (300, 300, 1, 4, 1), (130, 700, 1, 6, 2), (129, 129, 1, 3, 3), (500, 520, 20, 3, 1), (2500, 2500, 1, 4, 1),
+                                                     (200, 200, 1, 16, 1), (640, 640, 1, 1, 1), (1000, 9000, 1, 2, 1)])
+def test_last_keys_whose_gradients_have_few_terms(s3r, n, m, view, heads, kv_heads):
+    """bf16 keys that up to 64 rows see, counting those of all heads that share one: their gradients are off by their own rounding and 2^-16 of the terms, as in
+    sequences of so few rows (a term rounded once would be most of the error of such a sum)."""
+    q, k, v, d_out = inputs(n + m + heads, n, m, heads, kv_heads, BF16)
+    got = run(s3r, q, k, v, d_out, view)
+    share, seen = heads // kv_heads, what_rows_see(n, m, view)
+    keys = seen.sum(0) * share <= 64
+    assert keys[-1] and not keys[0]
+    rows = seen[:, keys].any(1)
+    for kh in range(kv_heads):
+        sums = {}
+        for h in range(kh * share, (kh + 1) * share):
+            x = attention_of_two_parts(q[rows, h], k[:, kh], v[:, kh], seen[rows], 0.125, d_out[rows, h])
+            for name in ("dk", "dk_tol", "dv", "dv_tol"):
+                sums[name] = sums.get(name, 0.0) + x[name][keys]
+        for name in ("dk", "dv"):
+            check(name, got[name][keys, kh], sums[name], sums[name + "_tol"])
+
+
+def test_last_keys_of_packed_sequences(s3r):
+    """The same over sequences side by side."""
+    rows, keys = [300, 70, 1, 129, 500], [300, 570, 40, 1000, 500]
+    q, k, v, d_out = inputs(5, sum(rows), sum(keys), 2, 1, BF16)
+    a, b = starts(rows), starts(keys)
+    got = run(s3r, q, k, v, d_out, q_start=a, kv_start=b)
+    q0 = k0 = 0
+    for n, m in zip(rows, keys):
+        seen = what_rows_see(n, m, 1)
+        last = seen.sum(0) * 2 <= 64
+        x = [attention_of_two_parts(q[q0:q0 + n, h], k[k0:k0 + m, 0], v[k0:k0 + m, 0], seen, 0.125, d_out[q0:q0 + n, h]) for h in range(2)]
+        for name in ("dk", "dv"):
+            check(name, got[name][k0:k0 + m, 0][last], (x[0][name] + x[1][name])[last], (x[0][name + "_tol"] + x[1][name + "_tol"])[last])
+        q0, k0 = q0 + n, k0 + m
