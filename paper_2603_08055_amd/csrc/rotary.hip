@@ -109,8 +109,9 @@ template <typename T, Mode MODE> struct Turn {
             }
         }
     }
-    // x cos + (partner) sin.  fp32: with the rounding of the second product made up for (a sum of products that cancel keeps its bits; where
-    // an infinity makes that NaN, the sum as it is).  lds: 512 floats of the wave's own.
+    // x cos + (partner) sin, with the rounding of the second product made up for: a sum of products that cancel keeps its bits, in bf16 as well, where
+    // equal products would else leave their rounding in place of 0 (27480 rows, 16 + 16 heads in bf16 with a norm 36.3 us without, 38.2 so).  Where an infinity
+    // makes that NaN, the sum as it is.  lds: 512 floats of the wave's own.
     __device__ __forceinline__ void apply(const RotaryArgs &a, const float (&x)[8], float (&y)[8], float *lds, int lane) const
     {
         float other[8];
@@ -133,10 +134,8 @@ template <typename T, Mode MODE> struct Turn {
         for (int j = 0; j < 8; ++j) {
             const float p = other[j] * si[j];
             y[j] = fmaf(x[j], co[j], p);
-            if constexpr (sizeof(T) == 4) {
-                const float whole = y[j] + fmaf(other[j], si[j], -p);
-                y[j] = whole == whole ? whole : y[j];
-            }
+            const float whole = y[j] + fmaf(other[j], si[j], -p);
+            y[j] = whole == whole ? whole : y[j];
         }
         if (a.n_pairs < 32)
 #pragma unroll
