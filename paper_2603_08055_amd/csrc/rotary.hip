@@ -110,8 +110,8 @@ template <typename T, Mode MODE> struct Turn {
         }
     }
     // x cos + (partner) sin, with the rounding of the second product made up for: a sum of products that cancel keeps its bits, in bf16 as well, where
-    // equal products would else leave their rounding in place of 0 (27480 rows, 16 + 16 heads in bf16 with a norm 36.3 us without, 38.2 so).  Where an infinity
-    // makes that NaN, the sum as it is.  lds: 512 floats of the wave's own.
+    // equal products would else leave their rounding in place of 0 (27480 rows, 16 + 16 heads in bf16 with a norm, one call after the other, 36.2 us without, 36.9 so).
+    // What is made up for is below 2^104; held to that, it leaves an infinity as it is.  lds: 512 floats of the wave's own.
     __device__ __forceinline__ void apply(const RotaryArgs &a, const float (&x)[8], float (&y)[8], float *lds, int lane) const
     {
         float other[8];
@@ -134,8 +134,7 @@ template <typename T, Mode MODE> struct Turn {
         for (int j = 0; j < 8; ++j) {
             const float p = other[j] * si[j];
             y[j] = fmaf(x[j], co[j], p);
-            const float whole = y[j] + fmaf(other[j], si[j], -p);
-            y[j] = whole == whole ? whole : y[j];
+            y[j] += __builtin_amdgcn_fmed3f(fmaf(other[j], si[j], -p), -0x1p104f, 0x1p104f);  // (the lower bound where it is NaN)
         }
         if (a.n_pairs < 32)
 #pragma unroll
