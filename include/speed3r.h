@@ -262,7 +262,8 @@ s3r_status speed3r_select_attn(const void *q, const void *k, const void *v, cons
  *   bf16 (errors of the results up to about 1.4 times that of rounding them); those of few rows in two bf16 parts (errors of the rounding
  *   alone): in the forward call of up to 64 (keys and values of up to 16 MiB together), 32 (48 MiB) or 16 rows, in the gradient of up to 64,
  *   counting those of all heads that share one, on average over the batch; in the gradient of causal rows the last 64 of a sequence, in what they give
- *   to the last keys.  A sequence's last bits thus depend on the lengths in its batch.
+ *   to the last keys.  A sequence's last bits thus depend on the lengths in its batch.  accurate_pv: two parts for all rows (causal or not; a fifth to a half more
+ *   time where there are many).
  *   fp32 data: products in bf16 parts, each off by up to 2^-21 of its magnitude (operands below 2^-102 keep fewer bits).
  *   Infinities: bf16 v and d_out: one in v reaches out, and one in d_out reaches dv, as an infinity, where its weight is above 2^-100; dq
  *   and dk are then infinities or NaN.  fp32 v and d_out: it may come out as NaN.
@@ -288,6 +289,7 @@ typedef struct s3r_cross_params {
     void *workspace;         /* caller-owned device scratch, 256-byte aligned                            */
     size_t workspace_bytes;  /* >= speed3r_cross_workspace_bytes(...)                                    */
     void *stream;
+    int accurate_pv;         /* nonzero: bf16 probabilities and dS in two parts, however many rows       */
 } s3r_cross_params;
 
 /* Bytes of device scratch that the forward call (backward 0) or the gradient (1) needs; only the shape fields are read.  May be 0;

@@ -191,8 +191,8 @@ template <bool CAUSAL> struct CausalTile {
     }
 };
 
-// Many rows: four waves hold 32 rows each and share every unit.
-template <typename T, bool CAUSAL> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) void cross_kernel(CrossArgs a)
+// Many rows: four waves hold 32 rows each and share every unit.  PP: parts of their probabilities.
+template <typename T, int PP, bool CAUSAL> __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) void cross_kernel(CrossArgs a)
 {
     constexpr int P = UnitPairs<T>::kParts;
     extern __shared__ __align__(16) unsigned char smem[];
@@ -242,7 +242,7 @@ template <typename T, bool CAUSAL> __global__ __launch_bounds__(256, sizeof(T) =
                 tame_unit(k + P * kPlane, threadIdx.x);
                 lds_barrier();
             }
-        if (sight.sees(u)) soft.template unit<P, CAUSAL>(k, k + P * kPlane, sight.of(seen, u), a.factor, at, lane);
+        if (sight.sees(u)) soft.template unit<P, PP, CAUSAL>(k, k + P * kPlane, sight.of(seen, u), a.factor, at, lane);
     }
     store_soft<T>(soft, a.factor, to, sh.split, row, head, ok, lane);
 }
@@ -897,6 +897,8 @@ template <typename T, int WAVES> hipError_t launch_few(const CrossArgs &a, int64
     return hipGetLastError();
 }
 
+template <typename T, int PP> auto cross_kernel_of(bool causal) { return causal ? &cross_kernel<T, PP, true> : &cross_kernel<T, PP, false>; }
+
 template <typename T> hipError_t launch_cross_t(const CrossArgs &a, bool few_rows, hipStream_t stream)
 {
     const int64_t shares = a.tiles * a.n_split * a.kv_heads, n = few_rows ? shares : xcd_padded(shares);
@@ -907,7 +909,9 @@ template <typename T> hipError_t launch_cross_t(const CrossArgs &a, bool few_row
         return launch_few<T, 4>(a, n, stream);
     } else {
         constexpr size_t kLds = UnitPairs<T>::kStages * UnitPairs<T>::kStage * sizeof(bf16_t);
-        auto kernel = a.view > 0 ? &cross_kernel<T, true> : &cross_kernel<T, false>;
+        auto kernel = cross_kernel_of<T, UnitPairs<T>::kParts>(a.view > 0);
+        if constexpr (sizeof(T) == 2)
+            if (a.accurate) kernel = cross_kernel_of<T, 2>(a.view > 0);
         hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(n)), dim3(256), kLds, stream, a);
     }
     return hipGetLastError();
@@ -925,7 +929,7 @@ template <typename T> hipError_t launch_grad_t(const CrossArgs &a, bool of_keys,
     const size_t lds = UnitPairs<T>::kStages * (UnitPairs<T>::kStage * sizeof(bf16_t) + (of_keys ? 128 * sizeof(float) : 0));
     auto kernel = grad_kernel<T, UnitPairs<T>::kParts>(of_keys, a.view > 0);
     if constexpr (sizeof(T) == 2)
-        if (a.n_q * a.per_row <= kFewItems * a.q_spans.batch) kernel = grad_kernel<T, 2>(of_keys, a.view > 0);
+        if (a.accurate || a.n_q * a.per_row <= kFewItems * a.q_spans.batch) kernel = grad_kernel<T, 2>(of_keys, a.view > 0);
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(n)), dim3(256), lds, stream, a);
     return hipGetLastError();
 }

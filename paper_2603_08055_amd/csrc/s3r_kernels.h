@@ -288,6 +288,7 @@ struct CrossArgs {
     int64_t n_q, n_kv, tiles;
     int heads, kv_heads, per_row, n_split, least;
     bool uneven;  // sequences of several lengths, or causal rows
+    bool accurate; // bf16: probabilities and dS in two parts, many rows or few
     int view;     // causal rows: tokens of a view, else 0
     int resident; // causal rows of 2 to 64 sequences that take n_split pieces or fewer by their lengths: workgroups that a CU has at once, else 0
     int join_ns, tile_ns;  // then: joining, and that for each tile's piece

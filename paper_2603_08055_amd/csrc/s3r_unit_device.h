@@ -613,14 +613,15 @@ template <int PQ> struct SoftRow {
     // `top` need not be the largest score so far: it is raised only where a row's exponentials of a unit add up to more than 255, that is
     // where one is above 2^8 times its like at `top`; the scores are then computed again.  That spares almost all units the search.
     // All LDS reads of a product are sent for before its first MFMA.
-    // bf16: probabilities enter the product with v rounded to bf16, as in the library's dense attention.  Two parts would leave of the error of
-    // out its own rounding alone (2.2e-3 -> 1.66e-3 against 64 bits, 2748 rows over 10992 keys) and take 24 matrix instructions for a unit in place of 16: us,
+    // bf16: probabilities enter the product with v rounded to bf16, as in the library's dense attention, unless the caller asks for two parts.  These leave of the error
+    // of out its own rounding alone (2.2e-3 -> 1.66e-3 against 64 bits, 2748 rows over 10992 keys) and take 24 matrix instructions for a unit in place of 16: us,
     // one part / two, 1374 rows over 27480 keys of 16 heads 203 / 297, 8192 over 8192 317 / 469, over cached tokens of 4 bits 402 / 517; causal, 10992 in views of
     // 1374 357 / 507, 8192 by token 186 / 268, 100 prompts of 200 38 / 51, the step of 8192 in three prompts with its gradients (theirs in two parts, too) 366 / 478.
     // The first rows of a prompt, which see few keys, are no worse off (2048 normal rows, those that see 2 to 64 keys 1.76e-3 to 1.86e-3, those that see more
     // 2.0e-3 to 2.2e-3): the largest probability, 1 before it is divided by the sum, is exact.
     // CAUSAL: o may hold infinities before the first score (add_wild), and they stay whatever the maximum rises to.
-    template <int PS, bool CAUSAL = false>
+    // PP: parts of the probabilities.
+    template <int PS, int PP = PQ, bool CAUSAL = false>
     __device__ __forceinline__ void unit(const bf16_t *k, const bf16_t *v, unsigned long long seen, float factor, const UnitLanes &at, int lane)
     {
         const bool all = __all(seen == ~0ull);
@@ -690,8 +691,8 @@ template <int PQ> struct SoftRow {
                 float x[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] = s[half][8 * u + j];
-                bf16x8 p[PQ];
-                split_parts<PQ>(x, p);
+                bf16x8 p[PP];
+                split_parts<PP>(x, p);
 #pragma unroll
                 for (int dt = 0; dt < 2; ++dt) multiply<PS>(o[dt], p, [&](int part) { return a[dt][part]; });
             }

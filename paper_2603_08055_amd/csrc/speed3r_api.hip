@@ -1248,6 +1248,7 @@ s3r_status cross_args(const s3r_cross_params *p, const CrossPlan &c, int view, s
     a.kv_spans = s3r::Spans{p->kv_start, c.batch, p->n_kv};
     a.n_q = p->n_q; a.n_kv = p->n_kv;
     a.heads = p->heads; a.kv_heads = p->kv_heads; a.per_row = c.per_row; a.uneven = c.batch > 1 || view > 0;
+    a.accurate = p->accurate_pv != 0;
     a.view = view;
     a.scale = resolve_scale(p->softmax_scale, 64);
     a.factor = a.scale * 1.4426950408889634f;

@@ -45,7 +45,7 @@ class s3r_cross_params(ctypes.Structure):
                 ("status", _vp), ("n_q", _i64), ("n_kv", _i64), ("q_stride_tok", _i64), ("q_stride_head", _i64),
                 ("kv_stride_tok", _i64), ("kv_stride_head", _i64), ("batch", _int), ("heads", _int),
                 ("kv_heads", _int), ("head_dim", _int), ("dtype", _int), ("softmax_scale", _flt),
-                ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t), ("stream", _vp)]
+                ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t), ("stream", _vp), ("accurate_pv", _int)]
 
 
 class s3r_cache_params(ctypes.Structure):
@@ -461,7 +461,7 @@ def _call(fn, p, need, workspace, index, stream=None, *more):
     return workspace
 
 
-def _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, status, stream, index):
+def _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, accurate_pv, status, stream, index):
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q must be [n_q, heads, head_dim], k and v [n_kv, kv_heads, head_dim]")
     n_q, heads, head_dim = shape = q.shape
@@ -476,7 +476,7 @@ def _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale,
         pq, pk, pv, _arg(out, "out", index, dtype, shape), _arg(lse, "lse", index, torch.float32, (heads, n_q)), None, None, None, None,
         _arg(q_start, "q_start", index, torch.int32, (batch + 1,)), _arg(kv_start, "kv_start", index, torch.int32, (batch + 1,)),
         _arg(key_mask, "key_mask", index, torch.uint8, (n_kv,)), _arg(status, "status", index, torch.int32, (1,)), n_q, n_kv,
-        q_row, q_head, kv_row, kv_head, batch, heads, kv_heads, head_dim, _dtype_code(q), softmax_scale, None, 0, _stream_of(stream, index))
+        q_row, q_head, kv_row, kv_head, batch, heads, kv_heads, head_dim, _dtype_code(q), softmax_scale, None, 0, _stream_of(stream, index), int(bool(accurate_pv)))
 
 
 def speed3r_cross_workspace_bytes(q, k, *, q_start=None, backward=False) -> int:
@@ -495,22 +495,22 @@ def speed3r_cross_workspace_bytes(q, k, *, q_start=None, backward=False) -> int:
 
 
 def speed3r_cross_attn(q, k, v, out, *, lse=None, q_start=None, kv_start=None, key_mask=None, softmax_scale=0.0,
-                       workspace=None, status=None, stream=None):
+                       accurate_pv=False, workspace=None, status=None, stream=None):
     """Attention of q [n_q, heads, 64] over k, v [n_kv, kv_heads, 64] into out (contiguous, like q); lse: fp32 [heads, n_q].
     q_start, kv_start: int32 [batch + 1], the sequences of a ragged batch; key_mask: bool or uint8 [n_kv], 0 leaves a key
-    out; status: int32 [1], receives 0 or S3R_DIAG_SPANS.  q, and k and v alike, may be strided views.  Returns the workspace
-    used (None: none was needed)."""
+    out; accurate_pv: bf16 probabilities enter their product in two parts, not one, also where there are many rows; status: int32 [1], receives 0 or
+    S3R_DIAG_SPANS.  q, and k and v alike, may be strided views.  Returns the workspace used (None: none was needed)."""
     index, lib = _gpu(q, "q"), load()
-    p = _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, status, stream, index)
+    p = _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, accurate_pv, status, stream, index)
     return _call(lib.speed3r_cross_attn, p, lib.speed3r_cross_workspace_bytes(ctypes.byref(p), 0), workspace, index, stream)
 
 
 def speed3r_cross_attn_backward(q, k, v, out, lse, d_out, dq, dk, dv, *, q_start=None, kv_start=None, key_mask=None,
-                                softmax_scale=0.0, workspace=None, status=None, stream=None):
+                                softmax_scale=0.0, accurate_pv=False, workspace=None, status=None, stream=None):
     """Gradients of speed3r_cross_attn into dq, dk, dv (contiguous, like q, k, v), from its out and lse and the gradient
-    d_out of out.  The other arguments are those of the forward call.  Returns the workspace used."""
+    d_out of out.  The other arguments are those of the forward call (accurate_pv: of probabilities and dS here).  Returns the workspace used."""
     index, lib = _gpu(q, "q"), load()
-    p = _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, status, stream, index)
+    p = _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, accurate_pv, status, stream, index)
     p.d_out, p.dq = _arg(d_out, "d_out", index, q.dtype, q.shape), _arg(dq, "dq", index, q.dtype, q.shape)
     p.dk, p.dv = _arg(dk, "dk", index, q.dtype, k.shape), _arg(dv, "dv", index, q.dtype, k.shape)
     return _call(lib.speed3r_cross_attn_backward, p, lib.speed3r_cross_workspace_bytes(ctypes.byref(p), 1), workspace, index, stream)
@@ -537,23 +537,23 @@ def speed3r_causal_workspace_bytes(q, k, *, q_start=None, tokens_per_view=1, bac
 
 
 def speed3r_causal_attn(q, k, v, out, *, tokens_per_view=1, lse=None, q_start=None, kv_start=None, key_mask=None, softmax_scale=0.0,
-                        workspace=None, status=None, stream=None):
+                        accurate_pv=False, workspace=None, status=None, stream=None):
     """speed3r_cross_attn where the rows of a sequence are its last tokens, and each sees the tokens of its own view and of earlier ones
     (tokens_per_view 1: the tokens up to itself).  The other arguments are the same; q_start and kv_start are the same list where rows
     and keys are of the same tokens.  Returns the workspace used (None: none was needed)."""
     index, lib = _gpu(q, "q"), load()
-    p = _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, status, stream, index)
+    p = _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, accurate_pv, status, stream, index)
     view = _view_arg(tokens_per_view)
     need = lib.speed3r_causal_workspace_bytes(ctypes.byref(p), view, 0)
     return _call(lib.speed3r_causal_attn, p, need, workspace, index, stream, view)
 
 
 def speed3r_causal_attn_backward(q, k, v, out, lse, d_out, dq, dk, dv, *, tokens_per_view=1, q_start=None, kv_start=None, key_mask=None,
-                                 softmax_scale=0.0, workspace=None, status=None, stream=None):
+                                 softmax_scale=0.0, accurate_pv=False, workspace=None, status=None, stream=None):
     """Gradients of speed3r_causal_attn into dq, dk, dv (contiguous, like q, k, v), from its out and lse and the gradient
-    d_out of out.  The other arguments are those of the forward call.  Returns the workspace used."""
+    d_out of out.  The other arguments are those of the forward call (accurate_pv: of probabilities and dS here).  Returns the workspace used."""
     index, lib = _gpu(q, "q"), load()
-    p = _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, status, stream, index)
+    p = _cross_params(q, k, v, out, lse, q_start, kv_start, key_mask, softmax_scale, accurate_pv, status, stream, index)
     p.d_out, p.dq = _arg(d_out, "d_out", index, q.dtype, q.shape), _arg(dq, "dq", index, q.dtype, q.shape)
     p.dk, p.dv = _arg(dk, "dk", index, q.dtype, k.shape), _arg(dv, "dv", index, q.dtype, k.shape)
     view = _view_arg(tokens_per_view)

@@ -124,3 +124,39 @@ def test_last_keys_of_packed_sequences(s3r):
         for name in ("dk", "dv"):
             check(name, got[name][k0:k0 + m, 0][last], (x[0][name] + x[1][name])[last], (x[0][name + "_tol"] + x[1][name + "_tol"])[last])
         q0, k0 = q0 + n, k0 + m
+
+
+@pytest.mark.parametrize("n,m,view,heads,kv_heads", [(700, 700, 1, 2, 2), (1500, 1500, 1, 4, 1), (300, 2000, 1, 6, 2), (900, 900, 100, 3, 3), (129, 5000, 1, 2, 2),
+                                                     (500, 300, 0, 2, 1), (1374, 2748, 0, 2, 2)])
+def test_two_parts_where_the_caller_asks_for_them(s3r, n, m, view, heads, kv_heads):
+    """accurate_pv: results of many bf16 rows are off by their own rounding and 2^-16 of the terms, causal (view > 0) and not; without it they need not be (which
+    the bounds of the other tests allow).  Rows in fp32 are as they were."""
+    q, k, v, d_out = inputs(n + m, n, m, heads, kv_heads, BF16)
+    share = heads // kv_heads
+
+    def results(accurate, *t):
+        if view:
+            return run(s3r, *t, view, accurate_pv=accurate)
+        q, k, v, d_out = t
+        r = {"out": torch.empty_like(q), "lse": torch.empty((heads, n), device="cuda"), "dq": torch.empty_like(q), "dk": torch.empty_like(k), "dv": torch.empty_like(v)}
+        s3r.speed3r_cross_attn(q, k, v, r["out"], lse=r["lse"], accurate_pv=accurate)
+        s3r.speed3r_cross_attn_backward(q, k, v, r["out"], r["lse"], d_out, r["dq"], r["dk"], r["dv"], accurate_pv=accurate)
+        return r
+
+    got, plain = results(True, q, k, v, d_out), results(False, q, k, v, d_out)
+    assert torch.equal(got["lse"], plain["lse"]) and not torch.equal(got["out"], plain["out"])
+    seen = what_rows_see(n, m, view) if view else torch.ones((n, m), dtype=torch.bool, device="cuda")
+    for kh in range(kv_heads):
+        sums = {}
+        for h in range(kh * share, (kh + 1) * share):
+            x = attention_of_two_parts(q[:, h], k[:, kh], v[:, kh], seen, 0.125, d_out[:, h])
+            for name in ("out", "dq"):
+                check(name, got[name][:, h], x[name], x[name + "_tol"])
+            for name in ("dk", "dk_tol", "dv", "dv_tol"):
+                sums[name] = sums.get(name, 0.0) + x[name]
+        for name in ("dk", "dv"):
+            check(name, got[name][:, kh], sums[name], sums[name + "_tol"])
+    f32 = [t[:200].float() for t in (q, k, v, d_out)]
+    n = m = 200
+    a, b = results(True, *f32), results(False, *f32)
+    assert all(torch.equal(a[name], b[name]) for name in a)
