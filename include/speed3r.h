@@ -71,12 +71,13 @@ enum { S3R_DIAG_PAGE = 4, S3R_DIAG_SPANS = 8, S3R_DIAG_LENGTH = 16, S3R_DIAG_POS
 
 /* Stages of the path, for speed3r_get_stage_ms(). */
 enum {
-    S3R_STAGE_POOL = 0,     /* block pooling (+ K/V tile re-layout for the MFMA path); cache rows in and out */
+    S3R_STAGE_POOL = 0,     /* block pooling (+ K/V tile re-layout for the MFMA path); cache rows in and out; rotary positions and
+                             * the residual stream's norms, forward and gradient      */
     S3R_STAGE_SPLIT = 1,    /* pooled fp32 -> operand tiles (+ their per-head statistics) */
     S3R_STAGE_COMPRESS = 2, /* S_guide + compressed attention (short sequences: + TopK) */
     S3R_STAGE_TOPK = 3,     /* per-query-block TopK (incl. its filter sweep)          */
     S3R_STAGE_SELECT = 4,   /* block-sparse attention + merge                         */
-    S3R_STAGE_DENSE = 5,    /* dense, cross and cache attention, and the gradient of cross attention */
+    S3R_STAGE_DENSE = 5,    /* dense, cross, causal and cache attention, and the gradients of cross and causal attention */
     S3R_N_STAGES = 6
 };
 
@@ -302,8 +303,10 @@ s3r_status speed3r_cross_attn_backward(const s3r_cross_params *p);
  * sequence, n = m: a prompt over itself, n < m: new tokens over earlier ones): a row sees the tokens of its own view of tokens_per_view
  * tokens and of the views before.  tokens_per_view 1: causal by token, up to the row itself; a view's tokens see one another otherwise, as views that arrive
  * one after another do.  Everything else, p's fields, masks, broken lists, workspaces and arithmetic, is as above.  A row before the first key (n > m)
- * sees none.  What stands in k and v of tokens that a row does not see, or in q and d_out of rows that do not see a key, does not matter to
- * it, infinities and NaN included. */
+ * sees none.  What stands in k and v of tokens that a row does not see, or in q and d_out of rows that do not see a key, takes no part in its
+ * results, infinities and NaN included; their last bits may differ with it, within the errors above (32 rows decide together when to look for a larger
+ * maximum, which is the unit that probabilities are rounded in).  bf16: an infinity in v stays one in the rows that see it, whatever its weight, where some of a
+ * tile's 128 rows (those of all heads that share keys count; of few rows 16) do not see all of its unit of 64 keys; elsewhere as above. */
 size_t speed3r_causal_workspace_bytes(const s3r_cross_params *p, int tokens_per_view, int backward);
 s3r_status speed3r_causal_attn(const s3r_cross_params *p, int tokens_per_view);
 s3r_status speed3r_causal_attn_backward(const s3r_cross_params *p, int tokens_per_view);
@@ -379,7 +382,7 @@ typedef enum { S3R_PAIRS_HALVES = 0, S3R_PAIRS_NEIGHBOURS = 1, S3R_PAIRS_WHOLE =
  *   magnitudes up to 2^56; everything is computed in fp32 and rounded once.
  * Either of q and k may be absent (heads or kv_heads 0); heads need not be a multiple of kv_heads.
  * The gradient takes those of q_out and k_out and, with a norm, q and k again.  The gradients of weights are sums over all rows and heads, in
- * an order that does not depend on that of the workgroups, up to 16 terms in fp32 and the rest in 64 bits.  Without a norm q, k, and weights are not read. */
+ * an order that does not depend on that of the workgroups, up to 16 terms and then four sums in fp32, the rest in 64 bits.  Without a norm q, k, and weights are not read. */
 typedef struct s3r_rotary_params {
     const void *q, *k;            /* in  [n_rows][heads][64], [n_rows][kv_heads][64] (or *_stride_*)     */
     void *q_out, *k_out;          /* out, packed; must not alias inputs                                  */

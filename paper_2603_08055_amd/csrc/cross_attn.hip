@@ -6,9 +6,9 @@
 // goes through partial results in the workspace, which another launch adds up in a fixed order.
 //
 // CAUSAL: the rows of a sequence are its last tokens, and see those of their own view and of earlier ones; units that no row of a tile (of a
-// wave) sees are not walked, and the tiles, which now differ in length, are dealt out the longest first.  What bounds a unit of keys is what bounds it
+// wave) sees are not walked, and the tiles, which now differ in length, are dealt out the longest first (of up to 64 sequences; of more, one sequence after the other).  What bounds a unit of keys is what bounds it
 // without (matrix pipe and vector ALU, which hardly overlap): 10992 rows in views of 1374, 16 heads in bf16, 344 to 367 us, 760 to 810 TFLOP/s of the
-// pairs that count; 8192 rows in three prompts, 16 heads that share 4: 86 us forward, 119 + 165 for the gradients.
+// pairs that count; 8192 rows in three prompts, 16 heads that share 4: 87 us forward, 119 + 144 + 12 (joining) for the gradients.
 #include "s3r_unit_device.h"
 
 namespace s3r {
@@ -128,7 +128,8 @@ template <bool OF_KEYS> __device__ __forceinline__ int tiles_of_units(const Cros
 
 // A workgroup's share of causal work.  The tiles are taken by the number of units they walk, the most first, so that the CUs that are done
 // first take short ones last; of up to 64 sequences, a lane for each: the number of units by bisection, then the tile among those that walk as
-// many.  (More sequences: one after the other, the longest tile of each first.)  8192 rows in three sequences, 16 heads that share 4, sequence by
+// many.  (More sequences: one after the other, the longest tile of each first, and pieces by their mean length: a long one among them that comes early is started late, and
+// in as many pieces as the mean asks for.)  8192 rows in three sequences, 16 heads that share 4, sequence by
 // sequence / so: forward 108 / 90 us, query gradient 157 / 131.
 template <bool OF_KEYS> __device__ __forceinline__ bool find_causal_share(const CrossArgs &a, int n_split, Share &s)
 {
@@ -677,7 +678,8 @@ template <typename T> __global__ __launch_bounds__(256) void causal_grad_q_combi
 // keys 55 / 60, 64 over 2000 24.8 / 26.6, 2748 over 10992 588 / 795, 8192 over 8192 1129 / 1554; dk and dv alone: 128 over 10992 71 / 80, 512 over
 // 10992 137 / 163.
 // CAUSAL: of many rows, too, the last keys are seen by few, and so the last tile of a sequence takes its last kFewItems items in two parts (errors of the last 16 keys
-// of 2048 2.9e-3 with one).
+// of 2048 2.9e-3 with one, 1.7e-3 so; forward and gradients, 17 sequences of 60 rows over 500 keys 66.7 / 68.7 us, 8192 rows in three 364 / 365).
+// All rows in two parts where the caller asks for it: causal, 10992 rows in views of 1374 1136 / 1527, 8192 by token 585 / 788, in three prompts 278 / 351.
 constexpr int kFewItems = kUnitRows;
 template <int N> struct Parts { static constexpr int value = N; };
 

@@ -12,8 +12,8 @@
 // registers for the rows of a workgroup, which follow one another; what the workgroups have is added up by another launch in a
 // fixed order.  256 terms and fewer are added in fp32 by a thread, then those of the workgroup's rows side by side; the rest in 64 bits.
 // Rows of 1024: 137400 with an fp32 stream beside bf16, channel scale and LayerNorm, 337 us, 5.0 TB/s, the rate of a copy of as much (4.97);
-// 41220 all in bf16 60 us, 5.7 TB/s, their gradient 109 us, 4.65 TB/s (six tensors at once), and 6 us for the sums.  3001 rows of 1000 in
-// fp32 with a post-norm and gates: 13 us (3.7 TB/s) and 27 + 7 (2.7 TB/s): four sums over a row, one after the other, and six rows for a workgroup, two at a time.
+// 41220 all in bf16 60 us, 5.6 TB/s, their gradient 109 us, 4.65 TB/s (six tensors at once), and 6 us for the sums.  3001 rows of 1000 in
+// fp32 with a post-norm and gates: 13 us (3.7 TB/s) and 25 + 6 (2.8 TB/s): four sums over a row, one after the other, and six rows for a workgroup, two at a time.
 #include "s3r_lanes_device.h"
 
 #include <type_traits>

@@ -6,9 +6,9 @@
 //
 // Bound by HBM: a row of a head is read and written once.  Eight lanes have a head's 64 channels, a wave eight rows and a run of
 // heads, so that a row's cosines and sines stay in registers for the heads in turn, and the sums over a head are three lane moves.
-// 27480 rows of 16 + 16 heads in bf16, LayerNorm and two axes of 16 pairs: 42 us, 5.4 TB/s of what is read and written (a copy of as much: 5.2 to
-// 5.4); the gradient, which reads q and k again beside the gradients, 73 us, 4.6 TB/s, and 5 us for adding up those of the weights.  3001 rows of
-// 15 + 5 heads in fp32, axes of 10, 11 and 11 pairs: 10.5 us (2.9 TB/s) and 14.4 + 3.8.
+// 27480 rows of 16 + 16 heads in bf16, LayerNorm and two axes of 16 pairs, by rocprofv3 in turn, the inputs changing: 45 us, 5.0 TB/s of what is read and written (a
+// copy of as much: 5.2 to 5.4; one call after the other on the same inputs 37 us by events, part of them from the caches); the gradient, which reads q and k again beside the
+// gradients, 69 us, 4.9 TB/s, and 5 us for adding up those of the weights.  3001 rows of 15 + 5 heads in fp32, axes of 10, 11 and 11 pairs: 10.5 us (2.9 TB/s) and 15.3 + 3.9.
 #include "s3r_lanes_device.h"
 
 namespace s3r {
@@ -16,7 +16,7 @@ namespace s3r {
 namespace {
 
 // Where a channel's partner is: in the same lane (neighbours, axes of multiples of four pairs); at the same place of the lane whose number
-// differs by 2 or 4 (all axes of 16 pairs, or one of 32, or halves of 32 pairs whatever their axes: the angles of a lane's channels then lie apart),
+// differs by 2 or 4 (all axes of 16 pairs, or one of 32, or, paired as halves of the whole, 32 pairs whatever their axes: the angles of a lane's channels then lie apart),
 // or of another of the eight (axes of multiples of eight); or anywhere: then through LDS.
 enum Mode { kInLane, kAcross2, kAcross4, kAcross4Apart, kAcross, kAnywhere };
 constexpr bool angles_apart(Mode mode) { return mode == kAcross4Apart || mode == kAnywhere; }
@@ -370,8 +370,8 @@ Mode mode_of(const RotaryArgs &a)
 }
 
 // Heads that a wave takes in a row: as many as leave the card 2048 waves, up to 4, 8 through a norm's gradient (more to be read for the
-// same angles), twice as many where a lane's angles lie apart, 16 where partners are looked up (whose places take longest to find).  us,
-// 1 / 2 / 4 / 8 / 16 of them: 27480 rows of 16 + 16 heads, norm and rotation 67 / 41 / 36 / 37 / 38, with the gradient 209 / 139 / 118 / 114 / 114; axes of
+// same angles), twice as many where a lane's angles lie apart, 16 where partners are looked up (whose places take longest to find).  us by events, one call after
+// the other, 1 / 2 / 4 / 8 / 16 of them: 27480 rows of 16 + 16 heads, norm and rotation 67 / 41 / 36 / 37 / 38, with the gradient 209 / 139 / 118 / 114 / 114; axes of
 // 10, 11 and 11 pairs 100 / 58 / 40 / 38 / 40, with the gradient 280 / 178 / 134 / 119 / 115, with partners looked up 370 / 229 / 168 / - / 133.
 int run_of_heads(const RotaryArgs &a, Mode mode, bool grad)
 {

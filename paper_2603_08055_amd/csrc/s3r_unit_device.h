@@ -616,7 +616,7 @@ template <int PQ> struct SoftRow {
     // bf16: probabilities enter the product with v rounded to bf16, as in the library's dense attention, unless the caller asks for two parts.  These leave of the error
     // of out its own rounding alone (2.2e-3 -> 1.66e-3 against 64 bits, 2748 rows over 10992 keys) and take 24 matrix instructions for a unit in place of 16: us,
     // one part / two, 1374 rows over 27480 keys of 16 heads 203 / 297, 8192 over 8192 317 / 469, over cached tokens of 4 bits 402 / 517; causal, 10992 in views of
-    // 1374 357 / 507, 8192 by token 186 / 268, 100 prompts of 200 38 / 51, the step of 8192 in three prompts with its gradients (theirs in two parts, too) 366 / 478.
+    // 1374 333 / 472, 8192 by token 168 / 249, 100 prompts of 200, heads that share four, 38 / 47.
     // The first rows of a prompt, which see few keys, are no worse off (2048 normal rows, those that see 2 to 64 keys 1.76e-3 to 1.86e-3, those that see more
     // 2.0e-3 to 2.2e-3): the largest probability, 1 before it is divided by the sum, is exact.
     // CAUSAL: o may hold infinities before the first score (add_wild), and they stay whatever the maximum rises to.
