@@ -557,11 +557,13 @@ template <typename TX, typename T, int L, int W, int CH, bool FULL, bool WIDE> _
                         } else {
                             own.add(sums, gate);
                         }
-                        clear(sums);
                     };
                     if (of_scale || !kWide) add(sc, kPartC, gc);
                     if (of_post_weight || !kWide) add(sa, kPartA, ga);
                     if (of_post_bias || !kWide) add(sb, kPartB, gb);
+                    clear(sa);
+                    clear(sb);
+                    clear(sc);
                     fresh = false;
                 }
             if constexpr (WIDE) {

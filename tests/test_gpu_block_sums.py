@@ -172,3 +172,23 @@ def test_workgroups_of_rotated_rows_are_added_up_in_64_bits(s3r, n, heads, bits)
     dq_bias = torch.full((64,), math.nan, device="cuda")
     s3r.speed3r_rotary_backward(q, None, d, None, torch.empty_like(q), None, norm="rms", dq_bias=dq_bias)
     assert torch.equal(dq_bias, d.sum((0, 1), dtype=torch.float64).float())
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("width,n", [(64, 700), (1024, 60), (4096, 60), (8192, 60), (8192, 1500), (64, 2 ** 17 + 700)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_each_gradient_by_itself(s3r, types, width, n, gated):
+    """A gradient that is asked for alone has the bits that it has beside all others (sequences that share a workgroup; 300 of a row in one, so that a thread's
+    sums go to the workspace in shares, where n is large)."""
+    rows = ([1] * 300 + [n - 310, 4, 0, 6] if n > 1000 else [n // 2, 1, 0, n - n // 2 - 1]) if gated else None
+    c = residual_case(n + width, n, width, *types, post="layer", rows=rows)
+    want = run_residual(s3r, c)
+    how = {name: c[name] for name in ("f", "norm", "weight", "post_norm", "post_weight", "post_bias", "scale", "gate", "row_start")}
+    for name in ("d_weight", "d_bias", "d_post_weight", "d_post_bias", "d_scale", "d_gate"):
+        if name not in want:
+            continue
+        got = torch.full_like(want[name], math.nan)
+        dx, df = torch.empty_like(c["x"]), torch.empty_like(c["f"])
+        s3r.speed3r_residual_norm_backward(c["x"], c["d_y"], dx, d_r=c["d_r"], df=df, eps=1e-6, residual_scale=0.75, **{name: got}, **how)
+        assert torch.equal(got, want[name]), name
+        assert torch.equal(dx, want["dx"]) and torch.equal(df, want["df"]), name
