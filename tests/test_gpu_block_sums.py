@@ -192,3 +192,34 @@ def test_each_gradient_by_itself(s3r, types, width, n, gated):
         s3r.speed3r_residual_norm_backward(c["x"], c["d_y"], dx, d_r=c["d_r"], df=df, eps=1e-6, residual_scale=0.75, **{name: got}, **how)
         assert torch.equal(got, want[name]), name
         assert torch.equal(dx, want["dx"]) and torch.equal(df, want["df"]), name
+
+
+@pytest.mark.parametrize("width,n", [(64, 2 ** 17 + 700), (8192, 1500)])
+def test_shares_replay_from_a_graph(s3r, width, n):
+    """Sums that go to the workspace in shares, replayed with other contents and sequences between eager calls: the bits of an eager call (places of the
+    workspace are written before they are added to)."""
+    c = residual_case(n, n, width, rows=[1] * 300 + [n - 310, 4, 0, 6], post="layer")
+    names = ("d_weight", "d_bias", "d_post_weight", "d_post_bias", "d_scale", "d_gate")
+    want = run_residual(s3r, c)
+    out = {name: torch.zeros_like(want[name]) for name in (*names, "dx", "df")}
+
+    def step():
+        how = {name: c[name] for name in ("f", "norm", "weight", "post_norm", "post_weight", "post_bias", "scale", "gate", "row_start")}
+        s3r.speed3r_residual_norm_backward(c["x"], c["d_y"], out["dx"], d_r=c["d_r"], df=out["df"], eps=1e-6, residual_scale=0.75,
+                                           **{name: out[name] for name in names}, **how)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for turn in range(3):
+        g = gen(turn)
+        for t in (c["x"], c["d_y"], c["gate"]):
+            t.copy_(normal(g, *t.shape, dtype=t.dtype))
+        c["row_start"].copy_(starts([[1] * 300 + [n - 310, 4, 0, 6], [0] * 303 + [n], [2] * 300 + [0, n - 600, 0, 0]][turn]))
+        for t in out.values():
+            t.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = run_residual(s3r, c)
+        assert all(torch.equal(out[name], want[name]) for name in out), turn
